@@ -1,0 +1,307 @@
+// Softmax cross entropy over a large vocabulary (include/dlion_layers.h, dlion_lm_loss).
+//
+// A piece of the rows at a time: one product gives the logits tile by tile, and its epilogue leaves, for
+// each row and group of columns (half a tile), the maximum and the sum of exp(l - maximum), and each logit
+// as a 16-bit distance below that maximum in steps of 2^-10 octaves (relative error of exp at most 3.4e-4, a
+// sixth of the bf16 rounding that d gets anyway; what lies 64 octaves, 5e-20, below its group's maximum counts
+// as 0, so that a word masked by a huge negative weight does not bring that weight into dx).  Once the rows' log-sum-exps are known the codes become d / g in bf16, in place, and two
+// more products give dx and dw.  6 m h v operations instead of the 8 of computing the logits twice; the codes
+// cost 6 bytes of traffic a logit, against the 6 h operations that the products spend on it.
+#include <climits>
+#include <cmath>
+
+#include "product_host.h"
+
+namespace {
+
+using namespace dlion;
+using namespace dlion::prod;
+
+constexpr float kStep = 1024.0f;            // codes per octave
+constexpr int64_t kPiece = 4096;
+constexpr int64_t kMost = int64_t{1} << 30;
+
+struct LossTile {
+    struct Args {
+        int m, n;
+        const int64_t* targets;
+        float2* stats;                      // [group][m]: maximum, sum of exp(l - maximum)
+        float* at_target;                   // [m]
+        uint16_t* codes;                    // nullable: [m][ld]
+        int64_t ld;
+    };
+
+    static __device__ void tile(const Args& p, uint32_t acc, int row0, int col0, int width, int, uint4* stage, int lane) {
+        if (row0 >= p.m || col0 >= p.n) return;
+        const int row = row0 + lane;
+        const int valid = min(width, p.n - col0);
+        const int rows = min(32, p.m - row0);
+        const int64_t target = lane < rows ? p.targets[row] : -1;
+        const int hit = target >= col0 && target < col0 + valid ? static_cast<int>(target - col0) : -1;
+        float top = -INFINITY;
+        for (int c = 0; c < valid; c += 32) {
+            float v[32];
+            tc::tmem_load32(acc + c, v);
+#pragma unroll
+            for (int j = 0; j < 32; ++j) {
+                if (c + j < valid) top = fmaxf(top, v[j]);
+            }
+            if (hit >= c && hit < c + 32) {
+                float l = 0.0f;
+#pragma unroll
+                for (int j = 0; j < 32; ++j) l = hit - c == j ? v[j] : l;
+                p.at_target[row] = l;
+            }
+        }
+        // A group that is masked whole (-infinity, or the type's lowest value) sums to 0, and so that it does, the
+        // difference must be finite; logits above 2e38 make the row NaN.
+        top = top > 2e38f ? NAN : fmaxf(top, -2e38f);
+        float sum = 0.0f;
+        for (int c = 0; c < valid; c += 32) {
+            float v[32];
+            tc::tmem_load32(acc + c, v);
+            uint32_t w[16];
+#pragma unroll
+            for (int j = 0; j < 32; ++j) {
+                const float x = v[j] - top;      // exact where it counts, near the maximum
+                const float e = exp2_fast(x * kLog2e);
+                if (c + j < valid) sum += e;
+                // x <= 0: 1.5 * 2^23 + the distance leaves it, rounded, in the low bits
+                const float d = fminf(__fmaf_rn(x, -kStep * kLog2e, 12582912.0f), 12582912.0f + 65535.0f);
+                const uint32_t u = __float_as_uint(d);
+                w[j / 2] = j % 2 == 0 ? u : __byte_perm(w[j / 2], u, 0x5410);
+            }
+            if (p.codes != nullptr) {
+                const Piece pc{stage, lane, row0, col0 + c, rows, 32};      // ld covers the last tile
+                pc.put16(w, p.codes, p.ld);
+            }
+        }
+        if (lane < rows) p.stats[static_cast<int64_t>(col0 / width) * p.m + row] = make_float2(top, sum);
+    }
+};
+
+__device__ __forceinline__ float block_sum(float v, float* shared) {       // 1024 threads, fixed order
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+    if (threadIdx.x % 32 == 0) shared[threadIdx.x / 32] = v;
+    __syncthreads();
+    v = shared[threadIdx.x % 32];
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+    __syncthreads();
+    return v;
+}
+
+// factor[0] = scale / (rows with a target)
+__global__ void __launch_bounds__(1024) factor_kernel(const int64_t* targets, int64_t m, int64_t ignore, int mean, float scale, float* factor) {
+    __shared__ int counts[32];
+    int n = 0;
+    for (int64_t i = threadIdx.x; i < m; i += 1024) n += targets[i] != ignore;
+    n = __reduce_add_sync(0xffffffffu, n);
+    if (threadIdx.x % 32 == 0) counts[threadIdx.x / 32] = n;
+    __syncthreads();
+    if (threadIdx.x != 0) return;
+    n = 0;
+    for (int i = 0; i < 32; ++i) n += counts[i];
+    factor[0] = mean && n > 0 ? scale / static_cast<float>(n) : scale;
+}
+
+// Joins the groups of 32 rows a block (lane = row, a warp every 32nd group): each row's maximum, the sum's logarithm in
+// octaves, and the loss.
+__global__ void __launch_bounds__(1024) rows_kernel(const float2* stats, int groups, int64_t m, const int64_t* targets, int64_t ignore,
+                                                    int64_t v, const float* at_target, float2* lse, float* rows) {
+    __shared__ float2 part[32][33];
+    const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
+    const int64_t row = static_cast<int64_t>(blockIdx.x) * 32 + lane;
+    float top = -INFINITY, sum = 0.0f;
+    if (row < m) {
+#pragma unroll 4
+        for (int g = warp; g < groups; g += 32) {
+            const float2 s = stats[g * m + row];
+            const float t = fmaxf(top, s.x);
+            sum = sum * exp2_fast((top - t) * kLog2e) + s.y * exp2_fast((s.x - t) * kLog2e);
+            top = t;
+        }
+    }
+    part[warp][lane] = make_float2(top, sum);
+    __syncthreads();
+    if (warp != 0 || row >= m) return;
+    for (int i = 0; i < 32; ++i) top = fmaxf(top, part[i][lane].x);
+    sum = 0.0f;
+    for (int i = 0; i < 32; ++i) {
+        const float2 s = part[i][lane];
+        if (s.x != -INFINITY) sum += s.y * exp2_fast((s.x - top) * kLog2e);     // a warp without a group has none
+    }
+    const float log_sum = logf(sum);
+    const int64_t t = targets[row];
+    float loss = (top - at_target[row]) + log_sum;
+    if (t < 0 || t >= v) loss = NAN;
+    if (t == ignore) loss = 0.0f;
+    rows[row] = loss;
+    lse[row] = make_float2(top, log_sum * kLog2e);
+}
+
+// Codes to softmax - [target] in bf16, in place, eight a thread; a block has 2048 columns of a row.  The factor
+// g is left to the products' epilogues: rounded into d it would shift the whole gradient by its own rounding,
+// since at the target d is close to -g in every row.
+__global__ void __launch_bounds__(256) gradient_kernel(uint16_t* codes, int64_t ld, int n, int width, const float2* stats, int64_t m,
+                                                       const int64_t* targets, int64_t ignore, const float2* lse) {
+    const int64_t row = blockIdx.y + static_cast<int64_t>(blockIdx.z) * 65535;
+    const int col = (blockIdx.x * 256 + threadIdx.x) * 8;
+    if (row >= m || col >= n) return;
+    const int64_t t = targets[row];
+    uint4* p = reinterpret_cast<uint4*>(codes + row * ld + col);
+    if (t == ignore) {
+        *p = make_uint4(0, 0, 0, 0);
+        return;
+    }
+    const float2 l = lse[row];
+    float at = __fmaf_rn(stats[static_cast<int64_t>(col / width) * m + row].x - l.x, kLog2e, -l.y);
+    if (t < 0 || t >= n) at = NAN;
+    const bool none = at == at;             // the last code stands for 0, unless the row is NaN
+    const uint4 u = *p;
+    const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+    uint32_t o[4];
+    const int hit = static_cast<int>(t - col);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const uint32_t ca = w[i] & 0xffffu, cb = w[i] >> 16;
+        float a = ca == 65535u && none ? 0.0f : exp2_fast(__fmaf_rn(static_cast<float>(ca), -1.0f / kStep, at));
+        float b = cb == 65535u && none ? 0.0f : exp2_fast(__fmaf_rn(static_cast<float>(cb), -1.0f / kStep, at));
+        if (hit == 2 * i) a -= 1.0f;
+        if (hit == 2 * i + 1) b -= 1.0f;
+        o[i] = pack_bf16(a, b);
+    }
+    *p = make_uint4(o[0], o[1], o[2], o[3]);
+}
+
+// The rows' losses to the loss, in a fixed order.
+__global__ void __launch_bounds__(1024) loss_kernel(const float* rows, const int64_t* targets, int64_t m, int64_t ignore, int mean, float* loss) {
+    __shared__ float shared[32];
+    float v = 0.0f, n = 0.0f;               // a thread counts at most 2^20 rows: exact
+    for (int64_t i = threadIdx.x; i < m; i += 1024) {
+        v += rows[i];
+        n += targets[i] != ignore ? 1.0f : 0.0f;
+    }
+    v = block_sum(v, shared);
+    n = block_sum(n, shared);
+    if (threadIdx.x == 0) loss[0] = mean && n > 0.0f ? v / n : v;
+}
+
+dlion_status check_loss(const dlion_loss* p) {
+    if (p == nullptr || p->m < 0 || p->m > kMost || p->h < 1 || p->h > kMost || p->v < 1 || p->v > kMost) return DLION_EINVAL;
+    if (p->x_rs < 0 || p->x_cs < 0 || p->w_rs < 0 || p->w_cs < 0 || p->piece < 0) return DLION_EINVAL;
+    if (p->mean != 0 && p->mean != 1) return DLION_EINVAL;
+    if (!std::isfinite(p->scale)) return DLION_EINVAL;
+    if (p->loss == nullptr || (p->m != 0 && (p->dx == nullptr) != (p->dw == nullptr))) return DLION_EINVAL;
+    if (!aligned(p->loss, 4) || !aligned(p->rows, 4)) return DLION_EALIGN;
+    if (p->dw != nullptr) {
+        if (p->grad_type != DLION_GRAD_F32 && p->grad_type != DLION_GRAD_BF16) return DLION_EINVAL;
+        if ((p->m > 1 && p->dx_ld < p->h) || (p->v > 1 && p->dw_ld < p->h)) return DLION_EINVAL;
+        if (!aligned(p->dx, 2) || !aligned(p->dw, p->grad_type == DLION_GRAD_F32 ? 4 : 2)) return DLION_EALIGN;
+    }
+    if (p->m == 0) return DLION_OK;
+    if (p->x == nullptr || p->w == nullptr || p->targets == nullptr || p->rows == nullptr) return DLION_EINVAL;
+    return aligned(p->x, 2) && aligned(p->w, 2) && aligned(p->targets, 8) ? DLION_OK : DLION_EALIGN;
+}
+
+void loss(Call& c, const dlion_loss& p) {
+    const bool grads = p.dw != nullptr, f32 = p.grad_type == DLION_GRAD_F32;
+    if (p.m == 0) {
+        if (!c.live()) return;
+        c.check(cudaMemsetAsync(p.loss, 0, sizeof(float), c.stream));
+        if (grads) c.check(cudaMemset2DAsync(p.dw, std::max(p.dw_ld, p.h) * (f32 ? 4 : 2), 0, p.h * (f32 ? 4 : 2), p.v, c.stream));
+        return;
+    }
+    const Matrix x = readable(c, Matrix{p.x, p.m, p.h, p.x_rs, p.x_cs});
+    const Matrix w = readable(c, Matrix{p.w, p.v, p.h, p.w_rs, p.w_cs});
+    const int64_t piece = std::min(p.m, p.piece == 0 ? kPiece : p.piece);
+    const int64_t ld = round_up(p.v, 256);
+    // without gradients nothing is kept of a piece, and all rows are one
+    const int64_t step = grads ? piece : p.m;
+    const Config cfg = choose(c, step, p.v, p.h, false);
+    const int width = cfg.bn / 2;
+    const int64_t groups = parts(p.v, width);
+    float2* stats = c.ws.take<float2>(static_cast<uint64_t>(groups) * step);
+    float* at_target = c.ws.take<float>(step);
+    float2* lse = c.ws.take<float2>(step);
+    float* factor = c.ws.take<float>(1);
+    uint16_t* codes = grads ? c.ws.take<uint16_t>(static_cast<uint64_t>(step) * ld) : nullptr;
+    float* sums = grads && !f32 && step < p.m ? c.ws.take<float>(static_cast<uint64_t>(p.v) * p.h) : nullptr;
+    if (grads && c.live()) {
+        factor_kernel<<<1, 1024, 0, c.stream>>>(p.targets, p.m, p.ignore_index, p.mean, p.scale, factor);
+        c.check(cudaGetLastError());
+    }
+    for (int64_t r = 0; r < p.m; r += step) {
+        const int64_t rows = std::min(step, p.m - r);
+        Matrix xp = x;
+        xp.p = static_cast<const uint16_t*>(x.p) + r * x.rs;
+        xp.rows = rows;
+        if (c.live()) {
+            Shape s{};
+            CUtensorMap ma, mb;
+            if (!shape_of(cfg, xp, w, &s)) {
+                c.status = DLION_EINVAL;
+                return;
+            }
+            if (!make_map(&ma, xp, &s.a_mn, 128) || !make_map(&mb, w, &s.b_mn, 128)) {
+                c.status = DLION_ECUDA;
+                return;
+            }
+            const LossTile::Args args{static_cast<int>(rows), static_cast<int>(p.v), p.targets + r, stats, at_target, codes, ld};
+            if (cfg.cg == 2) {
+                launch<2, 256, LossTile>(c, ma, mb, s, args);
+            } else {
+                launch<1, 128, LossTile>(c, ma, mb, s, args);
+            }
+            if (c.status != DLION_OK) return;
+            rows_kernel<<<static_cast<unsigned>(parts(rows, 32)), 1024, 0, c.stream>>>(
+                stats, static_cast<int>(groups), rows, p.targets + r, p.ignore_index, p.v, at_target, lse, p.rows + r);
+            c.check(cudaGetLastError());
+            if (grads) {
+                const dim3 grid(static_cast<unsigned>(parts(p.v, 2048)), static_cast<unsigned>(std::min<int64_t>(rows, 65535)),
+                                static_cast<unsigned>(parts(rows, 65535)));
+                gradient_kernel<<<grid, 256, 0, c.stream>>>(codes, ld, static_cast<int>(p.v), width, stats, rows, p.targets + r,
+                                                            p.ignore_index, lse);
+                c.check(cudaGetLastError());
+            }
+        }
+        if (!grads) continue;
+        const Matrix d{codes, rows, p.v, ld, 1};
+        Finish fx{};
+        fx.scale = factor;
+        fx.out = static_cast<uint16_t*>(p.dx) + r * p.dx_ld;
+        fx.out_ld = p.dx_ld;
+        product(c, d, transposed(w), fx);
+        Finish fw{};
+        fw.scale = factor;
+        const bool last = r + rows >= p.m;
+        float* so_far = f32 ? static_cast<float*>(p.dw) : sums;
+        const int64_t so_far_ld = f32 ? p.dw_ld : p.h;
+        if (r != 0) {
+            fw.accumulated = so_far;
+            fw.accumulated_ld = so_far_ld;
+        }
+        fw.out = last ? p.dw : so_far;
+        fw.out_ld = last ? p.dw_ld : so_far_ld;
+        fw.out_f32 = f32 || !last;
+        product(c, transposed(d), transposed(xp), fw);
+    }
+    if (c.live()) {
+        loss_kernel<<<1, 1024, 0, c.stream>>>(p.rows, p.targets, p.m, p.ignore_index, p.mean, p.loss);
+        c.check(cudaGetLastError());
+    }
+}
+
+}  // namespace
+
+extern "C" {
+
+uint64_t dlion_lm_loss_workspace(const dlion_loss* p) { return check_loss(p) == DLION_OK ? workspace_of(*p, loss) : 0; }
+
+dlion_status dlion_lm_loss(const dlion_loss* p, void* workspace, uint64_t workspace_bytes, void* cuda_stream) {
+    const dlion_status st = check_loss(p);
+    return st != DLION_OK ? st : run(*p, loss, workspace, workspace_bytes, cuda_stream);
+}
+
+}  // extern "C"

@@ -1,0 +1,248 @@
+// Launches of the layer products, the sum of split products, and the packing of operands that tiled
+// copies cannot read in place.
+#include "product_host.h"
+
+#include <algorithm>
+
+namespace dlion {
+namespace prod {
+
+__device__ unsigned int wait_ran_out = 0;
+
+namespace {
+
+using EncodeTiled = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
+                                 const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
+                                 CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+EncodeTiled encoder() {
+    static const EncodeTiled fn = [] {
+        void* p = nullptr;
+        cudaDriverEntryPointQueryResult r;
+        if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &p, 12000, cudaEnableDefault, &r) != cudaSuccess ||
+            r != cudaDriverEntryPointSuccess) {
+            p = nullptr;
+        }
+        return reinterpret_cast<EncodeTiled>(p);
+    }();
+    return fn;
+}
+
+// One element a thread: a warp has 32 columns of a row, so that the 8-bit form's blocks are warps.
+__global__ void __launch_bounds__(256) sum_splits_kernel(const Finish f, int splits) {
+    const int lane = threadIdx.x % 32;
+    const int64_t per_row = (f.n + 31) / 32;
+    const int64_t at = static_cast<int64_t>(blockIdx.x) * 8 + threadIdx.x / 32;
+    const int64_t row = at / per_row;
+    if (row >= f.m) return;
+    const int64_t col = (at - row * per_row) * 32 + lane;
+    const bool in = col < f.n;
+    const float* p = f.partial + row * f.partial_ld + col;     // padded columns exist
+    const int64_t step = f.partial_rows * f.partial_ld;
+    float v = 0.0f;
+    int i = 0;
+    for (; i + 4 <= splits; i += 4) {
+        const float a = p[i * step], b = p[(i + 1) * step], c = p[(i + 2) * step], d = p[(i + 3) * step];
+        v = (((v + a) + b) + c) + d;
+    }
+    for (; i < splits; ++i) v += p[i * step];
+    if (f.scale != nullptr) v *= *f.scale;
+    if (f.bias != nullptr && in) {
+        v += f.bias_f32 ? static_cast<const float*>(f.bias)[col] : __bfloat162float(static_cast<const __nv_bfloat16*>(f.bias)[col]);
+    }
+    if (f.keep == DLION_KEEP_8BIT) {
+        uint32_t top = in ? __float_as_uint(v) & 0x7fffffffu : 0u;
+        top = __reduce_max_sync(0xffffffffu, top);
+        const uint32_t e = block_exponent(top);
+        if (lane == 0) f.kept_e[(col / 32) * f.kept_e_ld + row] = static_cast<uint8_t>(e);
+        if (in) static_cast<int8_t*>(f.kept)[row * f.kept_ld + col] = static_cast<int8_t>(quantise8(v, block_inverse(e)));
+    } else if (f.keep == DLION_KEEP_BF16 && in) {
+        static_cast<__nv_bfloat16*>(f.kept)[row * f.kept_ld + col] = __float2bfloat16_rn(v);
+    }
+    if (!in) return;
+    v = act_value(f.act, v);
+    if (f.slope != DLION_ACT_NONE) {
+        float u;
+        if (f.saved8) {
+            u = static_cast<float>(static_cast<const int8_t*>(f.saved)[row * f.saved_ld + col]) *
+                block_scale(f.saved_e[(col / 32) * f.saved_e_ld + row]);
+        } else {
+            u = __bfloat162float(static_cast<const __nv_bfloat16*>(f.saved)[row * f.saved_ld + col]);
+        }
+        v *= act_slope(f.slope, u);
+    }
+    if (f.residual != nullptr) v += __bfloat162float(f.residual[row * f.residual_ld + col]);
+    if (f.accumulated != nullptr) v += f.accumulated[row * f.accumulated_ld + col];
+    if (f.out_f32) {
+        static_cast<float*>(f.out)[row * f.out_ld + col] = v;
+    } else {
+        static_cast<__nv_bfloat16*>(f.out)[row * f.out_ld + col] = __float2bfloat16_rn(v);
+    }
+}
+
+// out[r][c] = a[r * rs + c * cs], rows of ld elements; reads run along whichever stride is smaller.
+__global__ void __launch_bounds__(256) pack_kernel(const uint16_t* a, int64_t rs, int64_t cs, int64_t rows, int64_t cols,
+                                                   uint16_t* out, int64_t ld) {
+    __shared__ uint16_t t[32][34];
+    const int x = threadIdx.x % 32, y = threadIdx.x / 32;
+    const int64_t across = (cols + 31) / 32;
+    const int64_t r0 = blockIdx.x / across * 32, c0 = blockIdx.x % across * 32;
+    const bool along_rows = rs < cs;
+    for (int i = y; i < 32; i += 8) {
+        const int64_t r = r0 + (along_rows ? x : i), c = c0 + (along_rows ? i : x);
+        if (r < rows && c < cols) t[along_rows ? x : i][along_rows ? i : x] = a[r * rs + c * cs];
+    }
+    __syncthreads();
+    for (int i = y; i < 32; i += 8) {
+        if (r0 + i < rows && c0 + x < cols) out[(r0 + i) * ld + c0 + x] = t[i][x];
+    }
+}
+
+}  // namespace
+
+// Estimated time of a division of the work, in clocks of an SM: rounds of tiles, each of so many slices
+// and an epilogue that the next tile hides, the sum of the splits at the L2's rate.
+Config choose(const Call& c, int64_t m, int64_t n, int64_t k, bool may_split) {
+    const int64_t slices = std::max<int64_t>(1, parts(k, kSlice));
+    Config best{2, 256, 1, static_cast<int>(slices)};
+    double least = 1e300;
+    for (int pair = 1; pair >= 0; --pair) {
+        const int64_t tm = parts(m, pair ? 256 : 128), tn = parts(n, pair ? 256 : 128), tiles = tm * tn;
+        const int64_t workers = pair ? c.sms / 2 : c.sms;
+        const double slice = pair ? 540.0 : 400.0, fixed = pair ? 2600.0 : 2000.0;
+        const int64_t most = may_split ? std::min<int64_t>(64, std::max<int64_t>(1, slices / 4)) : 1;
+        for (int64_t s = 1; s <= most; ++s) {
+            const int64_t per = parts(slices, s);
+            const int64_t used = parts(slices, per);
+            if (used != s) continue;
+            double t = static_cast<double>(parts(tiles * s, workers)) * (per * slice + 600.0) + fixed;
+            if (s > 1) t += 4000.0 + static_cast<double>(s) * tm * tn * (pair ? 65536 : 16384) * 8.0 / 3000.0;
+            if (t < least) {
+                least = t;
+                best = Config{pair ? 2 : 1, pair ? 256 : 128, static_cast<int>(s), static_cast<int>(per)};
+            }
+        }
+    }
+    return best;
+}
+
+dlion_status begin(Call& c, void* workspace, uint64_t bytes, void* stream) {
+    c.ws.base = static_cast<uint8_t*>(workspace);
+    c.ws.size = bytes;
+    c.ws.dry = false;
+    c.stream = static_cast<cudaStream_t>(stream);
+    if (cudaGetDevice(&c.device) != cudaSuccess) return DLION_ECUDA;
+    if (cudaDeviceGetAttribute(&c.sms, cudaDevAttrMultiProcessorCount, c.device) != cudaSuccess) return DLION_ECUDA;
+    void* mark = nullptr;
+    if (cudaGetSymbolAddress(&mark, wait_ran_out) != cudaSuccess || encoder() == nullptr) return DLION_ECUDA;
+    c.mark = static_cast<unsigned int*>(mark);
+    return DLION_OK;
+}
+
+static bool rows_in_place(const void* p, int64_t rows, int64_t cols, int64_t rs, int64_t cs) {
+    if (cs != 1 && cols != 1) return false;
+    if (!aligned16(p)) return false;
+    return rows == 1 || (rs % 8 == 0 && rs >= cols);
+}
+
+Matrix readable(Call& c, const Matrix& a) {
+    Matrix r = a;
+    if (rows_in_place(a.p, a.rows, a.cols, a.rs, a.cs)) {
+        r.cs = 1;
+        if (a.rows == 1) r.rs = round_up(a.cols, 8);
+        return r;
+    }
+    if (rows_in_place(a.p, a.cols, a.rows, a.cs, a.rs)) {
+        r.rs = 1;
+        if (a.cols == 1) r.cs = round_up(a.rows, 8);
+        return r;
+    }
+    r.rs = round_up(a.cols, 8);
+    r.cs = 1;
+    uint16_t* out = c.ws.take<uint16_t>(static_cast<uint64_t>(a.rows) * r.rs);
+    r.p = out;
+    if (c.live()) {
+        const int64_t blocks = parts(a.rows, 32) * parts(a.cols, 32);
+        pack_kernel<<<static_cast<unsigned>(blocks), 256, 0, c.stream>>>(static_cast<const uint16_t*>(a.p), a.rs, a.cs, a.rows, a.cols,
+                                                                         out, r.rs);
+        c.check(cudaGetLastError());
+    }
+    return r;
+}
+
+bool make_map(CUtensorMap* map, const Matrix& a, int* mn_major, int box_rows) {
+    const bool mn = a.cs != 1;                 // adjacent rows
+    *mn_major = mn ? 1 : 0;
+    const cuuint64_t dims[2] = {static_cast<cuuint64_t>(mn ? a.rows : a.cols), static_cast<cuuint64_t>(mn ? a.cols : a.rows)};
+    const cuuint64_t strides[1] = {static_cast<cuuint64_t>(mn ? a.cs : a.rs) * 2};
+    const cuuint32_t box[2] = {64, static_cast<cuuint32_t>(mn ? kSlice : box_rows)};
+    const cuuint32_t one[2] = {1, 1};
+    return encoder()(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(a.p), dims, strides, box, one,
+                     CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                     CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+bool shape_of(const Config& cfg, const Matrix& a, const Matrix& b, Shape* s) {
+    s->m = static_cast<int>(a.rows);
+    s->n = static_cast<int>(b.rows);
+    s->k = static_cast<int>(a.cols);
+    s->tiles_m = static_cast<int>(parts(a.rows, 128 * cfg.cg));
+    s->tiles_n = static_cast<int>(parts(b.rows, cfg.bn));
+    s->slices = static_cast<int>(parts(a.cols, kSlice));
+    s->splits = cfg.splits;
+    s->split_slices = cfg.split_slices;
+    return static_cast<int64_t>(s->tiles_m) * s->tiles_n * s->splits < (int64_t{1} << 30);
+}
+
+void product(Call& c, const Matrix& a, const Matrix& b, Finish f) {
+    f.m = static_cast<int>(a.rows);
+    f.n = static_cast<int>(b.rows);
+    const Config cfg = choose(c, a.rows, b.rows, a.cols, true);
+    Shape s{};
+    if (!shape_of(cfg, a, b, &s)) {
+        c.status = DLION_EINVAL;
+        return;
+    }
+    const uint64_t mark = c.ws.used;
+    if (cfg.splits > 1) {
+        f.partial_ld = static_cast<int64_t>(s.tiles_n) * cfg.bn;
+        f.partial_rows = static_cast<int64_t>(s.tiles_m) * 128 * cfg.cg;
+        f.partial = c.ws.take<float>(static_cast<uint64_t>(cfg.splits) * f.partial_ld * f.partial_rows);
+    }
+    if (c.live()) {
+        CUtensorMap ma, mb;
+        const bool ok = make_map(&ma, a, &s.a_mn, 128) && make_map(&mb, b, &s.b_mn, 128);
+        if (!ok) {
+            c.status = DLION_ECUDA;
+            return;
+        }
+        if (cfg.cg == 2) {
+            launch<2, 256, General>(c, ma, mb, s, f);
+        } else {
+            launch<1, 128, General>(c, ma, mb, s, f);
+        }
+        if (cfg.splits > 1 && c.status == DLION_OK) {
+            const int64_t warps = static_cast<int64_t>(f.m) * parts(f.n, 32);
+            sum_splits_kernel<<<static_cast<unsigned>(parts(warps, 8)), 256, 0, c.stream>>>(f, cfg.splits);
+            c.check(cudaGetLastError());
+        }
+    }
+    if (c.ws.dry) {
+        // later products of the call reuse the split sums' place (the stream orders them): the size query keeps the maximum
+        c.ws.size = std::max(c.ws.size, c.ws.used);
+    }
+    c.ws.used = mark;
+}
+
+}  // namespace prod
+}  // namespace dlion
+
+extern "C" dlion_status dlion_layers_check(void* cuda_stream) {
+    if (cudaStreamSynchronize(static_cast<cudaStream_t>(cuda_stream)) != cudaSuccess) return DLION_ECUDA;
+    unsigned int mark = 0;
+    if (cudaMemcpyFromSymbol(&mark, dlion::prod::wait_ran_out, sizeof mark) != cudaSuccess) return DLION_ECUDA;
+    if (mark == 0) return DLION_OK;
+    mark = 0;
+    if (cudaMemcpyToSymbol(dlion::prod::wait_ran_out, &mark, sizeof mark) != cudaSuccess) return DLION_ECUDA;
+    return DLION_ESTATE;
+}

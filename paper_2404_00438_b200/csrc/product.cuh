@@ -1,0 +1,478 @@
+// D[m][n] = sum_k A[m][k] B[n][k] on the fifth-generation tensor cores, with the epilogue as a
+// template parameter.  One persistent block (or pair of blocks, CG = 2) per SM:
+//   warp 0      copies 64-wide slices of A and B into a ring of shared-memory stages,
+//   warp 1      issues the matrix instructions; accumulators are two sets of BN columns of tensor memory,
+//   warps 4-11  take the finished set out while the next one fills (rows 32 (w % 4).., half the columns each).
+// A pair computes 256 x 256 with each block holding half of A and half of B, so a block reads 32 KB of
+// shared memory for 128 x 256 x 64 products, where a single block's 128 x 128 tile reads the same 32 KB for
+// half of that: the pair is what large shapes use, the single block what small ones use.
+#pragma once
+
+#include "layers_math.cuh"
+#include "tensor_core.cuh"
+
+namespace dlion {
+namespace prod {
+
+constexpr int kSlice = 64;                 // values of k per stage: one 128-byte swizzled row
+constexpr int kStages = 6;
+constexpr int kStageBytes = 32768;         // A: 128 rows, B: 128 rows (of each block)
+constexpr int kThreads = 384;
+constexpr int kEpilogueWarps = 8;
+constexpr int kStaging = 4096;             // bytes of shared memory per epilogue warp
+constexpr int kSmem = kStages * kStageBytes + kEpilogueWarps * kStaging + 1024 + 256;
+
+struct Shape {
+    int m, n, k;
+    int a_mn, b_mn;                        // operand majors (1: adjacent values along m / n)
+    int tiles_m, tiles_n;
+    int splits, split_slices, slices;      // slices of k in all, and per split
+};
+
+// What happens to a sum; every part is optional.  Order: * scale, + bias, keep z, act, * act'(saved), + residual,
+// + accumulated, store.
+struct Finish {
+    int m, n;
+    const float* scale;                    // on the device
+    const void* bias;
+    int bias_f32;
+    int act;
+    int keep;
+    void* kept;
+    int64_t kept_ld;
+    uint8_t* kept_e;
+    int64_t kept_e_ld;
+    int slope;                             // activation whose slope at `saved` multiplies
+    int saved8;
+    const void* saved;
+    int64_t saved_ld;
+    const uint8_t* saved_e;
+    int64_t saved_e_ld;
+    const __nv_bfloat16* residual;
+    int64_t residual_ld;
+    const float* accumulated;
+    int64_t accumulated_ld;
+    void* out;
+    int64_t out_ld;
+    int out_f32;
+    float* partial;                        // split sums: [split][rows padded][cols padded], nothing else applies
+    int64_t partial_ld, partial_rows;
+};
+
+__device__ __forceinline__ bool on_grid(const void* p, int64_t ld, int bytes) {
+    return ((reinterpret_cast<uintptr_t>(p) | static_cast<uintptr_t>(ld * bytes)) & 15u) == 0;
+}
+
+// A warp's 32 x 32 piece of a row-major array goes through its staging memory, so that global accesses
+// run along rows (64 or 128 bytes a row) while each thread owns one row.  16-byte units are exchanged
+// within a row so that neither direction meets bank conflicts.
+struct Piece {
+    uint4* stage;
+    int lane;
+    int row0, col0;                        // first row and column of the piece
+    int rows, cols;                        // valid ones, 1..32
+
+    __device__ __forceinline__ int unit2(int r, int c) const { return r * 4 + (c ^ ((r >> 1) & 3)); }
+    __device__ __forceinline__ int unit4(int r, int c) const { return r * 8 + (c ^ (r & 7)); }
+
+    __device__ __forceinline__ void fetch16(const void* base, int64_t ld) const {
+        const __nv_bfloat16* p = static_cast<const __nv_bfloat16*>(base) + static_cast<int64_t>(row0) * ld + col0;
+        __syncwarp();
+        if (cols == 32 && on_grid(base, ld, 2)) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int r = lane / 4 + 8 * i, c = lane % 4;
+                if (r < rows) stage[unit2(r, c)] = *reinterpret_cast<const uint4*>(p + r * ld + c * 8);
+            }
+        } else {
+            __nv_bfloat16* s = reinterpret_cast<__nv_bfloat16*>(stage);
+            if (lane < cols) {
+                for (int r = 0; r < rows; ++r) s[unit2(r, lane / 8) * 8 + lane % 8] = p[r * ld + lane];
+            }
+        }
+        __syncwarp();
+    }
+
+    // f(j, value) for the 32 columns of this thread's row (columns beyond `cols` hold leftovers)
+    template <class F>
+    __device__ __forceinline__ void each16(F f) const {
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+            const uint4 u = stage[unit2(lane, c)];
+            const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                f(c * 8 + 2 * i, bf16_lo(w[i]));
+                f(c * 8 + 2 * i + 1, bf16_hi(w[i]));
+            }
+        }
+    }
+
+    __device__ __forceinline__ void put16(const uint32_t (&w)[16], void* base, int64_t ld) const {
+        __syncwarp();
+#pragma unroll
+        for (int c = 0; c < 4; ++c) stage[unit2(lane, c)] = make_uint4(w[4 * c], w[4 * c + 1], w[4 * c + 2], w[4 * c + 3]);
+        __syncwarp();
+        uint16_t* p = static_cast<uint16_t*>(base) + static_cast<int64_t>(row0) * ld + col0;
+        if (cols == 32 && on_grid(base, ld, 2)) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int r = lane / 4 + 8 * i, c = lane % 4;
+                if (r < rows) *reinterpret_cast<uint4*>(p + r * ld + c * 8) = stage[unit2(r, c)];
+            }
+        } else if (lane < cols) {
+            const uint16_t* s = reinterpret_cast<const uint16_t*>(stage);
+            for (int r = 0; r < rows; ++r) p[r * ld + lane] = s[unit2(r, lane / 8) * 8 + lane % 8];
+        }
+    }
+
+    __device__ __forceinline__ void put32(const float (&v)[32], float* base, int64_t ld) const {
+        __syncwarp();
+#pragma unroll
+        for (int c = 0; c < 8; ++c) {
+            stage[unit4(lane, c)] = make_uint4(__float_as_uint(v[4 * c]), __float_as_uint(v[4 * c + 1]),
+                                               __float_as_uint(v[4 * c + 2]), __float_as_uint(v[4 * c + 3]));
+        }
+        __syncwarp();
+        float* p = base + static_cast<int64_t>(row0) * ld + col0;
+        if (cols == 32 && on_grid(base, ld, 4)) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const int r = lane / 8 + 4 * i, c = lane % 8;
+                if (r < rows) *reinterpret_cast<uint4*>(p + r * ld + c * 4) = stage[unit4(r, c)];
+            }
+        } else if (lane < cols) {
+            const float* s = reinterpret_cast<const float*>(stage);
+            for (int r = 0; r < rows; ++r) p[r * ld + lane] = s[unit4(r, lane / 4) * 4 + lane % 4];
+        }
+    }
+
+    // adds a binary32 array's piece to v
+    __device__ __forceinline__ void add32(float (&v)[32], const float* base, int64_t ld) const {
+        const float* p = base + static_cast<int64_t>(row0) * ld + col0;
+        __syncwarp();
+        if (cols == 32 && on_grid(base, ld, 4)) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const int r = lane / 8 + 4 * i, c = lane % 8;
+                if (r < rows) stage[unit4(r, c)] = *reinterpret_cast<const uint4*>(p + r * ld + c * 4);
+            }
+        } else if (lane < cols) {
+            float* s = reinterpret_cast<float*>(stage);
+            for (int r = 0; r < rows; ++r) s[unit4(r, lane / 4) * 4 + lane % 4] = p[r * ld + lane];
+        }
+        __syncwarp();
+#pragma unroll
+        for (int c = 0; c < 8; ++c) {
+            const uint4 u = stage[unit4(lane, c)];
+            v[4 * c] += __uint_as_float(u.x);
+            v[4 * c + 1] += __uint_as_float(u.y);
+            v[4 * c + 2] += __uint_as_float(u.z);
+            v[4 * c + 3] += __uint_as_float(u.w);
+        }
+    }
+
+    __device__ __forceinline__ void add_bias(float (&v)[32], const void* bias, int f32) const {
+        float b = 0.0f;
+        if (lane < cols) {
+            b = f32 ? static_cast<const float*>(bias)[col0 + lane]
+                    : __bfloat162float(static_cast<const __nv_bfloat16*>(bias)[col0 + lane]);
+        }
+        __syncwarp();
+        reinterpret_cast<float*>(stage)[lane] = b;
+        __syncwarp();
+#pragma unroll
+        for (int c = 0; c < 8; ++c) {
+            const float4 u = reinterpret_cast<const float4*>(stage)[c];
+            v[4 * c] += u.x;
+            v[4 * c + 1] += u.y;
+            v[4 * c + 2] += u.z;
+            v[4 * c + 3] += u.w;
+        }
+    }
+};
+
+template <class T>
+__device__ __forceinline__ void to_bf16(const T (&v)[32], uint32_t (&w)[16]) {
+#pragma unroll
+    for (int j = 0; j < 16; ++j) w[j] = pack_bf16(v[2 * j], v[2 * j + 1]);
+}
+
+__device__ __forceinline__ void keep8(const Finish& f, const Piece& pc, const float (&v)[32]) {
+    const int row = pc.row0 + pc.lane;
+    uint32_t top = 0;
+#pragma unroll
+    for (int j = 0; j < 32; ++j) {
+        const uint32_t a = __float_as_uint(v[j]) & 0x7fffffffu;
+        top = (j < pc.cols && a > top) ? a : top;
+    }
+    const uint32_t e = block_exponent(top);
+    const float inv = block_inverse(e);
+    if (pc.lane >= pc.rows) return;
+    f.kept_e[static_cast<int64_t>(pc.col0 / 32) * f.kept_e_ld + row] = static_cast<uint8_t>(e);
+    uint32_t w[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        w[j] = 0;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) w[j] |= (static_cast<uint32_t>(quantise8(v[4 * j + i], inv)) & 255u) << (8 * i);
+    }
+    int8_t* q = static_cast<int8_t*>(f.kept) + static_cast<int64_t>(row) * f.kept_ld + pc.col0;
+    if (pc.cols == 32 && on_grid(f.kept, f.kept_ld, 1)) {
+        reinterpret_cast<uint4*>(q)[0] = make_uint4(w[0], w[1], w[2], w[3]);
+        reinterpret_cast<uint4*>(q)[1] = make_uint4(w[4], w[5], w[6], w[7]);
+    } else {
+#pragma unroll
+        for (int j = 0; j < 32; ++j) {
+            if (j < pc.cols) q[j] = static_cast<int8_t>(w[j / 4] >> (8 * (j % 4)));
+        }
+    }
+}
+
+__device__ __forceinline__ void times_slope8(const Finish& f, const Piece& pc, float (&v)[32]) {
+    if (pc.lane >= pc.rows) return;
+    const int row = pc.row0 + pc.lane;
+    const float s = block_scale(f.saved_e[static_cast<int64_t>(pc.col0 / 32) * f.saved_e_ld + row]);
+    const int8_t* q = static_cast<const int8_t*>(f.saved) + static_cast<int64_t>(row) * f.saved_ld + pc.col0;
+    uint32_t w[8];
+    if (pc.cols == 32 && on_grid(f.saved, f.saved_ld, 1)) {
+        const uint4 a = reinterpret_cast<const uint4*>(q)[0], b = reinterpret_cast<const uint4*>(q)[1];
+        w[0] = a.x, w[1] = a.y, w[2] = a.z, w[3] = a.w, w[4] = b.x, w[5] = b.y, w[6] = b.z, w[7] = b.w;
+    } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            w[j] = 0;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                if (4 * j + i < pc.cols) w[j] |= static_cast<uint32_t>(static_cast<uint8_t>(q[4 * j + i])) << (8 * i);
+            }
+        }
+    }
+#pragma unroll
+    for (int j = 0; j < 32; ++j) {
+        const float u = static_cast<float>(static_cast<int8_t>(w[j / 4] >> (8 * (j % 4)))) * s;
+        v[j] *= act_slope(f.slope, u);
+    }
+}
+
+// The epilogue of the layer products.
+struct General {
+    using Args = Finish;
+
+    static __device__ __forceinline__ void piece(const Finish& f, const Piece& pc, float (&v)[32]) {
+        if (f.scale != nullptr) {
+            const float g = *f.scale;
+#pragma unroll
+            for (int j = 0; j < 32; ++j) v[j] *= g;
+        }
+        if (f.bias != nullptr) pc.add_bias(v, f.bias, f.bias_f32);
+        if (f.keep == DLION_KEEP_8BIT) {
+            keep8(f, pc, v);
+        } else if (f.keep == DLION_KEEP_BF16) {
+            uint32_t w[16];
+            to_bf16(v, w);
+            pc.put16(w, f.kept, f.kept_ld);
+        }
+        if (f.act != DLION_ACT_NONE) {
+#pragma unroll
+            for (int j = 0; j < 32; ++j) v[j] = act_value(f.act, v[j]);
+        }
+        if (f.slope != DLION_ACT_NONE) {
+            if (f.saved8) {
+                times_slope8(f, pc, v);
+            } else {
+                pc.fetch16(f.saved, f.saved_ld);
+                pc.each16([&](int j, float u) { v[j] *= act_slope(f.slope, u); });
+            }
+        }
+        if (f.residual != nullptr) {
+            pc.fetch16(f.residual, f.residual_ld);
+            pc.each16([&](int j, float u) { v[j] += u; });
+        }
+        if (f.accumulated != nullptr) pc.add32(v, f.accumulated, f.accumulated_ld);
+        if (f.out_f32) {
+            pc.put32(v, static_cast<float*>(f.out), f.out_ld);
+        } else {
+            uint32_t w[16];
+            to_bf16(v, w);
+            pc.put16(w, f.out, f.out_ld);
+        }
+    }
+
+    // One warp's 32 rows and `width` columns of a finished accumulator.
+    static __device__ void tile(const Finish& f, uint32_t acc, int row0, int col0, int width, int split, uint4* stage, int lane) {
+        for (int c = 0; c < width; c += 32) {
+            float v[32];
+            if (f.partial != nullptr) {
+                tc::tmem_load32(acc + c, v);
+                const Piece pc{stage, lane, row0, col0 + c, 32, 32};
+                pc.put32(v, f.partial + split * f.partial_rows * f.partial_ld, f.partial_ld);
+                continue;
+            }
+            if (col0 + c >= f.n || row0 >= f.m) return;      // the same for the whole warp
+            tc::tmem_load32(acc + c, v);
+            const Piece pc{stage, lane, row0, col0 + c, min(32, f.m - row0), min(32, f.n - col0 - c)};
+            piece(f, pc, v);
+        }
+    }
+};
+
+// Tiles in groups of 8 rows of tiles, columns outermost within a group: the tiles in flight share
+// their operands' slices in L2.
+__device__ __forceinline__ void tile_of(const Shape& s, int t, int& tm, int& tn) {
+    constexpr int kGroup = 8;
+    const int per = kGroup * s.tiles_n, g = t / per, in = t - g * per;
+    const int rows = min(kGroup, s.tiles_m - g * kGroup);
+    tm = g * kGroup + in % rows;
+    tn = in / rows;
+}
+
+template <int CG, int BN, class E>
+__global__ void __launch_bounds__(kThreads, 1)
+product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const Shape s,
+               const __grid_constant__ typename E::Args args, unsigned int* mark) {
+    constexpr int kM = 128 * CG;               // rows of the tile; a block has 128 of them
+    constexpr int kBRows = BN / CG;            // of B, in this block
+    constexpr uint32_t kCols = 2 * BN;         // tensor memory columns
+    static_assert(16384 + kBRows * 128 <= kStageBytes, "stage");
+    constexpr uint32_t kBytes = CG * (16384 + kBRows * 128);
+
+    extern __shared__ uint8_t raw[];
+    const uint32_t base = (tc::smem_addr(raw) + 1023u) & ~1023u;
+    uint8_t* mem = raw + (base - tc::smem_addr(raw));
+    const uint32_t bars = base + kStages * kStageBytes + kEpilogueWarps * kStaging;
+    const uint32_t full = bars, empty = bars + 8 * kStages, ready = bars + 16 * kStages, drained = ready + 16;
+    const uint32_t slot = drained + 16;
+    volatile uint32_t* slot_mem = reinterpret_cast<volatile uint32_t*>(mem + (slot - base));
+
+    const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+    const uint32_t rank = CG == 2 ? tc::cluster_rank() : 0;
+    const int workers = gridDim.x / CG, worker = blockIdx.x / CG;
+    const int tiles = s.tiles_m * s.tiles_n, units = tiles * s.splits;
+
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < kStages; ++i) {
+            tc::bar_init(full + 8 * i, 1);
+            tc::bar_init(empty + 8 * i, 1);
+        }
+        for (int i = 0; i < 2; ++i) {
+            tc::bar_init(ready + 8 * i, 1);
+            tc::bar_init(drained + 8 * i, kEpilogueWarps * CG);
+        }
+        tc::bar_init_done();
+        slot_mem[1] = 0;                       // set when a wait ran out
+        tc::prefetch_map(&map_a);
+        tc::prefetch_map(&map_b);
+    }
+    if (warp == 1) tc::tmem_alloc<CG>(slot, kCols);
+    tc::fence_before();
+    __syncthreads();
+    if (CG == 2) tc::cluster_sync();
+    tc::fence_after();
+    const uint32_t tmem = *slot_mem;
+    bool fine = true;
+
+    if (warp == 0) {
+        if (lane == 0) {
+            const uint32_t lead_full = CG == 2 ? tc::map_to_rank(full, 0) : full;
+            int it = 0;
+            for (int u = worker; u < units && fine; u += workers) {
+                int tm, tn;
+                tile_of(s, u % tiles, tm, tn);
+                const int k0 = (u / tiles) * s.split_slices, k1 = min(s.slices, k0 + s.split_slices);
+                const int row = tm * kM + static_cast<int>(rank) * 128, col = tn * BN + static_cast<int>(rank) * kBRows;
+                for (int kb = k0; kb < k1; ++kb, ++it) {
+                    const int st = it % kStages;
+                    if (!(fine = tc::bar_wait(empty + 8 * st, ((it / kStages) & 1) ^ 1))) break;
+                    const uint32_t a = base + st * kStageBytes, b = a + 16384, bar = lead_full + 8 * st;
+                    if (rank == 0) tc::bar_expect(full + 8 * st, kBytes);
+                    if (s.a_mn) {
+                        tc::load_tile<CG>(a, &map_a, row, kb * kSlice, bar);
+                        tc::load_tile<CG>(a + 8192, &map_a, row + 64, kb * kSlice, bar);
+                    } else {
+                        tc::load_tile<CG>(a, &map_a, kb * kSlice, row, bar);
+                    }
+                    if (s.b_mn) {
+#pragma unroll
+                        for (int c = 0; c < kBRows / 64; ++c) tc::load_tile<CG>(b + 8192 * c, &map_b, col + 64 * c, kb * kSlice, bar);
+                    } else {
+                        tc::load_tile<CG>(b, &map_b, kb * kSlice, col, bar);
+                    }
+                }
+            }
+            // Where a wait ran out, what was asked for still lands in this block's memory: it is awaited.
+            if (!fine && rank == 0) {
+                for (int i = max(0, it - kStages); i < it; ++i) tc::bar_wait(full + 8 * (i % kStages), (i / kStages) & 1);
+            }
+        }
+    } else if (warp == 1) {
+        if (lane == 0 && rank == 0) {
+            const uint32_t inst = tc::instruction(kM, BN, s.a_mn, s.b_mn);
+            const uint64_t a_desc = tc::operand_base(s.a_mn), b_desc = tc::operand_base(s.b_mn);
+            const uint32_t a_step = (s.a_mn ? 2048 : 32) >> 4, b_step = (s.b_mn ? 2048 : 32) >> 4;   // 16 values of k
+            int it = 0, n = 0;
+            for (int u = worker; u < units && fine; u += workers, ++n) {
+                const int k0 = (u / tiles) * s.split_slices, k1 = min(s.slices, k0 + s.split_slices);
+                const int set = n & 1;
+                if (!(fine = tc::bar_wait(drained + 8 * set, ((n >> 1) & 1) ^ 1))) break;
+                tc::fence_after();
+                const uint32_t acc = tmem + set * BN;
+                for (int kb = k0; kb < k1; ++kb, ++it) {
+                    const int st = it % kStages;
+                    if (!(fine = tc::bar_wait(full + 8 * st, (it / kStages) & 1))) break;
+                    tc::fence_after();
+                    const uint32_t a = base + st * kStageBytes;
+                    const uint64_t da = a_desc | ((a >> 4) & 0x3fff), db = b_desc | (((a + 16384) >> 4) & 0x3fff);
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        tc::mma<CG>(acc, da + j * a_step, db + j * b_step, inst, (kb > k0 || j > 0) ? 1u : 0u);
+                    }
+                    tc::commit<CG>(empty + 8 * st);
+                }
+                if (fine) tc::commit<CG>(ready + 8 * set);
+            }
+        }
+    } else if (warp >= 4) {
+        const int quarter = warp % 4, half = (warp - 4) / 4;
+        uint4* stage = reinterpret_cast<uint4*>(mem + kStages * kStageBytes + (warp - 4) * kStaging);
+        const uint32_t lead_drained = CG == 2 ? tc::map_to_rank(drained, 0) : drained;
+        int n = 0;
+        for (int u = worker; u < units && fine; u += workers, ++n) {
+            int tm, tn;
+            tile_of(s, u % tiles, tm, tn);
+            const int set = n & 1;
+            if (!(fine = tc::bar_wait(ready + 8 * set, (n >> 1) & 1))) break;
+            tc::fence_after();
+            const uint32_t acc = tmem + set * BN + half * (BN / 2) + (static_cast<uint32_t>(quarter * 32) << 16);
+            E::tile(args, acc, tm * kM + static_cast<int>(rank) * 128 + quarter * 32, tn * BN + half * (BN / 2), BN / 2, u / tiles,
+                    stage, lane);
+            tc::fence_before();
+            __syncwarp();
+            if (lane == 0) {
+                if (CG == 2) {
+                    tc::bar_arrive_cluster(lead_drained + 8 * set);
+                } else {
+                    tc::bar_arrive(drained + 8 * set);
+                }
+            }
+        }
+    }
+    if (!fine) {
+        slot_mem[1] = 1;
+        *mark = 1;
+    }
+    __syncwarp();
+    tc::fence_before();
+    __syncthreads();
+    if (slot_mem[1] != 0) {                    // matrix instructions may still be running: let them end
+        const uint64_t t0 = tc::nanoseconds();
+        while (tc::nanoseconds() - t0 < 50000000ull) {
+        }
+    }
+    if (CG == 2) tc::cluster_sync();
+    tc::fence_after();
+    if (warp == 1) tc::tmem_free<CG>(tmem, kCols);
+}
+
+}  // namespace prod
+}  // namespace dlion

@@ -1,0 +1,121 @@
+// Host side of the layer products: operands, workspace, launches.
+#pragma once
+
+#include <algorithm>
+
+#include "host_checks.h"
+#include "product.cuh"
+
+namespace dlion {
+namespace prod {
+
+// bf16 matrix of any strides (in elements)
+struct Matrix {
+    const void* p;
+    int64_t rows, cols, rs, cs;
+};
+
+// Workspace handed out front to back.  With no memory behind it, it only counts: the size queries run
+// the same code as the calls.
+struct Workspace {
+    uint8_t* base = nullptr;
+    uint64_t used = 0, size = 0;
+    bool dry = true;
+    bool enough = true;
+
+    template <class T>
+    T* take(uint64_t count) {
+        const uint64_t at = used;
+        used += (count * sizeof(T) + 255u) & ~uint64_t{255};
+        if (dry) return nullptr;
+        if (used > size) {
+            enough = false;
+            return nullptr;
+        }
+        return reinterpret_cast<T*>(base + at);
+    }
+};
+
+struct Call {
+    Workspace ws;
+    cudaStream_t stream = nullptr;
+    int device = -1, sms = 148;
+    unsigned int* mark = nullptr;
+    dlion_status status = DLION_OK;
+
+    bool live() const { return !ws.dry && ws.enough && status == DLION_OK; }
+    void check(cudaError_t e) {
+        if (e != cudaSuccess && status == DLION_OK) status = DLION_ECUDA;
+    }
+    dlion_status end() const { return status != DLION_OK ? status : (ws.dry || ws.enough) ? DLION_OK : DLION_EINVAL; }
+};
+
+// Device, SM count and the mark's address; the workspace's extent.
+dlion_status begin(Call& c, void* workspace, uint64_t bytes, void* stream);
+
+// `a` itself if tiles of it can be copied in place, otherwise a packed copy in the workspace.
+Matrix readable(Call& c, const Matrix& a);
+
+// D[rows of a][rows of b] = sum over the columns of both; a.T / b.T by swapping rows and cols, rs and cs.
+// Both must be readable.  f.m, f.n are set here.
+void product(Call& c, const Matrix& a, const Matrix& b, Finish f);
+
+inline Matrix transposed(const Matrix& a) { return Matrix{a.p, a.cols, a.rows, a.cs, a.rs}; }
+
+// Tensor map of 64 x `box` tiles; `mn` of the operand's rows adjacent (1) or its columns (0).
+bool make_map(CUtensorMap* map, const Matrix& a, int* mn_major, int box_rows);
+
+struct Config {
+    int cg, bn, splits, split_slices;
+};
+Config choose(const Call& c, int64_t m, int64_t n, int64_t k, bool may_split);
+
+// Tile counts of a configuration; false if the tiles cannot be numbered.
+bool shape_of(const Config& cfg, const Matrix& a, const Matrix& b, Shape* s);
+
+template <int CG, int BN, class E>
+void launch(Call& c, const CUtensorMap& ma, const CUtensorMap& mb, const Shape& s, const typename E::Args& f) {
+    auto* kernel = &product_kernel<CG, BN, E>;
+    c.check(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem));
+    const int64_t units = static_cast<int64_t>(s.tiles_m) * s.tiles_n * s.splits;
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3(static_cast<unsigned>(std::min<int64_t>(units, c.sms / CG) * CG));
+    cfg.blockDim = dim3(kThreads);
+    cfg.dynamicSmemBytes = kSmem;
+    cfg.stream = c.stream;
+    cudaLaunchAttribute at[1];
+    at[0].id = cudaLaunchAttributeClusterDimension;
+    at[0].val.clusterDim.x = CG;
+    at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
+    cfg.attrs = at;
+    cfg.numAttrs = CG == 2 ? 1 : 0;
+    if (c.status == DLION_OK) c.check(cudaLaunchKernelEx(&cfg, kernel, ma, mb, s, f, c.mark));
+}
+
+
+inline int64_t round_up(int64_t v, int64_t to) { return (v + to - 1) / to * to; }
+inline int64_t parts(int64_t v, int64_t of) { return (v + of - 1) / of; }
+
+template <class P, class F>
+uint64_t workspace_of(const P& p, F f) {
+    Call c;
+    int dev = 0, sms = 0;
+    if (cudaGetDevice(&dev) == cudaSuccess && cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) == cudaSuccess) c.sms = sms;
+    f(c, p);
+    return std::max(c.ws.size, c.ws.used);
+}
+
+template <class P, class F>
+dlion_status run(const P& p, F f, void* workspace, uint64_t bytes, void* stream) {
+    if (bytes != 0 && workspace == nullptr) return DLION_EINVAL;
+    if (!aligned16(workspace)) return DLION_EALIGN;
+    if (bytes < workspace_of(p, f)) return DLION_EINVAL;        // nothing is launched
+    Call c;
+    const dlion_status st = begin(c, workspace, bytes, stream);
+    if (st != DLION_OK) return st;
+    f(c, p);
+    return c.end();
+}
+
+}  // namespace prod
+}  // namespace dlion
