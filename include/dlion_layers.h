@@ -20,7 +20,8 @@
  *   - NaN and infinities go through as the formulas say; relu(NaN) = NaN.
  *
  * Every buffer is DEVICE memory owned by the caller.  A matrix is a pointer and two strides in
- * ELEMENTS; rows, cols and strides are non-negative and at most 2^30 rows and columns.  Where a
+ * ELEMENTS; rows, cols and strides are non-negative and at most 2^30 rows and columns (2^24 - 256 columns
+ * of u and of the 8-bit form).  Where a
  * parameter has one stride ("ld", between rows) its columns are adjacent.  x, w, dy take any strides:
  * an operand that the copy engine cannot read in place (neither stride 1, a base or the other stride
  * off the 16-byte grid) is packed into the workspace first.  m = 0 (no rows) is allowed: sums over

@@ -11,102 +11,161 @@ using namespace dlion::prod;
 constexpr int64_t kMost = int64_t{1} << 30;
 
 bool size_ok(int64_t v, int64_t least) { return v >= least && v <= kMost; }
+constexpr int64_t kMostCols = 65535 * 256;   // blocks along a grid's second axis
 bool type_ok(int t) { return t == DLION_GRAD_F32 || t == DLION_GRAD_BF16; }
 int type_bytes(int t) { return t == DLION_GRAD_F32 ? 4 : 2; }
 bool stride_ok(int64_t s) { return s >= 0 && s <= (int64_t{1} << 40); }
 bool ld_ok(int64_t ld, int64_t rows, int64_t cols) { return stride_ok(ld) && (rows <= 1 || ld >= cols); }
 
-// act(u) as a bf16 operand, eight values a thread.  Bound by memory: 2 (or 33/32) + 2 bytes a value.
-__global__ void __launch_bounds__(256) operand_kernel(const void* u, int64_t u_ld, const uint8_t* e, int64_t e_ld, int eight, int act,
-                                                      int64_t m, int64_t k, __nv_bfloat16* out, int64_t out_ld, int wide) {
-    const int64_t per_row = (k + 7) / 8;
-    const int64_t at = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;
-    const int64_t row = at / per_row, col = (at - row * per_row) * 8;
-    if (row >= m) return;
-    const int valid = static_cast<int>(k - col < 8 ? k - col : 8);
-    float v[8];
-    if (eight) {
-        const int8_t* q = static_cast<const int8_t*>(u) + row * u_ld + col;
-        const float s = block_scale(e[(col / 32) * e_ld + row]);
-        int8_t b[8] = {};
-        if (wide && valid == 8) {
-            *reinterpret_cast<uint2*>(b) = *reinterpret_cast<const uint2*>(q);
-        } else {
-            for (int i = 0; i < valid; ++i) b[i] = q[i];
-        }
+// The element-wise kernels take 32 rows x 256 columns a block: a thread has eight columns of four rows, all
+// loads under way at once, and the block's 8 x 32 exponents go through shared memory, because a row's neighbours in
+// the exponents' array are the next rows, not the next blocks.
+constexpr int kTileRows = 32, kTileCols = 256;
+
+__device__ __forceinline__ uint32_t extent(int64_t left, int most) { return static_cast<uint32_t>(left < most ? (left > 0 ? left : 0) : most); }
+
+__device__ __forceinline__ void widen(const uint4& w, float (&v)[8]) {
+    const uint32_t x[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = static_cast<float>(b[i]) * s;
-    } else {
-        const __nv_bfloat16* p = static_cast<const __nv_bfloat16*>(u) + row * u_ld + col;
-        if (wide && valid == 8) {
-            const uint4 w = *reinterpret_cast<const uint4*>(p);
-            const uint32_t x[4] = {w.x, w.y, w.z, w.w};
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                v[2 * i] = bf16_lo(x[i]);
-                v[2 * i + 1] = bf16_hi(x[i]);
-            }
-        } else {
-            for (int i = 0; i < 8; ++i) v[i] = i < valid ? __bfloat162float(p[i]) : 0.0f;
-        }
-    }
-#pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = act_value(act, v[i]);
-    __nv_bfloat16* o = out + row * out_ld + col;
-    if (valid == 8 && on_grid(out, out_ld, 2)) {
-        *reinterpret_cast<uint4*>(o) = make_uint4(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7]));
-    } else {
-        for (int i = 0; i < valid; ++i) o[i] = __float2bfloat16_rn(v[i]);
+    for (int i = 0; i < 4; ++i) {
+        v[2 * i] = bf16_lo(x[i]);
+        v[2 * i + 1] = bf16_hi(x[i]);
     }
 }
 
-// Rows of x into the 8-bit form: four threads a block of 32 values, eight values each.
-__global__ void __launch_bounds__(256) checkpoint8_kernel(const __nv_bfloat16* x, int64_t x_ld, int64_t m, int64_t k, int8_t* q,
-                                                          int64_t q_ld, uint8_t* e, int64_t e_ld, int wide) {
-    const int64_t per_row = (k + 31) / 32 * 4;
-    const int64_t at = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;
-    const int64_t row = at / per_row, col = (at - row * per_row) * 8;
-    const bool in = row < m;                    // whole groups of four threads
-    const int valid = in && col < k ? static_cast<int>(k - col < 8 ? k - col : 8) : 0;
-    float v[8] = {};
-    if (valid != 0) {
-        const __nv_bfloat16* p = x + row * x_ld + col;
-        if (wide && valid == 8) {
-            const uint4 w = *reinterpret_cast<const uint4*>(p);
-            const uint32_t u[4] = {w.x, w.y, w.z, w.w};
+__device__ __forceinline__ uint4 narrow(const float (&v)[8]) {
+    return make_uint4(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7]));
+}
+
+// eight bf16 values at p, `valid` of them there (the rest 0)
+__device__ __forceinline__ uint4 take16(const __nv_bfloat16* p, uint32_t valid, bool wide) {
+    if (wide && valid == 8) return *reinterpret_cast<const uint4*>(p);
+    uint16_t b[8];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                v[2 * i] = bf16_lo(u[i]);
-                v[2 * i + 1] = bf16_hi(u[i]);
-            }
-        } else {
-            for (int i = 0; i < valid; ++i) v[i] = __bfloat162float(p[i]);
-        }
-    }
-    uint32_t top = 0;
+    for (int i = 0; i < 8; ++i) b[i] = static_cast<uint32_t>(i) < valid ? reinterpret_cast<const uint16_t*>(p)[i] : uint16_t{0};
+    uint32_t w[4];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) top = max(top, __float_as_uint(v[i]) & 0x7fffffffu);
-    top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
-    top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
-    if (!in) return;
-    const uint32_t ex = block_exponent(top);
-    const float inv = block_inverse(ex);
-    if (threadIdx.x % 4 == 0) e[(col / 32) * e_ld + row] = static_cast<uint8_t>(ex);
+    for (int i = 0; i < 4; ++i) w[i] = b[2 * i] | (static_cast<uint32_t>(b[2 * i + 1]) << 16);
+    return make_uint4(w[0], w[1], w[2], w[3]);
+}
+
+__device__ __forceinline__ uint2 take8(const int8_t* p, uint32_t valid, bool wide) {
+    if (wide && valid == 8) return *reinterpret_cast<const uint2*>(p);
     uint32_t w[2] = {0, 0};
 #pragma unroll
-    for (int i = 0; i < 8; ++i) w[i / 4] |= (static_cast<uint32_t>(quantise8(v[i], inv)) & 255u) << (8 * (i % 4));
-    int8_t* o = q + row * q_ld + col;
-    if (wide && valid == 8) {
-        *reinterpret_cast<uint2*>(o) = make_uint2(w[0], w[1]);
-    } else {
-        for (int i = 0; i < valid; ++i) o[i] = static_cast<int8_t>(w[i / 4] >> (8 * (i % 4)));
+    for (int i = 0; i < 8; ++i) {
+        if (static_cast<uint32_t>(i) < valid) w[i / 4] |= static_cast<uint32_t>(static_cast<uint8_t>(p[i])) << (8 * (i % 4));
     }
+    return make_uint2(w[0], w[1]);
+}
+
+// act(u) as a bf16 operand.  Bound by memory: 2 (or 33/32) + 2 bytes a value.
+template <bool EIGHT, int ACT>
+__global__ void __launch_bounds__(256) operand_kernel(const void* u, int64_t u_ld, const uint8_t* e, int64_t e_ld, int64_t m, int64_t k,
+                                                      __nv_bfloat16* out, int64_t out_ld, int wide, int wide_out) {
+    __shared__ uint8_t ex[8][kTileRows];
+    tc::let_next_start();
+    tc::wait_for_previous();
+    const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
+    const int64_t row0 = static_cast<int64_t>(blockIdx.x) * kTileRows, col0 = static_cast<int64_t>(blockIdx.y) * kTileCols;
+    const int64_t col = col0 + lane * 8;
+    const uint32_t valid = extent(k - col, 8);
+    if (EIGHT) {
+        if (row0 + lane < m && col0 + warp * 32 < k) ex[warp][lane] = e[(col0 / 32 + warp) * e_ld + row0 + lane];
+    }
+    uint4 w[4];
+    uint2 q[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int64_t row = row0 + warp + 8 * i;
+        const uint32_t n = row < m ? valid : 0;
+        if (EIGHT) {
+            q[i] = take8(static_cast<const int8_t*>(u) + row * u_ld + col, n, wide);
+        } else {
+            w[i] = take16(static_cast<const __nv_bfloat16*>(u) + row * u_ld + col, n, wide);
+        }
+    }
+    if (EIGHT) __syncthreads();
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int r = warp + 8 * i;
+        if (row0 + r >= m || valid == 0) continue;
+        float v[8];
+        if (EIGHT) {
+            const float s = block_scale(ex[lane / 4][r]);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[j] = static_cast<float>(static_cast<int8_t>((j < 4 ? q[i].x : q[i].y) >> (8 * (j % 4)))) * s;
+        } else {
+            widen(w[i], v);
+        }
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] = act_value<ACT>(v[j]);
+        __nv_bfloat16* o = out + (row0 + r) * out_ld + col;
+        if (wide_out && valid == 8) {
+            *reinterpret_cast<uint4*>(o) = narrow(v);
+        } else {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                if (static_cast<uint32_t>(j) < valid) o[j] = __float2bfloat16_rn(v[j]);
+            }
+        }
+    }
+}
+
+// Rows of x into the 8-bit form: a block of 32 values is four neighbouring threads.
+__global__ void __launch_bounds__(256) checkpoint8_kernel(const __nv_bfloat16* x, int64_t x_ld, int64_t m, int64_t k, int8_t* q,
+                                                          int64_t q_ld, uint8_t* e, int64_t e_ld, int wide, int wide_out) {
+    __shared__ uint8_t ex[8][kTileRows];
+    tc::let_next_start();
+    tc::wait_for_previous();
+    const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
+    const int64_t row0 = static_cast<int64_t>(blockIdx.x) * kTileRows, col0 = static_cast<int64_t>(blockIdx.y) * kTileCols;
+    const int64_t col = col0 + lane * 8;
+    const uint32_t valid = extent(k - col, 8);
+    uint4 w[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int64_t row = row0 + warp + 8 * i;
+        w[i] = take16(x + row * x_ld + col, row < m ? valid : 0, wide);
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int r = warp + 8 * i;
+        uint32_t top = 0;
+        const uint32_t b[4] = {w[i].x, w[i].y, w[i].z, w[i].w};
+#pragma unroll
+        for (int j = 0; j < 4; ++j) top = max(top, max((b[j] << 16) & 0x7fffffffu, b[j] & 0x7fff0000u));
+        top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
+        top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
+        const uint32_t scale = block_exponent(top);
+        const float inv = block_inverse(scale);
+        if (lane % 4 == 0) ex[lane / 4][r] = static_cast<uint8_t>(scale);
+        float v[8];
+        widen(w[i], v);
+        uint32_t o[2] = {0, 0};
+#pragma unroll
+        for (int j = 0; j < 8; ++j) o[j / 4] |= (static_cast<uint32_t>(quantise8(v[j], inv)) & 255u) << (8 * (j % 4));
+        if (row0 + r >= m || valid == 0) continue;
+        int8_t* p = q + (row0 + r) * q_ld + col;
+        if (wide_out && valid == 8) {
+            *reinterpret_cast<uint2*>(p) = make_uint2(o[0], o[1]);
+        } else {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                if (static_cast<uint32_t>(j) < valid) p[j] = static_cast<int8_t>(o[j / 4] >> (8 * (j % 4)));
+            }
+        }
+    }
+    __syncthreads();
+    if (row0 + lane < m && col0 + warp * 32 < k) e[(col0 / 32 + warp) * e_ld + row0 + lane] = ex[warp][lane];
 }
 
 // Sums over rows in two steps, in a fixed order: a block has 256 columns and a run of rows.
 __global__ void __launch_bounds__(256) column_sums_kernel(const __nv_bfloat16* a, int64_t rs, int64_t cs, int64_t rows, int64_t cols,
                                                           int64_t run, float* partial, int wide) {
     __shared__ float sum[8][257];
+    tc::let_next_start();
+    tc::wait_for_previous();
     const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
     const int64_t c0 = static_cast<int64_t>(blockIdx.x) * 256 + lane * 8;
     const int64_t r0 = static_cast<int64_t>(blockIdx.y) * run, r1 = r0 + run < rows ? r0 + run : rows;
@@ -142,6 +201,8 @@ __global__ void __launch_bounds__(256) column_sums_kernel(const __nv_bfloat16* a
 }
 
 __global__ void __launch_bounds__(256) join_sums_kernel(const float* partial, int runs, int64_t cols, void* out, int f32) {
+    tc::let_next_start();
+    tc::wait_for_previous();
     const int64_t c = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;
     if (c >= cols) return;
     float t = 0.0f;
@@ -161,20 +222,23 @@ void column_sums(Call& c, const Matrix& a, void* out, int type) {
     float* partial = c.ws.take<float>(static_cast<uint64_t>(runs) * a.cols);
     if (!c.live()) return;
     const int wide = a.cs == 1 && aligned16(a.p) && a.rs % 8 == 0;
-    column_sums_kernel<<<dim3(static_cast<unsigned>(strips), static_cast<unsigned>(runs)), 256, 0, c.stream>>>(
-        static_cast<const __nv_bfloat16*>(a.p), a.rs, a.cs, a.rows, a.cols, run, partial, wide);
-    c.check(cudaGetLastError());
-    join_sums_kernel<<<static_cast<unsigned>(strips), 256, 0, c.stream>>>(partial, static_cast<int>(runs), a.cols, out,
-                                                                         type == DLION_GRAD_F32);
-    c.check(cudaGetLastError());
+    start(c, column_sums_kernel, dim3(static_cast<unsigned>(strips), static_cast<unsigned>(runs)), dim3(256), 0, 1,
+          static_cast<const __nv_bfloat16*>(a.p), a.rs, a.cs, a.rows, a.cols, run, partial, wide);
+    start(c, join_sums_kernel, dim3(static_cast<unsigned>(strips)), dim3(256), 0, 1, partial, static_cast<int>(runs), a.cols, out,
+          type == DLION_GRAD_F32);
 }
 
 void operand(Call& c, const void* u, int64_t u_ld, const uint8_t* e, int64_t e_ld, int eight, int act, int64_t m, int64_t k,
              __nv_bfloat16* out, int64_t out_ld) {
-    const int wide = aligned(u, eight ? 8 : 16) && u_ld % 8 == 0;
-    const int64_t blocks = parts(m * parts(k, 8), 256);
-    operand_kernel<<<static_cast<unsigned>(blocks), 256, 0, c.stream>>>(u, u_ld, e, e_ld, eight, act, m, k, out, out_ld, wide);
-    c.check(cudaGetLastError());
+    const int wide = aligned(u, eight ? 8 : 16) && u_ld % 8 == 0, wide_out = aligned16(out) && out_ld % 8 == 0;
+    const dim3 grid(static_cast<unsigned>(parts(m, kTileRows)), static_cast<unsigned>(parts(k, kTileCols)));
+    auto go = [&](auto* kernel) { start(c, kernel, grid, dim3(256), 0, 1, u, u_ld, e, e_ld, m, k, out, out_ld, wide, wide_out); };
+    switch (act) {
+        case DLION_ACT_RELU: eight ? go(operand_kernel<true, DLION_ACT_RELU>) : go(operand_kernel<false, DLION_ACT_RELU>); break;
+        case DLION_ACT_GELU: eight ? go(operand_kernel<true, DLION_ACT_GELU>) : go(operand_kernel<false, DLION_ACT_GELU>); break;
+        case DLION_ACT_SILU: eight ? go(operand_kernel<true, DLION_ACT_SILU>) : go(operand_kernel<false, DLION_ACT_SILU>); break;
+        default: eight ? go(operand_kernel<true, DLION_ACT_NONE>) : go(operand_kernel<false, DLION_ACT_NONE>); break;
+    }
 }
 
 dlion_status check_forward(const dlion_linear_fwd* p) {
@@ -219,7 +283,7 @@ void forward(Call& c, const dlion_linear_fwd& p) {
 dlion_status check_backward(const dlion_linear_bwd* p) {
     if (p == nullptr || !size_ok(p->m, 0) || !size_ok(p->k, 1) || !size_ok(p->n, 1)) return DLION_EINVAL;
     if (p->act < DLION_ACT_NONE || p->act > DLION_ACT_SILU) return DLION_EINVAL;
-    if (p->saved != DLION_KEEP_BF16 && p->saved != DLION_KEEP_8BIT) return DLION_EINVAL;
+    if (p->k > kMostCols || (p->saved != DLION_KEEP_BF16 && p->saved != DLION_KEEP_8BIT)) return DLION_EINVAL;
     if (!type_ok(p->grad_type)) return DLION_EINVAL;
     if (!stride_ok(p->dy_rs) || !stride_ok(p->dy_cs)) return DLION_EINVAL;
     const bool needs_u = p->dw != nullptr || (p->dx != nullptr && p->act != DLION_ACT_NONE);
@@ -323,27 +387,28 @@ dlion_status dlion_linear_backward(const dlion_linear_bwd* p, void* workspace, u
 
 dlion_status dlion_checkpoint8(const void* x, int64_t x_ld, int64_t m, int64_t k, int8_t* q, int64_t q_ld, uint8_t* e, int64_t e_ld,
                                void* cuda_stream) {
-    if (!size_ok(m, 0) || !size_ok(k, 1) || !ld_ok(x_ld, m, k) || !ld_ok(q_ld, m, k) || !ld_ok(e_ld, parts(k, 32), m)) return DLION_EINVAL;
-    if (m == 0) return DLION_OK;
-    if (x == nullptr || q == nullptr || e == nullptr) return DLION_EINVAL;
-    if (!aligned(x, 2)) return DLION_EALIGN;
-    int dev = 0;
-    if (cudaGetDevice(&dev) != cudaSuccess) return DLION_ECUDA;
-    const int wide = aligned16(x) && x_ld % 8 == 0 && aligned(q, 8) && q_ld % 8 == 0;
-    checkpoint8_kernel<<<static_cast<unsigned>(parts(m * parts(k, 32) * 4, 256)), 256, 0, static_cast<cudaStream_t>(cuda_stream)>>>(
-        static_cast<const __nv_bfloat16*>(x), x_ld, m, k, q, q_ld, e, e_ld, wide);
-    return cudaGetLastError() == cudaSuccess ? DLION_OK : DLION_ECUDA;
-}
-
-dlion_status dlion_restore8(const int8_t* q, int64_t q_ld, const uint8_t* e, int64_t e_ld, int64_t m, int64_t k, void* x, int64_t x_ld,
-                            void* cuda_stream) {
-    if (!size_ok(m, 0) || !size_ok(k, 1) || !ld_ok(x_ld, m, k) || !ld_ok(q_ld, m, k) || !ld_ok(e_ld, parts(k, 32), m)) return DLION_EINVAL;
+    if (!size_ok(m, 0) || !size_ok(k, 1) || k > kMostCols || !ld_ok(x_ld, m, k) || !ld_ok(q_ld, m, k) || !ld_ok(e_ld, parts(k, 32), m)) return DLION_EINVAL;
     if (m == 0) return DLION_OK;
     if (x == nullptr || q == nullptr || e == nullptr) return DLION_EINVAL;
     if (!aligned(x, 2)) return DLION_EALIGN;
     Call c;
-    if (cudaGetDevice(&c.device) != cudaSuccess) return DLION_ECUDA;
     c.stream = static_cast<cudaStream_t>(cuda_stream);
+    if (!device_of(c)) return DLION_ECUDA;
+    const int wide = aligned16(x) && x_ld % 8 == 0, wide_out = aligned(q, 8) && q_ld % 8 == 0;
+    const dim3 grid(static_cast<unsigned>(parts(m, kTileRows)), static_cast<unsigned>(parts(k, kTileCols)));
+    start(c, checkpoint8_kernel, grid, dim3(256), 0, 1, static_cast<const __nv_bfloat16*>(x), x_ld, m, k, q, q_ld, e, e_ld, wide, wide_out);
+    return c.status;
+}
+
+dlion_status dlion_restore8(const int8_t* q, int64_t q_ld, const uint8_t* e, int64_t e_ld, int64_t m, int64_t k, void* x, int64_t x_ld,
+                            void* cuda_stream) {
+    if (!size_ok(m, 0) || !size_ok(k, 1) || k > kMostCols || !ld_ok(x_ld, m, k) || !ld_ok(q_ld, m, k) || !ld_ok(e_ld, parts(k, 32), m)) return DLION_EINVAL;
+    if (m == 0) return DLION_OK;
+    if (x == nullptr || q == nullptr || e == nullptr) return DLION_EINVAL;
+    if (!aligned(x, 2)) return DLION_EALIGN;
+    Call c;
+    c.stream = static_cast<cudaStream_t>(cuda_stream);
+    if (!device_of(c)) return DLION_ECUDA;
     operand(c, q, q_ld, e, e_ld, 1, DLION_ACT_NONE, m, k, static_cast<__nv_bfloat16*>(x), x_ld);
     return c.status;
 }

@@ -31,11 +31,11 @@ struct LossTile {
         int64_t ld;
     };
 
-    static __device__ void tile(const Args& p, uint32_t acc, int row0, int col0, int width, int, uint4* stage, int lane) {
+    static __device__ __forceinline__ void tile(const Args& p, uint32_t acc, int row0, int col0, int width, int, bool live, uint4* stage, int lane) {
         if (row0 >= p.m || col0 >= p.n) return;
         const int row = row0 + lane;
         const int valid = min(width, p.n - col0);
-        const int rows = min(32, p.m - row0);
+        const int rows = live ? min(32, p.m - row0) : 0;
         const int64_t target = lane < rows ? p.targets[row] : -1;
         const int hit = target >= col0 && target < col0 + valid ? static_cast<int>(target - col0) : -1;
         float top = -INFINITY;
@@ -73,7 +73,7 @@ struct LossTile {
             }
             if (p.codes != nullptr) {
                 const Piece pc{stage, lane, row0, col0 + c, rows, 32};      // ld covers the last tile
-                pc.put16(w, p.codes, p.ld);
+                pc.put16(w, p.codes, p.ld, true);
             }
         }
         if (lane < rows) p.stats[static_cast<int64_t>(col0 / width) * p.m + row] = make_float2(top, sum);
@@ -95,6 +95,8 @@ __device__ __forceinline__ float block_sum(float v, float* shared) {       // 10
 // factor[0] = scale / (rows with a target)
 __global__ void __launch_bounds__(1024) factor_kernel(const int64_t* targets, int64_t m, int64_t ignore, int mean, float scale, float* factor) {
     __shared__ int counts[32];
+    tc::let_next_start();
+    tc::wait_for_previous();
     int n = 0;
     for (int64_t i = threadIdx.x; i < m; i += 1024) n += targets[i] != ignore;
     n = __reduce_add_sync(0xffffffffu, n);
@@ -111,6 +113,8 @@ __global__ void __launch_bounds__(1024) factor_kernel(const int64_t* targets, in
 __global__ void __launch_bounds__(1024) rows_kernel(const float2* stats, int groups, int64_t m, const int64_t* targets, int64_t ignore,
                                                     int64_t v, const float* at_target, float2* lse, float* rows) {
     __shared__ float2 part[32][33];
+    tc::let_next_start();
+    tc::wait_for_previous();
     const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
     const int64_t row = static_cast<int64_t>(blockIdx.x) * 32 + lane;
     float top = -INFINITY, sum = 0.0f;
@@ -146,6 +150,8 @@ __global__ void __launch_bounds__(1024) rows_kernel(const float2* stats, int gro
 // since at the target d is close to -g in every row.
 __global__ void __launch_bounds__(256) gradient_kernel(uint16_t* codes, int64_t ld, int n, int width, const float2* stats, int64_t m,
                                                        const int64_t* targets, int64_t ignore, const float2* lse) {
+    tc::let_next_start();
+    tc::wait_for_previous();
     const int64_t row = blockIdx.y + static_cast<int64_t>(blockIdx.z) * 65535;
     const int col = (blockIdx.x * 256 + threadIdx.x) * 8;
     if (row >= m || col >= n) return;
@@ -178,6 +184,8 @@ __global__ void __launch_bounds__(256) gradient_kernel(uint16_t* codes, int64_t 
 // The rows' losses to the loss, in a fixed order.
 __global__ void __launch_bounds__(1024) loss_kernel(const float* rows, const int64_t* targets, int64_t m, int64_t ignore, int mean, float* loss) {
     __shared__ float shared[32];
+    tc::let_next_start();
+    tc::wait_for_previous();
     float v = 0.0f, n = 0.0f;               // a thread counts at most 2^20 rows: exact
     for (int64_t i = threadIdx.x; i < m; i += 1024) {
         v += rows[i];
@@ -219,7 +227,7 @@ void loss(Call& c, const dlion_loss& p) {
     const int64_t ld = round_up(p.v, 256);
     // without gradients nothing is kept of a piece, and all rows are one
     const int64_t step = grads ? piece : p.m;
-    const Config cfg = choose(c, step, p.v, p.h, false);
+    const Config cfg = choose(c, step, p.v, p.h, false, true);
     const int width = cfg.bn / 2;
     const int64_t groups = parts(p.v, width);
     float2* stats = c.ws.take<float2>(static_cast<uint64_t>(groups) * step);
@@ -229,8 +237,7 @@ void loss(Call& c, const dlion_loss& p) {
     uint16_t* codes = grads ? c.ws.take<uint16_t>(static_cast<uint64_t>(step) * ld) : nullptr;
     float* sums = grads && !f32 && step < p.m ? c.ws.take<float>(static_cast<uint64_t>(p.v) * p.h) : nullptr;
     if (grads && c.live()) {
-        factor_kernel<<<1, 1024, 0, c.stream>>>(p.targets, p.m, p.ignore_index, p.mean, p.scale, factor);
-        c.check(cudaGetLastError());
+        start(c, factor_kernel, dim3(1), dim3(1024), 0, 1, p.targets, p.m, p.ignore_index, p.mean, p.scale, factor);
     }
     for (int64_t r = 0; r < p.m; r += step) {
         const int64_t rows = std::min(step, p.m - r);
@@ -244,26 +251,23 @@ void loss(Call& c, const dlion_loss& p) {
                 c.status = DLION_EINVAL;
                 return;
             }
-            if (!make_map(&ma, xp, &s.a_mn, 128) || !make_map(&mb, w, &s.b_mn, 128)) {
+            if (!make_map(&ma, xp, &s.a_mn, 128) || !make_map(&mb, w, &s.b_mn, cfg.bn / cfg.cg)) {
                 c.status = DLION_ECUDA;
                 return;
             }
             const LossTile::Args args{static_cast<int>(rows), static_cast<int>(p.v), p.targets + r, stats, at_target, codes, ld};
             if (cfg.cg == 2) {
-                launch<2, 256, LossTile>(c, ma, mb, s, args);
+                launch<2, 256, LossTile, kWhole>(c, ma, mb, s, args);
             } else {
-                launch<1, 128, LossTile>(c, ma, mb, s, args);
+                launch<1, 128, LossTile, kWhole>(c, ma, mb, s, args);
             }
             if (c.status != DLION_OK) return;
-            rows_kernel<<<static_cast<unsigned>(parts(rows, 32)), 1024, 0, c.stream>>>(
-                stats, static_cast<int>(groups), rows, p.targets + r, p.ignore_index, p.v, at_target, lse, p.rows + r);
-            c.check(cudaGetLastError());
+            start(c, rows_kernel, dim3(static_cast<unsigned>(parts(rows, 32))), dim3(1024), 0, 1, stats, groups, rows, p.targets + r,
+                  p.ignore_index, p.v, at_target, lse, p.rows + r);
             if (grads) {
                 const dim3 grid(static_cast<unsigned>(parts(p.v, 2048)), static_cast<unsigned>(std::min<int64_t>(rows, 65535)),
                                 static_cast<unsigned>(parts(rows, 65535)));
-                gradient_kernel<<<grid, 256, 0, c.stream>>>(codes, ld, static_cast<int>(p.v), width, stats, rows, p.targets + r,
-                                                            p.ignore_index, lse);
-                c.check(cudaGetLastError());
+                start(c, gradient_kernel, grid, dim3(256), 0, 1, codes, ld, p.v, width, stats, rows, p.targets + r, p.ignore_index, lse);
             }
         }
         if (!grads) continue;
@@ -288,8 +292,7 @@ void loss(Call& c, const dlion_loss& p) {
         product(c, transposed(d), transposed(xp), fw);
     }
     if (c.live()) {
-        loss_kernel<<<1, 1024, 0, c.stream>>>(p.rows, p.targets, p.m, p.ignore_index, p.mean, p.loss);
-        c.check(cudaGetLastError());
+        start(c, loss_kernel, dim3(1), dim3(1024), 0, 1, p.rows, p.targets, p.m, p.ignore_index, p.mean, p.loss);
     }
 }
 

@@ -5,6 +5,7 @@
 #include <cuda_bf16.h>
 
 #include <cstdint>
+#include <type_traits>
 
 #include "dlion_layers.h"
 
@@ -33,29 +34,48 @@ __device__ __forceinline__ float gelu_arg(float z) { return fabsf(z) > 64.0f ? c
 constexpr float kGelu2c = 1.5957691216057308f;              // 2 sqrt(2/pi)
 
 // half of 1 + tanh(u) is the logistic function of 2u, so every activation costs one ex2 and one rcp.
-__device__ __forceinline__ float act_value(int act, float z) {
-    if (act == DLION_ACT_RELU) return z < 0.0f ? 0.0f : z;  // NaN stays
-    if (act == DLION_ACT_SILU) return z * logistic(z);
-    if (act == DLION_ACT_GELU) {
+// The kind is a template parameter: chosen element by element it would keep the elements of a thread from
+// overlapping, and a product's epilogue is bound by that latency (the 8192 x 2048 x 8192 product with gelu and
+// 8-bit z: 335 us so, 236 us with the choice made once for 32 elements).
+template <int ACT>
+__device__ __forceinline__ float act_value(float z) {
+    if (ACT == DLION_ACT_RELU) return z < 0.0f ? 0.0f : z;  // NaN stays
+    if (ACT == DLION_ACT_SILU) return z * logistic(z);
+    if (ACT == DLION_ACT_GELU) {
         const float c = gelu_arg(z);
         return z * logistic(kGelu2c * c * __fmaf_rn(0.044715f * c, c, 1.0f));
     }
     return z;
 }
 
-__device__ __forceinline__ float act_slope(int act, float z) {
-    if (act == DLION_ACT_RELU) return z > 0.0f ? 1.0f : (z == z ? 0.0f : z);
-    if (act == DLION_ACT_SILU) {
+template <int ACT>
+__device__ __forceinline__ float act_slope(float z) {
+    if (ACT == DLION_ACT_RELU) return z > 0.0f ? 1.0f : (z == z ? 0.0f : z);
+    if (ACT == DLION_ACT_SILU) {
         const float p = logistic(z);
         const float c = fabsf(z) > 128.0f ? copysignf(128.0f, z) : z;   // p (1 - p) is 0 there
         return __fmaf_rn(c * p, 1.0f - p, p);
     }
-    if (act == DLION_ACT_GELU) {
+    if (ACT == DLION_ACT_GELU) {
         const float c = gelu_arg(z), c2 = c * c;
         const float p = logistic(kGelu2c * c * __fmaf_rn(0.044715f, c2, 1.0f));
         return __fmaf_rn(c * kGelu2c * __fmaf_rn(0.134145f, c2, 1.0f), p * (1.0f - p), p);
     }
     return 1.0f;
+}
+
+// f(std::integral_constant<int, act>) for a kind known at run time
+template <class F>
+__device__ __forceinline__ void with_act(int act, F f) {
+    if (act == DLION_ACT_GELU) {
+        f(std::integral_constant<int, DLION_ACT_GELU>{});
+    } else if (act == DLION_ACT_SILU) {
+        f(std::integral_constant<int, DLION_ACT_SILU>{});
+    } else if (act == DLION_ACT_RELU) {
+        f(std::integral_constant<int, DLION_ACT_RELU>{});
+    } else {
+        f(std::integral_constant<int, DLION_ACT_NONE>{});
+    }
 }
 
 // ---- the 8-bit form: 32 values share 2^(e-127)

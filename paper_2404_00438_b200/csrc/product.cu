@@ -30,6 +30,8 @@ EncodeTiled encoder() {
 
 // One element a thread: a warp has 32 columns of a row, so that the 8-bit form's blocks are warps.
 __global__ void __launch_bounds__(256) sum_splits_kernel(const Finish f, int splits) {
+    tc::let_next_start();
+    tc::wait_for_previous();
     const int lane = threadIdx.x % 32;
     const int64_t per_row = (f.n + 31) / 32;
     const int64_t at = static_cast<int64_t>(blockIdx.x) * 8 + threadIdx.x / 32;
@@ -60,7 +62,7 @@ __global__ void __launch_bounds__(256) sum_splits_kernel(const Finish f, int spl
         static_cast<__nv_bfloat16*>(f.kept)[row * f.kept_ld + col] = __float2bfloat16_rn(v);
     }
     if (!in) return;
-    v = act_value(f.act, v);
+    with_act(f.act, [&](auto kind) { v = act_value<decltype(kind)::value>(v); });
     if (f.slope != DLION_ACT_NONE) {
         float u;
         if (f.saved8) {
@@ -69,7 +71,7 @@ __global__ void __launch_bounds__(256) sum_splits_kernel(const Finish f, int spl
         } else {
             u = __bfloat162float(static_cast<const __nv_bfloat16*>(f.saved)[row * f.saved_ld + col]);
         }
-        v *= act_slope(f.slope, u);
+        with_act(f.slope, [&](auto kind) { v *= act_slope<decltype(kind)::value>(u); });
     }
     if (f.residual != nullptr) v += __bfloat162float(f.residual[row * f.residual_ld + col]);
     if (f.accumulated != nullptr) v += f.accumulated[row * f.accumulated_ld + col];
@@ -84,6 +86,8 @@ __global__ void __launch_bounds__(256) sum_splits_kernel(const Finish f, int spl
 __global__ void __launch_bounds__(256) pack_kernel(const uint16_t* a, int64_t rs, int64_t cs, int64_t rows, int64_t cols,
                                                    uint16_t* out, int64_t ld) {
     __shared__ uint16_t t[32][34];
+    tc::let_next_start();
+    tc::wait_for_previous();
     const int x = threadIdx.x % 32, y = threadIdx.x / 32;
     const int64_t across = (cols + 31) / 32;
     const int64_t r0 = blockIdx.x / across * 32, c0 = blockIdx.x % across * 32;
@@ -100,30 +104,71 @@ __global__ void __launch_bounds__(256) pack_kernel(const uint16_t* a, int64_t rs
 
 }  // namespace
 
-// Estimated time of a division of the work, in clocks of an SM: rounds of tiles, each of so many slices
-// and an epilogue that the next tile hides, the sum of the splits at the L2's rate.
-Config choose(const Call& c, int64_t m, int64_t n, int64_t k, bool may_split) {
+// The division of the work with the least estimated time, in clocks of an SM: rounds of tiles, each of so many
+// slices and an epilogue that the next tile hides.
+//   pair        540 a slice (512 the tensor cores' own), splits summed by a second kernel at the L2's rate;
+//   block       560 a slice: its 32 KB come at the 57 bytes a clock that one SM gets from L2, measured on
+//               197 x 768 x 768, where 12 slices took 6850;
+//   joined      the same with fewer slices each, and the exchange.
+Config choose(const Call& c, int64_t m, int64_t n, int64_t k, bool sums, bool alone) {
     const int64_t slices = std::max<int64_t>(1, parts(k, kSlice));
-    Config best{2, 256, 1, static_cast<int>(slices)};
+    const bool long_sums = sums && slices > kSegment;
+    Config best{2, 256, kWhole, 1, static_cast<int>(slices)};
     double least = 1e300;
-    for (int pair = 1; pair >= 0; --pair) {
-        const int64_t tm = parts(m, pair ? 256 : 128), tn = parts(n, pair ? 256 : 128), tiles = tm * tn;
-        const int64_t workers = pair ? c.sms / 2 : c.sms;
-        const double slice = pair ? 540.0 : 400.0, fixed = pair ? 2600.0 : 2000.0;
-        const int64_t most = may_split ? std::min<int64_t>(64, std::max<int64_t>(1, slices / 4)) : 1;
-        for (int64_t s = 1; s <= most; ++s) {
-            const int64_t per = parts(slices, s);
-            const int64_t used = parts(slices, per);
-            if (used != s) continue;
-            double t = static_cast<double>(parts(tiles * s, workers)) * (per * slice + 600.0) + fixed;
-            if (s > 1) t += 4000.0 + static_cast<double>(s) * tm * tn * (pair ? 65536 : 16384) * 8.0 / 3000.0;
-            if (t < least) {
-                least = t;
-                best = Config{pair ? 2 : 1, pair ? 256 : 128, static_cast<int>(s), static_cast<int>(per)};
-            }
+    auto consider = [&](int cg, int bn, int form, int64_t s, double slice, double fixed) {
+        const int64_t per = parts(slices, s);
+        if (parts(slices, per) != s) return;
+        const int64_t tm = parts(m, 128 * cg), tn = parts(n, bn);
+        double t;
+        if (form == kJoined) {
+            if (tm * tn * s > 16 * 8) return;  // clusters of eight: sixteen at a time for certain
+            t = per * slice + fixed + 3000.0;
+        } else {
+            t = static_cast<double>(parts(tm * tn * s, c.sms / cg)) * (per * slice + 600.0) + fixed;
+            if (s > 1) t += 6000.0 + static_cast<double>(s) * tm * tn * cg * bn * 128 * 8.0 / 3000.0;
+        }
+        if (t < least) {
+            least = t;
+            best = Config{cg, bn, form, static_cast<int>(s), static_cast<int>(per)};
+        }
+    };
+    const int64_t most = alone ? 1 : std::min<int64_t>(32, std::max<int64_t>(1, slices / 8));
+    for (int64_t s = 1; s <= most; ++s) {
+        if (long_sums) {
+            consider(2, 128, kLong, s, 330.0, 5000.0);
+        } else {
+            consider(2, 256, kWhole, s, 540.0, 5000.0);
         }
     }
+    if (!long_sums) consider(1, 128, kWhole, 1, 560.0, 4500.0);
+    for (int64_t s = 2; !alone && s <= 8; s *= 2) {
+        if (sums && parts(slices, s) > kSegment) continue;
+        consider(1, 128, kJoined, s, 560.0, 4500.0);
+    }
     return best;
+}
+
+// What a device's properties and the library's symbols say, asked once a device.
+struct Device {
+    std::atomic<int> sms{0};
+    std::atomic<unsigned int*> mark{nullptr};
+};
+static Device devices[64];
+
+bool device_of(Call& c) {
+    if (cudaGetDevice(&c.device) != cudaSuccess || c.device < 0 || c.device >= 64) return false;
+    Device& d = devices[c.device];
+    int sms = d.sms.load(std::memory_order_acquire);
+    if (sms == 0) {
+        void* mark = nullptr;
+        if (cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, c.device) != cudaSuccess) return false;
+        if (cudaGetSymbolAddress(&mark, wait_ran_out) != cudaSuccess || encoder() == nullptr) return false;
+        d.mark.store(static_cast<unsigned int*>(mark), std::memory_order_relaxed);
+        d.sms.store(sms, std::memory_order_release);
+    }
+    c.sms = sms;
+    c.mark = d.mark.load(std::memory_order_relaxed);
+    return true;
 }
 
 dlion_status begin(Call& c, void* workspace, uint64_t bytes, void* stream) {
@@ -131,12 +176,7 @@ dlion_status begin(Call& c, void* workspace, uint64_t bytes, void* stream) {
     c.ws.size = bytes;
     c.ws.dry = false;
     c.stream = static_cast<cudaStream_t>(stream);
-    if (cudaGetDevice(&c.device) != cudaSuccess) return DLION_ECUDA;
-    if (cudaDeviceGetAttribute(&c.sms, cudaDevAttrMultiProcessorCount, c.device) != cudaSuccess) return DLION_ECUDA;
-    void* mark = nullptr;
-    if (cudaGetSymbolAddress(&mark, wait_ran_out) != cudaSuccess || encoder() == nullptr) return DLION_ECUDA;
-    c.mark = static_cast<unsigned int*>(mark);
-    return DLION_OK;
+    return device_of(c) ? DLION_OK : DLION_ECUDA;
 }
 
 static bool rows_in_place(const void* p, int64_t rows, int64_t cols, int64_t rs, int64_t cs) {
@@ -163,9 +203,8 @@ Matrix readable(Call& c, const Matrix& a) {
     r.p = out;
     if (c.live()) {
         const int64_t blocks = parts(a.rows, 32) * parts(a.cols, 32);
-        pack_kernel<<<static_cast<unsigned>(blocks), 256, 0, c.stream>>>(static_cast<const uint16_t*>(a.p), a.rs, a.cs, a.rows, a.cols,
-                                                                         out, r.rs);
-        c.check(cudaGetLastError());
+        start(c, pack_kernel, dim3(static_cast<unsigned>(blocks)), dim3(256), 0, 1, static_cast<const uint16_t*>(a.p), a.rs, a.cs, a.rows,
+              a.cols, out, r.rs);
     }
     return r;
 }
@@ -197,34 +236,42 @@ bool shape_of(const Config& cfg, const Matrix& a, const Matrix& b, Shape* s) {
 void product(Call& c, const Matrix& a, const Matrix& b, Finish f) {
     f.m = static_cast<int>(a.rows);
     f.n = static_cast<int>(b.rows);
-    const Config cfg = choose(c, a.rows, b.rows, a.cols, true);
+    f.todo = (f.scale != nullptr ? kScale : 0u) | (f.bias != nullptr ? kBias : 0u) | (f.keep == DLION_KEEP_BF16 ? kKeep16 : 0u) |
+             (f.keep == DLION_KEEP_8BIT ? kKeep8 : 0u) | (f.act != DLION_ACT_NONE ? kAct : 0u) | (f.slope != DLION_ACT_NONE ? kSlope : 0u) |
+             (f.residual != nullptr ? kResidual : 0u) | (f.accumulated != nullptr ? kAdd : 0u);
+    f.wide = aligned16(f.out) && f.out_ld * (f.out_f32 ? 4 : 2) % 16 == 0;
+    const Config cfg = choose(c, a.rows, b.rows, a.cols, f.out_f32 != 0, false);
     Shape s{};
     if (!shape_of(cfg, a, b, &s)) {
         c.status = DLION_EINVAL;
         return;
     }
     const uint64_t mark = c.ws.used;
-    if (cfg.splits > 1) {
+    const bool partial = cfg.splits > 1 && cfg.form != kJoined;
+    if (partial) {
         f.partial_ld = static_cast<int64_t>(s.tiles_n) * cfg.bn;
         f.partial_rows = static_cast<int64_t>(s.tiles_m) * 128 * cfg.cg;
         f.partial = c.ws.take<float>(static_cast<uint64_t>(cfg.splits) * f.partial_ld * f.partial_rows);
     }
     if (c.live()) {
         CUtensorMap ma, mb;
-        const bool ok = make_map(&ma, a, &s.a_mn, 128) && make_map(&mb, b, &s.b_mn, 128);
+        const bool ok = make_map(&ma, a, &s.a_mn, 128) && make_map(&mb, b, &s.b_mn, cfg.bn / cfg.cg);
         if (!ok) {
             c.status = DLION_ECUDA;
             return;
         }
-        if (cfg.cg == 2) {
-            launch<2, 256, General>(c, ma, mb, s, f);
+        if (cfg.form == kLong) {
+            launch<2, 128, General, kLong>(c, ma, mb, s, f);
+        } else if (cfg.form == kJoined) {
+            launch<1, 128, General, kJoined>(c, ma, mb, s, f);
+        } else if (cfg.cg == 2) {
+            launch<2, 256, General, kWhole>(c, ma, mb, s, f);
         } else {
-            launch<1, 128, General>(c, ma, mb, s, f);
+            launch<1, 128, General, kWhole>(c, ma, mb, s, f);
         }
-        if (cfg.splits > 1 && c.status == DLION_OK) {
+        if (partial) {
             const int64_t warps = static_cast<int64_t>(f.m) * parts(f.n, 32);
-            sum_splits_kernel<<<static_cast<unsigned>(parts(warps, 8)), 256, 0, c.stream>>>(f, cfg.splits);
-            c.check(cudaGetLastError());
+            start(c, sum_splits_kernel, dim3(static_cast<unsigned>(parts(warps, 8))), dim3(256), 0, 1, f, cfg.splits);
         }
     }
     if (c.ws.dry) {

@@ -3,6 +3,13 @@
 //   warp 0      copies 64-wide slices of A and B into a ring of shared-memory stages,
 //   warp 1      issues the matrix instructions; accumulators are two sets of BN columns of tensor memory,
 //   warps 4-11  take the finished set out while the next one fills (rows 32 (w % 4).., half the columns each).
+// A kernel's code is not in the instruction cache when it starts, and an epilogue met cold took 3500 clocks for 64
+// columns; so while the first slices are on their way the epilogue warps run it once on nothing (`live` false: no rows).
+// Three forms of the same kernel: kWhole (above); kJoined, where the blocks of a cluster each take a share of k of
+// one 128 x 128 tile and send each other their sums, every block adding a share of the tile, for products with fewer tiles than SMs;
+// kLong, for binary32 results of long sums: the tensor core's accumulator drops what does not fit, which after K
+// products shifts a sum by about K 2^-30 of itself, so it only adds kSegment of them and the epilogue
+// adds the segments in registers, rounding to nearest.
 // A pair computes 256 x 256 with each block holding half of A and half of B, so a block reads 32 KB of
 // shared memory for 128 x 256 x 64 products, where a single block's 128 x 128 tile reads the same 32 KB for
 // half of that: the pair is what large shapes use, the single block what small ones use.
@@ -14,6 +21,9 @@
 namespace dlion {
 namespace prod {
 
+enum Form { kWhole = 0, kJoined = 1, kLong = 2 };
+
+constexpr int kSegment = 16;               // slices
 constexpr int kSlice = 64;                 // values of k per stage: one 128-byte swizzled row
 constexpr int kStages = 6;
 constexpr int kStageBytes = 32768;         // A: 128 rows, B: 128 rows (of each block)
@@ -29,10 +39,14 @@ struct Shape {
     int splits, split_slices, slices;      // slices of k in all, and per split
 };
 
+enum Todo : unsigned { kScale = 1, kBias = 2, kKeep16 = 4, kKeep8 = 8, kAct = 16, kSlope = 32, kResidual = 64, kAdd = 128 };
+
 // What happens to a sum; every part is optional.  Order: * scale, + bias, keep z, act, * act'(saved), + residual,
 // + accumulated, store.
 struct Finish {
     int m, n;
+    unsigned todo;                         // kScale.. below: one test where nothing is asked for
+    int wide;                              // rows of out begin on the 16-byte grid
     const float* scale;                    // on the device
     const void* bias;
     int bias_f32;
@@ -86,9 +100,11 @@ struct Piece {
             }
         } else {
             __nv_bfloat16* s = reinterpret_cast<__nv_bfloat16*>(stage);
-            if (lane < cols) {
-                for (int r = 0; r < rows; ++r) s[unit2(r, lane / 8) * 8 + lane % 8] = p[r * ld + lane];
-            }
+            __nv_bfloat16 v[32];           // all on their way before the first is used
+#pragma unroll
+            for (int r = 0; r < 32; ++r) v[r] = lane < cols && r < rows ? p[r * ld + lane] : __nv_bfloat16();
+#pragma unroll
+            for (int r = 0; r < 32; ++r) s[unit2(r, lane / 8) * 8 + lane % 8] = v[r];
         }
         __syncwarp();
     }
@@ -108,13 +124,13 @@ struct Piece {
         }
     }
 
-    __device__ __forceinline__ void put16(const uint32_t (&w)[16], void* base, int64_t ld) const {
+    __device__ __forceinline__ void put16(const uint32_t (&w)[16], void* base, int64_t ld, bool wide) const {
         __syncwarp();
 #pragma unroll
         for (int c = 0; c < 4; ++c) stage[unit2(lane, c)] = make_uint4(w[4 * c], w[4 * c + 1], w[4 * c + 2], w[4 * c + 3]);
         __syncwarp();
         uint16_t* p = static_cast<uint16_t*>(base) + static_cast<int64_t>(row0) * ld + col0;
-        if (cols == 32 && on_grid(base, ld, 2)) {
+        if (cols == 32 && wide) {
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 const int r = lane / 4 + 8 * i, c = lane % 4;
@@ -122,11 +138,12 @@ struct Piece {
             }
         } else if (lane < cols) {
             const uint16_t* s = reinterpret_cast<const uint16_t*>(stage);
+            #pragma unroll 8
             for (int r = 0; r < rows; ++r) p[r * ld + lane] = s[unit2(r, lane / 8) * 8 + lane % 8];
         }
     }
 
-    __device__ __forceinline__ void put32(const float (&v)[32], float* base, int64_t ld) const {
+    __device__ __forceinline__ void put32(const float (&v)[32], float* base, int64_t ld, bool wide) const {
         __syncwarp();
 #pragma unroll
         for (int c = 0; c < 8; ++c) {
@@ -135,7 +152,7 @@ struct Piece {
         }
         __syncwarp();
         float* p = base + static_cast<int64_t>(row0) * ld + col0;
-        if (cols == 32 && on_grid(base, ld, 4)) {
+        if (cols == 32 && wide) {
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 const int r = lane / 8 + 4 * i, c = lane % 8;
@@ -143,6 +160,7 @@ struct Piece {
             }
         } else if (lane < cols) {
             const float* s = reinterpret_cast<const float*>(stage);
+            #pragma unroll 8
             for (int r = 0; r < rows; ++r) p[r * ld + lane] = s[unit4(r, lane / 4) * 4 + lane % 4];
         }
     }
@@ -157,9 +175,12 @@ struct Piece {
                 const int r = lane / 8 + 4 * i, c = lane % 8;
                 if (r < rows) stage[unit4(r, c)] = *reinterpret_cast<const uint4*>(p + r * ld + c * 4);
             }
-        } else if (lane < cols) {
+        } else {
             float* s = reinterpret_cast<float*>(stage);
-            for (int r = 0; r < rows; ++r) s[unit4(r, lane / 4) * 4 + lane % 4] = p[r * ld + lane];
+#pragma unroll 8
+            for (int r = 0; r < 32; ++r) {
+                if (lane < cols && r < rows) s[unit4(r, lane / 4) * 4 + lane % 4] = p[r * ld + lane];
+            }
         }
         __syncwarp();
 #pragma unroll
@@ -248,71 +269,95 @@ __device__ __forceinline__ void times_slope8(const Finish& f, const Piece& pc, f
             }
         }
     }
+    with_act(f.slope, [&](auto kind) {
 #pragma unroll
-    for (int j = 0; j < 32; ++j) {
-        const float u = static_cast<float>(static_cast<int8_t>(w[j / 4] >> (8 * (j % 4)))) * s;
-        v[j] *= act_slope(f.slope, u);
-    }
+        for (int j = 0; j < 32; ++j) {
+            const float u = static_cast<float>(static_cast<int8_t>(w[j / 4] >> (8 * (j % 4)))) * s;
+            v[j] *= act_slope<decltype(kind)::value>(u);
+        }
+    });
 }
 
-// The epilogue of the layer products.
+// The epilogue of the layer products.  What a call does not ask for is out of the way of what it does (the hints):
+// a small product runs this code once, and each jump over unused code costs a fetch of some 500 clocks.
 struct General {
     using Args = Finish;
 
-    static __device__ __forceinline__ void piece(const Finish& f, const Piece& pc, float (&v)[32]) {
-        if (f.scale != nullptr) {
-            const float g = *f.scale;
+    static __device__ __forceinline__ void piece(const Finish& f, unsigned todo, const Piece& pc, float (&v)[32]) {
+        if (__builtin_expect(todo != 0, 0)) {
+            if (todo & kScale) {
+                const float g = *f.scale;
 #pragma unroll
-            for (int j = 0; j < 32; ++j) v[j] *= g;
-        }
-        if (f.bias != nullptr) pc.add_bias(v, f.bias, f.bias_f32);
-        if (f.keep == DLION_KEEP_8BIT) {
-            keep8(f, pc, v);
-        } else if (f.keep == DLION_KEEP_BF16) {
-            uint32_t w[16];
-            to_bf16(v, w);
-            pc.put16(w, f.kept, f.kept_ld);
-        }
-        if (f.act != DLION_ACT_NONE) {
-#pragma unroll
-            for (int j = 0; j < 32; ++j) v[j] = act_value(f.act, v[j]);
-        }
-        if (f.slope != DLION_ACT_NONE) {
-            if (f.saved8) {
-                times_slope8(f, pc, v);
-            } else {
-                pc.fetch16(f.saved, f.saved_ld);
-                pc.each16([&](int j, float u) { v[j] *= act_slope(f.slope, u); });
+                for (int j = 0; j < 32; ++j) v[j] *= g;
             }
+            if (todo & kBias) pc.add_bias(v, f.bias, f.bias_f32);
+            if (todo & kKeep8) keep8(f, pc, v);
+            if (todo & kKeep16) {
+                uint32_t w[16];
+                to_bf16(v, w);
+                pc.put16(w, f.kept, f.kept_ld, on_grid(f.kept, f.kept_ld, 2));
+            }
+            if (todo & kAct) {
+                with_act(f.act, [&](auto kind) {
+#pragma unroll
+                    for (int j = 0; j < 32; ++j) v[j] = act_value<decltype(kind)::value>(v[j]);
+                });
+            }
+            if (todo & kSlope) {
+                if (f.saved8) {
+                    times_slope8(f, pc, v);
+                } else {
+                    pc.fetch16(f.saved, f.saved_ld);
+                    with_act(f.slope, [&](auto kind) {
+                        pc.each16([&](int j, float u) { v[j] *= act_slope<decltype(kind)::value>(u); });
+                    });
+                }
+            }
+            if (todo & kResidual) {
+                pc.fetch16(f.residual, f.residual_ld);
+                pc.each16([&](int j, float u) { v[j] += u; });
+            }
+            if (todo & kAdd) pc.add32(v, f.accumulated, f.accumulated_ld);
         }
-        if (f.residual != nullptr) {
-            pc.fetch16(f.residual, f.residual_ld);
-            pc.each16([&](int j, float u) { v[j] += u; });
-        }
-        if (f.accumulated != nullptr) pc.add32(v, f.accumulated, f.accumulated_ld);
-        if (f.out_f32) {
-            pc.put32(v, static_cast<float*>(f.out), f.out_ld);
+        if (__builtin_expect(f.out_f32, 0)) {
+            pc.put32(v, static_cast<float*>(f.out), f.out_ld, f.wide != 0);
         } else {
             uint32_t w[16];
             to_bf16(v, w);
-            pc.put16(w, f.out, f.out_ld);
+            pc.put16(w, f.out, f.out_ld, f.wide != 0);
+        }
+    }
+
+    // The same from registers.
+    template <int W>
+    static __device__ __forceinline__ void sums(const Finish& f, const float (&acc)[W], int row0, int col0, bool live, uint4* stage, int lane) {
+#pragma unroll
+        for (int c = 0; c < W; c += 32) {
+            if (col0 + c >= f.n || row0 >= f.m) return;
+            float v[32];
+#pragma unroll
+            for (int j = 0; j < 32; ++j) v[j] = acc[c + j];
+            piece(f, f.todo, Piece{stage, lane, row0, col0 + c, live ? min(32, f.m - row0) : 0, min(32, f.n - col0 - c)}, v);
         }
     }
 
     // One warp's 32 rows and `width` columns of a finished accumulator.
-    static __device__ void tile(const Finish& f, uint32_t acc, int row0, int col0, int width, int split, uint4* stage, int lane) {
+    static __device__ __forceinline__ void tile(const Finish& f, uint32_t acc, int row0, int col0, int width, int split, bool live, uint4* stage, int lane) {
+        const unsigned todo = f.todo;
+#pragma unroll 1
         for (int c = 0; c < width; c += 32) {
             float v[32];
-            if (f.partial != nullptr) {
+            if (__builtin_expect(f.partial != nullptr, 0)) {
                 tc::tmem_load32(acc + c, v);
-                const Piece pc{stage, lane, row0, col0 + c, 32, 32};
-                pc.put32(v, f.partial + split * f.partial_rows * f.partial_ld, f.partial_ld);
+                const Piece pc{stage, lane, row0, col0 + c, live ? 32 : 0, 32};
+                pc.put32(v, f.partial + split * f.partial_rows * f.partial_ld, f.partial_ld, true);
                 continue;
             }
             if (col0 + c >= f.n || row0 >= f.m) return;      // the same for the whole warp
             tc::tmem_load32(acc + c, v);
-            const Piece pc{stage, lane, row0, col0 + c, min(32, f.m - row0), min(32, f.n - col0 - c)};
-            piece(f, pc, v);
+            const Piece pc{stage, lane, row0, col0 + c, live ? min(32, f.m - row0) : 0, min(32, f.n - col0 - c)};
+            piece(f, todo, pc, v);
+            if (!live) return;
         }
     }
 };
@@ -327,7 +372,7 @@ __device__ __forceinline__ void tile_of(const Shape& s, int t, int& tm, int& tn)
     tn = in / rows;
 }
 
-template <int CG, int BN, class E>
+template <int CG, int BN, class E, int FORM>
 __global__ void __launch_bounds__(kThreads, 1)
 product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const Shape s,
                const __grid_constant__ typename E::Args args, unsigned int* mark) {
@@ -335,21 +380,29 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
     constexpr int kBRows = BN / CG;            // of B, in this block
     constexpr uint32_t kCols = 2 * BN;         // tensor memory columns
     static_assert(16384 + kBRows * 128 <= kStageBytes, "stage");
+    static_assert(FORM != kJoined || (CG == 1 && BN == 128), "joined tiles are a block's own");
     constexpr uint32_t kBytes = CG * (16384 + kBRows * 128);
 
     extern __shared__ uint8_t raw[];
     const uint32_t base = (tc::smem_addr(raw) + 1023u) & ~1023u;
     uint8_t* mem = raw + (base - tc::smem_addr(raw));
     const uint32_t bars = base + kStages * kStageBytes + kEpilogueWarps * kStaging;
+    constexpr int kRing = FORM == kJoined ? 4 : kStages;
+    constexpr uint32_t kPiece = 4096, kPieces = 16;                    // kJoined: 32 x 32 sums, behind a shorter ring
+    const uint32_t landing = base + 4 * kStageBytes, landed = bars + 16 * kStages + 40;
     const uint32_t full = bars, empty = bars + 8 * kStages, ready = bars + 16 * kStages, drained = ready + 16;
     const uint32_t slot = drained + 16;
     volatile uint32_t* slot_mem = reinterpret_cast<volatile uint32_t*>(mem + (slot - base));
 
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
     const uint32_t rank = CG == 2 ? tc::cluster_rank() : 0;
-    const int workers = gridDim.x / CG, worker = blockIdx.x / CG;
     const int tiles = s.tiles_m * s.tiles_n, units = tiles * s.splits;
+    // kJoined: the cluster is the worker, a block's place in it the split; one tile each
+    const int share = FORM == kJoined ? static_cast<int>(tc::cluster_rank()) : 0;
+    const int workers = FORM == kJoined ? units : gridDim.x / CG;
+    const int worker = FORM == kJoined ? static_cast<int>(blockIdx.x) / s.splits + share * tiles : static_cast<int>(blockIdx.x) / CG;
 
+    tc::let_next_start();
     if (threadIdx.x == 0) {
         for (int i = 0; i < kStages; ++i) {
             tc::bar_init(full + 8 * i, 1);
@@ -359,7 +412,9 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
             tc::bar_init(ready + 8 * i, 1);
             tc::bar_init(drained + 8 * i, kEpilogueWarps * CG);
         }
+        if (FORM == kJoined) tc::bar_init(landed, 1);
         tc::bar_init_done();
+        if (FORM == kJoined) tc::bar_expect(landed, kPieces * kPiece);
         slot_mem[1] = 0;                       // set when a wait ran out
         tc::prefetch_map(&map_a);
         tc::prefetch_map(&map_b);
@@ -368,9 +423,11 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
     tc::fence_before();
     __syncthreads();
     if (CG == 2) tc::cluster_sync();
+    if (FORM == kJoined) tc::cluster_arrive();
     tc::fence_after();
     const uint32_t tmem = *slot_mem;
     bool fine = true;
+    tc::wait_for_previous();
 
     if (warp == 0) {
         if (lane == 0) {
@@ -382,8 +439,8 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
                 const int k0 = (u / tiles) * s.split_slices, k1 = min(s.slices, k0 + s.split_slices);
                 const int row = tm * kM + static_cast<int>(rank) * 128, col = tn * BN + static_cast<int>(rank) * kBRows;
                 for (int kb = k0; kb < k1; ++kb, ++it) {
-                    const int st = it % kStages;
-                    if (!(fine = tc::bar_wait(empty + 8 * st, ((it / kStages) & 1) ^ 1))) break;
+                    const int st = it % kRing;
+                    if (!(fine = tc::bar_wait(empty + 8 * st, ((it / kRing) & 1) ^ 1))) break;
                     const uint32_t a = base + st * kStageBytes, b = a + 16384, bar = lead_full + 8 * st;
                     if (rank == 0) tc::bar_expect(full + 8 * st, kBytes);
                     if (s.a_mn) {
@@ -402,7 +459,7 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
             }
             // Where a wait ran out, what was asked for still lands in this block's memory: it is awaited.
             if (!fine && rank == 0) {
-                for (int i = max(0, it - kStages); i < it; ++i) tc::bar_wait(full + 8 * (i % kStages), (i / kStages) & 1);
+                for (int i = max(0, it - kRing); i < it; ++i) tc::bar_wait(full + 8 * (i % kRing), (i / kRing) & 1);
             }
         }
     } else if (warp == 1) {
@@ -411,41 +468,36 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
             const uint64_t a_desc = tc::operand_base(s.a_mn), b_desc = tc::operand_base(s.b_mn);
             const uint32_t a_step = (s.a_mn ? 2048 : 32) >> 4, b_step = (s.b_mn ? 2048 : 32) >> 4;   // 16 values of k
             int it = 0, n = 0;
-            for (int u = worker; u < units && fine; u += workers, ++n) {
+            for (int u = worker; u < units && fine; u += workers) {
                 const int k0 = (u / tiles) * s.split_slices, k1 = min(s.slices, k0 + s.split_slices);
-                const int set = n & 1;
-                if (!(fine = tc::bar_wait(drained + 8 * set, ((n >> 1) & 1) ^ 1))) break;
-                tc::fence_after();
-                const uint32_t acc = tmem + set * BN;
-                for (int kb = k0; kb < k1; ++kb, ++it) {
-                    const int st = it % kStages;
-                    if (!(fine = tc::bar_wait(full + 8 * st, (it / kStages) & 1))) break;
+                const int seg = FORM == kLong ? kSegment : k1 - k0;
+                for (int kb = k0; kb < k1 && fine; ++n) {
+                    const int set = n & 1, from = kb, to = min(k1, kb + seg);
+                    if (!(fine = tc::bar_wait(drained + 8 * set, ((n >> 1) & 1) ^ 1))) break;
                     tc::fence_after();
-                    const uint32_t a = base + st * kStageBytes;
-                    const uint64_t da = a_desc | ((a >> 4) & 0x3fff), db = b_desc | (((a + 16384) >> 4) & 0x3fff);
+                    const uint32_t acc = tmem + set * BN;
+                    for (; kb < to; ++kb, ++it) {
+                        const int st = it % kRing;
+                        if (!(fine = tc::bar_wait(full + 8 * st, (it / kRing) & 1))) break;
+                        tc::fence_after();
+                        const uint32_t a = base + st * kStageBytes;
+                        const uint64_t da = a_desc | ((a >> 4) & 0x3fff), db = b_desc | (((a + 16384) >> 4) & 0x3fff);
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        tc::mma<CG>(acc, da + j * a_step, db + j * b_step, inst, (kb > k0 || j > 0) ? 1u : 0u);
+                        for (int j = 0; j < 4; ++j) {
+                            tc::mma<CG>(acc, da + j * a_step, db + j * b_step, inst, (kb > from || j > 0) ? 1u : 0u);
+                        }
+                        tc::commit<CG>(empty + 8 * st);
                     }
-                    tc::commit<CG>(empty + 8 * st);
+                    if (fine) tc::commit<CG>(ready + 8 * set);
                 }
-                if (fine) tc::commit<CG>(ready + 8 * set);
             }
         }
     } else if (warp >= 4) {
         const int quarter = warp % 4, half = (warp - 4) / 4;
         uint4* stage = reinterpret_cast<uint4*>(mem + kStages * kStageBytes + (warp - 4) * kStaging);
         const uint32_t lead_drained = CG == 2 ? tc::map_to_rank(drained, 0) : drained;
-        int n = 0;
-        for (int u = worker; u < units && fine; u += workers, ++n) {
-            int tm, tn;
-            tile_of(s, u % tiles, tm, tn);
-            const int set = n & 1;
-            if (!(fine = tc::bar_wait(ready + 8 * set, (n >> 1) & 1))) break;
-            tc::fence_after();
-            const uint32_t acc = tmem + set * BN + half * (BN / 2) + (static_cast<uint32_t>(quarter * 32) << 16);
-            E::tile(args, acc, tm * kM + static_cast<int>(rank) * 128 + quarter * 32, tn * BN + half * (BN / 2), BN / 2, u / tiles,
-                    stage, lane);
+        const uint32_t part = tmem + half * (BN / 2) + (static_cast<uint32_t>(quarter * 32) << 16);
+        auto drain = [&](int set) {
             tc::fence_before();
             __syncwarp();
             if (lane == 0) {
@@ -455,6 +507,86 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
                     tc::bar_arrive(drained + 8 * set);
                 }
             }
+        };
+        if (FORM == kJoined) tc::cluster_wait();     // the others' barriers exist
+        int n = 0;
+        for (int u = worker - workers; u < units && fine; u += workers) {
+            const bool live = u >= 0 && (FORM == kJoined ? u == worker : true);
+            int tm, tn;
+            tile_of(s, (live ? u : worker) % tiles, tm, tn);
+            const int row0 = tm * kM + static_cast<int>(rank) * 128 + quarter * 32, col0 = tn * BN + half * (BN / 2);
+            if constexpr (FORM == kLong) {
+                const int k0 = (u / tiles) * s.split_slices, k1 = min(s.slices, k0 + s.split_slices);
+                float sum[BN / 2] = {};
+                for (int kb = k0; live && kb < k1; kb += kSegment, ++n) {
+                    const int set = n & 1;
+                    if (!(fine = tc::bar_wait(ready + 8 * set, (n >> 1) & 1))) break;
+                    tc::fence_after();
+#pragma unroll
+                    for (int c = 0; c < BN / 2; c += 32) {
+                        float v[32];
+                        tc::tmem_load32(part + set * BN + c, v);
+#pragma unroll
+                        for (int j = 0; j < 32; ++j) sum[c + j] += v[j];
+                    }
+                    drain(set);
+                }
+                if (fine) E::sums(args, sum, row0, col0, live, stage, lane);
+            } else if constexpr (FORM == kJoined) {
+                if (live) {
+                    if (!(fine = tc::bar_wait(ready, 0))) break;
+                    tc::fence_after();
+                    // into the ring, which has been read: 32 x 32 pieces, units exchanged as in Piece; and off to the
+                    // block that adds this piece of all shares
+                    const int p0 = half * (BN / 64) * 4 + quarter;
+#pragma unroll
+                    for (int c = 0; c < BN / 2; c += 32) {
+                        float v[32];
+                        tc::tmem_load32(part + c, v);
+                        float4* to = reinterpret_cast<float4*>(mem + (p0 + c / 8) * kPiece);
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) {
+                            to[lane * 8 + (i ^ (lane & 7))] = make_float4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
+                        }
+                    }
+                    tc::fence_for_copies();
+                    __syncwarp();
+                    if (lane < BN / 64) {
+                        const int p = p0 + lane * 4;
+                        const uint32_t owner = static_cast<uint32_t>(p % s.splits);
+                        tc::send(tc::map_to_rank(landing + ((p / s.splits) * s.splits + share) * kPiece, owner), base + p * kPiece, kPiece,
+                                 tc::map_to_rank(landed, owner));
+                    }
+                    if (!(fine = tc::bar_wait(landed, 0))) break;
+                }
+                for (int p = share + s.splits * (warp - 4); p < static_cast<int>(kPieces); p += s.splits * kEpilogueWarps) {
+                    const float4* from = reinterpret_cast<const float4*>(mem + 4 * kStageBytes + (p / s.splits) * s.splits * kPiece);
+                    float v[32] = {};
+                    for (int r = 0; r < s.splits; ++r, from += kPiece / 16) {
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) {
+                            const float4 w = from[lane * 8 + (i ^ (lane & 7))];
+                            v[4 * i] += w.x;
+                            v[4 * i + 1] += w.y;
+                            v[4 * i + 2] += w.z;
+                            v[4 * i + 3] += w.w;
+                        }
+                    }
+                    E::sums(args, v, tm * kM + (p % 4) * 32, tn * BN + (p / 4) * 32, live, stage, lane);
+                    if (!live) break;
+                }
+            } else {
+                const int set = n & 1;
+                if (live) {
+                    if (!(fine = tc::bar_wait(ready + 8 * set, (n >> 1) & 1))) break;
+                    tc::fence_after();
+                }
+                E::tile(args, part + set * BN, row0, col0, BN / 2, u / tiles, live, stage, lane);
+                if (live) {
+                    drain(set);
+                    ++n;
+                }
+            }
         }
     }
     if (!fine) {
@@ -462,6 +594,7 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
         *mark = 1;
     }
     __syncwarp();
+    if (FORM == kJoined && warp < 4) tc::cluster_wait();
     tc::fence_before();
     __syncthreads();
     if (slot_mem[1] != 0) {                    // matrix instructions may still be running: let them end
@@ -469,7 +602,7 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
         while (tc::nanoseconds() - t0 < 50000000ull) {
         }
     }
-    if (CG == 2) tc::cluster_sync();
+    if (CG == 2 || FORM == kJoined) tc::cluster_sync();
     tc::fence_after();
     if (warp == 1) tc::tmem_free<CG>(tmem, kCols);
 }

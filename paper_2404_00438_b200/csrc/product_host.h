@@ -2,6 +2,7 @@
 #pragma once
 
 #include <algorithm>
+#include <atomic>
 
 #include "host_checks.h"
 #include "product.cuh"
@@ -51,6 +52,7 @@ struct Call {
 };
 
 // Device, SM count and the mark's address; the workspace's extent.
+bool device_of(Call& c);
 dlion_status begin(Call& c, void* workspace, uint64_t bytes, void* stream);
 
 // `a` itself if tiles of it can be copied in place, otherwise a packed copy in the workspace.
@@ -66,32 +68,47 @@ inline Matrix transposed(const Matrix& a) { return Matrix{a.p, a.cols, a.rows, a
 bool make_map(CUtensorMap* map, const Matrix& a, int* mn_major, int box_rows);
 
 struct Config {
-    int cg, bn, splits, split_slices;
+    int cg, bn, form, splits, split_slices;
 };
-Config choose(const Call& c, int64_t m, int64_t n, int64_t k, bool may_split);
+// `sums`: binary32 results, whose long sums are taken in segments.  `alone`: no splits (the epilogue needs whole rows of tiles).
+Config choose(const Call& c, int64_t m, int64_t n, int64_t k, bool sums, bool alone);
 
 // Tile counts of a configuration; false if the tiles cannot be numbered.
 bool shape_of(const Config& cfg, const Matrix& a, const Matrix& b, Shape* s);
 
-template <int CG, int BN, class E>
-void launch(Call& c, const CUtensorMap& ma, const CUtensorMap& mb, const Shape& s, const typename E::Args& f) {
-    auto* kernel = &product_kernel<CG, BN, E>;
-    c.check(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem));
-    const int64_t units = static_cast<int64_t>(s.tiles_m) * s.tiles_n * s.splits;
+// Every kernel of the library's layer calls goes out like this: it may be set up while its predecessor drains.
+template <class... P, class... A>
+void start(Call& c, void (*kernel)(P...), dim3 grid, dim3 block, size_t shared, int cluster, const A&... args) {
+    if (c.status != DLION_OK) return;
     cudaLaunchConfig_t cfg{};
-    cfg.gridDim = dim3(static_cast<unsigned>(std::min<int64_t>(units, c.sms / CG) * CG));
-    cfg.blockDim = dim3(kThreads);
-    cfg.dynamicSmemBytes = kSmem;
+    cfg.gridDim = grid;
+    cfg.blockDim = block;
+    cfg.dynamicSmemBytes = shared;
     cfg.stream = c.stream;
-    cudaLaunchAttribute at[1];
-    at[0].id = cudaLaunchAttributeClusterDimension;
-    at[0].val.clusterDim.x = CG;
-    at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
+    cudaLaunchAttribute at[2];
+    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[0].val.programmaticStreamSerializationAllowed = 1;
+    at[1].id = cudaLaunchAttributeClusterDimension;
+    at[1].val.clusterDim.x = static_cast<unsigned>(cluster);
+    at[1].val.clusterDim.y = at[1].val.clusterDim.z = 1;
     cfg.attrs = at;
-    cfg.numAttrs = CG == 2 ? 1 : 0;
-    if (c.status == DLION_OK) c.check(cudaLaunchKernelEx(&cfg, kernel, ma, mb, s, f, c.mark));
+    cfg.numAttrs = cluster > 1 ? 2 : 1;
+    c.check(cudaLaunchKernelEx(&cfg, kernel, static_cast<P>(args)...));
 }
 
+template <int CG, int BN, class E, int FORM>
+void launch(Call& c, const CUtensorMap& ma, const CUtensorMap& mb, const Shape& s, const typename E::Args& f) {
+    auto* kernel = &product_kernel<CG, BN, E, FORM>;
+    static std::atomic<uint64_t> ready{0};     // devices whose limit of shared memory has been raised for this kernel
+    const uint64_t bit = uint64_t{1} << (c.device & 63);
+    if ((ready.load(std::memory_order_relaxed) & bit) == 0) {
+        c.check(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem));
+        if (c.status == DLION_OK && c.device < 64) ready.fetch_or(bit, std::memory_order_relaxed);
+    }
+    const int64_t units = static_cast<int64_t>(s.tiles_m) * s.tiles_n * s.splits;
+    const int64_t blocks = FORM == kJoined ? units : std::min<int64_t>(units, c.sms / CG) * CG;
+    start(c, kernel, dim3(static_cast<unsigned>(blocks)), dim3(kThreads), kSmem, FORM == kJoined ? s.splits : CG, ma, mb, s, f, c.mark);
+}
 
 inline int64_t round_up(int64_t v, int64_t to) { return (v + to - 1) / to * to; }
 inline int64_t parts(int64_t v, int64_t of) { return (v + of - 1) / of; }
@@ -99,8 +116,7 @@ inline int64_t parts(int64_t v, int64_t of) { return (v + of - 1) / of; }
 template <class P, class F>
 uint64_t workspace_of(const P& p, F f) {
     Call c;
-    int dev = 0, sms = 0;
-    if (cudaGetDevice(&dev) == cudaSuccess && cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) == cudaSuccess) c.sms = sms;
+    device_of(c);                              // without a GPU the SM count of a B200 stands
     f(c, p);
     return std::max(c.ws.size, c.ws.used);
 }
