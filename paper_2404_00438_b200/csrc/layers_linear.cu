@@ -93,8 +93,14 @@ __global__ void __launch_bounds__(256) operand_kernel(const void* u, int64_t u_l
         float v[8];
         if (EIGHT) {
             const float s = block_scale(ex[lane / 4][r]);
+            float a[4], b[4];
+            restore4(q[i].x, s, a);
+            restore4(q[i].y, s, b);
 #pragma unroll
-            for (int j = 0; j < 8; ++j) v[j] = static_cast<float>(static_cast<int8_t>((j < 4 ? q[i].x : q[i].y) >> (8 * (j % 4)))) * s;
+            for (int j = 0; j < 4; ++j) {
+                v[j] = a[j];
+                v[j + 4] = b[j];
+            }
         } else {
             widen(w[i], v);
         }
@@ -131,20 +137,19 @@ __global__ void __launch_bounds__(256) checkpoint8_kernel(const __nv_bfloat16* x
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         const int r = warp + 8 * i;
-        uint32_t top = 0;
-        const uint32_t b[4] = {w[i].x, w[i].y, w[i].z, w[i].w};
-#pragma unroll
-        for (int j = 0; j < 4; ++j) top = max(top, max((b[j] << 16) & 0x7fffffffu, b[j] & 0x7fff0000u));
-        top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
-        top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
+        // bf16 sizes order as integers, NaN and infinity last: two at a time
+        const uint32_t mask = 0x7fff7fffu;
+        uint32_t two = __vmaxu2(__vmaxu2(w[i].x & mask, w[i].y & mask), __vmaxu2(w[i].z & mask, w[i].w & mask));
+        two = __vmaxu2(two, __shfl_xor_sync(0xffffffffu, two, 1));
+        two = __vmaxu2(two, __shfl_xor_sync(0xffffffffu, two, 2));
+        const uint32_t top = max(two << 16, two & 0xffff0000u);
         const uint32_t scale = block_exponent(top);
         const float inv = block_inverse(scale);
         if (lane % 4 == 0) ex[lane / 4][r] = static_cast<uint8_t>(scale);
         float v[8];
         widen(w[i], v);
-        uint32_t o[2] = {0, 0};
-#pragma unroll
-        for (int j = 0; j < 8; ++j) o[j / 4] |= (static_cast<uint32_t>(quantise8(v[j], inv)) & 255u) << (8 * (j % 4));
+        const uint32_t o[2] = {bytes4(quantise8(v[0], inv), quantise8(v[1], inv), quantise8(v[2], inv), quantise8(v[3], inv)),
+                               bytes4(quantise8(v[4], inv), quantise8(v[5], inv), quantise8(v[6], inv), quantise8(v[7], inv))};
         if (row0 + r >= m || valid == 0) continue;
         int8_t* p = q + (row0 + r) * q_ld + col;
         if (wide_out && valid == 8) {
@@ -160,72 +165,83 @@ __global__ void __launch_bounds__(256) checkpoint8_kernel(const __nv_bfloat16* x
     if (row0 + lane < m && col0 + warp * 32 < k) e[(col0 / 32 + warp) * e_ld + row0 + lane] = ex[warp][lane];
 }
 
-// Sums over rows in two steps, in a fixed order: a block has 256 columns and a run of rows.
-__global__ void __launch_bounds__(256) column_sums_kernel(const __nv_bfloat16* a, int64_t rs, int64_t cs, int64_t rows, int64_t cols,
-                                                          int64_t run, float* partial, int wide) {
-    __shared__ float sum[8][257];
+// Sums over rows: a cluster of eight blocks has 64 columns, each block an eighth of the rows; the first adds the
+// others' sums, in their order.  Bound by memory (8192 x 8192: 134 MB).
+constexpr int kSumBlocks = 8;
+
+__global__ void __cluster_dims__(kSumBlocks, 1, 1) __launch_bounds__(256)
+column_sums_kernel(const __nv_bfloat16* a, int64_t rs, int64_t cs, int64_t rows, int64_t cols, void* out, int f32, int wide) {
+    __shared__ float sum[32][65];
+    __shared__ __align__(16) float total[64];
+    const int lane = threadIdx.x % 8, line = threadIdx.x / 8;             // 32 lines of 8 x 8 columns
+    const uint32_t rank = tc::cluster_rank();
+    const int64_t c0 = static_cast<int64_t>(blockIdx.x / kSumBlocks) * 64 + lane * 8;
     tc::let_next_start();
     tc::wait_for_previous();
-    const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
-    const int64_t c0 = static_cast<int64_t>(blockIdx.x) * 256 + lane * 8;
-    const int64_t r0 = static_cast<int64_t>(blockIdx.y) * run, r1 = r0 + run < rows ? r0 + run : rows;
     float v[8] = {};
+    const int64_t first = static_cast<int64_t>(rank) * 32 + line;
     if (wide && c0 + 8 <= cols) {
-#pragma unroll 4
-        for (int64_t r = r0 + warp; r < r1; r += 8) {
-            const uint4 w = *reinterpret_cast<const uint4*>(a + r * rs + c0);
-            const uint32_t u[4] = {w.x, w.y, w.z, w.w};
+        const uint4* p = reinterpret_cast<const uint4*>(a + first * rs + c0);
+        const int64_t step = rs * (kSumBlocks * 32 / 8);
+        int64_t r = first;
+        for (; r + 7 * kSumBlocks * 32 < rows; r += 8 * kSumBlocks * 32, p += 8 * step) {
+            uint4 w[8];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                v[2 * i] += bf16_lo(u[i]);
-                v[2 * i + 1] += bf16_hi(u[i]);
-            }
-        }
-    } else {
-        for (int64_t r = r0 + warp; r < r1; r += 8) {
+            for (int i = 0; i < 8; ++i) w[i] = p[i * step];
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                if (c0 + i < cols) v[i] += __bfloat162float(a[r * rs + (c0 + i) * cs]);
+                float x[8];
+                widen(w[i], x);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) v[j] += x[j];
+            }
+        }
+        for (; r < rows; r += kSumBlocks * 32, p += step) {
+            float x[8];
+            widen(*p, x);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[j] += x[j];
+        }
+    } else {
+        for (int64_t r = first; r < rows; r += kSumBlocks * 32) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                if (c0 + j < cols) v[j] += __bfloat162float(a[r * rs + (c0 + j) * cs]);
             }
         }
     }
 #pragma unroll
-    for (int i = 0; i < 8; ++i) sum[warp][lane * 8 + i] = v[i];
+    for (int j = 0; j < 8; ++j) sum[line][lane * 8 + j] = v[j];
     __syncthreads();
-    const int64_t c = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;
-    if (c >= cols) return;
-    float t = 0.0f;
+    if (threadIdx.x < 64) {
+        float t = 0.0f;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) t += sum[i][threadIdx.x];
-    partial[blockIdx.y * cols + c] = t;
-}
-
-__global__ void __launch_bounds__(256) join_sums_kernel(const float* partial, int runs, int64_t cols, void* out, int f32) {
-    tc::let_next_start();
-    tc::wait_for_previous();
-    const int64_t c = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;
-    if (c >= cols) return;
-    float t = 0.0f;
-#pragma unroll 8
-    for (int i = 0; i < runs; ++i) t += partial[i * cols + c];
-    if (f32) {
-        static_cast<float*>(out)[c] = t;
-    } else {
-        static_cast<__nv_bfloat16*>(out)[c] = __float2bfloat16_rn(t);
+        for (int i = 0; i < 32; ++i) t += sum[i][threadIdx.x];
+        total[threadIdx.x] = t;
     }
+    tc::cluster_sync();
+    const int64_t c = static_cast<int64_t>(blockIdx.x / kSumBlocks) * 64 + threadIdx.x;
+    if (rank == 0 && threadIdx.x < 64 && c < cols) {
+        const uint32_t mine = tc::smem_addr(total + threadIdx.x);
+        float w[kSumBlocks], t = 0.0f;
+#pragma unroll
+        for (int i = 0; i < kSumBlocks; ++i) w[i] = tc::load_cluster(tc::map_to_rank(mine, i));
+#pragma unroll
+        for (int i = 0; i < kSumBlocks; ++i) t += w[i];
+        if (f32) {
+            static_cast<float*>(out)[c] = t;
+        } else {
+            static_cast<__nv_bfloat16*>(out)[c] = __float2bfloat16_rn(t);
+        }
+    }
+    tc::cluster_sync();                        // the sums stay until they are read
 }
 
 void column_sums(Call& c, const Matrix& a, void* out, int type) {
-    const int64_t strips = parts(a.cols, 256);
-    const int64_t runs = std::max<int64_t>(1, std::min<int64_t>(parts(4 * c.sms, strips), parts(a.rows, 64)));
-    const int64_t run = std::max<int64_t>(1, parts(a.rows, runs));
-    float* partial = c.ws.take<float>(static_cast<uint64_t>(runs) * a.cols);
     if (!c.live()) return;
     const int wide = a.cs == 1 && aligned16(a.p) && a.rs % 8 == 0;
-    start(c, column_sums_kernel, dim3(static_cast<unsigned>(strips), static_cast<unsigned>(runs)), dim3(256), 0, 1,
-          static_cast<const __nv_bfloat16*>(a.p), a.rs, a.cs, a.rows, a.cols, run, partial, wide);
-    start(c, join_sums_kernel, dim3(static_cast<unsigned>(strips)), dim3(256), 0, 1, partial, static_cast<int>(runs), a.cols, out,
-          type == DLION_GRAD_F32);
+    start(c, column_sums_kernel, dim3(static_cast<unsigned>(parts(a.cols, 64) * kSumBlocks)), dim3(256), 0, 1,
+          static_cast<const __nv_bfloat16*>(a.p), a.rs, a.cs, a.rows, a.cols, out, type == DLION_GRAD_F32, wide);
 }
 
 void operand(Call& c, const void* u, int64_t u_ld, const uint8_t* e, int64_t e_ld, int eight, int act, int64_t m, int64_t k,

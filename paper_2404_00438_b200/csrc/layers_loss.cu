@@ -25,6 +25,7 @@ struct LossTile {
     struct Args {
         int m, n;
         const int64_t* targets;
+        unsigned int* blocks_done;          // set to 0 for the kernel that follows
         float2* stats;                      // [group][m]: maximum, sum of exp(l - maximum)
         float* at_target;                   // [m]
         uint16_t* codes;                    // nullable: [m][ld]
@@ -33,6 +34,7 @@ struct LossTile {
 
     static __device__ __forceinline__ void tile(const Args& p, uint32_t acc, int row0, int col0, int width, int, bool live, uint4* stage, int lane) {
         if (row0 >= p.m || col0 >= p.n) return;
+        if (row0 == 0 && col0 == 0 && lane == 0) *p.blocks_done = 0;
         const int row = row0 + lane;
         const int valid = min(width, p.n - col0);
         const int rows = live ? min(32, p.m - row0) : 0;
@@ -92,26 +94,40 @@ __device__ __forceinline__ float block_sum(float v, float* shared) {       // 10
     return v;
 }
 
-// factor[0] = scale / (rows with a target)
+__device__ __forceinline__ int block_count(const int64_t* targets, int64_t m, int64_t ignore, int* shared) {      // 1024 threads
+    int n = 0;
+    for (int64_t i = threadIdx.x; i < m; i += 1024) n += targets[i] != ignore;
+    n = __reduce_add_sync(0xffffffffu, n);
+    if (threadIdx.x % 32 == 0) shared[threadIdx.x / 32] = n;
+    __syncthreads();
+    return __reduce_add_sync(0xffffffffu, shared[threadIdx.x % 32]);
+}
+
+// factor[0] = scale / (rows with a target), where it is needed before the first piece's rows are done
 __global__ void __launch_bounds__(1024) factor_kernel(const int64_t* targets, int64_t m, int64_t ignore, int mean, float scale, float* factor) {
     __shared__ int counts[32];
     tc::let_next_start();
     tc::wait_for_previous();
-    int n = 0;
-    for (int64_t i = threadIdx.x; i < m; i += 1024) n += targets[i] != ignore;
-    n = __reduce_add_sync(0xffffffffu, n);
-    if (threadIdx.x % 32 == 0) counts[threadIdx.x / 32] = n;
-    __syncthreads();
-    if (threadIdx.x != 0) return;
-    n = 0;
-    for (int i = 0; i < 32; ++i) n += counts[i];
-    factor[0] = mean && n > 0 ? scale / static_cast<float>(n) : scale;
+    const int n = block_count(targets, m, ignore, counts);
+    if (threadIdx.x == 0) factor[0] = mean && n > 0 ? scale / static_cast<float>(n) : scale;
 }
+
+// What the last block of a piece's rows does: the loss of all rows (after the last piece), in a fixed order, and the factor.
+struct Last {
+    unsigned int* blocks_done;             // 0 before the piece
+    const float* rows;                     // of all pieces
+    const int64_t* targets;
+    int64_t m;
+    int mean;
+    float scale;
+    float* loss;                           // nullable
+    float* factor;                         // nullable
+};
 
 // Joins the groups of 32 rows a block (lane = row, a warp every 32nd group): each row's maximum, the sum's logarithm in
 // octaves, and the loss.
 __global__ void __launch_bounds__(1024) rows_kernel(const float2* stats, int groups, int64_t m, const int64_t* targets, int64_t ignore,
-                                                    int64_t v, const float* at_target, float2* lse, float* rows) {
+                                                    int64_t v, const float* at_target, float2* lse, float* rows, const Last end) {
     __shared__ float2 part[32][33];
     tc::let_next_start();
     tc::wait_for_previous();
@@ -129,21 +145,44 @@ __global__ void __launch_bounds__(1024) rows_kernel(const float2* stats, int gro
     }
     part[warp][lane] = make_float2(top, sum);
     __syncthreads();
-    if (warp != 0 || row >= m) return;
-    for (int i = 0; i < 32; ++i) top = fmaxf(top, part[i][lane].x);
-    sum = 0.0f;
-    for (int i = 0; i < 32; ++i) {
-        const float2 s = part[i][lane];
-        if (s.x != -INFINITY) sum += s.y * exp2_fast((s.x - top) * kLog2e);     // a warp without a group has none
+    if (warp == 0 && row < m) {
+        for (int i = 0; i < 32; ++i) top = fmaxf(top, part[i][lane].x);
+        sum = 0.0f;
+        for (int i = 0; i < 32; ++i) {
+            const float2 s = part[i][lane];
+            if (s.x != -INFINITY) sum += s.y * exp2_fast((s.x - top) * kLog2e);     // a warp without a group has none
+        }
+        const float log_sum = logf(sum);
+        const int64_t t = targets[row];
+        float loss = (top - at_target[row]) + log_sum;
+        if (t < 0 || t >= v) loss = NAN;
+        if (t == ignore) loss = 0.0f;
+        rows[row] = loss;
+        lse[row] = make_float2(top, log_sum * kLog2e);
     }
-    const float log_sum = logf(sum);
-    const int64_t t = targets[row];
-    float loss = (top - at_target[row]) + log_sum;
-    if (t < 0 || t >= v) loss = NAN;
-    if (t == ignore) loss = 0.0f;
-    rows[row] = loss;
-    lse[row] = make_float2(top, log_sum * kLog2e);
+    if (end.loss == nullptr && end.factor == nullptr) return;
+    __shared__ unsigned int before;
+    __shared__ int counts[32];
+    __shared__ float sums[32];
+    __threadfence();
+    __syncthreads();
+    if (threadIdx.x == 0) before = atomicAdd(end.blocks_done, 1u);
+    __syncthreads();
+    if (before != gridDim.x - 1) return;
+    __threadfence();
+    const int n = block_count(end.targets, end.m, ignore, counts);
+    float total = 0.0f;
+    if (end.loss != nullptr) {
+        for (int64_t i = threadIdx.x; i < end.m; i += 1024) total += __ldcg(end.rows + i);
+        total = block_sum(total, sums);
+    }
+    if (threadIdx.x != 0) return;
+    if (end.loss != nullptr) end.loss[0] = end.mean && n > 0 ? total / static_cast<float>(n) : total;
+    if (end.factor != nullptr) end.factor[0] = end.mean && n > 0 ? end.scale / static_cast<float>(n) : end.scale;
 }
+
+// (conversions run at an eighth of the rate of additions)
+__device__ __forceinline__ float code_value(uint32_t c) { return __uint_as_float(0x4b000000u | c) - 8388608.0f; }
 
 // Codes to softmax - [target] in bf16, in place, eight a thread; a block has 2048 columns of a row.  The factor
 // g is left to the products' epilogues: rounded into d it would shift the whole gradient by its own rounding,
@@ -172,28 +211,13 @@ __global__ void __launch_bounds__(256) gradient_kernel(uint16_t* codes, int64_t 
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         const uint32_t ca = w[i] & 0xffffu, cb = w[i] >> 16;
-        float a = ca == 65535u && none ? 0.0f : exp2_fast(__fmaf_rn(static_cast<float>(ca), -1.0f / kStep, at));
-        float b = cb == 65535u && none ? 0.0f : exp2_fast(__fmaf_rn(static_cast<float>(cb), -1.0f / kStep, at));
+        float a = ca == 65535u && none ? 0.0f : exp2_fast(__fmaf_rn(code_value(ca), -1.0f / kStep, at));
+        float b = cb == 65535u && none ? 0.0f : exp2_fast(__fmaf_rn(code_value(cb), -1.0f / kStep, at));
         if (hit == 2 * i) a -= 1.0f;
         if (hit == 2 * i + 1) b -= 1.0f;
         o[i] = pack_bf16(a, b);
     }
     *p = make_uint4(o[0], o[1], o[2], o[3]);
-}
-
-// The rows' losses to the loss, in a fixed order.
-__global__ void __launch_bounds__(1024) loss_kernel(const float* rows, const int64_t* targets, int64_t m, int64_t ignore, int mean, float* loss) {
-    __shared__ float shared[32];
-    tc::let_next_start();
-    tc::wait_for_previous();
-    float v = 0.0f, n = 0.0f;               // a thread counts at most 2^20 rows: exact
-    for (int64_t i = threadIdx.x; i < m; i += 1024) {
-        v += rows[i];
-        n += targets[i] != ignore ? 1.0f : 0.0f;
-    }
-    v = block_sum(v, shared);
-    n = block_sum(n, shared);
-    if (threadIdx.x == 0) loss[0] = mean && n > 0.0f ? v / n : v;
 }
 
 dlion_status check_loss(const dlion_loss* p) {
@@ -234,9 +258,10 @@ void loss(Call& c, const dlion_loss& p) {
     float* at_target = c.ws.take<float>(step);
     float2* lse = c.ws.take<float2>(step);
     float* factor = c.ws.take<float>(1);
+    unsigned int* blocks_done = c.ws.take<unsigned int>(1);
     uint16_t* codes = grads ? c.ws.take<uint16_t>(static_cast<uint64_t>(step) * ld) : nullptr;
     float* sums = grads && !f32 && step < p.m ? c.ws.take<float>(static_cast<uint64_t>(p.v) * p.h) : nullptr;
-    if (grads && c.live()) {
+    if (grads && step < p.m && c.live()) {
         start(c, factor_kernel, dim3(1), dim3(1024), 0, 1, p.targets, p.m, p.ignore_index, p.mean, p.scale, factor);
     }
     for (int64_t r = 0; r < p.m; r += step) {
@@ -255,15 +280,19 @@ void loss(Call& c, const dlion_loss& p) {
                 c.status = DLION_ECUDA;
                 return;
             }
-            const LossTile::Args args{static_cast<int>(rows), static_cast<int>(p.v), p.targets + r, stats, at_target, codes, ld};
-            if (cfg.cg == 2) {
-                launch<2, 256, LossTile, kWhole>(c, ma, mb, s, args);
+            const LossTile::Args args{static_cast<int>(rows), static_cast<int>(p.v), p.targets + r, blocks_done, stats, at_target, codes, ld};
+            if (cfg.cg == 1) {
+                launch<1, 64, LossTile, kWhole>(c, ma, mb, s, args);
+            } else if (cfg.bn == 128) {
+                launch<2, 128, LossTile, kWhole>(c, ma, mb, s, args);
             } else {
-                launch<1, 128, LossTile, kWhole>(c, ma, mb, s, args);
+                launch<2, 256, LossTile, kWhole>(c, ma, mb, s, args);
             }
             if (c.status != DLION_OK) return;
+            const Last end{blocks_done, p.rows, p.targets, p.m, p.mean, p.scale, r + rows >= p.m ? p.loss : nullptr,
+                           grads && step >= p.m ? factor : nullptr};
             start(c, rows_kernel, dim3(static_cast<unsigned>(parts(rows, 32))), dim3(1024), 0, 1, stats, groups, rows, p.targets + r,
-                  p.ignore_index, p.v, at_target, lse, p.rows + r);
+                  p.ignore_index, p.v, at_target, lse, p.rows + r, end);
             if (grads) {
                 const dim3 grid(static_cast<unsigned>(parts(p.v, 2048)), static_cast<unsigned>(std::min<int64_t>(rows, 65535)),
                                 static_cast<unsigned>(parts(rows, 65535)));
@@ -290,9 +319,6 @@ void loss(Call& c, const dlion_loss& p) {
         fw.out_ld = last ? p.dw_ld : so_far_ld;
         fw.out_f32 = f32 || !last;
         product(c, transposed(d), transposed(xp), fw);
-    }
-    if (c.live()) {
-        start(c, loss_kernel, dim3(1), dim3(1024), 0, 1, p.rows, p.targets, p.m, p.ignore_index, p.mean, p.loss);
     }
 }
 

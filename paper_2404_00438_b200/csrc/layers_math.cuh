@@ -26,24 +26,28 @@ __device__ __forceinline__ float recip_fast(float x) {      // 1 ulp
     return y;
 }
 
-__device__ __forceinline__ float logistic(float t) { return recip_fast(1.0f + exp2_fast(-kLog2e * t)); }
+// 1 / (1 + 2^t)
+__device__ __forceinline__ float logistic2(float t) { return recip_fast(1.0f + exp2_fast(t)); }
 
-// Beyond 64 the gelu argument only saturates the logistic; held there, its square cannot overflow.
-__device__ __forceinline__ float gelu_arg(float z) { return fabsf(z) > 64.0f ? copysignf(64.0f, z) : z; }
+// Beyond 64 the gelu argument only saturates the logistic; held there, its square cannot overflow.  (A NaN is lost here and
+// comes back with the factor z.)
+__device__ __forceinline__ float held(float z, float most) { return fminf(fmaxf(z, -most), most); }
 
+// half of 1 + tanh(u) is the logistic function of 2u = kGelu2c z (1 + 0.044715 z^2), so every activation costs one ex2 and
+// one rcp; -log2(e) is folded into the polynomial.
 constexpr float kGelu2c = 1.5957691216057308f;              // 2 sqrt(2/pi)
+constexpr float kGeluA = -kGelu2c * kLog2e, kGeluB = kGeluA * 0.044715f;
 
-// half of 1 + tanh(u) is the logistic function of 2u, so every activation costs one ex2 and one rcp.
 // The kind is a template parameter: chosen element by element it would keep the elements of a thread from
 // overlapping, and a product's epilogue is bound by that latency (the 8192 x 2048 x 8192 product with gelu and
 // 8-bit z: 335 us so, 236 us with the choice made once for 32 elements).
 template <int ACT>
 __device__ __forceinline__ float act_value(float z) {
     if (ACT == DLION_ACT_RELU) return z < 0.0f ? 0.0f : z;  // NaN stays
-    if (ACT == DLION_ACT_SILU) return z * logistic(z);
+    if (ACT == DLION_ACT_SILU) return z * logistic2(-kLog2e * z);
     if (ACT == DLION_ACT_GELU) {
-        const float c = gelu_arg(z);
-        return z * logistic(kGelu2c * c * __fmaf_rn(0.044715f * c, c, 1.0f));
+        const float c = held(z, 64.0f);
+        return z * logistic2(c * __fmaf_rn(kGeluB, c * c, kGeluA));
     }
     return z;
 }
@@ -52,14 +56,13 @@ template <int ACT>
 __device__ __forceinline__ float act_slope(float z) {
     if (ACT == DLION_ACT_RELU) return z > 0.0f ? 1.0f : (z == z ? 0.0f : z);
     if (ACT == DLION_ACT_SILU) {
-        const float p = logistic(z);
-        const float c = fabsf(z) > 128.0f ? copysignf(128.0f, z) : z;   // p (1 - p) is 0 there
-        return __fmaf_rn(c * p, 1.0f - p, p);
+        const float p = logistic2(-kLog2e * z);
+        return __fmaf_rn(z * p, 1.0f - p, p);
     }
     if (ACT == DLION_ACT_GELU) {
-        const float c = gelu_arg(z), c2 = c * c;
-        const float p = logistic(kGelu2c * c * __fmaf_rn(0.044715f, c2, 1.0f));
-        return __fmaf_rn(c * kGelu2c * __fmaf_rn(0.134145f, c2, 1.0f), p * (1.0f - p), p);
+        const float c = held(z, 64.0f), c2 = c * c;
+        const float p = logistic2(c * __fmaf_rn(kGeluB, c2, kGeluA));
+        return __fmaf_rn(z * __fmaf_rn(0.134145f * kGelu2c, c2, kGelu2c), __fmaf_rn(-p, p, p), p);
     }
     return 1.0f;
 }
@@ -92,8 +95,31 @@ __device__ __forceinline__ float block_scale(uint32_t e) { return __uint_as_floa
 // 1 / 2^(e-127), exact (e is in [1, 249] or marks a non-finite block, whose q is 0)
 __device__ __forceinline__ float block_inverse(uint32_t e) { return e == 255u ? 0.0f : __uint_as_float((254u - e) << 23); }
 
-__device__ __forceinline__ int quantise8(float v, float inverse) {
-    return __float2int_rn(v * inverse);                     // a non-finite v gives NaN * 0 -> 0, or inf * 0 -> 0
+// Conversions between integers and floats run at an eighth of the rate of additions, so the integer is read off, or put
+// into, the low bits of 1.5 * 2^23 (or 2^23) plus itself.
+
+// v / 2^(e-127) to the nearest integer, in the low 8 bits
+__device__ __forceinline__ uint32_t quantise8(float v, float inverse) { return __float_as_uint(__fmaf_rn(v, inverse, 12582912.0f)); }
+
+// bytes 0 of four words
+__device__ __forceinline__ uint32_t bytes4(uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
+    return __byte_perm(__byte_perm(a, b, 0x0040), __byte_perm(c, d, 0x0040), 0x5410);
+}
+
+// The signed bytes of a word, times 2^(e-127).
+__device__ __forceinline__ void restore4(uint32_t w, float scale, float (&v)[4]) {
+    w ^= 0x80808080u;                                       // q + 128
+    v[0] = (__uint_as_float(__byte_perm(w, 0x4b000000u, 0x7440)) - 8388736.0f) * scale;
+    v[1] = (__uint_as_float(__byte_perm(w, 0x4b000000u, 0x7441)) - 8388736.0f) * scale;
+    v[2] = (__uint_as_float(__byte_perm(w, 0x4b000000u, 0x7442)) - 8388736.0f) * scale;
+    v[3] = (__uint_as_float(__byte_perm(w, 0x4b000000u, 0x7443)) - 8388736.0f) * scale;
+}
+
+// the larger size, NaN if either is
+__device__ __forceinline__ float larger(float top, float v) {
+    float r;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(top), "f"(fabsf(v)));
+    return r;
 }
 
 __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {

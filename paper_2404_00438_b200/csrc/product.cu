@@ -104,27 +104,25 @@ __global__ void __launch_bounds__(256) pack_kernel(const uint16_t* a, int64_t rs
 
 }  // namespace
 
-// The division of the work with the least estimated time, in clocks of an SM: rounds of tiles, each of so many
-// slices and an epilogue that the next tile hides.
-//   pair        540 a slice (512 the tensor cores' own), splits summed by a second kernel at the L2's rate;
-//   block       560 a slice: its 32 KB come at the 57 bytes a clock that one SM gets from L2, measured on
-//               197 x 768 x 768, where 12 slices took 6850;
-//   joined      the same with fewer slices each, and the exchange.
+// The division of the work with the least estimated time, in clocks of an SM: rounds of tiles, each of so many slices
+// and an epilogue that the next tile hides.  A slice takes 540 (its 32 KB at 57 bytes a clock, or the tensor cores' 512)
+// in a pair's 256 x 256 tile and 420 (24 KB) in the others; splits of pairs are summed by a second kernel at the
+// L2's rate; joined blocks exchange their sums in about 3000.
 Config choose(const Call& c, int64_t m, int64_t n, int64_t k, bool sums, bool alone) {
     const int64_t slices = std::max<int64_t>(1, parts(k, kSlice));
     const bool long_sums = sums && slices > kSegment;
     Config best{2, 256, kWhole, 1, static_cast<int>(slices)};
     double least = 1e300;
-    auto consider = [&](int cg, int bn, int form, int64_t s, double slice, double fixed) {
+    auto consider = [&](int cg, int bn, int form, int64_t s, double slice, double piece) {
         const int64_t per = parts(slices, s);
         if (parts(slices, per) != s) return;
         const int64_t tm = parts(m, 128 * cg), tn = parts(n, bn);
         double t;
         if (form == kJoined) {
             if (tm * tn * s > 16 * 8) return;  // clusters of eight: sixteen at a time for certain
-            t = per * slice + fixed + 3000.0;
+            t = per * slice + 3000.0 + piece;
         } else {
-            t = static_cast<double>(parts(tm * tn * s, c.sms / cg)) * (per * slice + 600.0) + fixed;
+            t = static_cast<double>(parts(tm * tn * s, c.sms / cg)) * (per * slice + 500.0) + piece;
             if (s > 1) t += 6000.0 + static_cast<double>(s) * tm * tn * cg * bn * 128 * 8.0 / 3000.0;
         }
         if (t < least) {
@@ -135,15 +133,16 @@ Config choose(const Call& c, int64_t m, int64_t n, int64_t k, bool sums, bool al
     const int64_t most = alone ? 1 : std::min<int64_t>(32, std::max<int64_t>(1, slices / 8));
     for (int64_t s = 1; s <= most; ++s) {
         if (long_sums) {
-            consider(2, 128, kLong, s, 330.0, 5000.0);
+            consider(2, 128, kLong, s, 420.0, 2000.0);
         } else {
-            consider(2, 256, kWhole, s, 540.0, 5000.0);
+            consider(2, 256, kWhole, s, 540.0, 4000.0);
+            if (s == 1) consider(2, 128, kWhole, s, 420.0, 2000.0);
         }
     }
-    if (!long_sums) consider(1, 128, kWhole, 1, 560.0, 4500.0);
+    if (!long_sums) consider(1, 64, kWhole, 1, 420.0, 1000.0);
     for (int64_t s = 2; !alone && s <= 8; s *= 2) {
         if (sums && parts(slices, s) > kSegment) continue;
-        consider(1, 128, kJoined, s, 560.0, 4500.0);
+        consider(1, 64, kJoined, s, 420.0, 1000.0);
     }
     return best;
 }
@@ -263,11 +262,13 @@ void product(Call& c, const Matrix& a, const Matrix& b, Finish f) {
         if (cfg.form == kLong) {
             launch<2, 128, General, kLong>(c, ma, mb, s, f);
         } else if (cfg.form == kJoined) {
-            launch<1, 128, General, kJoined>(c, ma, mb, s, f);
-        } else if (cfg.cg == 2) {
-            launch<2, 256, General, kWhole>(c, ma, mb, s, f);
+            launch<1, 64, General, kJoined>(c, ma, mb, s, f);
+        } else if (cfg.cg == 1) {
+            launch<1, 64, General, kWhole>(c, ma, mb, s, f);
+        } else if (cfg.bn == 128) {
+            launch<2, 128, General, kWhole>(c, ma, mb, s, f);
         } else {
-            launch<1, 128, General, kWhole>(c, ma, mb, s, f);
+            launch<2, 256, General, kWhole>(c, ma, mb, s, f);
         }
         if (partial) {
             const int64_t warps = static_cast<int64_t>(f.m) * parts(f.n, 32);

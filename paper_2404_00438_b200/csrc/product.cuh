@@ -6,13 +6,14 @@
 // A kernel's code is not in the instruction cache when it starts, and an epilogue met cold took 3500 clocks for 64
 // columns; so while the first slices are on their way the epilogue warps run it once on nothing (`live` false: no rows).
 // Three forms of the same kernel: kWhole (above); kJoined, where the blocks of a cluster each take a share of k of
-// one 128 x 128 tile and send each other their sums, every block adding a share of the tile, for products with fewer tiles than SMs;
+// one 128 x 64 tile and send each other their sums, every block adding a share of the tile, for products with fewer tiles than SMs;
 // kLong, for binary32 results of long sums: the tensor core's accumulator drops what does not fit, which after K
 // products shifts a sum by about K 2^-30 of itself, so it only adds kSegment of them and the epilogue
 // adds the segments in registers, rounding to nearest.
-// A pair computes 256 x 256 with each block holding half of A and half of B, so a block reads 32 KB of
-// shared memory for 128 x 256 x 64 products, where a single block's 128 x 128 tile reads the same 32 KB for
-// half of that: the pair is what large shapes use, the single block what small ones use.
+// A pair computes 256 x BN with each block holding half of A and half of B.  An SM takes in 57 bytes a clock (measured:
+// 12 slices of a lone block's 128 x 128 tile, 393 KB, in 6850 clocks), so what a tile reads for its products decides: a pair's 256 x 256
+// needs 32 KB a block for 512 clocks of products, its 256 x 128 and a lone block's 128 x 64 24 KB for 256 and 128.  Large shapes
+// use the first, middling ones the second, those with few tiles the third.
 #pragma once
 
 #include "layers_math.cuh"
@@ -25,12 +26,11 @@ enum Form { kWhole = 0, kJoined = 1, kLong = 2 };
 
 constexpr int kSegment = 16;               // slices
 constexpr int kSlice = 64;                 // values of k per stage: one 128-byte swizzled row
-constexpr int kStages = 6;
-constexpr int kStageBytes = 32768;         // A: 128 rows, B: 128 rows (of each block)
+constexpr int kRingBytes = 196608;         // six stages of 32 KB or eight of 24 KB
 constexpr int kThreads = 384;
 constexpr int kEpilogueWarps = 8;
 constexpr int kStaging = 4096;             // bytes of shared memory per epilogue warp
-constexpr int kSmem = kStages * kStageBytes + kEpilogueWarps * kStaging + 1024 + 256;
+constexpr int kSmem = kRingBytes + kEpilogueWarps * kStaging + 1024 + 256;
 
 struct Shape {
     int m, n, k;
@@ -221,22 +221,19 @@ __device__ __forceinline__ void to_bf16(const T (&v)[32], uint32_t (&w)[16]) {
 
 __device__ __forceinline__ void keep8(const Finish& f, const Piece& pc, const float (&v)[32]) {
     const int row = pc.row0 + pc.lane;
-    uint32_t top = 0;
+    float top = 0.0f;
 #pragma unroll
     for (int j = 0; j < 32; ++j) {
-        const uint32_t a = __float_as_uint(v[j]) & 0x7fffffffu;
-        top = (j < pc.cols && a > top) ? a : top;
+        if (j < pc.cols) top = larger(top, v[j]);
     }
-    const uint32_t e = block_exponent(top);
+    const uint32_t e = block_exponent(__float_as_uint(top));
     const float inv = block_inverse(e);
     if (pc.lane >= pc.rows) return;
     f.kept_e[static_cast<int64_t>(pc.col0 / 32) * f.kept_e_ld + row] = static_cast<uint8_t>(e);
     uint32_t w[8];
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-        w[j] = 0;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) w[j] |= (static_cast<uint32_t>(quantise8(v[4 * j + i], inv)) & 255u) << (8 * i);
+        w[j] = bytes4(quantise8(v[4 * j], inv), quantise8(v[4 * j + 1], inv), quantise8(v[4 * j + 2], inv), quantise8(v[4 * j + 3], inv));
     }
     int8_t* q = static_cast<int8_t*>(f.kept) + static_cast<int64_t>(row) * f.kept_ld + pc.col0;
     if (pc.cols == 32 && on_grid(f.kept, f.kept_ld, 1)) {
@@ -271,9 +268,11 @@ __device__ __forceinline__ void times_slope8(const Finish& f, const Piece& pc, f
     }
     with_act(f.slope, [&](auto kind) {
 #pragma unroll
-        for (int j = 0; j < 32; ++j) {
-            const float u = static_cast<float>(static_cast<int8_t>(w[j / 4] >> (8 * (j % 4)))) * s;
-            v[j] *= act_slope<decltype(kind)::value>(u);
+        for (int j = 0; j < 8; ++j) {
+            float u[4];
+            restore4(w[j], s, u);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) v[4 * j + i] *= act_slope<decltype(kind)::value>(u[i]);
         }
     });
 }
@@ -379,19 +378,20 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
     constexpr int kM = 128 * CG;               // rows of the tile; a block has 128 of them
     constexpr int kBRows = BN / CG;            // of B, in this block
     constexpr uint32_t kCols = 2 * BN;         // tensor memory columns
-    static_assert(16384 + kBRows * 128 <= kStageBytes, "stage");
-    static_assert(FORM != kJoined || (CG == 1 && BN == 128), "joined tiles are a block's own");
-    constexpr uint32_t kBytes = CG * (16384 + kBRows * 128);
+    static_assert(FORM != kJoined || CG == 1, "joined tiles are a block's own");
+    constexpr int kStageBytes = 16384 + kBRows * 128;
+    constexpr uint32_t kBytes = CG * kStageBytes;
 
     extern __shared__ uint8_t raw[];
     const uint32_t base = (tc::smem_addr(raw) + 1023u) & ~1023u;
     uint8_t* mem = raw + (base - tc::smem_addr(raw));
-    const uint32_t bars = base + kStages * kStageBytes + kEpilogueWarps * kStaging;
-    constexpr int kRing = FORM == kJoined ? 4 : kStages;
-    constexpr uint32_t kPiece = 4096, kPieces = 16;                    // kJoined: 32 x 32 sums, behind a shorter ring
-    const uint32_t landing = base + 4 * kStageBytes, landed = bars + 16 * kStages + 40;
-    const uint32_t full = bars, empty = bars + 8 * kStages, ready = bars + 16 * kStages, drained = ready + 16;
-    const uint32_t slot = drained + 16;
+    const uint32_t bars = base + kRingBytes + kEpilogueWarps * kStaging;
+    constexpr uint32_t kPiece = 4096, kPieces = 4 * (BN / 32);         // kJoined: 32 x 32 sums land behind a shorter ring
+    constexpr uint32_t kLanding = FORM == kJoined ? kPieces * kPiece : 0;
+    constexpr int kRing = (kRingBytes - kLanding) / kStageBytes;
+    static_assert(kRing <= 8 && (FORM != kJoined || kLanding <= 2 * kStageBytes), "barriers; the ring holds what is sent");
+    const uint32_t landing = base + kRingBytes - kLanding;
+    const uint32_t full = bars, empty = bars + 64, ready = bars + 128, drained = bars + 144, slot = bars + 160, landed = bars + 168;
     volatile uint32_t* slot_mem = reinterpret_cast<volatile uint32_t*>(mem + (slot - base));
 
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
@@ -404,7 +404,7 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
 
     tc::let_next_start();
     if (threadIdx.x == 0) {
-        for (int i = 0; i < kStages; ++i) {
+        for (int i = 0; i < kRing; ++i) {
             tc::bar_init(full + 8 * i, 1);
             tc::bar_init(empty + 8 * i, 1);
         }
@@ -494,7 +494,7 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
         }
     } else if (warp >= 4) {
         const int quarter = warp % 4, half = (warp - 4) / 4;
-        uint4* stage = reinterpret_cast<uint4*>(mem + kStages * kStageBytes + (warp - 4) * kStaging);
+        uint4* stage = reinterpret_cast<uint4*>(mem + kRingBytes + (warp - 4) * kStaging);
         const uint32_t lead_drained = CG == 2 ? tc::map_to_rank(drained, 0) : drained;
         const uint32_t part = tmem + half * (BN / 2) + (static_cast<uint32_t>(quarter * 32) << 16);
         auto drain = [&](int set) {
@@ -560,7 +560,7 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
                     if (!(fine = tc::bar_wait(landed, 0))) break;
                 }
                 for (int p = share + s.splits * (warp - 4); p < static_cast<int>(kPieces); p += s.splits * kEpilogueWarps) {
-                    const float4* from = reinterpret_cast<const float4*>(mem + 4 * kStageBytes + (p / s.splits) * s.splits * kPiece);
+                    const float4* from = reinterpret_cast<const float4*>(mem + kRingBytes - kLanding + (p / s.splits) * s.splits * kPiece);
                     float v[32] = {};
                     for (int r = 0; r < s.splits; ++r, from += kPiece / 16) {
 #pragma unroll

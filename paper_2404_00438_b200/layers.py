@@ -18,6 +18,8 @@ from typing import NamedTuple, Optional, Tuple, Union
 
 import torch
 
+from torch.cuda import current_device as _current_device
+
 from . import dlion as _dlion
 from .dlion import DlionError, GRAD_BF16, GRAD_F32, OK
 
@@ -73,6 +75,9 @@ def _bind(lib):
 
 _lib = _bind(_dlion.lib())
 
+# the current stream's handle without the Stream object around it, where torch offers that
+_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda device: torch.cuda.current_stream(device).cuda_stream)
+
 
 class Checkpoint8(NamedTuple):
     """A matrix in 8 bits: value = q * 2^(e - 127), ``e`` shared by 32 values of a row ([ceil(k/32), m])."""
@@ -90,40 +95,42 @@ class Loss(NamedTuple):
 def _device(t, name: str) -> int:
     if not isinstance(t, torch.Tensor):
         raise ValueError(f"{name}: expected a torch.Tensor, got {type(t).__name__}")
-    if not t.is_cuda:
-        raise ValueError(f"{name}: must be a CUDA tensor (the library has no CPU path)")
     index = t.get_device()
-    if index != torch.cuda.current_device():
-        raise ValueError(f"{name}: is on cuda:{index}, the current device is cuda:{torch.cuda.current_device()}")
+    if index < 0:
+        raise ValueError(f"{name}: must be a CUDA tensor (the library has no CPU path)")
+    if index != _current_device():
+        raise ValueError(f"{name}: is on cuda:{index}, the current device is cuda:{_current_device()}")
     return index
 
 
-def _matrix(t, name: str, device: int, dtypes, rows: int, cols: int, adjacent: bool = False) -> None:
-    """Raises unless ``t`` is a [rows, cols] tensor of one of ``dtypes`` on ``device`` (``adjacent``:
-    with adjacent columns and rows that do not overlap)."""
-    if not isinstance(t, torch.Tensor):
-        raise ValueError(f"{name}: expected a torch.Tensor, got {type(t).__name__}")
-    if t.get_device() != device:
-        raise ValueError(f"{name}: is on {t.device}, the call is on cuda:{device}")
-    if t.dtype not in dtypes:
-        raise ValueError(f"{name}: dtype {t.dtype}, expected one of {tuple(dtypes)}")
-    if tuple(t.shape) != (rows, cols):
-        raise ValueError(f"{name}: shape {tuple(t.shape)}, expected {(rows, cols)}")
-    if adjacent:
+# The checks run on every call, and a small product takes a few microseconds: each is one expression while all is well,
+# and _refused finds the words.
+def _matrix(t, name: str, device: int, dtypes, shape, adjacent: bool = False) -> None:
+    """Raises unless ``t`` is a tensor of ``shape`` and of one of ``dtypes`` on ``device`` (``adjacent``: with
+    adjacent columns and rows that do not overlap)."""
+    if not (isinstance(t, torch.Tensor) and t.dtype in dtypes and t.shape == shape and t.get_device() == device):
+        _refused(t, name, device, dtypes, shape)
+    if adjacent and not t.is_contiguous():
         rs, cs = t.stride()
-        if (cs != 1 and cols != 1) or (rows > 1 and rs < cols):
+        if (cs != 1 and shape[1] != 1) or (shape[0] > 1 and rs < shape[1]):
             raise ValueError(f"{name}: needs adjacent columns (got strides {(rs, cs)})")
 
 
 def _vector(t, name: str, device: int, dtypes, n: int) -> None:
+    if not (isinstance(t, torch.Tensor) and t.dtype in dtypes and t.shape == (n,) and t.get_device() == device):
+        _refused(t, name, device, dtypes, (n,))
+    if not t.is_contiguous():
+        raise ValueError(f"{name}: expected {n} adjacent values, got strides {t.stride()}")
+
+
+def _refused(t, name: str, device: int, dtypes, shape) -> None:
     if not isinstance(t, torch.Tensor):
         raise ValueError(f"{name}: expected a torch.Tensor, got {type(t).__name__}")
     if t.get_device() != device:
         raise ValueError(f"{name}: is on {t.device}, the call is on cuda:{device}")
     if t.dtype not in dtypes:
         raise ValueError(f"{name}: dtype {t.dtype}, expected one of {tuple(dtypes)}")
-    if t.dim() != 1 or t.shape[0] != n or (n > 1 and t.stride(0) != 1):
-        raise ValueError(f"{name}: expected {n} adjacent values, got shape {tuple(t.shape)}, strides {t.stride()}")
+    raise ValueError(f"{name}: shape {tuple(t.shape)}, expected {tuple(shape)}")
 
 
 def _two_dim(t, name: str) -> Tuple[int, int]:
@@ -143,18 +150,17 @@ def _grad_type(dtype) -> int:
     return _enumerator(_TYPES, dtype, "grad_dtype")
 
 
-def _call(name: str, args, device: int, workspace: Optional[torch.Tensor]) -> None:
+def _call(size, call, args, device: int, workspace: Optional[torch.Tensor]) -> None:
     ref = ctypes.byref(args)
-    need = getattr(_lib, name + "_workspace")(ref)
+    need = size(ref)
     if workspace is None:
         if need:
             workspace = torch.empty(need, dtype=torch.uint8, device=device)
     else:
         _dlion.check_tensor(workspace, "workspace", (torch.uint8,), need, device)
-    st = getattr(_lib, name)(ref, workspace.data_ptr() if workspace is not None and need else None, need,
-                             torch.cuda.current_stream(device).cuda_stream)
+    st = call(ref, workspace.data_ptr() if need else None, need, _stream(device))
     if st != OK:
-        raise DlionError(st, name)
+        raise DlionError(st, call.__name__)
 
 
 def _ptr(t: Optional[torch.Tensor]) -> Optional[int]:
@@ -171,30 +177,33 @@ def linear_forward(x: torch.Tensor, w: torch.Tensor, bias: Optional[torch.Tensor
     device = _device(x, "x")
     m, k = _two_dim(x, "x")
     n = _two_dim(w, "w")[1]
-    _matrix(x, "x", device, (_BF16,), m, k)
-    _matrix(w, "w", device, (_BF16,), k, n)
+    _matrix(x, "x", device, (_BF16,), (m, k))
+    _matrix(w, "w", device, (_BF16,), (k, n))
     if bias is not None:
         _vector(bias, "bias", device, _TYPES, n)
     if residual is not None:
-        _matrix(residual, "residual", device, (_BF16,), m, n, True)
+        _matrix(residual, "residual", device, (_BF16,), (m, n), True)
     a, how = _enumerator(ACTS, act, "act"), _enumerator(KEEPS, keep, "keep")
     if out is None:
-        out = torch.empty((m, n), dtype=out_dtype, device=device)
-    _matrix(out, "out", device, _TYPES, m, n, True)
+        if out_dtype not in _TYPES:
+            raise ValueError(f"out_dtype: {out_dtype}, expected one of {tuple(_TYPES)}")
+        out = x.new_empty((m, n)) if out_dtype is _BF16 else x.new_empty((m, n), dtype=out_dtype)
+    else:
+        _matrix(out, "out", device, _TYPES, (m, n), True)
     kept = None
     q = e = None
     if how == KEEP_8BIT:
-        kept = Checkpoint8(torch.empty((m, n), dtype=torch.int8, device=device),
-                           torch.empty((-(-n // BLOCK8), m), dtype=torch.uint8, device=device))
+        kept = Checkpoint8(x.new_empty((m, n), dtype=torch.int8),
+                           x.new_empty((-(-n // BLOCK8), m), dtype=torch.uint8))
         q, e = kept
     elif how == KEEP_BF16:
-        q = kept = torch.empty((m, n), dtype=_BF16, device=device)
+        q = kept = x.new_empty((m, n))
     xs, ws = x.stride(), w.stride()
     args = _Forward(m, k, n, x.data_ptr(), xs[0], xs[1], w.data_ptr(), ws[0], ws[1], _ptr(bias),
                     0 if bias is None else _TYPES[bias.dtype], a, _ptr(residual),
                     0 if residual is None else residual.stride(0), out.data_ptr(), out.stride(0), _TYPES[out.dtype],
                     how, _ptr(q), n, _ptr(e), m)
-    _call("dlion_linear_forward", args, device, workspace)
+    _call(_lib.dlion_linear_forward_workspace, _lib.dlion_linear_forward, args, device, workspace)
     return out if kept is None else (out, kept)
 
 
@@ -210,8 +219,8 @@ def linear_backward(dy: torch.Tensor, w: torch.Tensor, saved: Union[torch.Tensor
     device = _device(dy, "dy")
     m, n = _two_dim(dy, "dy")
     k = _two_dim(w, "w")[0]
-    _matrix(dy, "dy", device, (_BF16,), m, n)
-    _matrix(w, "w", device, (_BF16,), k, n)
+    _matrix(dy, "dy", device, (_BF16,), (m, n))
+    _matrix(w, "w", device, (_BF16,), (k, n))
     a = _enumerator(ACTS, act, "act")
     u = e = None
     u_ld = e_ld = 0
@@ -223,55 +232,61 @@ def linear_backward(dy: torch.Tensor, w: torch.Tensor, saved: Union[torch.Tensor
         u_ld, e_ld = u.stride(0), e.stride(0)
     elif saved is not None:
         u = saved
-        _matrix(u, "saved", device, (_BF16,), m, k, True)
+        _matrix(u, "saved", device, (_BF16,), (m, k), True)
         u_ld = u.stride(0)
     elif need_dw or (need_dx and a):
         raise ValueError("saved: needed for dw, and for dx behind an activation")
     if residual is not None:
-        _matrix(residual, "residual", device, (_BF16,), m, k, True)
-    if need_dx and dx is None:
-        dx = torch.empty((m, k), dtype=_BF16, device=device)
+        _matrix(residual, "residual", device, (_BF16,), (m, k), True)
     g = _grad_type(grad_dtype)
-    if need_dw and dw is None:
-        ordered = w.stride(0) >= w.stride(1)
-        dw = torch.empty((k, n) if ordered else (n, k), dtype=grad_dtype, device=device)
-        dw = dw if ordered else dw.t()
-    if need_db and db is None:
-        db = torch.empty((n,), dtype=grad_dtype, device=device)
-    dx, dw, db = dx if need_dx else None, dw if need_dw else None, db if need_db else None
-    if dx is not None:
-        _matrix(dx, "dx", device, (_BF16,), m, k, True)
-    if dw is not None:
-        _matrix(dw, "dw", device, (grad_dtype,), k, n)
-        rs, cs = dw.stride()
-        if not ((cs == 1 and (k == 1 or rs >= n)) or (rs == 1 and (n == 1 or cs >= k))):
-            raise ValueError(f"dw: needs adjacent rows or columns (got strides {(rs, cs)})")
-    if db is not None:
+    ys, ws, gs = dy.stride(), w.stride(), (0, 0)
+    if not need_dx:
+        dx = None
+    elif dx is None:
+        dx = dy.new_empty((m, k))
+    else:
+        _matrix(dx, "dx", device, (_BF16,), (m, k), True)
+    if not need_dw:
+        dw = None
+    elif dw is None:
+        if ws[0] >= ws[1]:
+            dw, gs = dy.new_empty((k, n), dtype=grad_dtype), (n, 1)
+        else:
+            dw, gs = dy.new_empty((n, k), dtype=grad_dtype).t(), (1, k)
+    else:
+        _matrix(dw, "dw", device, (grad_dtype,), (k, n))
+        gs = dw.stride()
+        if not ((gs[1] == 1 and (k == 1 or gs[0] >= n)) or (gs[0] == 1 and (n == 1 or gs[1] >= k))):
+            raise ValueError(f"dw: needs adjacent rows or columns (got strides {gs})")
+    if not need_db:
+        db = None
+    elif db is None:
+        db = dy.new_empty((n,), dtype=grad_dtype)
+    else:
         _vector(db, "db", device, (grad_dtype,), n)
-    ys, ws, gs = dy.stride(), w.stride(), (0, 0) if dw is None else dw.stride()
     args = _Backward(m, k, n, dy.data_ptr(), ys[0], ys[1], w.data_ptr(), ws[0], ws[1], a, how, _ptr(u), u_ld, _ptr(e), e_ld,
                      _ptr(residual), 0 if residual is None else residual.stride(0), _ptr(dx),
                      0 if dx is None else dx.stride(0), _ptr(dw), gs[0], gs[1], _ptr(db), g)
-    _call("dlion_linear_backward", args, device, workspace)
+    _call(_lib.dlion_linear_backward_workspace, _lib.dlion_linear_backward, args, device, workspace)
     return dx, dw, db
 
 
 def _checkpoint(c: Checkpoint8, name: str, device: int, m: int, k: int) -> None:
-    _matrix(c.q, f"{name}.q", device, (torch.int8,), m, k, True)
-    _matrix(c.e, f"{name}.e", device, (torch.uint8,), -(-k // BLOCK8), m, True)
+    _matrix(c.q, name + ".q", device, (torch.int8,), (m, k), True)
+    _matrix(c.e, name + ".e", device, (torch.uint8,), (-(-k // BLOCK8), m), True)
 
 
 def checkpoint8(x: torch.Tensor, out: Optional[Checkpoint8] = None) -> Checkpoint8:
     """``x`` (bf16 [m, k], adjacent columns) in the 8-bit form."""
     device = _device(x, "x")
     m, k = _two_dim(x, "x")
-    _matrix(x, "x", device, (_BF16,), m, k, True)
+    _matrix(x, "x", device, (_BF16,), (m, k), True)
     if out is None:
-        out = Checkpoint8(torch.empty((m, k), dtype=torch.int8, device=device),
-                          torch.empty((-(-k // BLOCK8), m), dtype=torch.uint8, device=device))
+        out = Checkpoint8(x.new_empty((m, k), dtype=torch.int8),
+                          x.new_empty((-(-k // BLOCK8), m), dtype=torch.uint8))
     _checkpoint(out, "out", device, m, k)
     st = _lib.dlion_checkpoint8(x.data_ptr(), x.stride(0), m, k, out.q.data_ptr(), out.q.stride(0), out.e.data_ptr(),
-                                out.e.stride(0), torch.cuda.current_stream(device).cuda_stream)
+                                out.e.stride(0), _stream(device))
     if st != OK:
         raise DlionError(st, "dlion_checkpoint8")
     return out
@@ -286,9 +301,9 @@ def restore8(c: Checkpoint8, out: Optional[torch.Tensor] = None) -> torch.Tensor
     _checkpoint(c, "c", device, m, k)
     if out is None:
         out = torch.empty((m, k), dtype=_BF16, device=device)
-    _matrix(out, "out", device, (_BF16,), m, k, True)
+    _matrix(out, "out", device, (_BF16,), (m, k), True)
     st = _lib.dlion_restore8(c.q.data_ptr(), c.q.stride(0), c.e.data_ptr(), c.e.stride(0), m, k, out.data_ptr(),
-                             out.stride(0), torch.cuda.current_stream(device).cuda_stream)
+                             out.stride(0), _stream(device))
     if st != OK:
         raise DlionError(st, "dlion_restore8")
     return out
@@ -306,8 +321,8 @@ def lm_loss(x: torch.Tensor, w: torch.Tensor, targets: torch.Tensor, *, ignore_i
     device = _device(x, "x")
     m, h = _two_dim(x, "x")
     v = _two_dim(w, "w")[0]
-    _matrix(x, "x", device, (_BF16,), m, h)
-    _matrix(w, "w", device, (_BF16,), v, h)
+    _matrix(x, "x", device, (_BF16,), (m, h))
+    _matrix(w, "w", device, (_BF16,), (v, h))
     _vector(targets, "targets", device, (torch.int64,), m)
     mean = _enumerator({"sum": 0, "mean": 1}, reduction, "reduction")
     g = _grad_type(grad_dtype)
@@ -317,18 +332,20 @@ def lm_loss(x: torch.Tensor, w: torch.Tensor, targets: torch.Tensor, *, ignore_i
     loss, rows = stats[m], stats[:m]
     if grads:
         if dx is None:
-            dx = torch.empty((m, h), dtype=_BF16, device=device)
+            dx = x.new_empty((m, h))
+        else:
+            _matrix(dx, "dx", device, (_BF16,), (m, h), True)
         if dw is None:
-            dw = torch.empty((v, h), dtype=grad_dtype, device=device)
-        _matrix(dx, "dx", device, (_BF16,), m, h, True)
-        _matrix(dw, "dw", device, (grad_dtype,), v, h, True)
+            dw = x.new_empty((v, h), dtype=grad_dtype)
+        else:
+            _matrix(dw, "dw", device, (grad_dtype,), (v, h), True)
     else:
         dx = dw = None
     xs, ws = x.stride(), w.stride()
     args = _Loss(m, h, v, x.data_ptr(), xs[0], xs[1], w.data_ptr(), ws[0], ws[1], targets.data_ptr(), ignore_index, mean, scale,
                  loss.data_ptr(), rows.data_ptr(), _ptr(dx), 0 if dx is None else dx.stride(0), _ptr(dw),
                  0 if dw is None else dw.stride(0), g, piece)
-    _call("dlion_lm_loss", args, device, workspace)
+    _call(_lib.dlion_lm_loss_workspace, _lib.dlion_lm_loss, args, device, workspace)
     return Loss(loss, rows, dx, dw)
 
 
