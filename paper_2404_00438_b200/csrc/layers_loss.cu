@@ -22,6 +22,7 @@ constexpr int64_t kPiece = 4096;
 constexpr int64_t kMost = int64_t{1} << 30;
 
 struct LossTile {
+    static constexpr bool kSplits = false;
     struct Args {
         int m, n;
         const int64_t* targets;
@@ -32,7 +33,36 @@ struct LossTile {
         int64_t ld;
     };
 
-    static __device__ __forceinline__ void tile(const Args& p, uint32_t acc, int row0, int col0, int width, int, bool live, uint4* stage, int lane) {
+    // MASKED: columns from `valid` on do not exist
+    template <bool MASKED>
+    static __device__ __forceinline__ float greatest(const float (&v)[32], int valid, float top) {
+        float t[4] = {top, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+        for (int j = 0; j < 32; ++j) {
+            if (!MASKED || j < valid) t[j % 4] = fmaxf(t[j % 4], v[j]);
+        }
+        return fmaxf(fmaxf(t[0], t[1]), fmaxf(t[2], t[3]));
+    }
+
+    template <bool MASKED, bool CODES>
+    static __device__ __forceinline__ float exponentials(const float (&v)[32], int valid, float top, uint32_t (&w)[16]) {
+        float t[4] = {};
+#pragma unroll
+        for (int j = 0; j < 32; ++j) {
+            const float x = v[j] - top;     // exact where it counts, near the maximum
+            const float e = exp2_fast(x * kLog2e);
+            if (!MASKED || j < valid) t[j % 4] += e;
+            if (CODES) {
+                // x <= 0: 1.5 * 2^23 + the distance leaves it, rounded, in the low bits
+                const uint32_t u = __float_as_uint(fminf(__fmaf_rn(x, -kStep * kLog2e, 12582912.0f), 12582912.0f + 65535.0f));
+                w[j / 2] = j % 2 == 0 ? u : __byte_perm(w[j / 2], u, 0x5410);
+            }
+        }
+        return (t[0] + t[1]) + (t[2] + t[3]);
+    }
+
+    // Two passes over the accumulator, which is cheaper to read again than to hold: the maximum, then the exponentials.
+    static __device__ __forceinline__ void tile(const Args& p, uint32_t acc, int row0, int col0, int width, bool live, uint4* stage, int lane) {
         if (row0 >= p.m || col0 >= p.n) return;
         if (row0 == 0 && col0 == 0 && lane == 0) *p.blocks_done = 0;
         const int row = row0 + lane;
@@ -40,43 +70,41 @@ struct LossTile {
         const int rows = live ? min(32, p.m - row0) : 0;
         const int64_t target = lane < rows ? p.targets[row] : -1;
         const int hit = target >= col0 && target < col0 + valid ? static_cast<int>(target - col0) : -1;
+        const bool codes = p.codes != nullptr;
         float top = -INFINITY;
+#pragma unroll 1
         for (int c = 0; c < valid; c += 32) {
             float v[32];
             tc::tmem_load32(acc + c, v);
-#pragma unroll
-            for (int j = 0; j < 32; ++j) {
-                if (c + j < valid) top = fmaxf(top, v[j]);
-            }
-            if (hit >= c && hit < c + 32) {
+            top = c + 32 <= valid ? greatest<false>(v, 32, top) : greatest<true>(v, valid - c, top);
+            if (__any_sync(0xffffffffu, hit >= c && hit < c + 32)) {
                 float l = 0.0f;
 #pragma unroll
-                for (int j = 0; j < 32; ++j) l = hit - c == j ? v[j] : l;
-                p.at_target[row] = l;
+                for (int j = 0; j < 32; ++j) {          // a select each: indexed, the 32 sums would live in memory
+                    asm("{\n.reg .pred p;\nsetp.eq.s32 p, %2, 0;\nselp.f32 %0, %1, %0, p;\n}" : "+f"(l) : "f"(v[j]), "r"(hit - c - j));
+                }
+                if (hit >= c && hit < c + 32) p.at_target[row] = l;
             }
+            if (!live) break;
         }
         // A group that is masked whole (-infinity, or the type's lowest value) sums to 0, and so that it does, the
         // difference must be finite; logits above 2e38 make the row NaN.
         top = top > 2e38f ? NAN : fmaxf(top, -2e38f);
         float sum = 0.0f;
+#pragma unroll 1
         for (int c = 0; c < valid; c += 32) {
             float v[32];
-            tc::tmem_load32(acc + c, v);
             uint32_t w[16];
-#pragma unroll
-            for (int j = 0; j < 32; ++j) {
-                const float x = v[j] - top;      // exact where it counts, near the maximum
-                const float e = exp2_fast(x * kLog2e);
-                if (c + j < valid) sum += e;
-                // x <= 0: 1.5 * 2^23 + the distance leaves it, rounded, in the low bits
-                const float d = fminf(__fmaf_rn(x, -kStep * kLog2e, 12582912.0f), 12582912.0f + 65535.0f);
-                const uint32_t u = __float_as_uint(d);
-                w[j / 2] = j % 2 == 0 ? u : __byte_perm(w[j / 2], u, 0x5410);
+            tc::tmem_load32(acc + c, v);
+            if (c + 32 > valid) {
+                sum += exponentials<true, true>(v, valid - c, top, w);
+            } else if (codes) {
+                sum += exponentials<false, true>(v, 32, top, w);
+            } else {
+                sum += exponentials<false, false>(v, 32, top, w);
             }
-            if (p.codes != nullptr) {
-                const Piece pc{stage, lane, row0, col0 + c, rows, 32};      // ld covers the last tile
-                pc.put16(w, p.codes, p.ld, true);
-            }
+            if (codes) Piece{stage, lane, row0, col0 + c, rows, 32}.put16(w, p.codes, p.ld, true);      // ld covers the last tile
+            if (!live) break;
         }
         if (lane < rows) p.stats[static_cast<int64_t>(col0 / width) * p.m + row] = make_float2(top, sum);
     }

@@ -28,60 +28,6 @@ EncodeTiled encoder() {
     return fn;
 }
 
-// One element a thread: a warp has 32 columns of a row, so that the 8-bit form's blocks are warps.
-__global__ void __launch_bounds__(256) sum_splits_kernel(const Finish f, int splits) {
-    tc::let_next_start();
-    tc::wait_for_previous();
-    const int lane = threadIdx.x % 32;
-    const int64_t per_row = (f.n + 31) / 32;
-    const int64_t at = static_cast<int64_t>(blockIdx.x) * 8 + threadIdx.x / 32;
-    const int64_t row = at / per_row;
-    if (row >= f.m) return;
-    const int64_t col = (at - row * per_row) * 32 + lane;
-    const bool in = col < f.n;
-    const float* p = f.partial + row * f.partial_ld + col;     // padded columns exist
-    const int64_t step = f.partial_rows * f.partial_ld;
-    float v = 0.0f;
-    int i = 0;
-    for (; i + 4 <= splits; i += 4) {
-        const float a = p[i * step], b = p[(i + 1) * step], c = p[(i + 2) * step], d = p[(i + 3) * step];
-        v = (((v + a) + b) + c) + d;
-    }
-    for (; i < splits; ++i) v += p[i * step];
-    if (f.scale != nullptr) v *= *f.scale;
-    if (f.bias != nullptr && in) {
-        v += f.bias_f32 ? static_cast<const float*>(f.bias)[col] : __bfloat162float(static_cast<const __nv_bfloat16*>(f.bias)[col]);
-    }
-    if (f.keep == DLION_KEEP_8BIT) {
-        uint32_t top = in ? __float_as_uint(v) & 0x7fffffffu : 0u;
-        top = __reduce_max_sync(0xffffffffu, top);
-        const uint32_t e = block_exponent(top);
-        if (lane == 0) f.kept_e[(col / 32) * f.kept_e_ld + row] = static_cast<uint8_t>(e);
-        if (in) static_cast<int8_t*>(f.kept)[row * f.kept_ld + col] = static_cast<int8_t>(quantise8(v, block_inverse(e)));
-    } else if (f.keep == DLION_KEEP_BF16 && in) {
-        static_cast<__nv_bfloat16*>(f.kept)[row * f.kept_ld + col] = __float2bfloat16_rn(v);
-    }
-    if (!in) return;
-    with_act(f.act, [&](auto kind) { v = act_value<decltype(kind)::value>(v); });
-    if (f.slope != DLION_ACT_NONE) {
-        float u;
-        if (f.saved8) {
-            u = static_cast<float>(static_cast<const int8_t*>(f.saved)[row * f.saved_ld + col]) *
-                block_scale(f.saved_e[(col / 32) * f.saved_e_ld + row]);
-        } else {
-            u = __bfloat162float(static_cast<const __nv_bfloat16*>(f.saved)[row * f.saved_ld + col]);
-        }
-        with_act(f.slope, [&](auto kind) { v *= act_slope<decltype(kind)::value>(u); });
-    }
-    if (f.residual != nullptr) v += __bfloat162float(f.residual[row * f.residual_ld + col]);
-    if (f.accumulated != nullptr) v += f.accumulated[row * f.accumulated_ld + col];
-    if (f.out_f32) {
-        static_cast<float*>(f.out)[row * f.out_ld + col] = v;
-    } else {
-        static_cast<__nv_bfloat16*>(f.out)[row * f.out_ld + col] = __float2bfloat16_rn(v);
-    }
-}
-
 // out[r][c] = a[r * rs + c * cs], rows of ld elements; reads run along whichever stride is smaller.
 __global__ void __launch_bounds__(256) pack_kernel(const uint16_t* a, int64_t rs, int64_t cs, int64_t rows, int64_t cols,
                                                    uint16_t* out, int64_t ld) {
@@ -104,39 +50,42 @@ __global__ void __launch_bounds__(256) pack_kernel(const uint16_t* a, int64_t rs
 
 }  // namespace
 
-// The division of the work with the least estimated time, in clocks of an SM: rounds of tiles, each of so many slices
-// and an epilogue that the next tile hides.  A slice takes 540 (its 32 KB at 57 bytes a clock, or the tensor cores' 512)
-// in a pair's 256 x 256 tile and 420 (24 KB) in the others; splits of pairs are summed by a second kernel at the
-// L2's rate; joined blocks exchange their sums in about 3000.
+// The division of the work with the least estimated time, in clocks of an SM.  A slice takes 540 (its 32 KB at 57 bytes
+// a clock, or the tensor cores' 512) in a pair's 256 x 256 tile and 420 (24 KB) in the others.  Tiles that do not fill a last
+// round of the workers are split, which costs the writing and reading of their sums: 8192 x 8192 x 2048 has 256 tiles for
+// 74 pairs, 3.46 rounds; four rounds took 207 us, three and the halves of 34 tiles 187 us.  Joined blocks exchange
+// their sums in about 3000.
 Config choose(const Call& c, int64_t m, int64_t n, int64_t k, bool sums, bool alone) {
     const int64_t slices = std::max<int64_t>(1, parts(k, kSlice));
     const bool long_sums = sums && slices > kSegment;
-    Config best{2, 256, kWhole, 1, static_cast<int>(slices)};
+    Config best{2, 256, kWhole, 0, 1, static_cast<int>(slices)};
     double least = 1e300;
     auto consider = [&](int cg, int bn, int form, int64_t s, double slice, double piece) {
         const int64_t per = parts(slices, s);
         if (parts(slices, per) != s) return;
-        const int64_t tm = parts(m, 128 * cg), tn = parts(n, bn);
+        const int64_t tiles = parts(m, 128 * cg) * parts(n, bn), workers = c.sms / cg;
+        int64_t whole = 0;
         double t;
         if (form == kJoined) {
-            if (tm * tn * s > 16 * 8) return;  // clusters of eight: sixteen at a time for certain
+            if (tiles * s > 16 * 8) return;    // clusters of eight: sixteen at a time for certain
             t = per * slice + 3000.0 + piece;
         } else {
-            t = static_cast<double>(parts(tm * tn * s, c.sms / cg)) * (per * slice + 500.0) + piece;
-            if (s > 1) t += 6000.0 + static_cast<double>(s) * tm * tn * cg * bn * 128 * 8.0 / 3000.0;
+            whole = s == 1 ? tiles : tiles / workers * workers;
+            t = static_cast<double>(parts(whole, workers)) * (slices * slice + 500.0) + piece;
+            if (s > 1) t += static_cast<double>(parts((tiles - whole) * s, workers)) * (per * slice + 500.0) + 2000.0 + 1200.0 * s * (bn / 128);
         }
         if (t < least) {
             least = t;
-            best = Config{cg, bn, form, static_cast<int>(s), static_cast<int>(per)};
+            best = Config{cg, bn, form, static_cast<int>(whole), static_cast<int>(s), static_cast<int>(per)};
         }
     };
-    const int64_t most = alone ? 1 : std::min<int64_t>(32, std::max<int64_t>(1, slices / 8));
+    const int64_t most = alone ? 1 : std::min<int64_t>(16, std::max<int64_t>(1, slices / 8));
     for (int64_t s = 1; s <= most; ++s) {
         if (long_sums) {
             consider(2, 128, kLong, s, 420.0, 2000.0);
         } else {
             consider(2, 256, kWhole, s, 540.0, 4000.0);
-            if (s == 1) consider(2, 128, kWhole, s, 420.0, 2000.0);
+            consider(2, 128, kWhole, s, 420.0, 2000.0);
         }
     }
     if (!long_sums) consider(1, 64, kWhole, 1, 420.0, 1000.0);
@@ -227,6 +176,7 @@ bool shape_of(const Config& cfg, const Matrix& a, const Matrix& b, Shape* s) {
     s->tiles_m = static_cast<int>(parts(a.rows, 128 * cfg.cg));
     s->tiles_n = static_cast<int>(parts(b.rows, cfg.bn));
     s->slices = static_cast<int>(parts(a.cols, kSlice));
+    s->whole = cfg.whole;
     s->splits = cfg.splits;
     s->split_slices = cfg.split_slices;
     return static_cast<int64_t>(s->tiles_m) * s->tiles_n * s->splits < (int64_t{1} << 30);
@@ -246,11 +196,12 @@ void product(Call& c, const Matrix& a, const Matrix& b, Finish f) {
         return;
     }
     const uint64_t mark = c.ws.used;
-    const bool partial = cfg.splits > 1 && cfg.form != kJoined;
-    if (partial) {
-        f.partial_ld = static_cast<int64_t>(s.tiles_n) * cfg.bn;
-        f.partial_rows = static_cast<int64_t>(s.tiles_m) * 128 * cfg.cg;
-        f.partial = c.ws.take<float>(static_cast<uint64_t>(cfg.splits) * f.partial_ld * f.partial_rows);
+    const int64_t split_tiles = cfg.form == kJoined || cfg.splits == 1 ? 0 : static_cast<int64_t>(s.tiles_m) * s.tiles_n - cfg.whole;
+    uint64_t tickets = 0;
+    if (split_tiles != 0) {
+        tickets = static_cast<uint64_t>(split_tiles) * cfg.cg * kEpilogueWarps;
+        f.tickets = c.ws.take<unsigned int>(tickets);
+        f.parts = c.ws.take<float4>(tickets * cfg.splits * (cfg.bn / 2) * 8);
     }
     if (c.live()) {
         CUtensorMap ma, mb;
@@ -259,6 +210,7 @@ void product(Call& c, const Matrix& a, const Matrix& b, Finish f) {
             c.status = DLION_ECUDA;
             return;
         }
+        if (tickets != 0) c.check(cudaMemsetAsync(f.tickets, 0, tickets * sizeof(unsigned int), c.stream));
         if (cfg.form == kLong) {
             launch<2, 128, General, kLong>(c, ma, mb, s, f);
         } else if (cfg.form == kJoined) {
@@ -269,10 +221,6 @@ void product(Call& c, const Matrix& a, const Matrix& b, Finish f) {
             launch<2, 128, General, kWhole>(c, ma, mb, s, f);
         } else {
             launch<2, 256, General, kWhole>(c, ma, mb, s, f);
-        }
-        if (partial) {
-            const int64_t warps = static_cast<int64_t>(f.m) * parts(f.n, 32);
-            start(c, sum_splits_kernel, dim3(static_cast<unsigned>(parts(warps, 8))), dim3(256), 0, 1, f, cfg.splits);
         }
     }
     if (c.ws.dry) {

@@ -36,8 +36,26 @@ struct Shape {
     int m, n, k;
     int a_mn, b_mn;                        // operand majors (1: adjacent values along m / n)
     int tiles_m, tiles_n;
-    int splits, split_slices, slices;      // slices of k in all, and per split
+    int whole;                             // tiles that one worker sums; the rest are split
+    int splits, split_slices, slices;      // splits of a tile, slices of k per split and in all
 };
+
+// A worker's u-th piece of work: a tile and its slices.  The split tiles come last, the splits of one side by side.
+struct Unit {
+    int tile, split, k0, k1;
+    bool part;
+};
+
+__device__ __forceinline__ Unit unit_of(const Shape& s, int u) {
+    Unit x;
+    x.part = u >= s.whole;
+    const int rest = s.tiles_m * s.tiles_n - s.whole;
+    x.split = x.part ? (u - s.whole) / rest : 0;
+    x.tile = x.part ? s.whole + (u - s.whole) % rest : u;
+    x.k0 = x.part ? x.split * s.split_slices : 0;
+    x.k1 = x.part ? min(s.slices, x.k0 + s.split_slices) : s.slices;
+    return x;
+}
 
 enum Todo : unsigned { kScale = 1, kBias = 2, kKeep16 = 4, kKeep8 = 8, kAct = 16, kSlope = 32, kResidual = 64, kAdd = 128 };
 
@@ -69,8 +87,8 @@ struct Finish {
     void* out;
     int64_t out_ld;
     int out_f32;
-    float* partial;                        // split sums: [split][rows padded][cols padded], nothing else applies
-    int64_t partial_ld, partial_rows;
+    float4* parts;                         // sums of split tiles: [tile][block][epilogue warp][split][32 rows x half the columns]
+    unsigned int* tickets;                 // [tile][block][epilogue warp], 0 before the call
 };
 
 __device__ __forceinline__ bool on_grid(const void* p, int64_t ld, int bytes) {
@@ -281,6 +299,7 @@ __device__ __forceinline__ void times_slope8(const Finish& f, const Piece& pc, f
 // a small product runs this code once, and each jump over unused code costs a fetch of some 500 clocks.
 struct General {
     using Args = Finish;
+    static constexpr bool kSplits = true;
 
     static __device__ __forceinline__ void piece(const Finish& f, unsigned todo, const Piece& pc, float (&v)[32]) {
         if (__builtin_expect(todo != 0, 0)) {
@@ -341,22 +360,52 @@ struct General {
     }
 
     // One warp's 32 rows and `width` columns of a finished accumulator.
-    static __device__ __forceinline__ void tile(const Finish& f, uint32_t acc, int row0, int col0, int width, int split, bool live, uint4* stage, int lane) {
+    static __device__ __forceinline__ void tile(const Finish& f, uint32_t acc, int row0, int col0, int width, bool live, uint4* stage, int lane) {
         const unsigned todo = f.todo;
 #pragma unroll 1
         for (int c = 0; c < width; c += 32) {
             float v[32];
-            if (__builtin_expect(f.partial != nullptr, 0)) {
-                tc::tmem_load32(acc + c, v);
-                const Piece pc{stage, lane, row0, col0 + c, live ? 32 : 0, 32};
-                pc.put32(v, f.partial + split * f.partial_rows * f.partial_ld, f.partial_ld, true);
-                continue;
-            }
             if (col0 + c >= f.n || row0 >= f.m) return;      // the same for the whole warp
             tc::tmem_load32(acc + c, v);
             const Piece pc{stage, lane, row0, col0 + c, live ? min(32, f.m - row0) : 0, min(32, f.n - col0 - c)};
             piece(f, todo, pc, v);
             if (!live) return;
+        }
+    }
+
+    // 32 x 32 sums of a split, kept as the threads have them: 512 bytes side by side at a time
+    static __device__ __forceinline__ void put_part(float4* to, const float (&v)[32], int lane) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) __stcg(to + i * 32 + lane, make_float4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]));
+    }
+
+    // After a warp's part of a split is in place: whoever finds the other splits done adds them all, in their order, so that
+    // the sum does not depend on who that is.  Nobody waits.
+    static __device__ __forceinline__ void join(const Finish& f, int place, int splits, int row0, int col0, int width, uint4* stage, int lane) {
+        __threadfence();
+        __syncwarp();
+        unsigned int before = 0;
+        if (lane == 0) before = atomicAdd(f.tickets + place, 1u);
+        before = __shfl_sync(0xffffffffu, before, 0);
+        if (before != static_cast<unsigned int>(splits - 1)) return;
+        __threadfence();
+        const float4* from = f.parts + static_cast<int64_t>(place) * splits * (width * 8);
+#pragma unroll 1
+        for (int c = 0; c < width; c += 32) {
+            if (col0 + c >= f.n || row0 >= f.m) return;
+            float v[32] = {};
+#pragma unroll 2
+            for (int r = 0; r < splits; ++r) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const float4 w = __ldcg(from + (r * width + c) * 8 + i * 32 + lane);
+                    v[4 * i] += w.x;
+                    v[4 * i + 1] += w.y;
+                    v[4 * i + 2] += w.z;
+                    v[4 * i + 3] += w.w;
+                }
+            }
+            piece(f, f.todo, Piece{stage, lane, row0, col0 + c, min(32, f.m - row0), min(32, f.n - col0 - c)}, v);
         }
     }
 };
@@ -396,11 +445,11 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
 
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
     const uint32_t rank = CG == 2 ? tc::cluster_rank() : 0;
-    const int tiles = s.tiles_m * s.tiles_n, units = tiles * s.splits;
+    const int tiles = s.tiles_m * s.tiles_n, units = s.whole + (tiles - s.whole) * s.splits;
     // kJoined: the cluster is the worker, a block's place in it the split; one tile each
     const int share = FORM == kJoined ? static_cast<int>(tc::cluster_rank()) : 0;
     const int workers = FORM == kJoined ? units : gridDim.x / CG;
-    const int worker = FORM == kJoined ? static_cast<int>(blockIdx.x) / s.splits + share * tiles : static_cast<int>(blockIdx.x) / CG;
+    const int worker = FORM == kJoined ? static_cast<int>(blockIdx.x) / s.splits + share * tiles : static_cast<int>(blockIdx.x) / CG;   // whole = 0
 
     tc::let_next_start();
     if (threadIdx.x == 0) {
@@ -435,10 +484,10 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
             int it = 0;
             for (int u = worker; u < units && fine; u += workers) {
                 int tm, tn;
-                tile_of(s, u % tiles, tm, tn);
-                const int k0 = (u / tiles) * s.split_slices, k1 = min(s.slices, k0 + s.split_slices);
+                const Unit x = unit_of(s, u);
+                tile_of(s, x.tile, tm, tn);
                 const int row = tm * kM + static_cast<int>(rank) * 128, col = tn * BN + static_cast<int>(rank) * kBRows;
-                for (int kb = k0; kb < k1; ++kb, ++it) {
+                for (int kb = x.k0; kb < x.k1; ++kb, ++it) {
                     const int st = it % kRing;
                     if (!(fine = tc::bar_wait(empty + 8 * st, ((it / kRing) & 1) ^ 1))) break;
                     const uint32_t a = base + st * kStageBytes, b = a + 16384, bar = lead_full + 8 * st;
@@ -469,10 +518,10 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
             const uint32_t a_step = (s.a_mn ? 2048 : 32) >> 4, b_step = (s.b_mn ? 2048 : 32) >> 4;   // 16 values of k
             int it = 0, n = 0;
             for (int u = worker; u < units && fine; u += workers) {
-                const int k0 = (u / tiles) * s.split_slices, k1 = min(s.slices, k0 + s.split_slices);
-                const int seg = FORM == kLong ? kSegment : k1 - k0;
-                for (int kb = k0; kb < k1 && fine; ++n) {
-                    const int set = n & 1, from = kb, to = min(k1, kb + seg);
+                const Unit x = unit_of(s, u);
+                const int seg = FORM == kLong ? kSegment : x.k1 - x.k0;
+                for (int kb = x.k0; kb < x.k1 && fine; ++n) {
+                    const int set = n & 1, from = kb, to = min(x.k1, kb + seg);
                     if (!(fine = tc::bar_wait(drained + 8 * set, ((n >> 1) & 1) ^ 1))) break;
                     tc::fence_after();
                     const uint32_t acc = tmem + set * BN;
@@ -513,12 +562,13 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
         for (int u = worker - workers; u < units && fine; u += workers) {
             const bool live = u >= 0 && (FORM == kJoined ? u == worker : true);
             int tm, tn;
-            tile_of(s, (live ? u : worker) % tiles, tm, tn);
+            const Unit x = unit_of(s, live ? u : worker);
+            tile_of(s, x.tile, tm, tn);
+            const int place = ((x.tile - s.whole) * CG + static_cast<int>(rank)) * kEpilogueWarps + warp - 4;     // of a split tile's part
             const int row0 = tm * kM + static_cast<int>(rank) * 128 + quarter * 32, col0 = tn * BN + half * (BN / 2);
             if constexpr (FORM == kLong) {
-                const int k0 = (u / tiles) * s.split_slices, k1 = min(s.slices, k0 + s.split_slices);
                 float sum[BN / 2] = {};
-                for (int kb = k0; live && kb < k1; kb += kSegment, ++n) {
+                for (int kb = x.k0; live && kb < x.k1; kb += kSegment, ++n) {
                     const int set = n & 1;
                     if (!(fine = tc::bar_wait(ready + 8 * set, (n >> 1) & 1))) break;
                     tc::fence_after();
@@ -531,7 +581,20 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
                     }
                     drain(set);
                 }
-                if (fine) E::sums(args, sum, row0, col0, live, stage, lane);
+                if (!fine) break;
+                if (x.part && live) {
+                    float4* to = args.parts + (static_cast<int64_t>(place) * s.splits + x.split) * (BN / 2 * 8);
+#pragma unroll
+                    for (int c = 0; c < BN / 2; c += 32) {
+                        float v[32];
+#pragma unroll
+                        for (int j = 0; j < 32; ++j) v[j] = sum[c + j];
+                        E::put_part(to + c * 8, v, lane);
+                    }
+                    E::join(args, place, s.splits, row0, col0, BN / 2, stage, lane);
+                } else {
+                    E::sums(args, sum, row0, col0, live, stage, lane);
+                }
             } else if constexpr (FORM == kJoined) {
                 if (live) {
                     if (!(fine = tc::bar_wait(ready, 0))) break;
@@ -581,7 +644,22 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
                     if (!(fine = tc::bar_wait(ready + 8 * set, (n >> 1) & 1))) break;
                     tc::fence_after();
                 }
-                E::tile(args, part + set * BN, row0, col0, BN / 2, u / tiles, live, stage, lane);
+                if constexpr (E::kSplits) {
+                    if (x.part && live) {
+                        float4* to = args.parts + (static_cast<int64_t>(place) * s.splits + x.split) * (BN / 2 * 8);
+#pragma unroll 1
+                        for (int c = 0; c < BN / 2; c += 32) {
+                            float v[32];
+                            tc::tmem_load32(part + set * BN + c, v);
+                            E::put_part(to + c * 8, v, lane);
+                        }
+                        drain(set);
+                        ++n;
+                        E::join(args, place, s.splits, row0, col0, BN / 2, stage, lane);
+                        continue;
+                    }
+                }
+                E::tile(args, part + set * BN, row0, col0, BN / 2, live, stage, lane);
                 if (live) {
                     drain(set);
                     ++n;

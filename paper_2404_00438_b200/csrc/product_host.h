@@ -68,7 +68,7 @@ inline Matrix transposed(const Matrix& a) { return Matrix{a.p, a.cols, a.rows, a
 bool make_map(CUtensorMap* map, const Matrix& a, int* mn_major, int box_rows);
 
 struct Config {
-    int cg, bn, form, splits, split_slices;
+    int cg, bn, form, whole, splits, split_slices;
 };
 // `sums`: binary32 results, whose long sums are taken in segments.  `alone`: no splits (the epilogue needs whole rows of tiles).
 Config choose(const Call& c, int64_t m, int64_t n, int64_t k, bool sums, bool alone);
@@ -105,7 +105,7 @@ void launch(Call& c, const CUtensorMap& ma, const CUtensorMap& mb, const Shape& 
         c.check(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem));
         if (c.status == DLION_OK && c.device < 64) ready.fetch_or(bit, std::memory_order_relaxed);
     }
-    const int64_t units = static_cast<int64_t>(s.tiles_m) * s.tiles_n * s.splits;
+    const int64_t units = s.whole + (static_cast<int64_t>(s.tiles_m) * s.tiles_n - s.whole) * s.splits;
     const int64_t blocks = FORM == kJoined ? units : std::min<int64_t>(units, c.sms / CG) * CG;
     start(c, kernel, dim3(static_cast<unsigned>(blocks)), dim3(kThreads), kSmem, FORM == kJoined ? s.splits : CG, ma, mb, s, f, c.mark);
 }
