@@ -50,8 +50,8 @@ __global__ void __launch_bounds__(256) pack_kernel(const uint16_t* a, int64_t rs
 
 }  // namespace
 
-// The division of the work with the least estimated time, in clocks of an SM.  A slice takes 540 (its 32 KB at 57 bytes
-// a clock, or the tensor cores' 512) in a pair's 256 x 256 tile and 420 (24 KB) in the others.  Tiles that do not fill a last
+// The division of the work with the least estimated time, in clocks of an SM.  A slice takes 580 (its 32 KB come
+// at 57 to 64 bytes a clock, its products take 512) in a pair's 256 x 256 tile and 420 (24 KB) in the others.  Tiles that do not fill a last
 // round of the workers are split, which costs the writing and reading of their sums: 8192 x 8192 x 2048 has 256 tiles for
 // 74 pairs, 3.46 rounds; four rounds took 207 us, three and the halves of 34 tiles 187 us.  Joined blocks exchange
 // their sums in about 3000.
@@ -71,8 +71,9 @@ Config choose(const Call& c, int64_t m, int64_t n, int64_t k, bool sums, bool al
             t = per * slice + 3000.0 + piece;
         } else {
             whole = s == 1 ? tiles : tiles / workers * workers;
-            t = static_cast<double>(parts(whole, workers)) * (slices * slice + 500.0) + piece;
-            if (s > 1) t += static_cast<double>(parts((tiles - whole) * s, workers)) * (per * slice + 500.0) + 2000.0 + 1200.0 * s * (bn / 128);
+            const double round = 300.0;
+            t = static_cast<double>(parts(whole, workers)) * (slices * slice + round) + piece;
+            if (s > 1) t += static_cast<double>(parts((tiles - whole) * s, workers)) * (per * slice + round) + 2000.0 + 1200.0 * s * (bn / 128);
         }
         if (t < least) {
             least = t;
@@ -84,7 +85,7 @@ Config choose(const Call& c, int64_t m, int64_t n, int64_t k, bool sums, bool al
         if (long_sums) {
             consider(2, 128, kLong, s, 420.0, 2000.0);
         } else {
-            consider(2, 256, kWhole, s, 540.0, 4000.0);
+            consider(2, 256, kWhole, s, 580.0, 4000.0);
             consider(2, 128, kWhole, s, 420.0, 2000.0);
         }
     }

@@ -426,9 +426,10 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
                const __grid_constant__ typename E::Args args, unsigned int* mark) {
     constexpr int kM = 128 * CG;               // rows of the tile; a block has 128 of them
     constexpr int kBRows = BN / CG;            // of B, in this block
-    constexpr uint32_t kCols = 2 * BN;         // tensor memory columns
+    constexpr uint32_t kCols = 2 * BN;         // tensor memory columns: two accumulators
+    constexpr int kABytes = 16384;
     static_assert(FORM != kJoined || CG == 1, "joined tiles are a block's own");
-    constexpr int kStageBytes = 16384 + kBRows * 128;
+    constexpr int kStageBytes = kABytes + kBRows * 128;
     constexpr uint32_t kBytes = CG * kStageBytes;
 
     extern __shared__ uint8_t raw[];
@@ -478,19 +479,22 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
     bool fine = true;
     tc::wait_for_previous();
 
+    // The copying and the issuing warp go through their loops whole and elect a lane at the instructions themselves: so
+    // what describes the operands stays in uniform registers, where these instructions want it.  With one lane in the
+    // loop the issue of four instructions and the wait before them took 640 clocks, more than the 512 of the products.
     if (warp == 0) {
-        if (lane == 0) {
-            const uint32_t lead_full = CG == 2 ? tc::map_to_rank(full, 0) : full;
-            int it = 0;
-            for (int u = worker; u < units && fine; u += workers) {
-                int tm, tn;
-                const Unit x = unit_of(s, u);
-                tile_of(s, x.tile, tm, tn);
-                const int row = tm * kM + static_cast<int>(rank) * 128, col = tn * BN + static_cast<int>(rank) * kBRows;
-                for (int kb = x.k0; kb < x.k1; ++kb, ++it) {
-                    const int st = it % kRing;
-                    if (!(fine = tc::bar_wait(empty + 8 * st, ((it / kRing) & 1) ^ 1))) break;
-                    const uint32_t a = base + st * kStageBytes, b = a + 16384, bar = lead_full + 8 * st;
+        const uint32_t lead_full = CG == 2 ? tc::map_to_rank(full, 0) : full;
+        int st = 0, filled = 0;
+        uint32_t phase = 1;
+        for (int u = worker; u < units && fine; u += workers) {
+            int tm, tn;
+            const Unit x = unit_of(s, u);
+            tile_of(s, x.tile, tm, tn);
+            const int row = tm * kM + static_cast<int>(rank) * 128, col = tn * BN + static_cast<int>(rank) * kBRows;
+            for (int kb = x.k0; kb < x.k1; ++kb, ++filled) {
+                if (!(fine = tc::bar_wait(empty + 8 * st, phase))) break;
+                if (tc::elected()) {
+                    const uint32_t a = base + st * kStageBytes, b = a + kABytes, bar = lead_full + 8 * st;
                     if (rank == 0) tc::bar_expect(full + 8 * st, kBytes);
                     if (s.a_mn) {
                         tc::load_tile<CG>(a, &map_a, row, kb * kSlice, bar);
@@ -505,39 +509,56 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
                         tc::load_tile<CG>(b, &map_b, kb * kSlice, col, bar);
                     }
                 }
-            }
-            // Where a wait ran out, what was asked for still lands in this block's memory: it is awaited.
-            if (!fine && rank == 0) {
-                for (int i = max(0, it - kRing); i < it; ++i) tc::bar_wait(full + 8 * (i % kRing), (i / kRing) & 1);
+                __syncwarp();
+                if (++st == kRing) {
+                    st = 0;
+                    phase ^= 1;
+                }
             }
         }
+        // Where a wait ran out, what was asked for still lands in this block's memory: it is awaited.
+        if (!fine && rank == 0) {
+            for (int i = max(0, filled - kRing); i < filled; ++i) tc::bar_wait(full + 8 * (i % kRing), (i / kRing) & 1);
+        }
     } else if (warp == 1) {
-        if (lane == 0 && rank == 0) {
+        if (rank == 0) {
             const uint32_t inst = tc::instruction(kM, BN, s.a_mn, s.b_mn);
-            const uint64_t a_desc = tc::operand_base(s.a_mn), b_desc = tc::operand_base(s.b_mn);
             const uint32_t a_step = (s.a_mn ? 2048 : 32) >> 4, b_step = (s.b_mn ? 2048 : 32) >> 4;   // 16 values of k
-            int it = 0, n = 0;
+            // (a block's shared addresses have its place in the cluster above bit 23)
+            const uint64_t a_desc = tc::operand_base(s.a_mn) | ((base >> 4) & 0x3fff);
+            const uint64_t b_desc = tc::operand_base(s.b_mn) | (((base + kABytes) >> 4) & 0x3fff);
+            auto multiply = [&](uint32_t acc, int st, bool first) {         // four instructions on stage `st`
+                if (tc::elected()) {
+                    const uint32_t at = static_cast<uint32_t>(st * kStageBytes) >> 4;
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) tc::mma<CG>(acc, a_desc + at + j * a_step, b_desc + at + j * b_step, inst, (j > 0 || !first) ? 1u : 0u);
+                }
+                __syncwarp();
+            };
+            auto finished = [&](uint32_t bar) {
+                if (tc::elected()) tc::commit<CG>(bar);
+                __syncwarp();
+            };
+            int st = 0, n = 0;
+            uint32_t phase = 0;
             for (int u = worker; u < units && fine; u += workers) {
                 const Unit x = unit_of(s, u);
                 const int seg = FORM == kLong ? kSegment : x.k1 - x.k0;
                 for (int kb = x.k0; kb < x.k1 && fine; ++n) {
                     const int set = n & 1, from = kb, to = min(x.k1, kb + seg);
-                    if (!(fine = tc::bar_wait(drained + 8 * set, ((n >> 1) & 1) ^ 1))) break;
+                    if (!(fine = tc::bar_wait<CG == 2>(drained + 8 * set, ((n >> 1) & 1) ^ 1))) break;
                     tc::fence_after();
-                    const uint32_t acc = tmem + set * BN;
-                    for (; kb < to; ++kb, ++it) {
-                        const int st = it % kRing;
-                        if (!(fine = tc::bar_wait(full + 8 * st, (it / kRing) & 1))) break;
+                    for (; kb < to; ++kb) {
+                        if (!(fine = tc::bar_wait(full + 8 * st, phase))) break;
                         tc::fence_after();
-                        const uint32_t a = base + st * kStageBytes;
-                        const uint64_t da = a_desc | ((a >> 4) & 0x3fff), db = b_desc | (((a + 16384) >> 4) & 0x3fff);
-#pragma unroll
-                        for (int j = 0; j < 4; ++j) {
-                            tc::mma<CG>(acc, da + j * a_step, db + j * b_step, inst, (kb > from || j > 0) ? 1u : 0u);
+                        multiply(tmem + set * BN, st, kb == from);
+                        finished(empty + 8 * st);
+                        if (++st == kRing) {
+                            st = 0;
+                            phase ^= 1;
                         }
-                        tc::commit<CG>(empty + 8 * st);
                     }
-                    if (fine) tc::commit<CG>(ready + 8 * set);
+                    if (fine) finished(ready + 8 * set);
                 }
             }
         }
@@ -620,7 +641,7 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
                         tc::send(tc::map_to_rank(landing + ((p / s.splits) * s.splits + share) * kPiece, owner), base + p * kPiece, kPiece,
                                  tc::map_to_rank(landed, owner));
                     }
-                    if (!(fine = tc::bar_wait(landed, 0))) break;
+                    if (!(fine = tc::bar_wait<true>(landed, 0))) break;
                 }
                 for (int p = share + s.splits * (warp - 4); p < static_cast<int>(kPieces); p += s.splits * kEpilogueWarps) {
                     const float4* from = reinterpret_cast<const float4*>(mem + kRingBytes - kLanding + (p / s.splits) * s.splits * kPiece);

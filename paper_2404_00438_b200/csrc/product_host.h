@@ -70,7 +70,7 @@ bool make_map(CUtensorMap* map, const Matrix& a, int* mn_major, int box_rows);
 struct Config {
     int cg, bn, form, whole, splits, split_slices;
 };
-// `sums`: binary32 results, whose long sums are taken in segments.  `alone`: no splits (the epilogue needs whole rows of tiles).
+// `sums`: binary32 results, whose long sums are taken in segments.  `alone`: no splits.
 Config choose(const Call& c, int64_t m, int64_t n, int64_t k, bool sums, bool alone);
 
 // Tile counts of a configuration; false if the tiles cannot be numbered.

@@ -21,6 +21,13 @@ __device__ __forceinline__ uint32_t cluster_rank() {
     return r;
 }
 
+// One lane of a converged warp.
+__device__ __forceinline__ bool elected() {
+    uint32_t p;
+    asm volatile("{\n.reg .pred p;\nelect.sync _|p, 0xffffffff;\nselp.u32 %0, 1, 0, p;\n}" : "=r"(p));
+    return p != 0;
+}
+
 __device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
 __device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
 
@@ -74,32 +81,45 @@ __device__ __forceinline__ void bar_arrive(uint32_t bar) {
     asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
 }
 
+// FAR: what the barrier announces was done by another block of the cluster, which takes the wider scope.
+template <bool FAR>
 __device__ __forceinline__ bool bar_try(uint32_t bar, uint32_t parity) {
     uint32_t ok;
-    asm volatile(
-        "{\n.reg .pred p;\n"
-        "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n"
-        "selp.u32 %0, 1, 0, p;\n}"
-        : "=r"(ok)
-        : "r"(bar), "r"(parity)
-        : "memory");
+    if (FAR) {
+        asm volatile(
+            "{\n.reg .pred p;\n"
+            "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n"
+            "selp.u32 %0, 1, 0, p;\n}"
+            : "=r"(ok)
+            : "r"(bar), "r"(parity)
+            : "memory");
+    } else {
+        asm volatile(
+            "{\n.reg .pred p;\n"
+            "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n"
+            "selp.u32 %0, 1, 0, p;\n}"
+            : "=r"(ok)
+            : "r"(bar), "r"(parity)
+            : "memory");
+    }
     return ok != 0;
 }
 
-// No wait is unbounded: after four seconds it gives up and says so.
+// No wait is unbounded: after four seconds it gives up and says so.  Called by whole warps, whose lanes all get the
+// same answer (what they elect a lane for afterwards needs them together).
 constexpr uint64_t kWaitLimitNs = 4000000000ull;
 
+template <bool FAR = false>
 __device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity) {
-    for (int i = 0; i < 1024; ++i) {
-        if (bar_try(bar, parity)) return true;
-    }
+    bool ok = false;
+    for (int i = 0; i < 1024 && !ok; ++i) ok = bar_try<FAR>(bar, parity);
+    if (__all_sync(0xffffffffu, ok)) return true;
     const uint64_t t0 = nanoseconds();
-    do {
-        for (int i = 0; i < 256; ++i) {
-            if (bar_try(bar, parity)) return true;
-        }
-    } while (nanoseconds() - t0 < kWaitLimitNs);
-    return false;
+    while (true) {
+        for (int i = 0; i < 256 && !ok; ++i) ok = bar_try<FAR>(bar, parity);
+        if (__all_sync(0xffffffffu, ok)) return true;
+        if (__any_sync(0xffffffffu, nanoseconds() - t0 >= kWaitLimitNs)) return false;
+    }
 }
 
 // ---------------------------------------------------------------- tiled copies (global -> shared)
