@@ -62,6 +62,9 @@ Matrix readable(Call& c, const Matrix& a);
 // Both must be readable.  f.m, f.n are set here.
 void product(Call& c, const Matrix& a, const Matrix& b, Finish f);
 
+// The same for at most eight rows of a; false if this is not such a product.  (few_rows.cu)
+bool few_rows(Call& c, const Matrix& a, const Matrix& b, const Finish& f);
+
 inline Matrix transposed(const Matrix& a) { return Matrix{a.p, a.cols, a.rows, a.cs, a.rs}; }
 
 // Tensor map of 64 x `box` tiles; `mn` of the operand's rows adjacent (1) or its columns (0).
