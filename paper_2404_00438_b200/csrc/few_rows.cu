@@ -76,8 +76,8 @@ few_rows_along_k_kernel(const __nv_bfloat16* x, int64_t x_ld, const __nv_bfloat1
     tc::wait_for_previous();
     const __nv_bfloat16* xg = x + g * x_ld;
     const bool token = g < f.m;
-    const int units = (f.n + 31) / 32;
-    for (int u = blockIdx.x; u < units; u += gridDim.x) {
+    {
+        const int u = blockIdx.x;
         const __nv_bfloat16* rows[4];
         bool there[4];
 #pragma unroll
@@ -201,7 +201,7 @@ bool few_rows(Call& c, const Matrix& a, const Matrix& b, const Finish& f) {
     const int k = static_cast<int>(a.cols);
     if (b.cs == 1) {
         const int64_t units = parts(b.rows, 32);
-        start(c, few_rows_along_k_kernel, dim3(static_cast<unsigned>(std::min<int64_t>(units, 3 * c.sms))), dim3(kFewThreads), 0, 1, x, a.rs, w,
+        start(c, few_rows_along_k_kernel, dim3(static_cast<unsigned>(units)), dim3(kFewThreads), 0, 1, x, a.rs, w,
               b.rs, k, f);
     } else {
         // so many blocks a cluster that the SMs have one each, as long as a warp keeps 16 of k

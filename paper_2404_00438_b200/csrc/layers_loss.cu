@@ -212,40 +212,55 @@ __global__ void __launch_bounds__(1024) rows_kernel(const float2* stats, int gro
 // (conversions run at an eighth of the rate of additions)
 __device__ __forceinline__ float code_value(uint32_t c) { return __uint_as_float(0x4b000000u | c) - 8388608.0f; }
 
-// Codes to softmax - [target] in bf16, in place, eight a thread; a block has 2048 columns of a row.  The factor
+// Codes to softmax - [target] in bf16, in place; a block has 8192 columns of a row, a thread four times eight.  The factor
 // g is left to the products' epilogues: rounded into d it would shift the whole gradient by its own rounding,
-// since at the target d is close to -g in every row.
+// since at the target d is close to -g in every row.  Bound by memory, 4 bytes a logit; the rows are taken from the last, of
+// which the L2 still has some.
 __global__ void __launch_bounds__(256) gradient_kernel(uint16_t* codes, int64_t ld, int n, int width, const float2* stats, int64_t m,
                                                        const int64_t* targets, int64_t ignore, const float2* lse) {
     tc::let_next_start();
     tc::wait_for_previous();
-    const int64_t row = blockIdx.y + static_cast<int64_t>(blockIdx.z) * 65535;
-    const int col = (blockIdx.x * 256 + threadIdx.x) * 8;
-    if (row >= m || col >= n) return;
+    const int64_t row = m - 1 - (blockIdx.y + static_cast<int64_t>(blockIdx.z) * 65535);
+    if (row < 0) return;
+    const int col0 = (static_cast<int>(gridDim.x - 1 - blockIdx.x) * 1024 + static_cast<int>(threadIdx.x)) * 8;
+    uint4* p = reinterpret_cast<uint4*>(codes + row * ld + col0);
     const int64_t t = targets[row];
-    uint4* p = reinterpret_cast<uint4*>(codes + row * ld + col);
-    if (t == ignore) {
-        *p = make_uint4(0, 0, 0, 0);
-        return;
-    }
     const float2 l = lse[row];
-    float at = __fmaf_rn(stats[static_cast<int64_t>(col / width) * m + row].x - l.x, kLog2e, -l.y);
-    if (t < 0 || t >= n) at = NAN;
-    const bool none = at == at;             // the last code stands for 0, unless the row is NaN
-    const uint4 u = *p;
-    const uint32_t w[4] = {u.x, u.y, u.z, u.w};
-    uint32_t o[4];
-    const int hit = static_cast<int>(t - col);
+    uint4 u[4];
+    float top[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        const uint32_t ca = w[i] & 0xffffu, cb = w[i] >> 16;
-        float a = ca == 65535u && none ? 0.0f : exp2_fast(__fmaf_rn(code_value(ca), -1.0f / kStep, at));
-        float b = cb == 65535u && none ? 0.0f : exp2_fast(__fmaf_rn(code_value(cb), -1.0f / kStep, at));
-        if (hit == 2 * i) a -= 1.0f;
-        if (hit == 2 * i + 1) b -= 1.0f;
-        o[i] = pack_bf16(a, b);
+        const int col = col0 + i * 2048;
+        if (col < n) {
+            u[i] = p[i * 256];
+            top[i] = stats[static_cast<int64_t>(col / width) * m + row].x;
+        }
     }
-    *p = make_uint4(o[0], o[1], o[2], o[3]);
+    const bool ignored = t == ignore, known = t >= 0 && t < n;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int col = col0 + i * 2048;
+        if (col >= n) break;
+        if (ignored) {
+            p[i * 256] = make_uint4(0, 0, 0, 0);
+            continue;
+        }
+        const float at = known ? __fmaf_rn(top[i] - l.x, kLog2e, -l.y) : NAN;
+        const bool none = at == at;            // the last code stands for 0, unless the row is NaN
+        const uint32_t w[4] = {u[i].x, u[i].y, u[i].z, u[i].w};
+        uint32_t o[4];
+        const int hit = known ? static_cast<int>(t) - col : -1;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const uint32_t ca = w[j] & 0xffffu, cb = w[j] >> 16;
+            float a = ca == 65535u && none ? 0.0f : exp2_fast(__fmaf_rn(code_value(ca), -1.0f / kStep, at));
+            float b = cb == 65535u && none ? 0.0f : exp2_fast(__fmaf_rn(code_value(cb), -1.0f / kStep, at));
+            if (hit == 2 * j) a -= 1.0f;
+            if (hit == 2 * j + 1) b -= 1.0f;
+            o[j] = pack_bf16(a, b);
+        }
+        p[i * 256] = make_uint4(o[0], o[1], o[2], o[3]);
+    }
 }
 
 dlion_status check_loss(const dlion_loss* p) {
@@ -322,7 +337,7 @@ void loss(Call& c, const dlion_loss& p) {
             start(c, rows_kernel, dim3(static_cast<unsigned>(parts(rows, 32))), dim3(1024), 0, 1, stats, groups, rows, p.targets + r,
                   p.ignore_index, p.v, at_target, lse, p.rows + r, end);
             if (grads) {
-                const dim3 grid(static_cast<unsigned>(parts(p.v, 2048)), static_cast<unsigned>(std::min<int64_t>(rows, 65535)),
+                const dim3 grid(static_cast<unsigned>(parts(p.v, 8192)), static_cast<unsigned>(std::min<int64_t>(rows, 65535)),
                                 static_cast<unsigned>(parts(rows, 65535)));
                 start(c, gradient_kernel, grid, dim3(256), 0, 1, codes, ld, p.v, width, stats, rows, p.targets + r, p.ignore_index, lse);
             }
@@ -346,6 +361,7 @@ void loss(Call& c, const dlion_loss& p) {
         fw.out = last ? p.dw : so_far;
         fw.out_ld = last ? p.dw_ld : so_far_ld;
         fw.out_f32 = f32 || !last;
+        fw.rough = 1;
         product(c, transposed(d), transposed(xp), fw);
     }
 }

@@ -191,7 +191,7 @@ void product(Call& c, const Matrix& a, const Matrix& b, Finish f) {
              (f.residual != nullptr ? kResidual : 0u) | (f.accumulated != nullptr ? kAdd : 0u);
     f.wide = aligned16(f.out) && f.out_ld * (f.out_f32 ? 4 : 2) % 16 == 0;
     if (few_rows(c, a, b, f)) return;
-    const Config cfg = choose(c, a.rows, b.rows, a.cols, f.out_f32 != 0, false);
+    const Config cfg = choose(c, a.rows, b.rows, a.cols, f.out_f32 != 0 && f.rough == 0, false);
     Shape s{};
     if (!shape_of(cfg, a, b, &s)) {
         c.status = DLION_EINVAL;

@@ -87,6 +87,7 @@ struct Finish {
     void* out;
     int64_t out_ld;
     int out_f32;
+    int rough;                             // a binary32 result that needs no segments: its operands are rounded already
     float4* parts;                         // sums of split tiles: [tile][block][epilogue warp][split][32 rows x half the columns]
     unsigned int* tickets;                 // [tile][block][epilogue warp], 0 before the call
 };
