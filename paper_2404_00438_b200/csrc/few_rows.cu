@@ -1,8 +1,10 @@
-// Products of one to eight rows (a serving step): every weight is read once and used at most eight times, so the only
-// question is how fast the weights stream.  No shared-memory ring and no copy descriptors: the weights go from global memory
-// straight into the fragments of the warp-level 16 x 8 x 16 matrix instruction, whose k (or n) indices are
-// renamed so that each thread's fragment is 16 adjacent bytes.  (One row on fused multiply-adds would do, eight rows
-// would not: 64 of them, and 8 conversions, for every 16 bytes against the 23 bytes a clock that an SM streams.)
+// Products of one to 32 rows (a serving step): every weight is read once and used a few times, so the only
+// question is how fast the weights stream.  The arithmetic is the warp-level 16 x 8 x 16 matrix instruction with its k (or n)
+// indices renamed so that a thread's share of the weights is 16 adjacent bytes.  Each warp has a ring of its own, filled by
+// tiled copies of whole 128-byte lines, some 160 KB of which are under way on an SM, through the ends of the columns' sums
+// too.  (Shares of 16 bytes loaded by the threads themselves, to registers or to shared memory, cut the lines in half
+// between warps: 8 rows over 50257 x 2048 took 41 to 44 us.  One row on fused multiply-adds would do, eight rows would not: 64 of
+// them, and 8 conversions, for every 16 bytes against the 23 bytes a clock that an SM streams.)
 #include "product_host.h"
 
 namespace dlion {
@@ -10,7 +12,7 @@ namespace prod {
 
 namespace {
 
-constexpr int kFewThreads = 256, kFewWarps = 8, kTokens = 8;
+constexpr int kFewThreads = 256, kFewWarps = 8, kFewRows = 32;
 
 __device__ __forceinline__ void mma_16x8x16(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
     asm volatile(
@@ -19,24 +21,24 @@ __device__ __forceinline__ void mma_16x8x16(float (&c)[4], uint32_t a0, uint32_t
         : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
 
-// eight adjacent values, `valid` of them there (the rest, or all of a negative count, 0); p on 16 bytes
-__device__ __forceinline__ uint4 load8(const __nv_bfloat16* p, int valid) {
-    if (valid >= 8) return __ldg(reinterpret_cast<const uint4*>(p));
-    uint32_t w[4] = {0, 0, 0, 0};
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        if (i < valid) w[i / 2] |= static_cast<uint32_t>(__ldg(reinterpret_cast<const unsigned short*>(p) + i)) << (16 * (i % 2));
-    }
-    return make_uint4(w[0], w[1], w[2], w[3]);
+__device__ __forceinline__ uint4 shared16(uint32_t at) {
+    uint4 v;
+    asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(at) : "memory");
+    return v;
 }
+__device__ __forceinline__ uint32_t shared4(uint32_t at) {
+    uint32_t v;
+    asm volatile("ld.shared.u32 %0, [%1];" : "=r"(v) : "r"(at) : "memory");
+    return v;
+}
+// 16-byte unit c of row r of a tile of 128-byte rows, as the copies exchange them
+__device__ __forceinline__ uint32_t unit_at(int r, int c) { return static_cast<uint32_t>(r * 128 + ((c ^ (r & 7)) << 4)); }
 
 // A row's 32 columns, a lane each, through the rest of the product (see Finish).
-__device__ __forceinline__ void finish_row(const Finish& f, int row, int64_t col, float v) {
+__device__ __forceinline__ void finish_row(const Finish& f, int row, int64_t col, float v, float bias) {
     const bool in = col < f.n;
     if (f.scale != nullptr) v *= *f.scale;
-    if (f.bias != nullptr && in) {
-        v += f.bias_f32 ? static_cast<const float*>(f.bias)[col] : __bfloat162float(static_cast<const __nv_bfloat16*>(f.bias)[col]);
-    }
+    v += bias;
     if (f.keep == DLION_KEEP_8BIT) {
         const uint32_t top = __reduce_max_sync(0xffffffffu, in ? __float_as_uint(v) & 0x7fffffffu : 0u);
         const uint32_t e = block_exponent(top);
@@ -65,150 +67,253 @@ __device__ __forceinline__ void finish_row(const Finish& f, int row, int64_t col
     }
 }
 
-// Weights [n][k], k adjacent.  A block has 32 of the n at a time and its eight warps every eighth 32 of k.  Thread (g, q) = (lane / 4,
-// lane % 4) loads k = 8 q .. 8 q + 7 of rows g, g + 8, g + 16, g + 24 and of token g: as fragments these are k pairs q, and q + 4,
-// of two instructions, the same pairs on both sides.
-__global__ void __launch_bounds__(kFewThreads, 3)
-few_rows_along_k_kernel(const __nv_bfloat16* x, int64_t x_ld, const __nv_bfloat16* w, int64_t w_ld, int k, const __grid_constant__ Finish f) {
-    __shared__ float part[kFewWarps][32][kTokens + 1];
+// A warp's step is 64 of k.
+// ALONG_K: weights [n][k], k adjacent, T x 8 tokens.  A unit is 32 of the n.  Thread (g, q) = (lane / 4, lane % 4) has 16 bytes, k = 8 q ..
+// 8 q + 7 of either half step, of rows g, g + 8, g + 16, g + 24 and of tokens g, g + 8 ..: as fragments these are k pairs q,
+// and q + 4, of two instructions, the same pairs on both sides.
+// Otherwise: weights [k][n], n adjacent, T x 16 tokens.  A unit is 64 of the n.  Thread (g, q) has n = 8 g .. 8 g + 7 of k = 2 q, 2 q + 1,
+// 2 q + 8, 2 q + 9 of either quarter step; column g of the eight instructions' j-th is n = 8 g + j.
+// A block's warps, and a cluster's blocks, share the k of a unit.  What does not exist is copied as 0.
+template <bool ALONG_K, int T>
+struct Few {
+    static constexpr int kUnit = ALONG_K ? 32 : 64;
+    static constexpr int kRows = ALONG_K ? 8 * T : 16 * T;         // tokens
+    static constexpr int kWeights = ALONG_K ? 4096 : 8192;         // bytes of a stage
+    static constexpr int kStage = kWeights + kRows * 128;
+    static constexpr int kAhead = 163840 / (kFewWarps * kStage);
+    static constexpr int kRing = kFewWarps * kAhead * kStage;
+    static constexpr int kPitch = kRows + 1;                       // part[warp][column][token]
+    static constexpr int kPart = kFewWarps * 32 * kPitch * 4;
+    static constexpr int kTotal = kRows * kUnit * 4;
+    static constexpr int kShared = kRing + kPart + kTotal + kFewWarps * kAhead * 8 + 1024;
+};
+
+template <bool ALONG_K, int T>
+__global__ void __launch_bounds__(kFewThreads, 1)
+few_rows_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUtensorMap map_w, int k, int units,
+                const __grid_constant__ Finish f, unsigned int* mark) {
+    using S = Few<ALONG_K, T>;
+    extern __shared__ uint8_t raw[];
+    const uint32_t base = (tc::smem_addr(raw) + 1023u) & ~1023u;
+    uint8_t* mem = raw + (base - tc::smem_addr(raw));
+    float* part = reinterpret_cast<float*>(mem + S::kRing);
+    float* total = part + S::kPart / 4;
     const int lane = threadIdx.x % 32, warp = threadIdx.x / 32, g = lane / 4, q = lane % 4;
+    const uint32_t ring = base + warp * S::kAhead * S::kStage;
+    const uint32_t full = base + S::kRing + S::kPart + S::kTotal + warp * S::kAhead * 8;
+    const int rank = static_cast<int>(tc::cluster_rank()), blocks = static_cast<int>(tc::cluster_size());
+    const int first = static_cast<int>(blockIdx.x) / blocks, apart = static_cast<int>(gridDim.x) / blocks;
+    const int stride = blocks * kFewWarps * 64, from = (rank * kFewWarps + warp) * 64;
+    const int steps = from < k ? (k - from + stride - 1) / stride : 0;         // of this warp, a unit
+    const int mine = first < units ? (units - first + apart - 1) / apart : 0;
     tc::let_next_start();
+    if (lane == 0) {
+        for (int i = 0; i < S::kAhead; ++i) tc::bar_init(full + 8 * i, 1);
+        tc::bar_init_done();
+        tc::prefetch_map(&map_w);
+        tc::prefetch_map(&map_x);
+    }
+    __syncwarp();
     tc::wait_for_previous();
-    const __nv_bfloat16* xg = x + g * x_ld;
-    const bool token = g < f.m;
-    {
-        const int u = blockIdx.x;
-        const __nv_bfloat16* rows[4];
-        bool there[4];
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-            there[r] = u * 32 + g + 8 * r < f.n;
-            rows[r] = w + static_cast<int64_t>(u * 32 + g + 8 * r) * w_ld;
+
+    int ahead_unit = first, ahead_at = from, ahead_left = mine * steps, ahead_stage = 0;
+    auto fetch = [&] {
+        if (ahead_left == 0) return;
+        if (tc::elected()) {
+            const uint32_t to = ring + ahead_stage * S::kStage, bar = full + 8 * ahead_stage;
+            tc::bar_expect(bar, S::kStage);
+            if (ALONG_K) {
+                tc::load_tile<1>(to, &map_w, ahead_at, ahead_unit * 32, bar);
+            } else {
+                tc::load_tile<1>(to, &map_w, ahead_unit * 64, ahead_at, bar);
+            }
+            tc::load_tile<1>(to + S::kWeights, &map_x, ahead_at, 0, bar);
         }
-        float c[2][4] = {};
-#pragma unroll 3
-        for (int at = warp * 32 + q * 8; at < k + 31; at += kFewWarps * 32) {        // whole warps leave together: at - 8 q is a multiple of 32
-            if (at - q * 8 >= k) break;
-            const int valid = k - at;
-            uint4 a[4];
+        __syncwarp();
+        if (++ahead_stage == S::kAhead) ahead_stage = 0;
+        --ahead_left;
+        ahead_at += stride;
+        if (ahead_at >= k) {
+            ahead_at = from;
+            ahead_unit += apart;
+        }
+    };
+#pragma unroll 1
+    for (int i = 0; i < S::kAhead; ++i) fetch();
+
+    int stage = 0;
+    uint32_t phase = 0;
+    bool fine = true;
+    for (int u = first; u < units; u += apart) {
+        float c[T][8][4] = {};                 // along k the first two of eight
+        // asked for now and turned into a number at the unit's end, a load from memory is waited for nowhere
+        // (8 rows over 50257 x 2048: 43 us when loaded at the end)
+        uint32_t bias[S::kUnit / 32] = {};
+        if (f.bias != nullptr) {
 #pragma unroll
-            for (int r = 0; r < 4; ++r) a[r] = load8(rows[r] + at, there[r] ? valid : 0);
-            const uint4 b = load8(xg + at, token ? valid : 0);
-#pragma unroll
-            for (int t = 0; t < 2; ++t) {
-                mma_16x8x16(c[t], a[2 * t].x, a[2 * t + 1].x, a[2 * t].y, a[2 * t + 1].y, b.x, b.y);
-                mma_16x8x16(c[t], a[2 * t].z, a[2 * t + 1].z, a[2 * t].w, a[2 * t + 1].w, b.z, b.w);
+            for (int i = 0; i < S::kUnit / 32; ++i) {
+                const int64_t col = static_cast<int64_t>(u) * S::kUnit + i * 32 + lane;
+                if (col < f.n) {
+                    bias[i] = f.bias_f32 ? static_cast<const uint32_t*>(f.bias)[col] : static_cast<const unsigned short*>(f.bias)[col];
+                }
             }
         }
-        __syncthreads();                       // the previous columns' sums have been read
+#pragma unroll 1
+        for (int i = 0; i < steps; ++i) {
+            fine = fine && tc::bar_wait(full + 8 * stage, phase);
+            const uint32_t w = ring + stage * S::kStage, x = w + S::kWeights;
+            if constexpr (ALONG_K) {
 #pragma unroll
-        for (int t = 0; t < 2; ++t) {
+                for (int half = 0; half < 2; ++half) {
+                    uint4 a[4];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) part[warp][t * 16 + g + 8 * (i / 2)][2 * q + i % 2] = c[t][i];
+                    for (int r = 0; r < 4; ++r) a[r] = shared16(w + unit_at(g + 8 * r, 4 * half + q));
+#pragma unroll
+                    for (int t = 0; t < T; ++t) {
+                        const uint4 b = shared16(x + unit_at(g + 8 * t, 4 * half + q));
+#pragma unroll
+                        for (int h = 0; h < 2; ++h) {
+                            mma_16x8x16(c[t][h], a[2 * h].x, a[2 * h + 1].x, a[2 * h].y, a[2 * h + 1].y, b.x, b.y);
+                            mma_16x8x16(c[t][h], a[2 * h].z, a[2 * h + 1].z, a[2 * h].w, a[2 * h + 1].w, b.z, b.w);
+                        }
+                    }
+                }
+            } else {
+#pragma unroll
+                for (int part4 = 0; part4 < 4; ++part4) {
+                    uint32_t r[4][4], a[T][4];
+#pragma unroll
+                    for (int i4 = 0; i4 < 4; ++i4) {
+                        const uint4 v = shared16(w + unit_at(16 * part4 + 2 * q + 8 * (i4 / 2) + i4 % 2, g));
+                        r[i4][0] = v.x, r[i4][1] = v.y, r[i4][2] = v.z, r[i4][3] = v.w;
+                    }
+#pragma unroll
+                    for (int t = 0; t < T; ++t) {
+#pragma unroll
+                        for (int i4 = 0; i4 < 4; ++i4) {      // tokens g, g + 8; k 2 q and 2 q + 8: word q of two units
+                            a[t][i4] = shared4(x + unit_at(16 * t + g + 8 * (i4 % 2), 2 * part4 + i4 / 2) + 4 * q);
+                        }
+                    }
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        const uint32_t e0 = __byte_perm(r[0][j], r[1][j], 0x5410), e1 = __byte_perm(r[2][j], r[3][j], 0x5410);
+                        const uint32_t o0 = __byte_perm(r[0][j], r[1][j], 0x7632), o1 = __byte_perm(r[2][j], r[3][j], 0x7632);
+#pragma unroll
+                        for (int t = 0; t < T; ++t) {
+                            mma_16x8x16(c[t][2 * j], a[t][0], a[t][1], a[t][2], a[t][3], e0, e1);
+                            mma_16x8x16(c[t][2 * j + 1], a[t][0], a[t][1], a[t][2], a[t][3], o0, o1);
+                        }
+                    }
+                }
+            }
+            __syncwarp();                      // the stage has been read
+            if (++stage == S::kAhead) {
+                stage = 0;
+                phase ^= 1;
+            }
+            fetch();
         }
-        __syncthreads();
-        if (warp < f.m) {
-            float v = 0.0f;
+        // the warps' sums, 32 columns at a time, then the blocks'
 #pragma unroll
-            for (int i = 0; i < kFewWarps; ++i) v += part[i][lane][warp];
-            finish_row(f, warp, static_cast<int64_t>(u) * 32 + lane, v);
+        for (int half = 0; half < S::kUnit / 32; ++half) {
+            __syncthreads();                   // what was in `part` has been read
+            float* to = part + warp * 32 * S::kPitch;
+            if constexpr (ALONG_K) {
+#pragma unroll
+                for (int t = 0; t < T; ++t) {
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) to[(h * 16 + g + 8 * (i / 2)) * S::kPitch + 8 * t + 2 * q + i % 2] = c[t][h][i];
+                    }
+                }
+            } else if (q / 2 == half) {
+#pragma unroll
+                for (int t = 0; t < T; ++t) {
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) {
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) to[(16 * (q % 2) + 8 * (i % 2) + j) * S::kPitch + 16 * t + g + 8 * (i / 2)] = c[t][j][i];
+                    }
+                }
+            }
+            __syncthreads();
+#pragma unroll 1
+            for (int t = warp; t < f.m; t += kFewWarps) {
+                float v = 0.0f;
+#pragma unroll
+                for (int i = 0; i < kFewWarps; ++i) v += part[(i * 32 + lane) * S::kPitch + t];
+                total[t * S::kUnit + half * 32 + lane] = v;
+            }
+        }
+        if (blocks > 1) tc::cluster_sync();
+#pragma unroll 1
+        for (int t = warp; t < f.m; t += kFewWarps) {          // the row's own warp, or after the cluster's barrier
+            if (t % blocks != rank) continue;
+#pragma unroll
+            for (int i = 0; i < S::kUnit / 32; ++i) {
+                float v = 0.0f;
+                if (blocks == 1) {
+                    v = total[t * S::kUnit + i * 32 + lane];
+                } else {
+                    const uint32_t here = tc::smem_addr(total + t * S::kUnit + i * 32 + lane);
+#pragma unroll 4
+                    for (int r = 0; r < blocks; ++r) v += tc::load_cluster(tc::map_to_rank(here, static_cast<uint32_t>(r)));
+                }
+                const int64_t col0 = static_cast<int64_t>(u) * S::kUnit + i * 32;
+                if (col0 < f.n) finish_row(f, t, col0 + lane, v, __uint_as_float(f.bias_f32 ? bias[i] : bias[i] << 16));
+            }
+        }
+        if (blocks > 1) tc::cluster_sync();    // the sums stay until they are read
+    }
+    if (!fine) {                               // a wait ran out: copies may still be on their way
+        *mark = 1;
+        const uint64_t t0 = tc::nanoseconds();
+        while (tc::nanoseconds() - t0 < 50000000ull) {
         }
     }
 }
 
-// Weights [k][n], n adjacent.  A cluster has 64 of the n, its warps every so many 16 of k.  Thread (g, q) loads n = 8 g .. 8 g + 7 of k =
-// 2 q, 2 q + 1, 2 q + 8, 2 q + 9; column g of the eight instructions' j-th is n = 8 g + j.
-__global__ void __launch_bounds__(kFewThreads, 3)
-few_rows_along_n_kernel(const __nv_bfloat16* x, int64_t x_ld, const __nv_bfloat16* w, int64_t w_ld, int k, const __grid_constant__ Finish f) {
-    __shared__ float part[kFewWarps][kTokens][65];
-    __shared__ float total[kTokens][64];
-    const int lane = threadIdx.x % 32, warp = threadIdx.x / 32, g = lane / 4, q = lane % 4;
-    const int rank = static_cast<int>(tc::cluster_rank()), blocks = static_cast<int>(tc::cluster_size());
-    const int n0 = static_cast<int>(blockIdx.x) / blocks * 64, cols = f.n - n0 - g * 8;
-    tc::let_next_start();
-    tc::wait_for_previous();
-    const __nv_bfloat16* xg = x + g * x_ld;
-    const __nv_bfloat16* wg = w + n0 + g * 8;
-    const bool token = g < f.m;
-    float c[8][4] = {};
-#pragma unroll 2
-    for (int at = (rank * kFewWarps + warp) * 16; at < k; at += blocks * kFewWarps * 16) {
-        uint4 b[4];
-        uint32_t a[2];
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            const int k0 = at + 2 * q + 8 * h;
-            b[2 * h] = load8(wg + static_cast<int64_t>(k0) * w_ld, k0 < k ? cols : 0);
-            b[2 * h + 1] = load8(wg + static_cast<int64_t>(k0 + 1) * w_ld, k0 + 1 < k ? cols : 0);
-            if (!token || k0 >= k) {
-                a[h] = 0;
-            } else if (k0 + 1 < k) {
-                a[h] = __ldg(reinterpret_cast<const unsigned int*>(xg + k0));
-            } else {
-                a[h] = __ldg(reinterpret_cast<const unsigned short*>(xg + k0));
-            }
-        }
-        const uint32_t r0[4] = {b[0].x, b[0].y, b[0].z, b[0].w}, r1[4] = {b[1].x, b[1].y, b[1].z, b[1].w};
-        const uint32_t r2[4] = {b[2].x, b[2].y, b[2].z, b[2].w}, r3[4] = {b[3].x, b[3].y, b[3].z, b[3].w};
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            mma_16x8x16(c[2 * i], a[0], 0u, a[1], 0u, __byte_perm(r0[i], r1[i], 0x5410), __byte_perm(r2[i], r3[i], 0x5410));
-            mma_16x8x16(c[2 * i + 1], a[0], 0u, a[1], 0u, __byte_perm(r0[i], r1[i], 0x7632), __byte_perm(r2[i], r3[i], 0x7632));
+template <bool ALONG_K, int T>
+void start_few(Call& c, const Matrix& a, const Matrix& b, const Finish& f) {
+    using S = Few<ALONG_K, T>;
+    auto* kernel = &few_rows_kernel<ALONG_K, T>;
+    raise_shared(c, kernel, S::kShared);
+    CUtensorMap mx, mw;
+    int mn = 0;
+    if (!make_map(&mx, a, &mn, S::kRows) || !make_map(&mw, b, &mn, 32)) {
+        c.status = DLION_ECUDA;
+        return;
+    }
+    const int k = static_cast<int>(a.cols);
+    const int64_t units = parts(b.rows, S::kUnit);
+    // Clocks: an SM takes in 60 bytes a clock, all of them 3400; sharing k among the blocks of a cluster costs some 3500.
+    int blocks = 1;
+    double least = 1e300;
+    for (int n = 1; n <= 8; n *= 2) {
+        if (n > 1 && k <= (n / 2) * kFewWarps * 64) break;
+        const double rounds = static_cast<double>(parts(units, std::max<int64_t>(1, c.sms / n)));
+        const double t = std::max(rounds * S::kUnit * 2.0 * k / n / 60.0, 2.0 * k * b.rows / 3400.0) + (n > 1 ? 3500.0 * rounds : 0.0);
+        if (t < least) {
+            least = t;
+            blocks = n;
         }
     }
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-        part[warp][g][16 * q + j] = c[j][0];
-        part[warp][g][16 * q + 8 + j] = c[j][1];
-    }
-    __syncthreads();
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-        float v = 0.0f;
-#pragma unroll
-        for (int s = 0; s < kFewWarps; ++s) v += part[s][warp][i * 32 + lane];
-        total[warp][i * 32 + lane] = v;
-    }
-    if (blocks > 1) {
-        tc::cluster_sync();
-    } else {
-        __syncwarp();
-    }
-    if (warp < f.m && warp % blocks == rank) {
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            float v = 0.0f;
-            if (blocks == 1) {
-                v = total[warp][i * 32 + lane];
-            } else {
-                const uint32_t mine = tc::smem_addr(&total[warp][i * 32 + lane]);
-                for (int r = 0; r < blocks; ++r) v += tc::load_cluster(tc::map_to_rank(mine, static_cast<uint32_t>(r)));
-            }
-            if (n0 + i * 32 < f.n) finish_row(f, warp, static_cast<int64_t>(n0) + i * 32 + lane, v);
-        }
-    }
-    if (blocks > 1) tc::cluster_sync();        // the sums stay until they are read
+    const int64_t clusters = std::min<int64_t>(units, std::max<int64_t>(1, c.sms / blocks));
+    start(c, kernel, dim3(static_cast<unsigned>(clusters * blocks)), dim3(kFewThreads), S::kShared, blocks, mx, mw, k, units, f, c.mark);
 }
 
 }  // namespace
 
 // Rows of k adjacent on both the tokens' side and one of the weights' two orders; nothing accumulated.
 bool few_rows(Call& c, const Matrix& a, const Matrix& b, const Finish& f) {
-    if (a.rows > kTokens || (a.cs != 1 && a.cols != 1) || f.accumulated != nullptr) return false;
+    // (a single column's rows may be neighbours: those are not on the 16-byte grid)
+    if (a.rows > kFewRows || a.cs != 1 || (a.rows > 1 && a.rs % 8 != 0) || f.accumulated != nullptr) return false;
     if (!c.live()) return true;
-    const auto* x = static_cast<const __nv_bfloat16*>(a.p);
-    const auto* w = static_cast<const __nv_bfloat16*>(b.p);
-    const int k = static_cast<int>(a.cols);
     if (b.cs == 1) {
-        const int64_t units = parts(b.rows, 32);
-        start(c, few_rows_along_k_kernel, dim3(static_cast<unsigned>(units)), dim3(kFewThreads), 0, 1, x, a.rs, w,
-              b.rs, k, f);
+        a.rows <= 8 ? start_few<true, 1>(c, a, b, f) : a.rows <= 16 ? start_few<true, 2>(c, a, b, f) : start_few<true, 4>(c, a, b, f);
     } else {
-        // so many blocks a cluster that the SMs have one each, as long as a warp keeps 16 of k
-        const int64_t units = parts(b.rows, 64);
-        int blocks = 1;
-        while (blocks < 8 && units * blocks < c.sms && k > blocks * kFewWarps * 16) blocks *= 2;
-        start(c, few_rows_along_n_kernel, dim3(static_cast<unsigned>(units * blocks)), dim3(kFewThreads), 0, blocks, x, a.rs, w, b.cs, k, f);
+        a.rows <= 16 ? start_few<false, 1>(c, a, b, f) : start_few<false, 2>(c, a, b, f);
     }
     return true;
 }

@@ -62,7 +62,7 @@ Matrix readable(Call& c, const Matrix& a);
 // Both must be readable.  f.m, f.n are set here.
 void product(Call& c, const Matrix& a, const Matrix& b, Finish f);
 
-// The same for at most eight rows of a; false if this is not such a product.  (few_rows.cu)
+// The same for at most 32 rows of a; false if this is not such a product.  (few_rows.cu)
 bool few_rows(Call& c, const Matrix& a, const Matrix& b, const Finish& f);
 
 inline Matrix transposed(const Matrix& a) { return Matrix{a.p, a.cols, a.rows, a.cs, a.rs}; }
@@ -99,15 +99,30 @@ void start(Call& c, void (*kernel)(P...), dim3 grid, dim3 block, size_t shared, 
     c.check(cudaLaunchKernelEx(&cfg, kernel, static_cast<P>(args)...));
 }
 
+// More than 48 KB of shared memory for a kernel, asked for once a device.
+template <class K>
+void raise_shared(Call& c, K* kernel, int bytes) {
+    struct Entry {
+        std::atomic<const void*> kernel{nullptr};
+        std::atomic<uint64_t> devices{0};
+    };
+    static Entry entries[16];                  // of kernels of this type
+    const uint64_t bit = uint64_t{1} << (c.device & 63);
+    for (Entry& e : entries) {
+        const void* seen = nullptr;
+        if (!e.kernel.compare_exchange_strong(seen, reinterpret_cast<const void*>(kernel)) && seen != reinterpret_cast<const void*>(kernel)) continue;
+        if ((e.devices.load(std::memory_order_acquire) & bit) != 0) return;
+        c.check(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes));
+        if (c.status == DLION_OK) e.devices.fetch_or(bit, std::memory_order_release);
+        return;
+    }
+    c.check(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes));
+}
+
 template <int CG, int BN, class E, int FORM>
 void launch(Call& c, const CUtensorMap& ma, const CUtensorMap& mb, const Shape& s, const typename E::Args& f) {
     auto* kernel = &product_kernel<CG, BN, E, FORM>;
-    static std::atomic<uint64_t> ready{0};     // devices whose limit of shared memory has been raised for this kernel
-    const uint64_t bit = uint64_t{1} << (c.device & 63);
-    if ((ready.load(std::memory_order_relaxed) & bit) == 0) {
-        c.check(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem));
-        if (c.status == DLION_OK && c.device < 64) ready.fetch_or(bit, std::memory_order_relaxed);
-    }
+    raise_shared(c, kernel, kSmem);
     const int64_t units = s.whole + (static_cast<int64_t>(s.tiles_m) * s.tiles_n - s.whole) * s.splits;
     const int64_t blocks = FORM == kJoined ? units : std::min<int64_t>(units, c.sms / CG) * CG;
     start(c, kernel, dim3(static_cast<unsigned>(blocks)), dim3(kThreads), kSmem, FORM == kJoined ? s.splits : CG, ma, mb, s, f, c.mark);
