@@ -110,30 +110,35 @@ struct LossTile {
     }
 };
 
-__device__ __forceinline__ float block_sum(float v, float* shared) {       // 1024 threads, fixed order
+constexpr int kRowThreads = 256;
+
+__device__ __forceinline__ float block_sum(float v, float* shared) {       // kRowThreads threads, fixed order
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
     if (threadIdx.x % 32 == 0) shared[threadIdx.x / 32] = v;
     __syncthreads();
-    v = shared[threadIdx.x % 32];
+    v = 0.0f;
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
-    __syncthreads();
+    for (int i = 0; i < kRowThreads / 32; ++i) v += shared[i];
     return v;
 }
 
-__device__ __forceinline__ int block_count(const int64_t* targets, int64_t m, int64_t ignore, int* shared) {      // 1024 threads
+__device__ __forceinline__ int block_count(const int64_t* targets, int64_t m, int64_t ignore, int* shared) {
     int n = 0;
-    for (int64_t i = threadIdx.x; i < m; i += 1024) n += targets[i] != ignore;
+#pragma unroll 8
+    for (int64_t i = threadIdx.x; i < m; i += kRowThreads) n += targets[i] != ignore;
     n = __reduce_add_sync(0xffffffffu, n);
     if (threadIdx.x % 32 == 0) shared[threadIdx.x / 32] = n;
     __syncthreads();
-    return __reduce_add_sync(0xffffffffu, shared[threadIdx.x % 32]);
+    n = 0;
+#pragma unroll
+    for (int i = 0; i < kRowThreads / 32; ++i) n += shared[i];
+    return n;
 }
 
 // factor[0] = scale / (rows with a target), where it is needed before the first piece's rows are done
-__global__ void __launch_bounds__(1024) factor_kernel(const int64_t* targets, int64_t m, int64_t ignore, int mean, float scale, float* factor) {
-    __shared__ int counts[32];
+__global__ void __launch_bounds__(kRowThreads) factor_kernel(const int64_t* targets, int64_t m, int64_t ignore, int mean, float scale, float* factor) {
+    __shared__ int counts[kRowThreads / 32];
     tc::let_next_start();
     tc::wait_for_previous();
     const int n = block_count(targets, m, ignore, counts);
@@ -152,33 +157,45 @@ struct Last {
     float* factor;                         // nullable
 };
 
-// Joins the groups of 32 rows a block (lane = row, a warp every 32nd group): each row's maximum, the sum's logarithm in
-// octaves, and the loss.
-__global__ void __launch_bounds__(1024) rows_kernel(const float2* stats, int groups, int64_t m, const int64_t* targets, int64_t ignore,
-                                                    int64_t v, const float* at_target, float2* lse, float* rows, const Last end) {
-    __shared__ float2 part[32][33];
+// Joins the groups of eight rows a block: thread (i, r) = (thread / 8, thread % 8) takes every 32nd group of row r, eight at a
+// time; then each row's maximum, the sum's logarithm in octaves, and the loss.
+__global__ void __launch_bounds__(kRowThreads) rows_kernel(const float2* stats, int groups, int64_t m, const int64_t* targets, int64_t ignore,
+                                                           int64_t v, const float* at_target, float2* lse, float* rows, const Last end) {
+    constexpr int kEvery = kRowThreads / 8, kBatch = 8;
+    __shared__ float2 part[kEvery][9];
     tc::let_next_start();
     tc::wait_for_previous();
-    const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
-    const int64_t row = static_cast<int64_t>(blockIdx.x) * 32 + lane;
+    const int r = threadIdx.x % 8, i = threadIdx.x / 8;
+    const int64_t row = static_cast<int64_t>(blockIdx.x) * 8 + r;
     float top = -INFINITY, sum = 0.0f;
     if (row < m) {
-#pragma unroll 4
-        for (int g = warp; g < groups; g += 32) {
-            const float2 s = stats[g * m + row];
-            const float t = fmaxf(top, s.x);
-            sum = sum * exp2_fast((top - t) * kLog2e) + s.y * exp2_fast((s.x - t) * kLog2e);
+        for (int g = i; g < groups; g += kEvery * kBatch) {
+            float2 s[kBatch];
+#pragma unroll
+            for (int j = 0; j < kBatch; ++j) {
+                s[j] = g + j * kEvery < groups ? stats[static_cast<int64_t>(g + j * kEvery) * m + row] : make_float2(-INFINITY, 0.0f);
+            }
+            float t = top;
+#pragma unroll
+            for (int j = 0; j < kBatch; ++j) t = fmaxf(t, s[j].x);
+            sum *= exp2_fast((top - t) * kLog2e);
+#pragma unroll
+            for (int j = 0; j < kBatch; ++j) {
+                if (s[j].x != -INFINITY) sum += s[j].y * exp2_fast((s[j].x - t) * kLog2e);
+            }
             top = t;
         }
     }
-    part[warp][lane] = make_float2(top, sum);
+    part[i][r] = make_float2(top, sum);
     __syncthreads();
-    if (warp == 0 && row < m) {
-        for (int i = 0; i < 32; ++i) top = fmaxf(top, part[i][lane].x);
+    if (threadIdx.x < 8 && row < m) {
+#pragma unroll
+        for (int j = 0; j < kEvery; ++j) top = fmaxf(top, part[j][r].x);
         sum = 0.0f;
-        for (int i = 0; i < 32; ++i) {
-            const float2 s = part[i][lane];
-            if (s.x != -INFINITY) sum += s.y * exp2_fast((s.x - top) * kLog2e);     // a warp without a group has none
+#pragma unroll
+        for (int j = 0; j < kEvery; ++j) {
+            const float2 s = part[j][r];
+            if (s.x != -INFINITY) sum += s.y * exp2_fast((s.x - top) * kLog2e);     // a thread without a group has none
         }
         const float log_sum = logf(sum);
         const int64_t t = targets[row];
@@ -190,8 +207,8 @@ __global__ void __launch_bounds__(1024) rows_kernel(const float2* stats, int gro
     }
     if (end.loss == nullptr && end.factor == nullptr) return;
     __shared__ unsigned int before;
-    __shared__ int counts[32];
-    __shared__ float sums[32];
+    __shared__ int counts[kRowThreads / 32];
+    __shared__ float sums[kRowThreads / 32];
     __threadfence();
     __syncthreads();
     if (threadIdx.x == 0) before = atomicAdd(end.blocks_done, 1u);
@@ -201,7 +218,8 @@ __global__ void __launch_bounds__(1024) rows_kernel(const float2* stats, int gro
     const int n = block_count(end.targets, end.m, ignore, counts);
     float total = 0.0f;
     if (end.loss != nullptr) {
-        for (int64_t i = threadIdx.x; i < end.m; i += 1024) total += __ldcg(end.rows + i);
+#pragma unroll 8
+        for (int64_t j = threadIdx.x; j < end.m; j += kRowThreads) total += __ldcg(end.rows + j);
         total = block_sum(total, sums);
     }
     if (threadIdx.x != 0) return;
@@ -305,7 +323,7 @@ void loss(Call& c, const dlion_loss& p) {
     uint16_t* codes = grads ? c.ws.take<uint16_t>(static_cast<uint64_t>(step) * ld) : nullptr;
     float* sums = grads && !f32 && step < p.m ? c.ws.take<float>(static_cast<uint64_t>(p.v) * p.h) : nullptr;
     if (grads && step < p.m && c.live()) {
-        start(c, factor_kernel, dim3(1), dim3(1024), 0, 1, p.targets, p.m, p.ignore_index, p.mean, p.scale, factor);
+        start(c, factor_kernel, dim3(1), dim3(kRowThreads), 0, 1, p.targets, p.m, p.ignore_index, p.mean, p.scale, factor);
     }
     for (int64_t r = 0; r < p.m; r += step) {
         const int64_t rows = std::min(step, p.m - r);
@@ -334,7 +352,7 @@ void loss(Call& c, const dlion_loss& p) {
             if (c.status != DLION_OK) return;
             const Last end{blocks_done, p.rows, p.targets, p.m, p.mean, p.scale, r + rows >= p.m ? p.loss : nullptr,
                            grads && step >= p.m ? factor : nullptr};
-            start(c, rows_kernel, dim3(static_cast<unsigned>(parts(rows, 32))), dim3(1024), 0, 1, stats, groups, rows, p.targets + r,
+            start(c, rows_kernel, dim3(static_cast<unsigned>(parts(rows, 8))), dim3(kRowThreads), 0, 1, stats, groups, rows, p.targets + r,
                   p.ignore_index, p.v, at_target, lse, p.rows + r, end);
             if (grads) {
                 const dim3 grid(static_cast<unsigned>(parts(p.v, 8192)), static_cast<unsigned>(std::min<int64_t>(rows, 65535)),

@@ -18,8 +18,6 @@ from typing import NamedTuple, Optional, Tuple, Union
 
 import torch
 
-from torch.cuda import current_device as _current_device
-
 from . import dlion as _dlion
 from .dlion import DlionError, GRAD_BF16, GRAD_F32, OK
 
@@ -75,8 +73,14 @@ def _bind(lib):
 
 _lib = _bind(_dlion.lib())
 
-# the current stream's handle without the Stream object around it, where torch offers that
+# the current stream's handle and device without the objects and checks around them, where torch offers that
 _stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda device: torch.cuda.current_stream(device).cuda_stream)
+_current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
+_Tensor, _empty = torch.Tensor, torch.empty
+_FORWARD = (_lib.dlion_linear_forward_workspace, _lib.dlion_linear_forward)
+_BACKWARD = (_lib.dlion_linear_backward_workspace, _lib.dlion_linear_backward)
+_LOSS = (_lib.dlion_lm_loss_workspace, _lib.dlion_lm_loss)
+_ONLY_BF16 = (_BF16,)
 
 
 class Checkpoint8(NamedTuple):
@@ -108,7 +112,7 @@ def _device(t, name: str) -> int:
 def _matrix(t, name: str, device: int, dtypes, shape, adjacent: bool = False) -> None:
     """Raises unless ``t`` is a tensor of ``shape`` and of one of ``dtypes`` on ``device`` (``adjacent``: with
     adjacent columns and rows that do not overlap)."""
-    if not (isinstance(t, torch.Tensor) and t.dtype in dtypes and t.shape == shape and t.get_device() == device):
+    if not (isinstance(t, _Tensor) and t.dtype in dtypes and t.shape == shape and t.get_device() == device):
         _refused(t, name, device, dtypes, shape)
     if adjacent and not t.is_contiguous():
         rs, cs = t.stride()
@@ -117,7 +121,7 @@ def _matrix(t, name: str, device: int, dtypes, shape, adjacent: bool = False) ->
 
 
 def _vector(t, name: str, device: int, dtypes, n: int) -> None:
-    if not (isinstance(t, torch.Tensor) and t.dtype in dtypes and t.shape == (n,) and t.get_device() == device):
+    if not (isinstance(t, _Tensor) and t.dtype in dtypes and t.shape == (n,) and t.get_device() == device):
         _refused(t, name, device, dtypes, (n,))
     if not t.is_contiguous():
         raise ValueError(f"{name}: expected {n} adjacent values, got strides {t.stride()}")
@@ -134,9 +138,10 @@ def _refused(t, name: str, device: int, dtypes, shape) -> None:
 
 
 def _two_dim(t, name: str) -> Tuple[int, int]:
-    if t.dim() != 2:
+    shape = t.shape
+    if len(shape) != 2:
         raise ValueError(f"{name}: expected a matrix, got {t.dim()} dimensions")
-    return t.shape
+    return shape
 
 
 def _enumerator(table, value, name: str) -> int:
@@ -150,12 +155,13 @@ def _grad_type(dtype) -> int:
     return _enumerator(_TYPES, dtype, "grad_dtype")
 
 
-def _call(size, call, args, device: int, workspace: Optional[torch.Tensor]) -> None:
+def _call(calls, args, device: int, workspace: Optional[torch.Tensor]) -> None:
+    size, call = calls
     ref = ctypes.byref(args)
     need = size(ref)
     if workspace is None:
         if need:
-            workspace = torch.empty(need, dtype=torch.uint8, device=device)
+            workspace = _empty(need, dtype=torch.uint8, device=device)
     else:
         _dlion.check_tensor(workspace, "workspace", (torch.uint8,), need, device)
     st = call(ref, workspace.data_ptr() if need else None, need, _stream(device))
@@ -177,12 +183,12 @@ def linear_forward(x: torch.Tensor, w: torch.Tensor, bias: Optional[torch.Tensor
     device = _device(x, "x")
     m, k = _two_dim(x, "x")
     n = _two_dim(w, "w")[1]
-    _matrix(x, "x", device, (_BF16,), (m, k))
-    _matrix(w, "w", device, (_BF16,), (k, n))
+    _matrix(x, "x", device, _ONLY_BF16, (m, k))
+    _matrix(w, "w", device, _ONLY_BF16, (k, n))
     if bias is not None:
         _vector(bias, "bias", device, _TYPES, n)
     if residual is not None:
-        _matrix(residual, "residual", device, (_BF16,), (m, n), True)
+        _matrix(residual, "residual", device, _ONLY_BF16, (m, n), True)
     a, how = _enumerator(ACTS, act, "act"), _enumerator(KEEPS, keep, "keep")
     if out is None:
         if out_dtype not in _TYPES:
@@ -203,7 +209,7 @@ def linear_forward(x: torch.Tensor, w: torch.Tensor, bias: Optional[torch.Tensor
                     0 if bias is None else _TYPES[bias.dtype], a, _ptr(residual),
                     0 if residual is None else residual.stride(0), out.data_ptr(), out.stride(0), _TYPES[out.dtype],
                     how, _ptr(q), n, _ptr(e), m)
-    _call(_lib.dlion_linear_forward_workspace, _lib.dlion_linear_forward, args, device, workspace)
+    _call(_FORWARD, args, device, workspace)
     return out if kept is None else (out, kept)
 
 
@@ -219,8 +225,8 @@ def linear_backward(dy: torch.Tensor, w: torch.Tensor, saved: Union[torch.Tensor
     device = _device(dy, "dy")
     m, n = _two_dim(dy, "dy")
     k = _two_dim(w, "w")[0]
-    _matrix(dy, "dy", device, (_BF16,), (m, n))
-    _matrix(w, "w", device, (_BF16,), (k, n))
+    _matrix(dy, "dy", device, _ONLY_BF16, (m, n))
+    _matrix(w, "w", device, _ONLY_BF16, (k, n))
     a = _enumerator(ACTS, act, "act")
     u = e = None
     u_ld = e_ld = 0
@@ -232,12 +238,12 @@ def linear_backward(dy: torch.Tensor, w: torch.Tensor, saved: Union[torch.Tensor
         u_ld, e_ld = u.stride(0), e.stride(0)
     elif saved is not None:
         u = saved
-        _matrix(u, "saved", device, (_BF16,), (m, k), True)
+        _matrix(u, "saved", device, _ONLY_BF16, (m, k), True)
         u_ld = u.stride(0)
     elif need_dw or (need_dx and a):
         raise ValueError("saved: needed for dw, and for dx behind an activation")
     if residual is not None:
-        _matrix(residual, "residual", device, (_BF16,), (m, k), True)
+        _matrix(residual, "residual", device, _ONLY_BF16, (m, k), True)
     g = _grad_type(grad_dtype)
     ys, ws, gs = dy.stride(), w.stride(), (0, 0)
     if not need_dx:
@@ -245,7 +251,7 @@ def linear_backward(dy: torch.Tensor, w: torch.Tensor, saved: Union[torch.Tensor
     elif dx is None:
         dx = dy.new_empty((m, k))
     else:
-        _matrix(dx, "dx", device, (_BF16,), (m, k), True)
+        _matrix(dx, "dx", device, _ONLY_BF16, (m, k), True)
     if not need_dw:
         dw = None
     elif dw is None:
@@ -267,7 +273,7 @@ def linear_backward(dy: torch.Tensor, w: torch.Tensor, saved: Union[torch.Tensor
     args = _Backward(m, k, n, dy.data_ptr(), ys[0], ys[1], w.data_ptr(), ws[0], ws[1], a, how, _ptr(u), u_ld, _ptr(e), e_ld,
                      _ptr(residual), 0 if residual is None else residual.stride(0), _ptr(dx),
                      0 if dx is None else dx.stride(0), _ptr(dw), gs[0], gs[1], _ptr(db), g)
-    _call(_lib.dlion_linear_backward_workspace, _lib.dlion_linear_backward, args, device, workspace)
+    _call(_BACKWARD, args, device, workspace)
     return dx, dw, db
 
 
@@ -280,13 +286,15 @@ def checkpoint8(x: torch.Tensor, out: Optional[Checkpoint8] = None) -> Checkpoin
     """``x`` (bf16 [m, k], adjacent columns) in the 8-bit form."""
     device = _device(x, "x")
     m, k = _two_dim(x, "x")
-    _matrix(x, "x", device, (_BF16,), (m, k), True)
+    _matrix(x, "x", device, _ONLY_BF16, (m, k), True)
     if out is None:
-        out = Checkpoint8(x.new_empty((m, k), dtype=torch.int8),
-                          x.new_empty((-(-k // BLOCK8), m), dtype=torch.uint8))
-    _checkpoint(out, "out", device, m, k)
-    st = _lib.dlion_checkpoint8(x.data_ptr(), x.stride(0), m, k, out.q.data_ptr(), out.q.stride(0), out.e.data_ptr(),
-                                out.e.stride(0), _stream(device))
+        q, e = x.new_empty((m, k), dtype=torch.int8), x.new_empty((-(-k // BLOCK8), m), dtype=torch.uint8)
+        out, q_ld, e_ld = Checkpoint8(q, e), k, m
+    else:
+        _checkpoint(out, "out", device, m, k)
+        q, e = out
+        q_ld, e_ld = q.stride(0), e.stride(0)
+    st = _lib.dlion_checkpoint8(x.data_ptr(), x.stride(0), m, k, q.data_ptr(), q_ld, e.data_ptr(), e_ld, _stream(device))
     if st != OK:
         raise DlionError(st, "dlion_checkpoint8")
     return out
@@ -300,10 +308,11 @@ def restore8(c: Checkpoint8, out: Optional[torch.Tensor] = None) -> torch.Tensor
     m, k = _two_dim(c.q, "q")
     _checkpoint(c, "c", device, m, k)
     if out is None:
-        out = torch.empty((m, k), dtype=_BF16, device=device)
-    _matrix(out, "out", device, (_BF16,), (m, k), True)
-    st = _lib.dlion_restore8(c.q.data_ptr(), c.q.stride(0), c.e.data_ptr(), c.e.stride(0), m, k, out.data_ptr(),
-                             out.stride(0), _stream(device))
+        out, x_ld = c.q.new_empty((m, k), dtype=_BF16), k
+    else:
+        _matrix(out, "out", device, _ONLY_BF16, (m, k), True)
+        x_ld = out.stride(0)
+    st = _lib.dlion_restore8(c.q.data_ptr(), c.q.stride(0), c.e.data_ptr(), c.e.stride(0), m, k, out.data_ptr(), x_ld, _stream(device))
     if st != OK:
         raise DlionError(st, "dlion_restore8")
     return out
@@ -321,8 +330,8 @@ def lm_loss(x: torch.Tensor, w: torch.Tensor, targets: torch.Tensor, *, ignore_i
     device = _device(x, "x")
     m, h = _two_dim(x, "x")
     v = _two_dim(w, "w")[0]
-    _matrix(x, "x", device, (_BF16,), (m, h))
-    _matrix(w, "w", device, (_BF16,), (v, h))
+    _matrix(x, "x", device, _ONLY_BF16, (m, h))
+    _matrix(w, "w", device, _ONLY_BF16, (v, h))
     _vector(targets, "targets", device, (torch.int64,), m)
     mean = _enumerator({"sum": 0, "mean": 1}, reduction, "reduction")
     g = _grad_type(grad_dtype)
@@ -334,7 +343,7 @@ def lm_loss(x: torch.Tensor, w: torch.Tensor, targets: torch.Tensor, *, ignore_i
         if dx is None:
             dx = x.new_empty((m, h))
         else:
-            _matrix(dx, "dx", device, (_BF16,), (m, h), True)
+            _matrix(dx, "dx", device, _ONLY_BF16, (m, h), True)
         if dw is None:
             dw = x.new_empty((v, h), dtype=grad_dtype)
         else:
@@ -345,7 +354,7 @@ def lm_loss(x: torch.Tensor, w: torch.Tensor, targets: torch.Tensor, *, ignore_i
     args = _Loss(m, h, v, x.data_ptr(), xs[0], xs[1], w.data_ptr(), ws[0], ws[1], targets.data_ptr(), ignore_index, mean, scale,
                  loss.data_ptr(), rows.data_ptr(), _ptr(dx), 0 if dx is None else dx.stride(0), _ptr(dw),
                  0 if dw is None else dw.stride(0), g, piece)
-    _call(_lib.dlion_lm_loss_workspace, _lib.dlion_lm_loss, args, device, workspace)
+    _call(_LOSS, args, device, workspace)
     return Loss(loss, rows, dx, dw)
 
 
