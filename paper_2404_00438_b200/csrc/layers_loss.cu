@@ -33,6 +33,13 @@ struct LossTile {
         int64_t ld;
     };
 
+    using Ahead = int64_t;                  // this lane's target, asked for before the sums are waited for
+
+    template <int WIDTH>
+    static __device__ __forceinline__ Ahead ahead(const Args& p, int row0, int, int lane) {
+        return row0 + lane < p.m ? p.targets[row0 + lane] : -1;
+    }
+
     // MASKED: columns from `valid` on do not exist
     template <bool MASKED>
     static __device__ __forceinline__ float greatest(const float (&v)[32], int valid, float top) {
@@ -62,14 +69,13 @@ struct LossTile {
     }
 
     // Two passes over the accumulator, which is cheaper to read again than to hold: the maximum, then the exponentials.
-    static __device__ __forceinline__ void tile(const Args& p, uint32_t acc, int row0, int col0, int width, bool live, uint4* stage, int lane) {
+    static __device__ __forceinline__ void tile(const Args& p, int64_t target, uint32_t acc, int row0, int col0, int width, bool live, uint4* stage, int lane) {
         if (row0 >= p.m || col0 >= p.n) return;
         if (row0 == 0 && col0 == 0 && lane == 0) *p.blocks_done = 0;
         const int row = row0 + lane;
         const int valid = min(width, p.n - col0);
         const int rows = live ? min(32, p.m - row0) : 0;
-        const int64_t target = lane < rows ? p.targets[row] : -1;
-        const int hit = target >= col0 && target < col0 + valid ? static_cast<int>(target - col0) : -1;
+        const int hit = lane < rows && target >= col0 && target < col0 + valid ? static_cast<int>(target - col0) : -1;
         const bool codes = p.codes != nullptr;
         float top = -INFINITY;
 #pragma unroll 1

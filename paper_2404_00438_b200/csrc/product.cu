@@ -202,8 +202,9 @@ void product(Call& c, const Matrix& a, const Matrix& b, Finish f) {
     uint64_t tickets = 0;
     if (split_tiles != 0) {
         tickets = static_cast<uint64_t>(split_tiles) * cfg.cg * kEpilogueWarps;
-        f.tickets = c.ws.take<unsigned int>(tickets);
         f.parts = c.ws.take<float4>(tickets * cfg.splits * (cfg.bn / 2) * 8);
+        tickets *= 4;
+        f.tickets = c.ws.take<unsigned int>(tickets);
     }
     if (c.live()) {
         CUtensorMap ma, mb;

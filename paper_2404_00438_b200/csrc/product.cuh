@@ -89,7 +89,7 @@ struct Finish {
     int out_f32;
     int rough;                             // a binary32 result that needs no segments: its operands are rounded already
     float4* parts;                         // sums of split tiles: [tile][block][epilogue warp][split][32 rows x half the columns]
-    unsigned int* tickets;                 // [tile][block][epilogue warp], 0 before the call
+    unsigned int* tickets;                 // [tile][block][epilogue warp][4 pieces], 0 before the call
 };
 
 __device__ __forceinline__ bool on_grid(const void* p, int64_t ld, int bytes) {
@@ -212,12 +212,8 @@ struct Piece {
         }
     }
 
-    __device__ __forceinline__ void add_bias(float (&v)[32], const void* bias, int f32) const {
-        float b = 0.0f;
-        if (lane < cols) {
-            b = f32 ? static_cast<const float*>(bias)[col0 + lane]
-                    : __bfloat162float(static_cast<const __nv_bfloat16*>(bias)[col0 + lane]);
-        }
+    // each lane's value to its column
+    __device__ __forceinline__ void add_bias(float (&v)[32], float b) const {
         __syncwarp();
         reinterpret_cast<float*>(stage)[lane] = b;
         __syncwarp();
@@ -302,14 +298,55 @@ struct General {
     using Args = Finish;
     static constexpr bool kSplits = true;
 
-    static __device__ __forceinline__ void piece(const Finish& f, unsigned todo, const Piece& pc, float (&v)[32]) {
+    // What an epilogue needs of memory is asked for before its sums are waited for: a load met in the middle stops a warp for some
+    // 600 clocks, and there are four pieces in a tile.
+    struct Ahead {
+        float scale;
+        uint32_t bias[4];                      // as it is stored, a lane's column of each piece
+
+        __device__ __forceinline__ float bias_of(const Finish& f, int piece) const {
+            const uint32_t b = piece == 0 ? bias[0] : piece == 1 ? bias[1] : piece == 2 ? bias[2] : bias[3];
+            return __uint_as_float(f.bias_f32 ? b : b << 16);
+        }
+    };
+
+    template <int WIDTH>
+    static __device__ __forceinline__ Ahead ahead(const Finish& f, int row0, int col0, int lane) {
+        Ahead x{1.0f, {0, 0, 0, 0}};
+        if (__builtin_expect(f.todo == 0, 1)) return x;
+        if (f.todo & kScale) x.scale = *f.scale;
+        if (f.todo & kBias) {
+#pragma unroll
+            for (int i = 0; i < WIDTH / 32; ++i) {
+                const int col = col0 + i * 32 + lane;
+                if (col < f.n) x.bias[i] = f.bias_f32 ? static_cast<const uint32_t*>(f.bias)[col] : static_cast<const unsigned short*>(f.bias)[col];
+            }
+        }
+        if ((f.todo & (kSlope | kResidual)) && row0 + lane < f.m && col0 < f.n) {
+            const int last = min(f.n, col0 + WIDTH) - 1;
+            const int64_t row = row0 + lane;
+            auto touch = [](const void* p) { asm volatile("prefetch.global.L2 [%0];" ::"l"(p)); };
+            if (f.todo & kResidual) {
+                touch(f.residual + row * f.residual_ld + col0);
+                touch(f.residual + row * f.residual_ld + last);
+            }
+            if (f.todo & kSlope) {
+                const uint8_t* p = static_cast<const uint8_t*>(f.saved);
+                const int bytes = f.saved8 ? 1 : 2;
+                touch(p + (row * f.saved_ld + col0) * bytes);
+                touch(p + (row * f.saved_ld + last) * bytes);
+            }
+        }
+        return x;
+    }
+
+    static __device__ __forceinline__ void piece(const Finish& f, unsigned todo, const Piece& pc, float scale, float bias, float (&v)[32]) {
         if (__builtin_expect(todo != 0, 0)) {
             if (todo & kScale) {
-                const float g = *f.scale;
 #pragma unroll
-                for (int j = 0; j < 32; ++j) v[j] *= g;
+                for (int j = 0; j < 32; ++j) v[j] *= scale;
             }
-            if (todo & kBias) pc.add_bias(v, f.bias, f.bias_f32);
+            if (todo & kBias) pc.add_bias(v, bias);
             if (todo & kKeep8) keep8(f, pc, v);
             if (todo & kKeep16) {
                 uint32_t w[16];
@@ -349,19 +386,22 @@ struct General {
 
     // The same from registers.
     template <int W>
-    static __device__ __forceinline__ void sums(const Finish& f, const float (&acc)[W], int row0, int col0, bool live, uint4* stage, int lane) {
+    static __device__ __forceinline__ void sums(const Finish& f, const Ahead& x, const float (&acc)[W], int row0, int col0, bool live, uint4* stage,
+                                                int lane) {
 #pragma unroll
         for (int c = 0; c < W; c += 32) {
             if (col0 + c >= f.n || row0 >= f.m) return;
             float v[32];
 #pragma unroll
             for (int j = 0; j < 32; ++j) v[j] = acc[c + j];
-            piece(f, f.todo, Piece{stage, lane, row0, col0 + c, live ? min(32, f.m - row0) : 0, min(32, f.n - col0 - c)}, v);
+            piece(f, f.todo, Piece{stage, lane, row0, col0 + c, live ? min(32, f.m - row0) : 0, min(32, f.n - col0 - c)}, x.scale,
+                  x.bias_of(f, c / 32), v);
         }
     }
 
     // One warp's 32 rows and `width` columns of a finished accumulator.
-    static __device__ __forceinline__ void tile(const Finish& f, uint32_t acc, int row0, int col0, int width, bool live, uint4* stage, int lane) {
+    static __device__ __forceinline__ void tile(const Finish& f, const Ahead& x, uint32_t acc, int row0, int col0, int width, bool live, uint4* stage,
+                                                int lane) {
         const unsigned todo = f.todo;
 #pragma unroll 1
         for (int c = 0; c < width; c += 32) {
@@ -369,7 +409,7 @@ struct General {
             if (col0 + c >= f.n || row0 >= f.m) return;      // the same for the whole warp
             tc::tmem_load32(acc + c, v);
             const Piece pc{stage, lane, row0, col0 + c, live ? min(32, f.m - row0) : 0, min(32, f.n - col0 - c)};
-            piece(f, todo, pc, v);
+            piece(f, todo, pc, x.scale, x.bias_of(f, c / 32), v);
             if (!live) return;
         }
     }
@@ -380,33 +420,36 @@ struct General {
         for (int i = 0; i < 8; ++i) __stcg(to + i * 32 + lane, make_float4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]));
     }
 
-    // After a warp's part of a split is in place: whoever finds the other splits done adds them all, in their order, so that
-    // the sum does not depend on who that is.  Nobody waits.
-    static __device__ __forceinline__ void join(const Finish& f, int place, int splits, int row0, int col0, int width, uint4* stage, int lane) {
+    // After a warp's part of a split is in place: whoever finds a piece's other splits done adds them all, in their order, so that
+    // the sum does not depend on who that is.  Nobody waits.  The splits look at the pieces in different orders, or the
+    // last of them would add all four.
+    static __device__ __forceinline__ void join(const Finish& f, const Ahead& x, int place, int split, int splits, int row0, int col0, int width,
+                                                uint4* stage, int lane) {
         __threadfence();
         __syncwarp();
-        unsigned int before = 0;
-        if (lane == 0) before = atomicAdd(f.tickets + place, 1u);
-        before = __shfl_sync(0xffffffffu, before, 0);
-        if (before != static_cast<unsigned int>(splits - 1)) return;
-        __threadfence();
-        const float4* from = f.parts + static_cast<int64_t>(place) * splits * (width * 8);
+        const int pieces = width / 32;
 #pragma unroll 1
-        for (int c = 0; c < width; c += 32) {
-            if (col0 + c >= f.n || row0 >= f.m) return;
+        for (int i = 0; i < pieces; ++i) {
+            const int c = (i + split) % pieces * 32;
+            unsigned int before = 0;
+            if (lane == 0) before = atomicAdd(f.tickets + place * 4 + c / 32, 1u);
+            before = __shfl_sync(0xffffffffu, before, 0);
+            if (before != static_cast<unsigned int>(splits - 1) || col0 + c >= f.n || row0 >= f.m) continue;
+            __threadfence();
+            const float4* from = f.parts + static_cast<int64_t>(place) * splits * (width * 8);
             float v[32] = {};
 #pragma unroll 2
             for (int r = 0; r < splits; ++r) {
 #pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const float4 w = __ldcg(from + (r * width + c) * 8 + i * 32 + lane);
-                    v[4 * i] += w.x;
-                    v[4 * i + 1] += w.y;
-                    v[4 * i + 2] += w.z;
-                    v[4 * i + 3] += w.w;
+                for (int j = 0; j < 8; ++j) {
+                    const float4 w = __ldcg(from + (r * width + c) * 8 + j * 32 + lane);
+                    v[4 * j] += w.x;
+                    v[4 * j + 1] += w.y;
+                    v[4 * j + 2] += w.z;
+                    v[4 * j + 3] += w.w;
                 }
             }
-            piece(f, f.todo, Piece{stage, lane, row0, col0 + c, min(32, f.m - row0), min(32, f.n - col0 - c)}, v);
+            piece(f, f.todo, Piece{stage, lane, row0, col0 + c, min(32, f.m - row0), min(32, f.n - col0 - c)}, x.scale, x.bias_of(f, c / 32), v);
         }
     }
 };
@@ -588,6 +631,10 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
             tile_of(s, x.tile, tm, tn);
             const int place = ((x.tile - s.whole) * CG + static_cast<int>(rank)) * kEpilogueWarps + warp - 4;     // of a split tile's part
             const int row0 = tm * kM + static_cast<int>(rank) * 128 + quarter * 32, col0 = tn * BN + half * (BN / 2);
+            // (joined, a warp finishes the piece that it adds)
+            const int p_own = share + s.splits * (warp - 4);
+            const auto needs = FORM == kJoined ? E::template ahead<32>(args, tm * kM + (p_own % 4) * 32, tn * BN + (p_own / 4) * 32, lane)
+                                               : E::template ahead<BN / 2>(args, row0, col0, lane);
             if constexpr (FORM == kLong) {
                 float sum[BN / 2] = {};
                 for (int kb = x.k0; live && kb < x.k1; kb += kSegment, ++n) {
@@ -613,9 +660,9 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
                         for (int j = 0; j < 32; ++j) v[j] = sum[c + j];
                         E::put_part(to + c * 8, v, lane);
                     }
-                    E::join(args, place, s.splits, row0, col0, BN / 2, stage, lane);
+                    E::join(args, needs, place, x.split, s.splits, row0, col0, BN / 2, stage, lane);
                 } else {
-                    E::sums(args, sum, row0, col0, live, stage, lane);
+                    E::sums(args, needs, sum, row0, col0, live, stage, lane);
                 }
             } else if constexpr (FORM == kJoined) {
                 if (live) {
@@ -657,7 +704,7 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
                             v[4 * i + 3] += w.w;
                         }
                     }
-                    E::sums(args, v, tm * kM + (p % 4) * 32, tn * BN + (p / 4) * 32, live, stage, lane);
+                    E::sums(args, needs, v, tm * kM + (p % 4) * 32, tn * BN + (p / 4) * 32, live, stage, lane);
                     if (!live) break;
                 }
             } else {
@@ -677,11 +724,11 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
                         }
                         drain(set);
                         ++n;
-                        E::join(args, place, s.splits, row0, col0, BN / 2, stage, lane);
+                        E::join(args, needs, place, x.split, s.splits, row0, col0, BN / 2, stage, lane);
                         continue;
                     }
                 }
-                E::tile(args, part + set * BN, row0, col0, BN / 2, live, stage, lane);
+                E::tile(args, needs, part + set * BN, row0, col0, BN / 2, live, stage, lane);
                 if (live) {
                     drain(set);
                     ++n;
