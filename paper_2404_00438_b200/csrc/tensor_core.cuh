@@ -78,9 +78,10 @@ __device__ __forceinline__ void bar_expect(uint32_t bar, uint32_t bytes) {
     asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
 }
 
-// Arrival on a barrier of any CTA of the cluster (`bar` from map_to_rank).
+// Arrival on a barrier of any CTA of the cluster (`bar` from map_to_rank).  It announces reads of tensor memory, which their
+// own fence orders, and no writes: with the cluster's scope it would wait for the epilogue's stores.
 __device__ __forceinline__ void bar_arrive_cluster(uint32_t bar) {
-    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
+    asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
 }
 
 __device__ __forceinline__ void bar_arrive(uint32_t bar) {
