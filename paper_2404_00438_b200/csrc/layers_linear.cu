@@ -340,23 +340,23 @@ void backward(Call& c, const dlion_linear_bwd& p) {
         return;
     }
     const Matrix dy = readable(c, Matrix{p.dy, p.m, p.n, p.dy_rs, p.dy_cs});
+    Matrix w{}, a{};
+    Finish fx{}, fw{};
     if (p.dx != nullptr) {
-        const Matrix w = readable(c, Matrix{p.w, p.k, p.n, p.w_rs, p.w_cs});
-        Finish f{};
-        f.slope = p.act;
-        f.saved8 = p.saved == DLION_KEEP_8BIT;
-        f.saved = p.u;
-        f.saved_ld = p.u_ld;
-        f.saved_e = p.u_e;
-        f.saved_e_ld = p.u_e_ld;
-        f.residual = static_cast<const __nv_bfloat16*>(p.residual);
-        f.residual_ld = p.r_ld;
-        f.out = p.dx;
-        f.out_ld = p.dx_ld;
-        product(c, dy, w, f);
+        w = readable(c, Matrix{p.w, p.k, p.n, p.w_rs, p.w_cs});
+        fx.slope = p.act;
+        fx.saved8 = p.saved == DLION_KEEP_8BIT;
+        fx.saved = p.u;
+        fx.saved_ld = p.u_ld;
+        fx.saved_e = p.u_e;
+        fx.saved_e_ld = p.u_e_ld;
+        fx.residual = static_cast<const __nv_bfloat16*>(p.residual);
+        fx.residual_ld = p.r_ld;
+        fx.out = p.dx;
+        fx.out_ld = p.dx_ld;
     }
+    const bool rows = p.dw_cs == 1 && (p.k == 1 || p.dw_rs >= p.n);
     if (p.dw != nullptr) {
-        Matrix a;
         if (p.saved == DLION_KEEP_BF16 && p.act == DLION_ACT_NONE) {
             a = readable(c, Matrix{p.u, p.m, p.k, p.u_ld, 1});
         } else {
@@ -365,16 +365,17 @@ void backward(Call& c, const dlion_linear_bwd& p) {
             if (c.live()) operand(c, p.u, p.u_ld, p.u_e, p.u_e_ld, p.saved == DLION_KEEP_8BIT, p.act, p.m, p.k, out, ld);
             a = Matrix{out, p.m, p.k, ld, 1};
         }
-        Finish f{};
-        f.out = p.dw;
-        f.out_f32 = p.grad_type == DLION_GRAD_F32;
-        if (p.dw_cs == 1 && (p.k == 1 || p.dw_rs >= p.n)) {
-            f.out_ld = p.dw_rs;
-            product(c, transposed(a), transposed(dy), f);
-        } else {
-            f.out_ld = p.dw_cs;
-            product(c, transposed(dy), transposed(a), f);
-        }
+        fw.out = p.dw;
+        fw.out_f32 = p.grad_type == DLION_GRAD_F32;
+        fw.out_ld = rows ? p.dw_rs : p.dw_cs;
+    }
+    const Matrix wa = transposed(rows ? a : dy), wb = transposed(rows ? dy : a);
+    if (p.dx != nullptr && p.dw != nullptr) {
+        products(c, dy, w, fx, wa, wb, fw);
+    } else if (p.dx != nullptr) {
+        product(c, dy, w, fx);
+    } else if (p.dw != nullptr) {
+        product(c, wa, wb, fw);
     }
     if (p.db != nullptr) column_sums(c, dy, p.db, p.grad_type);
 }

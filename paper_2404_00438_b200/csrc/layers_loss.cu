@@ -337,23 +337,22 @@ void loss(Call& c, const dlion_loss& p) {
         xp.p = static_cast<const uint16_t*>(x.p) + r * x.rs;
         xp.rows = rows;
         if (c.live()) {
-            Shape s{};
-            CUtensorMap ma, mb;
-            if (!shape_of(cfg, xp, w, &s)) {
+            Work<LossTile::Args> work{};
+            if (!shape_of(cfg, xp, w, &work.s[0])) {
                 c.status = DLION_EINVAL;
                 return;
             }
-            if (!make_map(&ma, xp, &s.a_mn, 128) || !make_map(&mb, w, &s.b_mn, cfg.bn / cfg.cg)) {
+            if (!make_map(&work.a[0], xp, &work.s[0].a_mn, 128) || !make_map(&work.b[0], w, &work.s[0].b_mn, cfg.bn / cfg.cg)) {
                 c.status = DLION_ECUDA;
                 return;
             }
-            const LossTile::Args args{static_cast<int>(rows), static_cast<int>(p.v), p.targets + r, blocks_done, stats, at_target, codes, ld};
+            work.args[0] = LossTile::Args{static_cast<int>(rows), static_cast<int>(p.v), p.targets + r, blocks_done, stats, at_target, codes, ld};
             if (cfg.cg == 1) {
-                launch<1, 64, LossTile, kWhole>(c, ma, mb, s, args);
+                launch<1, 64, LossTile, kWhole>(c, work);
             } else if (cfg.bn == 128) {
-                launch<2, 128, LossTile, kWhole>(c, ma, mb, s, args);
+                launch<2, 128, LossTile, kWhole>(c, work);
             } else {
-                launch<2, 256, LossTile, kWhole>(c, ma, mb, s, args);
+                launch<2, 256, LossTile, kWhole>(c, work);
             }
             if (c.status != DLION_OK) return;
             const Last end{blocks_done, p.rows, p.targets, p.m, p.mean, p.scale, r + rows >= p.m ? p.loss : nullptr,
@@ -372,7 +371,6 @@ void loss(Call& c, const dlion_loss& p) {
         fx.scale = factor;
         fx.out = static_cast<uint16_t*>(p.dx) + r * p.dx_ld;
         fx.out_ld = p.dx_ld;
-        product(c, d, transposed(w), fx);
         Finish fw{};
         fw.scale = factor;
         const bool last = r + rows >= p.m;
@@ -386,7 +384,7 @@ void loss(Call& c, const dlion_loss& p) {
         fw.out_ld = last ? p.dw_ld : so_far_ld;
         fw.out_f32 = f32 || !last;
         fw.rough = 1;
-        product(c, transposed(d), transposed(xp), fw);
+        products(c, d, transposed(w), fx, transposed(d), transposed(xp), fw);
     }
 }
 

@@ -50,49 +50,59 @@ __global__ void __launch_bounds__(256) pack_kernel(const uint16_t* a, int64_t rs
 
 }  // namespace
 
-// The division of the work with the least estimated time, in clocks of an SM.  A slice takes 580 (its 32 KB come
-// at 57 to 64 bytes a clock, its products take 512) in a pair's 256 x 256 tile and 420 (24 KB) in the others.  Tiles that do not fill a last
-// round of the workers are split, which costs the writing and reading of their sums: 8192 x 8192 x 2048 has 256 tiles for
-// 74 pairs, 3.46 rounds; four rounds took 207 us, three and the halves of 34 tiles 187 us.  Joined blocks exchange
-// their sums in about 3000.
+namespace {
+
+// Clocks of an SM.  A slice takes 580 in a pair's 256 x 256 tile (its 32 KB come at 57 to 64 bytes a clock, its products take
+// 512) and 420 (24 KB) in the others; a tile costs 300 beside its slices, the last one its epilogue.
+struct Tiles {
+    int cg, bn, form;
+    double slice, last;
+};
+constexpr Tiles kPair{2, 256, kWhole, 580.0, 4000.0}, kHalfPair{2, 128, kWhole, 420.0, 2000.0}, kLongPair{2, 128, kLong, 420.0, 2000.0},
+    kBlock{1, 64, kWhole, 420.0, 1000.0}, kJoinedBlock{1, 64, kJoined, 420.0, 1000.0};
+constexpr double kLaunch = 4000.0;         // from one kernel's end to the next one's first products
+
+int64_t tiles_of(const Tiles& t, int64_t m, int64_t n) { return parts(m, 128 * t.cg) * parts(n, t.bn); }
+
+}  // namespace
+
+// The division of the work with the least estimated time.  Tiles that do not fill a last round of the workers may be split, and
+// joined by whoever finishes last, which takes some 12 us (2048 x 2048 x 8192, 256 tiles for 74 pairs: 48 us in four rounds, 55 us in
+// three and the halves of 34): it pays where a round is longer than that.  Blocks of a cluster exchange their sums in about
+// 4500 (197 x 768 x 768: 6.3 us with four shares of k, 5.7 us without).
 Config choose(const Call& c, int64_t m, int64_t n, int64_t k, bool sums, bool alone) {
     const int64_t slices = std::max<int64_t>(1, parts(k, kSlice));
     const bool long_sums = sums && slices > kSegment;
-    Config best{2, 256, kWhole, 0, 1, static_cast<int>(slices)};
-    double least = 1e300;
-    auto consider = [&](int cg, int bn, int form, int64_t s, double slice, double piece) {
+    Config best{2, 256, kWhole, 0, 1, static_cast<int>(slices), 1e300};
+    auto consider = [&](const Tiles& f, int64_t s) {
         const int64_t per = parts(slices, s);
         if (parts(slices, per) != s) return;
-        const int64_t tiles = parts(m, 128 * cg) * parts(n, bn), workers = c.sms / cg;
+        const int64_t tiles = tiles_of(f, m, n), workers = c.sms / f.cg;
         int64_t whole = 0;
         double t;
-        if (form == kJoined) {
-            if (tiles * s > 16 * 8) return;    // clusters of eight: sixteen at a time for certain
-            t = per * slice + 3000.0 + piece;
+        if (f.form == kJoined) {
+            if (tiles * s > 16 * 8) return;    // what fits at a time, or nearly (15 clusters of eight)
+            t = per * f.slice + 4500.0 + f.last;
         } else {
             whole = s == 1 ? tiles : tiles / workers * workers;
-            const double round = 300.0;
-            t = static_cast<double>(parts(whole, workers)) * (slices * slice + round) + piece;
-            if (s > 1) t += static_cast<double>(parts((tiles - whole) * s, workers)) * (per * slice + round) + 2000.0 + 1200.0 * s * (bn / 128);
+            t = static_cast<double>(parts(whole, workers)) * (slices * f.slice + 300.0) + f.last;
+            if (s > 1) t += static_cast<double>(parts((tiles - whole) * s, workers)) * (per * f.slice + 300.0) + 20000.0 + 1200.0 * s * (f.bn / 128);
         }
-        if (t < least) {
-            least = t;
-            best = Config{cg, bn, form, static_cast<int>(whole), static_cast<int>(s), static_cast<int>(per)};
-        }
+        if (t < best.clocks) best = Config{f.cg, f.bn, f.form, static_cast<int>(whole), static_cast<int>(s), static_cast<int>(per), t};
     };
     const int64_t most = alone ? 1 : std::min<int64_t>(16, std::max<int64_t>(1, slices / 8));
     for (int64_t s = 1; s <= most; ++s) {
         if (long_sums) {
-            consider(2, 128, kLong, s, 420.0, 2000.0);
+            consider(kLongPair, s);
         } else {
-            consider(2, 256, kWhole, s, 580.0, 4000.0);
-            consider(2, 128, kWhole, s, 420.0, 2000.0);
+            consider(kPair, s);
+            consider(kHalfPair, s);
         }
     }
-    if (!long_sums) consider(1, 64, kWhole, 1, 420.0, 1000.0);
+    if (!long_sums) consider(kBlock, 1);
     for (int64_t s = 2; !alone && s <= 8; s *= 2) {
         if (sums && parts(slices, s) > kSegment) continue;
-        consider(1, 64, kJoined, s, 420.0, 1000.0);
+        consider(kJoinedBlock, s);
     }
     return best;
 }
@@ -183,22 +193,49 @@ bool shape_of(const Config& cfg, const Matrix& a, const Matrix& b, Shape* s) {
     return static_cast<int64_t>(s->tiles_m) * s->tiles_n * s->splits < (int64_t{1} << 30);
 }
 
-void product(Call& c, const Matrix& a, const Matrix& b, Finish f) {
+static void complete(Finish& f, const Matrix& a, const Matrix& b) {
     f.m = static_cast<int>(a.rows);
     f.n = static_cast<int>(b.rows);
     f.todo = (f.scale != nullptr ? kScale : 0u) | (f.bias != nullptr ? kBias : 0u) | (f.keep == DLION_KEEP_BF16 ? kKeep16 : 0u) |
              (f.keep == DLION_KEEP_8BIT ? kKeep8 : 0u) | (f.act != DLION_ACT_NONE ? kAct : 0u) | (f.slope != DLION_ACT_NONE ? kSlope : 0u) |
              (f.residual != nullptr ? kResidual : 0u) | (f.accumulated != nullptr ? kAdd : 0u);
     f.wide = aligned16(f.out) && f.out_ld * (f.out_f32 ? 4 : 2) % 16 == 0;
+}
+
+static bool place(Call& c, const Config& cfg, const Matrix& a, const Matrix& b, Work<Finish>& w, int i) {
+    if (make_map(&w.a[i], a, &w.s[i].a_mn, 128) && make_map(&w.b[i], b, &w.s[i].b_mn, cfg.bn / cfg.cg)) return true;
+    c.status = DLION_ECUDA;
+    return false;
+}
+
+template <bool TWO>
+static void launch_as(Call& c, const Config& cfg, Work<Finish>& w) {
+    if (cfg.form == kLong) {
+        launch<2, 128, General, kLong, TWO>(c, w);
+    } else if (cfg.form == kJoined) {
+        if constexpr (!TWO) launch<1, 64, General, kJoined>(c, w);
+    } else if (cfg.cg == 1) {
+        launch<1, 64, General, kWhole, TWO>(c, w);
+    } else if (cfg.bn == 128) {
+        launch<2, 128, General, kWhole, TWO>(c, w);
+    } else {
+        launch<2, 256, General, kWhole, TWO>(c, w);
+    }
+}
+
+static bool long_sums(const Finish& f) { return f.out_f32 != 0 && f.rough == 0; }
+
+void product(Call& c, const Matrix& a, const Matrix& b, Finish f) {
+    complete(f, a, b);
     if (few_rows(c, a, b, f)) return;
-    const Config cfg = choose(c, a.rows, b.rows, a.cols, f.out_f32 != 0 && f.rough == 0, false);
-    Shape s{};
-    if (!shape_of(cfg, a, b, &s)) {
+    const Config cfg = choose(c, a.rows, b.rows, a.cols, long_sums(f), false);
+    Work<Finish> w{};
+    if (!shape_of(cfg, a, b, &w.s[0])) {
         c.status = DLION_EINVAL;
         return;
     }
     const uint64_t mark = c.ws.used;
-    const int64_t split_tiles = cfg.form == kJoined || cfg.splits == 1 ? 0 : static_cast<int64_t>(s.tiles_m) * s.tiles_n - cfg.whole;
+    const int64_t split_tiles = cfg.form == kJoined || cfg.splits == 1 ? 0 : static_cast<int64_t>(w.s[0].tiles_m) * w.s[0].tiles_n - cfg.whole;
     uint64_t tickets = 0;
     if (split_tiles != 0) {
         tickets = static_cast<uint64_t>(split_tiles) * cfg.cg * kEpilogueWarps;
@@ -206,31 +243,65 @@ void product(Call& c, const Matrix& a, const Matrix& b, Finish f) {
         tickets *= 4;
         f.tickets = c.ws.take<unsigned int>(tickets);
     }
-    if (c.live()) {
-        CUtensorMap ma, mb;
-        const bool ok = make_map(&ma, a, &s.a_mn, 128) && make_map(&mb, b, &s.b_mn, cfg.bn / cfg.cg);
-        if (!ok) {
-            c.status = DLION_ECUDA;
+    if (c.live() && place(c, cfg, a, b, w, 0)) {
+        w.args[0] = f;
+        if (tickets != 0) c.check(cudaMemsetAsync(f.tickets, 0, tickets * sizeof(unsigned int), c.stream));
+        launch_as<false>(c, cfg, w);
+    }
+    // later products of the call reuse the split sums' place (the stream orders them): the size query keeps the maximum
+    if (c.ws.dry) c.ws.size = std::max(c.ws.size, c.ws.used);
+    c.ws.used = mark;
+}
+
+void products(Call& c, const Matrix& a0, const Matrix& b0, Finish f0, const Matrix& a1, const Matrix& b1, Finish f1) {
+    // both as whole tiles of one kind, the longer sums first, against each for itself; few rows have their own kernel
+    const bool few = a0.rows <= 32 || a1.rows <= 32;
+    const Config best0 = choose(c, a0.rows, b0.rows, a0.cols, long_sums(f0), false), best1 = choose(c, a1.rows, b1.rows, a1.cols, long_sums(f1), false);
+    const int64_t slices0 = parts(a0.cols, kSlice), slices1 = parts(a1.cols, kSlice);
+    const bool swap = slices1 > slices0;
+    const bool sums = (long_sums(f0) && slices0 > kSegment) || (long_sums(f1) && slices1 > kSegment);
+    const int64_t most = std::max(slices0, slices1), least = std::min(slices0, slices1);
+    double clocks = best0.clocks + best1.clocks + kLaunch;
+    Config cfg{};
+    int64_t extra = 0;
+    for (const Tiles* f : {&kPair, &kHalfPair, &kBlock, &kLongPair}) {
+        if (few || sums != (f->form == kLong)) continue;
+        const int64_t t0 = tiles_of(*f, a0.rows, b0.rows), t1 = tiles_of(*f, a1.rows, b1.rows), workers = c.sms / f->cg;
+        if (t0 + t1 >= (int64_t{1} << 30)) continue;
+        const double big = most * f->slice + 300.0, small = least * f->slice + 300.0;
+        const int64_t first = swap ? t1 : t0, second = swap ? t0 : t1, over = first % workers;
+        const int64_t ahead = over == 0 ? 0 : static_cast<int64_t>(big / small + 0.5);
+        const int64_t rest = std::max<int64_t>(0, second - ahead * (workers - over));
+        const double t = parts(first, workers) * big + parts(rest, workers) * small + f->last;
+        if (t < clocks) {
+            clocks = t;
+            cfg = Config{f->cg, f->bn, f->form, 0, 1, 0, t};
+            extra = ahead;
+        }
+    }
+    if (cfg.cg == 0) {
+        product(c, a0, b0, f0);
+        product(c, a1, b1, f1);
+        return;
+    }
+    if (!c.live()) return;
+    complete(f0, a0, b0);
+    complete(f1, a1, b1);
+    Work<Finish> w{};
+    const Matrix *a[2] = {swap ? &a1 : &a0, swap ? &a0 : &a1}, *b[2] = {swap ? &b1 : &b0, swap ? &b0 : &b1};
+    w.args[0] = swap ? f1 : f0;
+    w.args[1] = swap ? f0 : f1;
+    w.extra = static_cast<int>(extra);
+    for (int i = 0; i < 2; ++i) {
+        cfg.split_slices = static_cast<int>(parts(a[i]->cols, kSlice));
+        cfg.whole = static_cast<int>(parts(a[i]->rows, 128 * cfg.cg) * parts(b[i]->rows, cfg.bn));
+        if (!shape_of(cfg, *a[i], *b[i], &w.s[i])) {
+            c.status = DLION_EINVAL;
             return;
         }
-        if (tickets != 0) c.check(cudaMemsetAsync(f.tickets, 0, tickets * sizeof(unsigned int), c.stream));
-        if (cfg.form == kLong) {
-            launch<2, 128, General, kLong>(c, ma, mb, s, f);
-        } else if (cfg.form == kJoined) {
-            launch<1, 64, General, kJoined>(c, ma, mb, s, f);
-        } else if (cfg.cg == 1) {
-            launch<1, 64, General, kWhole>(c, ma, mb, s, f);
-        } else if (cfg.bn == 128) {
-            launch<2, 128, General, kWhole>(c, ma, mb, s, f);
-        } else {
-            launch<2, 256, General, kWhole>(c, ma, mb, s, f);
-        }
+        if (!place(c, cfg, *a[i], *b[i], w, i)) return;
     }
-    if (c.ws.dry) {
-        // later products of the call reuse the split sums' place (the stream orders them): the size query keeps the maximum
-        c.ws.size = std::max(c.ws.size, c.ws.used);
-    }
-    c.ws.used = mark;
+    launch_as<true>(c, cfg, w);
 }
 
 }  // namespace prod

@@ -464,10 +464,40 @@ __device__ __forceinline__ void tile_of(const Shape& s, int t, int& tm, int& tn)
     tn = in / rows;
 }
 
-template <int CG, int BN, class E, int FORM>
+// One product, or two that do not depend on each other (a layer's dx and dW), so that the tiles of the second fill the SMs that
+// the first leaves idle.
+template <class Args>
+struct Work {
+    CUtensorMap a[2], b[2];
+    Shape s[2];
+    Args args[2];
+    int units[2];                          // pieces of work in each; those of the first take longer
+    int extra;                             // pieces of the second ahead of time for each worker that has one fewer of the first
+};
+
+// A worker's i-th piece of work, or -1: every `workers`-th of the first product, then, where that leaves some a piece
+// short, `extra` of the second for those, then every `workers`-th of the rest.
+template <bool TWO, class Args>
+__device__ __forceinline__ int unit_at(const Work<Args>& w, int worker, int workers, int i) {
+    if (!TWO) return worker + i * workers < w.units[0] ? worker + i * workers : -1;
+    const int rounds = w.units[0] / workers, over = w.units[0] - rounds * workers;
+    const int firsts = rounds + (worker < over ? 1 : 0);
+    if (i < firsts) return worker + i * workers;
+    int j = i - firsts, u;
+    const int extra = over == 0 ? 0 : w.extra, behind = workers - over;
+    if (worker >= over && j < extra) {
+        u = j * behind + worker - over;
+    } else {
+        if (worker >= over) j -= extra;
+        u = extra * behind + worker + j * workers;
+    }
+    return u < w.units[1] ? w.units[0] + u : -1;
+}
+
+// TWO: with a second product; with one, what describes it is at fixed places.
+template <int CG, int BN, class E, int FORM, bool TWO>
 __global__ void __launch_bounds__(kThreads, 1)
-product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const Shape s,
-               const __grid_constant__ typename E::Args args, unsigned int* mark) {
+product_kernel(const __grid_constant__ Work<typename E::Args> work, unsigned int* mark) {
     constexpr int kM = 128 * CG;               // rows of the tile; a block has 128 of them
     constexpr int kBRows = BN / CG;            // of B, in this block
     constexpr uint32_t kCols = 2 * BN;         // tensor memory columns: two accumulators
@@ -490,11 +520,11 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
 
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
     const uint32_t rank = CG == 2 ? tc::cluster_rank() : 0;
-    const int tiles = s.tiles_m * s.tiles_n, units = s.whole + (tiles - s.whole) * s.splits;
-    // kJoined: the cluster is the worker, a block's place in it the split; one tile each
+    // kJoined: the cluster is the worker, a block's place in it the split; one tile each (whole = 0, the second product empty)
     const int share = FORM == kJoined ? static_cast<int>(tc::cluster_rank()) : 0;
-    const int workers = FORM == kJoined ? units : gridDim.x / CG;
-    const int worker = FORM == kJoined ? static_cast<int>(blockIdx.x) / s.splits + share * tiles : static_cast<int>(blockIdx.x) / CG;   // whole = 0
+    const int workers = FORM == kJoined ? work.units[0] : gridDim.x / CG;
+    const int worker = FORM == kJoined ? static_cast<int>(blockIdx.x) / work.s[0].splits + share * (work.units[0] / work.s[0].splits)
+                                       : static_cast<int>(blockIdx.x) / CG;
 
     tc::let_next_start();
     if (threadIdx.x == 0) {
@@ -510,8 +540,8 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
         tc::bar_init_done();
         if (FORM == kJoined) tc::bar_expect(landed, kPieces * kPiece);
         slot_mem[1] = 0;                       // set when a wait ran out
-        tc::prefetch_map(&map_a);
-        tc::prefetch_map(&map_b);
+        tc::prefetch_map(&work.a[0]);
+        tc::prefetch_map(&work.b[0]);
     }
     if (warp == 1) tc::tmem_alloc<CG>(slot, kCols);
     tc::fence_before();
@@ -530,9 +560,14 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
         const uint32_t lead_full = CG == 2 ? tc::map_to_rank(full, 0) : full;
         int st = 0, filled = 0;
         uint32_t phase = 1;
-        for (int u = worker; u < units && fine; u += workers) {
+        for (int i = 0; fine; ++i) {
+            const int unit = unit_at<TWO>(work, worker, workers, i);
+            if (unit < 0) break;
+            const int which = TWO && unit >= work.units[0] ? 1 : 0;
+            const Shape& s = work.s[which];
+            const CUtensorMap *map_a = &work.a[which], *map_b = &work.b[which];
             int tm, tn;
-            const Unit x = unit_of(s, u);
+            const Unit x = unit_of(s, unit - which * work.units[0]);
             tile_of(s, x.tile, tm, tn);
             const int row = tm * kM + static_cast<int>(rank) * 128, col = tn * BN + static_cast<int>(rank) * kBRows;
             for (int kb = x.k0; kb < x.k1; ++kb, ++filled) {
@@ -541,16 +576,16 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
                     const uint32_t a = base + st * kStageBytes, b = a + kABytes, bar = lead_full + 8 * st;
                     if (rank == 0) tc::bar_expect(full + 8 * st, kBytes);
                     if (s.a_mn) {
-                        tc::load_tile<CG>(a, &map_a, row, kb * kSlice, bar);
-                        tc::load_tile<CG>(a + 8192, &map_a, row + 64, kb * kSlice, bar);
+                        tc::load_tile<CG>(a, map_a, row, kb * kSlice, bar);
+                        tc::load_tile<CG>(a + 8192, map_a, row + 64, kb * kSlice, bar);
                     } else {
-                        tc::load_tile<CG>(a, &map_a, kb * kSlice, row, bar);
+                        tc::load_tile<CG>(a, map_a, kb * kSlice, row, bar);
                     }
                     if (s.b_mn) {
 #pragma unroll
-                        for (int c = 0; c < kBRows / 64; ++c) tc::load_tile<CG>(b + 8192 * c, &map_b, col + 64 * c, kb * kSlice, bar);
+                        for (int c = 0; c < kBRows / 64; ++c) tc::load_tile<CG>(b + 8192 * c, map_b, col + 64 * c, kb * kSlice, bar);
                     } else {
-                        tc::load_tile<CG>(b, &map_b, kb * kSlice, col, bar);
+                        tc::load_tile<CG>(b, map_b, kb * kSlice, col, bar);
                     }
                 }
                 __syncwarp();
@@ -566,27 +601,31 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
         }
     } else if (warp == 1) {
         if (rank == 0) {
-            const uint32_t inst = tc::instruction(kM, BN, s.a_mn, s.b_mn);
-            const uint32_t a_step = (s.a_mn ? 2048 : 32) >> 4, b_step = (s.b_mn ? 2048 : 32) >> 4;   // 16 values of k
-            // (a block's shared addresses have its place in the cluster above bit 23)
-            const uint64_t a_desc = tc::operand_base(s.a_mn) | ((base >> 4) & 0x3fff);
-            const uint64_t b_desc = tc::operand_base(s.b_mn) | (((base + kABytes) >> 4) & 0x3fff);
-            auto multiply = [&](uint32_t acc, int st, bool first) {         // four instructions on stage `st`
-                if (tc::elected()) {
-                    const uint32_t at = static_cast<uint32_t>(st * kStageBytes) >> 4;
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) tc::mma<CG>(acc, a_desc + at + j * a_step, b_desc + at + j * b_step, inst, (j > 0 || !first) ? 1u : 0u);
-                }
-                __syncwarp();
-            };
             auto finished = [&](uint32_t bar) {
                 if (tc::elected()) tc::commit<CG>(bar);
                 __syncwarp();
             };
             int st = 0, n = 0;
             uint32_t phase = 0;
-            for (int u = worker; u < units && fine; u += workers) {
-                const Unit x = unit_of(s, u);
+            for (int i = 0; fine; ++i) {
+                const int unit = unit_at<TWO>(work, worker, workers, i);
+                if (unit < 0) break;
+                const int which = TWO && unit >= work.units[0] ? 1 : 0;
+                const Shape& s = work.s[which];
+                const Unit x = unit_of(s, unit - which * work.units[0]);
+                const uint32_t inst = tc::instruction(kM, BN, s.a_mn, s.b_mn);
+                const uint32_t a_step = (s.a_mn ? 2048 : 32) >> 4, b_step = (s.b_mn ? 2048 : 32) >> 4;   // 16 values of k
+                // (a block's shared addresses have its place in the cluster above bit 23)
+                const uint64_t a_desc = tc::operand_base(s.a_mn) | ((base >> 4) & 0x3fff);
+                const uint64_t b_desc = tc::operand_base(s.b_mn) | (((base + kABytes) >> 4) & 0x3fff);
+                auto multiply = [&](uint32_t acc, int st, bool first) {     // four instructions on stage `st`
+                    if (tc::elected()) {
+                        const uint32_t at = static_cast<uint32_t>(st * kStageBytes) >> 4;
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) tc::mma<CG>(acc, a_desc + at + j * a_step, b_desc + at + j * b_step, inst, (j > 0 || !first) ? 1u : 0u);
+                    }
+                    __syncwarp();
+                };
                 const int seg = FORM == kLong ? kSegment : x.k1 - x.k0;
                 for (int kb = x.k0; kb < x.k1 && fine; ++n) {
                     const int set = n & 1, from = kb, to = min(x.k1, kb + seg);
@@ -624,10 +663,15 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
         };
         if (FORM == kJoined) tc::cluster_wait();     // the others' barriers exist
         int n = 0;
-        for (int u = worker - workers; u < units && fine; u += workers) {
-            const bool live = u >= 0 && (FORM == kJoined ? u == worker : true);
+        for (int i = -1; fine; ++i) {
+            const bool live = i >= 0;
+            const int unit = unit_at<TWO>(work, worker, workers, live ? i : 0);
+            if (unit < 0) break;
+            const int which = TWO && unit >= work.units[0] ? 1 : 0;
+            const Shape& s = work.s[which];
+            const typename E::Args& args = work.args[which];
             int tm, tn;
-            const Unit x = unit_of(s, live ? u : worker);
+            const Unit x = unit_of(s, unit - which * work.units[0]);
             tile_of(s, x.tile, tm, tn);
             const int place = ((x.tile - s.whole) * CG + static_cast<int>(rank)) * kEpilogueWarps + warp - 4;     // of a split tile's part
             const int row0 = tm * kM + static_cast<int>(rank) * 128 + quarter * 32, col0 = tn * BN + half * (BN / 2);

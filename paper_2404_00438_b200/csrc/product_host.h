@@ -62,6 +62,9 @@ Matrix readable(Call& c, const Matrix& a);
 // Both must be readable.  f.m, f.n are set here.
 void product(Call& c, const Matrix& a, const Matrix& b, Finish f);
 
+// Two products that do not depend on each other, in one launch where that is expected to take less time.
+void products(Call& c, const Matrix& a0, const Matrix& b0, Finish f0, const Matrix& a1, const Matrix& b1, Finish f1);
+
 // The same for at most 32 rows of a; false if this is not such a product.  (few_rows.cu)
 bool few_rows(Call& c, const Matrix& a, const Matrix& b, const Finish& f);
 
@@ -72,6 +75,7 @@ bool make_map(CUtensorMap* map, const Matrix& a, int* mn_major, int box_rows);
 
 struct Config {
     int cg, bn, form, whole, splits, split_slices;
+    double clocks;                         // estimated
 };
 // `sums`: binary32 results, whose long sums are taken in segments.  `alone`: no splits.
 Config choose(const Call& c, int64_t m, int64_t n, int64_t k, bool sums, bool alone);
@@ -119,13 +123,17 @@ void raise_shared(Call& c, K* kernel, int bytes) {
     c.check(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes));
 }
 
-template <int CG, int BN, class E, int FORM>
-void launch(Call& c, const CUtensorMap& ma, const CUtensorMap& mb, const Shape& s, const typename E::Args& f) {
-    auto* kernel = &product_kernel<CG, BN, E, FORM>;
+inline int units_of(const Shape& s) { return s.whole + (s.tiles_m * s.tiles_n - s.whole) * s.splits; }
+
+// `w` but for its unit counts.
+template <int CG, int BN, class E, int FORM, bool TWO = false>
+void launch(Call& c, Work<typename E::Args>& w) {
+    auto* kernel = &product_kernel<CG, BN, E, FORM, TWO>;
     raise_shared(c, kernel, kSmem);
-    const int64_t units = s.whole + (static_cast<int64_t>(s.tiles_m) * s.tiles_n - s.whole) * s.splits;
-    const int64_t blocks = FORM == kJoined ? units : std::min<int64_t>(units, c.sms / CG) * CG;
-    start(c, kernel, dim3(static_cast<unsigned>(blocks)), dim3(kThreads), kSmem, FORM == kJoined ? s.splits : CG, ma, mb, s, f, c.mark);
+    w.units[0] = units_of(w.s[0]);
+    w.units[1] = TWO ? units_of(w.s[1]) : 0;
+    const int units = w.units[0] + w.units[1], blocks = FORM == kJoined ? units : std::min(units, c.sms / CG) * CG;
+    start(c, kernel, dim3(static_cast<unsigned>(blocks)), dim3(kThreads), kSmem, FORM == kJoined ? w.s[0].splits : CG, w, c.mark);
 }
 
 inline int64_t round_up(int64_t v, int64_t to) { return (v + to - 1) / to * to; }
