@@ -58,7 +58,7 @@ struct Tiles {
     int cg, bn, form;
     double slice, last;
 };
-constexpr Tiles kPair{2, 256, kWhole, 580.0, 4000.0}, kHalfPair{2, 128, kWhole, 420.0, 2000.0}, kLongPair{2, 128, kLong, 420.0, 2000.0},
+constexpr Tiles kPair{2, 256, kWhole, 580.0, 4000.0}, kHalfPair{2, 128, kWhole, 420.0, 2000.0}, kLongPair{2, 192, kLong, 560.0, 3000.0},
     kBlock{1, 64, kWhole, 420.0, 1000.0}, kJoinedBlock{1, 64, kJoined, 420.0, 1000.0};
 constexpr double kLaunch = 4000.0;         // from one kernel's end to the next one's first products
 
@@ -211,7 +211,7 @@ static bool place(Call& c, const Config& cfg, const Matrix& a, const Matrix& b, 
 template <bool TWO>
 static void launch_as(Call& c, const Config& cfg, Work<Finish>& w) {
     if (cfg.form == kLong) {
-        launch<2, 128, General, kLong, TWO>(c, w);
+        launch<2, 192, General, kLong, TWO>(c, w);
     } else if (cfg.form == kJoined) {
         if constexpr (!TWO) launch<1, 64, General, kJoined>(c, w);
     } else if (cfg.cg == 1) {

@@ -9,7 +9,7 @@
 // one 128 x 64 tile and send each other their sums, every block adding a share of the tile, for products with fewer tiles than SMs;
 // kLong, for binary32 results of long sums: the tensor core's accumulator drops what does not fit, which after K
 // products shifts a sum by about K 2^-30 of itself, so it only adds kSegment of them and the epilogue
-// adds the segments in registers, rounding to nearest.
+// adds the segments in registers, rounding to nearest (192 columns, so that they fit: 96 a thread).
 // A pair computes 256 x BN with each block holding half of A and half of B.  An SM takes in 57 bytes a clock (measured:
 // 12 slices of a lone block's 128 x 128 tile, 393 KB, in 6850 clocks), so what a tile reads for its products decides: a pair's 256 x 256
 // needs 32 KB a block for 512 clocks of products, its 256 x 128 and a lone block's 128 x 64 24 KB for 256 and 128.  Large shapes
@@ -500,11 +500,11 @@ __global__ void __launch_bounds__(kThreads, 1)
 product_kernel(const __grid_constant__ Work<typename E::Args> work, unsigned int* mark) {
     constexpr int kM = 128 * CG;               // rows of the tile; a block has 128 of them
     constexpr int kBRows = BN / CG;            // of B, in this block
-    constexpr uint32_t kCols = 2 * BN;         // tensor memory columns: two accumulators
+    constexpr uint32_t kCols = BN <= 128 ? 2 * BN : 512;               // tensor memory columns, a power of two: two accumulators
     constexpr int kABytes = 16384;
     static_assert(FORM != kJoined || CG == 1, "joined tiles are a block's own");
-    constexpr int kStageBytes = kABytes + kBRows * 128;
-    constexpr uint32_t kBytes = CG * kStageBytes;
+    constexpr int kBChunks = (kBRows + 63) / 64;                       // of 64 columns where they are adjacent
+    constexpr int kStageBytes = kABytes + kBChunks * 8192;
 
     extern __shared__ uint8_t raw[];
     const uint32_t base = (tc::smem_addr(raw) + 1023u) & ~1023u;
@@ -574,7 +574,7 @@ product_kernel(const __grid_constant__ Work<typename E::Args> work, unsigned int
                 if (!(fine = tc::bar_wait(empty + 8 * st, phase))) break;
                 if (tc::elected()) {
                     const uint32_t a = base + st * kStageBytes, b = a + kABytes, bar = lead_full + 8 * st;
-                    if (rank == 0) tc::bar_expect(full + 8 * st, kBytes);
+                    if (rank == 0) tc::bar_expect(full + 8 * st, CG * (kABytes + (s.b_mn ? kBChunks * 8192 : kBRows * 128)));
                     if (s.a_mn) {
                         tc::load_tile<CG>(a, map_a, row, kb * kSlice, bar);
                         tc::load_tile<CG>(a + 8192, map_a, row + 64, kb * kSlice, bar);
@@ -583,7 +583,7 @@ product_kernel(const __grid_constant__ Work<typename E::Args> work, unsigned int
                     }
                     if (s.b_mn) {
 #pragma unroll
-                        for (int c = 0; c < kBRows / 64; ++c) tc::load_tile<CG>(b + 8192 * c, map_b, col + 64 * c, kb * kSlice, bar);
+                        for (int c = 0; c < kBChunks; ++c) tc::load_tile<CG>(b + 8192 * c, map_b, col + 64 * c, kb * kSlice, bar);
                     } else {
                         tc::load_tile<CG>(b, map_b, kb * kSlice, col, bar);
                     }
