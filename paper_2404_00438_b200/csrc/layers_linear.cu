@@ -37,26 +37,96 @@ __device__ __forceinline__ uint4 narrow(const float (&v)[8]) {
     return make_uint4(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7]));
 }
 
-// eight bf16 values at p, `valid` of them there (the rest 0)
-__device__ __forceinline__ uint4 take16(const __nv_bfloat16* p, uint32_t valid, bool wide) {
-    if (wide && valid == 8) return *reinterpret_cast<const uint4*>(p);
-    uint16_t b[8];
+// eight bf16 values at p, `valid` of them there (the rest 0); off the 16-byte grid, in words where words begin
+__device__ __forceinline__ uint4 take16(const __nv_bfloat16* at, uint32_t valid, bool wide) {
+    if (wide && valid == 8) return *reinterpret_cast<const uint4*>(at);
+    const uint16_t* p = reinterpret_cast<const uint16_t*>(at);
+    if (valid == 8 && (reinterpret_cast<uintptr_t>(p) & 3u) == 0) {
+        const uint32_t* w = reinterpret_cast<const uint32_t*>(p);
+        return make_uint4(w[0], w[1], w[2], w[3]);
+    }
+    if (valid == 8) {
+        const uint32_t* w = reinterpret_cast<const uint32_t*>(p + 1);
+        const uint32_t first = p[0], a = w[0], b = w[1], c = w[2], last = p[7];
+        return make_uint4(first | (a << 16), __funnelshift_r(a, b, 16), __funnelshift_r(b, c, 16), (c >> 16) | (last << 16));
+    }
+    uint32_t w[4] = {0, 0, 0, 0};
 #pragma unroll
-    for (int i = 0; i < 8; ++i) b[i] = static_cast<uint32_t>(i) < valid ? reinterpret_cast<const uint16_t*>(p)[i] : uint16_t{0};
-    uint32_t w[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) w[i] = b[2 * i] | (static_cast<uint32_t>(b[2 * i + 1]) << 16);
+    for (int i = 0; i < 7; ++i) {
+        if (static_cast<uint32_t>(i) < valid) w[i / 2] |= static_cast<uint32_t>(p[i]) << (16 * (i % 2));
+    }
     return make_uint4(w[0], w[1], w[2], w[3]);
 }
 
-__device__ __forceinline__ uint2 take8(const int8_t* p, uint32_t valid, bool wide) {
-    if (wide && valid == 8) return *reinterpret_cast<const uint2*>(p);
+__device__ __forceinline__ void give16(__nv_bfloat16* at, const uint4& v, uint32_t valid, bool wide) {
+    if (wide && valid == 8) {
+        *reinterpret_cast<uint4*>(at) = v;
+        return;
+    }
+    uint16_t* p = reinterpret_cast<uint16_t*>(at);
+    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+    if (valid == 8 && (reinterpret_cast<uintptr_t>(p) & 3u) == 0) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) reinterpret_cast<uint32_t*>(p)[i] = w[i];
+    } else if (valid == 8) {
+        p[0] = static_cast<uint16_t>(v.x);
+#pragma unroll
+        for (int i = 0; i < 3; ++i) reinterpret_cast<uint32_t*>(p + 1)[i] = __funnelshift_r(w[i], w[i + 1], 16);
+        p[7] = static_cast<uint16_t>(v.w >> 16);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 7; ++i) {
+            if (static_cast<uint32_t>(i) < valid) p[i] = static_cast<uint16_t>(w[i / 2] >> (16 * (i % 2)));
+        }
+    }
+}
+
+__device__ __forceinline__ uint2 take8(const int8_t* at, uint32_t valid, bool wide) {
+    if (wide && valid == 8) return *reinterpret_cast<const uint2*>(at);
+    const uint8_t* p = reinterpret_cast<const uint8_t*>(at);
+    if (valid == 8 && (reinterpret_cast<uintptr_t>(p) & 1u) != 0) {
+        const uint16_t* h = reinterpret_cast<const uint16_t*>(p + 1);
+        const uint32_t first = p[0], a = h[0], b = h[1], c = h[2], last = p[7];
+        return make_uint2(first | (a << 8) | (b << 24), (b >> 8) | (c << 8) | (last << 24));
+    }
+    if (valid == 8) {
+        const uint16_t* h = reinterpret_cast<const uint16_t*>(p);
+        return make_uint2(h[0] | (static_cast<uint32_t>(h[1]) << 16), h[2] | (static_cast<uint32_t>(h[3]) << 16));
+    }
     uint32_t w[2] = {0, 0};
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        if (static_cast<uint32_t>(i) < valid) w[i / 4] |= static_cast<uint32_t>(static_cast<uint8_t>(p[i])) << (8 * (i % 4));
+    for (int i = 0; i < 7; ++i) {
+        if (static_cast<uint32_t>(i) < valid) w[i / 4] |= static_cast<uint32_t>(p[i]) << (8 * (i % 4));
     }
     return make_uint2(w[0], w[1]);
+}
+
+__device__ __forceinline__ void give8(int8_t* at, const uint2& v, uint32_t valid, bool wide) {
+    if (wide && valid == 8) {
+        *reinterpret_cast<uint2*>(at) = v;
+        return;
+    }
+    uint8_t* p = reinterpret_cast<uint8_t*>(at);
+    if (valid == 8 && (reinterpret_cast<uintptr_t>(p) & 1u) != 0) {
+        uint16_t* h = reinterpret_cast<uint16_t*>(p + 1);
+        p[0] = static_cast<uint8_t>(v.x);
+        h[0] = static_cast<uint16_t>(v.x >> 8);
+        h[1] = static_cast<uint16_t>((v.x >> 24) | (v.y << 8));
+        h[2] = static_cast<uint16_t>(v.y >> 8);
+        p[7] = static_cast<uint8_t>(v.y >> 24);
+    } else if (valid == 8) {
+        uint16_t* h = reinterpret_cast<uint16_t*>(p);
+        h[0] = static_cast<uint16_t>(v.x);
+        h[1] = static_cast<uint16_t>(v.x >> 16);
+        h[2] = static_cast<uint16_t>(v.y);
+        h[3] = static_cast<uint16_t>(v.y >> 16);
+    } else {
+        const uint32_t w[2] = {v.x, v.y};
+#pragma unroll
+        for (int i = 0; i < 7; ++i) {
+            if (static_cast<uint32_t>(i) < valid) p[i] = static_cast<uint8_t>(w[i / 4] >> (8 * (i % 4)));
+        }
+    }
 }
 
 // act(u) as a bf16 operand.  Bound by memory: 2 (or 33/32) + 2 bytes a value.
@@ -106,15 +176,7 @@ __global__ void __launch_bounds__(256) operand_kernel(const void* u, int64_t u_l
         }
 #pragma unroll
         for (int j = 0; j < 8; ++j) v[j] = act_value<ACT>(v[j]);
-        __nv_bfloat16* o = out + (row0 + r) * out_ld + col;
-        if (wide_out && valid == 8) {
-            *reinterpret_cast<uint4*>(o) = narrow(v);
-        } else {
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                if (static_cast<uint32_t>(j) < valid) o[j] = __float2bfloat16_rn(v[j]);
-            }
-        }
+        give16(out + (row0 + r) * out_ld + col, narrow(v), valid, wide_out);
     }
 }
 
@@ -151,15 +213,7 @@ __global__ void __launch_bounds__(256) checkpoint8_kernel(const __nv_bfloat16* x
         const uint32_t o[2] = {bytes4(quantise8(v[0], inv), quantise8(v[1], inv), quantise8(v[2], inv), quantise8(v[3], inv)),
                                bytes4(quantise8(v[4], inv), quantise8(v[5], inv), quantise8(v[6], inv), quantise8(v[7], inv))};
         if (row0 + r >= m || valid == 0) continue;
-        int8_t* p = q + (row0 + r) * q_ld + col;
-        if (wide_out && valid == 8) {
-            *reinterpret_cast<uint2*>(p) = make_uint2(o[0], o[1]);
-        } else {
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                if (static_cast<uint32_t>(j) < valid) p[j] = static_cast<int8_t>(o[j / 4] >> (8 * (j % 4)));
-            }
-        }
+        give8(q + (row0 + r) * q_ld + col, make_uint2(o[0], o[1]), valid, wide_out);
     }
     __syncthreads();
     if (row0 + lane < m && col0 + warp * 32 < k) e[(col0 / 32 + warp) * e_ld + row0 + lane] = ex[warp][lane];

@@ -28,6 +28,46 @@ EncodeTiled encoder() {
     return fn;
 }
 
+// Rows of `cols` adjacent values, off the 16-byte grid, to rows on it.  A thread puts eight values together from the two
+// 16-byte units that hold them (the second one comes from L1), all of a row shifted alike; units that reach beyond the row are
+// read value by value.  Bound by memory: 4 bytes a value (8192 x 8191: 150 us with 2-byte accesses).
+__device__ __forceinline__ uint4 unit_of_row(const uint8_t* unit, const uint8_t* from, const uint8_t* to) {
+    if (unit >= from && unit + 16 <= to) return __ldg(reinterpret_cast<const uint4*>(unit));
+    uint32_t w[4] = {0, 0, 0, 0};
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const uint8_t* p = unit + 2 * i;
+        if (p >= from && p < to) w[i / 2] |= static_cast<uint32_t>(__ldg(reinterpret_cast<const unsigned short*>(p))) << (16 * (i % 2));
+    }
+    return make_uint4(w[0], w[1], w[2], w[3]);
+}
+
+__global__ void __launch_bounds__(256) pack_rows_kernel(const uint16_t* a, int64_t rs, int64_t rows, int64_t cols, uint16_t* out, int64_t ld) {
+    tc::let_next_start();
+    tc::wait_for_previous();
+    const int64_t col = (static_cast<int64_t>(blockIdx.y) * 128 + threadIdx.x % 128) * 8;
+    if (col >= cols) return;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int64_t row = static_cast<int64_t>(blockIdx.x) * 8 + threadIdx.x / 128 + 2 * i;
+        if (row >= rows) break;
+        const uint8_t* from = reinterpret_cast<const uint8_t*>(a + row * rs);
+        const uint32_t off = static_cast<uint32_t>(reinterpret_cast<uintptr_t>(from) & 15u);
+        const uint8_t* unit = from - off + col * 2;
+        const uint4 x = unit_of_row(unit, from, from + cols * 2);
+        const uint4 y = off == 0 ? x : unit_of_row(unit + 16, from, from + cols * 2);
+        const uint32_t w[8] = {x.x, x.y, x.z, x.w, y.x, y.y, y.z, y.w};
+        uint32_t o[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {          // the row's offset is the same for the whole warp
+            const uint32_t lo = off < 4 ? w[j] : off < 8 ? w[j + 1] : off < 12 ? w[j + 2] : w[j + 3];
+            const uint32_t hi = off < 4 ? w[j + 1] : off < 8 ? w[j + 2] : off < 12 ? w[j + 3] : w[j + 4];
+            o[j] = (off & 2u) ? __funnelshift_r(lo, hi, 16) : lo;
+        }
+        *reinterpret_cast<uint4*>(out + row * ld + col) = make_uint4(o[0], o[1], o[2], o[3]);
+    }
+}
+
 // out[r][c] = a[r * rs + c * cs], rows of ld elements; reads run along whichever stride is smaller.
 __global__ void __launch_bounds__(256) pack_kernel(const uint16_t* a, int64_t rs, int64_t cs, int64_t rows, int64_t cols,
                                                    uint16_t* out, int64_t ld) {
@@ -156,14 +196,21 @@ Matrix readable(Call& c, const Matrix& a) {
         if (a.cols == 1) r.cs = round_up(a.rows, 8);
         return r;
     }
-    r.rs = round_up(a.cols, 8);
-    r.cs = 1;
-    uint16_t* out = c.ws.take<uint16_t>(static_cast<uint64_t>(a.rows) * r.rs);
+    // adjacent columns stay adjacent, adjacent rows too; anything else becomes adjacent columns
+    const bool along_rows = a.cs != 1 && a.rs == 1;
+    const int64_t rows = along_rows ? a.cols : a.rows, cols = along_rows ? a.rows : a.cols;
+    const int64_t ld = round_up(cols, 8);
+    r.rs = along_rows ? 1 : ld;
+    r.cs = along_rows ? ld : 1;
+    uint16_t* out = c.ws.take<uint16_t>(static_cast<uint64_t>(rows) * ld);
     r.p = out;
-    if (c.live()) {
-        const int64_t blocks = parts(a.rows, 32) * parts(a.cols, 32);
-        start(c, pack_kernel, dim3(static_cast<unsigned>(blocks)), dim3(256), 0, 1, static_cast<const uint16_t*>(a.p), a.rs, a.cs, a.rows,
-              a.cols, out, r.rs);
+    if (!c.live()) return r;
+    const auto* from = static_cast<const uint16_t*>(a.p);
+    if ((a.cs == 1 || a.rs == 1) && parts(cols, 1024) <= 65535) {
+        start(c, pack_rows_kernel, dim3(static_cast<unsigned>(parts(rows, 8)), static_cast<unsigned>(parts(cols, 1024))), dim3(256), 0, 1, from,
+              along_rows ? a.cs : a.rs, rows, cols, out, ld);
+    } else {
+        start(c, pack_kernel, dim3(static_cast<unsigned>(parts(rows, 32) * parts(cols, 32))), dim3(256), 0, 1, from, a.rs, a.cs, rows, cols, out, ld);
     }
     return r;
 }

@@ -155,6 +155,14 @@ struct Piece {
                 const int r = lane / 4 + 8 * i, c = lane % 4;
                 if (r < rows) *reinterpret_cast<uint4*>(p + r * ld + c * 8) = stage[unit2(r, c)];
             }
+        } else if (cols == 32 && ((reinterpret_cast<uintptr_t>(p) & 3u) | static_cast<uintptr_t>(ld & 1)) == 0) {
+            const uint32_t* s = reinterpret_cast<const uint32_t*>(stage);      // rows of words, two at a time
+            const int l = lane % 16;
+#pragma unroll 8
+            for (int i = 0; i < 16; ++i) {
+                const int r = 2 * i + lane / 16;
+                if (r < rows) *reinterpret_cast<uint32_t*>(p + r * ld + 2 * l) = s[unit2(r, l / 4) * 4 + l % 4];
+            }
         } else if (lane < cols) {
             const uint16_t* s = reinterpret_cast<const uint16_t*>(stage);
             #pragma unroll 8
