@@ -234,11 +234,14 @@ column_sums_kernel(const __nv_bfloat16* a, int64_t rs, int64_t cs, int64_t rows,
     tc::wait_for_previous();
     float v[8] = {};
     const int64_t first = static_cast<int64_t>(rank) * 32 + line;
-    if (wide && c0 + 8 <= cols) {
+    if (wide && c0 < cols && (c0 + 8 <= cols || c0 + 8 <= rs)) {
+        // a row's last columns may share their 16 bytes with what lies between it and the next row; after the last row may be nothing
+        const bool ragged = c0 + 8 > cols;
+        const int64_t whole = ragged ? rows - 1 : rows;
         const uint4* p = reinterpret_cast<const uint4*>(a + first * rs + c0);
         const int64_t step = rs * (kSumBlocks * 32 / 8);
         int64_t r = first;
-        for (; r + 7 * kSumBlocks * 32 < rows; r += 8 * kSumBlocks * 32, p += 8 * step) {
+        for (; r + 7 * kSumBlocks * 32 < whole; r += 8 * kSumBlocks * 32, p += 8 * step) {
             uint4 w[8];
 #pragma unroll
             for (int i = 0; i < 8; ++i) w[i] = p[i * step];
@@ -250,11 +253,17 @@ column_sums_kernel(const __nv_bfloat16* a, int64_t rs, int64_t cs, int64_t rows,
                 for (int j = 0; j < 8; ++j) v[j] += x[j];
             }
         }
-        for (; r < rows; r += kSumBlocks * 32, p += step) {
+        for (; r < whole; r += kSumBlocks * 32, p += step) {
             float x[8];
             widen(*p, x);
 #pragma unroll
             for (int j = 0; j < 8; ++j) v[j] += x[j];
+        }
+        if (ragged && r == rows - 1) {
+#pragma unroll
+            for (int j = 0; j < 7; ++j) {
+                if (c0 + j < cols) v[j] += __bfloat162float(a[r * rs + c0 + j]);
+            }
         }
     } else {
         for (int64_t r = first; r < rows; r += kSumBlocks * 32) {
