@@ -15,16 +15,15 @@
  *     follows a sum (bias, activation, residual, softmax statistics) is binary32, and an output
  *     is rounded once, when it is stored (bf16: nearest, ties to even);
  *   - act(u) is rounded to bf16 as an operand of dW (the forward product read the same values), and
- *     so is d_tv as an operand of dx and dW;
+ *     so is softmax_tv - [v = y_t] as an operand of dx and dW (g multiplies their sums);
  *   - gelu is the tanh form z/2 (1 + tanh(sqrt(2/pi) (z + 0.044715 z^3))); silu is z/(1 + exp(-z));
  *   - NaN and infinities go through as the formulas say; relu(NaN) = NaN.
  *
  * Every buffer is DEVICE memory owned by the caller.  A matrix is a pointer and two strides in
- * ELEMENTS; rows, cols and strides are non-negative and at most 2^30 rows and columns (2^24 - 256 columns
- * of u and of the 8-bit form).  Where a
- * parameter has one stride ("ld", between rows) its columns are adjacent.  x, w, dy take any strides:
- * an operand that the copy engine cannot read in place (neither stride 1, a base or the other stride
- * off the 16-byte grid) is packed into the workspace first.  m = 0 (no rows) is allowed: sums over
+ * ELEMENTS; strides are non-negative, rows and columns at most 2^30 (2^24 - 256 columns of u and of the
+ * 8-bit form).  Where a parameter has one stride ("ld", between rows) its columns are adjacent.  x, w, dy
+ * take any strides: an operand that the copy engine cannot read in place (neither stride 1, a base or the
+ * other stride off the 16-byte grid) is packed into the workspace first.  m = 0 (no rows) is allowed: sums over
  * no rows are zero.  Inputs and outputs must not overlap, except that residual may equal y or dx.
  *
  * Calls are asynchronous on the given stream, never synchronise, allocate nothing and keep no state:
@@ -115,8 +114,8 @@ dlion_status dlion_checkpoint8(const void* x, int64_t x_ld, int64_t m, int64_t k
 dlion_status dlion_restore8(const int8_t* q, int64_t q_ld, const uint8_t* e, int64_t e_ld, int64_t m, int64_t k,
                             void* x, int64_t x_ld, void* cuda_stream);
 
-/* Every wait inside the kernels ends after a time limit; a kernel whose wait ran out writes nothing
- * more and leaves a mark on the device.  Synchronises the stream and returns DLION_OK, DLION_ESTATE
+/* Every wait inside the kernels ends after a time limit; a kernel whose wait ran out ends, its outputs
+ * undefined, and leaves a mark on the device.  Synchronises the stream and returns DLION_OK, DLION_ESTATE
  * if a mark was left since the last call (and clears it), or DLION_ECUDA. */
 dlion_status dlion_layers_check(void* cuda_stream);
 
