@@ -1,4 +1,4 @@
-// Products of one to 32 rows (a serving step): every weight is read once and used a few times, so the only
+// Products of one to 16 rows (a serving step): every weight is read once and used a few times, so the only
 // question is how fast the weights stream.  The arithmetic is the warp-level 16 x 8 x 16 matrix instruction with its k (or n)
 // indices renamed so that a thread's share of the weights is 16 adjacent bytes.  Each warp has a ring of its own, filled by
 // tiled copies of whole 128-byte lines, some 160 KB of which are under way on an SM, through the ends of the columns' sums
@@ -12,7 +12,7 @@ namespace prod {
 
 namespace {
 
-constexpr int kFewThreads = 256, kFewWarps = 8, kFewRows = 32;
+constexpr int kFewThreads = 256, kFewWarps = 8;
 
 __device__ __forceinline__ void mma_16x8x16(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
     asm volatile(
@@ -311,9 +311,9 @@ bool few_rows(Call& c, const Matrix& a, const Matrix& b, const Finish& f) {
     if (a.rows > kFewRows || a.cs != 1 || (a.rows > 1 && a.rs % 8 != 0) || f.accumulated != nullptr) return false;
     if (!c.live()) return true;
     if (b.cs == 1) {
-        a.rows <= 8 ? start_few<true, 1>(c, a, b, f) : a.rows <= 16 ? start_few<true, 2>(c, a, b, f) : start_few<true, 4>(c, a, b, f);
+        a.rows <= 8 ? start_few<true, 1>(c, a, b, f) : start_few<true, 2>(c, a, b, f);
     } else {
-        a.rows <= 16 ? start_few<false, 1>(c, a, b, f) : start_few<false, 2>(c, a, b, f);
+        start_few<false, 1>(c, a, b, f);
     }
     return true;
 }

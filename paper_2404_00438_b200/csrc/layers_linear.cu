@@ -403,7 +403,7 @@ void backward(Call& c, const dlion_linear_bwd& p) {
         return;
     }
     const Matrix dy = readable(c, Matrix{p.dy, p.m, p.n, p.dy_rs, p.dy_cs});
-    Matrix w{}, a{};
+    Matrix w{nullptr, p.k, p.n, 0, 0}, a{nullptr, p.m, p.k, 0, 0};
     Finish fx{}, fw{};
     if (p.dx != nullptr) {
         w = readable(c, Matrix{p.w, p.k, p.n, p.w_rs, p.w_cs});
@@ -418,7 +418,8 @@ void backward(Call& c, const dlion_linear_bwd& p) {
         fx.out = p.dx;
         fx.out_ld = p.dx_ld;
     }
-    const bool rows = p.dw_cs == 1 && (p.k == 1 || p.dw_rs >= p.n);
+    // where no dw is wanted, the order of its arena's rows does not matter
+    const bool rows = p.dw == nullptr || (p.dw_cs == 1 && (p.k == 1 || p.dw_rs >= p.n));
     if (p.dw != nullptr) {
         if (p.saved == DLION_KEEP_BF16 && p.act == DLION_ACT_NONE) {
             a = readable(c, Matrix{p.u, p.m, p.k, p.u_ld, 1});
@@ -432,14 +433,7 @@ void backward(Call& c, const dlion_linear_bwd& p) {
         fw.out_f32 = p.grad_type == DLION_GRAD_F32;
         fw.out_ld = rows ? p.dw_rs : p.dw_cs;
     }
-    const Matrix wa = transposed(rows ? a : dy), wb = transposed(rows ? dy : a);
-    if (p.dx != nullptr && p.dw != nullptr) {
-        products(c, dy, w, fx, wa, wb, fw);
-    } else if (p.dx != nullptr) {
-        product(c, dy, w, fx);
-    } else if (p.dw != nullptr) {
-        product(c, wa, wb, fw);
-    }
+    products(c, Part{dy, w, fx, p.dx != nullptr}, Part{transposed(rows ? a : dy), transposed(rows ? dy : a), fw, p.dw != nullptr});
     if (p.db != nullptr) column_sums(c, dy, p.db, p.grad_type);
 }
 

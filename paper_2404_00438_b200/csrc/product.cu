@@ -113,7 +113,7 @@ int64_t tiles_of(const Tiles& t, int64_t m, int64_t n) { return parts(m, 128 * t
 Config choose(const Call& c, int64_t m, int64_t n, int64_t k, bool sums, bool alone) {
     const int64_t slices = std::max<int64_t>(1, parts(k, kSlice));
     const bool long_sums = sums && slices > kSegment;
-    Config best{2, 256, kWhole, 0, 1, static_cast<int>(slices), 1e300};
+    Config best{2, 256, kWhole, static_cast<int>(tiles_of(kPair, m, n)), 1, static_cast<int>(slices), 1e300};
     auto consider = [&](const Tiles& f, int64_t s) {
         const int64_t per = parts(slices, s);
         if (parts(slices, per) != s) return;
@@ -121,7 +121,7 @@ Config choose(const Call& c, int64_t m, int64_t n, int64_t k, bool sums, bool al
         int64_t whole = 0;
         double t;
         if (f.form == kJoined) {
-            if (tiles * s > 16 * 8) return;    // what fits at a time, or nearly (15 clusters of eight)
+            if (tiles > (s == 2 ? c.sms / 2 : s == 4 ? c.sms * 33 / 148 : c.sms * 15 / 148)) return;     // clusters that fit at a time
             t = per * f.slice + 4500.0 + f.last;
         } else {
             whole = s == 1 ? tiles : tiles / workers * workers;
@@ -300,26 +300,27 @@ void product(Call& c, const Matrix& a, const Matrix& b, Finish f) {
     c.ws.used = mark;
 }
 
-void products(Call& c, const Matrix& a0, const Matrix& b0, Finish f0, const Matrix& a1, const Matrix& b1, Finish f1) {
+void products(Call& c, const Part& first, const Part& second) {
     // both as whole tiles of one kind, the longer sums first, against each for itself; few rows have their own kernel
-    const bool few = a0.rows <= 32 || a1.rows <= 32;
-    const Config best0 = choose(c, a0.rows, b0.rows, a0.cols, long_sums(f0), false), best1 = choose(c, a1.rows, b1.rows, a1.cols, long_sums(f1), false);
-    const int64_t slices0 = parts(a0.cols, kSlice), slices1 = parts(a1.cols, kSlice);
-    const bool swap = slices1 > slices0;
-    const bool sums = (long_sums(f0) && slices0 > kSegment) || (long_sums(f1) && slices1 > kSegment);
-    const int64_t most = std::max(slices0, slices1), least = std::min(slices0, slices1);
+    const Part* parts_of[2] = {&first, &second};
+    if (second.a.cols > first.a.cols) std::swap(parts_of[0], parts_of[1]);
+    const Part &p0 = *parts_of[0], &p1 = *parts_of[1];
+    const bool few = p0.a.rows <= kFewRows || p1.a.rows <= kFewRows;
+    const Config best0 = choose(c, p0.a.rows, p0.b.rows, p0.a.cols, long_sums(p0.f), false);
+    const Config best1 = choose(c, p1.a.rows, p1.b.rows, p1.a.cols, long_sums(p1.f), false);
+    const int64_t slices0 = parts(p0.a.cols, kSlice), slices1 = parts(p1.a.cols, kSlice);
+    const bool sums = (long_sums(p0.f) && slices0 > kSegment) || (long_sums(p1.f) && slices1 > kSegment);
     double clocks = best0.clocks + best1.clocks + kLaunch;
     Config cfg{};
     int64_t extra = 0;
     for (const Tiles* f : {&kPair, &kHalfPair, &kBlock, &kLongPair}) {
         if (few || sums != (f->form == kLong)) continue;
-        const int64_t t0 = tiles_of(*f, a0.rows, b0.rows), t1 = tiles_of(*f, a1.rows, b1.rows), workers = c.sms / f->cg;
+        const int64_t t0 = tiles_of(*f, p0.a.rows, p0.b.rows), t1 = tiles_of(*f, p1.a.rows, p1.b.rows), workers = c.sms / f->cg;
         if (t0 + t1 >= (int64_t{1} << 30)) continue;
-        const double big = most * f->slice + 300.0, small = least * f->slice + 300.0;
-        const int64_t first = swap ? t1 : t0, second = swap ? t0 : t1, over = first % workers;
-        const int64_t ahead = over == 0 ? 0 : static_cast<int64_t>(big / small + 0.5);
-        const int64_t rest = std::max<int64_t>(0, second - ahead * (workers - over));
-        const double t = parts(first, workers) * big + parts(rest, workers) * small + f->last;
+        const double big = slices0 * f->slice + 300.0, small = slices1 * f->slice + 300.0;
+        const int64_t over = t0 % workers, ahead = over == 0 ? 0 : static_cast<int64_t>(big / small + 0.5);
+        const int64_t rest = std::max<int64_t>(0, t1 - ahead * (workers - over));
+        const double t = parts(t0, workers) * big + parts(rest, workers) * small + f->last;
         if (t < clocks) {
             clocks = t;
             cfg = Config{f->cg, f->bn, f->form, 0, 1, 0, t};
@@ -327,28 +328,29 @@ void products(Call& c, const Matrix& a0, const Matrix& b0, Finish f0, const Matr
         }
     }
     if (cfg.cg == 0) {
-        product(c, a0, b0, f0);
-        product(c, a1, b1, f1);
+        if (first.wanted) product(c, first.a, first.b, first.f);
+        if (second.wanted) product(c, second.a, second.b, second.f);
         return;
     }
     if (!c.live()) return;
-    complete(f0, a0, b0);
-    complete(f1, a1, b1);
     Work<Finish> w{};
-    const Matrix *a[2] = {swap ? &a1 : &a0, swap ? &a0 : &a1}, *b[2] = {swap ? &b1 : &b0, swap ? &b0 : &b1};
-    w.args[0] = swap ? f1 : f0;
-    w.args[1] = swap ? f0 : f1;
     w.extra = static_cast<int>(extra);
-    for (int i = 0; i < 2; ++i) {
-        cfg.split_slices = static_cast<int>(parts(a[i]->cols, kSlice));
-        cfg.whole = static_cast<int>(parts(a[i]->rows, 128 * cfg.cg) * parts(b[i]->rows, cfg.bn));
-        if (!shape_of(cfg, *a[i], *b[i], &w.s[i])) {
+    int n = 0;
+    for (const Part* part : parts_of) {
+        if (!part->wanted) continue;
+        w.args[n] = part->f;
+        complete(w.args[n], part->a, part->b);
+        cfg.split_slices = static_cast<int>(parts(part->a.cols, kSlice));
+        cfg.whole = static_cast<int>(parts(part->a.rows, 128 * cfg.cg) * parts(part->b.rows, cfg.bn));
+        if (!shape_of(cfg, part->a, part->b, &w.s[n])) {
             c.status = DLION_EINVAL;
             return;
         }
-        if (!place(c, cfg, *a[i], *b[i], w, i)) return;
+        if (!place(c, cfg, part->a, part->b, w, n)) return;
+        ++n;
     }
-    launch_as<true>(c, cfg, w);
+    if (n == 2) launch_as<true>(c, cfg, w);
+    if (n == 1) launch_as<false>(c, cfg, w);
 }
 
 }  // namespace prod

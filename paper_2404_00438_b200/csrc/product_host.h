@@ -62,10 +62,18 @@ Matrix readable(Call& c, const Matrix& a);
 // Both must be readable.  f.m, f.n are set here.
 void product(Call& c, const Matrix& a, const Matrix& b, Finish f);
 
-// Two products that do not depend on each other, in one launch where that is expected to take less time.
-void products(Call& c, const Matrix& a0, const Matrix& b0, Finish f0, const Matrix& a1, const Matrix& b1, Finish f1);
+// Two products that do not depend on each other, in one launch where that is expected to take less time.  One of them alone
+// (the other's matrices need only their sizes) is divided as it is beside the other, so that its bits are the same.
+struct Part {
+    Matrix a, b;
+    Finish f;
+    bool wanted;
+};
+void products(Call& c, const Part& first, const Part& second);
 
-// The same for at most 32 rows of a; false if this is not such a product.  (few_rows.cu)
+constexpr int64_t kFewRows = 16;
+
+// The same for at most kFewRows rows of a; false if this is not such a product.  (few_rows.cu)
 bool few_rows(Call& c, const Matrix& a, const Matrix& b, const Finish& f);
 
 inline Matrix transposed(const Matrix& a) { return Matrix{a.p, a.cols, a.rows, a.cs, a.rs}; }
