@@ -24,15 +24,6 @@ constexpr int kTileRows = 32, kTileCols = 256;
 
 __device__ __forceinline__ uint32_t extent(int64_t left, int most) { return static_cast<uint32_t>(left < most ? (left > 0 ? left : 0) : most); }
 
-__device__ __forceinline__ void widen(const uint4& w, float (&v)[8]) {
-    const uint32_t x[4] = {w.x, w.y, w.z, w.w};
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        v[2 * i] = bf16_lo(x[i]);
-        v[2 * i + 1] = bf16_hi(x[i]);
-    }
-}
-
 __device__ __forceinline__ uint4 narrow(const float (&v)[8]) {
     return make_uint4(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7]));
 }
@@ -433,8 +424,10 @@ void backward(Call& c, const dlion_linear_bwd& p) {
         fw.out_f32 = p.grad_type == DLION_GRAD_F32;
         fw.out_ld = rows ? p.dw_rs : p.dw_cs;
     }
-    products(c, Part{dy, w, fx, p.dx != nullptr}, Part{transposed(rows ? a : dy), transposed(rows ? dy : a), fw, p.dw != nullptr});
-    if (p.db != nullptr) column_sums(c, dy, p.db, p.grad_type);
+    Beside beside{static_cast<const __nv_bfloat16*>(dy.p), dy.rs, static_cast<int>(p.m), static_cast<int>(p.n), p.db, p.grad_type == DLION_GRAD_F32, 0};
+    if (p.db == nullptr || dy.cs != 1 || !aligned16(dy.p) || dy.rs % 8 != 0) beside.out = nullptr;
+    const bool summed = products(c, Part{dy, w, fx, p.dx != nullptr}, Part{transposed(rows ? a : dy), transposed(rows ? dy : a), fw, p.dw != nullptr}, beside);
+    if (p.db != nullptr && !summed) column_sums(c, dy, p.db, p.grad_type);
 }
 
 }  // namespace

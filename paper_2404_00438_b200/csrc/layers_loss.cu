@@ -384,7 +384,7 @@ void loss(Call& c, const dlion_loss& p) {
         fw.out_ld = last ? p.dw_ld : so_far_ld;
         fw.out_f32 = f32 || !last;
         fw.rough = 1;
-        products(c, Part{d, transposed(w), fx, true}, Part{transposed(d), transposed(xp), fw, true});
+        products(c, Part{d, transposed(w), fx, true}, Part{transposed(d), transposed(xp), fw, true}, Beside{});
     }
 }
 

@@ -272,14 +272,26 @@ static void launch_as(Call& c, const Config& cfg, Work<Finish>& w) {
 
 static bool long_sums(const Finish& f) { return f.out_f32 != 0 && f.rough == 0; }
 
-void product(Call& c, const Matrix& a, const Matrix& b, Finish f) {
+// Whether `blocks` blocks that are there for `clocks` have the time to sum the columns, and how: a warp has eight loads under way,
+// some 1500 clocks, and reads whole sectors where there are columns enough.
+static bool fits_beside(Beside& s, int64_t blocks, double clocks) {
+    if (s.out == nullptr) return false;
+    for (int lanes = 4; lanes >= 1; lanes /= 2) {
+        const double strips = static_cast<double>(parts(parts(s.cols, 8 * lanes), 2 * blocks));
+        s.lanes = lanes;
+        if (strips * parts(s.rows, 8 * (32 / lanes)) * 1500.0 + 1500.0 < 0.7 * clocks) return true;
+    }
+    return false;
+}
+
+static bool product_beside(Call& c, const Matrix& a, const Matrix& b, Finish f, Beside beside) {
     complete(f, a, b);
-    if (few_rows(c, a, b, f)) return;
+    if (few_rows(c, a, b, f)) return false;
     const Config cfg = choose(c, a.rows, b.rows, a.cols, long_sums(f), false);
     Work<Finish> w{};
     if (!shape_of(cfg, a, b, &w.s[0])) {
         c.status = DLION_EINVAL;
-        return;
+        return false;
     }
     const uint64_t mark = c.ws.used;
     const int64_t split_tiles = cfg.form == kJoined || cfg.splits == 1 ? 0 : static_cast<int64_t>(w.s[0].tiles_m) * w.s[0].tiles_n - cfg.whole;
@@ -290,17 +302,23 @@ void product(Call& c, const Matrix& a, const Matrix& b, Finish f) {
         tickets *= 4;
         f.tickets = c.ws.take<unsigned int>(tickets);
     }
+    const int64_t blocks = std::min<int64_t>(units_of(w.s[0]), c.sms / cfg.cg) * cfg.cg;
+    const bool summed = fits_beside(beside, blocks, cfg.clocks);
     if (c.live() && place(c, cfg, a, b, w, 0)) {
         w.args[0] = f;
+        if (summed) w.beside = beside;
         if (tickets != 0) c.check(cudaMemsetAsync(f.tickets, 0, tickets * sizeof(unsigned int), c.stream));
         launch_as<false>(c, cfg, w);
     }
     // later products of the call reuse the split sums' place (the stream orders them): the size query keeps the maximum
     if (c.ws.dry) c.ws.size = std::max(c.ws.size, c.ws.used);
     c.ws.used = mark;
+    return summed;
 }
 
-void products(Call& c, const Part& first, const Part& second) {
+void product(Call& c, const Matrix& a, const Matrix& b, Finish f) { product_beside(c, a, b, f, Beside{}); }
+
+bool products(Call& c, const Part& first, const Part& second, Beside beside) {
     // both as whole tiles of one kind, the longer sums first, against each for itself; few rows have their own kernel
     const Part* parts_of[2] = {&first, &second};
     if (second.a.cols > first.a.cols) std::swap(parts_of[0], parts_of[1]);
@@ -328,11 +346,15 @@ void products(Call& c, const Part& first, const Part& second) {
         }
     }
     if (cfg.cg == 0) {
-        if (first.wanted) product(c, first.a, first.b, first.f);
-        if (second.wanted) product(c, second.a, second.b, second.f);
-        return;
+        bool summed = false;
+        for (const Part* part : {&first, &second}) {
+            if (!part->wanted) continue;
+            summed = product_beside(c, part->a, part->b, part->f, beside) || summed;
+            if (summed) beside.out = nullptr;
+        }
+        return summed;
     }
-    if (!c.live()) return;
+    if (!first.wanted && !second.wanted) return false;
     Work<Finish> w{};
     w.extra = static_cast<int>(extra);
     int n = 0;
@@ -344,13 +366,18 @@ void products(Call& c, const Part& first, const Part& second) {
         cfg.whole = static_cast<int>(parts(part->a.rows, 128 * cfg.cg) * parts(part->b.rows, cfg.bn));
         if (!shape_of(cfg, part->a, part->b, &w.s[n])) {
             c.status = DLION_EINVAL;
-            return;
+            return false;
         }
-        if (!place(c, cfg, part->a, part->b, w, n)) return;
+        if (c.live() && !place(c, cfg, part->a, part->b, w, n)) return false;
         ++n;
     }
+    const int units = units_of(w.s[0]) + (n == 2 ? units_of(w.s[1]) : 0);
+    const bool summed = fits_beside(beside, std::min(units, c.sms / cfg.cg) * cfg.cg, n == 2 ? clocks : clocks / 2);
+    if (summed) w.beside = beside;
+    if (!c.live()) return summed;
     if (n == 2) launch_as<true>(c, cfg, w);
     if (n == 1) launch_as<false>(c, cfg, w);
+    return summed;
 }
 
 }  // namespace prod

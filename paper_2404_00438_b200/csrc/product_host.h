@@ -69,7 +69,8 @@ struct Part {
     Finish f;
     bool wanted;
 };
-void products(Call& c, const Part& first, const Part& second);
+// `beside`: column sums that the products' idle warps take along where they have the time for it; false if they do not.
+bool products(Call& c, const Part& first, const Part& second, Beside beside);
 
 constexpr int64_t kFewRows = 16;
 
