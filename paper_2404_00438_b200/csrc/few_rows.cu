@@ -2,7 +2,7 @@
 // question is how fast the weights stream.  The arithmetic is the warp-level 16 x 8 x 16 matrix instruction with its k (or n)
 // indices renamed so that a thread's share of the weights is 16 adjacent bytes.  Each warp has a ring of its own, filled by
 // tiled copies of whole 128-byte lines, some 160 KB of which are under way on an SM, through the ends of the columns' sums
-// too.  (Shares of 16 bytes loaded by the threads themselves, to registers or to shared memory, cut the lines in half
+// too.  8 rows over 50257 x 2048 with a bias: 35.6 us, 207.5 MB, 5.8 TB/s.  (Shares of 16 bytes loaded by the threads themselves, to registers or to shared memory, cut the lines in half
 // between warps: 8 rows over 50257 x 2048 took 41 to 44 us.  One row on fused multiply-adds would do, eight rows would not: 64 of
 // them, and 8 conversions, for every 16 bytes against the 23 bytes a clock that an SM streams.)
 #include "product_host.h"

@@ -228,9 +228,6 @@ bool make_map(CUtensorMap* map, const Matrix& a, int* mn_major, int box_rows) {
 }
 
 bool shape_of(const Config& cfg, const Matrix& a, const Matrix& b, Shape* s) {
-    s->m = static_cast<int>(a.rows);
-    s->n = static_cast<int>(b.rows);
-    s->k = static_cast<int>(a.cols);
     s->tiles_m = static_cast<int>(parts(a.rows, 128 * cfg.cg));
     s->tiles_n = static_cast<int>(parts(b.rows, cfg.bn));
     s->slices = static_cast<int>(parts(a.cols, kSlice));
