@@ -30,7 +30,10 @@ EncodeTiled encoder() {
 
 // Rows of `cols` adjacent values, off the 16-byte grid, to rows on it.  A thread puts eight values together from the two
 // 16-byte units that hold them (the second one comes from L1), all of a row shifted alike; units that reach beyond the row are
-// read value by value.  Bound by memory: 4 bytes a value (8192 x 8191: 150 us with 2-byte accesses).
+// read value by value.  Bound by memory: 4 bytes a value (8192 x 8191: 150 us with 2-byte accesses).  The grid's second axis has
+// 65535 blocks at most, so longer rows (a column-major operand of more than 67 million rows) take several turns.
+constexpr int kPackCols = 1024;
+
 __device__ __forceinline__ uint4 unit_of_row(const uint8_t* unit, const uint8_t* from, const uint8_t* to) {
     if (unit >= from && unit + 16 <= to) return __ldg(reinterpret_cast<const uint4*>(unit));
     uint32_t w[4] = {0, 0, 0, 0};
@@ -45,26 +48,26 @@ __device__ __forceinline__ uint4 unit_of_row(const uint8_t* unit, const uint8_t*
 __global__ void __launch_bounds__(256) pack_rows_kernel(const uint16_t* a, int64_t rs, int64_t rows, int64_t cols, uint16_t* out, int64_t ld) {
     tc::let_next_start();
     tc::wait_for_previous();
-    const int64_t col = (static_cast<int64_t>(blockIdx.y) * 128 + threadIdx.x % 128) * 8;
-    if (col >= cols) return;
+    for (int64_t col = static_cast<int64_t>(blockIdx.y) * kPackCols + threadIdx.x % 128 * 8; col < cols; col += static_cast<int64_t>(gridDim.y) * kPackCols) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const int64_t row = static_cast<int64_t>(blockIdx.x) * 8 + threadIdx.x / 128 + 2 * i;
-        if (row >= rows) break;
-        const uint8_t* from = reinterpret_cast<const uint8_t*>(a + row * rs);
-        const uint32_t off = static_cast<uint32_t>(reinterpret_cast<uintptr_t>(from) & 15u);
-        const uint8_t* unit = from - off + col * 2;
-        const uint4 x = unit_of_row(unit, from, from + cols * 2);
-        const uint4 y = off == 0 ? x : unit_of_row(unit + 16, from, from + cols * 2);
-        const uint32_t w[8] = {x.x, x.y, x.z, x.w, y.x, y.y, y.z, y.w};
-        uint32_t o[4];
+        for (int i = 0; i < 4; ++i) {
+            const int64_t row = static_cast<int64_t>(blockIdx.x) * 8 + threadIdx.x / 128 + 2 * i;
+            if (row >= rows) break;
+            const uint8_t* from = reinterpret_cast<const uint8_t*>(a + row * rs);
+            const uint32_t off = static_cast<uint32_t>(reinterpret_cast<uintptr_t>(from) & 15u);
+            const uint8_t* unit = from - off + col * 2;
+            const uint4 x = unit_of_row(unit, from, from + cols * 2);
+            const uint4 y = off == 0 ? x : unit_of_row(unit + 16, from, from + cols * 2);
+            const uint32_t w[8] = {x.x, x.y, x.z, x.w, y.x, y.y, y.z, y.w};
+            uint32_t o[4];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {          // the row's offset is the same for the whole warp
-            const uint32_t lo = off < 4 ? w[j] : off < 8 ? w[j + 1] : off < 12 ? w[j + 2] : w[j + 3];
-            const uint32_t hi = off < 4 ? w[j + 1] : off < 8 ? w[j + 2] : off < 12 ? w[j + 3] : w[j + 4];
-            o[j] = (off & 2u) ? __funnelshift_r(lo, hi, 16) : lo;
+            for (int j = 0; j < 4; ++j) {      // the row's offset is the same for the whole warp
+                const uint32_t lo = off < 4 ? w[j] : off < 8 ? w[j + 1] : off < 12 ? w[j + 2] : w[j + 3];
+                const uint32_t hi = off < 4 ? w[j + 1] : off < 8 ? w[j + 2] : off < 12 ? w[j + 3] : w[j + 4];
+                o[j] = (off & 2u) ? __funnelshift_r(lo, hi, 16) : lo;
+            }
+            *reinterpret_cast<uint4*>(out + row * ld + col) = make_uint4(o[0], o[1], o[2], o[3]);
         }
-        *reinterpret_cast<uint4*>(out + row * ld + col) = make_uint4(o[0], o[1], o[2], o[3]);
     }
 }
 
@@ -206,10 +209,10 @@ Matrix readable(Call& c, const Matrix& a) {
     r.p = out;
     if (!c.live()) return r;
     const auto* from = static_cast<const uint16_t*>(a.p);
-    if ((a.cs == 1 || a.rs == 1) && parts(cols, 1024) <= 65535) {
-        start(c, pack_rows_kernel, dim3(static_cast<unsigned>(parts(rows, 8)), static_cast<unsigned>(parts(cols, 1024))), dim3(256), 0, 1, from,
-              along_rows ? a.cs : a.rs, rows, cols, out, ld);
-    } else {
+    if (a.cs == 1 || a.rs == 1) {
+        const dim3 grid(static_cast<unsigned>(parts(rows, 8)), static_cast<unsigned>(std::min<int64_t>(parts(cols, kPackCols), 65535)));
+        start(c, pack_rows_kernel, grid, dim3(256), 0, 1, from, along_rows ? a.cs : a.rs, rows, cols, out, ld);
+    } else {                                   // neither adjacent: a.rows and a.cols as they are
         start(c, pack_kernel, dim3(static_cast<unsigned>(parts(rows, 32) * parts(cols, 32))), dim3(256), 0, 1, from, a.rs, a.cs, rows, cols, out, ld);
     }
     return r;

@@ -1,0 +1,34 @@
+"""The layer operators at the edges of what a call may hold: values at the ends of their types, operands and divisions that
+the ordinary sizes do not meet.  Tolerances as in test_layers_gpu, where they are derived."""
+import pytest
+import torch
+
+from tests.test_layers_gpu import F32, F64, close, normal, sum_error
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def L():
+    assert torch.cuda.is_available(), "this test needs a CUDA device"
+    from paper_2404_00438_b200 import build
+    build.build()
+    from paper_2404_00438_b200 import layers
+    yield layers
+    layers.check()
+
+
+def test_operand_of_more_adjacent_rows_than_one_turn_packs(L):
+    """Column-major and off the 16-byte grid, with more rows than the packing grid's 65535 x 1024."""
+    m = 65535 * 1024 + 3077
+    x = normal(1, 2, m + 1, std=1.0).t()[:m]
+    assert x.stride() == (1, m + 1) and m % 8 == 5
+    w = normal(2, 2, 8)
+    y = L.linear_forward(x, w)
+    for a in (0, 65535 * 1024 - 2000, m - 5000):
+        rows = slice(a, a + 5000)
+        want = x[rows].to(F64) @ w.to(F64)
+        close("y", y[rows], want, sum_error(2, x[rows].to(F64).abs() @ w.to(F64).abs()))
+    db = L.linear_backward(x, w.t(), None, need_dx=False, need_dw=False, grad_dtype=F32)[2]
+    want = x.to(F64).sum(0)
+    assert not ((db.to(F64) - want).abs() > (m / 8 + 600) * 2.0 ** -24 * x.to(F64).abs().sum(0)).any()
