@@ -35,12 +35,12 @@ EncodeTiled encoder() {
 constexpr int kPackCols = 1024;
 
 __device__ __forceinline__ uint4 unit_of_row(const uint8_t* unit, const uint8_t* from, const uint8_t* to) {
-    if (unit >= from && unit + 16 <= to) return __ldg(reinterpret_cast<const uint4*>(unit));
+    if (unit >= from && unit + 16 <= to) return *reinterpret_cast<const uint4*>(unit);
     uint32_t w[4] = {0, 0, 0, 0};
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
         const uint8_t* p = unit + 2 * i;
-        if (p >= from && p < to) w[i / 2] |= static_cast<uint32_t>(__ldg(reinterpret_cast<const unsigned short*>(p))) << (16 * (i % 2));
+        if (p >= from && p < to) w[i / 2] |= static_cast<uint32_t>(*reinterpret_cast<const unsigned short*>(p)) << (16 * (i % 2));
     }
     return make_uint4(w[0], w[1], w[2], w[3]);
 }

@@ -500,7 +500,7 @@ __device__ __forceinline__ void sum_columns(const Beside& s, int warp, int warps
             for (; r + 7 * rows_at_once < whole; r += 8 * rows_at_once, p += 8 * step) {
                 uint4 w[8];
 #pragma unroll
-                for (int i = 0; i < 8; ++i) w[i] = __ldg(p + i * step);
+                for (int i = 0; i < 8; ++i) w[i] = p[i * step];
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
                     float x[8];
@@ -511,7 +511,7 @@ __device__ __forceinline__ void sum_columns(const Beside& s, int warp, int warps
             }
             for (; r < whole; r += rows_at_once, p += step) {
                 float x[8];
-                widen(__ldg(p), x);
+                widen(*p, x);
 #pragma unroll
                 for (int j = 0; j < 8; ++j) v[j] += x[j];
             }

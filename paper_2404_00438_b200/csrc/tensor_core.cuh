@@ -55,7 +55,8 @@ __device__ __forceinline__ uint32_t map_to_rank(uint32_t local, uint32_t rank) {
 }
 
 // Programmatic launch: the next kernel of the stream may start its set-up now; everything this kernel's
-// predecessors wrote is there after the wait.  Every block of every kernel waits, so completion is transitive.
+// predecessors wrote is there after the wait.  Every block of every kernel waits, so completion is transitive.  What a
+// predecessor may have written is read by plain loads: the read-only path is for memory that nobody writes while a kernel lives.
 __device__ __forceinline__ void let_next_start() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 __device__ __forceinline__ void wait_for_previous() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 

@@ -1,5 +1,7 @@
 """Refusals of the layer operators, each by itself, in a process that sees no GPU."""
+import glob
 import os
+import re
 
 import pytest
 
@@ -46,3 +48,14 @@ def test_checkpoint_and_restore_refuse(lib, kw, status):
     a.update(kw)
     assert lib.dlion_checkpoint8(a["x"], a["x_ld"], a["m"], a["k"], a["q"], a["q_ld"], a["e"], a["e_ld"], None) == status
     assert lib.dlion_restore8(a["q"], a["q_ld"], a["e"], a["e_ld"], a["m"], a["k"], a["x"], a["x_ld"], None) == status
+
+
+def test_kernels_that_start_early_use_plain_loads():
+    """A kernel that starts beside its predecessor lives while that one writes, which the read-only path rules out."""
+    early = set()
+    for path in glob.glob(os.path.join(dl_build.CSRC, "*.cu*")):
+        source = open(path).read()
+        if "wait_for_previous()" in source:
+            early.add(os.path.basename(path))
+            assert not re.search(r"__ldg\b|\.nc\b|ld_nc|__restrict__", source), path
+    assert {"product.cu", "product.cuh", "few_rows.cu", "layers_linear.cu", "layers_loss.cu"} <= early
