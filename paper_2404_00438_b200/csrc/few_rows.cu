@@ -141,8 +141,12 @@ few_rows_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant
 #pragma unroll 1
     for (int i = 0; i < S::kAhead; ++i) fetch();
 
-    int stage = 0;
+    int stage = 0, left = mine * steps;
     uint32_t phase = 0;
+    // A wait that ran out ends the waiting and the copying; the sums that follow are of what is there.  The stages still under
+    // way are awaited at the end, so that no copy lands in memory that another block has by then.
+    int late = 0, late_stage = 0;
+    uint32_t late_phase = 0;
     bool fine = true;
     for (int u = first; u < units; u += apart) {
         float c[T][8][4] = {};                 // along k the first two of eight
@@ -160,7 +164,14 @@ few_rows_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant
         }
 #pragma unroll 1
         for (int i = 0; i < steps; ++i) {
-            fine = fine && tc::bar_wait(full + 8 * stage, phase);
+            if (fine && !tc::bar_wait(full + 8 * stage, phase)) {
+                fine = false;
+                late = left - ahead_left;
+                late_stage = stage;
+                late_phase = phase;
+                ahead_left = 0;
+            }
+            --left;
             const uint32_t w = ring + stage * S::kStage, x = w + S::kWeights;
             if constexpr (ALONG_K) {
 #pragma unroll
@@ -266,10 +277,14 @@ few_rows_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant
         }
         if (blocks > 1) tc::cluster_sync();    // the sums stay until they are read
     }
-    if (!fine) {                               // a wait ran out: copies may still be on their way
+    if (!fine) {
         *mark = 1;
-        const uint64_t t0 = tc::nanoseconds();
-        while (tc::nanoseconds() - t0 < 50000000ull) {
+        for (; late > 0; --late) {
+            tc::bar_wait(full + 8 * late_stage, late_phase);
+            if (++late_stage == S::kAhead) {
+                late_stage = 0;
+                late_phase ^= 1;
+            }
         }
     }
 }
