@@ -316,8 +316,9 @@ void loss(Call& c, const dlion_loss& p) {
     const Matrix w = readable(c, Matrix{p.w, p.v, p.h, p.w_rs, p.w_cs});
     const int64_t piece = std::min(p.m, p.piece == 0 ? kPiece : p.piece);
     const int64_t ld = round_up(p.v, 256);
-    // without gradients nothing is kept of a piece, and all rows are one
-    const int64_t step = grads ? piece : p.m;
+    // without gradients nothing is kept of a piece, and all rows are one; rows that are neighbours in memory begin a piece on
+    // the 16-byte grid
+    const int64_t step = !grads ? p.m : x.cs == 1 ? piece : std::min(p.m, round_up(piece, 8));
     const Config cfg = choose(c, step, p.v, p.h, false, true);
     const int width = cfg.bn / 2;
     const int64_t groups = parts(p.v, width);

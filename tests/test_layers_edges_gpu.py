@@ -3,7 +3,7 @@ the ordinary sizes do not meet.  Tolerances as in test_layers_gpu, where they ar
 import pytest
 import torch
 
-from tests.test_layers_gpu import F32, F64, close, normal, sum_error
+from tests.test_layers_gpu import DEV, F32, F64, check_loss, close, normal, sum_error
 
 pytestmark = pytest.mark.gpu
 
@@ -32,3 +32,19 @@ def test_operand_of_more_adjacent_rows_than_one_turn_packs(L):
     db = L.linear_backward(x, w.t(), None, need_dx=False, need_dw=False, grad_dtype=F32)[2]
     want = x.to(F64).sum(0)
     assert not ((db.to(F64) - want).abs() > (m / 8 + 600) * 2.0 ** -24 * x.to(F64).abs().sum(0)).any()
+
+
+@pytest.mark.parametrize("m,piece", [(100, 30), (100, 1), (101, 7), (101, 50), (104, 12), (96, 96)])
+@pytest.mark.parametrize("f32", [False, True])
+def test_loss_pieces_of_adjacent_rows(L, m, piece, f32):
+    """Rows of x next to each other (column-major, on and off the 16-byte grid), pieces of any size: no piece may begin where a
+    copy cannot."""
+    x, w = normal(1, 64, m).t()[:, :50], normal(2, 130, 50)
+    assert x.stride(0) == 1
+    check_loss(L, x, w, torch.arange(m, device=DEV), f32=f32, piece=piece)
+
+
+def test_loss_pieces_of_one_column(L):
+    x, w = normal(1, 100, 1), normal(2, 130, 1)
+    for piece in (1, 30, 99):
+        check_loss(L, x, w, torch.arange(100, device=DEV), piece=piece)
