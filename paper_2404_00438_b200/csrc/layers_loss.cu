@@ -201,7 +201,8 @@ __global__ void __launch_bounds__(kRowThreads) rows_kernel(const float2* stats, 
 #pragma unroll
         for (int j = 0; j < kEvery; ++j) {
             const float2 s = part[j][r];
-            if (s.x != -INFINITY) sum += s.y * exp2_fast((s.x - top) * kLog2e);     // a thread without a group has none
+            // a thread without a group has (-infinity, 0), one whose groups all are NaN has (-infinity, NaN)
+            if (s.x != -INFINITY || s.y != 0.0f) sum += s.y * exp2_fast((s.x - top) * kLog2e);
         }
         const float log_sum = logf(sum);
         const int64_t t = targets[row];

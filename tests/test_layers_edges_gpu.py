@@ -1,5 +1,7 @@
 """The layer operators at the edges of what a call may hold: values at the ends of their types, operands and divisions that
 the ordinary sizes do not meet.  Tolerances as in test_layers_gpu, where they are derived."""
+import math
+
 import pytest
 import torch
 
@@ -48,3 +50,16 @@ def test_loss_pieces_of_one_column(L):
     x, w = normal(1, 100, 1), normal(2, 130, 1)
     for piece in (1, 30, 99):
         check_loss(L, x, w, torch.arange(100, device=DEV), piece=piece)
+
+
+@pytest.mark.parametrize("v", [90, 700, 5003])
+def test_loss_of_a_row_with_one_infinite_logit(L, v):
+    """An infinity in one group of words is not dropped when the groups are joined."""
+    x, w = normal(1, 40, 64), normal(2, v, 64, std=0.2)
+    t = torch.arange(40, device=DEV) * 2
+    x[:, 0], w[:, 0] = 0, 2.0 ** -100
+    w[33, 0], x[3, 0] = 2.0 ** 100, 2.0 ** 100                     # 2^200 for one word alone
+    r = L.lm_loss(x, w, t)
+    ok = [i for i in range(40) if i != 3]
+    assert bool(r.rows[3].isnan()) and bool(r.dx[3].isnan().all()) and math.isnan(float(r.loss))
+    assert bool(r.rows[ok].isfinite().all()) and bool(r.dx[ok].isfinite().all())
