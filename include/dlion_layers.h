@@ -17,7 +17,9 @@
  *   - act(u) is rounded to bf16 as an operand of dW (the forward product read the same values), and
  *     so is softmax_tv - [v = y_t] as an operand of dx and dW (g multiplies their sums);
  *   - gelu is the tanh form z/2 (1 + tanh(sqrt(2/pi) (z + 0.044715 z^3))); silu is z/(1 + exp(-z));
- *   - NaN and infinities go through as the formulas say; relu(NaN) = NaN.
+ *   - NaN and infinities go through as the formulas say; relu(NaN) = NaN.  In the loss, words may be masked by -infinity or by
+ *     any finite value; a row with a logit that is NaN or +infinity, or with none above -infinity, has a loss and gradients
+ *     of NaN.
  *
  * Every buffer is DEVICE memory owned by the caller.  A matrix is a pointer and two strides in
  * ELEMENTS; strides are non-negative, rows and columns at most 2^30 (2^24 - 256 columns of u and of the

@@ -93,9 +93,10 @@ struct LossTile {
             }
             if (!live) break;
         }
-        // A group that is masked whole (-infinity, or the type's lowest value) sums to 0, and so that it does, the
-        // difference must be finite; logits above 2e38 make the row NaN.
-        top = top > 2e38f ? NAN : fmaxf(top, -2e38f);
+        // The differences need a finite reference: a group masked whole by -infinity has none of its own, and sums to 0 against
+        // any.  One masked by a finite value, the type's lowest even, keeps it, and vanishes when the groups are joined, unless
+        // all of the row's words have it.  An infinity above makes the row NaN.
+        const float zero = top == -INFINITY ? 0.0f : top;
         float sum = 0.0f;
 #pragma unroll 1
         for (int c = 0; c < valid; c += 32) {
@@ -103,11 +104,11 @@ struct LossTile {
             uint32_t w[16];
             tc::tmem_load32(acc + c, v);
             if (c + 32 > valid) {
-                sum += exponentials<true, true>(v, valid - c, top, w);
+                sum += exponentials<true, true>(v, valid - c, zero, w);
             } else if (codes) {
-                sum += exponentials<false, true>(v, 32, top, w);
+                sum += exponentials<false, true>(v, 32, zero, w);
             } else {
-                sum += exponentials<false, false>(v, 32, top, w);
+                sum += exponentials<false, false>(v, 32, zero, w);
             }
             if (codes) Piece{stage, lane, row0, col0 + c, rows, 32}.put16(w, p.codes, p.ld, true);      // ld covers the last tile
             if (!live) break;
@@ -184,10 +185,11 @@ __global__ void __launch_bounds__(kRowThreads) rows_kernel(const float2* stats, 
             float t = top;
 #pragma unroll
             for (int j = 0; j < kBatch; ++j) t = fmaxf(t, s[j].x);
-            sum *= exp2_fast((top - t) * kLog2e);
+            if (top != -INFINITY) sum *= exp2_fast((top - t) * kLog2e);
 #pragma unroll
             for (int j = 0; j < kBatch; ++j) {
-                if (s[j].x != -INFINITY) sum += s[j].y * exp2_fast((s[j].x - t) * kLog2e);
+                // (-infinity, 0): masked, or no group; (-infinity, NaN): a NaN among what is masked
+                if (s[j].x != -INFINITY || s[j].y != 0.0f) sum += s[j].y * exp2_fast((s[j].x - t) * kLog2e);
             }
             top = t;
         }
@@ -201,7 +203,6 @@ __global__ void __launch_bounds__(kRowThreads) rows_kernel(const float2* stats, 
 #pragma unroll
         for (int j = 0; j < kEvery; ++j) {
             const float2 s = part[j][r];
-            // a thread without a group has (-infinity, 0), one whose groups all are NaN has (-infinity, NaN)
             if (s.x != -INFINITY || s.y != 0.0f) sum += s.y * exp2_fast((s.x - top) * kLog2e);
         }
         const float log_sum = logf(sum);

@@ -5,7 +5,7 @@ import math
 import pytest
 import torch
 
-from tests.test_layers_gpu import DEV, F32, F64, check_loss, close, normal, sum_error
+from tests.test_layers_gpu import BF, DEV, F32, F64, check_loss, close, loss_reference, normal, sum_error
 
 pytestmark = pytest.mark.gpu
 
@@ -63,3 +63,58 @@ def test_loss_of_a_row_with_one_infinite_logit(L, v):
     ok = [i for i in range(40) if i != 3]
     assert bool(r.rows[3].isnan()) and bool(r.dx[3].isnan().all()) and math.isnan(float(r.loss))
     assert bool(r.rows[ok].isfinite().all()) and bool(r.dx[ok].isfinite().all())
+
+
+def masked_row(x, w, row, value):
+    """Makes every logit of `row` equal to `value`, and leaves the other rows' as they are."""
+    x[:, 0], w[:, 0] = 0, 1
+    x[row] = 0
+    x[row, 0] = value
+
+
+@pytest.mark.parametrize("v", [90, 700, 5003])
+def test_loss_of_a_row_at_the_lowest_value(L, v):
+    """All words of one row at the type's lowest value: equal logits, so its loss is log v and its softmax 1 / v.  The
+    exponentials' and the logarithm's errors are 2^-20, those of d 2^-8 (bf16) + 2^-11 (codes)."""
+    x, w = normal(1, 40, 64), normal(2, v, 64, std=0.2)
+    t = torch.arange(40, device=DEV) * 2
+    low = torch.finfo(BF).min
+    masked_row(x, w, 3, low)
+    r = L.lm_loss(x, w, t, grad_dtype=F32, reduction="sum")
+    assert abs(float(r.rows[3]) - math.log(v)) <= 2.0 ** -18 * (1 + math.log(v))
+    assert bool(r.rows.isfinite().all()) and math.isfinite(float(r.loss))
+    others = [i for i in range(40) if i != 3]
+    loss, rows, dx, dw, d, lse, logits = loss_reference(x[others], w, t[others], -100, False)
+    assert abs(float(r.loss) - float(loss) - math.log(v)) <= 1e-3 * float(loss)
+    # dx of the row, column 0 excepted: there w is 1 and the sum of d cancels
+    d3 = torch.full((v,), 1.0 / v, dtype=F64, device=DEV)
+    d3[int(t[3])] -= 1
+    W = w.to(F64)
+    e = d3.abs() * (2.0 ** -8 + 2.0 ** -11)
+    off = e @ W.abs() + sum_error(v, d3.abs() @ W.abs()) + 2.0 ** -8 * (d3 @ W).abs()
+    assert not ((r.dx[3].to(F64) - d3 @ W).abs() > off)[1:].any()
+    # column 0 of dw has the row's d times the lowest value, which nothing else comes near
+    got = r.dw[:, 0].to(F64) / low
+    assert not ((got - d3).abs() > e + 2.0 ** -20).any()
+
+
+def test_loss_of_rows_beyond_the_codes(L):
+    """Logits near both ends of binary32 keep their formulas; infinite ones make their row, and only it, NaN."""
+    for v in (90, 700, 5003):
+        t = torch.arange(40, device=DEV) * 2
+        x, w = normal(1, 40, 64), normal(2, v, 64, std=0.2)
+        x[:, 0], w[:, 0] = 0, 0
+        w[17, 0], x[4, 0], x[9, 0] = 1.0, 3e38, 3e38
+        t[9] = 17
+        r = L.lm_loss(x, w, t, grad_dtype=F32, reduction="sum")
+        big = float(torch.tensor(3e38).to(BF))
+        assert abs(float(r.rows[4]) - big) <= 2.0 ** -20 * big and abs(float(r.rows[9])) <= 1e-6
+        assert not ((r.dx[4].float() - (w[17].float() - w[8].float())).abs() > 2.0 ** -7 * (w[17].float().abs() + w[8].float().abs())).any()
+        assert not r.dx[9].any()
+        for value in (float("inf"), -float("inf"), float("nan")):
+            x, w = normal(1, 40, 64), normal(2, v, 64, std=0.2)
+            masked_row(x, w, 3, value)
+            r = L.lm_loss(x, w, t)
+            ok = [i for i in range(40) if i != 3]
+            assert bool(r.rows[3].isnan()) and bool(r.rows[ok].isfinite().all()) and math.isnan(float(r.loss))
+            assert bool(r.dx[3].isnan().all()) and bool(r.dx[ok].isfinite().all())
