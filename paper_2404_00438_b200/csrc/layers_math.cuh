@@ -62,7 +62,8 @@ __device__ __forceinline__ float act_slope(float z) {
     if (ACT == DLION_ACT_GELU) {
         const float c = held(z, 64.0f), c2 = c * c;
         const float p = logistic2(c * __fmaf_rn(kGeluB, c2, kGeluA));
-        return __fmaf_rn(z * __fmaf_rn(0.134145f * kGelu2c, c2, kGelu2c), __fmaf_rn(-p, p, p), p);
+        // the factor z last: p (1 - p) is 0 where z times the polynomial would overflow
+        return __fmaf_rn(z, __fmaf_rn(0.134145f * kGelu2c, c2, kGelu2c) * __fmaf_rn(-p, p, p), p);
     }
     return 1.0f;
 }

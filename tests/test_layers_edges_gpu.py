@@ -118,3 +118,16 @@ def test_loss_of_rows_beyond_the_codes(L):
             ok = [i for i in range(40) if i != 3]
             assert bool(r.rows[3].isnan()) and bool(r.rows[ok].isfinite().all()) and math.isnan(float(r.loss))
             assert bool(r.dx[3].isnan().all()) and bool(r.dx[ok].isfinite().all())
+
+
+@pytest.mark.parametrize("m", [2, 40])
+@pytest.mark.parametrize("kind", ["relu", "gelu", "silu"])
+def test_slopes_at_the_ends_of_the_type(L, m, kind):
+    """Far out an activation's slope is 0 or 1, up to the type's largest value, so du is 0 or the product itself."""
+    ends = torch.tensor([-3.3895313892515355e38, -1e36, -1e30, -1000.0, 1000.0, 1e30, 1e36, 3.3895313892515355e38], device=DEV)
+    u = ends.to(BF).repeat(m, 4).contiguous()
+    dy, w = normal(1, m, 48), normal(2, 32, 48)
+    plain = L.linear_backward(dy, w, u, need_dw=False, need_db=False)[0]
+    got = L.linear_backward(dy, w, u, act=kind, need_dw=False, need_db=False)[0]
+    want = torch.where(u > 0, plain, torch.zeros_like(plain))
+    assert torch.equal(got, want)
