@@ -50,8 +50,10 @@ typedef enum { DLION_KEEP_NONE = 0, DLION_KEEP_BF16 = 1, DLION_KEEP_8BIT = 2 } d
 
 /* A matrix in the 8-bit form: q[row * q_ld + col] is an int8, e[(col / 32) * e_ld + row] a byte, and
  * the value is q * 2^(e - 127), exact in bf16.  2^(e-127) is the smallest power of two, 2^-126 at
- * least, with max|v| <= 127 * 2^(e-127) over the block; q is v / 2^(e-127) to the nearest integer,
- * ties to even.  e = 255 marks a block that held a NaN or an infinity: its values are NaN. */
+ * least and 2^121 at most, with max|v| <= 127 * 2^(e-127) over the block; q is v / 2^(e-127) to the
+ * nearest integer, ties to even, and 127 or -127 for what lies beyond (above 127 * 2^121, where a larger
+ * power would restore the type's largest value as infinity).  e = 255 marks a block that held a NaN or an
+ * infinity: its values are NaN. */
 
 typedef struct {
     int64_t m, k, n;                       /* rows (tokens), inputs, outputs; k, n >= 1 */

@@ -43,7 +43,7 @@ __device__ __forceinline__ void finish_row(const Finish& f, int row, int64_t col
         const uint32_t top = __reduce_max_sync(0xffffffffu, in ? __float_as_uint(v) & 0x7fffffffu : 0u);
         const uint32_t e = block_exponent(top);
         if (threadIdx.x % 32 == 0 && in) f.kept_e[(col / 32) * f.kept_e_ld + row] = static_cast<uint8_t>(e);
-        if (in) static_cast<int8_t*>(f.kept)[row * f.kept_ld + col] = static_cast<int8_t>(quantise8(v, block_inverse(e)));
+        if (in) static_cast<int8_t*>(f.kept)[row * f.kept_ld + col] = static_cast<int8_t>(quantise8(e == kTop8 ? within8(v) : v, block_inverse(e)));
     } else if (f.keep == DLION_KEEP_BF16 && in) {
         static_cast<__nv_bfloat16*>(f.kept)[row * f.kept_ld + col] = __float2bfloat16_rn(v);
     }

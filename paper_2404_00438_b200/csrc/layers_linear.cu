@@ -203,6 +203,10 @@ __global__ void __launch_bounds__(256) checkpoint8_kernel(const __nv_bfloat16* x
         if (lane % 4 == 0) ex[lane / 4][r] = static_cast<uint8_t>(scale);
         float v[8];
         widen(w[i], v);
+        if (scale == kTop8) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[j] = within8(v[j]);
+        }
         const uint32_t o[2] = {bytes4(quantise8(v[0], inv), quantise8(v[1], inv), quantise8(v[2], inv), quantise8(v[3], inv)),
                                bytes4(quantise8(v[4], inv), quantise8(v[5], inv), quantise8(v[6], inv), quantise8(v[7], inv))};
         if (row0 + r >= m || valid == 0) continue;

@@ -83,17 +83,24 @@ __device__ __forceinline__ void with_act(int act, F f) {
 }
 
 // ---- the 8-bit form: 32 values share 2^(e-127)
+// The exponent stops at 248: a step more and what lies above 63.5 steps, bf16's largest value too, would be restored as
+// infinity.  There, and only there, a value can lie above 127 steps; it is held as 127 (within8).
+constexpr uint32_t kTop8 = 248;
+constexpr float kMost8 = 127.0f * 0x1p121f;
+
 // amax_bits: largest |v| of the block as its bit pattern (so that NaN and infinity order last).
 __device__ __forceinline__ uint32_t block_exponent(uint32_t amax_bits) {
     if (amax_bits >= 0x7f800000u) return 255u;
     // 127 = 1.984375 * 2^6: the power of two is 2^(E-6), or 2^(E-5) when the fraction is above that
     const int e = static_cast<int>(amax_bits >> 23) - 6 + ((amax_bits & 0x7fffffu) > 0x7e0000u ? 1 : 0);
-    return static_cast<uint32_t>(e < 1 ? 1 : e);
+    return e < 1 ? 1u : min(static_cast<uint32_t>(e), kTop8);
 }
+
+__device__ __forceinline__ float within8(float v) { return fminf(fmaxf(v, -kMost8), kMost8); }
 
 __device__ __forceinline__ float block_scale(uint32_t e) { return __uint_as_float(e == 255u ? 0x7fc00000u : e << 23); }
 
-// 1 / 2^(e-127), exact (e is in [1, 249] or marks a non-finite block, whose q is 0)
+// 1 / 2^(e-127), exact (e is in [1, 248] or marks a non-finite block, whose q says nothing)
 __device__ __forceinline__ float block_inverse(uint32_t e) { return e == 255u ? 0.0f : __uint_as_float((254u - e) << 23); }
 
 // Conversions between integers and floats run at an eighth of the rate of additions, so the integer is read off, or put

@@ -255,9 +255,17 @@ __device__ __forceinline__ void keep8(const Finish& f, const Piece& pc, const fl
     if (pc.lane >= pc.rows) return;
     f.kept_e[static_cast<int64_t>(pc.col0 / 32) * f.kept_e_ld + row] = static_cast<uint8_t>(e);
     uint32_t w[8];
+    auto quantise = [&](auto limited) {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-        w[j] = bytes4(quantise8(v[4 * j], inv), quantise8(v[4 * j + 1], inv), quantise8(v[4 * j + 2], inv), quantise8(v[4 * j + 3], inv));
+        for (int j = 0; j < 8; ++j) {
+            w[j] = bytes4(quantise8(limited(v[4 * j]), inv), quantise8(limited(v[4 * j + 1]), inv), quantise8(limited(v[4 * j + 2]), inv),
+                          quantise8(limited(v[4 * j + 3]), inv));
+        }
+    };
+    if (__builtin_expect(e == kTop8, 0)) {
+        quantise([](float x) { return within8(x); });
+    } else {
+        quantise([](float x) { return x; });
     }
     int8_t* q = static_cast<int8_t*>(f.kept) + static_cast<int64_t>(row) * f.kept_ld + pc.col0;
     if (pc.cols == 32 && on_grid(f.kept, f.kept_ld, 1)) {

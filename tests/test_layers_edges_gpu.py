@@ -131,3 +131,31 @@ def test_slopes_at_the_ends_of_the_type(L, m, kind):
     got = L.linear_backward(dy, w, u, act=kind, need_dw=False, need_db=False)[0]
     want = torch.where(u > 0, plain, torch.zeros_like(plain))
     assert torch.equal(got, want)
+
+
+def test_eight_bits_at_the_ends_of_the_type(L):
+    """The largest value lies half a step above 127 steps of 2^121: it is held as those, not as infinity."""
+    top, held = torch.finfo(BF).max, 127 * 2.0 ** 121
+    x = torch.zeros(6, 70, dtype=BF, device=DEV)
+    x[0, 3], x[1, 40], x[2, 69], x[3, 0], x[3, 1], x[4, :] = top, -top, top, -top, held, 2.0 ** 125
+    x[5, 5], x[5, 6] = top, 2.0 ** 121
+    c = L.checkpoint8(x)
+    assert bool(L.restore8(c).isfinite().all())
+    want = x.to(F64).clamp(-held, held)
+    assert torch.equal(L.restore8(c).to(F64), want)
+    assert int(c.q[0, 3]) == 127 and int(c.q[1, 40]) == -127
+
+
+@pytest.mark.parametrize("m", [2, 40])
+@pytest.mark.parametrize("v", [3.3895313892515355e38, 3.4028e38])
+def test_eight_bits_of_sums_at_the_end_of_binary32(L, m, v):
+    """z as a binary32 sum beyond the largest bf16 (its bias, 1.3e36, takes it there) in either kernel."""
+    x, w = torch.zeros(m, 8, dtype=BF, device=DEV), torch.zeros(8, 64, dtype=BF, device=DEV)
+    x[:, 0], w[0, 5], w[0, 40] = 1, torch.finfo(BF).max, -torch.finfo(BF).max
+    bias = torch.zeros(64, device=DEV)
+    bias[5], bias[40] = v - torch.finfo(BF).max, torch.finfo(BF).max - v
+    y, kept = L.linear_forward(x, w, bias, keep="8bit", out_dtype=F32)
+    z = L.restore8(kept).to(F64)
+    want = torch.zeros(m, 64, dtype=F64, device=DEV)
+    want[:, 5], want[:, 40] = 127 * 2.0 ** 121, -127 * 2.0 ** 121
+    assert torch.equal(z, want) and bool(y.isfinite().all())
