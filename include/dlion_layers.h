@@ -78,7 +78,9 @@ typedef struct {
     const uint8_t* u_e; int64_t u_e_ld;    /* 8 bits only: [ceil(k/32)][m] */
     const void* residual; int64_t r_ld;    /* nullable, bf16 [m][k]: added to dx */
     void* dx; int64_t dx_ld;               /* nullable, bf16 [m][k] */
-    void* dw; int64_t dw_rs, dw_cs;        /* nullable [k][n], one stride 1; dlion_gdtype grad_type */
+    void* dw; int64_t dw_rs, dw_cs;        /* nullable [k][n], one stride 1; dlion_gdtype grad_type.  dx and dw have the
+                                              same bits alone as together if grad_type and these strides are the same;
+                                              db may be added in another order */
     void* db;                              /* nullable [n]; grad_type */
     int32_t grad_type;                     /* dlion_gdtype, that of the optimizer's gradient arena */
 } dlion_linear_bwd;

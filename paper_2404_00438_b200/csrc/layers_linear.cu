@@ -356,6 +356,9 @@ void forward(Call& c, const dlion_linear_fwd& p) {
     product(c, x, transposed(w), f);
 }
 
+bool rows_of_dw(const dlion_linear_bwd& p) { return p.dw_cs == 1 && (p.k == 1 || p.dw_rs >= p.n); }
+bool cols_of_dw(const dlion_linear_bwd& p) { return p.dw_rs == 1 && (p.n == 1 || p.dw_cs >= p.k); }
+
 dlion_status check_backward(const dlion_linear_bwd* p) {
     if (p == nullptr || !size_ok(p->m, 0) || !size_ok(p->k, 1) || !size_ok(p->n, 1)) return DLION_EINVAL;
     if (p->act < DLION_ACT_NONE || p->act > DLION_ACT_SILU) return DLION_EINVAL;
@@ -371,8 +374,7 @@ dlion_status check_backward(const dlion_linear_bwd* p) {
     }
     if (p->dw != nullptr) {
         if (!stride_ok(p->dw_rs) || !stride_ok(p->dw_cs)) return DLION_EINVAL;
-        const bool rows = p->dw_cs == 1 && (p->k == 1 || p->dw_rs >= p->n), cols = p->dw_rs == 1 && (p->n == 1 || p->dw_cs >= p->k);
-        if (!rows && !cols) return DLION_EINVAL;
+        if (!rows_of_dw(*p) && !cols_of_dw(*p)) return DLION_EINVAL;
         if (!aligned(p->dw, type_bytes(p->grad_type))) return DLION_EALIGN;
     }
     if (p->db != nullptr && !aligned(p->db, type_bytes(p->grad_type))) return DLION_EALIGN;
@@ -392,7 +394,7 @@ void backward(Call& c, const dlion_linear_bwd& p) {
         if (!c.live()) return;
         const size_t el = type_bytes(p.grad_type);
         if (p.dw != nullptr) {
-            const bool rows = p.dw_cs == 1 && (p.k == 1 || p.dw_rs >= p.n);
+            const bool rows = rows_of_dw(p);
             c.check(cudaMemset2DAsync(p.dw, std::max<int64_t>(1, rows ? std::max(p.dw_rs, p.n) : std::max(p.dw_cs, p.k)) * el, 0,
                                       (rows ? p.n : p.k) * el, rows ? p.k : p.n, c.stream));
         }
@@ -415,8 +417,9 @@ void backward(Call& c, const dlion_linear_bwd& p) {
         fx.out = p.dx;
         fx.out_ld = p.dx_ld;
     }
-    // where no dw is wanted, the order of its arena's rows does not matter
-    const bool rows = p.dw == nullptr || (p.dw_cs == 1 && (p.k == 1 || p.dw_rs >= p.n));
+    // dw's type and order say how the two products are divided, of which dx alone has the same share
+    const bool rows = rows_of_dw(p) || (p.dw == nullptr && !cols_of_dw(p));
+    fw.out_f32 = p.grad_type == DLION_GRAD_F32;
     if (p.dw != nullptr) {
         if (p.saved == DLION_KEEP_BF16 && p.act == DLION_ACT_NONE) {
             a = readable(c, Matrix{p.u, p.m, p.k, p.u_ld, 1});
@@ -427,7 +430,6 @@ void backward(Call& c, const dlion_linear_bwd& p) {
             a = Matrix{out, p.m, p.k, ld, 1};
         }
         fw.out = p.dw;
-        fw.out_f32 = p.grad_type == DLION_GRAD_F32;
         fw.out_ld = rows ? p.dw_rs : p.dw_cs;
     }
     Beside beside{static_cast<const __nv_bfloat16*>(dy.p), dy.rs, static_cast<int>(p.m), static_cast<int>(p.n), p.db, p.grad_type == DLION_GRAD_F32, 0};

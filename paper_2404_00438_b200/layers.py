@@ -245,7 +245,8 @@ def linear_backward(dy: torch.Tensor, w: torch.Tensor, saved: Union[torch.Tensor
     if residual is not None:
         _matrix(residual, "residual", device, _ONLY_BF16, (m, k), True)
     g = _grad_type(grad_dtype)
-    ys, ws, gs = dy.stride(), w.stride(), (0, 0)
+    ys, ws = dy.stride(), w.stride()
+    gs = (n, 1) if ws[0] >= ws[1] else (1, k)       # of a dw that is not given (or not wanted: dx's bits are the same then)
     if not need_dx:
         dx = None
     elif dx is None:
@@ -255,10 +256,7 @@ def linear_backward(dy: torch.Tensor, w: torch.Tensor, saved: Union[torch.Tensor
     if not need_dw:
         dw = None
     elif dw is None:
-        if ws[0] >= ws[1]:
-            dw, gs = dy.new_empty((k, n), dtype=grad_dtype), (n, 1)
-        else:
-            dw, gs = dy.new_empty((n, k), dtype=grad_dtype).t(), (1, k)
+        dw = dy.new_empty((k, n), dtype=grad_dtype) if ws[0] >= ws[1] else dy.new_empty((n, k), dtype=grad_dtype).t()
     else:
         _matrix(dw, "dw", device, (grad_dtype,), (k, n))
         gs = dw.stride()

@@ -159,3 +159,16 @@ def test_eight_bits_of_sums_at_the_end_of_binary32(L, m, v):
     want = torch.zeros(m, 64, dtype=F64, device=DEV)
     want[:, 5], want[:, 40] = 127 * 2.0 ** 121, -127 * 2.0 ** 121
     assert torch.equal(z, want) and bool(y.isfinite().all())
+
+
+@pytest.mark.parametrize("m,k,n", [(9, 40, 48), (197, 768, 768), (2100, 700, 900), (2100, 2050, 2050), (520, 2050, 520), (3000, 100, 4000)])
+@pytest.mark.parametrize("transposed", [False, True])
+@pytest.mark.parametrize("dtype", [BF, F32])
+def test_gradients_have_the_same_bits_alone(L, m, k, n, transposed, dtype):
+    """dx and dw are divided as beside each other when only one of them is asked for, in either type and order of dw."""
+    u, dy = normal(1, m, k), normal(2, m, n)
+    w = normal(3, n, k, std=n ** -0.5).t() if transposed else normal(3, k, n, std=n ** -0.5)
+    args = dict(act="gelu", residual=u, grad_dtype=dtype)
+    dx, dw, _ = L.linear_backward(dy, w, u, **args)
+    assert torch.equal(L.linear_backward(dy, w, u, need_dw=False, need_db=False, **args)[0], dx)
+    assert torch.equal(L.linear_backward(dy, w, u, need_dx=False, need_db=False, **args)[1], dw)
