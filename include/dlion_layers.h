@@ -14,6 +14,9 @@
  *   - operands of a product are bf16; products are summed in binary32 on the tensor cores; what
  *     follows a sum (bias, activation, residual, softmax statistics) is binary32, and an output
  *     is rounded once, when it is stored (bf16: nearest, ties to even);
+ *   - the tensor cores drop what their accumulator does not hold: a binary32 result is off by about 1e-6 of the
+ *     products' sizes; one rounded to bf16, and the loss's dw, may come out low by up to 2^-28 of itself a product
+ *     (k products of one sign, k up to 131072; from there on as a binary32 result);
  *   - act(u) is rounded to bf16 as an operand of dW (the forward product read the same values), and
  *     so is softmax_tv - [v = y_t] as an operand of dx and dW (g multiplies their sums);
  *   - gelu is the tanh form z/2 (1 + tanh(sqrt(2/pi) (z + 0.044715 z^3))); silu is z/(1 + exp(-z));

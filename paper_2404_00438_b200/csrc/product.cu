@@ -270,7 +270,12 @@ static void launch_as(Call& c, const Config& cfg, Work<Finish>& w) {
     }
 }
 
-static bool long_sums(const Finish& f) { return f.out_f32 != 0 && f.rough == 0; }
+// Whether a sum of k products is taken in segments where it is longer than one.  Always for a binary32 result; for one rounded to
+// bf16, or whose operands are (rough), not before the tensor core's accumulator may have shifted it by a quarter of that rounding:
+// 2^-28 a product where all have one sign.  The segments' tiles take longer (131072 x 2048 x 2048, dx and dW: 1.42 ms without, 1.65 with).
+constexpr int64_t kRoughMost = 131072;
+
+static bool long_sums(const Finish& f, int64_t k) { return (f.out_f32 != 0 && f.rough == 0) || k > kRoughMost; }
 
 // Whether `blocks` blocks that are there for `clocks` have the time to sum the columns, and how: a warp has eight loads under way,
 // some 1500 clocks, and reads whole sectors where there are columns enough.
@@ -287,7 +292,7 @@ static bool fits_beside(Beside& s, int64_t blocks, double clocks) {
 static bool product_beside(Call& c, const Matrix& a, const Matrix& b, Finish f, Beside beside) {
     complete(f, a, b);
     if (few_rows(c, a, b, f)) return false;
-    const Config cfg = choose(c, a.rows, b.rows, a.cols, long_sums(f), false);
+    const Config cfg = choose(c, a.rows, b.rows, a.cols, long_sums(f, a.cols), false);
     Work<Finish> w{};
     if (!shape_of(cfg, a, b, &w.s[0])) {
         c.status = DLION_EINVAL;
@@ -324,10 +329,10 @@ bool products(Call& c, const Part& first, const Part& second, Beside beside) {
     if (second.a.cols > first.a.cols) std::swap(parts_of[0], parts_of[1]);
     const Part &p0 = *parts_of[0], &p1 = *parts_of[1];
     const bool few = p0.a.rows <= kFewRows || p1.a.rows <= kFewRows;
-    const Config best0 = choose(c, p0.a.rows, p0.b.rows, p0.a.cols, long_sums(p0.f), false);
-    const Config best1 = choose(c, p1.a.rows, p1.b.rows, p1.a.cols, long_sums(p1.f), false);
+    const Config best0 = choose(c, p0.a.rows, p0.b.rows, p0.a.cols, long_sums(p0.f, p0.a.cols), false);
+    const Config best1 = choose(c, p1.a.rows, p1.b.rows, p1.a.cols, long_sums(p1.f, p1.a.cols), false);
     const int64_t slices0 = parts(p0.a.cols, kSlice), slices1 = parts(p1.a.cols, kSlice);
-    const bool sums = (long_sums(p0.f) && slices0 > kSegment) || (long_sums(p1.f) && slices1 > kSegment);
+    const bool sums = (long_sums(p0.f, p0.a.cols) && slices0 > kSegment) || (long_sums(p1.f, p1.a.cols) && slices1 > kSegment);
     double clocks = best0.clocks + best1.clocks + kLaunch;
     Config cfg{};
     int64_t extra = 0;

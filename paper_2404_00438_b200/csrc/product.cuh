@@ -7,9 +7,10 @@
 // columns; so while the first slices are on their way the epilogue warps run it once on nothing (`live` false: no rows).
 // Three forms of the same kernel: kWhole (above); kJoined, where the blocks of a cluster each take a share of k of
 // one 128 x 64 tile and send each other their sums, every block adding a share of the tile, for products with fewer tiles than SMs;
-// kLong, for binary32 results of long sums: the tensor core's accumulator drops what does not fit, which after K
-// products shifts a sum by about K 2^-30 of itself, so it only adds kSegment of them and the epilogue
-// adds the segments in registers, rounding to nearest (192 columns, so that they fit: 96 a thread).
+// kLong, for long sums: the tensor core's accumulator drops what does not fit, which shifts a sum of K products of one sign by
+// K 2^-30 (K = 1024) to K 2^-28 (65536) of itself, so it only adds kSegment slices of them (8e-7, however long the sum) and
+// the epilogue adds the segments in registers, rounding to nearest (192 columns, so that they fit: 96 a thread).  A sum of K random
+// products is off by 1e-6 of its deviation in segments.
 // A pair computes 256 x BN with each block holding half of A and half of B.  An SM takes in 57 bytes a clock (measured:
 // 12 slices of a lone block's 128 x 128 tile, 393 KB, in 6850 clocks), so what a tile reads for its products decides: a pair's 256 x 256
 // needs 32 KB a block for 512 clocks of products, its 256 x 128 and a lone block's 128 x 64 24 KB for 256 and 128.  Large shapes
@@ -88,7 +89,7 @@ struct Finish {
     void* out;
     int64_t out_ld;
     int out_f32;
-    int rough;                             // a binary32 result that needs no segments: its operands are rounded already
+    int rough;                             // a binary32 result whose operands are rounded already: segments only where the sum is very long
     float4* parts;                         // sums of split tiles: [tile][block][epilogue warp][split][32 rows x half the columns]
     unsigned int* tickets;                 // [tile][block][epilogue warp][4 pieces], 0 before the call
 };

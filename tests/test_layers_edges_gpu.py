@@ -172,3 +172,17 @@ def test_gradients_have_the_same_bits_alone(L, m, k, n, transposed, dtype):
     dx, dw, _ = L.linear_backward(dy, w, u, **args)
     assert torch.equal(L.linear_backward(dy, w, u, need_dw=False, need_db=False, **args)[0], dx)
     assert torch.equal(L.linear_backward(dy, w, u, need_dx=False, need_db=False, **args)[1], dw)
+
+
+def test_long_sums_are_not_shifted(L):
+    """2^18 positive products a sum, in a form whose tiles are whole: the tensor core drops what its accumulator does not
+    hold, which unsegmented shifts every sum by 2^-10 of itself.  In segments of 1024 it is 2^-20, which turns the rounding of some
+    2^-20 2^8 of the results by 2^-8: on average over 4096 of them 2^-20, with a deviation of 2^-20.  2^-18 is allowed."""
+    m, k, n = 256, 1 << 18, 256 * 74
+    x, w = torch.empty(m, k, dtype=BF, device=DEV), torch.empty(k, n, dtype=BF, device=DEV)
+    g = torch.Generator(device=DEV).manual_seed(1)
+    x.uniform_(0.5, 1.5, generator=g)
+    w.uniform_(0.5, 1.5, generator=g)
+    y = L.linear_forward(x, w)[:64, :64].to(F64)
+    want = x[:64].to(F64) @ w[:, :64].to(F64)
+    assert abs(float(((y - want.to(BF).to(F64)) / want).mean())) <= 2.0 ** -18
