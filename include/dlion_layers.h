@@ -103,7 +103,8 @@ typedef struct {
     void* dw; int64_t dw_ld;               /* [v][h]; grad_type */
     int32_t grad_type;                     /* dlion_gdtype */
     int64_t piece;                         /* rows whose logits are held at a time, as 16-bit codes; 0: 4096;
-                                              rounded up to a multiple of 8 where x_cs is not 1 */
+                                              rounded up to a multiple of 8 where x_cs is not 1.  Without
+                                              gradients no logits are held, and 32768 rows at least are one */
 } dlion_loss;
 
 /* Bytes of workspace that the call needs (0 also for arguments that the call refuses). */

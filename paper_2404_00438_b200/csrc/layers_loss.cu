@@ -19,6 +19,9 @@ using namespace dlion::prod;
 
 constexpr float kStep = 1024.0f;            // codes per octave
 constexpr int64_t kPiece = 4096;
+// Without gradients nothing is kept of a piece but its groups' maxima and sums, 8 bytes a row and group (0.1 GB at 50257 words): the
+// largest batches alone are divided, whose products fill the GPU by far.
+constexpr int64_t kEvalPiece = 32768;
 constexpr int64_t kMost = int64_t{1} << 30;
 
 struct LossTile {
@@ -316,11 +319,10 @@ void loss(Call& c, const dlion_loss& p) {
     }
     const Matrix x = readable(c, Matrix{p.x, p.m, p.h, p.x_rs, p.x_cs});
     const Matrix w = readable(c, Matrix{p.w, p.v, p.h, p.w_rs, p.w_cs});
-    const int64_t piece = std::min(p.m, p.piece == 0 ? kPiece : p.piece);
+    const int64_t piece = std::min(p.m, !grads ? std::max(p.piece, kEvalPiece) : p.piece == 0 ? kPiece : p.piece);
     const int64_t ld = round_up(p.v, 256);
-    // without gradients nothing is kept of a piece, and all rows are one; rows that are neighbours in memory begin a piece on
-    // the 16-byte grid
-    const int64_t step = !grads ? p.m : x.cs == 1 ? piece : std::min(p.m, round_up(piece, 8));
+    // rows that are neighbours in memory begin a piece on the 16-byte grid
+    const int64_t step = x.cs == 1 ? piece : std::min(p.m, round_up(piece, 8));
     const Config cfg = choose(c, step, p.v, p.h, false, true);
     const int width = cfg.bn / 2;
     const int64_t groups = parts(p.v, width);

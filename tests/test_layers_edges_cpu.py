@@ -1,4 +1,5 @@
 """Refusals of the layer operators, each by itself, in a process that sees no GPU."""
+import ctypes
 import glob
 import os
 import re
@@ -59,3 +60,11 @@ def test_kernels_that_start_early_use_plain_loads():
             early.add(os.path.basename(path))
             assert not re.search(r"__ldg\b|\.nc\b|ld_nc|__restrict__", source), path
     assert {"product.cu", "product.cuh", "few_rows.cu", "layers_linear.cu", "layers_loss.cu"} <= early
+
+
+def test_evaluation_workspace_is_bounded(lib):
+    """The loss without gradients holds 8 bytes a row and group of 32768 rows at most, at 50257 words not a GB."""
+    from paper_2404_00438_b200 import layers
+    a = dict(h=768, v=50257, x=P, x_rs=768, x_cs=1, w=P, w_rs=768, w_cs=1, targets=P, ignore_index=-100, mean=1, scale=1.0, loss=P, rows=P)
+    sizes = [lib.dlion_lm_loss_workspace(ctypes.byref(layers._Loss(m=m, **a))) for m in (1 << 10, 1 << 15, 1 << 20, 1 << 30)]
+    assert sizes[0] < sizes[1] == sizes[2] == sizes[3] < 1 << 29

@@ -186,3 +186,19 @@ def test_long_sums_are_not_shifted(L):
     y = L.linear_forward(x, w)[:64, :64].to(F64)
     want = x[:64].to(F64) @ w[:, :64].to(F64)
     assert abs(float(((y - want.to(BF).to(F64)) / want).mean())) <= 2.0 ** -18
+
+
+def test_evaluation_in_several_pieces(L):
+    """More rows than the loss without gradients takes at once: the same rows' losses, and one loss of them all."""
+    m, h, v = 2 * 32768 + 1001, 40, 130
+    for x in (normal(1, m, h), normal(1, h, m).t()):
+        w, t = normal(2, v, h), torch.arange(m, device=DEV) % v
+        t[::11] = -100
+        for mean in (True, False):
+            r = L.lm_loss(x, w, t, grads=False, reduction="mean" if mean else "sum")
+            loss, rows = loss_reference(x, w, t, -100, mean)[:2]
+            X, W = x.to(F64).abs(), w.to(F64).abs()
+            off = 2 * sum_error(h, (X @ W.t()).amax(1)) + 2.0 ** -16 * (2 + rows.abs())
+            assert not ((r.rows.to(F64) - rows).abs() > off).any()
+            n = int((t != -100).sum()) if mean else 1
+            assert abs(float(r.loss) - float(loss)) <= float(off.sum()) / n + 2.0 ** -18 * abs(float(loss))
