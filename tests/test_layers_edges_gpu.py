@@ -202,3 +202,43 @@ def test_evaluation_in_several_pieces(L):
             assert not ((r.rows.to(F64) - rows).abs() > off).any()
             n = int((t != -100).sum()) if mean else 1
             assert abs(float(r.loss) - float(loss)) <= float(off.sum()) / n + 2.0 ** -18 * abs(float(loss))
+
+
+@pytest.mark.parametrize("piece", [1, 50, 64, 149])
+@pytest.mark.parametrize("dtype", [BF, F32])
+def test_loss_divided_and_whole(L, piece, dtype):
+    """However the rows are divided: each row's loss and dx from the same terms in another division of the same sums, twice the
+    bound of one against the formula; likewise the loss and dw."""
+    x, w = normal(1, 150, 72), normal(2, 333, 72)
+    t = torch.arange(150, device=DEV) * 2
+    whole = L.lm_loss(x, w, t, grad_dtype=dtype)
+    parts = L.lm_loss(x, w, t, grad_dtype=dtype, piece=piece)
+    loss, rows, dx, dw, d, lse, logits = loss_reference(x, w, t, -100, True)
+    X, W = x.to(F64).abs(), w.to(F64).abs()
+    off = 2 * sum_error(72, (X @ W.t()).amax(1)) + 2.0 ** -16 * (1 + lse.abs() + logits.abs().amax(1) * 2.0 ** -4)
+    assert not ((whole.rows.to(F64) - parts.rows.to(F64)).abs() > 2 * off).any()
+    assert abs(float(whole.loss) - float(parts.loss)) <= 2 * (float(off.sum()) / 150 + 2.0 ** -18 * float(loss))
+    e = d.abs() * (2.0 ** -8 + 2.0 ** -11) + (off * 1.1)[:, None] * (d.abs() + (1 / 150) * 2.0 ** -8 * (d != 0)) + 1e-19
+    dx_off = 2 * (e @ W + sum_error(333, d.abs() @ W) + 2.0 ** -8 * dx.abs())
+    assert not ((whole.dx.to(F64) - parts.dx.to(F64)).abs() > dx_off).any()
+    dw_off = 2 * (e.t() @ X + sum_error(150, d.abs().t() @ X) + 2.0 ** (-8 if dtype is BF else -22) * dw.abs())
+    assert not ((whole.dw.to(F64) - parts.dw.to(F64)).abs() > dw_off).any()
+
+
+@pytest.mark.parametrize("m,h,v", [(1, 64, 7), (40, 200, 50257), (130, 200, 5003), (300, 100, 1), (257, 65, 2051)])
+@pytest.mark.parametrize("mean", [True, False])
+def test_loss_without_gradients(L, m, h, v, mean):
+    """The evaluation's scalar against 64 bits, and its rows with the bits that the call with gradients has."""
+    x, w = normal(1, m, h), normal(2, v, h, std=2 * h ** -0.5)
+    t = (torch.arange(m, device=DEV) * 13) % v
+    if m > 2:
+        t[::7] = -100
+    args = dict(reduction="mean" if mean else "sum")
+    r = L.lm_loss(x, w, t, grads=False, **args)
+    loss, rows, _, _, _, lse, logits = loss_reference(x, w, t, -100, mean)
+    X, W = x.to(F64).abs(), w.to(F64).abs()
+    off = 2 * sum_error(h, (X @ W.t()).amax(1)) + 2.0 ** -16 * (1 + lse.abs() + logits.abs().amax(1) * 2.0 ** -4)
+    n = max(1, int((t != -100).sum())) if mean else 1
+    assert abs(float(r.loss) - float(loss)) <= float(off.sum()) / n + 2.0 ** -18 * abs(float(loss))
+    with_gradients = L.lm_loss(x, w, t, **args)
+    assert torch.equal(r.rows, with_gradients.rows) and torch.equal(r.loss, with_gradients.loss)
