@@ -97,6 +97,7 @@ def train(steps: int = 60, workers: int = 4, rows: int = 512, words: int = 1000,
         opt.worker_step(-1, grads, m, packed)
         opt.aggregate_apply(packed, x)
         losses.append(float(total) / workers)
+        layers.check()                                  # a kernel whose wait ran out leaves its outputs undefined
         if step % 10 == 0 or step == steps - 1:
             report(f"step {step}: loss {losses[-1]:.3f}")
     opt.destroy()

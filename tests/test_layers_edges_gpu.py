@@ -242,3 +242,14 @@ def test_loss_without_gradients(L, m, h, v, mean):
     assert abs(float(r.loss) - float(loss)) <= float(off.sum()) / n + 2.0 ** -18 * abs(float(loss))
     with_gradients = L.lm_loss(x, w, t, **args)
     assert torch.equal(r.rows, with_gradients.rows) and torch.equal(r.loss, with_gradients.loss)
+
+
+def test_the_example_checks_its_kernels(L, monkeypatch):
+    """A kernel that gave up a wait ends the training with an error instead of passing unnoticed."""
+    from paper_2404_00438_b200 import dlion, example
+
+    def gave_up():
+        raise dlion.DlionError(5, "dlion_layers_check")
+    monkeypatch.setattr(example.layers, "check", gave_up)
+    with pytest.raises(dlion.DlionError):
+        example.train(steps=1, workers=1, rows=32, words=50, width=32, hidden=32, blocks=1, report=lambda s: None)
