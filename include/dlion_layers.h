@@ -18,7 +18,10 @@
  *     products' sizes; one rounded to bf16, and the loss's dw, may come out low by up to 2^-28 of itself a product
  *     (k products of one sign, k up to 131072; from there on as a binary32 result);
  *   - act(u) is rounded to bf16 as an operand of dW (the forward product read the same values), and
- *     so is softmax_tv - [v = y_t] as an operand of dx and dW (g multiplies their sums);
+ *     so is softmax_tv - [v = y_t] as an operand of dx and dW (g multiplies their sums); between the two the
+ *     logits are held as 16-bit distances below a group's largest, 3.4e-4 relative in exp at most, exact where
+ *     the distance is 0, and softmax below 5e-20 of its group's largest counts as 0.  The losses do not
+ *     go through the codes.  dx is bf16;
  *   - gelu is the tanh form z/2 (1 + tanh(sqrt(2/pi) (z + 0.044715 z^3))); silu is z/(1 + exp(-z));
  *   - NaN and infinities go through as the formulas say; relu(NaN) = NaN.  In the loss, words may be masked by -infinity or by
  *     any finite value; a row with a logit that is NaN or +infinity, or with none above -infinity, has a loss and gradients
@@ -94,7 +97,8 @@ typedef struct {
     const void* w; int64_t w_rs, w_cs;     /* bf16 [v][h] */
     const int64_t* targets;                /* [m]; a target outside [0, v) that is not ignore_index makes
                                               its row's loss, and so the loss, and its gradients NaN */
-    int64_t ignore_index;
+    int64_t ignore_index;                  /* such a row has loss and gradients 0 (its x is multiplied by 0 for dw,
+                                              not left out: NaN there stays NaN) */
     int32_t mean;                          /* 1: g = scale / (rows with a target); 0: g = scale */
     float scale;                           /* factor of the gradients only (loss scaling) */
     float* loss;                           /* [1]: sum or mean of the rows' losses; 0 when no row has a target */

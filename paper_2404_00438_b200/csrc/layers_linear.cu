@@ -121,7 +121,9 @@ __device__ __forceinline__ void give8(int8_t* at, const uint2& v, uint32_t valid
 }
 
 // act(u) as a bf16 operand.  Bound by memory, 2 (or 33/32) + 2 bytes a value; issue slots are 70 % busy.  8192 x 8192 from 8
-// bits: 35 us plain (203 MB, 5.7 TB/s), 40 us with gelu, whose two special functions a value the loads do not cover.
+// bits: 35 us plain, launched again and again (203 MB, 5.7 TB/s); with gelu, whose two special functions a value the loads do not
+// cover, 40 us more for a call than without the operand, 47 us alone from cold caches.  Rows off the 16-byte grid take
+// accesses of 2 and 4 bytes: 8192 x 2047 19.5 us, 8192 x 2048 7.8 us (from L2).
 template <bool EIGHT, int ACT>
 __global__ void __launch_bounds__(256) operand_kernel(const void* u, int64_t u_ld, const uint8_t* e, int64_t e_ld, int64_t m, int64_t k,
                                                       __nv_bfloat16* out, int64_t out_ld, int wide, int wide_out) {
@@ -173,7 +175,7 @@ __global__ void __launch_bounds__(256) operand_kernel(const void* u, int64_t u_l
 }
 
 // Rows of x into the 8-bit form: a block of 32 values is four neighbouring threads.  Bound by memory, 2 + 33/32 bytes a value:
-// 8192 x 8192 34 us (203 MB, 5.9 TB/s).
+// 8192 x 8192 35 us (203 MB, 5.8 TB/s); off the 16-byte grid 8192 x 2047 14.4 us, 8192 x 2048 9.5 us (to L2).
 __global__ void __launch_bounds__(256) checkpoint8_kernel(const __nv_bfloat16* x, int64_t x_ld, int64_t m, int64_t k, int8_t* q,
                                                           int64_t q_ld, uint8_t* e, int64_t e_ld, int wide, int wide_out) {
     __shared__ uint8_t ex[8][kTileRows];

@@ -14,9 +14,9 @@
 // A pair computes 256 x BN with each block holding half of A and half of B.  An SM takes in 57 bytes a clock (measured:
 // 12 slices of a lone block's 128 x 128 tile, 393 KB, in 6850 clocks), so what a tile reads for its products decides: a pair's 256 x 256
 // needs 32 KB a block for 512 clocks of products, its 256 x 128 and a lone block's 128 x 64 24 KB for 256 and 128.  Large shapes
-// use the first, middling ones the second, those with few tiles the third.  8192 x 2048 x 8192 takes 177 us (1550 TFLOP/s, tensor pipe 91 %
-// of the active clocks), 4096 x 768 x 2304 13.5 us (1070), 197 x 768 x 768 5.7 us, which is latency.  Rows between: 160 x 4096 x
-// 4096 takes 18.3 us, bound by what the SMs take in, 34 MB of weights notwithstanding.
+// use the first, middling ones the second, those with few tiles the third.  8192 x 2048 x 8192 takes 177 to 187 us with the power cap (1550 to
+// 1470 TFLOP/s, tensor pipe 91 % of the active clocks), 4096 x 768 x 2304 13.5 to 14.2 us (1070 to 1020), 197 x 768 x 768 5.7 us, which is
+// latency.  Rows between: 160 x 4096 x 4096 takes 17.6 us, bound by what the SMs take in, 34 MB of weights notwithstanding.
 #pragma once
 
 #include "layers_math.cuh"
@@ -484,7 +484,8 @@ __device__ __forceinline__ void tile_of(const Shape& s, int t, int& tm, int& tn)
 
 // Sums over the rows of a matrix on the 16-byte grid (a bias' gradient), taken along by the two warps of a block that have nothing
 // to do: strips of 8 * lanes columns, a warp each, the rows 32 / lanes at a time.  They read what the products read
-// anyway; a kernel of its own takes 25 us for 8192 x 8192 and took 6 us for 4096 x 2304.
+// anyway; a kernel of its own takes 25 us for 8192 x 8192 and took 6 us for 4096 x 2304.  A lane adds rows * lanes / 32 values
+// one after another in binary32, each addition to 2^-24; the kernel of its own adds rows / 256 so.
 struct Beside {
     const __nv_bfloat16* a;
     int64_t rs;

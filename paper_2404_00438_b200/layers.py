@@ -9,7 +9,9 @@ declared in ``include/dlion_layers.h``.
 Argument marshalling only, as in ``dlion``: every tensor is checked, becomes a device address, and the
 current torch stream becomes the ``cudaStream_t``.  Outputs may be given (``out=``, ``dw=``, ...): a view
 into the optimizer's gradient arena is a valid ``dw`` or ``db``.  The workspace comes from torch's
-allocator on the current stream unless one is given.  There is no CPU path.
+allocator on the current stream unless one is given.  There is no CPU path, and no autograd: tensors that require
+gradients are read like any others and results have no graph; the gradients are what ``linear_backward``
+and ``lm_loss`` return.
 """
 from __future__ import annotations
 
