@@ -9,6 +9,8 @@
  *   8 bits    blocks of 32 values of a row share a power of two dlion_checkpoint8, dlion_restore8
  *   loss      L_t = log sum_v exp(x_t . w_v) - x_t . w_{y_t}    dlion_lm_loss
  *             d_tv = g (softmax_tv - [v = y_t]) ;  dx = d W ;  dW = d^T x
+ *   norm      y = (x - mean) rstd w + b                         dlion_norm_forward, dlion_norm_backward
+ *   attention out_i = sum_j softmax_j(scale q_i . k_j) v_j      dlion_attention_forward, dlion_attention_backward
  *
  * Conventions:
  *   - operands of a product are bf16; products are summed in binary32 on the tensor cores; what
@@ -128,6 +130,94 @@ dlion_status dlion_checkpoint8(const void* x, int64_t x_ld, int64_t m, int64_t k
                                uint8_t* e, int64_t e_ld, void* cuda_stream);
 dlion_status dlion_restore8(const int8_t* q, int64_t q_ld, const uint8_t* e, int64_t e_ld, int64_t m, int64_t k,
                             void* x, int64_t x_ld, void* cuda_stream);
+
+/* ---- layer norm of rows of n values, in binary32:
+ *   mean, rstd = 1 / sqrt(var + eps) of each row, var the mean of (x - mean)^2 ;  h = (x - mean) rstd
+ *   y = h w + b
+ *   with u = w dy:  dx = rstd (u - mean(u) - h mean(u h)) + r ;  dw = sum over rows of dy h ;  db = sum over rows of dy
+ * Values of the residual stream (x, r, dx) have one type, y and dy their own. */
+typedef struct {
+    int64_t m, n;                          /* rows, columns (n >= 1) */
+    const void* x; int64_t x_ld; int32_t x_type; /* [m][n]; dlion_gdtype */
+    const void* w; int32_t w_type;         /* nullable (all 1) [n]; dlion_gdtype */
+    const void* b; int32_t b_type;         /* nullable (all 0) [n] */
+    float eps;                             /* finite, 0 or more */
+    void* y; int64_t y_ld; int32_t y_type; /* [m][n]; may be x where the types are the same */
+    float* stats;                          /* [2][m]: the rows' means, then their rstd */
+} dlion_norm_fwd;
+
+typedef struct {
+    int64_t m, n;
+    const void* dy; int64_t dy_ld; int32_t dy_type;
+    const void* x; int64_t x_ld; int32_t x_type;
+    const void* w; int32_t w_type;         /* nullable */
+    const float* stats;                    /* as dlion_norm_forward left them */
+    const void* residual; int64_t r_ld;    /* nullable, of x_type: added to dx */
+    void* dx; int64_t dx_ld;               /* nullable, of x_type; may be dy (same type) or residual */
+    void* dw; void* db;                    /* nullable [n]; grad_type */
+    int32_t grad_type;                     /* dlion_gdtype */
+} dlion_norm_bwd;
+
+uint64_t dlion_norm_backward_workspace(const dlion_norm_bwd* p);
+dlion_status dlion_norm_forward(const dlion_norm_fwd* p, void* cuda_stream);
+dlion_status dlion_norm_backward(const dlion_norm_bwd* p, void* workspace, uint64_t workspace_bytes, void* cuda_stream);
+
+/* ---- attention of sequences that lie one behind the other in the rows:
+ *   s_ij = scale q_i . k_j  for the rows j of i's sequence, with `causal` only j <= i
+ *   lse_i = log sum_j exp s_ij ;  out_i = sum_j exp(s_ij - lse_i) v_j
+ *   p_ij = exp(s_ij - lse_i) ;  ds_ij = p_ij (dout_i . v_j - dout_i . out_i)
+ *   dq_i = scale sum_j ds_ij k_j ;  dk_j = scale sum_i ds_ij q_i ;  dv_j = sum_i p_ij dout_i
+ * for every head; heads / kv_heads query heads in a row share a head of keys and values, and dk, dv are their sums.
+ * Operands are bf16; p and ds are rounded to bf16 as operands of the second products, out is the rounded output; scores, softmax
+ * statistics and sums are binary32.  Rows of another sequence or of none do not take part whatever they hold, NaN too; a NaN
+ * or an infinity in a row of a sequence may reach every row of that sequence, a causal mask notwithstanding.
+ *
+ * The sequences: `offsets` (device memory, int32 or int64, sequences + 1 ascending values in [0, rows]; sequence i has the rows
+ * offsets[i] .. offsets[i + 1] - 1, which may be none), or, where that is null, rows / length sequences of `length` rows, or one
+ * of all rows (length 0).  Offsets outside [0, rows] are held to it; where they do not ascend the results are undefined, but
+ * nothing outside the tensors is touched.  Rows in no sequence (before the first, behind the last) are left as they were in
+ * every result, or cleared where zero_rest is set.
+ *
+ * All matrices are bf16 [rows][heads][dim], a pointer and the strides of rows and heads in elements; the dim columns of a head are
+ * adjacent, dim is a multiple of 8, at most 128; strides are multiples of 8 and at least dim, pointers 16-byte aligned. */
+typedef struct {
+    int64_t rows, heads, kv_heads, dim;    /* heads: a multiple of kv_heads, at most 65535 */
+    const void* q; int64_t q_rs, q_hs;
+    const void* k; int64_t k_rs, k_hs;     /* kv_heads */
+    const void* v; int64_t v_rs, v_hs;     /* kv_heads */
+    const void* offsets; int32_t offsets_64; /* nullable; 1: int64, 0: int32 */
+    int64_t sequences;                     /* with offsets; 0 otherwise */
+    int64_t length;                        /* without offsets; 0 otherwise */
+    int32_t causal;
+    float scale;                           /* positive, finite */
+    void* out; int64_t out_rs, out_hs;
+    float* lse; int64_t lse_ld;            /* [heads][rows], rows adjacent */
+    int32_t zero_rest;
+} dlion_attention_fwd;
+
+typedef struct {
+    int64_t rows, heads, kv_heads, dim;
+    const void* q; int64_t q_rs, q_hs;
+    const void* k; int64_t k_rs, k_hs;
+    const void* v; int64_t v_rs, v_hs;
+    const void* out; int64_t out_rs, out_hs; /* out, lse: of the forward call with the same arguments */
+    const void* dout; int64_t dout_rs, dout_hs;
+    const float* lse; int64_t lse_ld;
+    const void* offsets; int32_t offsets_64;
+    int64_t sequences;
+    int64_t length;
+    int32_t causal;
+    float scale;
+    void* dq; int64_t dq_rs, dq_hs;
+    void* dk; int64_t dk_rs, dk_hs;
+    void* dv; int64_t dv_rs, dv_hs;
+    int32_t zero_rest;
+} dlion_attention_bwd;
+
+uint64_t dlion_attention_forward_workspace(const dlion_attention_fwd* p);
+uint64_t dlion_attention_backward_workspace(const dlion_attention_bwd* p);
+dlion_status dlion_attention_forward(const dlion_attention_fwd* p, void* workspace, uint64_t workspace_bytes, void* cuda_stream);
+dlion_status dlion_attention_backward(const dlion_attention_bwd* p, void* workspace, uint64_t workspace_bytes, void* cuda_stream);
 
 /* Every wait inside the kernels ends after a time limit; a kernel whose wait ran out ends, its outputs
  * undefined, and leaves a mark on the device.  Synchronises the stream and returns DLION_OK, DLION_ESTATE

@@ -1,0 +1,242 @@
+// What the attention kernels share: the sequences' tiles, copies of rows of one head, products with an
+// operand in tensor memory, and the arithmetic on pairs of binary32 values.
+#pragma once
+
+#include <climits>
+
+#include "layers_math.cuh"
+#include "product_host.h"
+#include "tensor_core.cuh"
+
+namespace dlion {
+namespace att {
+
+constexpr int kTile = 128;                 // rows of queries or keys in a tile: the lanes of tensor memory
+
+// Which sequence and which of its tiles a piece of work is.  Sequences of one length are numbered by arithmetic; others by a
+// table in the workspace (plan_kernel), whose entries end with sequences of length -1.  The longest pieces come first, because
+// a block's work grows with the tile's place under a causal mask, and the last blocks should be short.
+struct Plan {
+    const int4* table;                     // {first row, length, tile, 0}
+    int length, sequences, tiles;          // without a table
+    int descending;
+};
+
+struct Piece {
+    int start, length, tile;
+};
+
+__device__ __forceinline__ Piece piece_of(const Plan& p, int i) {
+    if (p.table != nullptr) {
+        const int4 e = p.table[i];
+        return Piece{e.x, e.y, e.z};
+    }
+    const int rank = i / p.sequences;
+    return Piece{(i - rank * p.sequences) * p.length, p.length, p.descending ? p.tiles - 1 - rank : rank};
+}
+
+// bf16 [rows][heads][dim], strides in elements
+struct Rows {
+    __nv_bfloat16* p;
+    int64_t rs, hs;
+};
+
+// ---------------------------------------------------------------- copies
+// 64 columns of kTile rows of one head, 128-byte swizzled; x is 0 or 64.
+__device__ __forceinline__ void load_rows(uint32_t dst, const CUtensorMap* map, int x, int head, int row, uint32_t bar) {
+    asm volatile(
+        "cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(dst),
+        "l"(reinterpret_cast<uint64_t>(map)), "r"(x), "r"(head), "r"(row), "r"(bar)
+        : "memory");
+}
+
+constexpr uint32_t kChunk = kTile * 128;   // bytes of 64 columns
+
+template <int D>
+__device__ __forceinline__ void load_head(uint32_t dst, const CUtensorMap* map, int head, int row, uint32_t bar) {
+#pragma unroll
+    for (int c = 0; c < D / 64; ++c) load_rows(dst + c * kChunk, map, 64 * c, head, row, bar);
+}
+
+// Rows from `first` on of a tile become zero (by `threads` threads): they are other sequences' rows, or no one's, and what they
+// hold, NaN too, must not meet the zeros of a masked product.  The caller announces it to the matrix instructions by a barrier.
+template <int D>
+__device__ __forceinline__ void clear_rows(uint8_t* tile, int first, int thread, int threads) {
+    for (int i = first * 8 + thread; i < kTile * 8; i += threads) {
+#pragma unroll
+        for (int c = 0; c < D / 64; ++c) *reinterpret_cast<uint4*>(tile + c * kChunk + i * 16) = make_uint4(0, 0, 0, 0);
+    }
+    tc::fence_for_copies();
+}
+
+// ---------------------------------------------------------------- products
+// Operand whose k runs along a row of the tile (a head's columns): chunks of 64 columns, 32 bytes for 16 of k.
+__device__ __forceinline__ uint64_t along_row(uint32_t tile) { return tc::operand_base(0) | ((tile >> 4) & 0x3fff); }
+__device__ __forceinline__ uint32_t row_step(int k16) { return ((k16 >> 2) * kChunk + (k16 & 3) * 32) >> 4; }
+
+// Operand whose k is the tile's rows, its other axis the head's columns: 64 of them to a chunk, 2048 bytes for 16 of k.
+__device__ __forceinline__ uint64_t along_column(uint32_t tile) {
+    return (static_cast<uint64_t>(kChunk >> 4) << 16) | (static_cast<uint64_t>(1024 >> 4) << 32) | (1ull << 46) | (2ull << 61) |
+           ((tile >> 4) & 0x3fff);
+}
+__device__ __forceinline__ uint32_t column_step(int k16) { return (k16 * 2048) >> 4; }
+
+// The first operand out of tensor memory: 16 of k are 8 columns of bf16 pairs.
+__device__ __forceinline__ void mma_tmem(uint32_t d, uint32_t a, uint64_t b, uint32_t inst, uint32_t add) {
+    asm volatile(
+        "{\n.reg .pred p;\nsetp.ne.u32 p, %4, 0;\n"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}" ::"r"(d), "r"(a), "l"(b), "r"(inst), "r"(add)
+        : "memory");
+}
+
+// ---------------------------------------------------------------- tensor memory
+// 64 consecutive columns of this warp's 32 lanes, a row a thread.
+__device__ __forceinline__ void tmem_load64(uint32_t addr, float (&v)[64]) {
+    uint32_t* r = reinterpret_cast<uint32_t*>(v);
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x64.b32 {"
+        "%0, %1, %2, %3, %4, %5, %6, %7, "
+        "%8, %9, %10, %11, %12, %13, %14, %15, "
+        "%16, %17, %18, %19, %20, %21, %22, %23, "
+        "%24, %25, %26, %27, %28, %29, %30, %31, "
+        "%32, %33, %34, %35, %36, %37, %38, %39, "
+        "%40, %41, %42, %43, %44, %45, %46, %47, "
+        "%48, %49, %50, %51, %52, %53, %54, %55, "
+        "%56, %57, %58, %59, %60, %61, %62, %63"
+        "}, [%64];\n"
+        "tcgen05.wait::ld.sync.aligned;"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
+          "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]),
+          "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]),
+          "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31]),
+          "=r"(r[32]), "=r"(r[33]), "=r"(r[34]), "=r"(r[35]), "=r"(r[36]), "=r"(r[37]), "=r"(r[38]), "=r"(r[39]),
+          "=r"(r[40]), "=r"(r[41]), "=r"(r[42]), "=r"(r[43]), "=r"(r[44]), "=r"(r[45]), "=r"(r[46]), "=r"(r[47]),
+          "=r"(r[48]), "=r"(r[49]), "=r"(r[50]), "=r"(r[51]), "=r"(r[52]), "=r"(r[53]), "=r"(r[54]), "=r"(r[55]),
+          "=r"(r[56]), "=r"(r[57]), "=r"(r[58]), "=r"(r[59]), "=r"(r[60]), "=r"(r[61]), "=r"(r[62]), "=r"(r[63])
+        : "r"(addr)
+        : "memory");
+}
+
+// 32 columns of this warp's 32 lanes; there after tmem_stored().
+__device__ __forceinline__ void tmem_store32(uint32_t addr, const uint32_t (&r)[32]) {
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x32.b32 [%32], {"
+        "%0, %1, %2, %3, %4, %5, %6, %7, "
+        "%8, %9, %10, %11, %12, %13, %14, %15, "
+        "%16, %17, %18, %19, %20, %21, %22, %23, "
+        "%24, %25, %26, %27, %28, %29, %30, %31"
+        "};" ::"r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]),
+          "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]),
+          "r"(r[16]), "r"(r[17]), "r"(r[18]), "r"(r[19]), "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]),
+          "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31]),
+          "r"(addr)
+        : "memory");
+}
+
+__device__ __forceinline__ void tmem_stored() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+
+__device__ __forceinline__ void tmem_store_f32(uint32_t addr, const float (&v)[32]) {
+    tmem_store32(addr, reinterpret_cast<const uint32_t(&)[32]>(v));
+}
+
+// ---------------------------------------------------------------- pairs of binary32 values
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+    float2 r;
+    asm("{\n.reg .b64 a, b, c, d;\nmov.b64 a, {%2, %3};\nmov.b64 b, {%4, %5};\nmov.b64 c, {%6, %7};\n"
+        "fma.rn.f32x2 d, a, b, c;\nmov.b64 {%0, %1}, d;\n}"
+        : "=f"(r.x), "=f"(r.y)
+        : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
+    return r;
+}
+
+__device__ __forceinline__ float2 add2(float2 a, float2 b) {
+    float2 r;
+    asm("{\n.reg .b64 a, b, d;\nmov.b64 a, {%2, %3};\nmov.b64 b, {%4, %5};\nadd.rn.f32x2 d, a, b;\nmov.b64 {%0, %1}, d;\n}"
+        : "=f"(r.x), "=f"(r.y)
+        : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+    return r;
+}
+
+__device__ __forceinline__ float2 mul2(float2 a, float2 b) {
+    float2 r;
+    asm("{\n.reg .b64 a, b, d;\nmov.b64 a, {%2, %3};\nmov.b64 b, {%4, %5};\nmul.rn.f32x2 d, a, b;\nmov.b64 {%0, %1}, d;\n}"
+        : "=f"(r.x), "=f"(r.y)
+        : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+    return r;
+}
+
+__device__ __forceinline__ float max3(float a, float b, float c) {
+    float r;
+    asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+    return r;
+}
+
+// ---------------------------------------------------------------- results
+// COLS columns of a row a thread (binary32, in tensor memory at `addr`), times `factor`, as bf16 rows of a head: through
+// shared memory (`stage`, 32 x 2 COLS bytes, this warp's own), so that whole rows leave together.  row0: the warp's first row,
+// of which `rows` are there (may be negative); col0: the first column, of `dim`.
+template <int COLS>
+__device__ __forceinline__ void give_rows(uint32_t addr, float factor, uint8_t* stage, const Rows& to, int64_t row0, int rows, int head, int col0,
+                                          int dim, int lane) {
+    constexpr int kUnits = COLS / 8, kMix = kUnits < 8 ? kUnits - 1 : 7;
+#pragma unroll
+    for (int c = 0; c < COLS; c += 32) {
+        float v[32];
+        tc::tmem_load32(addr + c, v);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const uint4 w = make_uint4(pack_bf16(v[8 * i] * factor, v[8 * i + 1] * factor), pack_bf16(v[8 * i + 2] * factor, v[8 * i + 3] * factor),
+                                       pack_bf16(v[8 * i + 4] * factor, v[8 * i + 5] * factor), pack_bf16(v[8 * i + 6] * factor, v[8 * i + 7] * factor));
+            *reinterpret_cast<uint4*>(stage + lane * (COLS * 2) + (((c / 8 + i) ^ (lane & kMix)) * 16)) = w;
+        }
+    }
+    __syncwarp();
+    const int unit = lane % kUnits;
+    if (col0 + unit * 8 >= dim) return;
+#pragma unroll 4
+    for (int r = lane / kUnits; r < rows; r += 32 / kUnits) {
+        if (r >= 32) break;
+        const uint4 w = *reinterpret_cast<const uint4*>(stage + r * (COLS * 2) + ((unit ^ (r & kMix)) * 16));
+        *reinterpret_cast<uint4*>(to.p + (row0 + r) * to.rs + head * to.hs + col0 + unit * 8) = w;
+    }
+}
+
+// ---------------------------------------------------------------- host side (attention_plan.cu)
+constexpr int64_t kMostRows = int64_t{1} << 30;
+
+struct Operand {                           // bf16 [rows][heads][dim] as an argument
+    const void* p;
+    int64_t rs, hs, heads;
+};
+
+// DLION_OK if 16-byte accesses and tiled copies can take it.
+dlion_status check_operand(const Operand& a, int64_t rows, int64_t dim);
+bool map_rows(CUtensorMap* map, const Operand& a, int64_t rows, int64_t dim);
+
+struct Sequences {
+    int64_t rows, length, count;
+    const void* offsets;
+    int offsets64;
+};
+dlion_status check_sequences(const Sequences& s);
+
+// Pieces of `tile` rows that the sequences have at most, and the plan for them; with offsets, tables are filled by one launch
+// for all plans (fill_plans), which also clears what belongs to no sequence.
+struct PlanRequest {
+    int tile, causal, keys;                // keys: pieces are tiles of keys, of which the first have most queries
+};
+int64_t most_pieces(const Sequences& s, int tile);
+
+struct Clear {                             // rows in no sequence
+    Rows t[3];
+    int heads[3];
+    int count, dim;
+    float* lse;
+    int64_t lse_ld;
+    int lse_heads;
+};
+// tables: n device arrays of most_pieces() entries, from the workspace (nullptr without offsets)
+void make_plans(prod::Call& c, const Sequences& s, const PlanRequest* requests, int n, int4* const* tables, Plan* plans, const Clear* clear);
+
+}  // namespace att
+}  // namespace dlion

@@ -1,0 +1,631 @@
+// The gradients of attention (include/dlion_layers.h).
+//
+//   p_ij = exp(s_ij - lse_i),  dp_ij = do_i . v_j,  D_i = do_i . out_i,  ds_ij = p_ij (dp_ij - D_i)
+//   dq_i = scale sum_j ds_ij k_j,  dk_j = scale sum_i ds_ij q_i,  dv_j = sum_i p_ij do_i
+//
+// in two kernels, one whose blocks keep a tile of queries and its dq, and one whose blocks keep a tile of keys and its dk and dv.
+// Scores and dp are computed in both, seven products instead of five; in return nothing is added up across blocks: no atomics,
+// whose order would change the results, and no binary32 dq in memory.
+#include "attention.cuh"
+
+namespace dlion {
+namespace att {
+
+namespace {
+
+struct Backward {
+    CUtensorMap q, k, v, dout;
+    Plan plan;
+    int heads, kv_heads, group, dim, causal;
+    float c, scale;                        // scale * log2(e)
+    Rows out, dout_rows;                   // read row by row
+    const float* lse;
+    int64_t lse_ld;
+    float* delta;                          // [heads][rows], D
+    int64_t delta_ld;
+    Rows dq, dk, dv;
+};
+
+constexpr int kThreads = 320;              // eight warps of arithmetic, a copying and an issuing warp
+
+// The eight warps: lanes of tensor memory go by warp % 4, so two warps have the same rows, each 64 columns.  What a warp leaves
+// there as an operand (64 bf16, 32 columns) goes over the first of the columns that it has read itself.
+__device__ __forceinline__ uint32_t operand_column(int k16) { return (k16 >> 2) * 64 + (k16 & 3) * 8; }
+
+struct Finish {                            // the end of every kernel: see product_kernel
+    __device__ static void end(bool fine, volatile uint32_t* slot_mem, unsigned int* mark, uint32_t tmem, int warp) {
+        if (!fine) {
+            slot_mem[1] = 1;
+            *mark = 1;
+        }
+        __syncwarp();
+        tc::fence_before();
+        __syncthreads();
+        if (slot_mem[1] != 0) {            // matrix instructions may still be running: let them end
+            const uint64_t t0 = tc::nanoseconds();
+            while (tc::nanoseconds() - t0 < 50000000ull) {
+            }
+        }
+        tc::fence_after();
+        if (warp == 9) tc::tmem_free<1>(tmem, 512);
+    }
+};
+
+// ---------------------------------------------------------------- dq
+template <int D>
+struct QueryShared {
+    static constexpr uint32_t kBytes = kTile * D * 2;
+    static constexpr int kKeys = 3, kValues = 2;                     // stages
+    static constexpr uint32_t kSums = (2 + kKeys + kValues) * kBytes;
+    static constexpr uint32_t kBars = kSums + 2 * kTile * 4;
+    static constexpr uint32_t kAll = kBars + 256 + 1024;
+};
+
+template <int D>
+__global__ void __launch_bounds__(kThreads, 1) query_gradient_kernel(const __grid_constant__ Backward w, unsigned int* mark) {
+    using S = QueryShared<D>;
+    extern __shared__ uint8_t raw[];
+    const uint32_t base = (tc::smem_addr(raw) + 1023u) & ~1023u;
+    uint8_t* mem = raw + (base - tc::smem_addr(raw));
+    const uint32_t keys = base + 2 * S::kBytes, values = keys + S::kKeys * S::kBytes, bars = base + S::kBars;
+    const uint32_t k_full = bars, k_empty = bars + 32, v_full = bars + 64, v_empty = bars + 96, scores = bars + 128, products = bars + 144,
+                   taken = bars + 152, slopes = bars + 160, rows_full = bars + 168, done = bars + 176, slot = bars + 192;
+    volatile uint32_t* slot_mem = reinterpret_cast<volatile uint32_t*>(mem + (slot - base));
+    const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+
+    tc::let_next_start();
+    if (w.plan.table != nullptr) tc::wait_for_previous();
+    const int head = static_cast<int>(blockIdx.x) % w.heads;
+    const Piece piece = piece_of(w.plan, static_cast<int>(blockIdx.x) / w.heads);
+    if (piece.length < 0) return;
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < S::kKeys; ++i) {
+            tc::bar_init(k_full + 8 * i, 1);
+            tc::bar_init(k_empty + 8 * i, 1);
+        }
+        for (int i = 0; i < S::kValues; ++i) {
+            tc::bar_init(v_full + 8 * i, 1);
+            tc::bar_init(v_empty + 8 * i, 1);
+        }
+        tc::bar_init(scores, 1);
+        tc::bar_init(scores + 8, 1);
+        tc::bar_init(products, 1);
+        tc::bar_init(taken, 8);
+        tc::bar_init(slopes, 8);
+        tc::bar_init(rows_full, 1);
+        tc::bar_init(done, 1);
+        tc::bar_init_done();
+        slot_mem[1] = 0;
+        tc::prefetch_map(&w.q);
+        tc::prefetch_map(&w.k);
+        tc::prefetch_map(&w.v);
+        tc::prefetch_map(&w.dout);
+    }
+    if (warp == 9) tc::tmem_alloc<1>(slot, 512);
+    tc::fence_before();
+    __syncthreads();
+    tc::fence_after();
+    const uint32_t tmem = *slot_mem, products_at = tmem + 256, dq_at = tmem + 384;
+    const int row0 = piece.tile * kTile;
+    const int key_tiles = (piece.length + kTile - 1) / kTile;
+    const int n = w.causal ? min(key_tiles, piece.tile + 1) : key_tiles;              // tiles of keys, from the last to the first
+    const int kv_head = head / w.group;
+    bool fine = true;
+    if (w.plan.table == nullptr) tc::wait_for_previous();
+
+    if (warp == 8) {
+        if (tc::elected()) {
+            tc::bar_expect(rows_full, 2 * S::kBytes);
+            load_head<D>(base, &w.q, head, piece.start + row0, rows_full);
+            load_head<D>(base + S::kBytes, &w.dout, head, piece.start + row0, rows_full);
+        }
+        __syncwarp();
+        int i = 0;
+        for (; i < n && fine; ++i) {
+            const int row = piece.start + (n - 1 - i) * kTile, ks = i % S::kKeys, vs = i % S::kValues;
+            if (!(fine = tc::bar_wait(k_empty + 8 * ks, ((i / S::kKeys) & 1) ^ 1))) break;
+            if (tc::elected()) {
+                tc::bar_expect(k_full + 8 * ks, S::kBytes);
+                load_head<D>(keys + ks * S::kBytes, &w.k, kv_head, row, k_full + 8 * ks);
+            }
+            __syncwarp();
+            if (!(fine = tc::bar_wait(v_empty + 8 * vs, ((i / S::kValues) & 1) ^ 1))) break;
+            if (tc::elected()) {
+                tc::bar_expect(v_full + 8 * vs, S::kBytes);
+                load_head<D>(values + vs * S::kBytes, &w.v, kv_head, row, v_full + 8 * vs);
+            }
+            __syncwarp();
+        }
+        if (!fine) {                       // what was asked for still lands in this block's memory: it is awaited
+            tc::bar_wait(rows_full, 0);
+            for (int a = max(0, i + 1 - S::kKeys); a <= i && a < n; ++a) tc::bar_wait(k_full + 8 * (a % S::kKeys), (a / S::kKeys) & 1);
+            for (int a = max(0, i - S::kValues); a < i; ++a) tc::bar_wait(v_full + 8 * (a % S::kValues), (a / S::kValues) & 1);
+        }
+    } else if (warp == 9) {
+        const int k_steps = (w.dim + 15) / 16;
+        const uint32_t square = tc::instruction(kTile, kTile, 0, 0), wide = tc::instruction(kTile, k_steps * 16, 0, 1);
+        auto finished = [&](uint32_t bar) {
+            if (tc::elected()) tc::commit<1>(bar);
+            __syncwarp();
+        };
+        auto against = [&](uint32_t d, uint32_t a_tile, uint32_t b_tile) {            // rows of both, along the head's columns
+            if (tc::elected()) {
+                const uint64_t a = along_row(a_tile), b = along_row(b_tile);
+                for (int s = 0; s < k_steps; ++s) tc::mma<1>(d, a + row_step(s), b + row_step(s), square, s > 0 ? 1u : 0u);
+            }
+            __syncwarp();
+        };
+        fine = tc::bar_wait(rows_full, 0);
+        // round i: scores of tile i (two sets of columns in turn), its dp once the last one's has been read, then dq of tile i - 1
+        for (int i = 0; i <= n && fine; ++i) {
+            if (i < n) {
+                if (!(fine = tc::bar_wait(k_full + 8 * (i % S::kKeys), (i / S::kKeys) & 1))) break;
+                tc::fence_after();
+                against(tmem + (i & 1) * kTile, base, keys + (i % S::kKeys) * S::kBytes);
+                finished(scores + 8 * (i & 1));
+                if (!(fine = tc::bar_wait(v_full + 8 * (i % S::kValues), (i / S::kValues) & 1))) break;
+                if (i > 0 && !(fine = tc::bar_wait(taken, (i - 1) & 1))) break;
+                tc::fence_after();
+                against(products_at, base + S::kBytes, values + (i % S::kValues) * S::kBytes);
+                finished(products);
+                finished(v_empty + 8 * (i % S::kValues));
+            }
+            if (i > 0) {
+                const int b = i - 1;
+                if (!(fine = tc::bar_wait(slopes, b & 1))) break;
+                tc::fence_after();
+                if (tc::elected()) {
+                    const uint64_t at = along_column(keys + (b % S::kKeys) * S::kBytes);
+                    const int steps = (min(kTile, piece.length - (n - 1 - b) * kTile) + 15) / 16;
+                    for (int s = 0; s < steps; ++s) {
+                        mma_tmem(dq_at, tmem + (b & 1) * kTile + operand_column(s), at + column_step(s), wide, (s > 0 || b > 0) ? 1u : 0u);
+                    }
+                }
+                __syncwarp();
+                finished(k_empty + 8 * (b % S::kKeys));
+            }
+        }
+        if (fine) finished(done);
+    } else {
+        const int half = warp / 4, quarter = warp % 4;
+        const int in_tile = quarter * 32 + lane, row = row0 + in_tile;
+        const bool live = row < piece.length;
+        const uint32_t lanes = static_cast<uint32_t>(quarter * 32) << 16;
+        float* sums = reinterpret_cast<float*>(mem + S::kSums);
+        // D, half of the head's columns a thread
+        float part = 0.0f, lse2 = 0.0f;
+        if (live) {
+            const int64_t at = piece.start + row;
+            const __nv_bfloat16 *o = w.out.p + at * w.out.rs + head * w.out.hs, *d = w.dout_rows.p + at * w.dout_rows.rs + head * w.dout_rows.hs;
+            const int units = w.dim / 8, mid = (units + 1) / 2;
+#pragma unroll 4
+            for (int u = half ? mid : 0; u < (half ? units : mid); ++u) {
+                float x[8], y[8];
+                widen(*reinterpret_cast<const uint4*>(o + u * 8), x);
+                widen(*reinterpret_cast<const uint4*>(d + u * 8), y);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) part = __fmaf_rn(x[e], y[e], part);
+            }
+            lse2 = w.lse[head * w.lse_ld + at] * kLog2e;
+        }
+        sums[half * kTile + in_tile] = part;
+        asm volatile("bar.sync 1, 256;" ::: "memory");
+        const float delta = sums[in_tile] + sums[kTile + in_tile];
+        if (live && half == 0) w.delta[head * w.delta_ld + piece.start + row] = delta;
+        const float2 cc = make_float2(w.c, w.c), minus = make_float2(-lse2, -lse2), less = make_float2(-delta, -delta);
+        for (int i = 0; i < n; ++i) {
+            const int j = n - 1 - i, valid = piece.length - j * kTile;
+            const uint32_t s_at = tmem + (i & 1) * kTile + half * 64 + lanes;
+            if (!(fine = tc::bar_wait(scores + 8 * (i & 1), (i >> 1) & 1))) break;
+            tc::fence_after();
+            float s[64];
+            tmem_load64(s_at, s);
+#pragma unroll
+            for (int e = 0; e < 64; e += 2) {
+                const float2 x = fma2(make_float2(s[e], s[e + 1]), cc, minus);
+                s[e] = exp2_fast(x.x);
+                s[e + 1] = exp2_fast(x.y);
+            }
+            if (!(fine = tc::bar_wait(products, i & 1))) break;
+            tc::fence_after();
+            float dp[64];
+            tmem_load64(products_at + half * 64 + lanes, dp);
+            tc::fence_before();
+            __syncwarp();
+            if (lane == 0) tc::bar_arrive(taken);
+#pragma unroll
+            for (int e = 0; e < 64; e += 2) {
+                const float2 x = mul2(add2(make_float2(dp[e], dp[e + 1]), less), make_float2(s[e], s[e + 1]));
+                s[e] = x.x;
+                s[e + 1] = x.y;
+            }
+            if (valid < kTile || (w.causal && (j + 1) * kTile > row0)) {
+                const int last = (w.causal ? min(row, piece.length - 1) : piece.length - 1) - j * kTile - half * 64;
+#pragma unroll
+                for (int e = 0; e < 64; ++e) s[e] = e <= last ? s[e] : 0.0f;
+                if (valid < kTile) {       // the keys' rows behind the sequence
+                    if (!(fine = tc::bar_wait(k_full + 8 * (i % S::kKeys), (i / S::kKeys) & 1))) break;
+                    clear_rows<D>(mem + (keys - base) + (i % S::kKeys) * S::kBytes, valid, threadIdx.x, 256);
+                }
+            }
+            uint32_t p[32];
+#pragma unroll
+            for (int e = 0; e < 32; ++e) p[e] = pack_bf16(s[2 * e], s[2 * e + 1]);
+            tmem_store32(s_at, p);
+            tmem_stored();
+            tc::fence_before();
+            __syncwarp();
+            if (lane == 0) tc::bar_arrive(slopes);
+        }
+        if (fine) fine = tc::bar_wait(done, 0);
+        if (fine) {
+            tc::fence_after();
+            constexpr int kHalf = D / 2;
+            uint8_t* stage = mem + warp * (32 * kHalf * 2);          // over the queries, which have been read
+            give_rows<kHalf>(dq_at + half * kHalf + lanes, w.scale, stage, w.dq, piece.start + row - lane, piece.length - row0 - quarter * 32, head,
+                             half * kHalf, w.dim, lane);
+        }
+    }
+    Finish::end(fine, slot_mem, mark, tmem, warp);
+}
+
+// ---------------------------------------------------------------- dk, dv
+// Scores and dp are computed transposed, keys as rows: so p and ds are operands as they lie in tensor memory.
+template <int D>
+struct KeyShared {
+    static constexpr uint32_t kBytes = kTile * D * 2;
+    static constexpr int kStages = 2;                                // of queries and of do
+    static constexpr uint32_t kStats = (2 + 2 * kStages) * kBytes;   // lse and D of two tiles of queries
+    static constexpr uint32_t kBars = kStats + 2 * 2 * kTile * 4;
+    static constexpr uint32_t kAll = kBars + 256 + 1024;
+};
+
+constexpr int kKeyThreads = 352;           // and a warp that brings lse and D
+
+template <int D>
+__global__ void __launch_bounds__(kKeyThreads, 1) key_gradient_kernel(const __grid_constant__ Backward w, unsigned int* mark) {
+    using S = KeyShared<D>;
+    constexpr int kStages = S::kStages;
+    extern __shared__ uint8_t raw[];
+    const uint32_t base = (tc::smem_addr(raw) + 1023u) & ~1023u;
+    uint8_t* mem = raw + (base - tc::smem_addr(raw));
+    const uint32_t queries = base + 2 * S::kBytes, douts = queries + kStages * S::kBytes, bars = base + S::kBars;
+    const uint32_t q_full = bars, q_empty = bars + 16, d_full = bars + 32, d_empty = bars + 48, scores = bars + 64, products = bars + 72,
+                   weights = bars + 80, slopes = bars + 88, rows_full = bars + 96, done = bars + 104, stats_full = bars + 112,
+                   stats_empty = bars + 128, slot = bars + 144;
+    volatile uint32_t* slot_mem = reinterpret_cast<volatile uint32_t*>(mem + (slot - base));
+    const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+
+    tc::let_next_start();
+    if (w.plan.table != nullptr) tc::wait_for_previous();
+    const int kv_head = static_cast<int>(blockIdx.x) % w.kv_heads;
+    const Piece piece = piece_of(w.plan, static_cast<int>(blockIdx.x) / w.kv_heads);
+    if (piece.length < 0) return;
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < kStages; ++i) {
+            tc::bar_init(q_full + 8 * i, 1);
+            tc::bar_init(q_empty + 8 * i, 1);
+            tc::bar_init(d_full + 8 * i, 1);
+            tc::bar_init(d_empty + 8 * i, 1);
+            tc::bar_init(stats_full + 8 * i, 1);
+            tc::bar_init(stats_empty + 8 * i, 8);
+        }
+        tc::bar_init(scores, 1);
+        tc::bar_init(products, 1);
+        tc::bar_init(weights, 8);
+        tc::bar_init(slopes, 8);
+        tc::bar_init(rows_full, 1);
+        tc::bar_init(done, 1);
+        tc::bar_init_done();
+        slot_mem[1] = 0;
+        tc::prefetch_map(&w.q);
+        tc::prefetch_map(&w.k);
+        tc::prefetch_map(&w.v);
+        tc::prefetch_map(&w.dout);
+    }
+    if (warp == 9) tc::tmem_alloc<1>(slot, 512);
+    tc::fence_before();
+    __syncthreads();
+    tc::fence_after();
+    const uint32_t tmem = *slot_mem, products_at = tmem + 128, dk_at = tmem + 256, dv_at = tmem + 256 + D;
+    const int key0 = piece.tile * kTile;
+    const int tiles = (piece.length + kTile - 1) / kTile, first = w.causal ? piece.tile : 0;
+    const int per = tiles - first, n = per * w.group;                // tiles of queries, of each head that shares these keys
+    bool fine = true;
+    if (w.plan.table == nullptr) tc::wait_for_previous();
+
+    if (warp == 8) {
+        if (tc::elected()) {
+            tc::bar_expect(rows_full, 2 * S::kBytes);
+            load_head<D>(base, &w.k, kv_head, piece.start + key0, rows_full);
+            load_head<D>(base + S::kBytes, &w.v, kv_head, piece.start + key0, rows_full);
+        }
+        __syncwarp();
+        int i = 0;
+        bool half = false;                 // of round i
+        for (; i < n && fine; ++i) {
+            const int head = kv_head * w.group + i / per, row = piece.start + (first + i % per) * kTile, st = i % kStages;
+            const uint32_t parity = ((i / kStages) & 1) ^ 1;
+            if (!(fine = tc::bar_wait(q_empty + 8 * st, parity))) break;
+            if (tc::elected()) {
+                tc::bar_expect(q_full + 8 * st, S::kBytes);
+                load_head<D>(queries + st * S::kBytes, &w.q, head, row, q_full + 8 * st);
+            }
+            __syncwarp();
+            half = true;
+            if (!(fine = tc::bar_wait(d_empty + 8 * st, parity))) break;
+            if (tc::elected()) {
+                tc::bar_expect(d_full + 8 * st, S::kBytes);
+                load_head<D>(douts + st * S::kBytes, &w.dout, head, row, d_full + 8 * st);
+            }
+            __syncwarp();
+            half = false;
+        }
+        if (!fine) {                       // what was asked for still lands in this block's memory: it is awaited
+            tc::bar_wait(rows_full, 0);
+            for (int a = max(0, i - kStages); a < i; ++a) {
+                tc::bar_wait(q_full + 8 * (a % kStages), (a / kStages) & 1);
+                tc::bar_wait(d_full + 8 * (a % kStages), (a / kStages) & 1);
+            }
+            if (half) tc::bar_wait(q_full + 8 * (i % kStages), (i / kStages) & 1);
+        }
+    } else if (warp == 10) {
+        float* stats = reinterpret_cast<float*>(mem + S::kStats);
+        for (int i = 0; i < n; ++i) {
+            const int head = kv_head * w.group + i / per, tile = first + i % per, st = i & 1;
+            float lse[4], delta[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const int row = tile * kTile + e * 32 + lane;
+                const bool live = row < piece.length;
+                lse[e] = live ? w.lse[head * w.lse_ld + piece.start + row] * kLog2e : 0.0f;
+                delta[e] = live ? w.delta[head * w.delta_ld + piece.start + row] : 0.0f;
+            }
+            if (!(fine = tc::bar_wait(stats_empty + 8 * st, ((i >> 1) & 1) ^ 1))) break;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                stats[st * 2 * kTile + e * 32 + lane] = -lse[e];
+                stats[st * 2 * kTile + kTile + e * 32 + lane] = -delta[e];
+            }
+            __syncwarp();
+            if (lane == 0) tc::bar_arrive(stats_full + 8 * st);
+        }
+    } else if (warp == 9) {
+        const int k_steps = (w.dim + 15) / 16;
+        const uint32_t square = tc::instruction(kTile, kTile, 0, 0), wide = tc::instruction(kTile, k_steps * 16, 0, 1);
+        auto finished = [&](uint32_t bar) {
+            if (tc::elected()) tc::commit<1>(bar);
+            __syncwarp();
+        };
+        auto against = [&](uint32_t d, uint32_t a_tile, uint32_t b_tile) {
+            if (tc::elected()) {
+                const uint64_t a = along_row(a_tile), b = along_row(b_tile);
+                for (int s = 0; s < k_steps; ++s) tc::mma<1>(d, a + row_step(s), b + row_step(s), square, s > 0 ? 1u : 0u);
+            }
+            __syncwarp();
+        };
+        auto onto = [&](uint32_t d, uint32_t a, uint32_t b_tile, int i) {             // the rows of the queries' tile i
+            if (tc::elected()) {
+                const uint64_t b = along_column(b_tile);
+                const int steps = (min(kTile, piece.length - (first + i % per) * kTile) + 15) / 16;
+                for (int s = 0; s < steps; ++s) mma_tmem(d, a + operand_column(s), b + column_step(s), wide, (s > 0 || i > 0) ? 1u : 0u);
+            }
+            __syncwarp();
+        };
+        fine = tc::bar_wait(rows_full, 0);
+        // round i: dv of tile i - 1, scores of tile i over its weights; dk of tile i - 1, dp of tile i over its slopes
+        for (int i = 0; i <= n && fine; ++i) {
+            const int st = i % kStages, b = i - 1, sb = b % kStages;
+            const uint32_t parity = (i / kStages) & 1;
+            if (i > 0) {
+                if (!(fine = tc::bar_wait(weights, b & 1))) break;
+                tc::fence_after();
+                onto(dv_at, tmem, douts + sb * S::kBytes, b);
+                finished(d_empty + 8 * sb);
+            }
+            if (i < n) {
+                if (!(fine = tc::bar_wait(q_full + 8 * st, parity))) break;
+                tc::fence_after();
+                against(tmem, base, queries + st * S::kBytes);
+                finished(scores);
+            }
+            if (i > 0) {
+                if (!(fine = tc::bar_wait(slopes, b & 1))) break;
+                tc::fence_after();
+                onto(dk_at, products_at, queries + sb * S::kBytes, b);
+                finished(q_empty + 8 * sb);
+            }
+            if (i < n) {
+                if (!(fine = tc::bar_wait(d_full + 8 * st, parity))) break;
+                tc::fence_after();
+                against(products_at, base + S::kBytes, douts + st * S::kBytes);
+                finished(products);
+            }
+        }
+        if (fine) finished(done);
+    } else {
+        const int half = warp / 4, quarter = warp % 4;
+        const int key = key0 + quarter * 32 + lane;
+        const uint32_t lanes = static_cast<uint32_t>(quarter * 32) << 16;
+        const uint32_t s_at = tmem + half * 64 + lanes, d_at = products_at + half * 64 + lanes;
+        const float* stats = reinterpret_cast<const float*>(mem + S::kStats);
+        const float2 cc = make_float2(w.c, w.c);
+        for (int i = 0; i < n; ++i) {
+            const int tile = first + i % per, st = i & 1, valid = piece.length - tile * kTile;
+            const float4* lse = reinterpret_cast<const float4*>(stats + st * 2 * kTile + half * 64);
+            const float4* delta = lse + kTile / 4;
+            const bool masked = valid < kTile || (w.causal && tile == piece.tile);
+            const int low = w.causal ? key - tile * kTile - half * 64 : 0, high = valid - half * 64;  // queries [low, high) of this warp's columns
+            if (!(fine = tc::bar_wait(stats_full + 8 * st, (i >> 1) & 1))) break;
+            if (!(fine = tc::bar_wait(scores, i & 1))) break;
+            tc::fence_after();
+            float s[64];
+            tmem_load64(s_at, s);
+#pragma unroll
+            for (int e = 0; e < 64; e += 4) {
+                const float4 x = lse[e / 4];
+                const float2 a = fma2(make_float2(s[e], s[e + 1]), cc, make_float2(x.x, x.y)), b = fma2(make_float2(s[e + 2], s[e + 3]), cc, make_float2(x.z, x.w));
+                s[e] = exp2_fast(a.x);
+                s[e + 1] = exp2_fast(a.y);
+                s[e + 2] = exp2_fast(b.x);
+                s[e + 3] = exp2_fast(b.y);
+            }
+            if (masked) {
+#pragma unroll
+                for (int e = 0; e < 64; ++e) s[e] = e >= low && e < high ? s[e] : 0.0f;
+                if (valid < kTile) {       // the queries' rows behind the sequence
+                    const int at = i % kStages;
+                    const uint32_t parity = (i / kStages) & 1;
+                    if (!(fine = tc::bar_wait(q_full + 8 * at, parity) && tc::bar_wait(d_full + 8 * at, parity))) break;
+                    clear_rows<D>(mem + (queries - base) + at * S::kBytes, valid, threadIdx.x, 256);
+                    clear_rows<D>(mem + (douts - base) + at * S::kBytes, valid, threadIdx.x, 256);
+                }
+            }
+            uint32_t p[32];
+#pragma unroll
+            for (int e = 0; e < 32; ++e) p[e] = pack_bf16(s[2 * e], s[2 * e + 1]);
+            tmem_store32(s_at, p);
+            tmem_stored();
+            tc::fence_before();
+            __syncwarp();
+            if (lane == 0) tc::bar_arrive(weights);
+            if (!(fine = tc::bar_wait(products, i & 1))) break;
+            tc::fence_after();
+            float dp[64];
+            tmem_load64(d_at, dp);
+#pragma unroll
+            for (int e = 0; e < 64; e += 4) {
+                const float4 x = delta[e / 4];
+                const float2 a = mul2(add2(make_float2(dp[e], dp[e + 1]), make_float2(x.x, x.y)), make_float2(s[e], s[e + 1]));
+                const float2 b = mul2(add2(make_float2(dp[e + 2], dp[e + 3]), make_float2(x.z, x.w)), make_float2(s[e + 2], s[e + 3]));
+                dp[e] = a.x;
+                dp[e + 1] = a.y;
+                dp[e + 2] = b.x;
+                dp[e + 3] = b.y;
+            }
+            if (masked) {
+#pragma unroll
+                for (int e = 0; e < 64; ++e) dp[e] = e >= low && e < high ? dp[e] : 0.0f;
+            }
+#pragma unroll
+            for (int e = 0; e < 32; ++e) p[e] = pack_bf16(dp[2 * e], dp[2 * e + 1]);
+            tmem_store32(d_at, p);
+            tmem_stored();
+            tc::fence_before();
+            __syncwarp();
+            if (lane == 0) {
+                tc::bar_arrive(slopes);
+                tc::bar_arrive(stats_empty + 8 * st);
+            }
+        }
+        if (fine) fine = tc::bar_wait(done, 0);
+        if (fine) {
+            tc::fence_after();
+            constexpr int kHalf = D / 2;
+            const int rows = piece.length - key0 - quarter * 32;
+            uint8_t* stage = mem + warp * (32 * kHalf * 2);          // over the keys, then the values, which have been read
+            give_rows<kHalf>(dk_at + half * kHalf + lanes, w.scale, stage, w.dk, piece.start + key - lane, rows, kv_head, half * kHalf, w.dim, lane);
+            give_rows<kHalf>(dv_at + half * kHalf + lanes, 1.0f, stage + S::kBytes, w.dv, piece.start + key - lane, rows, kv_head, half * kHalf, w.dim, lane);
+        }
+    }
+    Finish::end(fine, slot_mem, mark, tmem, warp);
+}
+
+Sequences sequences_of(const dlion_attention_bwd& p) { return Sequences{p.rows, p.length, p.sequences, p.offsets, p.offsets_64}; }
+
+dlion_status check(const dlion_attention_bwd* p) {
+    if (p == nullptr || p->heads < 1 || p->kv_heads < 1 || p->heads > 65535 || p->heads % p->kv_heads != 0) return DLION_EINVAL;
+    if (p->dim < 8 || p->dim > 128 || p->dim % 8 != 0 || p->causal < 0 || p->causal > 1 || !(p->scale > 0.0f) || !(p->scale < INFINITY)) return DLION_EINVAL;
+    const dlion_status seq = check_sequences(sequences_of(*p));
+    if (seq != DLION_OK) return seq;
+    if (p->zero_rest < 0 || p->zero_rest > 1 || p->lse_ld < p->rows) return DLION_EINVAL;
+    for (const Operand& a : {Operand{p->q, p->q_rs, p->q_hs, p->heads}, Operand{p->k, p->k_rs, p->k_hs, p->kv_heads},
+                             Operand{p->v, p->v_rs, p->v_hs, p->kv_heads}, Operand{p->out, p->out_rs, p->out_hs, p->heads},
+                             Operand{p->dout, p->dout_rs, p->dout_hs, p->heads}, Operand{p->dq, p->dq_rs, p->dq_hs, p->heads},
+                             Operand{p->dk, p->dk_rs, p->dk_hs, p->kv_heads}, Operand{p->dv, p->dv_rs, p->dv_hs, p->kv_heads}}) {
+        const dlion_status st = check_operand(a, p->rows, p->dim);
+        if (st != DLION_OK) return st;
+    }
+    if (p->rows > 0 && p->lse == nullptr) return DLION_EINVAL;
+    if (!aligned(p->lse, 4)) return DLION_EALIGN;
+    return most_pieces(sequences_of(*p), kTile) * p->heads <= INT_MAX ? DLION_OK : DLION_EINVAL;
+}
+
+template <int D>
+void launch(prod::Call& c, Backward& w, const Plan* plans, int64_t pieces) {
+    prod::raise_shared(c, &query_gradient_kernel<D>, QueryShared<D>::kAll);
+    prod::raise_shared(c, &key_gradient_kernel<D>, KeyShared<D>::kAll);
+    w.plan = plans[0];
+    prod::start(c, query_gradient_kernel<D>, dim3(static_cast<unsigned>(pieces * w.heads)), dim3(kThreads), QueryShared<D>::kAll, 1, w, c.mark);
+    w.plan = plans[1];
+    prod::start(c, key_gradient_kernel<D>, dim3(static_cast<unsigned>(pieces * w.kv_heads)), dim3(kKeyThreads), KeyShared<D>::kAll, 1, w, c.mark);
+}
+
+void backward(prod::Call& c, const dlion_attention_bwd& p) {
+    const Sequences seq = sequences_of(p);
+    const int64_t pieces = most_pieces(seq, kTile);
+    if (p.rows == 0) return;
+    int4* tables[2] = {nullptr, nullptr};
+    if (p.offsets != nullptr) {
+        tables[0] = c.ws.take<int4>(pieces);
+        tables[1] = c.ws.take<int4>(pieces);
+    }
+    float* delta = c.ws.take<float>(static_cast<uint64_t>(p.rows) * p.heads);
+    if (!c.live()) return;
+    auto rows = [](const void* t, int64_t rs, int64_t hs) { return Rows{static_cast<__nv_bfloat16*>(const_cast<void*>(t)), rs, hs}; };
+    Backward w{};
+    w.dq = rows(p.dq, p.dq_rs, p.dq_hs);
+    w.dk = rows(p.dk, p.dk_rs, p.dk_hs);
+    w.dv = rows(p.dv, p.dv_rs, p.dv_hs);
+    Clear clear{};
+    if (p.zero_rest) {
+        clear.t[0] = w.dq;
+        clear.t[1] = w.dk;
+        clear.t[2] = w.dv;
+        clear.heads[0] = static_cast<int>(p.heads);
+        clear.heads[1] = clear.heads[2] = static_cast<int>(p.kv_heads);
+        clear.count = 3;
+        clear.dim = static_cast<int>(p.dim);
+    }
+    const PlanRequest requests[2] = {{kTile, p.causal, 0}, {kTile, p.causal, 1}};
+    Plan plans[2];
+    make_plans(c, seq, requests, 2, tables, plans, p.zero_rest ? &clear : nullptr);
+    if (pieces == 0) return;
+    if (!map_rows(&w.q, Operand{p.q, p.q_rs, p.q_hs, p.heads}, p.rows, p.dim) || !map_rows(&w.k, Operand{p.k, p.k_rs, p.k_hs, p.kv_heads}, p.rows, p.dim) ||
+        !map_rows(&w.v, Operand{p.v, p.v_rs, p.v_hs, p.kv_heads}, p.rows, p.dim) ||
+        !map_rows(&w.dout, Operand{p.dout, p.dout_rs, p.dout_hs, p.heads}, p.rows, p.dim)) {
+        c.status = DLION_ECUDA;
+        return;
+    }
+    w.heads = static_cast<int>(p.heads);
+    w.kv_heads = static_cast<int>(p.kv_heads);
+    w.group = static_cast<int>(p.heads / p.kv_heads);
+    w.dim = static_cast<int>(p.dim);
+    w.causal = p.causal;
+    w.c = p.scale * kLog2e;
+    w.scale = p.scale;
+    w.out = rows(p.out, p.out_rs, p.out_hs);
+    w.dout_rows = rows(p.dout, p.dout_rs, p.dout_hs);
+    w.lse = p.lse;
+    w.lse_ld = p.lse_ld;
+    w.delta = delta;
+    w.delta_ld = p.rows;
+    p.dim <= 64 ? launch<64>(c, w, plans, pieces) : launch<128>(c, w, plans, pieces);
+}
+
+}  // namespace
+}  // namespace att
+}  // namespace dlion
+
+extern "C" {
+
+uint64_t dlion_attention_backward_workspace(const dlion_attention_bwd* p) {
+    return dlion::att::check(p) == DLION_OK ? dlion::prod::workspace_of(*p, dlion::att::backward) : 0;
+}
+
+dlion_status dlion_attention_backward(const dlion_attention_bwd* p, void* workspace, uint64_t workspace_bytes, void* cuda_stream) {
+    const dlion_status st = dlion::att::check(p);
+    return st != DLION_OK ? st : dlion::prod::run(*p, dlion::att::backward, workspace, workspace_bytes, cuda_stream);
+}
+
+}  // extern "C"

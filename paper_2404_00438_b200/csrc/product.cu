@@ -218,16 +218,23 @@ Matrix readable(Call& c, const Matrix& a) {
     return r;
 }
 
+bool encode_map(CUtensorMap* map, const void* p, int rank, const uint64_t* dims, const uint64_t* strides, const uint32_t* box) {
+    const cuuint32_t one[3] = {1, 1, 1};
+    cuuint64_t d[3], s[2];
+    std::copy(dims, dims + rank, d);
+    std::copy(strides, strides + rank - 1, s);
+    return encoder()(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, static_cast<cuuint32_t>(rank), const_cast<void*>(p), d, s, box, one,
+                     CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                     CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 bool make_map(CUtensorMap* map, const Matrix& a, int* mn_major, int box_rows) {
     const bool mn = a.cs != 1;                 // adjacent rows
     *mn_major = mn ? 1 : 0;
-    const cuuint64_t dims[2] = {static_cast<cuuint64_t>(mn ? a.rows : a.cols), static_cast<cuuint64_t>(mn ? a.cols : a.rows)};
-    const cuuint64_t strides[1] = {static_cast<cuuint64_t>(mn ? a.cs : a.rs) * 2};
-    const cuuint32_t box[2] = {64, static_cast<cuuint32_t>(mn ? kSlice : box_rows)};
-    const cuuint32_t one[2] = {1, 1};
-    return encoder()(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(a.p), dims, strides, box, one,
-                     CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
-                     CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+    const uint64_t dims[2] = {static_cast<uint64_t>(mn ? a.rows : a.cols), static_cast<uint64_t>(mn ? a.cols : a.rows)};
+    const uint64_t strides[1] = {static_cast<uint64_t>(mn ? a.cs : a.rs) * 2};
+    const uint32_t box[2] = {64, static_cast<uint32_t>(mn ? kSlice : box_rows)};
+    return encode_map(map, a.p, 2, dims, strides, box);
 }
 
 bool shape_of(const Config& cfg, const Matrix& a, const Matrix& b, Shape* s) {

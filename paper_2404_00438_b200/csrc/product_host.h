@@ -79,6 +79,9 @@ bool few_rows(Call& c, const Matrix& a, const Matrix& b, const Finish& f);
 
 inline Matrix transposed(const Matrix& a) { return Matrix{a.p, a.cols, a.rows, a.cs, a.rs}; }
 
+// Tensor map of bf16, rank 2 or 3, the first dimension adjacent; strides in bytes, of the others.
+bool encode_map(CUtensorMap* map, const void* p, int rank, const uint64_t* dims, const uint64_t* strides, const uint32_t* box);
+
 // Tensor map of 64 x `box` tiles; `mn` of the operand's rows adjacent (1) or its columns (0).
 bool make_map(CUtensorMap* map, const Matrix& a, int* mn_major, int box_rows);
 

@@ -5,13 +5,17 @@ declared in ``include/dlion_layers.h``.
     du, dw, db = linear_backward(dy, w2, z8, act="gelu")           # gradients of y2 = act(z) w2 + b2
     x8 = checkpoint8(x); x = restore8(x8)                          # a 33/64 of bf16's bytes
     r = lm_loss(x, w, targets)                                     # r.loss, r.rows, r.dx, r.dw
+    y, stats = norm_forward(x, w, b)                               # layer norm
+    dx, dw, db = norm_backward(dy, x, w, stats, residual=r)        # its gradients, the skip's added
+    out, lse = attention_forward(q, k, v, offsets=offsets)         # of packed sequences
+    dq, dk, dv = attention_backward(dout, q, k, v, out, lse, offsets=offsets)
 
 Argument marshalling only, as in ``dlion``: every tensor is checked, becomes a device address, and the
 current torch stream becomes the ``cudaStream_t``.  Outputs may be given (``out=``, ``dw=``, ...): a view
 into the optimizer's gradient arena is a valid ``dw`` or ``db``.  The workspace comes from torch's
 allocator on the current stream unless one is given.  There is no CPU path, and no autograd: tensors that require
-gradients are read like any others and results have no graph; the gradients are what ``linear_backward``
-and ``lm_loss`` return.
+gradients are read like any others and results have no graph; the gradients are what the ``_backward`` calls and
+``lm_loss`` return.
 """
 from __future__ import annotations
 
@@ -32,7 +36,9 @@ _BF16 = torch.bfloat16
 
 EXPORTS = ("dlion_linear_forward_workspace", "dlion_linear_backward_workspace", "dlion_lm_loss_workspace",
            "dlion_linear_forward", "dlion_linear_backward", "dlion_lm_loss", "dlion_checkpoint8",
-           "dlion_restore8", "dlion_layers_check")
+           "dlion_restore8", "dlion_norm_forward", "dlion_norm_backward_workspace", "dlion_norm_backward",
+           "dlion_attention_forward_workspace", "dlion_attention_forward", "dlion_attention_backward_workspace",
+           "dlion_attention_backward", "dlion_layers_check")
 
 _i64, _i32, _vp, _f32 = ctypes.c_int64, ctypes.c_int32, ctypes.c_void_p, ctypes.c_float
 
@@ -59,11 +65,43 @@ class _Loss(ctypes.Structure):
                 ("dw", _vp), ("dw_ld", _i64), ("grad_type", _i32), ("piece", _i64)]
 
 
+class _NormForward(ctypes.Structure):
+    _fields_ = [("m", _i64), ("n", _i64), ("x", _vp), ("x_ld", _i64), ("x_type", _i32), ("w", _vp), ("w_type", _i32),
+                ("b", _vp), ("b_type", _i32), ("eps", _f32), ("y", _vp), ("y_ld", _i64), ("y_type", _i32), ("stats", _vp)]
+
+
+class _NormBackward(ctypes.Structure):
+    _fields_ = [("m", _i64), ("n", _i64), ("dy", _vp), ("dy_ld", _i64), ("dy_type", _i32), ("x", _vp), ("x_ld", _i64),
+                ("x_type", _i32), ("w", _vp), ("w_type", _i32), ("stats", _vp), ("residual", _vp), ("r_ld", _i64),
+                ("dx", _vp), ("dx_ld", _i64), ("dw", _vp), ("db", _vp), ("grad_type", _i32)]
+
+
+def _strided(*names):
+    return [f for n in names for f in ((n, _vp), (n + "_rs", _i64), (n + "_hs", _i64))]
+
+
+_ATTENTION_SIZES = [("rows", _i64), ("heads", _i64), ("kv_heads", _i64), ("dim", _i64)]
+_ATTENTION_SEQUENCES = [("offsets", _vp), ("offsets_64", _i32), ("sequences", _i64), ("length", _i64), ("causal", _i32), ("scale", _f32)]
+
+
+class _AttentionForward(ctypes.Structure):
+    _fields_ = (_ATTENTION_SIZES + _strided("q", "k", "v") + _ATTENTION_SEQUENCES + _strided("out")
+                + [("lse", _vp), ("lse_ld", _i64), ("zero_rest", _i32)])
+
+
+class _AttentionBackward(ctypes.Structure):
+    _fields_ = (_ATTENTION_SIZES + _strided("q", "k", "v", "out", "dout") + [("lse", _vp), ("lse_ld", _i64)] + _ATTENTION_SEQUENCES
+                + _strided("dq", "dk", "dv") + [("zero_rest", _i32)])
+
+
 def _bind(lib):
-    for name, struct in (("dlion_linear_forward", _Forward), ("dlion_linear_backward", _Backward), ("dlion_lm_loss", _Loss)):
+    for name, struct in (("dlion_linear_forward", _Forward), ("dlion_linear_backward", _Backward), ("dlion_lm_loss", _Loss),
+                         ("dlion_norm_backward", _NormBackward), ("dlion_attention_forward", _AttentionForward),
+                         ("dlion_attention_backward", _AttentionBackward)):
         size, call = getattr(lib, name + "_workspace"), getattr(lib, name)
         size.argtypes, size.restype = [ctypes.POINTER(struct)], ctypes.c_uint64
         call.argtypes, call.restype = [ctypes.POINTER(struct), _vp, ctypes.c_uint64, _vp], ctypes.c_int
+    lib.dlion_norm_forward.argtypes, lib.dlion_norm_forward.restype = [ctypes.POINTER(_NormForward), _vp], ctypes.c_int
     lib.dlion_checkpoint8.argtypes = [_vp, _i64, _i64, _i64, _vp, _i64, _vp, _i64, _vp]
     lib.dlion_checkpoint8.restype = ctypes.c_int
     lib.dlion_restore8.argtypes = [_vp, _i64, _vp, _i64, _i64, _i64, _vp, _i64, _vp]
@@ -82,6 +120,9 @@ _Tensor, _empty = torch.Tensor, torch.empty
 _FORWARD = (_lib.dlion_linear_forward_workspace, _lib.dlion_linear_forward)
 _BACKWARD = (_lib.dlion_linear_backward_workspace, _lib.dlion_linear_backward)
 _LOSS = (_lib.dlion_lm_loss_workspace, _lib.dlion_lm_loss)
+_NORM_BACKWARD = (_lib.dlion_norm_backward_workspace, _lib.dlion_norm_backward)
+_ATTENTION_FORWARD = (_lib.dlion_attention_forward_workspace, _lib.dlion_attention_forward)
+_ATTENTION_BACKWARD = (_lib.dlion_attention_backward_workspace, _lib.dlion_attention_backward)
 _ONLY_BF16 = (_BF16,)
 
 
@@ -89,6 +130,16 @@ class Checkpoint8(NamedTuple):
     """A matrix in 8 bits: value = q * 2^(e - 127), ``e`` shared by 32 values of a row ([ceil(k/32), m])."""
     q: torch.Tensor
     e: torch.Tensor
+
+
+class Normed(NamedTuple):
+    out: torch.Tensor
+    stats: torch.Tensor                # float32 [2, m]: the rows' means, then 1 / sqrt(var + eps)
+
+
+class Attended(NamedTuple):
+    out: torch.Tensor                  # bf16 [rows, heads, dim]
+    lse: torch.Tensor                  # float32 [heads, rows]: log of the sum of the scores' exponentials
 
 
 class Loss(NamedTuple):
@@ -356,6 +407,196 @@ def lm_loss(x: torch.Tensor, w: torch.Tensor, targets: torch.Tensor, *, ignore_i
                  0 if dw is None else dw.stride(0), g, piece)
     _call(_LOSS, args, device, workspace)
     return Loss(loss, rows, dx, dw)
+
+
+def norm_forward(x: torch.Tensor, w: Optional[torch.Tensor] = None, b: Optional[torch.Tensor] = None, *, eps: float = 1e-5,
+                 out: Optional[torch.Tensor] = None, out_dtype: torch.dtype = torch.bfloat16) -> Normed:
+    """Layer norm of the rows of ``x`` (bf16 or fp32 [m, n], adjacent columns): ``(x - mean) rstd w + b`` with ``w`` and
+    ``b`` [n] bf16 or fp32 (1 and 0 where they are not given), and the rows' statistics, which the backward pass takes."""
+    device = _device(x, "x")
+    m, n = _two_dim(x, "x")
+    _matrix(x, "x", device, _TYPES, (m, n), True)
+    if w is not None:
+        _vector(w, "w", device, _TYPES, n)
+    if b is not None:
+        _vector(b, "b", device, _TYPES, n)
+    if out is None:
+        if out_dtype not in _TYPES:
+            raise ValueError(f"out_dtype: {out_dtype}, expected one of {tuple(_TYPES)}")
+        out = x.new_empty((m, n), dtype=out_dtype)
+    else:
+        _matrix(out, "out", device, _TYPES, (m, n), True)
+    stats = x.new_empty((2, m), dtype=torch.float32)
+    args = _NormForward(m, n, x.data_ptr(), x.stride(0), _TYPES[x.dtype], _ptr(w), 0 if w is None else _TYPES[w.dtype], _ptr(b),
+                        0 if b is None else _TYPES[b.dtype], eps, out.data_ptr(), out.stride(0), _TYPES[out.dtype], stats.data_ptr())
+    st = _lib.dlion_norm_forward(ctypes.byref(args), _stream(device))
+    if st != OK:
+        raise DlionError(st, "dlion_norm_forward")
+    return Normed(out, stats)
+
+
+def norm_backward(dy: torch.Tensor, x: torch.Tensor, w: Optional[torch.Tensor], stats: torch.Tensor, *,
+                  residual: Optional[torch.Tensor] = None, need_dx: bool = True, need_dw: bool = True, need_db: bool = True,
+                  grad_dtype: torch.dtype = torch.bfloat16, dx: Optional[torch.Tensor] = None, dw: Optional[torch.Tensor] = None,
+                  db: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None):
+    """Gradients of ``norm_forward(x, w, b)``, whose ``stats`` these are: dx in ``x``'s type, ``residual`` (of that type too:
+    the gradient that goes past the norm) added, and ``dw``, ``db`` ([n]) in ``grad_dtype``.  Returns (dx, dw, db), None for what
+    is not needed."""
+    device = _device(dy, "dy")
+    m, n = _two_dim(dy, "dy")
+    _matrix(dy, "dy", device, _TYPES, (m, n), True)
+    _matrix(x, "x", device, _TYPES, (m, n), True)
+    if w is not None:
+        _vector(w, "w", device, _TYPES, n)
+    _matrix(stats, "stats", device, (torch.float32,), (2, m))
+    if not stats.is_contiguous():
+        raise ValueError(f"stats: expected adjacent values, got strides {stats.stride()}")
+    stream = (x.dtype,)
+    if residual is not None:
+        _matrix(residual, "residual", device, stream, (m, n), True)
+    g = _grad_type(grad_dtype)
+    if not need_dx:
+        dx = None
+    elif dx is None:
+        dx = x.new_empty((m, n))
+    else:
+        _matrix(dx, "dx", device, stream, (m, n), True)
+    if not need_dw:
+        dw = None
+    elif dw is None:
+        dw = x.new_empty((n,), dtype=grad_dtype)
+    else:
+        _vector(dw, "dw", device, (grad_dtype,), n)
+    if not need_db:
+        db = None
+    elif db is None:
+        db = x.new_empty((n,), dtype=grad_dtype)
+    else:
+        _vector(db, "db", device, (grad_dtype,), n)
+    args = _NormBackward(m, n, dy.data_ptr(), dy.stride(0), _TYPES[dy.dtype], x.data_ptr(), x.stride(0), _TYPES[x.dtype], _ptr(w),
+                         0 if w is None else _TYPES[w.dtype], stats.data_ptr(), _ptr(residual),
+                         0 if residual is None else residual.stride(0), _ptr(dx), 0 if dx is None else dx.stride(0), _ptr(dw), _ptr(db), g)
+    _call(_NORM_BACKWARD, args, device, workspace)
+    return dx, dw, db
+
+
+def _heads(t, name: str, device: int, shape) -> None:
+    """Raises unless ``t`` is a bf16 tensor of ``shape`` (rows, heads, dim) that 16-byte accesses can take: adjacent columns of a head,
+    rows and heads that begin on the 16-byte grid and are not broadcast."""
+    if not (isinstance(t, _Tensor) and t.dtype is _BF16 and t.shape == shape and t.get_device() == device):
+        _refused(t, name, device, _ONLY_BF16, shape)
+    rs, hs, cs = t.stride()
+    if (cs != 1 or (shape[1] > 1 and (hs % 8 or hs < shape[2])) or (shape[0] > 1 and (rs % 8 or rs < shape[2]))
+            or t.data_ptr() % 16):
+        raise ValueError(f"{name}: needs adjacent columns, and rows and heads on the 16-byte grid (got strides {(rs, hs, cs)}, "
+                         f"address {t.data_ptr() % 16} beyond a multiple of 16)")
+
+
+def _attention_sizes(q, k, v, device: int):
+    for t, name in ((q, "q"), (k, "k"), (v, "v")):
+        if not isinstance(t, _Tensor):
+            raise ValueError(f"{name}: expected a torch.Tensor, got {type(t).__name__}")
+        if t.dim() != 3:
+            raise ValueError(f"{name}: expected [rows, heads, dim], got {t.dim()} dimensions")
+    rows, heads, dim = q.shape
+    kv = k.shape[1]
+    if kv < 1 or heads < 1 or heads % kv:
+        raise ValueError(f"q: {heads} heads, not a multiple of the {kv} of k and v")
+    if dim < 8 or dim > 128 or dim % 8:
+        raise ValueError(f"q: heads of {dim} columns, expected a multiple of 8, at most 128")
+    _heads(q, "q", device, (rows, heads, dim))
+    _heads(k, "k", device, (rows, kv, dim))
+    _heads(v, "v", device, (rows, kv, dim))
+    return rows, heads, kv, dim
+
+
+def _sequences(offsets, length, rows: int, device: int):
+    """The fields offsets, offsets_64, sequences, length."""
+    if offsets is None:
+        if length is None:
+            return None, 0, 0, 0
+        if not isinstance(length, int) or length < 1 or rows % length:
+            raise ValueError(f"length: {length!r}, expected a number that divides the {rows} rows")
+        return None, 0, 0, length
+    if length is not None:
+        raise ValueError("offsets and length: one of them at most")
+    if not isinstance(offsets, _Tensor) or offsets.dim() != 1 or offsets.shape[0] < 1:
+        raise ValueError("offsets: expected a tensor of sequences + 1 values")
+    _vector(offsets, "offsets", device, (torch.int32, torch.int64), offsets.shape[0])
+    return offsets.data_ptr(), int(offsets.dtype == torch.int64), offsets.shape[0] - 1, 0
+
+
+def _given(t, name: str, device: int, shape, like, zero_rest: bool, offsets):
+    """An output tensor and whether its rows in no sequence are to be cleared."""
+    if t is None:
+        return like.new_empty(shape), offsets is not None
+    _heads(t, name, device, shape)
+    return t, bool(zero_rest)
+
+
+def _scale(scale, dim: int) -> float:
+    if scale is None:
+        return dim ** -0.5
+    if not 0.0 < scale < 3.4e38:
+        raise ValueError(f"scale: {scale!r}, expected a positive number")
+    return scale
+
+
+def attention_forward(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, *, causal: bool = True, scale: Optional[float] = None,
+                      offsets: Optional[torch.Tensor] = None, length: Optional[int] = None, out: Optional[torch.Tensor] = None,
+                      lse: Optional[torch.Tensor] = None, zero_rest: bool = False, workspace: Optional[torch.Tensor] = None) -> Attended:
+    """Attention within sequences that lie one behind the other: ``q`` [rows, heads, dim], ``k`` and ``v`` [rows, kv_heads, dim],
+    bf16, each a view of any row and head strides on the 16-byte grid (of one product's output, say); heads / kv_heads query
+    heads in a row share a key head.  ``offsets`` (int32 or int64 on the device, ascending, sequences + 1 of them) says where
+    the sequences begin and end, ``length`` that all have so many rows; with neither all rows are one.  ``scale`` is
+    1 / sqrt(dim) where it is not given.  Rows in no sequence are left as they were in ``out`` and ``lse``, unless
+    ``zero_rest``; they are zero in results that are not given."""
+    device = _device(q, "q")
+    rows, heads, kv, dim = _attention_sizes(q, k, v, device)
+    sequences = _sequences(offsets, length, rows, device)
+    own = out is None and lse is None
+    out, zero = _given(out, "out", device, (rows, heads, dim), q, zero_rest, offsets)
+    if lse is None:
+        lse = (torch.empty if own or offsets is None else torch.zeros)((heads, rows), dtype=torch.float32, device=q.device)
+    else:
+        _matrix(lse, "lse", device, (torch.float32,), (heads, rows), True)
+        if zero and not zero_rest:             # a result of each kind: the given one is left as it was
+            out, zero = out.zero_(), False
+    qs, ks, vs, os = q.stride(), k.stride(), v.stride(), out.stride()
+    args = _AttentionForward(rows, heads, kv, dim, q.data_ptr(), qs[0], qs[1], k.data_ptr(), ks[0], ks[1], v.data_ptr(), vs[0], vs[1],
+                             *sequences, int(bool(causal)), _scale(scale, dim), out.data_ptr(), os[0], os[1], lse.data_ptr(),
+                             max(lse.stride(0), rows), int(zero))
+    _call(_ATTENTION_FORWARD, args, device, workspace)
+    return Attended(out, lse)
+
+
+def attention_backward(dout: torch.Tensor, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, out: torch.Tensor, lse: torch.Tensor, *,
+                       causal: bool = True, scale: Optional[float] = None, offsets: Optional[torch.Tensor] = None,
+                       length: Optional[int] = None, dq: Optional[torch.Tensor] = None, dk: Optional[torch.Tensor] = None,
+                       dv: Optional[torch.Tensor] = None, zero_rest: bool = False, workspace: Optional[torch.Tensor] = None):
+    """Gradients (dq, dk, dv) of ``attention_forward`` with the same arguments, whose results ``out`` and ``lse`` are.  ``dk`` and
+    ``dv`` are summed over the query heads that share them.  Views of one tensor are valid results: the gradient
+    of the product that made q, k and v.  Rows in no sequence as in ``attention_forward``."""
+    device = _device(dout, "dout")
+    rows, heads, kv, dim = _attention_sizes(q, k, v, device)
+    sequences = _sequences(offsets, length, rows, device)
+    _heads(dout, "dout", device, (rows, heads, dim))
+    _heads(out, "out", device, (rows, heads, dim))
+    _matrix(lse, "lse", device, (torch.float32,), (heads, rows), True)
+    given = [t is not None for t in (dq, dk, dv)]
+    mixed = offsets is not None and any(given) and not all(given) and not zero_rest
+    results, zero = [], False
+    for t, name, shape in ((dq, "dq", (rows, heads, dim)), (dk, "dk", (rows, kv, dim)), (dv, "dv", (rows, kv, dim))):
+        r, z = _given(t, name, device, shape, q, zero_rest, offsets)
+        if mixed:                              # the given ones are left as they were
+            r = r if t is not None else r.zero_()
+        results.append(r)
+        zero = zero or (z and not mixed)
+    strides = [f for t in (q, k, v, out, dout) for f in (t.data_ptr(), t.stride(0), t.stride(1))]
+    args = _AttentionBackward(rows, heads, kv, dim, *strides, lse.data_ptr(), max(lse.stride(0), rows), *sequences, int(bool(causal)),
+                              _scale(scale, dim), *[f for t in results for f in (t.data_ptr(), t.stride(0), t.stride(1))], int(zero))
+    _call(_ATTENTION_BACKWARD, args, device, workspace)
+    return tuple(results)
 
 
 def check() -> None:
