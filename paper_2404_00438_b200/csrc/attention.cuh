@@ -35,6 +35,39 @@ __device__ __forceinline__ Piece piece_of(const Plan& p, int i) {
     return Piece{(i - rank * p.sequences) * p.length, p.length, p.descending ? p.tiles - 1 - rank : rank};
 }
 
+// A value that all lanes of a converged warp have, as one that the compiler knows to be the same in all (and may keep in a uniform
+// register): what comes out of memory is otherwise one value a lane, and the operands of a matrix instruction are then brought
+// over one by one before each.
+__device__ __forceinline__ int same(int v) { return static_cast<int>(__reduce_or_sync(0xffffffffu, static_cast<unsigned>(v))); }
+
+// A block's pieces of work, each a tile of a sequence and a head: every gridDim.x-th of them, in turn from either end, since they
+// become lighter along the list.  The kernels are persistent: while a tile's last rows are weighed and its results leave, the next
+// one's first products run (197 rows, 12 heads, 64 images forward: 47 us with a block for each tile).  The next entry is asked for
+// ahead of time.
+struct Pieces {
+    const Plan* plan;
+    int heads, units, round;
+    Piece next;
+
+    __device__ __forceinline__ int unit() const {
+        const int g = static_cast<int>(gridDim.x), b = static_cast<int>(blockIdx.x);
+        return round * g + ((round & 1) ? g - 1 - b : b);
+    }
+    __device__ __forceinline__ Pieces(const Plan& p, int heads_, int units_) : plan(&p), heads(heads_), units(units_), round(-1) { look(); }
+    __device__ __forceinline__ void look() {
+        ++round;
+        next = unit() < units ? piece_of(*plan, unit() / heads) : Piece{0, -1, 0};
+    }
+    // false when there are no more
+    __device__ __forceinline__ bool take(Piece& piece, int& head) {
+        piece = Piece{same(next.start), same(next.length), same(next.tile)};
+        if (piece.length < 0) return false;
+        head = unit() % heads;
+        look();
+        return true;
+    }
+};
+
 // bf16 [rows][heads][dim], strides in elements
 struct Rows {
     __nv_bfloat16* p;
@@ -89,6 +122,39 @@ __device__ __forceinline__ void mma_tmem(uint32_t d, uint32_t a, uint64_t b, uin
         : "memory");
 }
 
+// The matrix instructions of one product, by a converged warp: what describes the operands is worked out by the whole warp, so
+// that it stays in uniform registers, where these instructions want it, and the instructions of a full product stand one behind
+// the other.  (Inside a branch that one lane has taken, with a loop, an instruction took 150 clocks to issue, and its product 64.)
+//
+// d = rows of a times rows of b, both along a head's columns, 16 * steps of them (the rest of D is not there).
+template <int D>
+__device__ __forceinline__ void rows_by_rows(uint32_t d, uint32_t a_tile, uint32_t b_tile, int steps) {
+    const uint64_t a = along_row(a_tile), b = along_row(b_tile);
+    const uint32_t inst = tc::instruction(kTile, kTile, 0, 0);
+    if (tc::elected()) {
+#pragma unroll
+        for (int i = 0; i < D / 16; ++i) {
+            if (i < steps) tc::mma<1>(d, a + row_step(i), b + row_step(i), inst, i > 0 ? 1u : 0u);
+        }
+    }
+    __syncwarp();
+}
+
+// d (+)= the 16-value steps [FROM, TO) of a, in tensor memory 8 columns a step (GAP more between the halves), times the tile's
+// rows; `steps` of all eight are there.
+template <int FROM, int TO, int GAP>
+__device__ __forceinline__ void weights_by_rows(uint32_t d, uint32_t a, uint32_t b_tile, uint32_t inst, int steps, bool add) {
+    const uint64_t b = along_column(b_tile);
+    const uint32_t onto = add ? 1u : 0u;
+    if (tc::elected()) {
+#pragma unroll
+        for (int i = FROM; i < TO; ++i) {
+            if (i < steps) mma_tmem(d, a + 8 * i + (i >= 4 ? GAP : 0), b + column_step(i), inst, i > 0 ? 1u : onto);
+        }
+    }
+    __syncwarp();
+}
+
 // ---------------------------------------------------------------- tensor memory
 // 64 consecutive columns of this warp's 32 lanes, a row a thread.
 __device__ __forceinline__ void tmem_load64(uint32_t addr, float (&v)[64]) {
@@ -114,6 +180,51 @@ __device__ __forceinline__ void tmem_load64(uint32_t addr, float (&v)[64]) {
           "=r"(r[48]), "=r"(r[49]), "=r"(r[50]), "=r"(r[51]), "=r"(r[52]), "=r"(r[53]), "=r"(r[54]), "=r"(r[55]),
           "=r"(r[56]), "=r"(r[57]), "=r"(r[58]), "=r"(r[59]), "=r"(r[60]), "=r"(r[61]), "=r"(r[62]), "=r"(r[63])
         : "r"(addr)
+        : "memory");
+}
+
+// 128 columns: both halves asked for before the first is waited for.
+__device__ __forceinline__ void tmem_load128(uint32_t addr, float (&v)[128]) {
+    uint32_t* r = reinterpret_cast<uint32_t*>(v);
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x64.b32 {"
+        "%0, %1, %2, %3, %4, %5, %6, %7, "
+        "%8, %9, %10, %11, %12, %13, %14, %15, "
+        "%16, %17, %18, %19, %20, %21, %22, %23, "
+        "%24, %25, %26, %27, %28, %29, %30, %31, "
+        "%32, %33, %34, %35, %36, %37, %38, %39, "
+        "%40, %41, %42, %43, %44, %45, %46, %47, "
+        "%48, %49, %50, %51, %52, %53, %54, %55, "
+        "%56, %57, %58, %59, %60, %61, %62, %63"
+        "}, [%128];\n"
+        "tcgen05.ld.sync.aligned.32x32b.x64.b32 {"
+        "%64, %65, %66, %67, %68, %69, %70, %71, "
+        "%72, %73, %74, %75, %76, %77, %78, %79, "
+        "%80, %81, %82, %83, %84, %85, %86, %87, "
+        "%88, %89, %90, %91, %92, %93, %94, %95, "
+        "%96, %97, %98, %99, %100, %101, %102, %103, "
+        "%104, %105, %106, %107, %108, %109, %110, %111, "
+        "%112, %113, %114, %115, %116, %117, %118, %119, "
+        "%120, %121, %122, %123, %124, %125, %126, %127"
+        "}, [%129];\n"
+        "tcgen05.wait::ld.sync.aligned;"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
+          "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]),
+          "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]),
+          "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31]),
+          "=r"(r[32]), "=r"(r[33]), "=r"(r[34]), "=r"(r[35]), "=r"(r[36]), "=r"(r[37]), "=r"(r[38]), "=r"(r[39]),
+          "=r"(r[40]), "=r"(r[41]), "=r"(r[42]), "=r"(r[43]), "=r"(r[44]), "=r"(r[45]), "=r"(r[46]), "=r"(r[47]),
+          "=r"(r[48]), "=r"(r[49]), "=r"(r[50]), "=r"(r[51]), "=r"(r[52]), "=r"(r[53]), "=r"(r[54]), "=r"(r[55]),
+          "=r"(r[56]), "=r"(r[57]), "=r"(r[58]), "=r"(r[59]), "=r"(r[60]), "=r"(r[61]), "=r"(r[62]), "=r"(r[63]),
+          "=r"(r[64]), "=r"(r[65]), "=r"(r[66]), "=r"(r[67]), "=r"(r[68]), "=r"(r[69]), "=r"(r[70]), "=r"(r[71]),
+          "=r"(r[72]), "=r"(r[73]), "=r"(r[74]), "=r"(r[75]), "=r"(r[76]), "=r"(r[77]), "=r"(r[78]), "=r"(r[79]),
+          "=r"(r[80]), "=r"(r[81]), "=r"(r[82]), "=r"(r[83]), "=r"(r[84]), "=r"(r[85]), "=r"(r[86]), "=r"(r[87]),
+          "=r"(r[88]), "=r"(r[89]), "=r"(r[90]), "=r"(r[91]), "=r"(r[92]), "=r"(r[93]), "=r"(r[94]), "=r"(r[95]),
+          "=r"(r[96]), "=r"(r[97]), "=r"(r[98]), "=r"(r[99]), "=r"(r[100]), "=r"(r[101]), "=r"(r[102]), "=r"(r[103]),
+          "=r"(r[104]), "=r"(r[105]), "=r"(r[106]), "=r"(r[107]), "=r"(r[108]), "=r"(r[109]), "=r"(r[110]), "=r"(r[111]),
+          "=r"(r[112]), "=r"(r[113]), "=r"(r[114]), "=r"(r[115]), "=r"(r[116]), "=r"(r[117]), "=r"(r[118]), "=r"(r[119]),
+          "=r"(r[120]), "=r"(r[121]), "=r"(r[122]), "=r"(r[123]), "=r"(r[124]), "=r"(r[125]), "=r"(r[126]), "=r"(r[127])
+        : "r"(addr), "r"(addr + 64)
         : "memory");
 }
 
@@ -165,40 +276,61 @@ __device__ __forceinline__ float2 mul2(float2 a, float2 b) {
     return r;
 }
 
+// NaN if any is
 __device__ __forceinline__ float max3(float a, float b, float c) {
     float r;
-    asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+    asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
     return r;
+}
+
+// 2^x for two x of 2^7 at most, on the multiply-add pipe: x = n + f, n the nearest integer (read off the low bits of 1.5 2^23 + x), 2^f
+// a polynomial of degree 5, its coefficients from an exchange algorithm for the least relative error on [-1/2, 1/2]: 2.2e-7 in
+// binary32, as much as the special function unit's.  Below 2^-126 it stops there; NaN is lost.
+__device__ __forceinline__ float2 exp2_poly(float2 x) {
+    const float2 magic = make_float2(12582912.0f, 12582912.0f);
+    x.x = fmaxf(x.x, -126.0f);
+    x.y = fmaxf(x.y, -126.0f);
+    const float2 r = add2(x, magic), f = add2(x, fma2(r, make_float2(-1.0f, -1.0f), magic));
+    auto twice = [](float v) { return make_float2(v, v); };
+    float2 p = fma2(f, twice(0.0013276472454890609f), twice(0.009675540961325169f));
+    p = fma2(p, f, twice(0.05550713092088699f));
+    p = fma2(p, f, twice(0.24022120237350464f));
+    p = fma2(p, f, twice(0.6931469440460205f));
+    p = fma2(p, f, twice(1.0000001192092896f));
+    return make_float2(__uint_as_float(__float_as_uint(p.x) + (__float_as_uint(r.x) << 23)),
+                       __uint_as_float(__float_as_uint(p.y) + (__float_as_uint(r.y) << 23)));
 }
 
 // ---------------------------------------------------------------- results
 // COLS columns of a row a thread (binary32, in tensor memory at `addr`), times `factor`, as bf16 rows of a head: through
-// shared memory (`stage`, 32 x 2 COLS bytes, this warp's own), so that whole rows leave together.  row0: the warp's first row,
-// of which `rows` are there (may be negative); col0: the first column, of `dim`.
+// shared memory (`stage`, 32 x 64 bytes, this warp's own), 32 columns at a time, so that 64 bytes of a row leave together.  row0: the
+// warp's first row, of which `rows` are there (may be negative); col0: the first column, of `dim`.
+constexpr uint32_t kStage = 2048;
+
 template <int COLS>
 __device__ __forceinline__ void give_rows(uint32_t addr, float factor, uint8_t* stage, const Rows& to, int64_t row0, int rows, int head, int col0,
                                           int dim, int lane) {
-    constexpr int kUnits = COLS / 8, kMix = kUnits < 8 ? kUnits - 1 : 7;
+    const int unit = lane % 4;
+    __nv_bfloat16* out = to.p + row0 * to.rs + head * to.hs + col0 + unit * 8;
 #pragma unroll
     for (int c = 0; c < COLS; c += 32) {
         float v[32];
         tc::tmem_load32(addr + c, v);
+        __syncwarp();                      // what was there has left
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const uint4 w = make_uint4(pack_bf16(v[8 * i] * factor, v[8 * i + 1] * factor), pack_bf16(v[8 * i + 2] * factor, v[8 * i + 3] * factor),
                                        pack_bf16(v[8 * i + 4] * factor, v[8 * i + 5] * factor), pack_bf16(v[8 * i + 6] * factor, v[8 * i + 7] * factor));
-            *reinterpret_cast<uint4*>(stage + lane * (COLS * 2) + (((c / 8 + i) ^ (lane & kMix)) * 16)) = w;
+            *reinterpret_cast<uint4*>(stage + lane * 64 + ((i ^ (lane / 2 % 4)) * 16)) = w;
+        }
+        __syncwarp();
+        if (col0 + c + unit * 8 >= dim) continue;
+#pragma unroll
+        for (int r = lane / 4; r < 32; r += 8) {
+            if (r < rows) *reinterpret_cast<uint4*>(out + r * to.rs + c) = *reinterpret_cast<const uint4*>(stage + r * 64 + ((unit ^ (r / 2 % 4)) * 16));
         }
     }
     __syncwarp();
-    const int unit = lane % kUnits;
-    if (col0 + unit * 8 >= dim) return;
-#pragma unroll 4
-    for (int r = lane / kUnits; r < rows; r += 32 / kUnits) {
-        if (r >= 32) break;
-        const uint4 w = *reinterpret_cast<const uint4*>(stage + r * (COLS * 2) + ((unit ^ (r & kMix)) * 16));
-        *reinterpret_cast<uint4*>(to.p + (row0 + r) * to.rs + head * to.hs + col0 + unit * 8) = w;
-    }
 }
 
 // ---------------------------------------------------------------- host side (attention_plan.cu)

@@ -29,8 +29,8 @@ struct Backward {
 constexpr int kThreads = 320;              // eight warps of arithmetic, a copying and an issuing warp
 
 // The eight warps: lanes of tensor memory go by warp % 4, so two warps have the same rows, each 64 columns.  What a warp leaves
-// there as an operand (64 bf16, 32 columns) goes over the first of the columns that it has read itself.
-__device__ __forceinline__ uint32_t operand_column(int k16) { return (k16 >> 2) * 64 + (k16 & 3) * 8; }
+// there as an operand (64 bf16, 32 columns) goes over the first of the columns that it has read itself, which leaves a gap of 32
+// between the operand's halves.
 
 struct Finish {                            // the end of every kernel: see product_kernel
     __device__ static void end(bool fine, volatile uint32_t* slot_mem, unsigned int* mark, uint32_t tmem, int warp) {
@@ -76,7 +76,8 @@ __global__ void __launch_bounds__(kThreads, 1) query_gradient_kernel(const __gri
     tc::let_next_start();
     if (w.plan.table != nullptr) tc::wait_for_previous();
     const int head = static_cast<int>(blockIdx.x) % w.heads;
-    const Piece piece = piece_of(w.plan, static_cast<int>(blockIdx.x) / w.heads);
+    const Piece found = piece_of(w.plan, static_cast<int>(blockIdx.x) / w.heads);
+    const Piece piece{same(found.start), same(found.length), same(found.tile)};
     if (piece.length < 0) return;
     if (threadIdx.x == 0) {
         for (int i = 0; i < S::kKeys; ++i) {
@@ -105,7 +106,7 @@ __global__ void __launch_bounds__(kThreads, 1) query_gradient_kernel(const __gri
     tc::fence_before();
     __syncthreads();
     tc::fence_after();
-    const uint32_t tmem = *slot_mem, products_at = tmem + 256, dq_at = tmem + 384;
+    const uint32_t tmem = same(*slot_mem), products_at = tmem + 256, dq_at = tmem + 384;
     const int row0 = piece.tile * kTile;
     const int key_tiles = (piece.length + kTile - 1) / kTile;
     const int n = w.causal ? min(key_tiles, piece.tile + 1) : key_tiles;              // tiles of keys, from the last to the first
@@ -143,16 +144,9 @@ __global__ void __launch_bounds__(kThreads, 1) query_gradient_kernel(const __gri
         }
     } else if (warp == 9) {
         const int k_steps = (w.dim + 15) / 16;
-        const uint32_t square = tc::instruction(kTile, kTile, 0, 0), wide = tc::instruction(kTile, k_steps * 16, 0, 1);
+        const uint32_t wide = tc::instruction(kTile, k_steps * 16, 0, 1);
         auto finished = [&](uint32_t bar) {
             if (tc::elected()) tc::commit<1>(bar);
-            __syncwarp();
-        };
-        auto against = [&](uint32_t d, uint32_t a_tile, uint32_t b_tile) {            // rows of both, along the head's columns
-            if (tc::elected()) {
-                const uint64_t a = along_row(a_tile), b = along_row(b_tile);
-                for (int s = 0; s < k_steps; ++s) tc::mma<1>(d, a + row_step(s), b + row_step(s), square, s > 0 ? 1u : 0u);
-            }
             __syncwarp();
         };
         fine = tc::bar_wait(rows_full, 0);
@@ -161,12 +155,12 @@ __global__ void __launch_bounds__(kThreads, 1) query_gradient_kernel(const __gri
             if (i < n) {
                 if (!(fine = tc::bar_wait(k_full + 8 * (i % S::kKeys), (i / S::kKeys) & 1))) break;
                 tc::fence_after();
-                against(tmem + (i & 1) * kTile, base, keys + (i % S::kKeys) * S::kBytes);
+                rows_by_rows<D>(tmem + (i & 1) * kTile, base, keys + (i % S::kKeys) * S::kBytes, k_steps);
                 finished(scores + 8 * (i & 1));
                 if (!(fine = tc::bar_wait(v_full + 8 * (i % S::kValues), (i / S::kValues) & 1))) break;
                 if (i > 0 && !(fine = tc::bar_wait(taken, (i - 1) & 1))) break;
                 tc::fence_after();
-                against(products_at, base + S::kBytes, values + (i % S::kValues) * S::kBytes);
+                rows_by_rows<D>(products_at, base + S::kBytes, values + (i % S::kValues) * S::kBytes, k_steps);
                 finished(products);
                 finished(v_empty + 8 * (i % S::kValues));
             }
@@ -174,14 +168,8 @@ __global__ void __launch_bounds__(kThreads, 1) query_gradient_kernel(const __gri
                 const int b = i - 1;
                 if (!(fine = tc::bar_wait(slopes, b & 1))) break;
                 tc::fence_after();
-                if (tc::elected()) {
-                    const uint64_t at = along_column(keys + (b % S::kKeys) * S::kBytes);
-                    const int steps = (min(kTile, piece.length - (n - 1 - b) * kTile) + 15) / 16;
-                    for (int s = 0; s < steps; ++s) {
-                        mma_tmem(dq_at, tmem + (b & 1) * kTile + operand_column(s), at + column_step(s), wide, (s > 0 || b > 0) ? 1u : 0u);
-                    }
-                }
-                __syncwarp();
+                weights_by_rows<0, 8, 32>(dq_at, tmem + (b & 1) * kTile, keys + (b % S::kKeys) * S::kBytes, wide,
+                                          (min(kTile, piece.length - (n - 1 - b) * kTile) + 15) / 16, b > 0);
                 finished(k_empty + 8 * (b % S::kKeys));
             }
         }
@@ -299,7 +287,8 @@ __global__ void __launch_bounds__(kKeyThreads, 1) key_gradient_kernel(const __gr
     tc::let_next_start();
     if (w.plan.table != nullptr) tc::wait_for_previous();
     const int kv_head = static_cast<int>(blockIdx.x) % w.kv_heads;
-    const Piece piece = piece_of(w.plan, static_cast<int>(blockIdx.x) / w.kv_heads);
+    const Piece found = piece_of(w.plan, static_cast<int>(blockIdx.x) / w.kv_heads);
+    const Piece piece{same(found.start), same(found.length), same(found.tile)};
     if (piece.length < 0) return;
     if (threadIdx.x == 0) {
         for (int i = 0; i < kStages; ++i) {
@@ -327,7 +316,7 @@ __global__ void __launch_bounds__(kKeyThreads, 1) key_gradient_kernel(const __gr
     tc::fence_before();
     __syncthreads();
     tc::fence_after();
-    const uint32_t tmem = *slot_mem, products_at = tmem + 128, dk_at = tmem + 256, dv_at = tmem + 256 + D;
+    const uint32_t tmem = same(*slot_mem), products_at = tmem + 128, dk_at = tmem + 256, dv_at = tmem + 256 + D;
     const int key0 = piece.tile * kTile;
     const int tiles = (piece.length + kTile - 1) / kTile, first = w.causal ? piece.tile : 0;
     const int per = tiles - first, n = per * w.group;                // tiles of queries, of each head that shares these keys
@@ -392,25 +381,13 @@ __global__ void __launch_bounds__(kKeyThreads, 1) key_gradient_kernel(const __gr
         }
     } else if (warp == 9) {
         const int k_steps = (w.dim + 15) / 16;
-        const uint32_t square = tc::instruction(kTile, kTile, 0, 0), wide = tc::instruction(kTile, k_steps * 16, 0, 1);
+        const uint32_t wide = tc::instruction(kTile, k_steps * 16, 0, 1);
         auto finished = [&](uint32_t bar) {
             if (tc::elected()) tc::commit<1>(bar);
             __syncwarp();
         };
-        auto against = [&](uint32_t d, uint32_t a_tile, uint32_t b_tile) {
-            if (tc::elected()) {
-                const uint64_t a = along_row(a_tile), b = along_row(b_tile);
-                for (int s = 0; s < k_steps; ++s) tc::mma<1>(d, a + row_step(s), b + row_step(s), square, s > 0 ? 1u : 0u);
-            }
-            __syncwarp();
-        };
         auto onto = [&](uint32_t d, uint32_t a, uint32_t b_tile, int i) {             // the rows of the queries' tile i
-            if (tc::elected()) {
-                const uint64_t b = along_column(b_tile);
-                const int steps = (min(kTile, piece.length - (first + i % per) * kTile) + 15) / 16;
-                for (int s = 0; s < steps; ++s) mma_tmem(d, a + operand_column(s), b + column_step(s), wide, (s > 0 || i > 0) ? 1u : 0u);
-            }
-            __syncwarp();
+            weights_by_rows<0, 8, 32>(d, a, b_tile, wide, (min(kTile, piece.length - (first + i % per) * kTile) + 15) / 16, i > 0);
         };
         fine = tc::bar_wait(rows_full, 0);
         // round i: dv of tile i - 1, scores of tile i over its weights; dk of tile i - 1, dp of tile i over its slopes
@@ -426,7 +403,7 @@ __global__ void __launch_bounds__(kKeyThreads, 1) key_gradient_kernel(const __gr
             if (i < n) {
                 if (!(fine = tc::bar_wait(q_full + 8 * st, parity))) break;
                 tc::fence_after();
-                against(tmem, base, queries + st * S::kBytes);
+                rows_by_rows<D>(tmem, base, queries + st * S::kBytes, k_steps);
                 finished(scores);
             }
             if (i > 0) {
@@ -438,7 +415,7 @@ __global__ void __launch_bounds__(kKeyThreads, 1) key_gradient_kernel(const __gr
             if (i < n) {
                 if (!(fine = tc::bar_wait(d_full + 8 * st, parity))) break;
                 tc::fence_after();
-                against(products_at, base + S::kBytes, douts + st * S::kBytes);
+                rows_by_rows<D>(products_at, base + S::kBytes, douts + st * S::kBytes, k_steps);
                 finished(products);
             }
         }
@@ -548,7 +525,7 @@ dlion_status check(const dlion_attention_bwd* p) {
     }
     if (p->rows > 0 && p->lse == nullptr) return DLION_EINVAL;
     if (!aligned(p->lse, 4)) return DLION_EALIGN;
-    return most_pieces(sequences_of(*p), kTile) * p->heads <= INT_MAX ? DLION_OK : DLION_EINVAL;
+    return most_pieces(sequences_of(*p), kTile) * p->heads <= INT_MAX / 2 ? DLION_OK : DLION_EINVAL;
 }
 
 template <int D>

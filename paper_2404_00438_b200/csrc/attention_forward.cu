@@ -11,53 +11,59 @@ namespace att {
 
 namespace {
 
+constexpr int64_t kLongSequence = 1024;
+
 struct Forward {
     CUtensorMap q, k, v;
     Plan plan;
-    int heads, group, dim, causal;
+    int units, heads, group, dim, causal;
     float c;                               // scale * log2(e)
     Rows out;
     float* lse;
     int64_t lse_ld;
 };
 
-constexpr int kForwardThreads = 320;       // two groups of four warps with a tile of queries each, a copying and an issuing warp
-constexpr int kForwardRows = 2 * kTile;
-
-template <int D>
+// SIDES tiles of queries share each tile of keys and values that a block copies.  Every side has a group of four warps, a row a
+// thread; one warp copies and one issues the products.  With two sides one's exponentials run while the tensor cores work for the
+// other; with one, two blocks an SM do that for each other.
+template <int D, int SIDES>
 struct ForwardShared {
     static constexpr uint32_t kBytes = kTile * D * 2;                // of a tile
-    static constexpr int kRing = D == 128 ? 4 : 8;                   // tiles of keys and values, in turn
-    static constexpr uint32_t kBars = (2 + kRing) * kBytes;
+    static constexpr int kRing = D == 128 && SIDES == 1 ? 2 : 4;     // tiles of keys and values, in turn
+    static constexpr uint32_t kStages = (SIDES + kRing) * kBytes;
+    static constexpr uint32_t kBars = kStages + 4 * SIDES * kStage;
     static constexpr uint32_t kAll = kBars + 256 + 1024;
+    static constexpr int kThreads = 128 * SIDES + 64;
+    static constexpr uint32_t kColumns = SIDES == 2 ? 512 : 256;     // of tensor memory: scores, outputs, weights
+    static constexpr bool kApart = SIDES * (kTile + D + kTile / 2) <= kColumns;       // otherwise weights lie over the scores
 };
 
-template <int D>
-__global__ void __launch_bounds__(kForwardThreads, 1) attend_kernel(const __grid_constant__ Forward w, unsigned int* mark) {
-    using S = ForwardShared<D>;
-    constexpr int kRing = S::kRing;
+template <int D, int SIDES>
+__global__ void __launch_bounds__(ForwardShared<D, SIDES>::kThreads, 3 - SIDES) attend_kernel(const __grid_constant__ Forward w, unsigned int* mark) {
+    using S = ForwardShared<D, SIDES>;
+    constexpr int kRing = S::kRing, kCopying = 4 * SIDES, kIssuing = kCopying + 1;    // warps: SIDES groups of four, and one each
     extern __shared__ uint8_t raw[];
     const uint32_t base = (tc::smem_addr(raw) + 1023u) & ~1023u;
     uint8_t* mem = raw + (base - tc::smem_addr(raw));
-    const uint32_t ring = base + 2 * S::kBytes, bars = base + S::kBars;
-    const uint32_t full = bars, empty = bars + 64, q_full = bars + 128, scores = bars + 144, weights = bars + 160, done = bars + 176, slot = bars + 192;
+    const uint32_t ring = base + SIDES * S::kBytes, bars = base + S::kBars;
+    const uint32_t full = bars, empty = bars + 64, q_full = bars + 128, scores = bars + 144, weights = bars + 160, done = bars + 192,
+                   taken = bars + 208, q_empty = bars + 216, slot = bars + 240;
     volatile uint32_t* slot_mem = reinterpret_cast<volatile uint32_t*>(mem + (slot - base));
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
 
     tc::let_next_start();
-    if (w.plan.table != nullptr) tc::wait_for_previous();            // the table is the kernel's before
-    const int head = static_cast<int>(blockIdx.x) % w.heads;
-    const Piece piece = piece_of(w.plan, static_cast<int>(blockIdx.x) / w.heads);
-    if (piece.length < 0) return;
     if (threadIdx.x == 0) {
         for (int i = 0; i < kRing; ++i) {
             tc::bar_init(full + 8 * i, 1);
             tc::bar_init(empty + 8 * i, 1);
         }
-        for (int i = 0; i < 2; ++i) {
+        tc::bar_init(taken, 4);
+        for (int i = 0; i < SIDES; ++i) {
             tc::bar_init(q_full + 8 * i, 1);
+            tc::bar_init(q_empty + 8 * i, 1);
             tc::bar_init(scores + 8 * i, 1);
-            tc::bar_init(weights + 8 * i, 4);
+            tc::bar_init(weights + 16 * i, 4);                       // the first half's and the second's
+            tc::bar_init(weights + 16 * i + 8, 4);
             tc::bar_init(done + 8 * i, 1);
         }
         tc::bar_init_done();
@@ -66,180 +72,250 @@ __global__ void __launch_bounds__(kForwardThreads, 1) attend_kernel(const __grid
         tc::prefetch_map(&w.k);
         tc::prefetch_map(&w.v);
     }
-    if (warp == 9) tc::tmem_alloc<1>(slot, 512);
+    if (warp == kIssuing) tc::tmem_alloc<1>(slot, S::kColumns);
     tc::fence_before();
     __syncthreads();
     tc::fence_after();
-    const uint32_t tmem = *slot_mem;
-    const int row0 = piece.tile * kForwardRows;                      // in the sequence
-    const int sides = piece.length - row0 > kTile ? 2 : 1;           // tiles of queries
-    const int key_tiles = (piece.length + kTile - 1) / kTile;
-    // tiles of keys of each side, taken from the last to the first
-    const int n0 = w.causal ? min(key_tiles, 2 * piece.tile + 1) : key_tiles;
-    const int n1 = sides == 2 ? (w.causal ? min(key_tiles, 2 * piece.tile + 2) : key_tiles) : 0;
-    const int most = max(n0, n1);
-    const int kv_head = head / w.group;
+    const uint32_t tmem = same(*slot_mem);
     bool fine = true;
-    if (w.plan.table == nullptr) tc::wait_for_previous();
+    tc::wait_for_previous();
 
-    if (warp == 8) {
-        if (tc::elected()) {
-            for (int i = 0; i < sides; ++i) {
-                tc::bar_expect(q_full + 8 * i, S::kBytes);
-                load_head<D>(base + i * S::kBytes, &w.q, head, piece.start + row0 + i * kTile, q_full + 8 * i);
-            }
-        }
-        __syncwarp();
-        int st = 0, filled = 0;
-        uint32_t phase = 1;
-        for (int j = most - 1; j >= 0 && fine; --j) {
-            for (int kind = 0; kind < 2; ++kind, ++filled) {
-                if (!(fine = tc::bar_wait(empty + 8 * st, phase))) break;
-                if (tc::elected()) {
-                    tc::bar_expect(full + 8 * st, S::kBytes);
-                    load_head<D>(ring + st * S::kBytes, kind ? &w.v : &w.k, kv_head, piece.start + j * kTile, full + 8 * st);
-                }
-                __syncwarp();
-                if (++st == kRing) {
-                    st = 0;
-                    phase ^= 1;
+    Pieces pieces(w.plan, w.heads, w.units);
+    Piece piece{};
+    int head = 0;
+    // What a piece is made of: tiles of queries (sides) and each side's tiles of keys, taken from the last to the first
+    int row0 = 0, n0 = 0, n1 = 0, most = 0;
+    auto divide = [&] {
+        row0 = piece.tile * SIDES * kTile;
+        const int key_tiles = (piece.length + kTile - 1) / kTile;
+        n0 = w.causal ? min(key_tiles, SIDES * piece.tile + 1) : key_tiles;
+        n1 = SIDES == 2 && piece.length - row0 > kTile ? (w.causal ? min(key_tiles, SIDES * piece.tile + 2) : key_tiles) : 0;
+        most = max(n0, n1);
+    };
+
+    if (warp == kCopying) {
+        int filled = 0, queries = 0, others = 0;                     // tiles asked for: into the ring, of either side
+        while (fine && pieces.take(piece, head)) {
+            divide();
+            const int kv_head = head / w.group;
+            for (int r = 0; r < most && fine; ++r) {
+                const int row = piece.start + (most - 1 - r) * kTile;
+                for (int kind = 0; kind < 2; ++kind, ++filled) {
+                    const int st = filled % kRing;
+                    if (!(fine = tc::bar_wait(empty + 8 * st, ((filled / kRing) & 1) ^ 1))) break;
+                    if (tc::elected()) {
+                        tc::bar_expect(full + 8 * st, S::kBytes);
+                        load_head<D>(ring + st * S::kBytes, kind ? &w.v : &w.k, kv_head, row, full + 8 * st);
+                    }
+                    __syncwarp();
+                    if (r > 0 || kind > 0) continue;
+                    for (int side = 0; side < (n1 > 0 ? 2 : 1); ++side) {             // behind the first keys
+                        int& count = side ? others : queries;
+                        if (!(fine = tc::bar_wait(q_empty + 8 * side, (count & 1) ^ 1))) break;
+                        if (tc::elected()) {
+                            tc::bar_expect(q_full + 8 * side, S::kBytes);
+                            load_head<D>(base + side * S::kBytes, &w.q, head, piece.start + row0 + side * kTile, q_full + 8 * side);
+                        }
+                        __syncwarp();
+                        ++count;
+                    }
+                    if (!fine) {
+                        ++filled;
+                        break;
+                    }
                 }
             }
         }
         if (!fine) {                       // what was asked for still lands in this block's memory: it is awaited
-            for (int i = 0; i < sides; ++i) tc::bar_wait(q_full + 8 * i, 0);
+            if (queries > 0) tc::bar_wait(q_full, (queries - 1) & 1);
+            if (others > 0) tc::bar_wait(q_full + 8, (others - 1) & 1);
             for (int i = max(0, filled - kRing); i < filled; ++i) tc::bar_wait(full + 8 * (i % kRing), (i / kRing) & 1);
         }
-    } else if (warp == 9) {
+    } else if (warp == kIssuing) {
         const int k_steps = (w.dim + 15) / 16;
-        const uint32_t score_inst = tc::instruction(kTile, kTile, 0, 0), out_inst = tc::instruction(kTile, k_steps * 16, 0, 1);
+        const uint32_t out_inst = tc::instruction(kTile, k_steps * 16, 0, 1);
         auto finished = [&](uint32_t bar) {
             if (tc::elected()) tc::commit<1>(bar);
             __syncwarp();
         };
         auto filled = [&](int i) { return tc::bar_wait(full + 8 * (i % kRing), (i / kRing) & 1); };
-        // round r: the weighted values of round r - 1 and the scores of round r, first for one side, then for the other, so that
-        // one side's products run while the other's exponentials do
-        for (int r = 0; r <= most && fine; ++r) {
-            const int j = most - 1 - r;    // tile of keys of this round
-            bool have_k = false, have_v = false;
-            for (int side = 0; side < sides && fine; ++side) {
-                const int n = side ? n1 : n0;
-                if (r > 0 && j + 1 < n) {
-                    const int before = 2 * (r - 1) + 1;              // the values' place in the ring's order
-                    if (!have_v && !(fine = filled(before))) break;
-                    have_v = true;
-                    if (!(fine = tc::bar_wait(weights + 8 * side, (n - 2 - j) & 1))) break;
-                    tc::fence_after();
-                    if (tc::elected()) {
-                        const uint64_t b = along_column(ring + (before % kRing) * S::kBytes);
-                        const uint32_t a = tmem + side * kTile, d = tmem + 2 * kTile + side * D;
-                        const int steps = (min(kTile, piece.length - (j + 1) * kTile) + 15) / 16;
-                        for (int i = 0; i < steps; ++i) mma_tmem(d, a + 8 * i, b + column_step(i), out_inst, (i > 0 || j + 1 < n - 1) ? 1u : 0u);
+        int round = 0;                     // of all pieces: its keys and values are the ring's 2 round and 2 round + 1
+        int scored[2] = {}, weighed[2] = {}, begun[2] = {};          // tiles of each side; pieces
+        // What is left of the last round: the weighted values
+        bool waiting[2] = {}, first[2] = {};
+        int steps = 0;
+        bool last = false;
+        auto gather = [&](int side) {
+            const uint32_t values = ring + ((2 * round - 1) % kRing) * S::kBytes, p_at = S::kApart ? tmem + kTile + D : tmem + side * kTile,
+                           o_at = tmem + SIDES * kTile + side * D;
+            if (!(fine = tc::bar_wait(weights + 16 * side, weighed[side] & 1))) return;
+            tc::fence_after();
+            weights_by_rows<0, 4, 0>(o_at, p_at, values, out_inst, steps, !first[side]);
+            if (!(fine = tc::bar_wait(weights + 16 * side + 8, weighed[side] & 1))) return;
+            tc::fence_after();
+            weights_by_rows<4, 8, 0>(o_at, p_at, values, out_inst, steps, true);
+            ++weighed[side];
+            if (S::kApart || last) finished(done + 8 * side);
+        };
+        auto score = [&](int side, int r) {
+            const int n = side ? n1 : n0;
+            if (r == most - n && !(fine = tc::bar_wait(q_full + 8 * side, begun[side] & 1))) return;
+            if (S::kApart && scored[side] > 0 && !(fine = tc::bar_wait(taken, (scored[side] - 1) & 1))) return;
+            tc::fence_after();
+            rows_by_rows<D>(tmem + side * kTile, base + side * S::kBytes, ring + (2 * round % kRing) * S::kBytes, k_steps);
+            ++scored[side];
+            finished(scores + 8 * side);
+            if (r == most - 1) {
+                ++begun[side];
+                finished(q_empty + 8 * side);
+            }
+        };
+        auto release = [&] {               // the last round's values
+            if (round > 0) finished(empty + 8 * ((2 * round - 1) % kRing));
+        };
+        // A round: the scores of a tile of keys, and the weighted values of the round before it.  Where weights lie over the scores
+        // these come first, and one side after the other, so that a side's products run while the other's exponentials do
+        // (with a warp to issue each side's, both sides' came to run and to wait together: a quarter slower).
+        while (fine && pieces.take(piece, head)) {
+            divide();
+            for (int r = 0; r < most && fine; ++r, ++round) {
+                if (round > 0 && !(fine = filled(2 * round - 1))) break;
+                if (!(fine = filled(2 * round))) break;
+                if (S::kApart) {
+                    score(0, r);
+                    if (fine && waiting[0]) gather(0);
+                } else {
+#pragma unroll
+                    for (int side = 0; side < SIDES; ++side) {
+                        if (fine && waiting[side]) gather(side);
+                        if (fine && r >= most - (side ? n1 : n0)) score(side, r);
                     }
-                    __syncwarp();
-                    if (j < 0) finished(done + 8 * side);
                 }
-                if (j >= 0 && j < n) {
-                    if (!have_k && !(fine = filled(2 * r))) break;
-                    have_k = true;
-                    if (r == most - n && !(fine = tc::bar_wait(q_full + 8 * side, 0))) break;
-                    tc::fence_after();
-                    if (tc::elected()) {
-                        const uint64_t a = along_row(base + side * S::kBytes), b = along_row(ring + (2 * r % kRing) * S::kBytes);
-                        for (int i = 0; i < k_steps; ++i) tc::mma<1>(tmem + side * kTile, a + row_step(i), b + row_step(i), score_inst, i > 0 ? 1u : 0u);
-                    }
-                    __syncwarp();
-                    finished(scores + 8 * side);
+                if (!fine) break;
+                release();
+                finished(empty + 8 * (2 * round % kRing));
+                steps = (min(kTile, piece.length - (most - 1 - r) * kTile) + 15) / 16;
+                last = r == most - 1;
+#pragma unroll
+                for (int side = 0; side < SIDES; ++side) {
+                    const int n = side ? n1 : n0;
+                    waiting[side] = r >= most - n;
+                    first[side] = r == most - n;
                 }
             }
-            if (!fine) break;
-            if (r > 0) finished(empty + 8 * ((2 * r - 1) % kRing));
-            if (j >= 0) finished(empty + 8 * (2 * r % kRing));
+        }
+        if (fine && round > 0 && (fine = filled(2 * round - 1))) {
+#pragma unroll
+            for (int side = 0; side < SIDES; ++side) {
+                if (fine && waiting[side]) gather(side);
+            }
         }
     } else {
         const int side = warp / 4, quarter = warp % 4;
-        const int n = side ? n1 : n0;
-        const int row = row0 + side * kTile + quarter * 32 + lane;                    // in the sequence
         const uint32_t lanes = static_cast<uint32_t>(quarter * 32) << 16;
-        const uint32_t s_at = tmem + side * kTile + lanes, o_at = tmem + 2 * kTile + side * D + lanes;
+        const uint32_t s_at = tmem + side * kTile + lanes, o_at = tmem + SIDES * kTile + side * D + lanes;
+        const uint32_t p_at = S::kApart ? tmem + kTile + D + lanes : s_at;
         const float c = w.c;
-        float m = -INFINITY, mc = 0.0f;    // the row's reference, and c times it
-        float2 l = make_float2(0.0f, 0.0f);
-        for (int r = 0; r < n; ++r) {
-            const int j = n - 1 - r;
-            if (!(fine = tc::bar_wait(scores + 8 * side, r & 1))) break;
-            tc::fence_after();
-            float s[kTile];
-            tmem_load64(s_at, *reinterpret_cast<float(*)[64]>(s));
-            tmem_load64(s_at + 64, *reinterpret_cast<float(*)[64]>(s + 64));
-            const int valid = piece.length - j * kTile;              // keys of the tile that are the sequence's
-            if (valid < kTile || (w.causal && (j + 1) * kTile > row0 + side * kTile)) {
-                const int last = (w.causal ? min(row, piece.length - 1) : piece.length - 1) - j * kTile;
+        int round = 0, scored = 0, ended = 0;                        // rounds of all pieces; this side's tiles; its pieces
+        while (fine && pieces.take(piece, head)) {
+            divide();
+            const int n = side ? n1 : n0;
+            const int row = row0 + side * kTile + quarter * 32 + lane;                // in the sequence
+            float m = -INFINITY, mc = 0.0f;                          // the row's reference, and c times it
+            float2 l = make_float2(0.0f, 0.0f);
+            for (int r = 0; r < n; ++r, ++scored) {
+                const int j = n - 1 - r;
+                if (!(fine = tc::bar_wait(scores + 8 * side, scored & 1))) break;
+                tc::fence_after();
+                float s[kTile];
+                tmem_load128(s_at, s);
+                if (S::kApart) {
+                    tc::fence_before();
+                    __syncwarp();
+                    if (lane == 0) tc::bar_arrive(taken);
+                }
+                const int valid = piece.length - j * kTile;          // keys of the tile that are the sequence's
+                if (valid < kTile || (w.causal && (j + 1) * kTile > row0 + side * kTile)) {
+                    const int behind = (w.causal ? min(row, piece.length - 1) : piece.length - 1) - j * kTile;
 #pragma unroll
-                for (int i = 0; i < kTile; ++i) s[i] = i <= last ? s[i] : -INFINITY;
-            }
-            float top = max3(s[0], s[1], s[2]), top1 = s[3];
+                    for (int i = 0; i < kTile; ++i) s[i] = i <= behind ? s[i] : -INFINITY;
+                }
+                float top4[4] = {s[0], s[1], s[2], s[3]};
 #pragma unroll
-            for (int i = 4; i < kTile; i += 4) {
-                top = max3(top, s[i], s[i + 1]);
-                top1 = max3(top1, s[i + 2], s[i + 3]);
-            }
-            top = fmaxf(top, top1);
-            // The reference follows the maximum only where weights would exceed 2^8: bf16 and binary32 hold them as exactly, and
-            // the output is seldom taken out and put back.
-            const bool grows = r == 0 ? top > -INFINITY : !(m > -INFINITY ? (top - m) * c <= 8.0f : top == -INFINITY);
-            if (__any_sync(0xffffffffu, grows)) {
-                const float to = grows ? top : m, to_c = to > -INFINITY ? to * c : 0.0f;
-                if (r > 0) {
-                    const float f = grows ? (m > -INFINITY ? exp2_fast(mc - to_c) : 0.0f) : 1.0f;
-                    l = mul2(l, make_float2(f, f));
+                for (int i = 4; i < kTile; i += 8) {
 #pragma unroll
-                    for (int i = 0; i < D; i += 32) {
-                        float o[32];
-                        tc::tmem_load32(o_at + i, o);
-#pragma unroll
-                        for (int e = 0; e < 32; ++e) o[e] *= f;
-                        tmem_store_f32(o_at + i, o);
+                    for (int e = 0; e < 4; ++e) {
+                        if (i + 2 * e + 1 < kTile) top4[e] = max3(top4[e], s[i + 2 * e], s[i + 2 * e + 1]);
                     }
                 }
-                m = to;
-                mc = to_c;
-            }
-            const float2 cc = make_float2(c, c), minus = make_float2(-mc, -mc);
+                const float top = max3(max3(top4[0], top4[1], top4[2]), top4[3], top4[3]);
+                // The reference follows the maximum only where weights would exceed 2^8: bf16 and binary32 hold them as exactly, and
+                // the output is seldom taken out and put back.  It is -infinity as long as all scores are; a score that is NaN or
+                // +infinity makes c times it, and so all of the row's weights, NaN.
+                const bool grows = m > -INFINITY ? !((top - m) * c <= 8.0f) : !(top == -INFINITY);
+                const bool any = __any_sync(0xffffffffu, grows);
+                // weights' columns of their own: the last ones have been used, and so is the output at rest
+                auto used = [&] { return !S::kApart || scored == 0 || tc::bar_wait(done, (scored - 1) & 1); };
+                if (any) {
+                    const float to = grows ? top : m, to_c = to == -INFINITY ? 0.0f : (to - to) + to * c;
+                    if (r > 0) {
+                        fine = used();
+                        if (!fine) break;
+                        tc::fence_after();
+                        const float f = grows ? (m == -INFINITY ? 0.0f : exp2_fast(mc - to_c)) : 1.0f;
+                        l = mul2(l, make_float2(f, f));
 #pragma unroll
-            for (int h = 0; h < kTile; h += 64) {
-                uint32_t p[32];
+                        for (int i = 0; i < D; i += 32) {
+                            float o[32];
+                            tc::tmem_load32(o_at + i, o);
 #pragma unroll
-                for (int i = 0; i < 32; ++i) {
-                    float2 e = fma2(make_float2(s[h + 2 * i], s[h + 2 * i + 1]), cc, minus);
-                    e.x = exp2_fast(e.x);
-                    e.y = exp2_fast(e.y);
-                    l = add2(l, e);
-                    p[i] = pack_bf16(e.x, e.y);
+                            for (int e = 0; e < 32; ++e) o[e] *= f;
+                            tmem_store_f32(o_at + i, o);
+                        }
+                    }
+                    m = to;
+                    mc = to_c;
                 }
-                tmem_store32(s_at + h / 2, p);
+                if (valid < kTile) {       // the values' rows behind the sequence
+                    const int at = 2 * (round + most - 1 - j) + 1;
+                    if (!(fine = tc::bar_wait(full + 8 * (at % kRing), (at / kRing) & 1))) break;
+                    clear_rows<D>(mem + (ring - base) + (at % kRing) * S::kBytes, valid, threadIdx.x % 128, 128);
+                }
+                const float2 cc = make_float2(c, c), minus = make_float2(-mc, -mc);
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    uint32_t p[32];
+#pragma unroll
+                    for (int i = 0; i < 32; ++i) {
+                        float2 e = fma2(make_float2(s[h * 64 + 2 * i], s[h * 64 + 2 * i + 1]), cc, minus);
+                        e.x = exp2_fast(e.x);
+                        e.y = exp2_fast(e.y);
+                        l = add2(l, e);
+                        p[i] = pack_bf16(e.x, e.y);
+                    }
+                    if (h == 0) {
+                        fine = used();
+                        if (!fine) break;
+                        tc::fence_after();
+                    }
+                    tmem_store32(p_at + 32 * h, p);
+                    tmem_stored();
+                    tc::fence_before();
+                    __syncwarp();
+                    if (lane == 0) tc::bar_arrive(weights + 16 * side + 8 * h);
+                }
+                if (!fine) break;
             }
-            if (valid < kTile) {           // the values' rows behind the sequence
-                const int at = 2 * (most - 1 - j) + 1;
-                if (!(fine = tc::bar_wait(full + 8 * (at % kRing), (at / kRing) & 1))) break;
-                clear_rows<D>(mem + (ring - base) + (at % kRing) * S::kBytes, valid, threadIdx.x % 128, 128);
-            }
-            tmem_stored();
-            tc::fence_before();
-            __syncwarp();
-            if (lane == 0) tc::bar_arrive(weights + 8 * side);
-        }
-        if (n > 0 && fine) fine = tc::bar_wait(done + 8 * side, 0);
-        if (n > 0 && fine) {
+            round += most;
+            if (n == 0 || !fine) continue;
+            if (!(fine = tc::bar_wait(done + 8 * side, (S::kApart ? scored - 1 : ended) & 1))) break;
+            ++ended;
             tc::fence_after();
             const float sum = l.x + l.y;
             const int rows = piece.length - row0 - side * kTile - quarter * 32;
             if (lane < rows) w.lse[head * w.lse_ld + piece.start + row] = (mc + log2f(sum)) * kLn2;
-            const float inverse = 1.0f / sum;
-            // 64 columns at a time, through this side's queries, which have been read
-            uint8_t* stage = mem + side * S::kBytes + quarter * (32 * D * 2);
-            give_rows<D>(o_at, inverse, stage, w.out, piece.start + row - lane, rows, head, 0, w.dim, lane);
+            give_rows<D>(o_at, 1.0f / sum, mem + S::kStages + warp * kStage, w.out, piece.start + row - lane, rows, head, 0, w.dim, lane);
+            tc::fence_before();
         }
     }
     if (!fine) {
@@ -255,7 +331,7 @@ __global__ void __launch_bounds__(kForwardThreads, 1) attend_kernel(const __grid
         }
     }
     tc::fence_after();
-    if (warp == 9) tc::tmem_free<1>(tmem, 512);
+    if (warp == kIssuing) tc::tmem_free<1>(tmem, S::kColumns);
 }
 
 dlion_status check(const dlion_attention_fwd* p) {
@@ -271,13 +347,28 @@ dlion_status check(const dlion_attention_fwd* p) {
     }
     if (p->rows > 0 && p->lse == nullptr) return DLION_EINVAL;
     if (!aligned(p->lse, 4)) return DLION_EALIGN;
-    return most_pieces(Sequences{p->rows, p->length, p->sequences, p->offsets, p->offsets_64}, kForwardRows) * p->heads <= INT_MAX ? DLION_OK : DLION_EINVAL;
+    return most_pieces(Sequences{p->rows, p->length, p->sequences, p->offsets, p->offsets_64}, kTile) * p->heads <= INT_MAX / 2 ? DLION_OK : DLION_EINVAL;
+}
+
+// Two tiles of queries to a block where heads are wide and sequences long on average.
+int sides_of(const dlion_attention_fwd& p) {
+    const int64_t count = p.offsets != nullptr ? p.sequences : p.length == 0 ? 1 : p.rows / p.length;
+    return p.dim > 64 && p.rows >= count * kLongSequence ? 2 : 1;
+}
+
+template <int D, int SIDES>
+void launch(prod::Call& c, Forward& w, int64_t pieces) {
+    using S = ForwardShared<D, SIDES>;
+    w.units = static_cast<int>(pieces * w.heads);
+    prod::raise_shared(c, &attend_kernel<D, SIDES>, S::kAll);
+    prod::start(c, attend_kernel<D, SIDES>, dim3(static_cast<unsigned>(std::min(w.units, (3 - SIDES) * c.sms))), dim3(S::kThreads), S::kAll, 1, w, c.mark);
 }
 
 void forward(prod::Call& c, const dlion_attention_fwd& p) {
     const Sequences seq{p.rows, p.length, p.sequences, p.offsets, p.offsets_64};
-    const int64_t pieces = most_pieces(seq, kForwardRows);
     if (p.rows == 0) return;
+    const int sides = sides_of(p);
+    const int64_t pieces = most_pieces(seq, sides * kTile);
     int4* table = p.offsets != nullptr ? c.ws.take<int4>(pieces) : nullptr;
     if (!c.live()) return;
     Forward w{};
@@ -290,7 +381,7 @@ void forward(prod::Call& c, const dlion_attention_fwd& p) {
         clear.lse = p.lse;
         clear.lse_ld = p.lse_ld;
     }
-    const PlanRequest request{kForwardRows, p.causal, 0};
+    const PlanRequest request{sides * kTile, p.causal, 0};
     make_plans(c, seq, &request, 1, &table, &w.plan, p.zero_rest ? &clear : nullptr);
     if (pieces == 0) return;
     if (!map_rows(&w.q, Operand{p.q, p.q_rs, p.q_hs, p.heads}, p.rows, p.dim) || !map_rows(&w.k, Operand{p.k, p.k_rs, p.k_hs, p.kv_heads}, p.rows, p.dim) ||
@@ -306,13 +397,10 @@ void forward(prod::Call& c, const dlion_attention_fwd& p) {
     w.out = Rows{static_cast<__nv_bfloat16*>(p.out), p.out_rs, p.out_hs};
     w.lse = p.lse;
     w.lse_ld = p.lse_ld;
-    const dim3 grid(static_cast<unsigned>(pieces * p.heads)), block(kForwardThreads);
     if (p.dim <= 64) {
-        prod::raise_shared(c, &attend_kernel<64>, ForwardShared<64>::kAll);
-        prod::start(c, attend_kernel<64>, grid, block, ForwardShared<64>::kAll, 1, w, c.mark);
+        launch<64, 1>(c, w, pieces);
     } else {
-        prod::raise_shared(c, &attend_kernel<128>, ForwardShared<128>::kAll);
-        prod::start(c, attend_kernel<128>, grid, block, ForwardShared<128>::kAll, 1, w, c.mark);
+        sides == 1 ? launch<128, 1>(c, w, pieces) : launch<128, 2>(c, w, pieces);
     }
 }
 
