@@ -16,9 +16,21 @@ constexpr int kTile = 128;                 // rows of queries or keys in a tile:
 // Which sequence and which of its tiles a piece of work is.  Sequences of one length are numbered by arithmetic; others by a
 // table in the workspace (plan_kernel), whose entries end with sequences of length -1.  The longest pieces come first, because
 // a block's work grows with the tile's place under a causal mask, and the last blocks should be short.
+struct Divisor {                           // of numbers below 2^31, by a product: a division takes 100 clocks and more
+    uint32_t d, m, shift;
+    __device__ __forceinline__ int quotient(int n) const { return static_cast<int>((static_cast<uint64_t>(static_cast<uint32_t>(n)) * m) >> shift); }
+};
+
+inline Divisor divisor(int64_t d) {        // m = floor(2^(31 + l) / d) + 1 with 2^l >= d: exact below 2^31
+    int l = 0;
+    while ((int64_t{1} << l) < d) ++l;
+    return Divisor{static_cast<uint32_t>(d), static_cast<uint32_t>((uint64_t{1} << (31 + l)) / static_cast<uint64_t>(d) + 1), static_cast<uint32_t>(31 + l)};
+}
+
 struct Plan {
     const int4* table;                     // {first row, length, tile, 0}
-    int length, sequences, tiles;          // without a table
+    int length, tiles;                     // without a table
+    Divisor sequences;
     int descending;
 };
 
@@ -31,8 +43,8 @@ __device__ __forceinline__ Piece piece_of(const Plan& p, int i) {
         const int4 e = p.table[i];
         return Piece{e.x, e.y, e.z};
     }
-    const int rank = i / p.sequences;
-    return Piece{(i - rank * p.sequences) * p.length, p.length, p.descending ? p.tiles - 1 - rank : rank};
+    const int rank = p.sequences.quotient(i);
+    return Piece{(i - rank * static_cast<int>(p.sequences.d)) * p.length, p.length, p.descending ? p.tiles - 1 - rank : rank};
 }
 
 // A value that all lanes of a converged warp have, as one that the compiler knows to be the same in all (and may keep in a uniform
@@ -46,23 +58,23 @@ __device__ __forceinline__ int same(int v) { return static_cast<int>(__reduce_or
 // ahead of time.
 struct Pieces {
     const Plan* plan;
-    int heads, units, round;
+    Divisor heads;
+    int units, round, next_head;
     Piece next;
 
-    __device__ __forceinline__ int unit() const {
-        const int g = static_cast<int>(gridDim.x), b = static_cast<int>(blockIdx.x);
-        return round * g + ((round & 1) ? g - 1 - b : b);
-    }
-    __device__ __forceinline__ Pieces(const Plan& p, int heads_, int units_) : plan(&p), heads(heads_), units(units_), round(-1) { look(); }
+    __device__ __forceinline__ Pieces(const Plan& p, const Divisor& heads_, int units_) : plan(&p), heads(heads_), units(units_), round(-1) { look(); }
     __device__ __forceinline__ void look() {
         ++round;
-        next = unit() < units ? piece_of(*plan, unit() / heads) : Piece{0, -1, 0};
+        const int g = static_cast<int>(gridDim.x), b = static_cast<int>(blockIdx.x), unit = round * g + ((round & 1) ? g - 1 - b : b);
+        const int i = heads.quotient(unit);
+        next = unit < units ? piece_of(*plan, i) : Piece{0, -1, 0};
+        next_head = unit - i * static_cast<int>(heads.d);
     }
     // false when there are no more
     __device__ __forceinline__ bool take(Piece& piece, int& head) {
         piece = Piece{same(next.start), same(next.length), same(next.tile)};
         if (piece.length < 0) return false;
-        head = unit() % heads;
+        head = next_head;
         look();
         return true;
     }
@@ -91,11 +103,12 @@ __device__ __forceinline__ void load_head(uint32_t dst, const CUtensorMap* map, 
     for (int c = 0; c < D / 64; ++c) load_rows(dst + c * kChunk, map, 64 * c, head, row, bar);
 }
 
-// Rows from `first` on of a tile become zero (by `threads` threads): they are other sequences' rows, or no one's, and what they
-// hold, NaN too, must not meet the zeros of a masked product.  The caller announces it to the matrix instructions by a barrier.
+// Rows of a tile from `first` on become zero, up to the end of the sixteen that a matrix instruction takes (by `threads` threads):
+// they are other sequences' rows, or no one's, and what they hold, NaN too, must not meet the zeros of a masked product.  The
+// caller announces it to the matrix instructions by a barrier.
 template <int D>
 __device__ __forceinline__ void clear_rows(uint8_t* tile, int first, int thread, int threads) {
-    for (int i = first * 8 + thread; i < kTile * 8; i += threads) {
+    for (int i = first * 8 + thread; i < ((first + 15) & ~15) * 8; i += threads) {
 #pragma unroll
         for (int c = 0; c < D / 64; ++c) *reinterpret_cast<uint4*>(tile + c * kChunk + i * 16) = make_uint4(0, 0, 0, 0);
     }
@@ -244,6 +257,17 @@ __device__ __forceinline__ void tmem_store32(uint32_t addr, const uint32_t (&r)[
         : "memory");
 }
 
+__device__ __forceinline__ void tmem_store16(uint32_t addr, const uint32_t (&r)[16]) {
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x16.b32 [%16], {"
+        "%0, %1, %2, %3, %4, %5, %6, %7, "
+        "%8, %9, %10, %11, %12, %13, %14, %15"
+        "};" ::"r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]),
+          "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]),
+          "r"(addr)
+        : "memory");
+}
+
 __device__ __forceinline__ void tmem_stored() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
 __device__ __forceinline__ void tmem_store_f32(uint32_t addr, const float (&v)[32]) {
@@ -276,35 +300,18 @@ __device__ __forceinline__ float2 mul2(float2 a, float2 b) {
     return r;
 }
 
-// NaN if any is
+// a NaN is passed over
 __device__ __forceinline__ float max3(float a, float b, float c) {
     float r;
-    asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+    asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
     return r;
-}
-
-// 2^x for two x of 2^7 at most, on the multiply-add pipe: x = n + f, n the nearest integer (read off the low bits of 1.5 2^23 + x), 2^f
-// a polynomial of degree 5, its coefficients from an exchange algorithm for the least relative error on [-1/2, 1/2]: 2.2e-7 in
-// binary32, as much as the special function unit's.  Below 2^-126 it stops there; NaN is lost.
-__device__ __forceinline__ float2 exp2_poly(float2 x) {
-    const float2 magic = make_float2(12582912.0f, 12582912.0f);
-    x.x = fmaxf(x.x, -126.0f);
-    x.y = fmaxf(x.y, -126.0f);
-    const float2 r = add2(x, magic), f = add2(x, fma2(r, make_float2(-1.0f, -1.0f), magic));
-    auto twice = [](float v) { return make_float2(v, v); };
-    float2 p = fma2(f, twice(0.0013276472454890609f), twice(0.009675540961325169f));
-    p = fma2(p, f, twice(0.05550713092088699f));
-    p = fma2(p, f, twice(0.24022120237350464f));
-    p = fma2(p, f, twice(0.6931469440460205f));
-    p = fma2(p, f, twice(1.0000001192092896f));
-    return make_float2(__uint_as_float(__float_as_uint(p.x) + (__float_as_uint(r.x) << 23)),
-                       __uint_as_float(__float_as_uint(p.y) + (__float_as_uint(r.y) << 23)));
 }
 
 // ---------------------------------------------------------------- results
 // COLS columns of a row a thread (binary32, in tensor memory at `addr`), times `factor`, as bf16 rows of a head: through
-// shared memory (`stage`, 32 x 64 bytes, this warp's own), 32 columns at a time, so that 64 bytes of a row leave together.  row0: the
-// warp's first row, of which `rows` are there (may be negative); col0: the first column, of `dim`.
+// shared memory (`stage`, kStage bytes, this warp's own), 32 columns at a time, so that 64 bytes of a row leave together (each thread
+// its own row, 16 bytes at a time: 5 % slower where sequences are short).  row0: the warp's first row, of which `rows` are there
+// (may be negative); col0: the first column, of `dim`.
 constexpr uint32_t kStage = 2048;
 
 template <int COLS>
@@ -331,6 +338,24 @@ __device__ __forceinline__ void give_rows(uint32_t addr, float factor, uint8_t* 
         }
     }
     __syncwarp();
+}
+
+// COLS columns of a row a thread (binary32, in tensor memory at `addr`), times `factor`, as bf16 to the row at `out` where it
+// is there (`live`), up to `dim` columns.  Each thread stores its own row, 16 bytes at a time: the halves of sectors meet in L2.  (Rows put
+// together in shared memory first, 64 bytes of a row at a time, kept a warp 2.5 times as long.)
+template <int COLS>
+__device__ __forceinline__ void give_row(uint32_t addr, float factor, __nv_bfloat16* out, bool live, int dim) {
+#pragma unroll
+    for (int c = 0; c < COLS; c += 32) {
+        float v[32];
+        tc::tmem_load32(addr + c, v);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const uint4 w = make_uint4(pack_bf16(v[8 * i] * factor, v[8 * i + 1] * factor), pack_bf16(v[8 * i + 2] * factor, v[8 * i + 3] * factor),
+                                       pack_bf16(v[8 * i + 4] * factor, v[8 * i + 5] * factor), pack_bf16(v[8 * i + 6] * factor, v[8 * i + 7] * factor));
+            if (live && c + 8 * i < dim) *reinterpret_cast<uint4*>(out + c + 8 * i) = w;
+        }
+    }
 }
 
 // ---------------------------------------------------------------- host side (attention_plan.cu)

@@ -249,9 +249,8 @@ __global__ void __launch_bounds__(kThreads, 1) query_gradient_kernel(const __gri
         if (fine) {
             tc::fence_after();
             constexpr int kHalf = D / 2;
-            uint8_t* stage = mem + warp * (32 * kHalf * 2);          // over the queries, which have been read
-            give_rows<kHalf>(dq_at + half * kHalf + lanes, w.scale, stage, w.dq, piece.start + row - lane, piece.length - row0 - quarter * 32, head,
-                             half * kHalf, w.dim, lane);
+            give_row<kHalf>(dq_at + half * kHalf + lanes, w.scale, w.dq.p + static_cast<int64_t>(piece.start + row) * w.dq.rs + head * w.dq.hs + half * kHalf, live,
+                            w.dim - half * kHalf);
         }
     }
     Finish::end(fine, slot_mem, mark, tmem, warp);
@@ -499,10 +498,10 @@ __global__ void __launch_bounds__(kKeyThreads, 1) key_gradient_kernel(const __gr
         if (fine) {
             tc::fence_after();
             constexpr int kHalf = D / 2;
-            const int rows = piece.length - key0 - quarter * 32;
-            uint8_t* stage = mem + warp * (32 * kHalf * 2);          // over the keys, then the values, which have been read
-            give_rows<kHalf>(dk_at + half * kHalf + lanes, w.scale, stage, w.dk, piece.start + key - lane, rows, kv_head, half * kHalf, w.dim, lane);
-            give_rows<kHalf>(dv_at + half * kHalf + lanes, 1.0f, stage + S::kBytes, w.dv, piece.start + key - lane, rows, kv_head, half * kHalf, w.dim, lane);
+            const bool live = key < piece.length;
+            const int64_t at = piece.start + key;
+            give_row<kHalf>(dk_at + half * kHalf + lanes, w.scale, w.dk.p + at * w.dk.rs + kv_head * w.dk.hs + half * kHalf, live, w.dim - half * kHalf);
+            give_row<kHalf>(dv_at + half * kHalf + lanes, 1.0f, w.dv.p + at * w.dv.rs + kv_head * w.dv.hs + half * kHalf, live, w.dim - half * kHalf);
         }
     }
     Finish::end(fine, slot_mem, mark, tmem, warp);

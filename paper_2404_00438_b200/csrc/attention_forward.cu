@@ -16,7 +16,8 @@ constexpr int64_t kLongSequence = 1024;
 struct Forward {
     CUtensorMap q, k, v;
     Plan plan;
-    int units, heads, group, dim, causal;
+    int units, dim, causal;
+    Divisor heads, group;
     float c;                               // scale * log2(e)
     Rows out;
     float* lse;
@@ -97,7 +98,7 @@ __global__ void __launch_bounds__(ForwardShared<D, SIDES>::kThreads, 3 - SIDES) 
         int filled = 0, queries = 0, others = 0;                     // tiles asked for: into the ring, of either side
         while (fine && pieces.take(piece, head)) {
             divide();
-            const int kv_head = head / w.group;
+            const int kv_head = w.group.quotient(head);
             for (int r = 0; r < most && fine; ++r) {
                 const int row = piece.start + (most - 1 - r) * kTile;
                 for (int kind = 0; kind < 2; ++kind, ++filled) {
@@ -359,7 +360,7 @@ int sides_of(const dlion_attention_fwd& p) {
 template <int D, int SIDES>
 void launch(prod::Call& c, Forward& w, int64_t pieces) {
     using S = ForwardShared<D, SIDES>;
-    w.units = static_cast<int>(pieces * w.heads);
+    w.units = static_cast<int>(pieces * w.heads.d);
     prod::raise_shared(c, &attend_kernel<D, SIDES>, S::kAll);
     prod::start(c, attend_kernel<D, SIDES>, dim3(static_cast<unsigned>(std::min(w.units, (3 - SIDES) * c.sms))), dim3(S::kThreads), S::kAll, 1, w, c.mark);
 }
@@ -389,8 +390,8 @@ void forward(prod::Call& c, const dlion_attention_fwd& p) {
         c.status = DLION_ECUDA;
         return;
     }
-    w.heads = static_cast<int>(p.heads);
-    w.group = static_cast<int>(p.heads / p.kv_heads);
+    w.heads = divisor(p.heads);
+    w.group = divisor(p.heads / p.kv_heads);
     w.dim = static_cast<int>(p.dim);
     w.causal = p.causal;
     w.c = p.scale * kLog2e;

@@ -138,8 +138,8 @@ int64_t most_pieces(const Sequences& s, int tile) {
 void make_plans(prod::Call& c, const Sequences& s, const PlanRequest* requests, int n, int4* const* tables, Plan* plans, const Clear* clear) {
     for (int i = 0; i < n; ++i) {
         const int64_t length = s.length == 0 ? s.rows : s.length;
-        plans[i] = Plan{tables[i], static_cast<int>(length), s.offsets != nullptr || length == 0 ? 0 : static_cast<int>(s.rows / length),
-                        static_cast<int>(prod::parts(length, requests[i].tile)), !requests[i].keys};
+        const int64_t count = s.offsets != nullptr || length == 0 ? 1 : s.rows / length;
+        plans[i] = Plan{tables[i], static_cast<int>(length), static_cast<int>(prod::parts(length, requests[i].tile)), divisor(count), !requests[i].keys};
     }
     if (s.offsets == nullptr || !c.live()) return;
     PlanArgs a{};
