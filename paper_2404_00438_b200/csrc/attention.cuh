@@ -14,7 +14,7 @@ namespace att {
 constexpr int kTile = 128;                 // rows of queries or keys in a tile: the lanes of tensor memory
 
 // Which sequence and which of its tiles a piece of work is.  Sequences of one length are numbered by arithmetic; others by a
-// table in the workspace (plan_kernel), whose entries end with sequences of length -1.  The longest pieces come first, because
+// table in the workspace (plan_kernel), which ends with entries of length -1.  The longest pieces come first, because
 // a block's work grows with the tile's place under a causal mask, and the last blocks should be short.
 struct Divisor {                           // of numbers below 2^31, by a product: a division takes 100 clocks and more
     uint32_t d, m, shift;
@@ -52,31 +52,74 @@ __device__ __forceinline__ Piece piece_of(const Plan& p, int i) {
 // over one by one before each.
 __device__ __forceinline__ int same(int v) { return static_cast<int>(__reduce_or_sync(0xffffffffu, static_cast<unsigned>(v))); }
 
-// A block's pieces of work, each a tile of a sequence and a head: every gridDim.x-th of them, in turn from either end, since they
-// become lighter along the list.  The kernels are persistent: while a tile's last rows are weighed and its results leave, the next
-// one's first products run (197 rows, 12 heads, 64 images forward: 47 us with a block for each tile).  The next entry is asked for
-// ahead of time.
+// A block's pieces of work, each a tile of a sequence and a head.  The kernels are persistent: a block takes over the work of blocks
+// that have not started (the grid has one for each piece), so that while a tile's last rows are weighed and its results leave, the
+// next one's first products run, and whoever is free takes the next piece.  (64 images of 197 rows forward: 47 us with a block for
+// each tile, 41 so.  With every so many-th piece for each block, 8192 rows of 11 documents: 12 % slower backward.)  The copying warp asks
+// for the next piece when it comes to a piece's last tile (at its first, everyone would take two of the longest pieces), in two places of
+// shared memory in turn; every warp of the block reads the answer.
+constexpr uint32_t kTurnBytes = 64;        // two barriers for answers, two for their readers, the answers
+
 struct Pieces {
     const Plan* plan;
     Divisor heads;
-    int units, round, next_head;
-    Piece next;
+    uint32_t at;                           // shared memory
+    int turn;                              // pieces taken
 
-    __device__ __forceinline__ Pieces(const Plan& p, const Divisor& heads_, int units_) : plan(&p), heads(heads_), units(units_), round(-1) { look(); }
-    __device__ __forceinline__ void look() {
-        ++round;
-        const int g = static_cast<int>(gridDim.x), b = static_cast<int>(blockIdx.x), unit = round * g + ((round & 1) ? g - 1 - b : b);
-        const int i = heads.quotient(unit);
-        next = unit < units ? piece_of(*plan, i) : Piece{0, -1, 0};
-        next_head = unit - i * static_cast<int>(heads.d);
+    __device__ __forceinline__ Pieces(const Plan& p, const Divisor& heads_, uint32_t at_) : plan(&p), heads(heads_), at(at_), turn(0) {}
+
+    __device__ static void init(uint32_t at, int warps) {
+        for (int i = 0; i < 2; ++i) {
+            tc::bar_init(at + 8 * i, 1);
+            tc::bar_init(at + 16 + 8 * i, warps);
+        }
     }
-    // false when there are no more
-    __device__ __forceinline__ bool take(Piece& piece, int& head) {
-        piece = Piece{same(next.start), same(next.length), same(next.tile)};
-        if (piece.length < 0) return false;
-        head = next_head;
-        look();
+    __device__ __forceinline__ uint32_t parity(int k) const { return ((k - 1) >> 1) & 1; }
+
+    // False when there are no more (or a wait ran out, and `fine` says so).
+    __device__ __forceinline__ bool take(Piece& piece, int& head, bool& fine) {
+        int unit = static_cast<int>(blockIdx.x);
+        if (turn > 0) {
+            const uint32_t place = turn & 1;
+            if (!(fine = tc::bar_wait(at + 8 * place, parity(turn)))) return false;
+            uint32_t got, first;
+            asm volatile(
+                "{\n.reg .pred p;\n.reg .b128 r;\nld.shared.b128 r, [%2];\n"
+                "clusterlaunchcontrol.query_cancel.is_canceled.pred.b128 p, r;\nselp.u32 %0, 1, 0, p;\nmov.u32 %1, 0;\n"
+                "@p clusterlaunchcontrol.query_cancel.get_first_ctaid::x.b32.b128 %1, r;\n}"
+                : "=r"(got), "=r"(first)
+                : "r"(at + 32 + 16 * place)
+                : "memory");
+            tc::fence_for_copies();        // read, before the next answer comes to this place
+            __syncwarp();
+            if (threadIdx.x % 32 == 0) tc::bar_arrive(at + 16 + 8 * place);
+            if (same(got) == 0) return false;
+            unit = same(first);
+        }
+        ++turn;
+        const int i = heads.quotient(unit);
+        const Piece found = piece_of(*plan, i);
+        piece = Piece{same(found.start), same(found.length), same(found.tile)};
+        head = unit - i * static_cast<int>(heads.d);
+        return piece.length >= 0;
+    }
+
+    // By the copying warp, in a piece that it has taken: the next one.
+    __device__ __forceinline__ bool ask() const {
+        const uint32_t place = turn & 1;
+        if (!tc::bar_wait(at + 16 + 8 * place, parity(turn) ^ 1)) return false;
+        if (tc::elected()) {
+            tc::bar_expect(at + 8 * place, 16);
+            asm volatile("clusterlaunchcontrol.try_cancel.async.shared::cta.mbarrier::complete_tx::bytes.b128 [%0], [%1];" ::"r"(at + 32 + 16 * place),
+                         "r"(at + 8 * place)
+                         : "memory");
+        }
+        __syncwarp();
         return true;
+    }
+    // An answer that may still be on its way, where a wait ran out.
+    __device__ __forceinline__ void settle(int asked) const {
+        if (asked >= turn && asked > 0) tc::bar_wait(at + 8 * (asked & 1), parity(asked));
     }
 };
 
@@ -274,32 +317,6 @@ __device__ __forceinline__ void tmem_store_f32(uint32_t addr, const float (&v)[3
     tmem_store32(addr, reinterpret_cast<const uint32_t(&)[32]>(v));
 }
 
-// ---------------------------------------------------------------- pairs of binary32 values
-__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
-    float2 r;
-    asm("{\n.reg .b64 a, b, c, d;\nmov.b64 a, {%2, %3};\nmov.b64 b, {%4, %5};\nmov.b64 c, {%6, %7};\n"
-        "fma.rn.f32x2 d, a, b, c;\nmov.b64 {%0, %1}, d;\n}"
-        : "=f"(r.x), "=f"(r.y)
-        : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
-    return r;
-}
-
-__device__ __forceinline__ float2 add2(float2 a, float2 b) {
-    float2 r;
-    asm("{\n.reg .b64 a, b, d;\nmov.b64 a, {%2, %3};\nmov.b64 b, {%4, %5};\nadd.rn.f32x2 d, a, b;\nmov.b64 {%0, %1}, d;\n}"
-        : "=f"(r.x), "=f"(r.y)
-        : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
-    return r;
-}
-
-__device__ __forceinline__ float2 mul2(float2 a, float2 b) {
-    float2 r;
-    asm("{\n.reg .b64 a, b, d;\nmov.b64 a, {%2, %3};\nmov.b64 b, {%4, %5};\nmul.rn.f32x2 d, a, b;\nmov.b64 {%0, %1}, d;\n}"
-        : "=f"(r.x), "=f"(r.y)
-        : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
-    return r;
-}
-
 // a NaN is passed over
 __device__ __forceinline__ float max3(float a, float b, float c) {
     float r;
@@ -340,9 +357,8 @@ __device__ __forceinline__ void give_rows(uint32_t addr, float factor, uint8_t* 
     __syncwarp();
 }
 
-// COLS columns of a row a thread (binary32, in tensor memory at `addr`), times `factor`, as bf16 to the row at `out` where it
-// is there (`live`), up to `dim` columns.  Each thread stores its own row, 16 bytes at a time: the halves of sectors meet in L2.  (Rows put
-// together in shared memory first, 64 bytes of a row at a time, kept a warp 2.5 times as long.)
+// The same to the row at `out` where it is there (`live`), without a place to put rows together: each thread stores its own row, 16
+// bytes at a time, and the halves of sectors meet in L2.
 template <int COLS>
 __device__ __forceinline__ void give_row(uint32_t addr, float factor, __nv_bfloat16* out, bool live, int dim) {
 #pragma unroll

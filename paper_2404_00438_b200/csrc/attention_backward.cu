@@ -16,7 +16,8 @@ namespace {
 struct Backward {
     CUtensorMap q, k, v, dout;
     Plan plan;
-    int heads, kv_heads, group, dim, causal;
+    int dim, causal;
+    Divisor heads, group;                  // heads: of the tiles' own kind
     float c, scale;                        // scale * log2(e)
     Rows out, dout_rows;                   // read row by row
     const float* lse;
@@ -26,9 +27,7 @@ struct Backward {
     Rows dq, dk, dv;
 };
 
-constexpr int kThreads = 320;              // eight warps of arithmetic, a copying and an issuing warp
-
-// The eight warps: lanes of tensor memory go by warp % 4, so two warps have the same rows, each 64 columns.  What a warp leaves
+// Eight warps of arithmetic, a copying, an issuing and other warps.  Of the eight: lanes of tensor memory go by warp % 4, so two warps have the same rows, each 64 columns.  What a warp leaves
 // there as an operand (64 bf16, 32 columns) goes over the first of the columns that it has read itself, which leaves a gap of 32
 // between the operand's halves.
 
@@ -52,34 +51,35 @@ struct Finish {                            // the end of every kernel: see produ
 };
 
 // ---------------------------------------------------------------- dq
+// Tensor memory: two sets of scores in turn, dp, dq; ds goes over its scores.
 template <int D>
 struct QueryShared {
     static constexpr uint32_t kBytes = kTile * D * 2;
     static constexpr int kKeys = 3, kValues = 2;                     // stages
-    static constexpr uint32_t kSums = (2 + kKeys + kValues) * kBytes;
-    static constexpr uint32_t kBars = kSums + 2 * kTile * 4;
-    static constexpr uint32_t kAll = kBars + 256 + 1024;
+    static constexpr uint32_t kStats = (2 + kKeys + kValues) * kBytes;                // lse and D of the tile of queries
+    static constexpr uint32_t kBars = kStats + 2 * kTile * 4;
+    static constexpr uint32_t kAll = kBars + 256 + kTurnBytes + 1024;
 };
 
+constexpr int kQueryThreads = 384;         // and two warps that work out D ahead of time
+
 template <int D>
-__global__ void __launch_bounds__(kThreads, 1) query_gradient_kernel(const __grid_constant__ Backward w, unsigned int* mark) {
+__global__ void __launch_bounds__(kQueryThreads, 1) query_gradient_kernel(const __grid_constant__ Backward w, unsigned int* mark) {
     using S = QueryShared<D>;
     extern __shared__ uint8_t raw[];
     const uint32_t base = (tc::smem_addr(raw) + 1023u) & ~1023u;
     uint8_t* mem = raw + (base - tc::smem_addr(raw));
     const uint32_t keys = base + 2 * S::kBytes, values = keys + S::kKeys * S::kBytes, bars = base + S::kBars;
     const uint32_t k_full = bars, k_empty = bars + 32, v_full = bars + 64, v_empty = bars + 96, scores = bars + 128, products = bars + 144,
-                   taken = bars + 152, slopes = bars + 160, rows_full = bars + 168, done = bars + 176, slot = bars + 192;
+                   taken = bars + 152, slopes = bars + 160, rows_full = bars + 168, done = bars + 176, rows_empty = bars + 184, stats_full = bars + 192, stats_empty = bars + 200, slot = bars + 208;
+    const uint32_t turns = bars + 256;
     volatile uint32_t* slot_mem = reinterpret_cast<volatile uint32_t*>(mem + (slot - base));
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
 
     tc::let_next_start();
-    if (w.plan.table != nullptr) tc::wait_for_previous();
-    const int head = static_cast<int>(blockIdx.x) % w.heads;
-    const Piece found = piece_of(w.plan, static_cast<int>(blockIdx.x) / w.heads);
-    const Piece piece{same(found.start), same(found.length), same(found.tile)};
-    if (piece.length < 0) return;
     if (threadIdx.x == 0) {
+        tc::bar_init(stats_full, 2);
+        tc::bar_init(stats_empty, 8);
         for (int i = 0; i < S::kKeys; ++i) {
             tc::bar_init(k_full + 8 * i, 1);
             tc::bar_init(k_empty + 8 * i, 1);
@@ -94,7 +94,9 @@ __global__ void __launch_bounds__(kThreads, 1) query_gradient_kernel(const __gri
         tc::bar_init(taken, 8);
         tc::bar_init(slopes, 8);
         tc::bar_init(rows_full, 1);
+        tc::bar_init(rows_empty, 1);
         tc::bar_init(done, 1);
+        Pieces::init(turns, blockDim.x / 32);
         tc::bar_init_done();
         slot_mem[1] = 0;
         tc::prefetch_map(&w.q);
@@ -107,40 +109,60 @@ __global__ void __launch_bounds__(kThreads, 1) query_gradient_kernel(const __gri
     __syncthreads();
     tc::fence_after();
     const uint32_t tmem = same(*slot_mem), products_at = tmem + 256, dq_at = tmem + 384;
-    const int row0 = piece.tile * kTile;
-    const int key_tiles = (piece.length + kTile - 1) / kTile;
-    const int n = w.causal ? min(key_tiles, piece.tile + 1) : key_tiles;              // tiles of keys, from the last to the first
-    const int kv_head = head / w.group;
     bool fine = true;
-    if (w.plan.table == nullptr) tc::wait_for_previous();
+    tc::wait_for_previous();
+
+    Pieces pieces(w.plan, w.heads, turns);
+    Piece piece{};
+    int head = 0, row0 = 0, n = 0;         // a piece's first row in the sequence, and its tiles of keys, from the last to the first
+    auto divide = [&] {
+        row0 = piece.tile * kTile;
+        const int key_tiles = (piece.length + kTile - 1) / kTile;
+        n = w.causal ? min(key_tiles, piece.tile + 1) : key_tiles;
+    };
 
     if (warp == 8) {
-        if (tc::elected()) {
-            tc::bar_expect(rows_full, 2 * S::kBytes);
-            load_head<D>(base, &w.q, head, piece.start + row0, rows_full);
-            load_head<D>(base + S::kBytes, &w.dout, head, piece.start + row0, rows_full);
-        }
-        __syncwarp();
-        int i = 0;
-        for (; i < n && fine; ++i) {
-            const int row = piece.start + (n - 1 - i) * kTile, ks = i % S::kKeys, vs = i % S::kValues;
-            if (!(fine = tc::bar_wait(k_empty + 8 * ks, ((i / S::kKeys) & 1) ^ 1))) break;
-            if (tc::elected()) {
-                tc::bar_expect(k_full + 8 * ks, S::kBytes);
-                load_head<D>(keys + ks * S::kBytes, &w.k, kv_head, row, k_full + 8 * ks);
+        int i = 0, begun = 0, k_asked = 0, v_asked = 0, asked = 0;           // tiles of keys, and pieces, of all
+        while (fine && pieces.take(piece, head, fine)) {
+            divide();
+            const int kv_head = w.group.quotient(head);
+            for (int r = 0; r < n && fine; ++r, ++i) {
+                if (r == n - 1) {
+                    asked = pieces.turn;
+                    if (!(fine = pieces.ask())) break;
+                }
+                const int row = piece.start + (n - 1 - r) * kTile, ks = i % S::kKeys, vs = i % S::kValues;
+                if (!(fine = tc::bar_wait(k_empty + 8 * ks, ((i / S::kKeys) & 1) ^ 1))) break;
+                if (tc::elected()) {
+                    tc::bar_expect(k_full + 8 * ks, S::kBytes);
+                    load_head<D>(keys + ks * S::kBytes, &w.k, kv_head, row, k_full + 8 * ks);
+                }
+                __syncwarp();
+                ++k_asked;
+                if (r == 0) {
+                    if (!(fine = tc::bar_wait(rows_empty, (begun & 1) ^ 1))) break;
+                    if (tc::elected()) {
+                        tc::bar_expect(rows_full, 2 * S::kBytes);
+                        load_head<D>(base, &w.q, head, piece.start + row0, rows_full);
+                        load_head<D>(base + S::kBytes, &w.dout, head, piece.start + row0, rows_full);
+                    }
+                    __syncwarp();
+                    ++begun;
+                }
+                if (!(fine = tc::bar_wait(v_empty + 8 * vs, ((i / S::kValues) & 1) ^ 1))) break;
+                if (tc::elected()) {
+                    tc::bar_expect(v_full + 8 * vs, S::kBytes);
+                    load_head<D>(values + vs * S::kBytes, &w.v, kv_head, row, v_full + 8 * vs);
+                }
+                __syncwarp();
+                ++v_asked;
             }
-            __syncwarp();
-            if (!(fine = tc::bar_wait(v_empty + 8 * vs, ((i / S::kValues) & 1) ^ 1))) break;
-            if (tc::elected()) {
-                tc::bar_expect(v_full + 8 * vs, S::kBytes);
-                load_head<D>(values + vs * S::kBytes, &w.v, kv_head, row, v_full + 8 * vs);
-            }
-            __syncwarp();
         }
         if (!fine) {                       // what was asked for still lands in this block's memory: it is awaited
-            tc::bar_wait(rows_full, 0);
-            for (int a = max(0, i + 1 - S::kKeys); a <= i && a < n; ++a) tc::bar_wait(k_full + 8 * (a % S::kKeys), (a / S::kKeys) & 1);
-            for (int a = max(0, i - S::kValues); a < i; ++a) tc::bar_wait(v_full + 8 * (a % S::kValues), (a / S::kValues) & 1);
+            pieces.settle(asked);
+            if (begun > 0) tc::bar_wait(rows_full, (begun - 1) & 1);
+            for (int a = max(0, k_asked - S::kKeys); a < k_asked; ++a) tc::bar_wait(k_full + 8 * (a % S::kKeys), (a / S::kKeys) & 1);
+            for (int a = max(0, v_asked - S::kValues); a < v_asked; ++a) tc::bar_wait(v_full + 8 * (a % S::kValues), (a / S::kValues) & 1);
         }
     } else if (warp == 9) {
         const int k_steps = (w.dim + 15) / 16;
@@ -149,10 +171,22 @@ __global__ void __launch_bounds__(kThreads, 1) query_gradient_kernel(const __gri
             if (tc::elected()) tc::commit<1>(bar);
             __syncwarp();
         };
-        fine = tc::bar_wait(rows_full, 0);
-        // round i: scores of tile i (two sets of columns in turn), its dp once the last one's has been read, then dq of tile i - 1
-        for (int i = 0; i <= n && fine; ++i) {
-            if (i < n) {
+        // A round: scores of a tile of keys (two sets of columns in turn), its dp once the last one's has been read, then dq of the
+        // round before, which may be the last piece's.
+        int i = 0, begun = 0, steps = 0;
+        bool first = false, last = false;
+        auto gather = [&] {
+            const int b = i - 1;
+            if (!(fine = tc::bar_wait(slopes, b & 1))) return;
+            tc::fence_after();
+            weights_by_rows<0, 8, 32>(dq_at, tmem + (b & 1) * kTile, keys + (b % S::kKeys) * S::kBytes, wide, steps, !first);
+            if (last) finished(done);
+            finished(k_empty + 8 * (b % S::kKeys));
+        };
+        while (fine && pieces.take(piece, head, fine)) {
+            divide();
+            for (int r = 0; r < n && fine; ++r, ++i) {
+                if (r == 0 && !(fine = tc::bar_wait(rows_full, begun++ & 1))) break;
                 if (!(fine = tc::bar_wait(k_full + 8 * (i % S::kKeys), (i / S::kKeys) & 1))) break;
                 tc::fence_after();
                 rows_by_rows<D>(tmem + (i & 1) * kTile, base, keys + (i % S::kKeys) * S::kBytes, k_steps);
@@ -163,108 +197,144 @@ __global__ void __launch_bounds__(kThreads, 1) query_gradient_kernel(const __gri
                 rows_by_rows<D>(products_at, base + S::kBytes, values + (i % S::kValues) * S::kBytes, k_steps);
                 finished(products);
                 finished(v_empty + 8 * (i % S::kValues));
-            }
-            if (i > 0) {
-                const int b = i - 1;
-                if (!(fine = tc::bar_wait(slopes, b & 1))) break;
-                tc::fence_after();
-                weights_by_rows<0, 8, 32>(dq_at, tmem + (b & 1) * kTile, keys + (b % S::kKeys) * S::kBytes, wide,
-                                          (min(kTile, piece.length - (n - 1 - b) * kTile) + 15) / 16, b > 0);
-                finished(k_empty + 8 * (b % S::kKeys));
+                if (r == n - 1) finished(rows_empty);
+                if (i > 0) gather();
+                steps = (min(kTile, piece.length - (n - 1 - r) * kTile) + 15) / 16;
+                first = r == 0;
+                last = r == n - 1;
             }
         }
-        if (fine) finished(done);
-    } else {
-        const int half = warp / 4, quarter = warp % 4;
-        const int in_tile = quarter * 32 + lane, row = row0 + in_tile;
-        const bool live = row < piece.length;
-        const uint32_t lanes = static_cast<uint32_t>(quarter * 32) << 16;
-        float* sums = reinterpret_cast<float*>(mem + S::kSums);
-        // D, half of the head's columns a thread
-        float part = 0.0f, lse2 = 0.0f;
-        if (live) {
-            const int64_t at = piece.start + row;
-            const __nv_bfloat16 *o = w.out.p + at * w.out.rs + head * w.out.hs, *d = w.dout_rows.p + at * w.dout_rows.rs + head * w.dout_rows.hs;
-            const int units = w.dim / 8, mid = (units + 1) / 2;
-#pragma unroll 4
-            for (int u = half ? mid : 0; u < (half ? units : mid); ++u) {
-                float x[8], y[8];
-                widen(*reinterpret_cast<const uint4*>(o + u * 8), x);
-                widen(*reinterpret_cast<const uint4*>(d + u * 8), y);
+        if (fine && i > 0) gather();
+    } else if (warp >= 10) {
+        // D = do . out of half the tile's rows, D / 8 lanes a row, while the others work on the piece before
+        constexpr int kLanes = D / 8, kRows = 32 / kLanes, kAtOnce = 8;
+        float* stats = reinterpret_cast<float*>(mem + S::kStats);
+        const int unit = lane % kLanes;
+        int begun = 0;
+        while (fine && pieces.take(piece, head, fine)) {
+            divide();
+            float lse[2];
 #pragma unroll
-                for (int e = 0; e < 8; ++e) part = __fmaf_rn(x[e], y[e], part);
+            for (int e = 0; e < 2; ++e) {
+                const int row = row0 + (warp - 10) * (kTile / 2) + e * 32 + lane;
+                lse[e] = row < piece.length ? w.lse[head * w.lse_ld + piece.start + row] * kLog2e : 0.0f;
             }
-            lse2 = w.lse[head * w.lse_ld + at] * kLog2e;
-        }
-        sums[half * kTile + in_tile] = part;
-        asm volatile("bar.sync 1, 256;" ::: "memory");
-        const float delta = sums[in_tile] + sums[kTile + in_tile];
-        if (live && half == 0) w.delta[head * w.delta_ld + piece.start + row] = delta;
-        const float2 cc = make_float2(w.c, w.c), minus = make_float2(-lse2, -lse2), less = make_float2(-delta, -delta);
-        for (int i = 0; i < n; ++i) {
-            const int j = n - 1 - i, valid = piece.length - j * kTile;
-            const uint32_t s_at = tmem + (i & 1) * kTile + half * 64 + lanes;
-            if (!(fine = tc::bar_wait(scores + 8 * (i & 1), (i >> 1) & 1))) break;
-            tc::fence_after();
-            float s[64];
-            tmem_load64(s_at, s);
+            if (!(fine = tc::bar_wait(stats_empty, (begun & 1) ^ 1))) break;
+            for (int first = (warp - 10) * (kTile / 2); first < (warp - 9) * (kTile / 2); first += kAtOnce * kRows) {
+                uint4 o[kAtOnce], d[kAtOnce];
 #pragma unroll
-            for (int e = 0; e < 64; e += 2) {
-                const float2 x = fma2(make_float2(s[e], s[e + 1]), cc, minus);
-                s[e] = exp2_fast(x.x);
-                s[e + 1] = exp2_fast(x.y);
-            }
-            if (!(fine = tc::bar_wait(products, i & 1))) break;
-            tc::fence_after();
-            float dp[64];
-            tmem_load64(products_at + half * 64 + lanes, dp);
-            tc::fence_before();
-            __syncwarp();
-            if (lane == 0) tc::bar_arrive(taken);
+                for (int u = 0; u < kAtOnce; ++u) {
+                    const int row = row0 + first + u * kRows + lane / kLanes;
+                    const bool live = row < piece.length && unit * 8 < w.dim;
+                    const int64_t at = piece.start + row;
+                    o[u] = live ? *reinterpret_cast<const uint4*>(w.out.p + at * w.out.rs + head * w.out.hs + unit * 8) : make_uint4(0, 0, 0, 0);
+                    d[u] = live ? *reinterpret_cast<const uint4*>(w.dout_rows.p + at * w.dout_rows.rs + head * w.dout_rows.hs + unit * 8) : make_uint4(0, 0, 0, 0);
+                }
 #pragma unroll
-            for (int e = 0; e < 64; e += 2) {
-                const float2 x = mul2(add2(make_float2(dp[e], dp[e + 1]), less), make_float2(s[e], s[e + 1]));
-                s[e] = x.x;
-                s[e + 1] = x.y;
-            }
-            if (valid < kTile || (w.causal && (j + 1) * kTile > row0)) {
-                const int last = (w.causal ? min(row, piece.length - 1) : piece.length - 1) - j * kTile - half * 64;
+                for (int u = 0; u < kAtOnce; ++u) {
+                    float2 x[4], y[4], sum = twice(0.0f);
+                    widen(o[u], x);
+                    widen(d[u], y);
 #pragma unroll
-                for (int e = 0; e < 64; ++e) s[e] = e <= last ? s[e] : 0.0f;
-                if (valid < kTile) {       // the keys' rows behind the sequence
-                    if (!(fine = tc::bar_wait(k_full + 8 * (i % S::kKeys), (i / S::kKeys) & 1))) break;
-                    clear_rows<D>(mem + (keys - base) + (i % S::kKeys) * S::kBytes, valid, threadIdx.x, 256);
+                    for (int e = 0; e < 4; ++e) sum = fma2(x[e], y[e], sum);
+                    float delta = sum.x + sum.y;
+#pragma unroll
+                    for (int e = kLanes / 2; e >= 1; e /= 2) delta += __shfl_xor_sync(0xffffffffu, delta, e);
+                    const int in_tile = first + u * kRows + lane / kLanes;
+                    if (unit == 0 && row0 + in_tile < piece.length) {
+                        const int64_t at = piece.start + row0 + in_tile;
+                        w.delta[head * w.delta_ld + at] = delta;
+                        stats[kTile + in_tile] = delta;
+                    }
                 }
             }
-            uint32_t p[32];
 #pragma unroll
-            for (int e = 0; e < 32; ++e) p[e] = pack_bf16(s[2 * e], s[2 * e + 1]);
-            tmem_store32(s_at, p);
-            tmem_stored();
-            tc::fence_before();
+            for (int e = 0; e < 2; ++e) stats[(warp - 10) * (kTile / 2) + e * 32 + lane] = lse[e];
             __syncwarp();
-            if (lane == 0) tc::bar_arrive(slopes);
+            if (lane == 0) tc::bar_arrive(stats_full);
+            ++begun;
         }
-        if (fine) fine = tc::bar_wait(done, 0);
-        if (fine) {
+    } else {
+        const int half = warp / 4, quarter = warp % 4;
+        const float* stats = reinterpret_cast<const float*>(mem + S::kStats);
+        const uint32_t lanes = static_cast<uint32_t>(quarter * 32) << 16;
+        const float2 cc = twice(w.c);
+        int i = 0, ended = 0;
+        while (fine && pieces.take(piece, head, fine)) {
+            divide();
+            const int row = row0 + quarter * 32 + lane;
+            const bool live = row < piece.length;
+            if (!(fine = tc::bar_wait(stats_full, ended & 1))) break;
+            const float lse2 = live ? stats[quarter * 32 + lane] : 0.0f, delta = live ? stats[kTile + quarter * 32 + lane] : 0.0f;
+            __syncwarp();
+            if (lane == 0) tc::bar_arrive(stats_empty);
+            const float2 minus = twice(-lse2), less = twice(-delta);
+            for (int r = 0; r < n; ++r, ++i) {
+                const int j = n - 1 - r, valid = piece.length - j * kTile;
+                const uint32_t s_at = tmem + (i & 1) * kTile + half * 64 + lanes;
+                if (!(fine = tc::bar_wait(scores + 8 * (i & 1), (i >> 1) & 1))) break;
+                tc::fence_after();
+                float s[64];
+                tmem_load64(s_at, s);
+#pragma unroll
+                for (int e = 0; e < 64; e += 2) {
+                    const float2 x = fma2(make_float2(s[e], s[e + 1]), cc, minus);
+                    s[e] = exp2_fast(x.x);
+                    s[e + 1] = exp2_fast(x.y);
+                }
+                if (!(fine = tc::bar_wait(products, i & 1))) break;
+                tc::fence_after();
+                float dp[64];
+                tmem_load64(products_at + half * 64 + lanes, dp);
+                tc::fence_before();
+                __syncwarp();
+                if (lane == 0) tc::bar_arrive(taken);
+#pragma unroll
+                for (int e = 0; e < 64; e += 2) {
+                    const float2 x = mul2(add2(make_float2(dp[e], dp[e + 1]), less), make_float2(s[e], s[e + 1]));
+                    s[e] = x.x;
+                    s[e + 1] = x.y;
+                }
+                if (valid < kTile || (w.causal && (j + 1) * kTile > row0)) {
+                    const int behind = (w.causal ? min(row, piece.length - 1) : piece.length - 1) - j * kTile - half * 64;
+#pragma unroll
+                    for (int e = 0; e < 64; ++e) s[e] = e <= behind ? s[e] : 0.0f;
+                    if (valid < kTile) {   // the keys' rows behind the sequence
+                        if (!(fine = tc::bar_wait(k_full + 8 * (i % S::kKeys), (i / S::kKeys) & 1))) break;
+                        clear_rows<D>(mem + (keys - base) + (i % S::kKeys) * S::kBytes, valid, threadIdx.x, 256);
+                    }
+                }
+                uint32_t p[32];
+#pragma unroll
+                for (int e = 0; e < 32; ++e) p[e] = pack_bf16(s[2 * e], s[2 * e + 1]);
+                tmem_store32(s_at, p);
+                tmem_stored();
+                tc::fence_before();
+                __syncwarp();
+                if (lane == 0) tc::bar_arrive(slopes);
+            }
+            if (!fine || !(fine = tc::bar_wait(done, ended++ & 1))) break;
             tc::fence_after();
             constexpr int kHalf = D / 2;
             give_row<kHalf>(dq_at + half * kHalf + lanes, w.scale, w.dq.p + static_cast<int64_t>(piece.start + row) * w.dq.rs + head * w.dq.hs + half * kHalf, live,
                             w.dim - half * kHalf);
+            tc::fence_before();
         }
     }
     Finish::end(fine, slot_mem, mark, tmem, warp);
 }
 
 // ---------------------------------------------------------------- dk, dv
-// Scores and dp are computed transposed, keys as rows: so p and ds are operands as they lie in tensor memory.
+// Scores and dp are computed transposed, keys as rows: so p and ds are operands as they lie in tensor memory.  There is room for a second
+// set of scores beside dk and dv of 64 columns: the next scores then do not wait for dv.
 template <int D>
 struct KeyShared {
     static constexpr uint32_t kBytes = kTile * D * 2;
-    static constexpr int kStages = 2;                                // of queries and of do
+    static constexpr int kStages = D == 64 ? 3 : 2;                  // of queries and of do
     static constexpr uint32_t kStats = (2 + 2 * kStages) * kBytes;   // lse and D of two tiles of queries
     static constexpr uint32_t kBars = kStats + 2 * 2 * kTile * 4;
-    static constexpr uint32_t kAll = kBars + 256 + 1024;
+    static constexpr uint32_t kAll = kBars + 256 + kTurnBytes + 1024;
+    static constexpr int kSets = D == 64 ? 2 : 1;
 };
 
 constexpr int kKeyThreads = 352;           // and a warp that brings lse and D
@@ -272,38 +342,38 @@ constexpr int kKeyThreads = 352;           // and a warp that brings lse and D
 template <int D>
 __global__ void __launch_bounds__(kKeyThreads, 1) key_gradient_kernel(const __grid_constant__ Backward w, unsigned int* mark) {
     using S = KeyShared<D>;
-    constexpr int kStages = S::kStages;
+    constexpr int kStages = S::kStages, kSets = S::kSets;
     extern __shared__ uint8_t raw[];
     const uint32_t base = (tc::smem_addr(raw) + 1023u) & ~1023u;
     uint8_t* mem = raw + (base - tc::smem_addr(raw));
     const uint32_t queries = base + 2 * S::kBytes, douts = queries + kStages * S::kBytes, bars = base + S::kBars;
-    const uint32_t q_full = bars, q_empty = bars + 16, d_full = bars + 32, d_empty = bars + 48, scores = bars + 64, products = bars + 72,
-                   weights = bars + 80, slopes = bars + 88, rows_full = bars + 96, done = bars + 104, stats_full = bars + 112,
-                   stats_empty = bars + 128, slot = bars + 144;
+    const uint32_t q_full = bars, q_empty = bars + 24, d_full = bars + 48, d_empty = bars + 72, scores = bars + 96, products = bars + 112,
+                   weights = bars + 120, slopes = bars + 128, rows_full = bars + 136, done = bars + 144, rows_empty = bars + 152,
+                   stats_full = bars + 160, stats_empty = bars + 176, slot = bars + 192;
+    const uint32_t turns = bars + 256;
     volatile uint32_t* slot_mem = reinterpret_cast<volatile uint32_t*>(mem + (slot - base));
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
 
     tc::let_next_start();
-    if (w.plan.table != nullptr) tc::wait_for_previous();
-    const int kv_head = static_cast<int>(blockIdx.x) % w.kv_heads;
-    const Piece found = piece_of(w.plan, static_cast<int>(blockIdx.x) / w.kv_heads);
-    const Piece piece{same(found.start), same(found.length), same(found.tile)};
-    if (piece.length < 0) return;
     if (threadIdx.x == 0) {
         for (int i = 0; i < kStages; ++i) {
             tc::bar_init(q_full + 8 * i, 1);
             tc::bar_init(q_empty + 8 * i, 1);
             tc::bar_init(d_full + 8 * i, 1);
             tc::bar_init(d_empty + 8 * i, 1);
+        }
+        for (int i = 0; i < 2; ++i) {
+            tc::bar_init(scores + 8 * i, 1);
             tc::bar_init(stats_full + 8 * i, 1);
             tc::bar_init(stats_empty + 8 * i, 8);
         }
-        tc::bar_init(scores, 1);
         tc::bar_init(products, 1);
         tc::bar_init(weights, 8);
         tc::bar_init(slopes, 8);
         tc::bar_init(rows_full, 1);
+        tc::bar_init(rows_empty, 1);
         tc::bar_init(done, 1);
+        Pieces::init(turns, blockDim.x / 32);
         tc::bar_init_done();
         slot_mem[1] = 0;
         tc::prefetch_map(&w.q);
@@ -315,68 +385,102 @@ __global__ void __launch_bounds__(kKeyThreads, 1) key_gradient_kernel(const __gr
     tc::fence_before();
     __syncthreads();
     tc::fence_after();
-    const uint32_t tmem = same(*slot_mem), products_at = tmem + 128, dk_at = tmem + 256, dv_at = tmem + 256 + D;
-    const int key0 = piece.tile * kTile;
-    const int tiles = (piece.length + kTile - 1) / kTile, first = w.causal ? piece.tile : 0;
-    const int per = tiles - first, n = per * w.group;                // tiles of queries, of each head that shares these keys
+    const uint32_t tmem = same(*slot_mem), products_at = tmem + kSets * kTile, dk_at = products_at + kTile, dv_at = dk_at + D;
     bool fine = true;
-    if (w.plan.table == nullptr) tc::wait_for_previous();
+    tc::wait_for_previous();
+
+    Pieces pieces(w.plan, w.heads, turns);
+    Piece piece{};
+    int kv_head = 0, key0 = 0, first = 0, per = 0, n = 0;            // tiles of queries: of a head, the first of them, and in all
+    const int group = static_cast<int>(w.group.d);
+    auto divide = [&] {
+        key0 = piece.tile * kTile;
+        first = w.causal ? piece.tile : 0;
+        per = (piece.length + kTile - 1) / kTile - first;
+        n = per * group;
+    };
+    // The tiles of queries in turn: the query heads that share these keys one after the other.
+    int head = 0, tile = 0;
+    auto begin = [&] {
+        head = kv_head * group;
+        tile = first;
+    };
+    auto advance = [&] {
+        if (++tile == first + per) {
+            tile = first;
+            ++head;
+        }
+    };
 
     if (warp == 8) {
-        if (tc::elected()) {
-            tc::bar_expect(rows_full, 2 * S::kBytes);
-            load_head<D>(base, &w.k, kv_head, piece.start + key0, rows_full);
-            load_head<D>(base + S::kBytes, &w.v, kv_head, piece.start + key0, rows_full);
-        }
-        __syncwarp();
-        int i = 0;
-        bool half = false;                 // of round i
-        for (; i < n && fine; ++i) {
-            const int head = kv_head * w.group + i / per, row = piece.start + (first + i % per) * kTile, st = i % kStages;
-            const uint32_t parity = ((i / kStages) & 1) ^ 1;
-            if (!(fine = tc::bar_wait(q_empty + 8 * st, parity))) break;
-            if (tc::elected()) {
-                tc::bar_expect(q_full + 8 * st, S::kBytes);
-                load_head<D>(queries + st * S::kBytes, &w.q, head, row, q_full + 8 * st);
+        int i = 0, begun = 0, q_asked = 0, d_asked = 0, asked = 0;
+        while (fine && pieces.take(piece, kv_head, fine)) {
+            divide();
+            begin();
+            for (int r = 0; r < n && fine; ++r, ++i, advance()) {
+                if (r == n - 1) {
+                    asked = pieces.turn;
+                    if (!(fine = pieces.ask())) break;
+                }
+                const int row = piece.start + tile * kTile, st = i % kStages;
+                const uint32_t parity = ((i / kStages) & 1) ^ 1;
+                if (!(fine = tc::bar_wait(q_empty + 8 * st, parity))) break;
+                if (tc::elected()) {
+                    tc::bar_expect(q_full + 8 * st, S::kBytes);
+                    load_head<D>(queries + st * S::kBytes, &w.q, head, row, q_full + 8 * st);
+                }
+                __syncwarp();
+                ++q_asked;
+                if (r == 0) {
+                    if (!(fine = tc::bar_wait(rows_empty, (begun & 1) ^ 1))) break;
+                    if (tc::elected()) {
+                        tc::bar_expect(rows_full, 2 * S::kBytes);
+                        load_head<D>(base, &w.k, kv_head, piece.start + key0, rows_full);
+                        load_head<D>(base + S::kBytes, &w.v, kv_head, piece.start + key0, rows_full);
+                    }
+                    __syncwarp();
+                    ++begun;
+                }
+                if (!(fine = tc::bar_wait(d_empty + 8 * st, parity))) break;
+                if (tc::elected()) {
+                    tc::bar_expect(d_full + 8 * st, S::kBytes);
+                    load_head<D>(douts + st * S::kBytes, &w.dout, head, row, d_full + 8 * st);
+                }
+                __syncwarp();
+                ++d_asked;
             }
-            __syncwarp();
-            half = true;
-            if (!(fine = tc::bar_wait(d_empty + 8 * st, parity))) break;
-            if (tc::elected()) {
-                tc::bar_expect(d_full + 8 * st, S::kBytes);
-                load_head<D>(douts + st * S::kBytes, &w.dout, head, row, d_full + 8 * st);
-            }
-            __syncwarp();
-            half = false;
         }
         if (!fine) {                       // what was asked for still lands in this block's memory: it is awaited
-            tc::bar_wait(rows_full, 0);
-            for (int a = max(0, i - kStages); a < i; ++a) {
-                tc::bar_wait(q_full + 8 * (a % kStages), (a / kStages) & 1);
-                tc::bar_wait(d_full + 8 * (a % kStages), (a / kStages) & 1);
-            }
-            if (half) tc::bar_wait(q_full + 8 * (i % kStages), (i / kStages) & 1);
+            pieces.settle(asked);
+            if (begun > 0) tc::bar_wait(rows_full, (begun - 1) & 1);
+            for (int a = max(0, q_asked - kStages); a < q_asked; ++a) tc::bar_wait(q_full + 8 * (a % kStages), (a / kStages) & 1);
+            for (int a = max(0, d_asked - kStages); a < d_asked; ++a) tc::bar_wait(d_full + 8 * (a % kStages), (a / kStages) & 1);
         }
     } else if (warp == 10) {
         float* stats = reinterpret_cast<float*>(mem + S::kStats);
-        for (int i = 0; i < n; ++i) {
-            const int head = kv_head * w.group + i / per, tile = first + i % per, st = i & 1;
-            float lse[4], delta[4];
+        int i = 0;
+        while (fine && pieces.take(piece, kv_head, fine)) {
+            divide();
+            begin();
+            for (int r = 0; r < n; ++r, ++i, advance()) {
+                const int st = i & 1;
+                float lse[4], delta[4];
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const int row = tile * kTile + e * 32 + lane;
-                const bool live = row < piece.length;
-                lse[e] = live ? w.lse[head * w.lse_ld + piece.start + row] * kLog2e : 0.0f;
-                delta[e] = live ? w.delta[head * w.delta_ld + piece.start + row] : 0.0f;
-            }
-            if (!(fine = tc::bar_wait(stats_empty + 8 * st, ((i >> 1) & 1) ^ 1))) break;
+                for (int e = 0; e < 4; ++e) {
+                    const int row = tile * kTile + e * 32 + lane;
+                    const bool live = row < piece.length;
+                    lse[e] = live ? w.lse[head * w.lse_ld + piece.start + row] * kLog2e : 0.0f;
+                    delta[e] = live ? w.delta[head * w.delta_ld + piece.start + row] : 0.0f;
+                }
+                if (!(fine = tc::bar_wait(stats_empty + 8 * st, ((i >> 1) & 1) ^ 1))) break;
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                stats[st * 2 * kTile + e * 32 + lane] = -lse[e];
-                stats[st * 2 * kTile + kTile + e * 32 + lane] = -delta[e];
+                for (int e = 0; e < 4; ++e) {
+                    stats[st * 2 * kTile + e * 32 + lane] = -lse[e];
+                    stats[st * 2 * kTile + kTile + e * 32 + lane] = -delta[e];
+                }
+                __syncwarp();
+                if (lane == 0) tc::bar_arrive(stats_full + 8 * st);
             }
-            __syncwarp();
-            if (lane == 0) tc::bar_arrive(stats_full + 8 * st);
         }
     } else if (warp == 9) {
         const int k_steps = (w.dim + 15) / 16;
@@ -385,123 +489,146 @@ __global__ void __launch_bounds__(kKeyThreads, 1) key_gradient_kernel(const __gr
             if (tc::elected()) tc::commit<1>(bar);
             __syncwarp();
         };
-        auto onto = [&](uint32_t d, uint32_t a, uint32_t b_tile, int i) {             // the rows of the queries' tile i
-            weights_by_rows<0, 8, 32>(d, a, b_tile, wide, (min(kTile, piece.length - (first + i % per) * kTile) + 15) / 16, i > 0);
+        int i = 0, begun = 0, steps = 0;
+        bool opening = false, last = false;                          // of the round before
+        auto score = [&] {
+            const int st = i % kStages;
+            if (!(fine = tc::bar_wait(q_full + 8 * st, (i / kStages) & 1))) return;
+            tc::fence_after();
+            rows_by_rows<D>(tmem + (i % kSets) * kTile, base, queries + st * S::kBytes, k_steps);
+            finished(scores + 8 * (i % kSets));
         };
-        fine = tc::bar_wait(rows_full, 0);
-        // round i: dv of tile i - 1, scores of tile i over its weights; dk of tile i - 1, dp of tile i over its slopes
-        for (int i = 0; i <= n && fine; ++i) {
-            const int st = i % kStages, b = i - 1, sb = b % kStages;
-            const uint32_t parity = (i / kStages) & 1;
-            if (i > 0) {
-                if (!(fine = tc::bar_wait(weights, b & 1))) break;
-                tc::fence_after();
-                onto(dv_at, tmem, douts + sb * S::kBytes, b);
-                finished(d_empty + 8 * sb);
-            }
-            if (i < n) {
-                if (!(fine = tc::bar_wait(q_full + 8 * st, parity))) break;
-                tc::fence_after();
-                rows_by_rows<D>(tmem, base, queries + st * S::kBytes, k_steps);
-                finished(scores);
-            }
-            if (i > 0) {
-                if (!(fine = tc::bar_wait(slopes, b & 1))) break;
-                tc::fence_after();
-                onto(dk_at, products_at, queries + sb * S::kBytes, b);
-                finished(q_empty + 8 * sb);
-            }
-            if (i < n) {
-                if (!(fine = tc::bar_wait(d_full + 8 * st, parity))) break;
-                tc::fence_after();
-                rows_by_rows<D>(products_at, base + S::kBytes, douts + st * S::kBytes, k_steps);
-                finished(products);
+        auto product = [&] {
+            const int st = i % kStages;
+            if (!(fine = tc::bar_wait(d_full + 8 * st, (i / kStages) & 1))) return;
+            tc::fence_after();
+            rows_by_rows<D>(products_at, base + S::kBytes, douts + st * S::kBytes, k_steps);
+            finished(products);
+        };
+        auto gather_v = [&] {
+            const int b = i - 1, sb = b % kStages;
+            if (!(fine = tc::bar_wait(weights, b & 1))) return;
+            tc::fence_after();
+            weights_by_rows<0, 8, 32>(dv_at, tmem + (b % kSets) * kTile, douts + sb * S::kBytes, wide, steps, !opening);
+            finished(d_empty + 8 * sb);
+        };
+        auto gather_k = [&] {
+            const int b = i - 1, sb = b % kStages;
+            if (!(fine = tc::bar_wait(slopes, b & 1))) return;
+            tc::fence_after();
+            weights_by_rows<0, 8, 32>(dk_at, products_at, queries + sb * S::kBytes, wide, steps, !opening);
+            finished(q_empty + 8 * sb);
+            if (last) finished(done);
+        };
+        // A round: dv of the round before, the scores, over its weights where there is one set; dk of the round before, dp over its slopes.
+        while (fine && pieces.take(piece, kv_head, fine)) {
+            divide();
+            begin();
+            for (int r = 0; r < n && fine; ++r, ++i, advance()) {
+                if (r == 0 && !(fine = tc::bar_wait(rows_full, begun++ & 1))) break;
+                if (kSets == 2) score();
+                if (fine && i > 0) gather_v();
+                if (fine && kSets == 1) score();
+                if (fine && i > 0) gather_k();
+                if (fine) product();
+                if (!fine) break;
+                if (r == n - 1) finished(rows_empty);
+                steps = (min(kTile, piece.length - tile * kTile) + 15) / 16;
+                opening = r == 0;
+                last = r == n - 1;
             }
         }
-        if (fine) finished(done);
+        if (fine && i > 0) gather_v();
+        if (fine && i > 0) gather_k();
     } else {
         const int half = warp / 4, quarter = warp % 4;
-        const int key = key0 + quarter * 32 + lane;
         const uint32_t lanes = static_cast<uint32_t>(quarter * 32) << 16;
-        const uint32_t s_at = tmem + half * 64 + lanes, d_at = products_at + half * 64 + lanes;
+        const uint32_t d_at = products_at + half * 64 + lanes;
         const float* stats = reinterpret_cast<const float*>(mem + S::kStats);
-        const float2 cc = make_float2(w.c, w.c);
-        for (int i = 0; i < n; ++i) {
-            const int tile = first + i % per, st = i & 1, valid = piece.length - tile * kTile;
-            const float4* lse = reinterpret_cast<const float4*>(stats + st * 2 * kTile + half * 64);
-            const float4* delta = lse + kTile / 4;
-            const bool masked = valid < kTile || (w.causal && tile == piece.tile);
-            const int low = w.causal ? key - tile * kTile - half * 64 : 0, high = valid - half * 64;  // queries [low, high) of this warp's columns
-            if (!(fine = tc::bar_wait(stats_full + 8 * st, (i >> 1) & 1))) break;
-            if (!(fine = tc::bar_wait(scores, i & 1))) break;
-            tc::fence_after();
-            float s[64];
-            tmem_load64(s_at, s);
+        const float2 cc = twice(w.c);
+        int i = 0, ended = 0;
+        while (fine && pieces.take(piece, kv_head, fine)) {
+            divide();
+            begin();
+            const int key = key0 + quarter * 32 + lane;
+            for (int r = 0; r < n; ++r, ++i, advance()) {
+                const int st = i & 1, valid = piece.length - tile * kTile;
+                const uint32_t s_at = tmem + (i % kSets) * kTile + half * 64 + lanes;
+                const float4* lse = reinterpret_cast<const float4*>(stats + st * 2 * kTile + half * 64);
+                const float4* delta = lse + kTile / 4;
+                const bool masked = valid < kTile || (w.causal && tile == piece.tile);
+                const int low = w.causal ? key - tile * kTile - half * 64 : 0, high = valid - half * 64;     // queries [low, high) of this warp's columns
+                if (!(fine = tc::bar_wait(stats_full + 8 * st, (i >> 1) & 1))) break;
+                if (!(fine = tc::bar_wait(scores + 8 * (i % kSets), (i / kSets) & 1))) break;
+                tc::fence_after();
+                float s[64];
+                tmem_load64(s_at, s);
 #pragma unroll
-            for (int e = 0; e < 64; e += 4) {
-                const float4 x = lse[e / 4];
-                const float2 a = fma2(make_float2(s[e], s[e + 1]), cc, make_float2(x.x, x.y)), b = fma2(make_float2(s[e + 2], s[e + 3]), cc, make_float2(x.z, x.w));
-                s[e] = exp2_fast(a.x);
-                s[e + 1] = exp2_fast(a.y);
-                s[e + 2] = exp2_fast(b.x);
-                s[e + 3] = exp2_fast(b.y);
-            }
-            if (masked) {
+                for (int e = 0; e < 64; e += 4) {
+                    const float4 x = lse[e / 4];
+                    const float2 a = fma2(make_float2(s[e], s[e + 1]), cc, make_float2(x.x, x.y)), b = fma2(make_float2(s[e + 2], s[e + 3]), cc, make_float2(x.z, x.w));
+                    s[e] = exp2_fast(a.x);
+                    s[e + 1] = exp2_fast(a.y);
+                    s[e + 2] = exp2_fast(b.x);
+                    s[e + 3] = exp2_fast(b.y);
+                }
+                if (masked) {
 #pragma unroll
-                for (int e = 0; e < 64; ++e) s[e] = e >= low && e < high ? s[e] : 0.0f;
-                if (valid < kTile) {       // the queries' rows behind the sequence
-                    const int at = i % kStages;
-                    const uint32_t parity = (i / kStages) & 1;
-                    if (!(fine = tc::bar_wait(q_full + 8 * at, parity) && tc::bar_wait(d_full + 8 * at, parity))) break;
-                    clear_rows<D>(mem + (queries - base) + at * S::kBytes, valid, threadIdx.x, 256);
-                    clear_rows<D>(mem + (douts - base) + at * S::kBytes, valid, threadIdx.x, 256);
+                    for (int e = 0; e < 64; ++e) s[e] = e >= low && e < high ? s[e] : 0.0f;
+                    if (valid < kTile) {   // the queries' rows behind the sequence
+                        const int at = i % kStages;
+                        const uint32_t parity = (i / kStages) & 1;
+                        if (!(fine = tc::bar_wait(q_full + 8 * at, parity))) break;
+                        if (!(fine = tc::bar_wait(d_full + 8 * at, parity))) break;
+                        clear_rows<D>(mem + (queries - base) + at * S::kBytes, valid, threadIdx.x, 256);
+                        clear_rows<D>(mem + (douts - base) + at * S::kBytes, valid, threadIdx.x, 256);
+                    }
+                }
+                uint32_t p[32];
+#pragma unroll
+                for (int e = 0; e < 32; ++e) p[e] = pack_bf16(s[2 * e], s[2 * e + 1]);
+                tmem_store32(s_at, p);
+                tmem_stored();
+                tc::fence_before();
+                __syncwarp();
+                if (lane == 0) tc::bar_arrive(weights);
+                if (!(fine = tc::bar_wait(products, i & 1))) break;
+                tc::fence_after();
+                float dp[64];
+                tmem_load64(d_at, dp);
+#pragma unroll
+                for (int e = 0; e < 64; e += 4) {
+                    const float4 x = delta[e / 4];
+                    const float2 a = mul2(add2(make_float2(dp[e], dp[e + 1]), make_float2(x.x, x.y)), make_float2(s[e], s[e + 1]));
+                    const float2 b = mul2(add2(make_float2(dp[e + 2], dp[e + 3]), make_float2(x.z, x.w)), make_float2(s[e + 2], s[e + 3]));
+                    dp[e] = a.x;
+                    dp[e + 1] = a.y;
+                    dp[e + 2] = b.x;
+                    dp[e + 3] = b.y;
+                }
+                if (masked) {
+#pragma unroll
+                    for (int e = 0; e < 64; ++e) dp[e] = e >= low && e < high ? dp[e] : 0.0f;
+                }
+#pragma unroll
+                for (int e = 0; e < 32; ++e) p[e] = pack_bf16(dp[2 * e], dp[2 * e + 1]);
+                tmem_store32(d_at, p);
+                tmem_stored();
+                tc::fence_before();
+                __syncwarp();
+                if (lane == 0) {
+                    tc::bar_arrive(slopes);
+                    tc::bar_arrive(stats_empty + 8 * st);
                 }
             }
-            uint32_t p[32];
-#pragma unroll
-            for (int e = 0; e < 32; ++e) p[e] = pack_bf16(s[2 * e], s[2 * e + 1]);
-            tmem_store32(s_at, p);
-            tmem_stored();
-            tc::fence_before();
-            __syncwarp();
-            if (lane == 0) tc::bar_arrive(weights);
-            if (!(fine = tc::bar_wait(products, i & 1))) break;
-            tc::fence_after();
-            float dp[64];
-            tmem_load64(d_at, dp);
-#pragma unroll
-            for (int e = 0; e < 64; e += 4) {
-                const float4 x = delta[e / 4];
-                const float2 a = mul2(add2(make_float2(dp[e], dp[e + 1]), make_float2(x.x, x.y)), make_float2(s[e], s[e + 1]));
-                const float2 b = mul2(add2(make_float2(dp[e + 2], dp[e + 3]), make_float2(x.z, x.w)), make_float2(s[e + 2], s[e + 3]));
-                dp[e] = a.x;
-                dp[e + 1] = a.y;
-                dp[e + 2] = b.x;
-                dp[e + 3] = b.y;
-            }
-            if (masked) {
-#pragma unroll
-                for (int e = 0; e < 64; ++e) dp[e] = e >= low && e < high ? dp[e] : 0.0f;
-            }
-#pragma unroll
-            for (int e = 0; e < 32; ++e) p[e] = pack_bf16(dp[2 * e], dp[2 * e + 1]);
-            tmem_store32(d_at, p);
-            tmem_stored();
-            tc::fence_before();
-            __syncwarp();
-            if (lane == 0) {
-                tc::bar_arrive(slopes);
-                tc::bar_arrive(stats_empty + 8 * st);
-            }
-        }
-        if (fine) fine = tc::bar_wait(done, 0);
-        if (fine) {
+            if (!fine || !(fine = tc::bar_wait(done, ended++ & 1))) break;
             tc::fence_after();
             constexpr int kHalf = D / 2;
             const bool live = key < piece.length;
             const int64_t at = piece.start + key;
             give_row<kHalf>(dk_at + half * kHalf + lanes, w.scale, w.dk.p + at * w.dk.rs + kv_head * w.dk.hs + half * kHalf, live, w.dim - half * kHalf);
             give_row<kHalf>(dv_at + half * kHalf + lanes, 1.0f, w.dv.p + at * w.dv.rs + kv_head * w.dv.hs + half * kHalf, live, w.dim - half * kHalf);
+            tc::fence_before();
         }
     }
     Finish::end(fine, slot_mem, mark, tmem, warp);
@@ -528,13 +655,15 @@ dlion_status check(const dlion_attention_bwd* p) {
 }
 
 template <int D>
-void launch(prod::Call& c, Backward& w, const Plan* plans, int64_t pieces) {
+void launch(prod::Call& c, Backward& w, const Plan* plans, int64_t pieces, int64_t heads, int64_t kv_heads) {
     prod::raise_shared(c, &query_gradient_kernel<D>, QueryShared<D>::kAll);
     prod::raise_shared(c, &key_gradient_kernel<D>, KeyShared<D>::kAll);
     w.plan = plans[0];
-    prod::start(c, query_gradient_kernel<D>, dim3(static_cast<unsigned>(pieces * w.heads)), dim3(kThreads), QueryShared<D>::kAll, 1, w, c.mark);
+    w.heads = divisor(heads);
+    prod::start(c, query_gradient_kernel<D>, dim3(static_cast<unsigned>(pieces * heads)), dim3(kQueryThreads), QueryShared<D>::kAll, 1, w, c.mark);
     w.plan = plans[1];
-    prod::start(c, key_gradient_kernel<D>, dim3(static_cast<unsigned>(pieces * w.kv_heads)), dim3(kKeyThreads), KeyShared<D>::kAll, 1, w, c.mark);
+    w.heads = divisor(kv_heads);
+    prod::start(c, key_gradient_kernel<D>, dim3(static_cast<unsigned>(pieces * kv_heads)), dim3(kKeyThreads), KeyShared<D>::kAll, 1, w, c.mark);
 }
 
 void backward(prod::Call& c, const dlion_attention_bwd& p) {
@@ -573,9 +702,7 @@ void backward(prod::Call& c, const dlion_attention_bwd& p) {
         c.status = DLION_ECUDA;
         return;
     }
-    w.heads = static_cast<int>(p.heads);
-    w.kv_heads = static_cast<int>(p.kv_heads);
-    w.group = static_cast<int>(p.heads / p.kv_heads);
+    w.group = divisor(p.heads / p.kv_heads);
     w.dim = static_cast<int>(p.dim);
     w.causal = p.causal;
     w.c = p.scale * kLog2e;
@@ -586,7 +713,7 @@ void backward(prod::Call& c, const dlion_attention_bwd& p) {
     w.lse_ld = p.lse_ld;
     w.delta = delta;
     w.delta_ld = p.rows;
-    p.dim <= 64 ? launch<64>(c, w, plans, pieces) : launch<128>(c, w, plans, pieces);
+    p.dim <= 64 ? launch<64>(c, w, plans, pieces, p.heads, p.kv_heads) : launch<128>(c, w, plans, pieces, p.heads, p.kv_heads);
 }
 
 }  // namespace

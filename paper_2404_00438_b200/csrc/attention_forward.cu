@@ -16,7 +16,7 @@ constexpr int64_t kLongSequence = 1024;
 struct Forward {
     CUtensorMap q, k, v;
     Plan plan;
-    int units, dim, causal;
+    int dim, causal;
     Divisor heads, group;
     float c;                               // scale * log2(e)
     Rows out;
@@ -33,7 +33,7 @@ struct ForwardShared {
     static constexpr int kRing = D == 128 && SIDES == 1 ? 2 : 4;     // tiles of keys and values, in turn
     static constexpr uint32_t kStages = (SIDES + kRing) * kBytes;
     static constexpr uint32_t kBars = kStages + 4 * SIDES * kStage;
-    static constexpr uint32_t kAll = kBars + 256 + 1024;
+    static constexpr uint32_t kAll = kBars + 256 + kTurnBytes + 1024;
     static constexpr int kThreads = 128 * SIDES + 64;
     static constexpr uint32_t kColumns = SIDES == 2 ? 512 : 256;     // of tensor memory: scores, outputs, weights
     static constexpr bool kApart = SIDES * (kTile + D + kTile / 2) <= kColumns;       // otherwise weights lie over the scores
@@ -49,6 +49,7 @@ __global__ void __launch_bounds__(ForwardShared<D, SIDES>::kThreads, 3 - SIDES) 
     const uint32_t ring = base + SIDES * S::kBytes, bars = base + S::kBars;
     const uint32_t full = bars, empty = bars + 64, q_full = bars + 128, scores = bars + 144, weights = bars + 160, done = bars + 192,
                    taken = bars + 208, q_empty = bars + 216, slot = bars + 240;
+    const uint32_t turns = bars + 256;
     volatile uint32_t* slot_mem = reinterpret_cast<volatile uint32_t*>(mem + (slot - base));
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
 
@@ -67,6 +68,7 @@ __global__ void __launch_bounds__(ForwardShared<D, SIDES>::kThreads, 3 - SIDES) 
             tc::bar_init(weights + 16 * i + 8, 4);
             tc::bar_init(done + 8 * i, 1);
         }
+        Pieces::init(turns, blockDim.x / 32);
         tc::bar_init_done();
         slot_mem[1] = 0;                   // set when a wait ran out
         tc::prefetch_map(&w.q);
@@ -81,7 +83,7 @@ __global__ void __launch_bounds__(ForwardShared<D, SIDES>::kThreads, 3 - SIDES) 
     bool fine = true;
     tc::wait_for_previous();
 
-    Pieces pieces(w.plan, w.heads, w.units);
+    Pieces pieces(w.plan, w.heads, turns);
     Piece piece{};
     int head = 0;
     // What a piece is made of: tiles of queries (sides) and each side's tiles of keys, taken from the last to the first
@@ -95,11 +97,15 @@ __global__ void __launch_bounds__(ForwardShared<D, SIDES>::kThreads, 3 - SIDES) 
     };
 
     if (warp == kCopying) {
-        int filled = 0, queries = 0, others = 0;                     // tiles asked for: into the ring, of either side
-        while (fine && pieces.take(piece, head)) {
+        int filled = 0, queries = 0, others = 0, asked = 0;                    // tiles asked for: into the ring, of either side
+        while (fine && pieces.take(piece, head, fine)) {
             divide();
             const int kv_head = w.group.quotient(head);
             for (int r = 0; r < most && fine; ++r) {
+                if (r == most - 1) {
+                    asked = pieces.turn;
+                    if (!(fine = pieces.ask())) break;
+                }
                 const int row = piece.start + (most - 1 - r) * kTile;
                 for (int kind = 0; kind < 2; ++kind, ++filled) {
                     const int st = filled % kRing;
@@ -128,6 +134,7 @@ __global__ void __launch_bounds__(ForwardShared<D, SIDES>::kThreads, 3 - SIDES) 
             }
         }
         if (!fine) {                       // what was asked for still lands in this block's memory: it is awaited
+            pieces.settle(asked);
             if (queries > 0) tc::bar_wait(q_full, (queries - 1) & 1);
             if (others > 0) tc::bar_wait(q_full + 8, (others - 1) & 1);
             for (int i = max(0, filled - kRing); i < filled; ++i) tc::bar_wait(full + 8 * (i % kRing), (i / kRing) & 1);
@@ -177,7 +184,7 @@ __global__ void __launch_bounds__(ForwardShared<D, SIDES>::kThreads, 3 - SIDES) 
         // A round: the scores of a tile of keys, and the weighted values of the round before it.  Where weights lie over the scores
         // these come first, and one side after the other, so that a side's products run while the other's exponentials do
         // (with a warp to issue each side's, both sides' came to run and to wait together: a quarter slower).
-        while (fine && pieces.take(piece, head)) {
+        while (fine && pieces.take(piece, head, fine)) {
             divide();
             for (int r = 0; r < most && fine; ++r, ++round) {
                 if (round > 0 && !(fine = filled(2 * round - 1))) break;
@@ -218,7 +225,7 @@ __global__ void __launch_bounds__(ForwardShared<D, SIDES>::kThreads, 3 - SIDES) 
         const uint32_t p_at = S::kApart ? tmem + kTile + D + lanes : s_at;
         const float c = w.c;
         int round = 0, scored = 0, ended = 0;                        // rounds of all pieces; this side's tiles; its pieces
-        while (fine && pieces.take(piece, head)) {
+        while (fine && pieces.take(piece, head, fine)) {
             divide();
             const int n = side ? n1 : n0;
             const int row = row0 + side * kTile + quarter * 32 + lane;                // in the sequence
@@ -360,9 +367,8 @@ int sides_of(const dlion_attention_fwd& p) {
 template <int D, int SIDES>
 void launch(prod::Call& c, Forward& w, int64_t pieces) {
     using S = ForwardShared<D, SIDES>;
-    w.units = static_cast<int>(pieces * w.heads.d);
     prod::raise_shared(c, &attend_kernel<D, SIDES>, S::kAll);
-    prod::start(c, attend_kernel<D, SIDES>, dim3(static_cast<unsigned>(std::min(w.units, (3 - SIDES) * c.sms))), dim3(S::kThreads), S::kAll, 1, w, c.mark);
+    prod::start(c, attend_kernel<D, SIDES>, dim3(static_cast<unsigned>(pieces * w.heads.d)), dim3(S::kThreads), S::kAll, 1, w, c.mark);
 }
 
 void forward(prod::Call& c, const dlion_attention_fwd& p) {

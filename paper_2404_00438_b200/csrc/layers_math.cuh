@@ -147,4 +147,39 @@ __device__ __forceinline__ void widen(const uint4& w, float (&v)[8]) {
     }
 }
 
+// ---- pairs of binary32 values: one instruction for two (in the time of two: it saves issue slots)
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+    float2 r;
+    asm("{\n.reg .b64 a, b, c, d;\nmov.b64 a, {%2, %3};\nmov.b64 b, {%4, %5};\nmov.b64 c, {%6, %7};\n"
+        "fma.rn.f32x2 d, a, b, c;\nmov.b64 {%0, %1}, d;\n}"
+        : "=f"(r.x), "=f"(r.y)
+        : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
+    return r;
+}
+
+__device__ __forceinline__ float2 add2(float2 a, float2 b) {
+    float2 r;
+    asm("{\n.reg .b64 a, b, d;\nmov.b64 a, {%2, %3};\nmov.b64 b, {%4, %5};\nadd.rn.f32x2 d, a, b;\nmov.b64 {%0, %1}, d;\n}"
+        : "=f"(r.x), "=f"(r.y)
+        : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+    return r;
+}
+
+__device__ __forceinline__ float2 mul2(float2 a, float2 b) {
+    float2 r;
+    asm("{\n.reg .b64 a, b, d;\nmov.b64 a, {%2, %3};\nmov.b64 b, {%4, %5};\nmul.rn.f32x2 d, a, b;\nmov.b64 {%0, %1}, d;\n}"
+        : "=f"(r.x), "=f"(r.y)
+        : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+    return r;
+}
+
+__device__ __forceinline__ float2 twice(float v) { return make_float2(v, v); }
+
+__device__ __forceinline__ void widen(const uint4& w, float2 (&v)[4]) {
+    v[0] = make_float2(bf16_lo(w.x), bf16_hi(w.x));
+    v[1] = make_float2(bf16_lo(w.y), bf16_hi(w.y));
+    v[2] = make_float2(bf16_lo(w.z), bf16_hi(w.z));
+    v[3] = make_float2(bf16_lo(w.w), bf16_hi(w.w));
+}
+
 }  // namespace dlion

@@ -16,7 +16,10 @@ using namespace dlion::prod;
 using bf16 = __nv_bfloat16;
 
 constexpr int64_t kMost = int64_t{1} << 30;
-constexpr int kBlock = 256;
+constexpr int kBlock = 256, kWarpColumns = 2048;
+constexpr int kRowsThreads = 512, kManyRows = 32;                   // rows an SM, from which on blocks stay
+constexpr int kBackThreads = 512;          // 128 registers a thread: a row's values and sums for as many columns
+
 
 bool type_ok(int t) { return t == DLION_GRAD_F32 || t == DLION_GRAD_BF16; }
 int type_bytes(int t) { return t == DLION_GRAD_F32 ? 4 : 2; }
@@ -28,51 +31,68 @@ struct Eight;
 template <>
 struct Eight<bf16> {
     uint4 w;
-    __device__ __forceinline__ void get(float (&v)[8]) const { widen(w, v); }
+    __device__ __forceinline__ void get(float2 (&v)[4]) const { widen(w, v); }
 };
 template <>
 struct Eight<float> {
-    float v8[8];
-    __device__ __forceinline__ void get(float (&v)[8]) const {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = v8[i];
+    float4 a, b;
+    __device__ __forceinline__ void get(float2 (&v)[4]) const {
+        v[0] = make_float2(a.x, a.y);
+        v[1] = make_float2(a.z, a.w);
+        v[2] = make_float2(b.x, b.y);
+        v[3] = make_float2(b.z, b.w);
     }
 };
 
-// The columns of thread t of a row's g threads.  WIDE: eight adjacent ones at a time, by 16-byte accesses.  Otherwise (rows off the
-// 16-byte grid) single ones, g apart, so that a warp's accesses are adjacent.
-template <bool WIDE>
+// The columns of thread t of a row's G threads (0: `g`, known at run time).  WIDE: eight adjacent ones at a time, by 16-byte accesses.
+// Otherwise (rows off the 16-byte grid) single ones, G apart, so that a warp's accesses are adjacent.
+template <bool WIDE, int G>
 struct Columns {
-    int64_t n;
-    int t, g;
-    __device__ __forceinline__ int64_t at(int c, int e) const { return WIDE ? (static_cast<int64_t>(c) * g + t) * 8 + e : (static_cast<int64_t>(c) * 8 + e) * g + t; }
+    int n, t, g;
+    __device__ __forceinline__ int threads() const { return G != 0 ? G : g; }
+    __device__ __forceinline__ int at(int c, int e) const { return WIDE ? (c * threads() + t) * 8 + e : (c * 8 + e) * threads() + t; }
+    __device__ __forceinline__ bool whole(int c) const { return (c + 1) * 8 * threads() <= n; }    // for every thread of the row
+    __device__ __forceinline__ bool has(int c, int e) const { return at(c, e) < n; }
 
     __device__ __forceinline__ void load(const bf16* p, int c, Eight<bf16>& o) const {
         if (WIDE) {
-            o.w = at(c, 0) < n ? *reinterpret_cast<const uint4*>(p + at(c, 0)) : make_uint4(0, 0, 0, 0);
+            o.w = has(c, 0) ? *reinterpret_cast<const uint4*>(p + at(c, 0)) : make_uint4(0, 0, 0, 0);
         } else {
+            const uint16_t* q = reinterpret_cast<const uint16_t*>(p);
             uint32_t w[8];
+            if (whole(c)) {
 #pragma unroll
-            for (int e = 0; e < 8; ++e) w[e] = at(c, e) < n ? reinterpret_cast<const uint16_t*>(p)[at(c, e)] : 0u;
+                for (int e = 0; e < 8; ++e) w[e] = q[at(c, e)];
+            } else {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) w[e] = has(c, e) ? q[at(c, e)] : 0u;
+            }
             o.w = make_uint4(w[0] | w[1] << 16, w[2] | w[3] << 16, w[4] | w[5] << 16, w[6] | w[7] << 16);
         }
     }
     __device__ __forceinline__ void load(const float* p, int c, Eight<float>& o) const {
         if (WIDE) {
-            const bool in = at(c, 0) < n;
+            const bool in = has(c, 0);
             const float4* q = reinterpret_cast<const float4*>(p + at(c, 0));
-            const float4 a = in ? q[0] : make_float4(0, 0, 0, 0), b = in ? q[1] : make_float4(0, 0, 0, 0);
-            o.v8[0] = a.x, o.v8[1] = a.y, o.v8[2] = a.z, o.v8[3] = a.w;
-            o.v8[4] = b.x, o.v8[5] = b.y, o.v8[6] = b.z, o.v8[7] = b.w;
+            o.a = in ? q[0] : make_float4(0, 0, 0, 0);
+            o.b = in ? q[1] : make_float4(0, 0, 0, 0);
         } else {
+            float v[8];
+            if (whole(c)) {
 #pragma unroll
-            for (int e = 0; e < 8; ++e) o.v8[e] = at(c, e) < n ? p[at(c, e)] : 0.0f;
+                for (int e = 0; e < 8; ++e) v[e] = p[at(c, e)];
+            } else {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) v[e] = has(c, e) ? p[at(c, e)] : 0.0f;
+            }
+            o.a = make_float4(v[0], v[1], v[2], v[3]);
+            o.b = make_float4(v[4], v[5], v[6], v[7]);
         }
     }
     // eight values of a vector of either type (`other` where there is none)
-    __device__ __forceinline__ void vector(const void* p, int f32, int c, float other, float (&v)[8]) const {
+    __device__ __forceinline__ void vector(const void* p, int f32, int c, float other, float2 (&v)[4]) const {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = other;
+        for (int e = 0; e < 4; ++e) v[e] = twice(other);
         if (p == nullptr) return;
         if (f32) {
             Eight<float> o;
@@ -84,57 +104,66 @@ struct Columns {
             o.get(v);
         }
     }
-    __device__ __forceinline__ void store(bf16* p, int c, const float (&v)[8]) const {
+    __device__ __forceinline__ void store(bf16* p, int c, const float2 (&v)[4]) const {
         if (WIDE) {
-            if (at(c, 0) < n) {
-                *reinterpret_cast<uint4*>(p + at(c, 0)) = make_uint4(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7]));
+            if (has(c, 0)) {
+                *reinterpret_cast<uint4*>(p + at(c, 0)) = make_uint4(pack_bf16(v[0].x, v[0].y), pack_bf16(v[1].x, v[1].y), pack_bf16(v[2].x, v[2].y), pack_bf16(v[3].x, v[3].y));
             }
         } else {
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                if (at(c, e) < n) p[at(c, e)] = __float2bfloat16_rn(v[e]);
+                if (has(c, e)) p[at(c, e)] = __float2bfloat16_rn(e % 2 ? v[e / 2].y : v[e / 2].x);
             }
         }
     }
-    __device__ __forceinline__ void store(float* p, int c, const float (&v)[8]) const {
+    __device__ __forceinline__ void store(float* p, int c, const float2 (&v)[4]) const {
         if (WIDE) {
-            if (at(c, 0) < n) {
+            if (has(c, 0)) {
                 float4* q = reinterpret_cast<float4*>(p + at(c, 0));
-                q[0] = make_float4(v[0], v[1], v[2], v[3]);
-                q[1] = make_float4(v[4], v[5], v[6], v[7]);
+                q[0] = make_float4(v[0].x, v[0].y, v[1].x, v[1].y);
+                q[1] = make_float4(v[2].x, v[2].y, v[3].x, v[3].y);
             }
         } else {
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                if (at(c, e) < n) p[at(c, e)] = v[e];
+                if (has(c, e)) p[at(c, e)] = e % 2 ? v[e / 2].y : v[e / 2].x;
             }
+        }
+    }
+    // differences from the mean; 0 in columns that are not there
+    __device__ __forceinline__ void centre(int c, float mean, float2 (&v)[4]) const {
+        const bool full = WIDE ? has(c, 0) : whole(c);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            v[e] = add2(v[e], twice(-mean));
+            if (!full) v[e] = make_float2(has(c, 2 * e) ? v[e].x : 0.0f, has(c, 2 * e + 1) ? v[e].y : 0.0f);
         }
     }
 };
 
-// Sums over the g threads of a row (a power of two, 32 at least); every thread of the block calls it.
-__device__ __forceinline__ float2 row_sum(float2 v, int g, float2* shared) {
+// Sums over the g threads of a row (a power of two, 32 at least), which are neighbours in the block and all call it.  `shared`: 32 values
+// a block and turn; two turns, so that one barrier a sum is enough.
+__device__ __forceinline__ float2 row_sum(float2 v, int g, float2 (*shared)[32], int turn) {
 #pragma unroll
     for (int d = 16; d >= 1; d /= 2) {
         v.x += __shfl_xor_sync(0xffffffffu, v.x, d);
         v.y += __shfl_xor_sync(0xffffffffu, v.y, d);
     }
     if (g == 32) return v;
-    const int warp = threadIdx.x / 32, each = g / 32;
-    __syncthreads();                       // the last sums have been read
-    if (threadIdx.x % 32 == 0) shared[warp] = v;
-    __syncthreads();
-    const float2* from = shared + warp / each * each;
-    v = from[0];
+    const int warp = threadIdx.x / 32, each = g / 32, first = warp / each * each;
+    if (threadIdx.x % 32 == 0) shared[turn & 1][warp] = v;
+    asm volatile("bar.sync %0, %1;" ::"r"(1 + warp / each), "r"(g) : "memory");
+    v = shared[turn & 1][first];
     for (int i = 1; i < each; ++i) {
-        v.x += from[i].x;
-        v.y += from[i].y;
+        v.x += shared[turn & 1][first + i].x;
+        v.y += shared[turn & 1][first + i].y;
     }
     return v;
 }
 
 struct Norm {
-    int64_t m, n;
+    int64_t m;
+    int n;
     const void* x;
     int64_t x_ld;
     const void *w, *b;
@@ -146,41 +175,26 @@ struct Norm {
     int g;                                 // threads a row
 };
 
-// A row's CHUNKS x 8 values a thread stay in registers between the two sums of the variance.
-template <class X, class Y, bool WIDE, int CHUNKS>
-__global__ void __launch_bounds__(1024) norm_kernel(const __grid_constant__ Norm a) {
-    __shared__ float2 sums[32];
-    tc::let_next_start();
-    tc::wait_for_previous();
-    const int per = blockDim.x / a.g;
-    const int64_t row = static_cast<int64_t>(blockIdx.x) * per + threadIdx.x / a.g;
-    const bool live = row < a.m;
-    const Columns<WIDE> cols{live ? a.n : 0, static_cast<int>(threadIdx.x) & (a.g - 1), a.g};
-    const X* x = static_cast<const X*>(a.x) + row * a.x_ld;
-    Eight<X> held[CHUNKS];
-#pragma unroll
-    for (int c = 0; c < CHUNKS; ++c) cols.load(x, c, held[c]);
-    float s = 0.0f;
+// A row's CHUNKS x 8 values a thread, between the two sums of its variance.
+template <class X, class Y, bool WIDE, int CHUNKS, int G, class F>
+__device__ __forceinline__ void norm_row(const Norm& a, const Columns<WIDE, G>& cols, int g, float2 (*sums)[32], int turn, int64_t row, bool live,
+                                         const Eight<X> (&held)[CHUNKS], F weights) {
+    float2 v[CHUNKS][4], s = twice(0.0f);
 #pragma unroll
     for (int c = 0; c < CHUNKS; ++c) {
-        float v[8];
-        held[c].get(v);
+        held[c].get(v[c]);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) s += v[e];
+        for (int e = 0; e < 4; ++e) s = add2(s, v[c][e]);
     }
-    const float n = static_cast<float>(a.n), mean = row_sum(make_float2(s, 0.0f), a.g, sums).x / n;
-    s = 0.0f;
+    const float n = static_cast<float>(a.n), mean = row_sum(make_float2(s.x + s.y, 0.0f), g, sums, turn).x / n;
+    s = twice(0.0f);
 #pragma unroll
     for (int c = 0; c < CHUNKS; ++c) {
-        float v[8];
-        held[c].get(v);
+        cols.centre(c, mean, v[c]);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            const float d = v[e] - mean;
-            if (cols.at(c, e) < cols.n) s = __fmaf_rn(d, d, s);
-        }
+        for (int e = 0; e < 4; ++e) s = fma2(v[c][e], v[c][e], s);
     }
-    const float rstd = 1.0f / sqrtf(row_sum(make_float2(s, 0.0f), a.g, sums).x / n + a.eps);
+    const float rstd = 1.0f / sqrtf(row_sum(make_float2(s.x + s.y, 0.0f), g, sums, turn + 1).x / n + a.eps);
     if (!live) return;
     if (cols.t == 0) {
         a.stats[row] = mean;
@@ -189,70 +203,124 @@ __global__ void __launch_bounds__(1024) norm_kernel(const __grid_constant__ Norm
     Y* y = static_cast<Y*>(a.y) + row * a.y_ld;
 #pragma unroll
     for (int c = 0; c < CHUNKS; ++c) {
-        float v[8], w[8], b[8];
-        held[c].get(v);
+        float2 w[4], b[4];
+        weights(c, w, b);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[c][e] = fma2(mul2(v[c][e], twice(rstd)), w[e], b[e]);
+        cols.store(y, c, v[c]);
+    }
+}
+
+// Few rows, or wide ones: a set of rows a block.  Up to 2048 columns a warp has a row (G = 32), and no barrier.
+template <class X, class Y, bool WIDE, int CHUNKS, int G>
+__global__ void __launch_bounds__(G != 0 ? 128 : 1024) norm_kernel(const __grid_constant__ Norm a) {
+    __shared__ float2 sums[2][32];
+    tc::let_next_start();
+    tc::wait_for_previous();
+    const int g = G != 0 ? G : a.g;
+    const int64_t row = static_cast<int64_t>(blockIdx.x) * (blockDim.x / g) + threadIdx.x / g;
+    const bool live = row < a.m;
+    const Columns<WIDE, G> cols{live ? a.n : 0, static_cast<int>(threadIdx.x) & (g - 1), g};
+    Eight<X> held[CHUNKS];
+#pragma unroll
+    for (int c = 0; c < CHUNKS; ++c) cols.load(static_cast<const X*>(a.x) + row * a.x_ld, c, held[c]);
+    norm_row<X, Y, WIDE, CHUNKS, G>(a, cols, g, sums, 0, row, live, held, [&](int c, float2 (&w)[4], float2 (&b)[4]) {
+        cols.vector(a.w, a.w_f32, c, 1.0f, w);
+        cols.vector(a.b, a.b_f32, c, 0.0f, b);
+    });
+}
+
+// Many rows of up to 2048 columns: as many blocks as there is room for, a warp for every so many-th row, its next row on its way while it
+// works on this one; weight and bias in shared memory, as binary32 and in the order in which the threads want them.
+template <class X, class Y, bool WIDE, int CHUNKS>
+__global__ void __launch_bounds__(kRowsThreads, 1) norm_rows_kernel(const __grid_constant__ Norm a) {
+    extern __shared__ float4 vectors[];    // [CHUNKS][4][32]: w, b of two columns
+    tc::let_next_start();
+    tc::wait_for_previous();
+    const int lane = threadIdx.x % 32, warp = threadIdx.x / 32, warps = kRowsThreads / 32;
+    const Columns<WIDE, 32> cols{a.n, lane, 32};
+    const int64_t step = static_cast<int64_t>(gridDim.x) * warps;
+    int64_t row = static_cast<int64_t>(blockIdx.x) * warps + warp;
+    Eight<X> now[CHUNKS], next[CHUNKS];
+    auto load = [&](int64_t r, Eight<X> (&to)[CHUNKS]) {
+        if (r >= a.m) return;
+#pragma unroll
+        for (int c = 0; c < CHUNKS; ++c) cols.load(static_cast<const X*>(a.x) + r * a.x_ld, c, to[c]);
+    };
+    load(row, now);
+    for (int c = warp; c < CHUNKS; c += warps) {
+        float2 w[4], b[4];
         cols.vector(a.w, a.w_f32, c, 1.0f, w);
         cols.vector(a.b, a.b_f32, c, 0.0f, b);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = __fmaf_rn((v[e] - mean) * rstd, w[e], b[e]);
-        cols.store(y, c, v);
+        for (int e = 0; e < 4; ++e) vectors[(c * 4 + e) * 32 + lane] = make_float4(w[e].x, w[e].y, b[e].x, b[e].y);
+    }
+    __syncthreads();
+    for (; row < a.m; row += step) {
+        load(row + step, next);
+        norm_row<X, Y, WIDE, CHUNKS, 32>(a, cols, 32, nullptr, 0, row, true, now, [&](int c, float2 (&w)[4], float2 (&b)[4]) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const float4 x = vectors[(c * 4 + e) * 32 + lane];
+                w[e] = make_float2(x.x, x.y);
+                b[e] = make_float2(x.z, x.w);
+            }
+        });
+#pragma unroll
+        for (int c = 0; c < CHUNKS; ++c) now[c] = next[c];
     }
 }
 
 // Rows too wide for registers: a block reads its row three times.
 template <class X, class Y, bool WIDE>
 __global__ void __launch_bounds__(1024) norm_long_kernel(const __grid_constant__ Norm a) {
-    __shared__ float2 sums[32];
+    __shared__ float2 sums[2][32];
     tc::let_next_start();
     tc::wait_for_previous();
     const int64_t row = blockIdx.x;
-    const Columns<WIDE> cols{a.n, static_cast<int>(threadIdx.x), a.g};
+    const Columns<WIDE, 1024> cols{a.n, static_cast<int>(threadIdx.x), 1024};
     const X* x = static_cast<const X*>(a.x) + row * a.x_ld;
-    const int chunks = static_cast<int>((a.n + a.g * 8 - 1) / (a.g * 8));
+    const int chunks = (a.n + 8191) / 8192;
     const float n = static_cast<float>(a.n);
-    float s = 0.0f;
-    for (int c = 0; c < chunks; ++c) {
+    float2 s = twice(0.0f), v[4];
+    auto take = [&](int c) {
         Eight<X> o;
-        float v[8];
         cols.load(x, c, o);
         o.get(v);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) s += v[e];
-    }
-    const float mean = row_sum(make_float2(s, 0.0f), a.g, sums).x / n;
-    s = 0.0f;
+    };
     for (int c = 0; c < chunks; ++c) {
-        Eight<X> o;
-        float v[8];
-        cols.load(x, c, o);
-        o.get(v);
+        take(c);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            const float d = v[e] - mean;
-            if (cols.at(c, e) < a.n) s = __fmaf_rn(d, d, s);
-        }
+        for (int e = 0; e < 4; ++e) s = add2(s, v[e]);
     }
-    const float rstd = 1.0f / sqrtf(row_sum(make_float2(s, 0.0f), a.g, sums).x / n + a.eps);
+    const float mean = row_sum(make_float2(s.x + s.y, 0.0f), 1024, sums, 0).x / n;
+    s = twice(0.0f);
+    for (int c = 0; c < chunks; ++c) {
+        take(c);
+        cols.centre(c, mean, v);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) s = fma2(v[e], v[e], s);
+    }
+    const float rstd = 1.0f / sqrtf(row_sum(make_float2(s.x + s.y, 0.0f), 1024, sums, 1).x / n + a.eps);
     if (threadIdx.x == 0) {
         a.stats[row] = mean;
         a.stats[a.m + row] = rstd;
     }
     Y* y = static_cast<Y*>(a.y) + row * a.y_ld;
     for (int c = 0; c < chunks; ++c) {
-        Eight<X> o;
-        float v[8], w[8], b[8];
-        cols.load(x, c, o);
-        o.get(v);
+        float2 w[4], b[4];
+        take(c);
         cols.vector(a.w, a.w_f32, c, 1.0f, w);
         cols.vector(a.b, a.b_f32, c, 0.0f, b);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = __fmaf_rn((v[e] - mean) * rstd, w[e], b[e]);
+        for (int e = 0; e < 4; ++e) v[e] = fma2(mul2(add2(v[e], twice(-mean)), twice(rstd)), w[e], b[e]);
         cols.store(y, c, v);
     }
 }
 
 struct NormBack {
-    int64_t m, n;
+    int64_t m;
+    int n;
     const void* dy;
     int64_t dy_ld;
     const void* x;
@@ -268,121 +336,202 @@ struct NormBack {
     int g;
 };
 
-// A block takes every gridDim.x-th set of rows and keeps its share of dw and db in registers; the rows' sums are added in the
-// order of the block's rows, the blocks' in the order of the blocks (norm_sums_kernel): the same result every time.
+__device__ __forceinline__ void copy16(void* to, const void* from, bool there) {       // 16 bytes, zero where they are not there
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(tc::smem_addr(to)), "l"(from), "r"(there ? 16 : 0) : "memory");
+}
+
+// What a thread has of a row, and how its next rows come.  On the 16-byte grid they come through shared memory, DEPTH rows ahead
+// (each thread copies and reads only its own 16 bytes, so that it waits for nobody); elsewhere into registers, at once.
 template <class X, class Y, bool WIDE, int CHUNKS>
-__global__ void __launch_bounds__(512) norm_backward_kernel(const __grid_constant__ NormBack a) {
-    extern __shared__ float total[];       // [2][n]
-    __shared__ float2 sums[32];
+struct NormRow {
+    Eight<X> x[CHUNKS], r[CHUNKS];
+    Eight<Y> dy[CHUNKS];
+    float mean, rstd;
+    static constexpr int kUnits = CHUNKS * (4 * sizeof(X) + 2 * sizeof(Y)) / 4;       // of 16 bytes a row
+    static constexpr int kFit = 24 / kUnits;                         // rows a thread in some 200 KB
+    static constexpr int kDepth = !WIDE ? 1 : kFit > 4 ? 4 : kFit > 2 ? kFit : 2;
+
+    template <class C>
+    __device__ __forceinline__ void ask(const NormBack& a, const C& all, int64_t row, uint4* ring, int stage) const {
+        if (!WIDE) return;
+        const int threads = static_cast<int>(blockDim.x);
+        uint4* to = ring + stage * kUnits * threads + threadIdx.x;
+        auto copy = [&](const auto* p, int c) {
+            constexpr int kParts = sizeof(*p) / 2;
+            const bool there = row < a.m && all.has(c, 0);
+#pragma unroll
+            for (int i = 0; i < kParts; ++i, to += threads) copy16(to, there ? reinterpret_cast<const uint4*>(p + all.at(c, 0)) + i : reinterpret_cast<const uint4*>(a.x), there);
+        };
+#pragma unroll
+        for (int c = 0; c < CHUNKS; ++c) {
+            copy(static_cast<const X*>(a.x) + row * a.x_ld, c);
+            copy(static_cast<const Y*>(a.dy) + row * a.dy_ld, c);
+            if (a.residual != nullptr) copy(static_cast<const X*>(a.residual) + row * a.r_ld, c);
+        }
+        asm volatile("cp.async.commit_group;" ::: "memory");
+    }
+
+    template <class C>
+    __device__ __forceinline__ void take(const NormBack& a, const C& all, int64_t row, const uint4* ring, int stage) {
+        const bool live = row < a.m;
+        mean = live ? a.stats[row] : 0.0f;
+        rstd = live ? a.stats[a.m + row] : 0.0f;                     // a row that is not there: h = 0, dy = 0
+        if (!WIDE) {
+            const C cols{live ? all.n : 0, all.t, all.g};
+#pragma unroll
+            for (int c = 0; c < CHUNKS; ++c) {
+                cols.load(static_cast<const X*>(a.x) + row * a.x_ld, c, x[c]);
+                cols.load(static_cast<const Y*>(a.dy) + row * a.dy_ld, c, dy[c]);
+                if (a.residual != nullptr) cols.load(static_cast<const X*>(a.residual) + row * a.r_ld, c, r[c]);
+            }
+            return;
+        }
+        asm volatile("cp.async.wait_group %0;" ::"n"(kDepth - 1) : "memory");
+        const int threads = static_cast<int>(blockDim.x);
+        const uint4* from = ring + stage * kUnits * threads + threadIdx.x;
+        auto read = [&](auto& to) {
+            uint4* t = reinterpret_cast<uint4*>(&to);
+#pragma unroll
+            for (int i = 0; i < static_cast<int>(sizeof(to) / 16); ++i, from += threads) t[i] = *from;
+        };
+#pragma unroll
+        for (int c = 0; c < CHUNKS; ++c) {
+            read(x[c]);
+            read(dy[c]);
+            if (a.residual != nullptr) read(r[c]);
+        }
+    }
+};
+
+// A block takes every gridDim.x-th set of rows and keeps its share of dw and db in registers; the rows' sums are added in the order of
+// the block's rows, the blocks' in the order of the blocks (norm_sums_kernel): the same result every time.
+template <class X, class Y, bool WIDE, int CHUNKS, int G>
+__global__ void __launch_bounds__(kBackThreads, 1) norm_backward_kernel(const __grid_constant__ NormBack a) {
+    extern __shared__ uint4 memory[];      // rows on their way; at the end [2][n], the block's dw and db
+    __shared__ float2 sums[2][32];
+    using Row = NormRow<X, Y, WIDE, CHUNKS>;
     tc::let_next_start();
     tc::wait_for_previous();
-    const int per = blockDim.x / a.g, group = threadIdx.x / a.g;
-    const Columns<WIDE> all{a.n, static_cast<int>(threadIdx.x) & (a.g - 1), a.g};
+    const int g = G != 0 ? G : a.g, per = blockDim.x / g, group = threadIdx.x / g;
+    const Columns<WIDE, G> all{a.n, static_cast<int>(threadIdx.x) & (g - 1), g};
     const float n = static_cast<float>(a.n);
-    float dw[CHUNKS][8] = {}, db[CHUNKS][8] = {};
-    for (int64_t first = static_cast<int64_t>(blockIdx.x) * per; first < a.m; first += static_cast<int64_t>(gridDim.x) * per) {
+    const float share = 1.0f / n;
+    float2 dw[CHUNKS][4] = {}, db[CHUNKS][4] = {}, w[CHUNKS][4];
+    const int64_t step = static_cast<int64_t>(gridDim.x) * per;
+    Row now;
+#pragma unroll
+    for (int i = 0; i + 1 < Row::kDepth; ++i) now.ask(a, all, static_cast<int64_t>(blockIdx.x) * per + group + i * step, memory, i);
+#pragma unroll
+    for (int c = 0; c < CHUNKS; ++c) all.vector(a.w, a.w_f32, c, 1.0f, w[c]);
+    int turn = 0, stage = 0;
+    for (int64_t first = static_cast<int64_t>(blockIdx.x) * per; first < a.m; first += step, ++turn) {
         const int64_t row = first + group;
         const bool live = row < a.m;
-        const Columns<WIDE> cols{live ? a.n : 0, all.t, a.g};
-        Eight<X> x[CHUNKS], r[CHUNKS];
-        Eight<Y> dy[CHUNKS];
+        now.ask(a, all, row + (Row::kDepth - 1) * step, memory, stage == 0 ? Row::kDepth - 1 : stage - 1);
+        now.take(a, all, row, memory, stage);
+        stage = stage + 1 == Row::kDepth ? 0 : stage + 1;
+        float2 h[CHUNKS][4], u[CHUNKS][4], sx = twice(0.0f), sy = twice(0.0f);
 #pragma unroll
         for (int c = 0; c < CHUNKS; ++c) {
-            cols.load(static_cast<const X*>(a.x) + row * a.x_ld, c, x[c]);
-            cols.load(static_cast<const Y*>(a.dy) + row * a.dy_ld, c, dy[c]);
-            if (a.residual != nullptr) cols.load(static_cast<const X*>(a.residual) + row * a.r_ld, c, r[c]);
-        }
-        const float mean = live ? a.stats[row] : 0.0f, rstd = live ? a.stats[a.m + row] : 0.0f;
-        float2 s = make_float2(0.0f, 0.0f);
+            now.x[c].get(h[c]);
+            now.dy[c].get(u[c]);
 #pragma unroll
-        for (int c = 0; c < CHUNKS; ++c) {
-            float v[8], d[8], w[8];
-            x[c].get(v);
-            dy[c].get(d);
-            all.vector(a.w, a.w_f32, c, 1.0f, w);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const bool in = cols.at(c, e) < cols.n;
-                const float h = in ? (v[e] - mean) * rstd : 0.0f, u = w[e] * d[e];
-                dw[c][e] = __fmaf_rn(d[e], h, dw[c][e]);
-                db[c][e] += d[e];
-                s.x += u;
-                s.y = __fmaf_rn(u, h, s.y);
+            for (int e = 0; e < 4; ++e) {  // a column that is not there has dy = 0
+                h[c][e] = mul2(add2(h[c][e], twice(-now.mean)), twice(now.rstd));
+                dw[c][e] = fma2(u[c][e], h[c][e], dw[c][e]);
+                db[c][e] = add2(db[c][e], u[c][e]);
+                u[c][e] = mul2(u[c][e], w[c][e]);
+                sx = add2(sx, u[c][e]);
+                sy = fma2(u[c][e], h[c][e], sy);
             }
         }
         if (a.dx == nullptr) continue;
-        s = row_sum(s, a.g, sums);
-        const float along = s.x / n, turn = s.y / n;
+        const float2 s = row_sum(make_float2(sx.x + sx.y, sy.x + sy.y), g, sums, turn);
+        const float2 along = twice(-s.x * share), turned = twice(-s.y * share);
+        const Columns<WIDE, G> cols{live ? a.n : 0, all.t, g};
 #pragma unroll
         for (int c = 0; c < CHUNKS; ++c) {
-            float v[8], d[8], w[8], skip[8] = {};
-            x[c].get(v);
-            dy[c].get(d);
-            all.vector(a.w, a.w_f32, c, 1.0f, w);
-            if (a.residual != nullptr) r[c].get(skip);
+            float2 skip[4] = {};
+            if (a.residual != nullptr) now.r[c].get(skip);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const float h = (v[e] - mean) * rstd;
-                v[e] = __fmaf_rn(rstd, __fmaf_rn(-h, turn, __fmaf_rn(w[e], d[e], -along)), skip[e]);
-            }
-            cols.store(static_cast<X*>(a.dx) + row * a.dx_ld, c, v);
+            for (int e = 0; e < 4; ++e) u[c][e] = fma2(twice(now.rstd), fma2(h[c][e], turned, add2(u[c][e], along)), skip[e]);
+            cols.store(static_cast<X*>(a.dx) + row * a.dx_ld, c, u[c]);
         }
     }
+    if (WIDE) asm volatile("cp.async.wait_all;" ::: "memory");
     if (a.parts == nullptr) return;
+    float* total = reinterpret_cast<float*>(memory);
+    __syncthreads();
     for (int i = 0; i < per; ++i) {
         if (group == i) {
 #pragma unroll
             for (int c = 0; c < CHUNKS; ++c) {
+                if (WIDE) {
+                    if (!all.has(c, 0)) continue;
+                    float4 *pw = reinterpret_cast<float4*>(total + all.at(c, 0)), *pb = reinterpret_cast<float4*>(total + a.n + all.at(c, 0));
 #pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const int64_t at = all.at(c, e);
-                    if (at >= a.n) continue;
-                    total[at] = i == 0 ? dw[c][e] : total[at] + dw[c][e];
-                    total[a.n + at] = i == 0 ? db[c][e] : total[a.n + at] + db[c][e];
+                    for (int h = 0; h < 2; ++h) {
+                        const float4 x = i == 0 ? make_float4(0, 0, 0, 0) : pw[h], y = i == 0 ? make_float4(0, 0, 0, 0) : pb[h];
+                        pw[h] = make_float4(x.x + dw[c][2 * h].x, x.y + dw[c][2 * h].y, x.z + dw[c][2 * h + 1].x, x.w + dw[c][2 * h + 1].y);
+                        pb[h] = make_float4(y.x + db[c][2 * h].x, y.y + db[c][2 * h].y, y.z + db[c][2 * h + 1].x, y.w + db[c][2 * h + 1].y);
+                    }
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        const int at = all.at(c, e);
+                        if (at >= a.n) continue;
+                        const float pw = e % 2 ? dw[c][e / 2].y : dw[c][e / 2].x, pb = e % 2 ? db[c][e / 2].y : db[c][e / 2].x;
+                        total[at] = i == 0 ? pw : total[at] + pw;
+                        total[a.n + at] = i == 0 ? pb : total[a.n + at] + pb;
+                    }
                 }
             }
         }
         __syncthreads();
     }
     float* to = a.parts + static_cast<int64_t>(blockIdx.x) * 2 * a.n;
-    for (int64_t i = threadIdx.x; i < 2 * a.n; i += blockDim.x) to[i] = total[i];
+    for (int i = threadIdx.x; i < 2 * a.n; i += blockDim.x) to[i] = total[i];
 }
 
 // Rows too wide for registers: a block a row for dx, which reads the row twice ...
 template <class X, class Y, bool WIDE>
 __global__ void __launch_bounds__(1024) norm_backward_long_kernel(const __grid_constant__ NormBack a) {
-    __shared__ float2 sums[32];
+    __shared__ float2 sums[2][32];
     tc::let_next_start();
     tc::wait_for_previous();
     const int64_t row = blockIdx.x;
-    const Columns<WIDE> cols{a.n, static_cast<int>(threadIdx.x), a.g};
+    const Columns<WIDE, 1024> cols{a.n, static_cast<int>(threadIdx.x), 1024};
     const X* x = static_cast<const X*>(a.x) + row * a.x_ld;
     const Y* dy = static_cast<const Y*>(a.dy) + row * a.dy_ld;
-    const int chunks = static_cast<int>((a.n + a.g * 8 - 1) / (a.g * 8));
+    const int chunks = (a.n + 8191) / 8192;
     const float n = static_cast<float>(a.n), mean = a.stats[row], rstd = a.stats[a.m + row];
-    float2 s = make_float2(0.0f, 0.0f);
-    float v[8], d[8], w[8], skip[8] = {};
+    float2 h[4], u[4], sx = twice(0.0f), sy = twice(0.0f);
     auto take = [&](int c) {
         Eight<X> ox;
         Eight<Y> oy;
+        float2 w[4];
         cols.load(x, c, ox);
         cols.load(dy, c, oy);
-        ox.get(v);
-        oy.get(d);
+        ox.get(h);
+        oy.get(u);
         cols.vector(a.w, a.w_f32, c, 1.0f, w);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {      // a column that is not there has dy = 0
+            h[e] = mul2(add2(h[e], twice(-mean)), twice(rstd));
+            u[e] = mul2(u[e], w[e]);
+        }
     };
     for (int c = 0; c < chunks; ++c) {
         take(c);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            const float h = cols.at(c, e) < a.n ? (v[e] - mean) * rstd : 0.0f, u = w[e] * d[e];
-            s.x += u;
-            s.y = __fmaf_rn(u, h, s.y);
+        for (int e = 0; e < 4; ++e) {
+            sx = add2(sx, u[e]);
+            sy = fma2(u[e], h[e], sy);
         }
     }
-    s = row_sum(s, a.g, sums);
-    const float along = s.x / n, turn = s.y / n;
+    const float2 s = row_sum(make_float2(sx.x + sx.y, sy.x + sy.y), 1024, sums, 0), along = twice(-s.x / n), turned = twice(-s.y / n);
     for (int c = 0; c < chunks; ++c) {
+        float2 skip[4] = {};
         take(c);
         if (a.residual != nullptr) {
             Eight<X> o;
@@ -390,11 +539,8 @@ __global__ void __launch_bounds__(1024) norm_backward_long_kernel(const __grid_c
             o.get(skip);
         }
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            const float h = (v[e] - mean) * rstd;
-            v[e] = __fmaf_rn(rstd, __fmaf_rn(-h, turn, __fmaf_rn(w[e], d[e], -along)), skip[e]);
-        }
-        cols.store(static_cast<X*>(a.dx) + row * a.dx_ld, c, v);
+        for (int e = 0; e < 4; ++e) u[e] = fma2(twice(rstd), fma2(h[e], turned, add2(u[e], along)), skip[e]);
+        cols.store(static_cast<X*>(a.dx) + row * a.dx_ld, c, u);
     }
 }
 
@@ -403,7 +549,7 @@ template <class X, class Y>
 __global__ void __launch_bounds__(128) norm_columns_kernel(const __grid_constant__ NormBack a) {
     tc::let_next_start();
     tc::wait_for_previous();
-    const int64_t col = static_cast<int64_t>(blockIdx.x) * 128 + threadIdx.x;
+    const int col = static_cast<int>(blockIdx.x) * 128 + static_cast<int>(threadIdx.x);
     if (col >= a.n) return;
     float dw = 0.0f, db = 0.0f;
 #pragma unroll 4
@@ -421,8 +567,7 @@ __global__ void __launch_bounds__(128) norm_columns_kernel(const __grid_constant
 // dw and db out of the blocks' shares: 32 columns a block, 32 threads a column.
 struct NormSums {
     const float* parts;
-    int64_t n;
-    int count, f32;
+    int n, count, f32;
     void *dw, *db;
 };
 
@@ -436,7 +581,7 @@ __global__ void __launch_bounds__(1024) norm_sums_kernel(const __grid_constant__
     const int64_t col = static_cast<int64_t>(blockIdx.x) * 32 + lane;
     float s = 0.0f;
     if (col < a.n) {
-        const float* p = a.parts + blockIdx.y * a.n + col;
+        const float* p = a.parts + static_cast<int64_t>(blockIdx.y) * a.n + col;
 #pragma unroll 8
         for (int i = line; i < a.count; i += 32) s += p[static_cast<int64_t>(i) * 2 * a.n];
     }
@@ -488,30 +633,45 @@ dlion_status check(const dlion_norm_fwd* p) {
 
 void forward(Call& c, const dlion_norm_fwd& p) {
     if (p.m == 0 || !c.live()) return;
-    Norm a{p.m, p.n, p.x, p.x_ld, p.w, p.b, p.w_type == DLION_GRAD_F32, p.b_type == DLION_GRAD_F32, p.eps, p.y, p.y_ld, p.stats, 0};
+    Norm a{p.m, static_cast<int>(p.n), p.x, p.x_ld, p.w, p.b, p.w_type == DLION_GRAD_F32, p.b_type == DLION_GRAD_F32, p.eps, p.y, p.y_ld, p.stats, 0};
     const bool grid16 = p.n % 8 == 0 && wide(p.x, p.x_ld, p.x_type, p.m) && wide(p.y, p.y_ld, p.y_type, p.m) && wide(p.w, 0, 0, 1) && wide(p.b, 0, 0, 1);
-    a.g = group_of(p.n, 4, 1024);
     with_types(p.x_type, p.y_type, [&](auto x, auto y) {
         using X = decltype(x);
         using Y = decltype(y);
+        if (p.n <= kWarpColumns) {         // a warp a row
+            auto go = [&](auto* kernel) { start(c, kernel, dim3(static_cast<unsigned>(parts(p.m, 4))), dim3(128), 0, 1, a); };
+            const int chunks = static_cast<int>(parts(p.n, 256));
+            if (p.m >= kManyRows * c.sms) {
+                auto rows = [&](auto* kernel, int of) { start(c, kernel, dim3(static_cast<unsigned>(c.sms)), dim3(kRowsThreads), of * 4 * 32 * sizeof(float4), 1, a); };
+                if (!grid16) {
+                    chunks <= 2 ? rows(&norm_rows_kernel<X, Y, false, 2>, 2) : chunks <= 4 ? rows(&norm_rows_kernel<X, Y, false, 4>, 4) : rows(&norm_rows_kernel<X, Y, false, 8>, 8);
+                } else if (chunks <= 2) {
+                    chunks == 1 ? rows(&norm_rows_kernel<X, Y, true, 1>, 1) : rows(&norm_rows_kernel<X, Y, true, 2>, 2);
+                } else if (chunks <= 4) {
+                    chunks == 3 ? rows(&norm_rows_kernel<X, Y, true, 3>, 3) : rows(&norm_rows_kernel<X, Y, true, 4>, 4);
+                } else {
+                    chunks <= 6 ? rows(&norm_rows_kernel<X, Y, true, 6>, 6) : rows(&norm_rows_kernel<X, Y, true, 8>, 8);
+                }
+                return;
+            }
+            if (!grid16) {
+                chunks <= 2 ? go(&norm_kernel<X, Y, false, 2, 32>) : chunks <= 4 ? go(&norm_kernel<X, Y, false, 4, 32>) : go(&norm_kernel<X, Y, false, 8, 32>);
+            } else if (chunks <= 2) {
+                chunks == 1 ? go(&norm_kernel<X, Y, true, 1, 32>) : go(&norm_kernel<X, Y, true, 2, 32>);
+            } else if (chunks <= 4) {
+                chunks == 3 ? go(&norm_kernel<X, Y, true, 3, 32>) : go(&norm_kernel<X, Y, true, 4, 32>);
+            } else {
+                chunks <= 6 ? go(&norm_kernel<X, Y, true, 6, 32>) : go(&norm_kernel<X, Y, true, 8, 32>);
+            }
+            return;
+        }
+        a.g = group_of(p.n, 4, 1024);
         if (a.g == 0) {
-            a.g = 1024;
             start(c, grid16 ? &norm_long_kernel<X, Y, true> : &norm_long_kernel<X, Y, false>, dim3(static_cast<unsigned>(p.m)), dim3(1024), 0, 1, a);
             return;
         }
         const int threads = std::max(a.g, kBlock);
-        const dim3 grid(static_cast<unsigned>(parts(p.m, threads / a.g)));
-        auto go = [&](auto* kernel) { start(c, kernel, grid, dim3(threads), 0, 1, a); };
-        const int chunks = static_cast<int>(parts(p.n, a.g * 8));
-        if (!grid16) {
-            chunks <= 2 ? go(norm_kernel<X, Y, false, 2>) : go(norm_kernel<X, Y, false, 4>);
-        } else if (chunks == 1) {
-            go(norm_kernel<X, Y, true, 1>);
-        } else if (chunks == 2) {
-            go(norm_kernel<X, Y, true, 2>);
-        } else {
-            chunks == 3 ? go(norm_kernel<X, Y, true, 3>) : go(norm_kernel<X, Y, true, 4>);
-        }
+        start(c, grid16 ? &norm_kernel<X, Y, true, 4, 0> : &norm_kernel<X, Y, false, 4, 0>, dim3(static_cast<unsigned>(parts(p.m, threads / a.g))), dim3(threads), 0, 1, a);
     });
 }
 
@@ -530,7 +690,8 @@ dlion_status check(const dlion_norm_bwd* p) {
     return DLION_OK;
 }
 
-constexpr int kBackChunks = 3, kBackThreads = 512;
+constexpr int kMostShared = 224 * 1024;
+constexpr int kBackColumns = 8 * 1024;     // a thread has two chunks of eight at most, and three (to 768 columns) where a warp has the row
 
 void backward(Call& c, const dlion_norm_bwd& p) {
     const bool sums = p.dw != nullptr || p.db != nullptr;
@@ -542,42 +703,55 @@ void backward(Call& c, const dlion_norm_bwd& p) {
         return;
     }
     if (p.dx == nullptr && !sums) return;
-    NormBack a{p.m, p.n, p.dy, p.dy_ld, p.x, p.x_ld, p.w, p.w_type == DLION_GRAD_F32, p.stats, p.dx != nullptr ? p.residual : nullptr, p.r_ld, p.dx, p.dx_ld, nullptr, 0};
+    NormBack a{p.m, static_cast<int>(p.n), p.dy, p.dy_ld, p.x, p.x_ld, p.w, p.w_type == DLION_GRAD_F32, p.stats, p.dx != nullptr ? p.residual : nullptr, p.r_ld, p.dx, p.dx_ld, nullptr, 0};
     const bool grid16 = p.n % 8 == 0 && wide(p.x, p.x_ld, p.x_type, p.m) && wide(p.dy, p.dy_ld, p.dy_type, p.m) && wide(p.w, 0, 0, 1) &&
                         wide(a.residual, p.r_ld, p.x_type, p.m) && wide(p.dx, p.dx_ld, p.x_type, p.m);
-    a.g = group_of(p.n, kBackChunks, kBackThreads);
+    a.g = p.n <= 768 ? 32 : group_of(p.n, 2, 512);
     const bool whole = a.g != 0;
-    const int threads = std::max(a.g, kBlock);
-    const int64_t blocks = whole ? std::min<int64_t>(parts(p.m, threads / a.g), 2 * c.sms) : std::min<int64_t>(p.m, 64);
+    // one block an SM, or smaller ones where the rows are so few that those have no more than one turn
+    const int units = (p.x_type == DLION_GRAD_F32 ? 4 : 2) + (p.dy_type == DLION_GRAD_F32 ? 2 : 1);       // of 16 bytes a chunk
+    const int small = std::max(a.g, 128), large = a.g == 32 && units * 3 > 13 ? 384 : kBackThreads;          // two rows ahead have to fit
+    const int threads = whole && parts(p.m, small / a.g) > 2 * c.sms ? large : small;
+    const int64_t blocks = whole ? std::min<int64_t>(parts(p.m, threads / a.g), threads == 128 ? 2 * c.sms : c.sms) : std::min<int64_t>(p.m, 64);
     if (sums) a.parts = c.ws.take<float>(static_cast<uint64_t>(blocks) * 2 * p.n);
     if (!c.live()) return;
     with_types(p.x_type, p.dy_type, [&](auto x, auto y) {
         using X = decltype(x);
         using Y = decltype(y);
         if (!whole) {
-            a.g = 1024;
             if (p.dx != nullptr) {
                 start(c, grid16 ? &norm_backward_long_kernel<X, Y, true> : &norm_backward_long_kernel<X, Y, false>, dim3(static_cast<unsigned>(p.m)), dim3(1024), 0, 1, a);
             }
             if (sums) start(c, norm_columns_kernel<X, Y>, dim3(static_cast<unsigned>(parts(p.n, 128)), static_cast<unsigned>(blocks)), dim3(128), 0, 1, a);
             return;
         }
-        const size_t shared = sums ? static_cast<size_t>(p.n) * 8 : 0;
-        auto go = [&](auto* kernel) {
-            if (shared > 48 * 1024) raise_shared(c, kernel, kBackChunks * 8 * kBackThreads * 8);
-            start(c, kernel, dim3(static_cast<unsigned>(blocks)), dim3(threads), shared, 1, a);
+        const size_t vectors = sums ? static_cast<size_t>(p.n) * 8 : 0;
+        auto go = [&](auto* kernel, size_t ring, int most) {
+            if (std::max(ring, vectors) > 47 * 1024) raise_shared(c, kernel, std::max(most, kBackColumns * 8));
+            start(c, kernel, dim3(static_cast<unsigned>(blocks)), dim3(threads), std::max(ring, vectors), 1, a);
         };
+        auto with = [&](auto chunk, auto threads_a_row) {
+            constexpr int C = decltype(chunk)::value, G = decltype(threads_a_row)::value;
+            using Row = NormRow<X, Y, true, C>;
+            grid16 ? go(&norm_backward_kernel<X, Y, true, C, G>, static_cast<size_t>(Row::kDepth) * Row::kUnits * threads * 16, std::min(Row::kDepth * Row::kUnits * kBackThreads * 16, kMostShared))
+                   : go(&norm_backward_kernel<X, Y, false, C, G>, 0, 0);
+        };
+        using std::integral_constant;
         const int chunks = static_cast<int>(parts(p.n, a.g * 8));
-        if (!grid16) {
-            chunks <= 2 ? go(&norm_backward_kernel<X, Y, false, 2>) : go(&norm_backward_kernel<X, Y, false, 3>);
-        } else if (chunks == 1) {
-            go(&norm_backward_kernel<X, Y, true, 1>);
+        if (a.g == 32) {
+            if (chunks == 1) {
+                with(integral_constant<int, 1>{}, integral_constant<int, 32>{});
+            } else {
+                chunks == 2 ? with(integral_constant<int, 2>{}, integral_constant<int, 32>{}) : with(integral_constant<int, 3>{}, integral_constant<int, 32>{});
+            }
+        } else if (a.g == 64) {
+            with(integral_constant<int, 2>{}, integral_constant<int, 64>{});
         } else {
-            chunks == 2 ? go(&norm_backward_kernel<X, Y, true, 2>) : go(&norm_backward_kernel<X, Y, true, 3>);
+            a.g == 128 ? with(integral_constant<int, 2>{}, integral_constant<int, 128>{}) : with(integral_constant<int, 2>{}, integral_constant<int, 0>{});
         }
     });
     if (!sums) return;
-    const NormSums s{a.parts, p.n, static_cast<int>(blocks), p.grad_type == DLION_GRAD_F32, p.dw, p.db};
+    const NormSums s{a.parts, static_cast<int>(p.n), static_cast<int>(blocks), p.grad_type == DLION_GRAD_F32, p.dw, p.db};
     start(c, norm_sums_kernel, dim3(static_cast<unsigned>(parts(p.n, 32)), 2), dim3(1024), 0, 1, s);
 }
 
