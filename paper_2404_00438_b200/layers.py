@@ -480,34 +480,34 @@ def norm_backward(dy: torch.Tensor, x: torch.Tensor, w: Optional[torch.Tensor], 
     return dx, dw, db
 
 
-def _heads(t, name: str, device: int, shape) -> None:
-    """Raises unless ``t`` is a bf16 tensor of ``shape`` (rows, heads, dim) that 16-byte accesses can take: adjacent columns of a head,
-    rows and heads that begin on the 16-byte grid and are not broadcast."""
+def _heads(t, name: str, device: int, shape):
+    """The address and the strides of rows and heads of ``t``.  Raises unless it is a bf16 tensor of ``shape`` (rows, heads, dim) that
+    16-byte accesses can take: adjacent columns of a head, rows and heads that begin on the 16-byte grid and are not broadcast."""
     if not (isinstance(t, _Tensor) and t.dtype is _BF16 and t.shape == shape and t.get_device() == device):
         _refused(t, name, device, _ONLY_BF16, shape)
     rs, hs, cs = t.stride()
-    if (cs != 1 or (shape[1] > 1 and (hs % 8 or hs < shape[2])) or (shape[0] > 1 and (rs % 8 or rs < shape[2]))
-            or t.data_ptr() % 16):
+    p = t.data_ptr()
+    if cs != 1 or p % 16 or (shape[1] > 1 and (hs % 8 or hs < shape[2])) or (shape[0] > 1 and (rs % 8 or rs < shape[2])):
         raise ValueError(f"{name}: needs adjacent columns, and rows and heads on the 16-byte grid (got strides {(rs, hs, cs)}, "
-                         f"address {t.data_ptr() % 16} beyond a multiple of 16)")
+                         f"address {p % 16} beyond a multiple of 16)")
+    return p, rs, hs
 
 
 def _attention_sizes(q, k, v, device: int):
+    """(rows, heads, kv_heads, dim), and the fields of q, k and v."""
     for t, name in ((q, "q"), (k, "k"), (v, "v")):
         if not isinstance(t, _Tensor):
             raise ValueError(f"{name}: expected a torch.Tensor, got {type(t).__name__}")
-        if t.dim() != 3:
-            raise ValueError(f"{name}: expected [rows, heads, dim], got {t.dim()} dimensions")
+    if len(q.shape) != 3 or len(k.shape) != 3:
+        raise ValueError(f"q, k: expected [rows, heads, dim], got {q.dim()} and {k.dim()} dimensions")
     rows, heads, dim = q.shape
     kv = k.shape[1]
     if kv < 1 or heads < 1 or heads % kv:
         raise ValueError(f"q: {heads} heads, not a multiple of the {kv} of k and v")
     if dim < 8 or dim > 128 or dim % 8:
         raise ValueError(f"q: heads of {dim} columns, expected a multiple of 8, at most 128")
-    _heads(q, "q", device, (rows, heads, dim))
-    _heads(k, "k", device, (rows, kv, dim))
-    _heads(v, "v", device, (rows, kv, dim))
-    return rows, heads, kv, dim
+    shared = (rows, kv, dim)
+    return (rows, heads, kv, dim), (*_heads(q, "q", device, (rows, heads, dim)), *_heads(k, "k", device, shared), *_heads(v, "v", device, shared))
 
 
 def _sequences(offsets, length, rows: int, device: int):
@@ -524,14 +524,6 @@ def _sequences(offsets, length, rows: int, device: int):
         raise ValueError("offsets: expected a tensor of sequences + 1 values")
     _vector(offsets, "offsets", device, (torch.int32, torch.int64), offsets.shape[0])
     return offsets.data_ptr(), int(offsets.dtype == torch.int64), offsets.shape[0] - 1, 0
-
-
-def _given(t, name: str, device: int, shape, like, zero_rest: bool, offsets):
-    """An output tensor and whether its rows in no sequence are to be cleared."""
-    if t is None:
-        return like.new_empty(shape), offsets is not None
-    _heads(t, name, device, shape)
-    return t, bool(zero_rest)
 
 
 def _scale(scale, dim: int) -> float:
@@ -552,20 +544,28 @@ def attention_forward(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, *, caus
     1 / sqrt(dim) where it is not given.  Rows in no sequence are left as they were in ``out`` and ``lse``, unless
     ``zero_rest``; they are zero in results that are not given."""
     device = _device(q, "q")
-    rows, heads, kv, dim = _attention_sizes(q, k, v, device)
+    sizes, inputs = _attention_sizes(q, k, v, device)
+    rows, heads, _, dim = sizes
     sequences = _sequences(offsets, length, rows, device)
-    own = out is None and lse is None
-    out, zero = _given(out, "out", device, (rows, heads, dim), q, zero_rest, offsets)
+    clear = zero_rest
+    if out is None:
+        out, given = q.new_empty((rows, heads, dim)), False
+        fields = (out.data_ptr(), heads * dim, dim)
+        clear = offsets is not None
+    else:
+        fields, given = _heads(out, "out", device, (rows, heads, dim)), True
     if lse is None:
-        lse = (torch.empty if own or offsets is None else torch.zeros)((heads, rows), dtype=torch.float32, device=q.device)
+        lse = q.new_empty((heads, rows), dtype=torch.float32)
+        ld = rows
+        if given and offsets is not None and not zero_rest:
+            lse.zero_()                        # a result of each kind: the given one is left as it was
     else:
         _matrix(lse, "lse", device, (torch.float32,), (heads, rows), True)
-        if zero and not zero_rest:             # a result of each kind: the given one is left as it was
-            out, zero = out.zero_(), False
-    qs, ks, vs, os = q.stride(), k.stride(), v.stride(), out.stride()
-    args = _AttentionForward(rows, heads, kv, dim, q.data_ptr(), qs[0], qs[1], k.data_ptr(), ks[0], ks[1], v.data_ptr(), vs[0], vs[1],
-                             *sequences, int(bool(causal)), _scale(scale, dim), out.data_ptr(), os[0], os[1], lse.data_ptr(),
-                             max(lse.stride(0), rows), int(zero))
+        ld = max(lse.stride(0), rows)
+        if not given and clear and not zero_rest:
+            out.zero_()
+            clear = False
+    args = _AttentionForward(*sizes, *inputs, *sequences, 1 if causal else 0, _scale(scale, dim), *fields, lse.data_ptr(), ld, 1 if clear else 0)
     _call(_ATTENTION_FORWARD, args, device, workspace)
     return Attended(out, lse)
 
@@ -578,23 +578,28 @@ def attention_backward(dout: torch.Tensor, q: torch.Tensor, k: torch.Tensor, v: 
     ``dv`` are summed over the query heads that share them.  Views of one tensor are valid results: the gradient
     of the product that made q, k and v.  Rows in no sequence as in ``attention_forward``."""
     device = _device(dout, "dout")
-    rows, heads, kv, dim = _attention_sizes(q, k, v, device)
+    sizes, inputs = _attention_sizes(q, k, v, device)
+    rows, heads, kv, dim = sizes
     sequences = _sequences(offsets, length, rows, device)
-    _heads(dout, "dout", device, (rows, heads, dim))
-    _heads(out, "out", device, (rows, heads, dim))
+    own, shared = (rows, heads, dim), (rows, kv, dim)
+    saved = (*_heads(out, "out", device, own), *_heads(dout, "dout", device, own))
     _matrix(lse, "lse", device, (torch.float32,), (heads, rows), True)
-    given = [t is not None for t in (dq, dk, dv)]
-    mixed = offsets is not None and any(given) and not all(given) and not zero_rest
-    results, zero = [], False
-    for t, name, shape in ((dq, "dq", (rows, heads, dim)), (dk, "dk", (rows, kv, dim)), (dv, "dv", (rows, kv, dim))):
-        r, z = _given(t, name, device, shape, q, zero_rest, offsets)
-        if mixed:                              # the given ones are left as they were
-            r = r if t is not None else r.zero_()
-        results.append(r)
-        zero = zero or (z and not mixed)
-    strides = [f for t in (q, k, v, out, dout) for f in (t.data_ptr(), t.stride(0), t.stride(1))]
-    args = _AttentionBackward(rows, heads, kv, dim, *strides, lse.data_ptr(), max(lse.stride(0), rows), *sequences, int(bool(causal)),
-                              _scale(scale, dim), *[f for t in results for f in (t.data_ptr(), t.stride(0), t.stride(1))], int(zero))
+    results, fields, given = [], [], 0
+    for t, name, shape in ((dq, "dq", own), (dk, "dk", shared), (dv, "dv", shared)):
+        if t is None:
+            t = q.new_empty(shape)
+            fields += (t.data_ptr(), shape[1] * dim, dim)
+        else:
+            fields += _heads(t, name, device, shape)
+            given += 1
+        results.append(t)
+    clear = zero_rest or (offsets is not None and given == 0)
+    if offsets is not None and not clear and given < 3:        # results of each kind: the given ones are left as they were
+        for t, was in zip(results, (dq, dk, dv)):
+            if was is None:
+                t.zero_()
+    args = _AttentionBackward(*sizes, *inputs, *saved, lse.data_ptr(), max(lse.stride(0), rows), *sequences, 1 if causal else 0, _scale(scale, dim),
+                              *fields, 1 if clear else 0)
     _call(_ATTENTION_BACKWARD, args, device, workspace)
     return tuple(results)
 

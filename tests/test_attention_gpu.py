@@ -129,6 +129,33 @@ def test_equal_lengths(L, causal):
     verify(L, q, k, v, [150] * 5, causal=causal, do=normal(3, 750, 4, 64), length=150)
 
 
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("n,heads,kv,dim", [(1024, 2, 1, 128), (1153, 1, 1, 96), (1300, 2, 2, 72), (1025, 3, 1, 120)])
+def test_long_sequences_of_wide_heads(L, n, heads, kv, dim, causal):
+    """Two tiles of queries to a block: with and without a second one at the end, its rows few and many."""
+    q, k, v = qkv(n + dim, n, heads, kv, dim)
+    verify(L, q, k, v, [n], causal=causal, do=normal(3, n, heads, dim))
+
+
+@pytest.mark.parametrize("dim,lengths,heads,kv", [(128, [2500, 0, 129, 1], 3, 1), (64, [130] * 60 + [700, 1, 128, 129], 6, 2), (128, [300] * 30, 8, 4), (128, [1100] * 5, 16, 8)])
+def test_more_pieces_than_blocks(L, dim, lengths, heads, kv):
+    """Blocks that take over one piece of work after another, of all lengths, from a table and by numbers alone."""
+    rows = sum(lengths)
+    q, k, v = qkv(dim, rows, heads, kv, dim)
+    do = normal(3, rows, heads, dim)
+    for causal in (True, False):
+        how = [dict(offsets=torch.tensor([0] + lengths, device=DEV).cumsum(0))] + ([dict(length=lengths[0])] if len(set(lengths)) == 1 else [])
+        runs = []
+        for kw in how:
+            f = L.attention_forward(q, k, v, causal=causal, **kw)
+            runs.append((*f, *L.attention_backward(do, q, k, v, *f, causal=causal, **kw)))
+        assert all(torch.equal(a, b) for r in runs for a, b in zip(r, runs[0]))
+        picked = [i for i in range(len(lengths)) if i % 7 == 0 or i == len(lengths) - 1 or lengths[i] != lengths[0]]
+        ends = torch.tensor([0] + lengths).cumsum(0).tolist()
+        for i in picked:
+            verify(L, q, k, v, [lengths[i]], ends[i], causal, do=do, results=runs[0])
+
+
 # ------------------------------------------------------------------------------------------------ packed sequences
 LENGTHS = [0, 1, 0, 130, 5, 0, 256, 77, 0, 128, 3, 300, 0]
 
