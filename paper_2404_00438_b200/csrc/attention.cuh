@@ -336,15 +336,20 @@ __device__ __forceinline__ void give_rows(uint32_t addr, float factor, uint8_t* 
                                           int dim, int lane) {
     const int unit = lane % 4;
     __nv_bfloat16* out = to.p + row0 * to.rs + head * to.hs + col0 + unit * 8;
+    float v[COLS];
+    if constexpr (COLS == 128) {
+        tmem_load128(addr, v);
+    } else {
+        tmem_load64(addr, v);
+    }
 #pragma unroll
     for (int c = 0; c < COLS; c += 32) {
-        float v[32];
-        tc::tmem_load32(addr + c, v);
         __syncwarp();                      // what was there has left
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const uint4 w = make_uint4(pack_bf16(v[8 * i] * factor, v[8 * i + 1] * factor), pack_bf16(v[8 * i + 2] * factor, v[8 * i + 3] * factor),
-                                       pack_bf16(v[8 * i + 4] * factor, v[8 * i + 5] * factor), pack_bf16(v[8 * i + 6] * factor, v[8 * i + 7] * factor));
+            const float* x = v + c + 8 * i;
+            const uint4 w = make_uint4(pack_bf16(x[0] * factor, x[1] * factor), pack_bf16(x[2] * factor, x[3] * factor), pack_bf16(x[4] * factor, x[5] * factor),
+                                       pack_bf16(x[6] * factor, x[7] * factor));
             *reinterpret_cast<uint4*>(stage + lane * 64 + ((i ^ (lane / 2 % 4)) * 16)) = w;
         }
         __syncwarp();

@@ -260,7 +260,8 @@ __global__ void __launch_bounds__(kQueryThreads, 1) query_gradient_kernel(const 
         const uint32_t lanes = static_cast<uint32_t>(quarter * 32) << 16;
         const float2 cc = twice(w.c);
         int i = 0, ended = 0;
-        while (fine && pieces.take(piece, head, fine)) {
+        bool more = pieces.take(piece, head, fine);
+        while (fine && more) {
             divide();
             const int row = row0 + quarter * 32 + lane;
             const bool live = row < piece.length;
@@ -313,11 +314,12 @@ __global__ void __launch_bounds__(kQueryThreads, 1) query_gradient_kernel(const 
                 __syncwarp();
                 if (lane == 0) tc::bar_arrive(slopes);
             }
+            if (!fine) break;
+            __nv_bfloat16* to = w.dq.p + static_cast<int64_t>(piece.start + row) * w.dq.rs + head * w.dq.hs + half * (D / 2);
+            more = pieces.take(piece, head, fine);                   // the next one's whereabouts, while the last product runs
             if (!fine || !(fine = tc::bar_wait(done, ended++ & 1))) break;
             tc::fence_after();
-            constexpr int kHalf = D / 2;
-            give_row<kHalf>(dq_at + half * kHalf + lanes, w.scale, w.dq.p + static_cast<int64_t>(piece.start + row) * w.dq.rs + head * w.dq.hs + half * kHalf, live,
-                            w.dim - half * kHalf);
+            give_row<D / 2>(dq_at + half * (D / 2) + lanes, w.scale, to, live, w.dim - half * (D / 2));
             tc::fence_before();
         }
     }
@@ -547,7 +549,8 @@ __global__ void __launch_bounds__(kKeyThreads, 1) key_gradient_kernel(const __gr
         const float* stats = reinterpret_cast<const float*>(mem + S::kStats);
         const float2 cc = twice(w.c);
         int i = 0, ended = 0;
-        while (fine && pieces.take(piece, kv_head, fine)) {
+        bool more = pieces.take(piece, kv_head, fine);
+        while (fine && more) {
             divide();
             begin();
             const int key = key0 + quarter * 32 + lane;
@@ -621,13 +624,16 @@ __global__ void __launch_bounds__(kKeyThreads, 1) key_gradient_kernel(const __gr
                     tc::bar_arrive(stats_empty + 8 * st);
                 }
             }
-            if (!fine || !(fine = tc::bar_wait(done, ended++ & 1))) break;
-            tc::fence_after();
+            if (!fine) break;
             constexpr int kHalf = D / 2;
             const bool live = key < piece.length;
             const int64_t at = piece.start + key;
-            give_row<kHalf>(dk_at + half * kHalf + lanes, w.scale, w.dk.p + at * w.dk.rs + kv_head * w.dk.hs + half * kHalf, live, w.dim - half * kHalf);
-            give_row<kHalf>(dv_at + half * kHalf + lanes, 1.0f, w.dv.p + at * w.dv.rs + kv_head * w.dv.hs + half * kHalf, live, w.dim - half * kHalf);
+            __nv_bfloat16 *to_k = w.dk.p + at * w.dk.rs + kv_head * w.dk.hs + half * kHalf, *to_v = w.dv.p + at * w.dv.rs + kv_head * w.dv.hs + half * kHalf;
+            more = pieces.take(piece, kv_head, fine);                // the next one's whereabouts, while the last products run
+            if (!fine || !(fine = tc::bar_wait(done, ended++ & 1))) break;
+            tc::fence_after();
+            give_row<kHalf>(dk_at + half * kHalf + lanes, w.scale, to_k, live, w.dim - half * kHalf);
+            give_row<kHalf>(dv_at + half * kHalf + lanes, 1.0f, to_v, live, w.dim - half * kHalf);
             tc::fence_before();
         }
     }
