@@ -11,7 +11,12 @@
 namespace dlion {
 namespace att {
 
-constexpr int kTile = 128;                 // rows of queries or keys in a tile: the lanes of tensor memory
+constexpr int kTile = 128;                 // rows of the tile that a block keeps: the lanes of tensor memory
+
+// Rows of the tiles that pass by it.  With heads of up to 64 columns these are short: then two blocks fit an SM (forward four), whose
+// warps wait at different times (with tiles of 128, 8 x 1024 rows, 12 heads of 64: forward 35 us, dq 57, dk and dv 68).
+template <int D>
+constexpr int kPassing = D == 64 ? 64 : 128;
 
 // Which sequence and which of its tiles a piece of work is.  Sequences of one length are numbered by arithmetic; others by a
 // table in the workspace (plan_kernel), which ends with entries of length -1.  The longest pieces come first, because
@@ -130,7 +135,7 @@ struct Rows {
 };
 
 // ---------------------------------------------------------------- copies
-// 64 columns of kTile rows of one head, 128-byte swizzled; x is 0 or 64.
+// 64 columns of some rows of one head, 128-byte swizzled; x is 0 or 64.
 __device__ __forceinline__ void load_rows(uint32_t dst, const CUtensorMap* map, int x, int head, int row, uint32_t bar) {
     asm volatile(
         "cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(dst),
@@ -182,11 +187,12 @@ __device__ __forceinline__ void mma_tmem(uint32_t d, uint32_t a, uint64_t b, uin
 // that it stays in uniform registers, where these instructions want it, and the instructions of a full product stand one behind
 // the other.  (Inside a branch that one lane has taken, with a loop, an instruction took 150 clocks to issue, and its product 64.)
 //
-// d = rows of a times rows of b, both along a head's columns, 16 * steps of them (the rest of D is not there).
-template <int D>
+// d = kTile rows of a times N rows of b, both along a head's columns, 16 * steps of them (the rest of D is not there).
+template <int D, int N>
 __device__ __forceinline__ void rows_by_rows(uint32_t d, uint32_t a_tile, uint32_t b_tile, int steps) {
+    static_assert(D == 64 || N == kTile, "a tile's chunks of 64 columns are kChunk apart");
     const uint64_t a = along_row(a_tile), b = along_row(b_tile);
-    const uint32_t inst = tc::instruction(kTile, kTile, 0, 0);
+    const uint32_t inst = tc::instruction(kTile, N, 0, 0);
     if (tc::elected()) {
 #pragma unroll
         for (int i = 0; i < D / 16; ++i) {
@@ -328,14 +334,13 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
 // COLS columns of a row a thread (binary32, in tensor memory at `addr`), times `factor`, as bf16 rows of a head: through
 // shared memory (`stage`, kStage bytes, this warp's own), 32 columns at a time, so that 64 bytes of a row leave together (each thread
 // its own row, 16 bytes at a time: 5 % slower where sequences are short).  row0: the warp's first row, of which `rows` are there
-// (may be negative); col0: the first column, of `dim`.
+// (may be negative).
 constexpr uint32_t kStage = 2048;
 
 template <int COLS>
-__device__ __forceinline__ void give_rows(uint32_t addr, float factor, uint8_t* stage, const Rows& to, int64_t row0, int rows, int head, int col0,
-                                          int dim, int lane) {
+__device__ __forceinline__ void give_rows(uint32_t addr, float factor, uint8_t* stage, const Rows& to, int64_t row0, int rows, int head, int dim, int lane) {
     const int unit = lane % 4;
-    __nv_bfloat16* out = to.p + row0 * to.rs + head * to.hs + col0 + unit * 8;
+    __nv_bfloat16* out = to.p + row0 * to.rs + head * to.hs + unit * 8;
     float v[COLS];
     if constexpr (COLS == 128) {
         tmem_load128(addr, v);
@@ -347,16 +352,21 @@ __device__ __forceinline__ void give_rows(uint32_t addr, float factor, uint8_t* 
         __syncwarp();                      // what was there has left
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const float* x = v + c + 8 * i;
-            const uint4 w = make_uint4(pack_bf16(x[0] * factor, x[1] * factor), pack_bf16(x[2] * factor, x[3] * factor), pack_bf16(x[4] * factor, x[5] * factor),
-                                       pack_bf16(x[6] * factor, x[7] * factor));
+            float* x = v + c + 8 * i;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) x[e] *= factor;
+            const uint4 w = make_uint4(pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]), pack_bf16(x[4], x[5]), pack_bf16(x[6], x[7]));
             *reinterpret_cast<uint4*>(stage + lane * 64 + ((i ^ (lane / 2 % 4)) * 16)) = w;
         }
         __syncwarp();
-        if (col0 + c + unit * 8 >= dim) continue;
+        const bool inside = c + unit * 8 < dim;
+        __nv_bfloat16* at = out + (lane / 4) * to.rs + c;
+        uint4 got[4];
 #pragma unroll
-        for (int r = lane / 4; r < 32; r += 8) {
-            if (r < rows) *reinterpret_cast<uint4*>(out + r * to.rs + c) = *reinterpret_cast<const uint4*>(stage + r * 64 + ((unit ^ (r / 2 % 4)) * 16));
+        for (int r = 0; r < 4; ++r) got[r] = *reinterpret_cast<const uint4*>(stage + (lane / 4 + 8 * r) * 64 + ((unit ^ ((lane / 4 + 8 * r) / 2 % 4)) * 16));
+#pragma unroll
+        for (int r = 0; r < 4; ++r, at += 8 * to.rs) {
+            if (inside && lane / 4 + 8 * r < rows) *reinterpret_cast<uint4*>(at) = got[r];
         }
     }
     __syncwarp();
@@ -389,7 +399,7 @@ struct Operand {                           // bf16 [rows][heads][dim] as an argu
 
 // DLION_OK if 16-byte accesses and tiled copies can take it.
 dlion_status check_operand(const Operand& a, int64_t rows, int64_t dim);
-bool map_rows(CUtensorMap* map, const Operand& a, int64_t rows, int64_t dim);
+bool map_rows(CUtensorMap* map, const Operand& a, int64_t rows, int64_t dim, int tile);
 
 struct Sequences {
     int64_t rows, length, count;

@@ -189,12 +189,12 @@ __global__ void __launch_bounds__(kQueryThreads, 1) query_gradient_kernel(const 
                 if (r == 0 && !(fine = tc::bar_wait(rows_full, begun++ & 1))) break;
                 if (!(fine = tc::bar_wait(k_full + 8 * (i % S::kKeys), (i / S::kKeys) & 1))) break;
                 tc::fence_after();
-                rows_by_rows<D>(tmem + (i & 1) * kTile, base, keys + (i % S::kKeys) * S::kBytes, k_steps);
+                rows_by_rows<D, kTile>(tmem + (i & 1) * kTile, base, keys + (i % S::kKeys) * S::kBytes, k_steps);
                 finished(scores + 8 * (i & 1));
                 if (!(fine = tc::bar_wait(v_full + 8 * (i % S::kValues), (i / S::kValues) & 1))) break;
                 if (i > 0 && !(fine = tc::bar_wait(taken, (i - 1) & 1))) break;
                 tc::fence_after();
-                rows_by_rows<D>(products_at, base + S::kBytes, values + (i % S::kValues) * S::kBytes, k_steps);
+                rows_by_rows<D, kTile>(products_at, base + S::kBytes, values + (i % S::kValues) * S::kBytes, k_steps);
                 finished(products);
                 finished(v_empty + 8 * (i % S::kValues));
                 if (r == n - 1) finished(rows_empty);
@@ -497,14 +497,14 @@ __global__ void __launch_bounds__(kKeyThreads, 1) key_gradient_kernel(const __gr
             const int st = i % kStages;
             if (!(fine = tc::bar_wait(q_full + 8 * st, (i / kStages) & 1))) return;
             tc::fence_after();
-            rows_by_rows<D>(tmem + (i % kSets) * kTile, base, queries + st * S::kBytes, k_steps);
+            rows_by_rows<D, kTile>(tmem + (i % kSets) * kTile, base, queries + st * S::kBytes, k_steps);
             finished(scores + 8 * (i % kSets));
         };
         auto product = [&] {
             const int st = i % kStages;
             if (!(fine = tc::bar_wait(d_full + 8 * st, (i / kStages) & 1))) return;
             tc::fence_after();
-            rows_by_rows<D>(products_at, base + S::kBytes, douts + st * S::kBytes, k_steps);
+            rows_by_rows<D, kTile>(products_at, base + S::kBytes, douts + st * S::kBytes, k_steps);
             finished(products);
         };
         auto gather_v = [&] {
@@ -702,9 +702,9 @@ void backward(prod::Call& c, const dlion_attention_bwd& p) {
     Plan plans[2];
     make_plans(c, seq, requests, 2, tables, plans, p.zero_rest ? &clear : nullptr);
     if (pieces == 0) return;
-    if (!map_rows(&w.q, Operand{p.q, p.q_rs, p.q_hs, p.heads}, p.rows, p.dim) || !map_rows(&w.k, Operand{p.k, p.k_rs, p.k_hs, p.kv_heads}, p.rows, p.dim) ||
-        !map_rows(&w.v, Operand{p.v, p.v_rs, p.v_hs, p.kv_heads}, p.rows, p.dim) ||
-        !map_rows(&w.dout, Operand{p.dout, p.dout_rs, p.dout_hs, p.heads}, p.rows, p.dim)) {
+    if (!map_rows(&w.q, Operand{p.q, p.q_rs, p.q_hs, p.heads}, p.rows, p.dim, kTile) || !map_rows(&w.k, Operand{p.k, p.k_rs, p.k_hs, p.kv_heads}, p.rows, p.dim, kTile) ||
+        !map_rows(&w.v, Operand{p.v, p.v_rs, p.v_hs, p.kv_heads}, p.rows, p.dim, kTile) ||
+        !map_rows(&w.dout, Operand{p.dout, p.dout_rs, p.dout_hs, p.heads}, p.rows, p.dim, kTile)) {
         c.status = DLION_ECUDA;
         return;
     }

@@ -26,29 +26,31 @@ struct Forward {
 
 // SIDES tiles of queries share each tile of keys and values that a block copies.  Every side has a group of four warps, a row a
 // thread; one warp copies and one issues the products.  With two sides one's exponentials run while the tensor cores work for the
-// other; with one, two blocks an SM do that for each other.
+// other; with one, the blocks of an SM do that for each other.
 template <int D, int SIDES>
 struct ForwardShared {
-    static constexpr uint32_t kBytes = kTile * D * 2;                // of a tile
+    static constexpr int kKeys = kPassing<D>;
+    static constexpr uint32_t kBytes = kTile * D * 2, kKeyBytes = kKeys * D * 2;      // of a tile
     static constexpr int kRing = D == 128 && SIDES == 1 ? 2 : 4;     // tiles of keys and values, in turn
-    static constexpr uint32_t kStages = (SIDES + kRing) * kBytes;
+    static constexpr uint32_t kStages = SIDES * kBytes + kRing * kKeyBytes;           // results on their way out
     static constexpr uint32_t kBars = kStages + 4 * SIDES * kStage;
     static constexpr uint32_t kAll = kBars + 256 + kTurnBytes + 1024;
     static constexpr int kThreads = 128 * SIDES + 64;
-    static constexpr uint32_t kColumns = SIDES == 2 ? 512 : 256;     // of tensor memory: scores, outputs, weights
-    static constexpr bool kApart = SIDES * (kTile + D + kTile / 2) <= kColumns;       // otherwise weights lie over the scores
+    static constexpr uint32_t kColumns = SIDES * (kKeys + D);        // of tensor memory: scores, over them weights, and outputs
+    static constexpr int kBlocks = kColumns == 128 ? 3 : 512 / kColumns;              // an SM: of four, warps would have 80 registers
+    static constexpr int kHalves = kKeys / 64;                       // of the weights, announced one by one
 };
 
 template <int D, int SIDES>
-__global__ void __launch_bounds__(ForwardShared<D, SIDES>::kThreads, 3 - SIDES) attend_kernel(const __grid_constant__ Forward w, unsigned int* mark) {
+__global__ void __launch_bounds__(ForwardShared<D, SIDES>::kThreads, ForwardShared<D, SIDES>::kBlocks) attend_kernel(const __grid_constant__ Forward w, unsigned int* mark) {
     using S = ForwardShared<D, SIDES>;
-    constexpr int kRing = S::kRing, kCopying = 4 * SIDES, kIssuing = kCopying + 1;    // warps: SIDES groups of four, and one each
+    constexpr int kRing = S::kRing, kKeys = S::kKeys, kCopying = 4 * SIDES, kIssuing = kCopying + 1;    // warps: SIDES groups of four, and one each
     extern __shared__ uint8_t raw[];
     const uint32_t base = (tc::smem_addr(raw) + 1023u) & ~1023u;
     uint8_t* mem = raw + (base - tc::smem_addr(raw));
     const uint32_t ring = base + SIDES * S::kBytes, bars = base + S::kBars;
     const uint32_t full = bars, empty = bars + 64, q_full = bars + 128, scores = bars + 144, weights = bars + 160, done = bars + 192,
-                   taken = bars + 208, q_empty = bars + 216, slot = bars + 240;
+                   q_empty = bars + 216, slot = bars + 240;
     const uint32_t turns = bars + 256;
     volatile uint32_t* slot_mem = reinterpret_cast<volatile uint32_t*>(mem + (slot - base));
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
@@ -59,7 +61,6 @@ __global__ void __launch_bounds__(ForwardShared<D, SIDES>::kThreads, 3 - SIDES) 
             tc::bar_init(full + 8 * i, 1);
             tc::bar_init(empty + 8 * i, 1);
         }
-        tc::bar_init(taken, 4);
         for (int i = 0; i < SIDES; ++i) {
             tc::bar_init(q_full + 8 * i, 1);
             tc::bar_init(q_empty + 8 * i, 1);
@@ -90,9 +91,9 @@ __global__ void __launch_bounds__(ForwardShared<D, SIDES>::kThreads, 3 - SIDES) 
     int row0 = 0, n0 = 0, n1 = 0, most = 0;
     auto divide = [&] {
         row0 = piece.tile * SIDES * kTile;
-        const int key_tiles = (piece.length + kTile - 1) / kTile;
-        n0 = w.causal ? min(key_tiles, SIDES * piece.tile + 1) : key_tiles;
-        n1 = SIDES == 2 && piece.length - row0 > kTile ? (w.causal ? min(key_tiles, SIDES * piece.tile + 2) : key_tiles) : 0;
+        auto keys = [&](int row) { return (min(piece.length, w.causal ? row + kTile : piece.length) + kKeys - 1) / kKeys; };
+        n0 = keys(row0);
+        n1 = SIDES == 2 && piece.length - row0 > kTile ? keys(row0 + kTile) : 0;
         most = max(n0, n1);
     };
 
@@ -106,13 +107,13 @@ __global__ void __launch_bounds__(ForwardShared<D, SIDES>::kThreads, 3 - SIDES) 
                     asked = pieces.turn;
                     if (!(fine = pieces.ask())) break;
                 }
-                const int row = piece.start + (most - 1 - r) * kTile;
+                const int row = piece.start + (most - 1 - r) * kKeys;
                 for (int kind = 0; kind < 2; ++kind, ++filled) {
                     const int st = filled % kRing;
                     if (!(fine = tc::bar_wait(empty + 8 * st, ((filled / kRing) & 1) ^ 1))) break;
                     if (tc::elected()) {
-                        tc::bar_expect(full + 8 * st, S::kBytes);
-                        load_head<D>(ring + st * S::kBytes, kind ? &w.v : &w.k, kv_head, row, full + 8 * st);
+                        tc::bar_expect(full + 8 * st, S::kKeyBytes);
+                        load_head<D>(ring + st * S::kKeyBytes, kind ? &w.v : &w.k, kv_head, row, full + 8 * st);
                     }
                     __syncwarp();
                     if (r > 0 || kind > 0) continue;
@@ -148,30 +149,29 @@ __global__ void __launch_bounds__(ForwardShared<D, SIDES>::kThreads, 3 - SIDES) 
         };
         auto filled = [&](int i) { return tc::bar_wait(full + 8 * (i % kRing), (i / kRing) & 1); };
         int round = 0;                     // of all pieces: its keys and values are the ring's 2 round and 2 round + 1
-        int scored[2] = {}, weighed[2] = {}, begun[2] = {};          // tiles of each side; pieces
+        int weighed[2] = {}, begun[2] = {};                          // tiles of each side; pieces
         // What is left of the last round: the weighted values
         bool waiting[2] = {}, first[2] = {};
         int steps = 0;
         bool last = false;
         auto gather = [&](int side) {
-            const uint32_t values = ring + ((2 * round - 1) % kRing) * S::kBytes, p_at = S::kApart ? tmem + kTile + D : tmem + side * kTile,
-                           o_at = tmem + SIDES * kTile + side * D;
+            const uint32_t values = ring + ((2 * round - 1) % kRing) * S::kKeyBytes, p_at = tmem + side * kKeys, o_at = tmem + SIDES * kKeys + side * D;
             if (!(fine = tc::bar_wait(weights + 16 * side, weighed[side] & 1))) return;
             tc::fence_after();
             weights_by_rows<0, 4, 0>(o_at, p_at, values, out_inst, steps, !first[side]);
-            if (!(fine = tc::bar_wait(weights + 16 * side + 8, weighed[side] & 1))) return;
-            tc::fence_after();
-            weights_by_rows<4, 8, 0>(o_at, p_at, values, out_inst, steps, true);
+            if (S::kHalves == 2) {
+                if (!(fine = tc::bar_wait(weights + 16 * side + 8, weighed[side] & 1))) return;
+                tc::fence_after();
+                weights_by_rows<4, 8, 0>(o_at, p_at, values, out_inst, steps, true);
+            }
             ++weighed[side];
-            if (S::kApart || last) finished(done + 8 * side);
+            if (last) finished(done + 8 * side);
         };
         auto score = [&](int side, int r) {
             const int n = side ? n1 : n0;
             if (r == most - n && !(fine = tc::bar_wait(q_full + 8 * side, begun[side] & 1))) return;
-            if (S::kApart && scored[side] > 0 && !(fine = tc::bar_wait(taken, (scored[side] - 1) & 1))) return;
             tc::fence_after();
-            rows_by_rows<D>(tmem + side * kTile, base + side * S::kBytes, ring + (2 * round % kRing) * S::kBytes, k_steps);
-            ++scored[side];
+            rows_by_rows<D, kKeys>(tmem + side * kKeys, base + side * S::kBytes, ring + (2 * round % kRing) * S::kKeyBytes, k_steps);
             finished(scores + 8 * side);
             if (r == most - 1) {
                 ++begun[side];
@@ -181,28 +181,23 @@ __global__ void __launch_bounds__(ForwardShared<D, SIDES>::kThreads, 3 - SIDES) 
         auto release = [&] {               // the last round's values
             if (round > 0) finished(empty + 8 * ((2 * round - 1) % kRing));
         };
-        // A round: the scores of a tile of keys, and the weighted values of the round before it.  Where weights lie over the scores
-        // these come first, and one side after the other, so that a side's products run while the other's exponentials do
-        // (with a warp to issue each side's, both sides' came to run and to wait together: a quarter slower).
+        // A round: the weighted values of the round before it, then, over its weights, the scores of a tile of keys; one side after the
+        // other, so that a side's products run while the other's exponentials do (with a warp to issue each side's, both sides' came to
+        // run and to wait together: a quarter slower).
         while (fine && pieces.take(piece, head, fine)) {
             divide();
             for (int r = 0; r < most && fine; ++r, ++round) {
                 if (round > 0 && !(fine = filled(2 * round - 1))) break;
                 if (!(fine = filled(2 * round))) break;
-                if (S::kApart) {
-                    score(0, r);
-                    if (fine && waiting[0]) gather(0);
-                } else {
 #pragma unroll
-                    for (int side = 0; side < SIDES; ++side) {
-                        if (fine && waiting[side]) gather(side);
-                        if (fine && r >= most - (side ? n1 : n0)) score(side, r);
-                    }
+                for (int side = 0; side < SIDES; ++side) {
+                    if (fine && waiting[side]) gather(side);
+                    if (fine && r >= most - (side ? n1 : n0)) score(side, r);
                 }
                 if (!fine) break;
                 release();
                 finished(empty + 8 * (2 * round % kRing));
-                steps = (min(kTile, piece.length - (most - 1 - r) * kTile) + 15) / 16;
+                steps = (min(kKeys, piece.length - (most - 1 - r) * kKeys) + 15) / 16;
                 last = r == most - 1;
 #pragma unroll
                 for (int side = 0; side < SIDES; ++side) {
@@ -221,8 +216,7 @@ __global__ void __launch_bounds__(ForwardShared<D, SIDES>::kThreads, 3 - SIDES) 
     } else {
         const int side = warp / 4, quarter = warp % 4;
         const uint32_t lanes = static_cast<uint32_t>(quarter * 32) << 16;
-        const uint32_t s_at = tmem + side * kTile + lanes, o_at = tmem + SIDES * kTile + side * D + lanes;
-        const uint32_t p_at = S::kApart ? tmem + kTile + D + lanes : s_at;
+        const uint32_t s_at = tmem + side * kKeys + lanes, o_at = tmem + SIDES * kKeys + side * D + lanes;
         const float c = w.c;
         int round = 0, scored = 0, ended = 0;                        // rounds of all pieces; this side's tiles; its pieces
         bool more = pieces.take(piece, head, fine);
@@ -236,25 +230,24 @@ __global__ void __launch_bounds__(ForwardShared<D, SIDES>::kThreads, 3 - SIDES) 
                 const int j = n - 1 - r;
                 if (!(fine = tc::bar_wait(scores + 8 * side, scored & 1))) break;
                 tc::fence_after();
-                float s[kTile];
-                tmem_load128(s_at, s);
-                if (S::kApart) {
-                    tc::fence_before();
-                    __syncwarp();
-                    if (lane == 0) tc::bar_arrive(taken);
+                float s[kKeys];
+                if constexpr (kKeys == 64) {
+                    tmem_load64(s_at, s);
+                } else {
+                    tmem_load128(s_at, s);
                 }
-                const int valid = piece.length - j * kTile;          // keys of the tile that are the sequence's
-                if (valid < kTile || (w.causal && (j + 1) * kTile > row0 + side * kTile)) {
-                    const int behind = (w.causal ? min(row, piece.length - 1) : piece.length - 1) - j * kTile;
+                const int valid = piece.length - j * kKeys;          // keys of the tile that are the sequence's
+                if (valid < kKeys || (w.causal && (j + 1) * kKeys > row0 + side * kTile)) {
+                    const int behind = (w.causal ? min(row, piece.length - 1) : piece.length - 1) - j * kKeys;
 #pragma unroll
-                    for (int i = 0; i < kTile; ++i) s[i] = i <= behind ? s[i] : -INFINITY;
+                    for (int i = 0; i < kKeys; ++i) s[i] = i <= behind ? s[i] : -INFINITY;
                 }
                 float top4[4] = {s[0], s[1], s[2], s[3]};
 #pragma unroll
-                for (int i = 4; i < kTile; i += 8) {
+                for (int i = 4; i < kKeys; i += 8) {
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
-                        if (i + 2 * e + 1 < kTile) top4[e] = max3(top4[e], s[i + 2 * e], s[i + 2 * e + 1]);
+                        if (i + 2 * e + 1 < kKeys) top4[e] = max3(top4[e], s[i + 2 * e], s[i + 2 * e + 1]);
                     }
                 }
                 const float top = max3(max3(top4[0], top4[1], top4[2]), top4[3], top4[3]);
@@ -262,15 +255,9 @@ __global__ void __launch_bounds__(ForwardShared<D, SIDES>::kThreads, 3 - SIDES) 
                 // the output is seldom taken out and put back.  It is -infinity as long as all scores are; a score that is NaN or
                 // +infinity makes c times it, and so all of the row's weights, NaN.
                 const bool grows = m > -INFINITY ? !((top - m) * c <= 8.0f) : !(top == -INFINITY);
-                const bool any = __any_sync(0xffffffffu, grows);
-                // weights' columns of their own: the last ones have been used, and so is the output at rest
-                auto used = [&] { return !S::kApart || scored == 0 || tc::bar_wait(done, (scored - 1) & 1); };
-                if (any) {
+                if (__any_sync(0xffffffffu, grows)) {
                     const float to = grows ? top : m, to_c = to == -INFINITY ? 0.0f : (to - to) + to * c;
-                    if (r > 0) {
-                        fine = used();
-                        if (!fine) break;
-                        tc::fence_after();
+                    if (r > 0) {           // (the last scores came after the weighted values before them: the output is at rest)
                         const float f = grows ? (m == -INFINITY ? 0.0f : exp2_fast(mc - to_c)) : 1.0f;
                         l = mul2(l, make_float2(f, f));
 #pragma unroll
@@ -285,14 +272,14 @@ __global__ void __launch_bounds__(ForwardShared<D, SIDES>::kThreads, 3 - SIDES) 
                     m = to;
                     mc = to_c;
                 }
-                if (valid < kTile) {       // the values' rows behind the sequence
+                if (valid < kKeys) {       // the values' rows behind the sequence
                     const int at = 2 * (round + most - 1 - j) + 1;
                     if (!(fine = tc::bar_wait(full + 8 * (at % kRing), (at / kRing) & 1))) break;
-                    clear_rows<D>(mem + (ring - base) + (at % kRing) * S::kBytes, valid, threadIdx.x % 128, 128);
+                    clear_rows<D>(mem + (ring - base) + (at % kRing) * S::kKeyBytes, valid, threadIdx.x % 128, 128);
                 }
                 const float2 cc = make_float2(c, c), minus = make_float2(-mc, -mc);
 #pragma unroll
-                for (int h = 0; h < 2; ++h) {
+                for (int h = 0; h < S::kHalves; ++h) {
                     uint32_t p[32];
 #pragma unroll
                     for (int i = 0; i < 32; ++i) {
@@ -302,18 +289,12 @@ __global__ void __launch_bounds__(ForwardShared<D, SIDES>::kThreads, 3 - SIDES) 
                         l = add2(l, e);
                         p[i] = pack_bf16(e.x, e.y);
                     }
-                    if (h == 0) {
-                        fine = used();
-                        if (!fine) break;
-                        tc::fence_after();
-                    }
-                    tmem_store32(p_at + 32 * h, p);
+                    tmem_store32(s_at + 32 * h, p);
                     tmem_stored();
                     tc::fence_before();
                     __syncwarp();
                     if (lane == 0) tc::bar_arrive(weights + 16 * side + 8 * h);
                 }
-                if (!fine) break;
             }
             round += most;
             if (!fine) break;
@@ -321,12 +302,12 @@ __global__ void __launch_bounds__(ForwardShared<D, SIDES>::kThreads, 3 - SIDES) 
             more = pieces.take(piece, head, fine);                   // the next one's whereabouts, while the last values are being weighed
             if (!fine) break;
             if (n == 0) continue;
-            if (!(fine = tc::bar_wait(done + 8 * side, (S::kApart ? scored - 1 : ended) & 1))) break;
+            if (!(fine = tc::bar_wait(done + 8 * side, ended & 1))) break;
             ++ended;
             tc::fence_after();
             const float sum = l.x + l.y;
             if (left > 0) w.lse[mine * w.lse_ld + start + row] = (mc + log2f(sum)) * kLn2;
-            give_rows<D>(o_at, 1.0f / sum, mem + S::kStages + warp * kStage, w.out, start + row - lane, left + lane, mine, 0, w.dim, lane);
+            give_rows<D>(o_at, 1.0f / sum, mem + S::kStages + warp * kStage, w.out, start + row - lane, left + lane, mine, w.dim, lane);
             tc::fence_before();
         }
     }
@@ -396,8 +377,9 @@ void forward(prod::Call& c, const dlion_attention_fwd& p) {
     const PlanRequest request{sides * kTile, p.causal, 0};
     make_plans(c, seq, &request, 1, &table, &w.plan, p.zero_rest ? &clear : nullptr);
     if (pieces == 0) return;
-    if (!map_rows(&w.q, Operand{p.q, p.q_rs, p.q_hs, p.heads}, p.rows, p.dim) || !map_rows(&w.k, Operand{p.k, p.k_rs, p.k_hs, p.kv_heads}, p.rows, p.dim) ||
-        !map_rows(&w.v, Operand{p.v, p.v_rs, p.v_hs, p.kv_heads}, p.rows, p.dim)) {
+    const int passing = p.dim <= 64 ? kPassing<64> : kPassing<128>;
+    if (!map_rows(&w.q, Operand{p.q, p.q_rs, p.q_hs, p.heads}, p.rows, p.dim, kTile) || !map_rows(&w.k, Operand{p.k, p.k_rs, p.k_hs, p.kv_heads}, p.rows, p.dim, passing) ||
+        !map_rows(&w.v, Operand{p.v, p.v_rs, p.v_hs, p.kv_heads}, p.rows, p.dim, passing)) {
         c.status = DLION_ECUDA;
         return;
     }

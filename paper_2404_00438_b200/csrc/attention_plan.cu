@@ -115,10 +115,10 @@ dlion_status check_operand(const Operand& a, int64_t rows, int64_t dim) {
     return aligned16(a.p) ? DLION_OK : DLION_EALIGN;
 }
 
-bool map_rows(CUtensorMap* map, const Operand& a, int64_t rows, int64_t dim) {
+bool map_rows(CUtensorMap* map, const Operand& a, int64_t rows, int64_t dim, int tile) {
     const uint64_t sizes[3] = {static_cast<uint64_t>(dim), static_cast<uint64_t>(a.heads), static_cast<uint64_t>(rows)};
     const uint64_t strides[2] = {static_cast<uint64_t>(a.heads > 1 ? a.hs : dim) * 2, static_cast<uint64_t>(rows > 1 ? a.rs : dim) * 2};
-    const uint32_t box[3] = {64, 1, kTile};
+    const uint32_t box[3] = {64, 1, static_cast<uint32_t>(tile)};
     return prod::encode_map(map, a.p, 3, sizes, strides, box);
 }
 
