@@ -27,12 +27,14 @@ struct Backward {
     Rows dq, dk, dv;
 };
 
-// Eight warps of arithmetic, a copying, an issuing and other warps.  Of the eight: lanes of tensor memory go by warp % 4, so two warps have the same rows, each 64 columns.  What a warp leaves
+// Four or eight warps of arithmetic, a copying, an issuing and other warps.  Lanes of tensor memory go by warp % 4; of eight warps two
+// have the same rows, each 64 columns.  What a warp leaves
 // there as an operand (64 bf16, 32 columns) goes over the first of the columns that it has read itself, which leaves a gap of 32
 // between the operand's halves.
 
 struct Finish {                            // the end of every kernel: see product_kernel
-    __device__ static void end(bool fine, volatile uint32_t* slot_mem, unsigned int* mark, uint32_t tmem, int warp) {
+    template <uint32_t COLUMNS>
+    __device__ static void end(bool fine, volatile uint32_t* slot_mem, unsigned int* mark, uint32_t tmem, bool frees) {
         if (!fine) {
             slot_mem[1] = 1;
             *mark = 1;
@@ -46,7 +48,7 @@ struct Finish {                            // the end of every kernel: see produ
             }
         }
         tc::fence_after();
-        if (warp == 9) tc::tmem_free<1>(tmem, 512);
+        if (frees) tc::tmem_free<1>(tmem, COLUMNS);
     }
 };
 
@@ -54,24 +56,27 @@ struct Finish {                            // the end of every kernel: see produ
 // Tensor memory: two sets of scores in turn, dp, dq; ds goes over its scores.
 template <int D>
 struct QueryShared {
-    static constexpr uint32_t kBytes = kTile * D * 2;
+    static constexpr int kRows = kPassing<D>, kWarps = kRows / 16;   // of a tile of keys; warps of arithmetic
+    static constexpr uint32_t kBytes = kTile * D * 2, kRowBytes = kRows * D * 2;
     static constexpr int kKeys = 3, kValues = 2;                     // stages
-    static constexpr uint32_t kStats = (2 + kKeys + kValues) * kBytes;                // lse and D of the tile of queries
+    static constexpr uint32_t kStats = 2 * kBytes + (kKeys + kValues) * kRowBytes;    // lse and D of the tile of queries
     static constexpr uint32_t kBars = kStats + 2 * kTile * 4;
     static constexpr uint32_t kAll = kBars + 256 + kTurnBytes + 1024;
+    static constexpr uint32_t kColumns = D == 64 ? 256 : 512;        // of tensor memory
+    static constexpr int kThreads = 32 * kWarps + 128;               // a copying and an issuing warp, and two that work out D ahead of time
 };
 
-constexpr int kQueryThreads = 384;         // and two warps that work out D ahead of time
-
 template <int D>
-__global__ void __launch_bounds__(kQueryThreads, 1) query_gradient_kernel(const __grid_constant__ Backward w, unsigned int* mark) {
+__global__ void __launch_bounds__(QueryShared<D>::kThreads, 512 / QueryShared<D>::kColumns) query_gradient_kernel(const __grid_constant__ Backward w, unsigned int* mark) {
     using S = QueryShared<D>;
+    constexpr int kRows = S::kRows, kCopying = S::kWarps, kIssuing = kCopying + 1, kAhead = kCopying + 2;
     extern __shared__ uint8_t raw[];
     const uint32_t base = (tc::smem_addr(raw) + 1023u) & ~1023u;
     uint8_t* mem = raw + (base - tc::smem_addr(raw));
-    const uint32_t keys = base + 2 * S::kBytes, values = keys + S::kKeys * S::kBytes, bars = base + S::kBars;
+    const uint32_t keys = base + 2 * S::kBytes, values = keys + S::kKeys * S::kRowBytes, bars = base + S::kBars;
     const uint32_t k_full = bars, k_empty = bars + 32, v_full = bars + 64, v_empty = bars + 96, scores = bars + 128, products = bars + 144,
-                   taken = bars + 152, slopes = bars + 160, rows_full = bars + 168, done = bars + 176, rows_empty = bars + 184, stats_full = bars + 192, stats_empty = bars + 200, slot = bars + 208;
+                   taken = bars + 152, slopes = bars + 160, rows_full = bars + 176, done = bars + 184, rows_empty = bars + 192, stats_full = bars + 200,
+                   stats_empty = bars + 208, slot = bars + 216;
     const uint32_t turns = bars + 256;
     volatile uint32_t* slot_mem = reinterpret_cast<volatile uint32_t*>(mem + (slot - base));
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
@@ -79,7 +84,7 @@ __global__ void __launch_bounds__(kQueryThreads, 1) query_gradient_kernel(const 
     tc::let_next_start();
     if (threadIdx.x == 0) {
         tc::bar_init(stats_full, 2);
-        tc::bar_init(stats_empty, 8);
+        tc::bar_init(stats_empty, S::kWarps);
         for (int i = 0; i < S::kKeys; ++i) {
             tc::bar_init(k_full + 8 * i, 1);
             tc::bar_init(k_empty + 8 * i, 1);
@@ -91,8 +96,9 @@ __global__ void __launch_bounds__(kQueryThreads, 1) query_gradient_kernel(const 
         tc::bar_init(scores, 1);
         tc::bar_init(scores + 8, 1);
         tc::bar_init(products, 1);
-        tc::bar_init(taken, 8);
-        tc::bar_init(slopes, 8);
+        tc::bar_init(taken, S::kWarps);
+        tc::bar_init(slopes, S::kWarps);                             // in turn: the next ones may all be there before these have been awaited
+        tc::bar_init(slopes + 8, S::kWarps);
         tc::bar_init(rows_full, 1);
         tc::bar_init(rows_empty, 1);
         tc::bar_init(done, 1);
@@ -104,11 +110,11 @@ __global__ void __launch_bounds__(kQueryThreads, 1) query_gradient_kernel(const 
         tc::prefetch_map(&w.v);
         tc::prefetch_map(&w.dout);
     }
-    if (warp == 9) tc::tmem_alloc<1>(slot, 512);
+    if (warp == kIssuing) tc::tmem_alloc<1>(slot, S::kColumns);
     tc::fence_before();
     __syncthreads();
     tc::fence_after();
-    const uint32_t tmem = same(*slot_mem), products_at = tmem + 256, dq_at = tmem + 384;
+    const uint32_t tmem = same(*slot_mem), products_at = tmem + 2 * kRows, dq_at = products_at + kRows;
     bool fine = true;
     tc::wait_for_previous();
 
@@ -117,11 +123,10 @@ __global__ void __launch_bounds__(kQueryThreads, 1) query_gradient_kernel(const 
     int head = 0, row0 = 0, n = 0;         // a piece's first row in the sequence, and its tiles of keys, from the last to the first
     auto divide = [&] {
         row0 = piece.tile * kTile;
-        const int key_tiles = (piece.length + kTile - 1) / kTile;
-        n = w.causal ? min(key_tiles, piece.tile + 1) : key_tiles;
+        n = (min(piece.length, w.causal ? row0 + kTile : piece.length) + kRows - 1) / kRows;
     };
 
-    if (warp == 8) {
+    if (warp == kCopying) {
         int i = 0, begun = 0, k_asked = 0, v_asked = 0, asked = 0;           // tiles of keys, and pieces, of all
         while (fine && pieces.take(piece, head, fine)) {
             divide();
@@ -131,11 +136,11 @@ __global__ void __launch_bounds__(kQueryThreads, 1) query_gradient_kernel(const 
                     asked = pieces.turn;
                     if (!(fine = pieces.ask())) break;
                 }
-                const int row = piece.start + (n - 1 - r) * kTile, ks = i % S::kKeys, vs = i % S::kValues;
+                const int row = piece.start + (n - 1 - r) * kRows, ks = i % S::kKeys, vs = i % S::kValues;
                 if (!(fine = tc::bar_wait(k_empty + 8 * ks, ((i / S::kKeys) & 1) ^ 1))) break;
                 if (tc::elected()) {
-                    tc::bar_expect(k_full + 8 * ks, S::kBytes);
-                    load_head<D>(keys + ks * S::kBytes, &w.k, kv_head, row, k_full + 8 * ks);
+                    tc::bar_expect(k_full + 8 * ks, S::kRowBytes);
+                    load_head<D>(keys + ks * S::kRowBytes, &w.k, kv_head, row, k_full + 8 * ks);
                 }
                 __syncwarp();
                 ++k_asked;
@@ -151,8 +156,8 @@ __global__ void __launch_bounds__(kQueryThreads, 1) query_gradient_kernel(const 
                 }
                 if (!(fine = tc::bar_wait(v_empty + 8 * vs, ((i / S::kValues) & 1) ^ 1))) break;
                 if (tc::elected()) {
-                    tc::bar_expect(v_full + 8 * vs, S::kBytes);
-                    load_head<D>(values + vs * S::kBytes, &w.v, kv_head, row, v_full + 8 * vs);
+                    tc::bar_expect(v_full + 8 * vs, S::kRowBytes);
+                    load_head<D>(values + vs * S::kRowBytes, &w.v, kv_head, row, v_full + 8 * vs);
                 }
                 __syncwarp();
                 ++v_asked;
@@ -164,7 +169,7 @@ __global__ void __launch_bounds__(kQueryThreads, 1) query_gradient_kernel(const 
             for (int a = max(0, k_asked - S::kKeys); a < k_asked; ++a) tc::bar_wait(k_full + 8 * (a % S::kKeys), (a / S::kKeys) & 1);
             for (int a = max(0, v_asked - S::kValues); a < v_asked; ++a) tc::bar_wait(v_full + 8 * (a % S::kValues), (a / S::kValues) & 1);
         }
-    } else if (warp == 9) {
+    } else if (warp == kIssuing) {
         const int k_steps = (w.dim + 15) / 16;
         const uint32_t wide = tc::instruction(kTile, k_steps * 16, 0, 1);
         auto finished = [&](uint32_t bar) {
@@ -177,9 +182,9 @@ __global__ void __launch_bounds__(kQueryThreads, 1) query_gradient_kernel(const 
         bool first = false, last = false;
         auto gather = [&] {
             const int b = i - 1;
-            if (!(fine = tc::bar_wait(slopes, b & 1))) return;
+            if (!(fine = tc::bar_wait(slopes + 8 * (b & 1), (b >> 1) & 1))) return;
             tc::fence_after();
-            weights_by_rows<0, 8, 32>(dq_at, tmem + (b & 1) * kTile, keys + (b % S::kKeys) * S::kBytes, wide, steps, !first);
+            weights_by_rows<0, kRows / 16, 32>(dq_at, tmem + (b & 1) * kRows, keys + (b % S::kKeys) * S::kRowBytes, wide, steps, !first);
             if (last) finished(done);
             finished(k_empty + 8 * (b % S::kKeys));
         };
@@ -189,25 +194,25 @@ __global__ void __launch_bounds__(kQueryThreads, 1) query_gradient_kernel(const 
                 if (r == 0 && !(fine = tc::bar_wait(rows_full, begun++ & 1))) break;
                 if (!(fine = tc::bar_wait(k_full + 8 * (i % S::kKeys), (i / S::kKeys) & 1))) break;
                 tc::fence_after();
-                rows_by_rows<D, kTile>(tmem + (i & 1) * kTile, base, keys + (i % S::kKeys) * S::kBytes, k_steps);
+                rows_by_rows<D, kRows>(tmem + (i & 1) * kRows, base, keys + (i % S::kKeys) * S::kRowBytes, k_steps);
                 finished(scores + 8 * (i & 1));
                 if (!(fine = tc::bar_wait(v_full + 8 * (i % S::kValues), (i / S::kValues) & 1))) break;
                 if (i > 0 && !(fine = tc::bar_wait(taken, (i - 1) & 1))) break;
                 tc::fence_after();
-                rows_by_rows<D, kTile>(products_at, base + S::kBytes, values + (i % S::kValues) * S::kBytes, k_steps);
+                rows_by_rows<D, kRows>(products_at, base + S::kBytes, values + (i % S::kValues) * S::kRowBytes, k_steps);
                 finished(products);
                 finished(v_empty + 8 * (i % S::kValues));
                 if (r == n - 1) finished(rows_empty);
                 if (i > 0) gather();
-                steps = (min(kTile, piece.length - (n - 1 - r) * kTile) + 15) / 16;
+                steps = (min(kRows, piece.length - (n - 1 - r) * kRows) + 15) / 16;
                 first = r == 0;
                 last = r == n - 1;
             }
         }
         if (fine && i > 0) gather();
-    } else if (warp >= 10) {
+    } else if (warp >= kAhead) {
         // D = do . out of half the tile's rows, D / 8 lanes a row, while the others work on the piece before
-        constexpr int kLanes = D / 8, kRows = 32 / kLanes, kAtOnce = 8;
+        constexpr int kLanes = D / 8, kEach = 32 / kLanes, kAtOnce = D == 64 ? 4 : 8;
         float* stats = reinterpret_cast<float*>(mem + S::kStats);
         const int unit = lane % kLanes;
         int begun = 0;
@@ -216,15 +221,15 @@ __global__ void __launch_bounds__(kQueryThreads, 1) query_gradient_kernel(const 
             float lse[2];
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
-                const int row = row0 + (warp - 10) * (kTile / 2) + e * 32 + lane;
+                const int row = row0 + (warp - kAhead) * (kTile / 2) + e * 32 + lane;
                 lse[e] = row < piece.length ? w.lse[head * w.lse_ld + piece.start + row] * kLog2e : 0.0f;
             }
             if (!(fine = tc::bar_wait(stats_empty, (begun & 1) ^ 1))) break;
-            for (int first = (warp - 10) * (kTile / 2); first < (warp - 9) * (kTile / 2); first += kAtOnce * kRows) {
+            for (int first = (warp - kAhead) * (kTile / 2); first < (warp - kAhead + 1) * (kTile / 2); first += kAtOnce * kEach) {
                 uint4 o[kAtOnce], d[kAtOnce];
 #pragma unroll
                 for (int u = 0; u < kAtOnce; ++u) {
-                    const int row = row0 + first + u * kRows + lane / kLanes;
+                    const int row = row0 + first + u * kEach + lane / kLanes;
                     const bool live = row < piece.length && unit * 8 < w.dim;
                     const int64_t at = piece.start + row;
                     o[u] = live ? *reinterpret_cast<const uint4*>(w.out.p + at * w.out.rs + head * w.out.hs + unit * 8) : make_uint4(0, 0, 0, 0);
@@ -240,7 +245,7 @@ __global__ void __launch_bounds__(kQueryThreads, 1) query_gradient_kernel(const 
                     float delta = sum.x + sum.y;
 #pragma unroll
                     for (int e = kLanes / 2; e >= 1; e /= 2) delta += __shfl_xor_sync(0xffffffffu, delta, e);
-                    const int in_tile = first + u * kRows + lane / kLanes;
+                    const int in_tile = first + u * kEach + lane / kLanes;
                     if (unit == 0 && row0 + in_tile < piece.length) {
                         const int64_t at = piece.start + row0 + in_tile;
                         w.delta[head * w.delta_ld + at] = delta;
@@ -249,7 +254,7 @@ __global__ void __launch_bounds__(kQueryThreads, 1) query_gradient_kernel(const 
                 }
             }
 #pragma unroll
-            for (int e = 0; e < 2; ++e) stats[(warp - 10) * (kTile / 2) + e * 32 + lane] = lse[e];
+            for (int e = 0; e < 2; ++e) stats[(warp - kAhead) * (kTile / 2) + e * 32 + lane] = lse[e];
             __syncwarp();
             if (lane == 0) tc::bar_arrive(stats_full);
             ++begun;
@@ -271,8 +276,8 @@ __global__ void __launch_bounds__(kQueryThreads, 1) query_gradient_kernel(const 
             if (lane == 0) tc::bar_arrive(stats_empty);
             const float2 minus = twice(-lse2), less = twice(-delta);
             for (int r = 0; r < n; ++r, ++i) {
-                const int j = n - 1 - r, valid = piece.length - j * kTile;
-                const uint32_t s_at = tmem + (i & 1) * kTile + half * 64 + lanes;
+                const int j = n - 1 - r, valid = piece.length - j * kRows;
+                const uint32_t s_at = tmem + (i & 1) * kRows + half * 64 + lanes;
                 if (!(fine = tc::bar_wait(scores + 8 * (i & 1), (i >> 1) & 1))) break;
                 tc::fence_after();
                 float s[64];
@@ -296,13 +301,13 @@ __global__ void __launch_bounds__(kQueryThreads, 1) query_gradient_kernel(const 
                     s[e] = x.x;
                     s[e + 1] = x.y;
                 }
-                if (valid < kTile || (w.causal && (j + 1) * kTile > row0)) {
-                    const int behind = (w.causal ? min(row, piece.length - 1) : piece.length - 1) - j * kTile - half * 64;
+                if (valid < kRows || (w.causal && (j + 1) * kRows > row0)) {
+                    const int behind = (w.causal ? min(row, piece.length - 1) : piece.length - 1) - j * kRows - half * 64;
 #pragma unroll
                     for (int e = 0; e < 64; ++e) s[e] = e <= behind ? s[e] : 0.0f;
-                    if (valid < kTile) {   // the keys' rows behind the sequence
+                    if (valid < kRows) {   // the keys' rows behind the sequence
                         if (!(fine = tc::bar_wait(k_full + 8 * (i % S::kKeys), (i / S::kKeys) & 1))) break;
-                        clear_rows<D>(mem + (keys - base) + (i % S::kKeys) * S::kBytes, valid, threadIdx.x, 256);
+                        clear_rows<D>(mem + (keys - base) + (i % S::kKeys) * S::kRowBytes, valid, threadIdx.x, 32 * S::kWarps);
                     }
                 }
                 uint32_t p[32];
@@ -312,43 +317,43 @@ __global__ void __launch_bounds__(kQueryThreads, 1) query_gradient_kernel(const 
                 tmem_stored();
                 tc::fence_before();
                 __syncwarp();
-                if (lane == 0) tc::bar_arrive(slopes);
+                if (lane == 0) tc::bar_arrive(slopes + 8 * (i & 1));
             }
             if (!fine) break;
-            __nv_bfloat16* to = w.dq.p + static_cast<int64_t>(piece.start + row) * w.dq.rs + head * w.dq.hs + half * (D / 2);
+            constexpr int kColumns = D * 64 / kRows;                 // of dq: all, or half of them a warp
+            __nv_bfloat16* to = w.dq.p + static_cast<int64_t>(piece.start + row) * w.dq.rs + head * w.dq.hs + half * kColumns;
             more = pieces.take(piece, head, fine);                   // the next one's whereabouts, while the last product runs
             if (!fine || !(fine = tc::bar_wait(done, ended++ & 1))) break;
             tc::fence_after();
-            give_row<D / 2>(dq_at + half * (D / 2) + lanes, w.scale, to, live, w.dim - half * (D / 2));
+            give_row<kColumns>(dq_at + half * kColumns + lanes, w.scale, to, live, w.dim - half * kColumns);
             tc::fence_before();
         }
     }
-    Finish::end(fine, slot_mem, mark, tmem, warp);
+    Finish::end<S::kColumns>(fine, slot_mem, mark, tmem, warp == kIssuing);
 }
 
 // ---------------------------------------------------------------- dk, dv
-// Scores and dp are computed transposed, keys as rows: so p and ds are operands as they lie in tensor memory.  There is room for a second
-// set of scores beside dk and dv of 64 columns: the next scores then do not wait for dv.
+// Scores and dp are computed transposed, keys as rows: so p and ds are operands as they lie in tensor memory.
 template <int D>
 struct KeyShared {
-    static constexpr uint32_t kBytes = kTile * D * 2;
+    static constexpr int kRows = kPassing<D>, kWarps = kRows / 16;   // of a tile of queries; warps of arithmetic
+    static constexpr uint32_t kBytes = kTile * D * 2, kRowBytes = kRows * D * 2;
     static constexpr int kStages = D == 64 ? 3 : 2;                  // of queries and of do
-    static constexpr uint32_t kStats = (2 + 2 * kStages) * kBytes;   // lse and D of two tiles of queries
-    static constexpr uint32_t kBars = kStats + 2 * 2 * kTile * 4;
+    static constexpr uint32_t kStats = 2 * kBytes + 2 * kStages * kRowBytes;          // lse and D of two tiles of queries
+    static constexpr uint32_t kBars = kStats + 2 * 2 * kRows * 4;
     static constexpr uint32_t kAll = kBars + 256 + kTurnBytes + 1024;
-    static constexpr int kSets = D == 64 ? 2 : 1;
+    static constexpr uint32_t kColumns = D == 64 ? 256 : 512;        // of tensor memory
+    static constexpr int kThreads = 32 * kWarps + 96;                // a copying and an issuing warp, and one that brings lse and D
 };
 
-constexpr int kKeyThreads = 352;           // and a warp that brings lse and D
-
 template <int D>
-__global__ void __launch_bounds__(kKeyThreads, 1) key_gradient_kernel(const __grid_constant__ Backward w, unsigned int* mark) {
+__global__ void __launch_bounds__(KeyShared<D>::kThreads, 512 / KeyShared<D>::kColumns) key_gradient_kernel(const __grid_constant__ Backward w, unsigned int* mark) {
     using S = KeyShared<D>;
-    constexpr int kStages = S::kStages, kSets = S::kSets;
+    constexpr int kRows = S::kRows, kStages = S::kStages, kCopying = S::kWarps, kIssuing = kCopying + 1, kAhead = kCopying + 2;
     extern __shared__ uint8_t raw[];
     const uint32_t base = (tc::smem_addr(raw) + 1023u) & ~1023u;
     uint8_t* mem = raw + (base - tc::smem_addr(raw));
-    const uint32_t queries = base + 2 * S::kBytes, douts = queries + kStages * S::kBytes, bars = base + S::kBars;
+    const uint32_t queries = base + 2 * S::kBytes, douts = queries + kStages * S::kRowBytes, bars = base + S::kBars;
     const uint32_t q_full = bars, q_empty = bars + 24, d_full = bars + 48, d_empty = bars + 72, scores = bars + 96, products = bars + 112,
                    weights = bars + 120, slopes = bars + 128, rows_full = bars + 136, done = bars + 144, rows_empty = bars + 152,
                    stats_full = bars + 160, stats_empty = bars + 176, slot = bars + 192;
@@ -365,13 +370,13 @@ __global__ void __launch_bounds__(kKeyThreads, 1) key_gradient_kernel(const __gr
             tc::bar_init(d_empty + 8 * i, 1);
         }
         for (int i = 0; i < 2; ++i) {
-            tc::bar_init(scores + 8 * i, 1);
             tc::bar_init(stats_full + 8 * i, 1);
-            tc::bar_init(stats_empty + 8 * i, 8);
+            tc::bar_init(stats_empty + 8 * i, S::kWarps);
         }
+        tc::bar_init(scores, 1);
         tc::bar_init(products, 1);
-        tc::bar_init(weights, 8);
-        tc::bar_init(slopes, 8);
+        tc::bar_init(weights, S::kWarps);
+        tc::bar_init(slopes, S::kWarps);
         tc::bar_init(rows_full, 1);
         tc::bar_init(rows_empty, 1);
         tc::bar_init(done, 1);
@@ -383,11 +388,11 @@ __global__ void __launch_bounds__(kKeyThreads, 1) key_gradient_kernel(const __gr
         tc::prefetch_map(&w.v);
         tc::prefetch_map(&w.dout);
     }
-    if (warp == 9) tc::tmem_alloc<1>(slot, 512);
+    if (warp == kIssuing) tc::tmem_alloc<1>(slot, S::kColumns);
     tc::fence_before();
     __syncthreads();
     tc::fence_after();
-    const uint32_t tmem = same(*slot_mem), products_at = tmem + kSets * kTile, dk_at = products_at + kTile, dv_at = dk_at + D;
+    const uint32_t tmem = same(*slot_mem), products_at = tmem + kRows, dk_at = products_at + kRows, dv_at = dk_at + D;
     bool fine = true;
     tc::wait_for_previous();
 
@@ -397,8 +402,8 @@ __global__ void __launch_bounds__(kKeyThreads, 1) key_gradient_kernel(const __gr
     const int group = static_cast<int>(w.group.d);
     auto divide = [&] {
         key0 = piece.tile * kTile;
-        first = w.causal ? piece.tile : 0;
-        per = (piece.length + kTile - 1) / kTile - first;
+        first = w.causal ? key0 / kRows : 0;
+        per = (piece.length + kRows - 1) / kRows - first;
         n = per * group;
     };
     // The tiles of queries in turn: the query heads that share these keys one after the other.
@@ -414,7 +419,7 @@ __global__ void __launch_bounds__(kKeyThreads, 1) key_gradient_kernel(const __gr
         }
     };
 
-    if (warp == 8) {
+    if (warp == kCopying) {
         int i = 0, begun = 0, q_asked = 0, d_asked = 0, asked = 0;
         while (fine && pieces.take(piece, kv_head, fine)) {
             divide();
@@ -424,12 +429,12 @@ __global__ void __launch_bounds__(kKeyThreads, 1) key_gradient_kernel(const __gr
                     asked = pieces.turn;
                     if (!(fine = pieces.ask())) break;
                 }
-                const int row = piece.start + tile * kTile, st = i % kStages;
+                const int row = piece.start + tile * kRows, st = i % kStages;
                 const uint32_t parity = ((i / kStages) & 1) ^ 1;
                 if (!(fine = tc::bar_wait(q_empty + 8 * st, parity))) break;
                 if (tc::elected()) {
-                    tc::bar_expect(q_full + 8 * st, S::kBytes);
-                    load_head<D>(queries + st * S::kBytes, &w.q, head, row, q_full + 8 * st);
+                    tc::bar_expect(q_full + 8 * st, S::kRowBytes);
+                    load_head<D>(queries + st * S::kRowBytes, &w.q, head, row, q_full + 8 * st);
                 }
                 __syncwarp();
                 ++q_asked;
@@ -445,8 +450,8 @@ __global__ void __launch_bounds__(kKeyThreads, 1) key_gradient_kernel(const __gr
                 }
                 if (!(fine = tc::bar_wait(d_empty + 8 * st, parity))) break;
                 if (tc::elected()) {
-                    tc::bar_expect(d_full + 8 * st, S::kBytes);
-                    load_head<D>(douts + st * S::kBytes, &w.dout, head, row, d_full + 8 * st);
+                    tc::bar_expect(d_full + 8 * st, S::kRowBytes);
+                    load_head<D>(douts + st * S::kRowBytes, &w.dout, head, row, d_full + 8 * st);
                 }
                 __syncwarp();
                 ++d_asked;
@@ -458,7 +463,7 @@ __global__ void __launch_bounds__(kKeyThreads, 1) key_gradient_kernel(const __gr
             for (int a = max(0, q_asked - kStages); a < q_asked; ++a) tc::bar_wait(q_full + 8 * (a % kStages), (a / kStages) & 1);
             for (int a = max(0, d_asked - kStages); a < d_asked; ++a) tc::bar_wait(d_full + 8 * (a % kStages), (a / kStages) & 1);
         }
-    } else if (warp == 10) {
+    } else if (warp == kAhead) {
         float* stats = reinterpret_cast<float*>(mem + S::kStats);
         int i = 0;
         while (fine && pieces.take(piece, kv_head, fine)) {
@@ -466,25 +471,25 @@ __global__ void __launch_bounds__(kKeyThreads, 1) key_gradient_kernel(const __gr
             begin();
             for (int r = 0; r < n; ++r, ++i, advance()) {
                 const int st = i & 1;
-                float lse[4], delta[4];
+                float lse[kRows / 32], delta[kRows / 32];
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const int row = tile * kTile + e * 32 + lane;
+                for (int e = 0; e < kRows / 32; ++e) {
+                    const int row = tile * kRows + e * 32 + lane;
                     const bool live = row < piece.length;
                     lse[e] = live ? w.lse[head * w.lse_ld + piece.start + row] * kLog2e : 0.0f;
                     delta[e] = live ? w.delta[head * w.delta_ld + piece.start + row] : 0.0f;
                 }
                 if (!(fine = tc::bar_wait(stats_empty + 8 * st, ((i >> 1) & 1) ^ 1))) break;
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    stats[st * 2 * kTile + e * 32 + lane] = -lse[e];
-                    stats[st * 2 * kTile + kTile + e * 32 + lane] = -delta[e];
+                for (int e = 0; e < kRows / 32; ++e) {
+                    stats[st * 2 * kRows + e * 32 + lane] = -lse[e];
+                    stats[st * 2 * kRows + kRows + e * 32 + lane] = -delta[e];
                 }
                 __syncwarp();
                 if (lane == 0) tc::bar_arrive(stats_full + 8 * st);
             }
         }
-    } else if (warp == 9) {
+    } else if (warp == kIssuing) {
         const int k_steps = (w.dim + 15) / 16;
         const uint32_t wide = tc::instruction(kTile, k_steps * 16, 0, 1);
         auto finished = [&](uint32_t bar) {
@@ -497,45 +502,44 @@ __global__ void __launch_bounds__(kKeyThreads, 1) key_gradient_kernel(const __gr
             const int st = i % kStages;
             if (!(fine = tc::bar_wait(q_full + 8 * st, (i / kStages) & 1))) return;
             tc::fence_after();
-            rows_by_rows<D, kTile>(tmem + (i % kSets) * kTile, base, queries + st * S::kBytes, k_steps);
-            finished(scores + 8 * (i % kSets));
+            rows_by_rows<D, kRows>(tmem, base, queries + st * S::kRowBytes, k_steps);
+            finished(scores);
         };
         auto product = [&] {
             const int st = i % kStages;
             if (!(fine = tc::bar_wait(d_full + 8 * st, (i / kStages) & 1))) return;
             tc::fence_after();
-            rows_by_rows<D, kTile>(products_at, base + S::kBytes, douts + st * S::kBytes, k_steps);
+            rows_by_rows<D, kRows>(products_at, base + S::kBytes, douts + st * S::kRowBytes, k_steps);
             finished(products);
         };
         auto gather_v = [&] {
             const int b = i - 1, sb = b % kStages;
             if (!(fine = tc::bar_wait(weights, b & 1))) return;
             tc::fence_after();
-            weights_by_rows<0, 8, 32>(dv_at, tmem + (b % kSets) * kTile, douts + sb * S::kBytes, wide, steps, !opening);
+            weights_by_rows<0, kRows / 16, 32>(dv_at, tmem, douts + sb * S::kRowBytes, wide, steps, !opening);
             finished(d_empty + 8 * sb);
         };
         auto gather_k = [&] {
             const int b = i - 1, sb = b % kStages;
             if (!(fine = tc::bar_wait(slopes, b & 1))) return;
             tc::fence_after();
-            weights_by_rows<0, 8, 32>(dk_at, products_at, queries + sb * S::kBytes, wide, steps, !opening);
+            weights_by_rows<0, kRows / 16, 32>(dk_at, products_at, queries + sb * S::kRowBytes, wide, steps, !opening);
             finished(q_empty + 8 * sb);
             if (last) finished(done);
         };
-        // A round: dv of the round before, the scores, over its weights where there is one set; dk of the round before, dp over its slopes.
+        // A round: dv of the round before, the scores over its weights, dk of the round before, dp over its slopes.
         while (fine && pieces.take(piece, kv_head, fine)) {
             divide();
             begin();
             for (int r = 0; r < n && fine; ++r, ++i, advance()) {
                 if (r == 0 && !(fine = tc::bar_wait(rows_full, begun++ & 1))) break;
-                if (kSets == 2) score();
-                if (fine && i > 0) gather_v();
-                if (fine && kSets == 1) score();
+                if (i > 0) gather_v();
+                if (fine) score();
                 if (fine && i > 0) gather_k();
                 if (fine) product();
                 if (!fine) break;
                 if (r == n - 1) finished(rows_empty);
-                steps = (min(kTile, piece.length - tile * kTile) + 15) / 16;
+                steps = (min(kRows, piece.length - tile * kRows) + 15) / 16;
                 opening = r == 0;
                 last = r == n - 1;
             }
@@ -545,7 +549,7 @@ __global__ void __launch_bounds__(kKeyThreads, 1) key_gradient_kernel(const __gr
     } else {
         const int half = warp / 4, quarter = warp % 4;
         const uint32_t lanes = static_cast<uint32_t>(quarter * 32) << 16;
-        const uint32_t d_at = products_at + half * 64 + lanes;
+        const uint32_t s_at = tmem + half * 64 + lanes, d_at = products_at + half * 64 + lanes;
         const float* stats = reinterpret_cast<const float*>(mem + S::kStats);
         const float2 cc = twice(w.c);
         int i = 0, ended = 0;
@@ -555,14 +559,13 @@ __global__ void __launch_bounds__(kKeyThreads, 1) key_gradient_kernel(const __gr
             begin();
             const int key = key0 + quarter * 32 + lane;
             for (int r = 0; r < n; ++r, ++i, advance()) {
-                const int st = i & 1, valid = piece.length - tile * kTile;
-                const uint32_t s_at = tmem + (i % kSets) * kTile + half * 64 + lanes;
-                const float4* lse = reinterpret_cast<const float4*>(stats + st * 2 * kTile + half * 64);
-                const float4* delta = lse + kTile / 4;
-                const bool masked = valid < kTile || (w.causal && tile == piece.tile);
-                const int low = w.causal ? key - tile * kTile - half * 64 : 0, high = valid - half * 64;     // queries [low, high) of this warp's columns
+                const int st = i & 1, valid = piece.length - tile * kRows;
+                const float4* lse = reinterpret_cast<const float4*>(stats + st * 2 * kRows + half * 64);
+                const float4* delta = lse + kRows / 4;
+                const bool masked = valid < kRows || (w.causal && tile * kRows < key0 + kTile);
+                const int low = w.causal ? key - tile * kRows - half * 64 : 0, high = valid - half * 64;     // queries [low, high) of this warp's columns
                 if (!(fine = tc::bar_wait(stats_full + 8 * st, (i >> 1) & 1))) break;
-                if (!(fine = tc::bar_wait(scores + 8 * (i % kSets), (i / kSets) & 1))) break;
+                if (!(fine = tc::bar_wait(scores, i & 1))) break;
                 tc::fence_after();
                 float s[64];
                 tmem_load64(s_at, s);
@@ -578,13 +581,13 @@ __global__ void __launch_bounds__(kKeyThreads, 1) key_gradient_kernel(const __gr
                 if (masked) {
 #pragma unroll
                     for (int e = 0; e < 64; ++e) s[e] = e >= low && e < high ? s[e] : 0.0f;
-                    if (valid < kTile) {   // the queries' rows behind the sequence
+                    if (valid < kRows) {   // the queries' rows behind the sequence
                         const int at = i % kStages;
                         const uint32_t parity = (i / kStages) & 1;
                         if (!(fine = tc::bar_wait(q_full + 8 * at, parity))) break;
                         if (!(fine = tc::bar_wait(d_full + 8 * at, parity))) break;
-                        clear_rows<D>(mem + (queries - base) + at * S::kBytes, valid, threadIdx.x, 256);
-                        clear_rows<D>(mem + (douts - base) + at * S::kBytes, valid, threadIdx.x, 256);
+                        clear_rows<D>(mem + (queries - base) + at * S::kRowBytes, valid, threadIdx.x, 32 * S::kWarps);
+                        clear_rows<D>(mem + (douts - base) + at * S::kRowBytes, valid, threadIdx.x, 32 * S::kWarps);
                     }
                 }
                 uint32_t p[32];
@@ -625,7 +628,7 @@ __global__ void __launch_bounds__(kKeyThreads, 1) key_gradient_kernel(const __gr
                 }
             }
             if (!fine) break;
-            constexpr int kHalf = D / 2;
+            constexpr int kHalf = D * 64 / kRows;                    // columns of a warp: all, or half of them
             const bool live = key < piece.length;
             const int64_t at = piece.start + key;
             __nv_bfloat16 *to_k = w.dk.p + at * w.dk.rs + kv_head * w.dk.hs + half * kHalf, *to_v = w.dv.p + at * w.dv.rs + kv_head * w.dv.hs + half * kHalf;
@@ -637,7 +640,7 @@ __global__ void __launch_bounds__(kKeyThreads, 1) key_gradient_kernel(const __gr
             tc::fence_before();
         }
     }
-    Finish::end(fine, slot_mem, mark, tmem, warp);
+    Finish::end<S::kColumns>(fine, slot_mem, mark, tmem, warp == kIssuing);
 }
 
 Sequences sequences_of(const dlion_attention_bwd& p) { return Sequences{p.rows, p.length, p.sequences, p.offsets, p.offsets_64}; }
@@ -661,15 +664,24 @@ dlion_status check(const dlion_attention_bwd* p) {
 }
 
 template <int D>
-void launch(prod::Call& c, Backward& w, const Plan* plans, int64_t pieces, int64_t heads, int64_t kv_heads) {
+void launch(prod::Call& c, Backward& w, const dlion_attention_bwd& p, const Plan* plans, int64_t pieces) {
     prod::raise_shared(c, &query_gradient_kernel<D>, QueryShared<D>::kAll);
     prod::raise_shared(c, &key_gradient_kernel<D>, KeyShared<D>::kAll);
+    // the tiles that a block keeps, and those that pass by
+    auto maps = [&](int queries, int keys) {
+        return map_rows(&w.q, Operand{p.q, p.q_rs, p.q_hs, p.heads}, p.rows, p.dim, queries) &&
+               map_rows(&w.dout, Operand{p.dout, p.dout_rs, p.dout_hs, p.heads}, p.rows, p.dim, queries) &&
+               map_rows(&w.k, Operand{p.k, p.k_rs, p.k_hs, p.kv_heads}, p.rows, p.dim, keys) &&
+               map_rows(&w.v, Operand{p.v, p.v_rs, p.v_hs, p.kv_heads}, p.rows, p.dim, keys);
+    };
+    if (!maps(kTile, kPassing<D>)) c.status = DLION_ECUDA;
     w.plan = plans[0];
-    w.heads = divisor(heads);
-    prod::start(c, query_gradient_kernel<D>, dim3(static_cast<unsigned>(pieces * heads)), dim3(kQueryThreads), QueryShared<D>::kAll, 1, w, c.mark);
+    w.heads = divisor(p.heads);
+    prod::start(c, query_gradient_kernel<D>, dim3(static_cast<unsigned>(pieces * p.heads)), dim3(QueryShared<D>::kThreads), QueryShared<D>::kAll, 1, w, c.mark);
+    if (!maps(kPassing<D>, kTile)) c.status = DLION_ECUDA;
     w.plan = plans[1];
-    w.heads = divisor(kv_heads);
-    prod::start(c, key_gradient_kernel<D>, dim3(static_cast<unsigned>(pieces * kv_heads)), dim3(kKeyThreads), KeyShared<D>::kAll, 1, w, c.mark);
+    w.heads = divisor(p.kv_heads);
+    prod::start(c, key_gradient_kernel<D>, dim3(static_cast<unsigned>(pieces * p.kv_heads)), dim3(KeyShared<D>::kThreads), KeyShared<D>::kAll, 1, w, c.mark);
 }
 
 void backward(prod::Call& c, const dlion_attention_bwd& p) {
@@ -702,12 +714,6 @@ void backward(prod::Call& c, const dlion_attention_bwd& p) {
     Plan plans[2];
     make_plans(c, seq, requests, 2, tables, plans, p.zero_rest ? &clear : nullptr);
     if (pieces == 0) return;
-    if (!map_rows(&w.q, Operand{p.q, p.q_rs, p.q_hs, p.heads}, p.rows, p.dim, kTile) || !map_rows(&w.k, Operand{p.k, p.k_rs, p.k_hs, p.kv_heads}, p.rows, p.dim, kTile) ||
-        !map_rows(&w.v, Operand{p.v, p.v_rs, p.v_hs, p.kv_heads}, p.rows, p.dim, kTile) ||
-        !map_rows(&w.dout, Operand{p.dout, p.dout_rs, p.dout_hs, p.heads}, p.rows, p.dim, kTile)) {
-        c.status = DLION_ECUDA;
-        return;
-    }
     w.group = divisor(p.heads / p.kv_heads);
     w.dim = static_cast<int>(p.dim);
     w.causal = p.causal;
@@ -719,7 +725,7 @@ void backward(prod::Call& c, const dlion_attention_bwd& p) {
     w.lse_ld = p.lse_ld;
     w.delta = delta;
     w.delta_ld = p.rows;
-    p.dim <= 64 ? launch<64>(c, w, plans, pieces, p.heads, p.kv_heads) : launch<128>(c, w, plans, pieces, p.heads, p.kv_heads);
+    p.dim <= 64 ? launch<64>(c, w, p, plans, pieces) : launch<128>(c, w, p, plans, pieces);
 }
 
 }  // namespace
