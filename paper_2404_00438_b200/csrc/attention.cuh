@@ -318,6 +318,15 @@ __device__ __forceinline__ void tmem_store16(uint32_t addr, const uint32_t (&r)[
         : "memory");
 }
 
+// One column, a value a thread.
+__device__ __forceinline__ void tmem_store1(uint32_t addr, float v) {
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x1.b32 [%0], {%1};" ::"r"(addr), "r"(__float_as_uint(v)) : "memory");
+}
+__device__ __forceinline__ float tmem_load1(uint32_t addr) {
+    uint32_t v;
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x1.b32 {%0}, [%1];\ntcgen05.wait::ld.sync.aligned;" : "=r"(v) : "r"(addr) : "memory");
+    return __uint_as_float(v);
+}
 __device__ __forceinline__ void tmem_stored() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
 __device__ __forceinline__ void tmem_store_f32(uint32_t addr, const float (&v)[32]) {
