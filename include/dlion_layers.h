@@ -168,8 +168,9 @@ dlion_status dlion_norm_backward(const dlion_norm_bwd* p, void* workspace, uint6
  *   p_ij = exp(s_ij - lse_i) ;  ds_ij = p_ij (dout_i . v_j - dout_i . out_i)
  *   dq_i = scale sum_j ds_ij k_j ;  dk_j = scale sum_i ds_ij q_i ;  dv_j = sum_i p_ij dout_i
  * for every head; heads / kv_heads query heads in a row share a head of keys and values, and dk, dv are their sums.
- * Operands are bf16; p and ds are rounded to bf16 as operands of the second products, out is the rounded output; scores, softmax
- * statistics and sums are binary32.  Rows of another sequence or of none do not take part whatever they hold, NaN too; a NaN
+ * Operands are bf16; p and ds are rounded to bf16 as operands of the second products; dout_i . out_i is taken from the rounded out,
+ * but for rows of a tile that sees at most 128 keys, where it is sum_j p_ij dout_i . v_j; scores, softmax statistics and sums are
+ * binary32.  Rows of another sequence or of none do not take part whatever they hold, NaN too; a NaN
  * or an infinity in a row of a sequence may reach every row of that sequence, a causal mask notwithstanding.
  *
  * The sequences: `offsets` (device memory, int32 or int64, sequences + 1 ascending values in [0, rows]; sequence i has the rows

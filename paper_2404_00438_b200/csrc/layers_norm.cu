@@ -3,7 +3,8 @@
 //   y = (x - mean) rstd w + b,  rstd = 1 / sqrt(var + eps)
 //   with h = (x - mean) rstd and u = w dy:  dx = rstd (u - mean(u) - h mean(u h)) + r,  dw = sum dy h,  db = sum dy
 //
-// Bound by memory: every value is read once and stays in registers, all arithmetic is binary32.
+// Bound by memory: every value is read once and stays in registers, all arithmetic is binary32.  dw and db of rows beyond 8192 columns are
+// the exception (a kernel of their own reads dy and x again), and y of rows beyond 32768.
 #include <climits>
 
 #include "layers_math.cuh"
@@ -230,7 +231,7 @@ __global__ void __launch_bounds__(G != 0 ? 128 : 1024) norm_kernel(const __grid_
     });
 }
 
-// Many rows of up to 2048 columns: as many blocks as there is room for, a warp for every so many-th row, its next row on its way while it
+// Many rows of up to 2048 columns (16384 x 2048 bf16: 27 us, 134 MB, 5.0 TB/s; with 64 threads a row and two barriers 42 us): as many blocks as there is room for, a warp for every so many-th row, its next row on its way while it
 // works on this one; weight and bias in shared memory, as binary32 and in the order in which the threads want them.
 template <class X, class Y, bool WIDE, int CHUNKS>
 __global__ void __launch_bounds__(kRowsThreads, 1) norm_rows_kernel(const __grid_constant__ Norm a) {
@@ -332,7 +333,10 @@ struct NormBack {
     int64_t r_ld;
     void* dx;
     int64_t dx_ld;
-    float* parts;                          // [blocks][2][n]: each block's share of dw and db; null if neither is wanted
+    float* parts;                          // [blocks][2][n]: each block's share of dw and db; null if neither is wanted, or
+    int joined;                            // the blocks, a cluster, that add their shares up themselves
+    void *dw, *db;                         // joined: where to
+    int grads_f32;
     int g;
 };
 
@@ -403,11 +407,13 @@ struct NormRow {
     }
 };
 
-// A block takes every gridDim.x-th set of rows and keeps its share of dw and db in registers; the rows' sums are added in the order of
-// the block's rows, the blocks' in the order of the blocks (norm_sums_kernel): the same result every time.
+// A block takes every gridDim.x-th set of rows and keeps its share of dw and db in registers; groups' and blocks' shares are added in
+// their order, by norm_sums_kernel or, where a cluster has all the rows, by its blocks: the same result every time.  Bound by memory and, with
+// one row a group under way, by the latency of a row's sums: 16384 x 2048 bf16 with a residual 56 us (268 MB, 4.8 TB/s); with
+// a row ahead in registers and three groups 89 us; 4097 x 1001 binary32, off the 16-byte grid, 18 us (49 MB).
 template <class X, class Y, bool WIDE, int CHUNKS, int G>
 __global__ void __launch_bounds__(kBackThreads, 1) norm_backward_kernel(const __grid_constant__ NormBack a) {
-    extern __shared__ uint4 memory[];      // rows on their way; at the end [2][n], the block's dw and db
+    extern __shared__ uint4 memory[];      // rows on their way; at the end the groups' dw and db
     __shared__ float2 sums[2][32];
     using Row = NormRow<X, Y, WIDE, CHUNKS>;
     tc::let_next_start();
@@ -459,38 +465,61 @@ __global__ void __launch_bounds__(kBackThreads, 1) norm_backward_kernel(const __
         }
     }
     if (WIDE) asm volatile("cp.async.wait_all;" ::: "memory");
-    if (a.parts == nullptr) return;
-    float* total = reinterpret_cast<float*>(memory);
+    if (a.parts == nullptr && a.joined == 0) return;
+    float* total = reinterpret_cast<float*>(memory);                 // [per][2][n], then the block's in the first of them
     __syncthreads();
-    for (int i = 0; i < per; ++i) {
-        if (group == i) {
+    float* mine = total + group * 2 * a.n;
 #pragma unroll
-            for (int c = 0; c < CHUNKS; ++c) {
-                if (WIDE) {
-                    if (!all.has(c, 0)) continue;
-                    float4 *pw = reinterpret_cast<float4*>(total + all.at(c, 0)), *pb = reinterpret_cast<float4*>(total + a.n + all.at(c, 0));
+    for (int c = 0; c < CHUNKS; ++c) {
+        if (WIDE) {
+            if (!all.has(c, 0)) continue;
+            float4 *pw = reinterpret_cast<float4*>(mine + all.at(c, 0)), *pb = reinterpret_cast<float4*>(mine + a.n + all.at(c, 0));
 #pragma unroll
-                    for (int h = 0; h < 2; ++h) {
-                        const float4 x = i == 0 ? make_float4(0, 0, 0, 0) : pw[h], y = i == 0 ? make_float4(0, 0, 0, 0) : pb[h];
-                        pw[h] = make_float4(x.x + dw[c][2 * h].x, x.y + dw[c][2 * h].y, x.z + dw[c][2 * h + 1].x, x.w + dw[c][2 * h + 1].y);
-                        pb[h] = make_float4(y.x + db[c][2 * h].x, y.y + db[c][2 * h].y, y.z + db[c][2 * h + 1].x, y.w + db[c][2 * h + 1].y);
-                    }
-                } else {
+            for (int h = 0; h < 2; ++h) {
+                pw[h] = make_float4(dw[c][2 * h].x, dw[c][2 * h].y, dw[c][2 * h + 1].x, dw[c][2 * h + 1].y);
+                pb[h] = make_float4(db[c][2 * h].x, db[c][2 * h].y, db[c][2 * h + 1].x, db[c][2 * h + 1].y);
+            }
+        } else {
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) {
-                        const int at = all.at(c, e);
-                        if (at >= a.n) continue;
-                        const float pw = e % 2 ? dw[c][e / 2].y : dw[c][e / 2].x, pb = e % 2 ? db[c][e / 2].y : db[c][e / 2].x;
-                        total[at] = i == 0 ? pw : total[at] + pw;
-                        total[a.n + at] = i == 0 ? pb : total[a.n + at] + pb;
-                    }
-                }
+            for (int e = 0; e < 8; ++e) {
+                if (!all.has(c, e)) continue;
+                mine[all.at(c, e)] = e % 2 ? dw[c][e / 2].y : dw[c][e / 2].x;
+                mine[a.n + all.at(c, e)] = e % 2 ? db[c][e / 2].y : db[c][e / 2].x;
             }
         }
-        __syncthreads();
     }
+    __syncthreads();
     float* to = a.parts + static_cast<int64_t>(blockIdx.x) * 2 * a.n;
-    for (int i = threadIdx.x; i < 2 * a.n; i += blockDim.x) to[i] = total[i];
+    for (int i = threadIdx.x; i < 2 * a.n; i += blockDim.x) {
+        float s = total[i];
+#pragma unroll 4
+        for (int r = 1; r < per; ++r) s += total[r * 2 * a.n + i];
+        if (a.joined != 0) {
+            total[i] = s;
+        } else {
+            to[i] = s;
+        }
+    }
+    if (a.joined != 0) {
+        tc::cluster_sync();
+        for (int i = static_cast<int>(blockIdx.x * blockDim.x + threadIdx.x); i < 2 * a.n; i += a.joined * static_cast<int>(blockDim.x)) {
+            const uint32_t at = tc::smem_addr(total + i);
+            float s = 0.0f;
+#pragma unroll
+            for (int r = 0; r < 8; ++r) {
+                if (r < a.joined) s += tc::load_cluster(tc::map_to_rank(at, r));
+            }
+            void* out = i < a.n ? a.dw : a.db;
+            const int col = i < a.n ? i : i - a.n;
+            if (out == nullptr) continue;
+            if (a.grads_f32) {
+                static_cast<float*>(out)[col] = s;
+            } else {
+                static_cast<bf16*>(out)[col] = __float2bfloat16_rn(s);
+            }
+        }
+        tc::cluster_sync();                // the shares stay until they are read
+    }
 }
 
 // Rows too wide for registers: a block a row for dx, which reads the row twice ...
@@ -690,8 +719,7 @@ dlion_status check(const dlion_norm_bwd* p) {
     return DLION_OK;
 }
 
-constexpr int kMostShared = 224 * 1024;
-constexpr int kBackColumns = 8 * 1024;     // a thread has two chunks of eight at most, and three (to 768 columns) where a warp has the row
+constexpr int kMostShared = 224 * 1024, kMostVectors = 16 * 768 * 8;
 
 void backward(Call& c, const dlion_norm_bwd& p) {
     const bool sums = p.dw != nullptr || p.db != nullptr;
@@ -703,17 +731,25 @@ void backward(Call& c, const dlion_norm_bwd& p) {
         return;
     }
     if (p.dx == nullptr && !sums) return;
-    NormBack a{p.m, static_cast<int>(p.n), p.dy, p.dy_ld, p.x, p.x_ld, p.w, p.w_type == DLION_GRAD_F32, p.stats, p.dx != nullptr ? p.residual : nullptr, p.r_ld, p.dx, p.dx_ld, nullptr, 0};
+    NormBack a{p.m, static_cast<int>(p.n), p.dy, p.dy_ld, p.x, p.x_ld, p.w, p.w_type == DLION_GRAD_F32, p.stats, p.dx != nullptr ? p.residual : nullptr, p.r_ld, p.dx, p.dx_ld, nullptr, 0, p.dw, p.db, p.grad_type == DLION_GRAD_F32, 0};
     const bool grid16 = p.n % 8 == 0 && wide(p.x, p.x_ld, p.x_type, p.m) && wide(p.dy, p.dy_ld, p.dy_type, p.m) && wide(p.w, 0, 0, 1) &&
                         wide(a.residual, p.r_ld, p.x_type, p.m) && wide(p.dx, p.dx_ld, p.x_type, p.m);
     a.g = p.n <= 768 ? 32 : group_of(p.n, 2, 512);
     const bool whole = a.g != 0;
-    // one block an SM, or smaller ones where the rows are so few that those have no more than one turn
+    // One block an SM, or smaller ones where the rows are so few that those have no more than one turn; or, where up to eight blocks
+    // have no more than two, a cluster, which needs no second kernel and no workspace.
     const int units = (p.x_type == DLION_GRAD_F32 ? 4 : 2) + (p.dy_type == DLION_GRAD_F32 ? 2 : 1);       // of 16 bytes a chunk
     const int small = std::max(a.g, 128), large = a.g == 32 && units * 3 > 13 ? 384 : kBackThreads;          // two rows ahead have to fit
-    const int threads = whole && parts(p.m, small / a.g) > 2 * c.sms ? large : small;
-    const int64_t blocks = whole ? std::min<int64_t>(parts(p.m, threads / a.g), threads == 128 ? 2 * c.sms : c.sms) : std::min<int64_t>(p.m, 64);
-    if (sums) a.parts = c.ws.take<float>(static_cast<uint64_t>(blocks) * 2 * p.n);
+    const int64_t turns = whole ? parts(p.m, large / a.g) : 0;
+    if (whole && sums && turns <= 16) {
+        for (a.joined = 1; a.joined < 8 && a.joined < turns; a.joined *= 2) {
+        }
+    }
+    const int threads = a.joined != 0 || (whole && parts(p.m, small / a.g) > 2 * c.sms) ? large : small;
+    const int64_t blocks = a.joined != 0 ? a.joined
+                           : whole       ? std::min<int64_t>(parts(p.m, threads / a.g), threads == 128 ? 2 * c.sms : c.sms)
+                                         : std::min<int64_t>(p.m, 64);
+    if (sums && a.joined == 0) a.parts = c.ws.take<float>(static_cast<uint64_t>(blocks) * 2 * p.n);
     if (!c.live()) return;
     with_types(p.x_type, p.dy_type, [&](auto x, auto y) {
         using X = decltype(x);
@@ -725,10 +761,10 @@ void backward(Call& c, const dlion_norm_bwd& p) {
             if (sums) start(c, norm_columns_kernel<X, Y>, dim3(static_cast<unsigned>(parts(p.n, 128)), static_cast<unsigned>(blocks)), dim3(128), 0, 1, a);
             return;
         }
-        const size_t vectors = sums ? static_cast<size_t>(p.n) * 8 : 0;
+        const size_t vectors = sums ? static_cast<size_t>(p.n) * 8 * (threads / a.g) : 0;
         auto go = [&](auto* kernel, size_t ring, int most) {
-            if (std::max(ring, vectors) > 47 * 1024) raise_shared(c, kernel, std::max(most, kBackColumns * 8));
-            start(c, kernel, dim3(static_cast<unsigned>(blocks)), dim3(threads), std::max(ring, vectors), 1, a);
+            if (std::max(ring, vectors) > 47 * 1024) raise_shared(c, kernel, std::max(most, kMostVectors));
+            start(c, kernel, dim3(static_cast<unsigned>(blocks)), dim3(threads), std::max(ring, vectors), std::max(a.joined, 1), a);
         };
         auto with = [&](auto chunk, auto threads_a_row) {
             constexpr int C = decltype(chunk)::value, G = decltype(threads_a_row)::value;
@@ -750,7 +786,7 @@ void backward(Call& c, const dlion_norm_bwd& p) {
             a.g == 128 ? with(integral_constant<int, 2>{}, integral_constant<int, 128>{}) : with(integral_constant<int, 2>{}, integral_constant<int, 0>{});
         }
     });
-    if (!sums) return;
+    if (!sums || a.joined != 0) return;
     const NormSums s{a.parts, static_cast<int>(p.n), static_cast<int>(blocks), p.grad_type == DLION_GRAD_F32, p.dw, p.db};
     start(c, norm_sums_kernel, dim3(static_cast<unsigned>(parts(p.n, 32)), 2), dim3(1024), 0, 1, s);
 }

@@ -208,13 +208,24 @@ def _grad_type(dtype) -> int:
     return _enumerator(_TYPES, dtype, "grad_dtype")
 
 
+# an empty tensor on each device: its new_empty(n) takes 1.4 us, torch.empty(n, dtype=, device=) 2.3
+_bytes = {}
+
+
+def _space(need: int, device: int) -> torch.Tensor:
+    none = _bytes.get(device)
+    if none is None:
+        none = _bytes[device] = _empty(0, dtype=torch.uint8, device=device)
+    return none.new_empty(need)
+
+
 def _call(calls, args, device: int, workspace: Optional[torch.Tensor]) -> None:
     size, call = calls
     ref = ctypes.byref(args)
     need = size(ref)
     if workspace is None:
         if need:
-            workspace = _empty(need, dtype=torch.uint8, device=device)
+            workspace = _space(need, device)
     else:
         _dlion.check_tensor(workspace, "workspace", (torch.uint8,), need, device)
     st = call(ref, workspace.data_ptr() if need else None, need, _stream(device))
@@ -423,10 +434,10 @@ def norm_forward(x: torch.Tensor, w: Optional[torch.Tensor] = None, b: Optional[
     if out is None:
         if out_dtype not in _TYPES:
             raise ValueError(f"out_dtype: {out_dtype}, expected one of {tuple(_TYPES)}")
-        out = x.new_empty((m, n), dtype=out_dtype)
+        out = x.new_empty(m, n, dtype=out_dtype)
     else:
         _matrix(out, "out", device, _TYPES, (m, n), True)
-    stats = x.new_empty((2, m), dtype=torch.float32)
+    stats = x.new_empty(2, m, dtype=torch.float32)
     args = _NormForward(m, n, x.data_ptr(), x.stride(0), _TYPES[x.dtype], _ptr(w), 0 if w is None else _TYPES[w.dtype], _ptr(b),
                         0 if b is None else _TYPES[b.dtype], eps, out.data_ptr(), out.stride(0), _TYPES[out.dtype], stats.data_ptr())
     st = _lib.dlion_norm_forward(ctypes.byref(args), _stream(device))
@@ -458,19 +469,19 @@ def norm_backward(dy: torch.Tensor, x: torch.Tensor, w: Optional[torch.Tensor], 
     if not need_dx:
         dx = None
     elif dx is None:
-        dx = x.new_empty((m, n))
+        dx = x.new_empty(m, n)
     else:
         _matrix(dx, "dx", device, stream, (m, n), True)
     if not need_dw:
         dw = None
     elif dw is None:
-        dw = x.new_empty((n,), dtype=grad_dtype)
+        dw = x.new_empty(n, dtype=grad_dtype)
     else:
         _vector(dw, "dw", device, (grad_dtype,), n)
     if not need_db:
         db = None
     elif db is None:
-        db = x.new_empty((n,), dtype=grad_dtype)
+        db = x.new_empty(n, dtype=grad_dtype)
     else:
         _vector(db, "db", device, (grad_dtype,), n)
     args = _NormBackward(m, n, dy.data_ptr(), dy.stride(0), _TYPES[dy.dtype], x.data_ptr(), x.stride(0), _TYPES[x.dtype], _ptr(w),
@@ -549,13 +560,13 @@ def attention_forward(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, *, caus
     sequences = _sequences(offsets, length, rows, device)
     clear = zero_rest
     if out is None:
-        out, given = q.new_empty((rows, heads, dim)), False
+        out, given = q.new_empty(rows, heads, dim), False
         fields = (out.data_ptr(), heads * dim, dim)
         clear = offsets is not None
     else:
         fields, given = _heads(out, "out", device, (rows, heads, dim)), True
     if lse is None:
-        lse = q.new_empty((heads, rows), dtype=torch.float32)
+        lse = q.new_empty(heads, rows, dtype=torch.float32)
         ld = rows
         if given and offsets is not None and not zero_rest:
             lse.zero_()                        # a result of each kind: the given one is left as it was
@@ -587,7 +598,7 @@ def attention_backward(dout: torch.Tensor, q: torch.Tensor, k: torch.Tensor, v: 
     results, fields, given = [], [], 0
     for t, name, shape in ((dq, "dq", own), (dk, "dk", shared), (dv, "dv", shared)):
         if t is None:
-            t = q.new_empty(shape)
+            t = q.new_empty(*shape)
             fields += (t.data_ptr(), shape[1] * dim, dim)
         else:
             fields += _heads(t, name, device, shape)

@@ -378,6 +378,71 @@ def test_same_bits_every_time_and_in_any_company(L):
     assert all(torch.equal(a, b[340:]) for a, b in zip(grads, runs[0][2:]))
 
 
+@pytest.mark.parametrize("rows,length,heads,dim,causal", [(64 * 197, 197, 6, 64, False), (4000, 250, 4, 128, True), (4096, 64, 8, 64, True)])
+def test_many_runs_are_alike_and_no_wait_runs_out(L, rows, length, heads, dim, causal):
+    q, k, v = qkv(1, rows, heads, heads, dim)
+    do = normal(3, rows, heads, dim)
+
+    def both():
+        f = L.attention_forward(q, k, v, causal=causal, length=length)
+        return (*f, *L.attention_backward(do, q, k, v, *f, causal=causal, length=length))
+
+    want = both()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = both()
+    for _ in range(1500):
+        graph.replay()
+    L.check()
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+def test_two_streams_at_once(L):
+    """Two calls that run at the same time, each with its own workspace, do not disturb each other."""
+    data = [(qkv(s, 2048, 8, 2, 64), normal(s + 9, 2048, 8, 64)) for s in (1, 2)]
+
+    def both(d):
+        (q, k, v), do = d
+        f = L.attention_forward(q, k, v)
+        return (*f, *L.attention_backward(do, q, k, v, *f))
+
+    want = [both(d) for d in data]
+    streams = [torch.cuda.Stream() for _ in data]
+    torch.cuda.synchronize()
+    got = [None, None]
+    for _ in range(20):
+        for i, st in enumerate(streams):
+            with torch.cuda.stream(st):
+                got[i] = both(data[i])
+    torch.cuda.synchronize()
+    for g, w in zip(got, want):
+        assert all(torch.equal(a, b) for a, b in zip(g, w))
+
+
+def test_rows_with_few_keys(L):
+    """A sequence's first row sees one key: its weight is 1, and neither q nor k has a gradient from it but for the
+    weight's error, 2^-19, times dp (2^6 here), the other operand (4) and the scale (1/8); rows that see few keys are as exact as
+    others."""
+    for dim in (64, 128):
+        lengths = [1, 2, 3, 17, 64, 65, 128, 129]
+        rows = sum(lengths)
+        offsets = torch.tensor([0] + lengths, device=DEV).cumsum(0)
+        q, k, v = qkv(dim, rows, 4, 2, dim)
+        do = normal(3, rows, 4, dim)
+        for causal in (True, False):
+            out, lse = L.attention_forward(q, k, v, causal=causal, offsets=offsets)
+            dq, dk, dv = L.attention_backward(do, q, k, v, out, lse, causal=causal, offsets=offsets)
+            firsts = offsets[:-1] if causal else offsets[:1]
+            assert torch.equal(out[firsts], v[firsts].repeat_interleave(2, 1)) and float(dq[firsts].abs().max()) <= 2.0 ** -14
+            assert float(dk[0].abs().max()) <= 2.0 ** -14
+            at = 0
+            for n in lengths:              # the whole gradients' errors: operands and results rounded, 2^-9 each on average: 0.0028 together
+                if n >= 17:
+                    w = one_head(q[at:at + n, 0].to(F64), k[at:at + n, 0].to(F64), v[at:at + n, 0].to(F64), do[at:at + n, 0].to(F64), causal, dim ** -0.5)
+                    assert float((dq[at:at + n, 0].to(F64) - w["dq"][0]).norm() / w["dq"][0].norm()) <= 0.0028
+                at += n
+
+
 def test_streams_graphs_and_workspaces(L):
     """On another stream; captured and replayed with new inputs and new offsets; a workspace of the caller's."""
     rows = 600

@@ -63,7 +63,7 @@ def test_norm_backward_refusals(layers, kw, status):
 
 
 def test_norm_workspace(layers):
-    a = layers._NormBackward(m=400, n=16, dy=P, dy_ld=16, dy_type=1, x=P, x_ld=16, x_type=1, stats=P, dx=P, dx_ld=16, dw=P, grad_type=0)
+    a = layers._NormBackward(m=4000, n=16, dy=P, dy_ld=16, dy_type=1, x=P, x_ld=16, x_type=1, stats=P, dx=P, dx_ld=16, dw=P, grad_type=0)
     need = layers._lib.dlion_norm_backward_workspace(ctypes.byref(a))
     assert need > 0
     assert layers._lib.dlion_norm_backward(ctypes.byref(a), P, need - 1, None) == 1
