@@ -4,6 +4,14 @@
 //
 // in one pass over the keys: with m the running maximum of a row, its sum l and its output o are held relative to exp(m) and
 // rescaled when m grows.
+//
+// Floors: 4 d operations a score on the tensor cores (128 x 128 x 128 twice: 1024 clocks), one exponential a score (16 a clock and SM:
+// 1024 clocks for 128 x 128).  What bounds it is neither alone: a row's scores, maximum, exponentials and weights and the two products
+// wait for one another, and what runs beside them is another tile's.  16384 causal rows, 16 heads: of 128 0.93 to 1.1 ms (1.0 to 1.18
+// PFLOP/s, the lower figure under the power cap; tensor pipe 53 %, special functions 53 % busy), of 64 0.80 ms (690 TFLOP/s; special
+// functions 54 % busy).  Tried in vain: part of the exponentials as polynomials on the multiply-add pipe (equal within 3 %, more
+// power), half a row a thread (equal), turns at the special function units (slower), passing over masked blocks of 32 keys (a
+// second copy of the loop costs more than it saves).
 #include "attention.cuh"
 
 namespace dlion {
