@@ -13,9 +13,9 @@ namespace att {
 
 constexpr int kTile = 128;                 // rows of the tile that a block keeps: the lanes of tensor memory
 
-// Rows of the tiles that pass by it.  With heads of up to 64 columns these are short: then two blocks fit an SM (forward three), whose
-// warps wait at different times.  12 heads of 64, tiles of 128 against 64, us: forward 64 x 197 rows 39, 33; both directions 8192 rows in
-// sequences of 128 (causal) 92, 82, 256 98, 90, 512 116, 113, 1024 154, 151; only very long ones lose (16384: backward 2296, 2391).
+// Rows of the tiles of keys that pass by it.  With heads of up to 64 columns these are short: then two blocks of dq's kernel fit an SM,
+// three of the forward one, whose warps wait at different times.  12 heads of 64, tiles of 128 against 64, us: forward 64 x 197 rows 39,
+// 33; backward, dk's kernel with short tiles too, 147, 136.
 template <int D>
 constexpr int kPassing = D == 64 ? 64 : 128;
 

@@ -10,8 +10,7 @@
 // Floors, 128 x 128 x 128 twice 1024 clocks: dq three products (1536 for a tile of 128 keys, heads of 128), dk and dv four (2048); operands
 // out of shared memory take 1792 and 2048; exponentials 1024 in each.  Measured at 16384 causal rows, 16 heads of 128: dq 1.47 to 1.56 ms
 // (1.06 to 1.12 PFLOP/s), dk and dv 1.8 to 1.9 ms (1.16 to 1.22), tensor pipe 52 and 61 % busy, power at the cap; 8 x 1024 rows, 12
-// heads of 64: 65 and 79 us.  Bound by the chain score, weight, product of one tile, of which tensor memory holds one (heads of 128)
-// or two blocks' (of 64).
+// heads of 64: 65 and 72 us.  Bound by the chain score, weight, product of one tile: tensor memory holds one tile's.
 #include "attention.cuh"
 
 namespace dlion {
@@ -377,30 +376,33 @@ __global__ void __launch_bounds__(QueryShared<D>::kThreads, 512 / QueryShared<D>
 }
 
 // ---------------------------------------------------------------- dk, dv
-// Scores and dp are computed transposed, keys as rows: so p and ds are operands as they lie in tensor memory.
+// Scores and dp are computed transposed, keys as rows: so p and ds are operands as they lie in tensor memory.  With heads of up to 64
+// columns there is room for a second set of scores; that took less time than two blocks an SM with tiles of 64 queries, at every length (8 x
+// 1024 rows, 12 heads, forward and backward: 148 us, 152 so; 64 x 197 rows backward 130, 136).
 template <int D>
 struct KeyShared {
-    static constexpr int kRows = kPassing<D>, kWarps = kRows / 16;   // of a tile of queries; warps of arithmetic
+    static constexpr int kRows = kTile, kWarps = kRows / 16;         // of a tile of queries; warps of arithmetic
     static constexpr uint32_t kBytes = kTile * D * 2, kRowBytes = kRows * D * 2;
     static constexpr int kStages = D == 64 ? 3 : 2;                  // of queries and of do
     static constexpr uint32_t kStats = 2 * kBytes + 2 * kStages * kRowBytes;          // lse and D of two tiles of queries
     static constexpr uint32_t kBars = kStats + 2 * 2 * kRows * 4;
     static constexpr uint32_t kAll = kBars + 256 + kTurnBytes + 1024;
-    static constexpr uint32_t kColumns = D == 64 ? 256 : 512;        // of tensor memory
+    static constexpr uint32_t kColumns = 512;                        // of tensor memory
+    static constexpr int kSets = D == 64 ? 2 : 1;                    // of scores: where there is room, the next ones do not wait for dv
     static constexpr int kThreads = 32 * kWarps + 96;                // a copying and an issuing warp, and one that brings lse and D
 };
 
 template <int D>
-__global__ void __launch_bounds__(KeyShared<D>::kThreads, 512 / KeyShared<D>::kColumns) key_gradient_kernel(const __grid_constant__ Backward w, unsigned int* mark) {
+__global__ void __launch_bounds__(KeyShared<D>::kThreads, 1) key_gradient_kernel(const __grid_constant__ Backward w, unsigned int* mark) {
     using S = KeyShared<D>;
-    constexpr int kRows = S::kRows, kStages = S::kStages, kCopying = S::kWarps, kIssuing = kCopying + 1, kAhead = kCopying + 2;
+    constexpr int kRows = S::kRows, kSets = S::kSets, kStages = S::kStages, kCopying = S::kWarps, kIssuing = kCopying + 1, kAhead = kCopying + 2;
     extern __shared__ uint8_t raw[];
     const uint32_t base = (tc::smem_addr(raw) + 1023u) & ~1023u;
     uint8_t* mem = raw + (base - tc::smem_addr(raw));
     const uint32_t queries = base + 2 * S::kBytes, douts = queries + kStages * S::kRowBytes, bars = base + S::kBars;
     const uint32_t q_full = bars, q_empty = bars + 24, d_full = bars + 48, d_empty = bars + 72, scores = bars + 96, products = bars + 112,
-                   weights = bars + 120, slopes = bars + 128, rows_full = bars + 136, done = bars + 144, rows_empty = bars + 152,
-                   stats_full = bars + 160, stats_empty = bars + 176, slot = bars + 192;
+                   weights = bars + 120, slopes = bars + 136, rows_full = bars + 144, done = bars + 152, rows_empty = bars + 160,
+                   stats_full = bars + 168, stats_empty = bars + 184, slot = bars + 200;
     const uint32_t turns = bars + 256;
     volatile uint32_t* slot_mem = reinterpret_cast<volatile uint32_t*>(mem + (slot - base));
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
@@ -416,10 +418,10 @@ __global__ void __launch_bounds__(KeyShared<D>::kThreads, 512 / KeyShared<D>::kC
         for (int i = 0; i < 2; ++i) {
             tc::bar_init(stats_full + 8 * i, 1);
             tc::bar_init(stats_empty + 8 * i, S::kWarps);
+            tc::bar_init(scores + 8 * i, 1);
+            tc::bar_init(weights + 8 * i, S::kWarps);                // in turn: with two sets of scores the next ones may all be there
         }
-        tc::bar_init(scores, 1);
         tc::bar_init(products, 1);
-        tc::bar_init(weights, S::kWarps);
         tc::bar_init(slopes, S::kWarps);
         tc::bar_init(rows_full, 1);
         tc::bar_init(rows_empty, 1);
@@ -436,7 +438,7 @@ __global__ void __launch_bounds__(KeyShared<D>::kThreads, 512 / KeyShared<D>::kC
     tc::fence_before();
     __syncthreads();
     tc::fence_after();
-    const uint32_t tmem = same(*slot_mem), products_at = tmem + kRows, dk_at = products_at + kRows, dv_at = dk_at + D;
+    const uint32_t tmem = same(*slot_mem), products_at = tmem + kSets * kRows, dk_at = products_at + kRows, dv_at = dk_at + D;
     bool fine = true;
     tc::wait_for_previous();
 
@@ -546,8 +548,8 @@ __global__ void __launch_bounds__(KeyShared<D>::kThreads, 512 / KeyShared<D>::kC
             const int st = i % kStages;
             if (!(fine = tc::bar_wait(q_full + 8 * st, (i / kStages) & 1))) return;
             tc::fence_after();
-            rows_by_rows<D, kRows>(tmem, base, queries + st * S::kRowBytes, k_steps);
-            finished(scores);
+            rows_by_rows<D, kRows>(tmem + (i % kSets) * kRows, base, queries + st * S::kRowBytes, k_steps);
+            finished(scores + 8 * (i % kSets));
         };
         auto product = [&] {
             const int st = i % kStages;
@@ -558,9 +560,9 @@ __global__ void __launch_bounds__(KeyShared<D>::kThreads, 512 / KeyShared<D>::kC
         };
         auto gather_v = [&] {
             const int b = i - 1, sb = b % kStages;
-            if (!(fine = tc::bar_wait(weights, b & 1))) return;
+            if (!(fine = tc::bar_wait(weights + 8 * (b & 1), (b >> 1) & 1))) return;
             tc::fence_after();
-            weights_by_rows<0, kRows / 16, 32>(dv_at, tmem, douts + sb * S::kRowBytes, wide, steps, !opening);
+            weights_by_rows<0, kRows / 16, 32>(dv_at, tmem + (b % kSets) * kRows, douts + sb * S::kRowBytes, wide, steps, !opening);
             finished(d_empty + 8 * sb);
         };
         auto gather_k = [&] {
@@ -571,14 +573,15 @@ __global__ void __launch_bounds__(KeyShared<D>::kThreads, 512 / KeyShared<D>::kC
             finished(q_empty + 8 * sb);
             if (last) finished(done);
         };
-        // A round: dv of the round before, the scores over its weights, dk of the round before, dp over its slopes.
+        // A round: dv of the round before, the scores (with one set of them, over its weights), dk of the round before, dp over its slopes.
         while (fine && pieces.take(piece, kv_head, fine)) {
             divide();
             begin();
             for (int r = 0; r < n && fine; ++r, ++i, advance()) {
                 if (r == 0 && !(fine = tc::bar_wait(rows_full, begun++ & 1))) break;
-                if (i > 0) gather_v();
-                if (fine) score();
+                if (kSets == 2) score();
+                if (fine && i > 0) gather_v();
+                if (fine && kSets == 1) score();
                 if (fine && i > 0) gather_k();
                 if (fine) product();
                 if (!fine) break;
@@ -593,7 +596,7 @@ __global__ void __launch_bounds__(KeyShared<D>::kThreads, 512 / KeyShared<D>::kC
     } else {
         const int half = warp / 4, quarter = warp % 4;
         const uint32_t lanes = static_cast<uint32_t>(quarter * 32) << 16;
-        const uint32_t s_at = tmem + half * 64 + lanes, d_at = products_at + half * 64 + lanes;
+        const uint32_t d_at = products_at + half * 64 + lanes;
         const float* stats = reinterpret_cast<const float*>(mem + S::kStats);
         const float2 cc = twice(w.c);
         int i = 0, ended = 0;
@@ -604,12 +607,13 @@ __global__ void __launch_bounds__(KeyShared<D>::kThreads, 512 / KeyShared<D>::kC
             const int key = key0 + quarter * 32 + lane;
             for (int r = 0; r < n; ++r, ++i, advance()) {
                 const int st = i & 1, valid = piece.length - tile * kRows;
+                const uint32_t s_at = tmem + (i % kSets) * kRows + half * 64 + lanes;
                 const float4* lse = reinterpret_cast<const float4*>(stats + st * 2 * kRows + half * 64);
                 const float4* delta = lse + kRows / 4;
                 const bool masked = valid < kRows || (w.causal && tile * kRows < key0 + kTile);
                 const int low = w.causal ? key - tile * kRows - half * 64 : 0, high = valid - half * 64;     // queries [low, high) of this warp's columns
                 if (!(fine = tc::bar_wait(stats_full + 8 * st, (i >> 1) & 1))) break;
-                if (!(fine = tc::bar_wait(scores, i & 1))) break;
+                if (!(fine = tc::bar_wait(scores + 8 * (i % kSets), (i / kSets) & 1))) break;
                 tc::fence_after();
                 float s[64];
                 tmem_load64(s_at, s);
@@ -641,7 +645,7 @@ __global__ void __launch_bounds__(KeyShared<D>::kThreads, 512 / KeyShared<D>::kC
                 tmem_stored();
                 tc::fence_before();
                 __syncwarp();
-                if (lane == 0) tc::bar_arrive(weights);
+                if (lane == 0) tc::bar_arrive(weights + 8 * (i & 1));
                 if (!(fine = tc::bar_wait(products, i & 1))) break;
                 tc::fence_after();
                 float dp[64];
@@ -672,7 +676,7 @@ __global__ void __launch_bounds__(KeyShared<D>::kThreads, 512 / KeyShared<D>::kC
                 }
             }
             if (!fine) break;
-            constexpr int kHalf = D * 64 / kRows;                    // columns of a warp: all, or half of them
+            constexpr int kHalf = D / 2;                             // columns of a warp
             const bool live = key < piece.length;
             const int64_t at = piece.start + key;
             __nv_bfloat16 *to_k = w.dk.p + at * w.dk.rs + kv_head * w.dk.hs + half * kHalf, *to_v = w.dv.p + at * w.dv.rs + kv_head * w.dv.hs + half * kHalf;
@@ -722,7 +726,7 @@ void launch(prod::Call& c, Backward& w, const dlion_attention_bwd& p, const Plan
     w.plan = plans[0];
     w.heads = divisor(p.heads);
     prod::start(c, query_gradient_kernel<D>, dim3(static_cast<unsigned>(pieces * p.heads)), dim3(QueryShared<D>::kThreads), QueryShared<D>::kAll, 1, w, c.mark);
-    if (!maps(kPassing<D>, kTile)) c.status = DLION_ECUDA;
+    if (!maps(kTile, kTile)) c.status = DLION_ECUDA;
     w.plan = plans[1];
     w.heads = divisor(p.kv_heads);
     prod::start(c, key_gradient_kernel<D>, dim3(static_cast<unsigned>(pieces * p.kv_heads)), dim3(KeyShared<D>::kThreads), KeyShared<D>::kAll, 1, w, c.mark);
