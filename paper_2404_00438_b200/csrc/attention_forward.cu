@@ -260,8 +260,9 @@ __global__ void __launch_bounds__(ForwardShared<D, SIDES>::kThreads, ForwardShar
                 }
                 const float top = max3(max3(top4[0], top4[1], top4[2]), top4[3], top4[3]);
                 // The reference follows the maximum only where weights would exceed 2^8: bf16 and binary32 hold them as exactly, and
-                // the output is seldom taken out and put back.  It is -infinity as long as all scores are; a score that is NaN or
-                // +infinity makes c times it, and so all of the row's weights, NaN.
+                // the output is seldom taken out and put back.  It is -infinity as long as all scores are.  A score of +infinity makes
+                // c times it, and so all of the row's weights, NaN; one that is NaN (the maximum passes it over) its own weight, and so
+                // the sum.
                 const bool grows = m > -INFINITY ? !((top - m) * c <= 8.0f) : !(top == -INFINITY);
                 if (__any_sync(0xffffffffu, grows)) {
                     const float to = grows ? top : m, to_c = to == -INFINITY ? 0.0f : (to - to) + to * c;
