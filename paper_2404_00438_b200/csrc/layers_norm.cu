@@ -18,7 +18,7 @@ using bf16 = __nv_bfloat16;
 
 constexpr int64_t kMost = int64_t{1} << 30;
 constexpr int kBlock = 256, kWarpColumns = 2048;
-constexpr int kRowsThreads = 512, kManyRows = 32;                   // rows an SM, from which on blocks stay
+constexpr int kRowsThreads = 512, kManyRows = 32, kManyWide = 2;     // rows an SM, and turns of wide rows, from which on blocks stay
 constexpr int kBackThreads = 512;          // 128 registers a thread: a row's values and sums for as many columns
 
 
@@ -231,17 +231,20 @@ __global__ void __launch_bounds__(G != 0 ? 128 : 1024) norm_kernel(const __grid_
     });
 }
 
-// Many rows of up to 2048 columns (16384 x 2048 bf16: 27 us, 134 MB, 5.0 TB/s; with 64 threads a row and two barriers 42 us): as many blocks as there is room for, a warp for every so many-th row, its next row on its way while it
-// works on this one; weight and bias in shared memory, as binary32 and in the order in which the threads want them.
-template <class X, class Y, bool WIDE, int CHUNKS>
+// Many rows of up to 16384 columns (16384 x 2048 bf16: 27 us, 134 MB, 5.0 TB/s; with 64 threads a row, two barriers and a block for
+// each set of rows 42 us; 4000 x 8192 31 against 38 us, 2817 x 4450, off the 16-byte grid, 28 against 41, 700 x 4450 10.2 against 13.3): one block an SM, G threads for every so many-th row, their next row on its way while they work on this one; weight
+// and bias in shared memory, as binary32 and in the order in which the threads want them.
+template <class X, class Y, bool WIDE, int CHUNKS, int G>
 __global__ void __launch_bounds__(kRowsThreads, 1) norm_rows_kernel(const __grid_constant__ Norm a) {
-    extern __shared__ float4 vectors[];    // [CHUNKS][4][32]: w, b of two columns
+    extern __shared__ float4 vectors[];    // [CHUNKS][4][G]: w, b of two columns
+    __shared__ float2 sums[2][32];
     tc::let_next_start();
     tc::wait_for_previous();
-    const int lane = threadIdx.x % 32, warp = threadIdx.x / 32, warps = kRowsThreads / 32;
-    const Columns<WIDE, 32> cols{a.n, lane, 32};
-    const int64_t step = static_cast<int64_t>(gridDim.x) * warps;
-    int64_t row = static_cast<int64_t>(blockIdx.x) * warps + warp;
+    constexpr int kGroups = kRowsThreads / G;
+    const int t = threadIdx.x % G, group = threadIdx.x / G;
+    const Columns<WIDE, G> cols{a.n, t, G};
+    const int64_t step = static_cast<int64_t>(gridDim.x) * kGroups;
+    int64_t row = static_cast<int64_t>(blockIdx.x) * kGroups + group;
     Eight<X> now[CHUNKS], next[CHUNKS];
     auto load = [&](int64_t r, Eight<X> (&to)[CHUNKS]) {
         if (r >= a.m) return;
@@ -249,20 +252,20 @@ __global__ void __launch_bounds__(kRowsThreads, 1) norm_rows_kernel(const __grid
         for (int c = 0; c < CHUNKS; ++c) cols.load(static_cast<const X*>(a.x) + r * a.x_ld, c, to[c]);
     };
     load(row, now);
-    for (int c = warp; c < CHUNKS; c += warps) {
+    for (int c = group; c < CHUNKS; c += kGroups) {
         float2 w[4], b[4];
         cols.vector(a.w, a.w_f32, c, 1.0f, w);
         cols.vector(a.b, a.b_f32, c, 0.0f, b);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) vectors[(c * 4 + e) * 32 + lane] = make_float4(w[e].x, w[e].y, b[e].x, b[e].y);
+        for (int e = 0; e < 4; ++e) vectors[(c * 4 + e) * G + t] = make_float4(w[e].x, w[e].y, b[e].x, b[e].y);
     }
     __syncthreads();
-    for (; row < a.m; row += step) {
+    for (; row < a.m; row += step) {       // (a group's threads leave together: its barriers are its own)
         load(row + step, next);
-        norm_row<X, Y, WIDE, CHUNKS, 32>(a, cols, 32, nullptr, 0, row, true, now, [&](int c, float2 (&w)[4], float2 (&b)[4]) {
+        norm_row<X, Y, WIDE, CHUNKS, G>(a, cols, G, sums, 0, row, true, now, [&](int c, float2 (&w)[4], float2 (&b)[4]) {
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                const float4 x = vectors[(c * 4 + e) * 32 + lane];
+                const float4 x = vectors[(c * 4 + e) * G + t];
                 w[e] = make_float2(x.x, x.y);
                 b[e] = make_float2(x.z, x.w);
             }
@@ -667,19 +670,23 @@ void forward(Call& c, const dlion_norm_fwd& p) {
     with_types(p.x_type, p.y_type, [&](auto x, auto y) {
         using X = decltype(x);
         using Y = decltype(y);
+        auto rows = [&](auto* kernel, int units) {                   // chunks times threads a row
+            const int shared = units * 4 * static_cast<int>(sizeof(float4));
+            if (shared > 47 * 1024) raise_shared(c, kernel, shared);
+            start(c, kernel, dim3(static_cast<unsigned>(c.sms)), dim3(kRowsThreads), shared, 1, a);
+        };
         if (p.n <= kWarpColumns) {         // a warp a row
             auto go = [&](auto* kernel) { start(c, kernel, dim3(static_cast<unsigned>(parts(p.m, 4))), dim3(128), 0, 1, a); };
             const int chunks = static_cast<int>(parts(p.n, 256));
             if (p.m >= kManyRows * c.sms) {
-                auto rows = [&](auto* kernel, int of) { start(c, kernel, dim3(static_cast<unsigned>(c.sms)), dim3(kRowsThreads), of * 4 * 32 * sizeof(float4), 1, a); };
-                if (!grid16) {
-                    chunks <= 2 ? rows(&norm_rows_kernel<X, Y, false, 2>, 2) : chunks <= 4 ? rows(&norm_rows_kernel<X, Y, false, 4>, 4) : rows(&norm_rows_kernel<X, Y, false, 8>, 8);
+                                if (!grid16) {
+                    chunks <= 2 ? rows(&norm_rows_kernel<X, Y, false, 2, 32>, 2 * 32) : chunks <= 4 ? rows(&norm_rows_kernel<X, Y, false, 4, 32>, 4 * 32) : rows(&norm_rows_kernel<X, Y, false, 8, 32>, 8 * 32);
                 } else if (chunks <= 2) {
-                    chunks == 1 ? rows(&norm_rows_kernel<X, Y, true, 1>, 1) : rows(&norm_rows_kernel<X, Y, true, 2>, 2);
+                    chunks == 1 ? rows(&norm_rows_kernel<X, Y, true, 1, 32>, 1 * 32) : rows(&norm_rows_kernel<X, Y, true, 2, 32>, 2 * 32);
                 } else if (chunks <= 4) {
-                    chunks == 3 ? rows(&norm_rows_kernel<X, Y, true, 3>, 3) : rows(&norm_rows_kernel<X, Y, true, 4>, 4);
+                    chunks == 3 ? rows(&norm_rows_kernel<X, Y, true, 3, 32>, 3 * 32) : rows(&norm_rows_kernel<X, Y, true, 4, 32>, 4 * 32);
                 } else {
-                    chunks <= 6 ? rows(&norm_rows_kernel<X, Y, true, 6>, 6) : rows(&norm_rows_kernel<X, Y, true, 8>, 8);
+                    chunks <= 6 ? rows(&norm_rows_kernel<X, Y, true, 6, 32>, 6 * 32) : rows(&norm_rows_kernel<X, Y, true, 8, 32>, 8 * 32);
                 }
                 return;
             }
@@ -697,6 +704,16 @@ void forward(Call& c, const dlion_norm_fwd& p) {
         a.g = group_of(p.n, 4, 1024);
         if (a.g == 0) {
             start(c, grid16 ? &norm_long_kernel<X, Y, true> : &norm_long_kernel<X, Y, false>, dim3(static_cast<unsigned>(p.m)), dim3(1024), 0, 1, a);
+            return;
+        }
+        if (a.g <= 512 && p.m >= kManyWide * c.sms * (kRowsThreads / a.g)) {
+            if (a.g == 128) {
+                grid16 ? rows(&norm_rows_kernel<X, Y, true, 4, 128>, 4 * 128) : rows(&norm_rows_kernel<X, Y, false, 4, 128>, 4 * 128);
+            } else if (a.g == 256) {
+                grid16 ? rows(&norm_rows_kernel<X, Y, true, 4, 256>, 4 * 256) : rows(&norm_rows_kernel<X, Y, false, 4, 256>, 4 * 256);
+            } else {
+                grid16 ? rows(&norm_rows_kernel<X, Y, true, 4, 512>, 4 * 512) : rows(&norm_rows_kernel<X, Y, false, 4, 512>, 4 * 512);
+            }
             return;
         }
         const int threads = std::max(a.g, kBlock);

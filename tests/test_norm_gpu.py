@@ -103,6 +103,16 @@ def test_rows(L, m, n):
     verify(x, w, None, 1e-6, y, stats, dy, None, L.norm_backward(dy, x, w, stats))
 
 
+@pytest.mark.parametrize("n,m", [(1001, 4801), (1536, 5003), (2047, 4750), (2056, 1300), (2303, 1250), (4096, 1201), (4450, 700), (5000, 1001), (8192, 603), (9001, 301), (16384, 300)])
+@pytest.mark.parametrize("stream", [BF, F32])
+def test_many_wide_rows(L, n, m, stream):
+    """Blocks that stay, with several threads to a row."""
+    x, w, b = normal(1, m, n, std=2.0, mean=0.5, dtype=stream), normal(2, n, std=0.3, mean=1.0), normal(3, n, dtype=F32)
+    y, stats = L.norm_forward(x, w, b)
+    dy = normal(4, m, n)
+    verify(x, w, b, 1e-5, y, stats, dy, x, L.norm_backward(dy, x, w, stats, residual=x, grad_dtype=F32))
+
+
 @pytest.mark.parametrize("n", [96, 99, 14000])
 def test_what_is_not_needed(L, n):
     m = 50
