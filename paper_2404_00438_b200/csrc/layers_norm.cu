@@ -525,7 +525,8 @@ __global__ void __launch_bounds__(kBackThreads, 1) norm_backward_kernel(const __
     }
 }
 
-// Rows too wide for registers: a block a row for dx, which reads the row twice ...
+// Rows too wide for registers: a block a row for dx, which reads the row twice (and stores what it has read the second time: dx may lie
+// over dy or r) ...
 template <class X, class Y, bool WIDE>
 __global__ void __launch_bounds__(1024) norm_backward_long_kernel(const __grid_constant__ NormBack a) {
     __shared__ float2 sums[2][32];
@@ -771,11 +772,11 @@ void backward(Call& c, const dlion_norm_bwd& p) {
     with_types(p.x_type, p.dy_type, [&](auto x, auto y) {
         using X = decltype(x);
         using Y = decltype(y);
-        if (!whole) {
+        if (!whole) {                      // the sums first: dx may lie over dy
+            if (sums) start(c, norm_columns_kernel<X, Y>, dim3(static_cast<unsigned>(parts(p.n, 128)), static_cast<unsigned>(blocks)), dim3(128), 0, 1, a);
             if (p.dx != nullptr) {
                 start(c, grid16 ? &norm_backward_long_kernel<X, Y, true> : &norm_backward_long_kernel<X, Y, false>, dim3(static_cast<unsigned>(p.m)), dim3(1024), 0, 1, a);
             }
-            if (sums) start(c, norm_columns_kernel<X, Y>, dim3(static_cast<unsigned>(parts(p.n, 128)), static_cast<unsigned>(blocks)), dim3(128), 0, 1, a);
             return;
         }
         const size_t vectors = sums ? static_cast<size_t>(p.n) * 8 * (threads / a.g) : 0;
