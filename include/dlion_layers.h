@@ -175,8 +175,8 @@ dlion_status dlion_norm_backward(const dlion_norm_bwd* p, void* workspace, uint6
  *
  * The sequences: `offsets` (device memory, int32 or int64, sequences + 1 ascending values in [0, rows]; sequence i has the rows
  * offsets[i] .. offsets[i + 1] - 1, which may be none), or, where that is null, rows / length sequences of `length` rows, or one
- * of all rows (length 0).  Offsets outside [0, rows] are held to it; where they do not ascend the results are undefined, but
- * nothing outside the tensors is touched.  Rows in no sequence (before the first, behind the last) are left as they were in
+ * of all rows (length 0).  Offsets outside [0, rows] are held to it; where they then do not ascend, no sequence is worked on and no row
+ * from the first offset to the last is written.  Rows in no sequence (before the first, behind the last) are left as they were in
  * every result, or cleared where zero_rest is set.
  *
  * All matrices are bf16 [rows][heads][dim], a pointer and the strides of rows and heads in elements; the dim columns of a head are

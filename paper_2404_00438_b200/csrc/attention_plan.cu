@@ -33,7 +33,9 @@ __device__ __forceinline__ int work_of(const PlanRequest& r, int length, int til
 
 // One block a table: pieces are counted by their work, the counts summed from the longest on, and the pieces put in their
 // places; which of two equal pieces comes first is left to chance and changes no result.  Offsets are held to the rows there
-// are, and places to the table's size, so that offsets that do not ascend give wrong results but no access out of range.
+// are; if they ascend, the pieces are no more than the table's entries.  Offsets that do not ascend are found while counting (some
+// length is negative; a warp that has met more pieces than there can be stops, so that their number bounds the time), and
+// then there are no pieces: the counts, which may have passed 32 bits, are not used.
 // A few us where there are some hundred sequences; the launch is most of it.
 __global__ void __launch_bounds__(1024) plan_kernel(const __grid_constant__ PlanArgs a) {
     __shared__ int place[kBuckets];
@@ -66,16 +68,20 @@ __global__ void __launch_bounds__(1024) plan_kernel(const __grid_constant__ Plan
     const int most = a.most[blockIdx.x];
     place[threadIdx.x] = 0;
     __syncthreads();
-    // twice over the sequences, a warp for each: counting, then placing
+    // twice over the sequences, a warp for each: counting, then placing; false where the offsets are seen not to ascend
     auto pieces = [&](auto f) {
+        int met = 0;                       // by this warp: most + 2^23 at most, below 2^31
         for (int s = warp; s < a.count; s += 32) {
             const int start = offset_at(a, s), length = offset_at(a, s + 1) - start;
             const int tiles = length <= 0 ? 0 : (length + request.tile - 1) / request.tile;
+            met += tiles;
+            if (length < 0 || met > most) return false;
             for (int t = lane; t < tiles; t += 32) f(start, length, t, kBuckets - 1 - min(work_of(request, length, t), kBuckets - 1));
         }
+        return true;
     };
-    pieces([&](int, int, int, int bucket) { atomicAdd(&place[bucket], 1); });
-    __syncthreads();
+    const bool counted = pieces([&](int, int, int, int bucket) { atomicAdd(&place[bucket], 1); });
+    const bool ascend = __syncthreads_and(counted) != 0;
     const int mine = place[threadIdx.x];
     int upto = mine;
 #pragma unroll
@@ -96,12 +102,14 @@ __global__ void __launch_bounds__(1024) plan_kernel(const __grid_constant__ Plan
     }
     __syncthreads();
     place[threadIdx.x] = upto - mine + (warp > 0 ? sums[warp - 1] : 0);
-    const int total = sums[31];
+    const int total = ascend ? sums[31] : 0;
     __syncthreads();
-    pieces([&](int start, int length, int tile, int bucket) {
-        const int at = atomicAdd(&place[bucket], 1);
-        if (at < most) table[at] = make_int4(start, length, tile, 0);
-    });
+    if (ascend) {
+        pieces([&](int start, int length, int tile, int bucket) {
+            const int at = atomicAdd(&place[bucket], 1);
+            if (at < most) table[at] = make_int4(start, length, tile, 0);
+        });
+    }
     for (int i = total + threadIdx.x; i < most; i += 1024) table[i] = make_int4(0, -1, 0, 0);
 }
 
