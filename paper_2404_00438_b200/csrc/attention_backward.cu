@@ -90,7 +90,6 @@ __global__ void __launch_bounds__(QueryShared<D>::kThreads, 512 / QueryShared<D>
     volatile uint32_t* slot_mem = reinterpret_cast<volatile uint32_t*>(mem + (slot - base));
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
 
-    tc::let_next_start();
     if (threadIdx.x == 0) {
         tc::bar_init(stats_full, 2);
         tc::bar_init(meet, S::kWarps);
@@ -123,6 +122,7 @@ __global__ void __launch_bounds__(QueryShared<D>::kThreads, 512 / QueryShared<D>
     if (warp == kIssuing) tc::tmem_alloc<1>(slot, S::kColumns);
     tc::fence_before();
     __syncthreads();
+    tc::let_next_start();                  // now that this block has its tensor memory
     tc::fence_after();
     const uint32_t tmem = same(*slot_mem), products_at = tmem + 2 * kRows, dq_at = products_at + kRows;
     bool fine = true;
@@ -407,7 +407,6 @@ __global__ void __launch_bounds__(KeyShared<D>::kThreads, 1) key_gradient_kernel
     volatile uint32_t* slot_mem = reinterpret_cast<volatile uint32_t*>(mem + (slot - base));
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
 
-    tc::let_next_start();
     if (threadIdx.x == 0) {
         for (int i = 0; i < kStages; ++i) {
             tc::bar_init(q_full + 8 * i, 1);
@@ -437,6 +436,7 @@ __global__ void __launch_bounds__(KeyShared<D>::kThreads, 1) key_gradient_kernel
     if (warp == kIssuing) tc::tmem_alloc<1>(slot, S::kColumns);
     tc::fence_before();
     __syncthreads();
+    tc::let_next_start();                  // now that this block has its tensor memory
     tc::fence_after();
     const uint32_t tmem = same(*slot_mem), products_at = tmem + kSets * kRows, dk_at = products_at + kRows, dv_at = dk_at + D;
     bool fine = true;

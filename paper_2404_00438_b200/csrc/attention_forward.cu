@@ -63,7 +63,6 @@ __global__ void __launch_bounds__(ForwardShared<D, SIDES>::kThreads, ForwardShar
     volatile uint32_t* slot_mem = reinterpret_cast<volatile uint32_t*>(mem + (slot - base));
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
 
-    tc::let_next_start();
     if (threadIdx.x == 0) {
         for (int i = 0; i < kRing; ++i) {
             tc::bar_init(full + 8 * i, 1);
@@ -87,6 +86,7 @@ __global__ void __launch_bounds__(ForwardShared<D, SIDES>::kThreads, ForwardShar
     if (warp == kIssuing) tc::tmem_alloc<1>(slot, S::kColumns);
     tc::fence_before();
     __syncthreads();
+    tc::let_next_start();                  // now that this block has its tensor memory
     tc::fence_after();
     const uint32_t tmem = same(*slot_mem);
     bool fine = true;
