@@ -190,7 +190,7 @@ typedef struct {
     int64_t sequences;                     /* with offsets; 0 otherwise */
     int64_t length;                        /* without offsets; 0 otherwise */
     int32_t causal;
-    float scale;                           /* positive, finite */
+    float scale;                           /* positive, at most 2e38 (log2(e) times it is finite) */
     void* out; int64_t out_rs, out_hs;
     float* lse; int64_t lse_ld;            /* [heads][rows], rows adjacent */
     int32_t zero_rest;

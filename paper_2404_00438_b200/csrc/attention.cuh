@@ -402,6 +402,8 @@ __device__ __forceinline__ void give_row(uint32_t addr, float factor, __nv_bfloa
 // ---------------------------------------------------------------- host side (attention_plan.cu)
 constexpr int64_t kMostRows = int64_t{1} << 30;
 
+inline bool scale_ok(float scale) { return scale > 0.0f && scale <= 2e38f; }          // log2(e) times it is finite
+
 struct Operand {                           // bf16 [rows][heads][dim] as an argument
     const void* p;
     int64_t rs, hs, heads;

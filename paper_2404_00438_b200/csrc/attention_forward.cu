@@ -338,7 +338,7 @@ __global__ void __launch_bounds__(ForwardShared<D, SIDES>::kThreads, ForwardShar
 
 dlion_status check(const dlion_attention_fwd* p) {
     if (p == nullptr || p->heads < 1 || p->kv_heads < 1 || p->heads > 65535 || p->heads % p->kv_heads != 0) return DLION_EINVAL;
-    if (p->dim < 8 || p->dim > 128 || p->dim % 8 != 0 || p->causal < 0 || p->causal > 1 || !(p->scale > 0.0f) || !(p->scale < INFINITY)) return DLION_EINVAL;
+    if (p->dim < 8 || p->dim > 128 || p->dim % 8 != 0 || p->causal < 0 || p->causal > 1 || !scale_ok(p->scale)) return DLION_EINVAL;
     const dlion_status seq = check_sequences(Sequences{p->rows, p->length, p->sequences, p->offsets, p->offsets_64});
     if (seq != DLION_OK) return seq;
     if (p->zero_rest < 0 || p->zero_rest > 1 || p->lse_ld < p->rows) return DLION_EINVAL;

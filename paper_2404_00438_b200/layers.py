@@ -540,8 +540,8 @@ def _sequences(offsets, length, rows: int, device: int):
 def _scale(scale, dim: int) -> float:
     if scale is None:
         return dim ** -0.5
-    if not 0.0 < scale < 3.4e38:
-        raise ValueError(f"scale: {scale!r}, expected a positive number")
+    if not 0.0 < scale <= 2e38:
+        raise ValueError(f"scale: {scale!r}, expected a positive number of at most 2e38")
     return scale
 
 
