@@ -307,17 +307,6 @@ __device__ __forceinline__ void tmem_store32(uint32_t addr, const uint32_t (&r)[
         : "memory");
 }
 
-__device__ __forceinline__ void tmem_store16(uint32_t addr, const uint32_t (&r)[16]) {
-    asm volatile(
-        "tcgen05.st.sync.aligned.32x32b.x16.b32 [%16], {"
-        "%0, %1, %2, %3, %4, %5, %6, %7, "
-        "%8, %9, %10, %11, %12, %13, %14, %15"
-        "};" ::"r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]),
-          "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]),
-          "r"(addr)
-        : "memory");
-}
-
 // One column, a value a thread.
 __device__ __forceinline__ void tmem_store1(uint32_t addr, float v) {
     asm volatile("tcgen05.st.sync.aligned.32x32b.x1.b32 [%0], {%1};" ::"r"(addr), "r"(__float_as_uint(v)) : "memory");
@@ -421,7 +410,7 @@ struct Sequences {
 dlion_status check_sequences(const Sequences& s);
 
 // Pieces of `tile` rows that the sequences have at most, and the plan for them; with offsets, tables are filled by one launch
-// for all plans (fill_plans), which also clears what belongs to no sequence.
+// for all plans (make_plans), which also clears what belongs to no sequence.
 struct PlanRequest {
     int tile, causal, keys;                // keys: pieces are tiles of keys, of which the first have most queries
 };
