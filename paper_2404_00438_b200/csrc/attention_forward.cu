@@ -5,13 +5,19 @@
 // in one pass over the keys: with m the running maximum of a row, its sum l and its output o are held relative to exp(m) and
 // rescaled when m grows.
 //
+// The weights are rounded to bf16 as operands of the second product: the matrix instruction takes both of one type, and v is bf16.  l is
+// their sum before that.  A weight is off by 2^-8 of itself at most, the output by about as much again as by its own rounding (0.0018 to
+// 0.0023 of its norm against 64 bits, where the rounding of the result alone is 0.0017).
+//
 // Floors: 4 d operations a score on the tensor cores (128 x 128 x 128 twice: 1024 clocks), one exponential a score (16 a clock and SM:
 // 1024 clocks for 128 x 128).  What bounds it is neither alone: a row's scores, maximum, exponentials and weights and the two products
 // wait for one another, and what runs beside them is another tile's.  16384 causal rows, 16 heads: of 128 0.93 to 1.1 ms (1.0 to 1.18
 // PFLOP/s, the lower figure under the power cap; tensor pipe 53 %, special functions 53 % busy), of 64 0.80 ms (690 TFLOP/s; special
-// functions 54 % busy).  Tried in vain: part of the exponentials as polynomials on the multiply-add pipe (equal within 3 %, more
-// power), half a row a thread (equal), turns at the special function units (slower), passing over masked blocks of 32 keys (a
-// second copy of the loop costs more than it saves).
+// functions 54 % busy).  All warps of a block have the same number of registers, and those of the arithmetic have too few: with heads
+// of 64 (96 registers, three blocks an SM) they spill 290 bytes a thread, with wider ones (168) 120 to 160.  Tried in vain, with these
+// spills: part of the exponentials as polynomials on the multiply-add pipe (equal within 3 %, more power), half a row a thread (equal),
+// turns at the special function units (slower), passing over masked blocks of 32 keys (a second copy of the loop costs more than it
+// saves).
 #include "attention.cuh"
 
 namespace dlion {
@@ -45,7 +51,7 @@ struct ForwardShared {
     static constexpr uint32_t kAll = kBars + 256 + kTurnBytes + 1024;
     static constexpr int kThreads = 128 * SIDES + 64;
     static constexpr uint32_t kColumns = SIDES * (kKeys + D);        // of tensor memory: scores, over them weights, and outputs
-    static constexpr int kBlocks = kColumns == 128 ? 3 : 512 / kColumns;              // an SM: of four, warps would have 80 registers
+    static constexpr int kBlocks = kColumns == 128 ? 3 : 512 / kColumns;              // an SM: three spill at 96 registers; of four, warps would have 80
     static constexpr int kHalves = kKeys / 64;                       // of the weights, announced one by one
 };
 

@@ -3,8 +3,9 @@
 //   y = (x - mean) rstd w + b,  rstd = 1 / sqrt(var + eps)
 //   with h = (x - mean) rstd and u = w dy:  dx = rstd (u - mean(u) - h mean(u h)) + r,  dw = sum dy h,  db = sum dy
 //
-// Bound by memory: every value is read once and stays in registers, all arithmetic is binary32.  dw and db of rows beyond 8192 columns are
-// the exception (a kernel of their own reads dy and x again), and y of rows beyond 32768.
+// Bound by memory: every value is read once and stays in registers, all arithmetic is binary32.  The exceptions are rows too wide for
+// registers: y beyond 32768 columns reads x three times, and beyond 8192 dx reads x, dy and w twice, and dw and db, in a kernel of their
+// own, x and dy once more.
 #include <climits>
 
 #include "layers_math.cuh"
@@ -20,7 +21,6 @@ constexpr int64_t kMost = int64_t{1} << 30;
 constexpr int kBlock = 256, kWarpColumns = 2048;
 constexpr int kRowsThreads = 512, kManyRows = 32, kManyWide = 2;     // rows an SM, and turns of wide rows, from which on blocks stay
 constexpr int kBackThreads = 512;          // 128 registers a thread: a row's values and sums for as many columns
-
 
 bool type_ok(int t) { return t == DLION_GRAD_F32 || t == DLION_GRAD_BF16; }
 int type_bytes(int t) { return t == DLION_GRAD_F32 ? 4 : 2; }
@@ -231,9 +231,11 @@ __global__ void __launch_bounds__(G != 0 ? 128 : 1024) norm_kernel(const __grid_
     });
 }
 
-// Many rows of up to 16384 columns (16384 x 2048 bf16: 27 us, 134 MB, 5.0 TB/s; with 64 threads a row, two barriers and a block for
-// each set of rows 42 us; 4000 x 8192 31 against 38 us, 2817 x 4450, off the 16-byte grid, 28 against 41, 700 x 4450 10.2 against 13.3): one block an SM, G threads for every so many-th row, their next row on its way while they work on this one; weight
-// and bias in shared memory, as binary32 and in the order in which the threads want them.
+// Many rows of up to 16384 columns: one block an SM, G threads for every so many-th row, their next row on its way while they work on
+// this one; weight and bias in shared memory, as binary32 and in the order in which the threads want them.  16384 x 2048 bf16: 27 us
+// (134 MB, 5.0 TB/s; with 64 threads a row, two barriers and a block for each set of rows 42 us).  Against a block for each set of rows,
+// us: 4000 x 8192 31, 38; off the 16-byte grid 2817 x 4450 28, 41, 700 x 4450 10.2, 13.3.  Binary32 rows of 1025 to 2048 columns
+// spill 60 to 280 bytes a thread.
 template <class X, class Y, bool WIDE, int CHUNKS, int G>
 __global__ void __launch_bounds__(kRowsThreads, 1) norm_rows_kernel(const __grid_constant__ Norm a) {
     extern __shared__ float4 vectors[];    // [CHUNKS][4][G]: w, b of two columns
@@ -413,7 +415,8 @@ struct NormRow {
 // A block takes every gridDim.x-th set of rows and keeps its share of dw and db in registers; groups' and blocks' shares are added in
 // their order, by norm_sums_kernel or, where a cluster has all the rows, by its blocks: the same result every time.  Bound by memory and, with
 // one row a group under way, by the latency of a row's sums: 16384 x 2048 bf16 with a residual 56 us (268 MB, 4.8 TB/s); with
-// a row ahead in registers and three groups 89 us; 4097 x 1001 binary32, off the 16-byte grid, 18 us (49 MB).
+// a row ahead in registers and three groups 89 us; 4097 x 1001 binary32, off the 16-byte grid, 18 us (49 MB).  128 registers do not
+// suffice for three chunks a thread (513 to 768 columns: 230 to 580 bytes spilled), nor off the grid for two of 256 or 512 threads.
 template <class X, class Y, bool WIDE, int CHUNKS, int G>
 __global__ void __launch_bounds__(kBackThreads, 1) norm_backward_kernel(const __grid_constant__ NormBack a) {
     extern __shared__ uint4 memory[];      // rows on their way; at the end the groups' dw and db
@@ -680,7 +683,7 @@ void forward(Call& c, const dlion_norm_fwd& p) {
             auto go = [&](auto* kernel) { start(c, kernel, dim3(static_cast<unsigned>(parts(p.m, 4))), dim3(128), 0, 1, a); };
             const int chunks = static_cast<int>(parts(p.n, 256));
             if (p.m >= kManyRows * c.sms) {
-                                if (!grid16) {
+                if (!grid16) {
                     chunks <= 2 ? rows(&norm_rows_kernel<X, Y, false, 2, 32>, 2 * 32) : chunks <= 4 ? rows(&norm_rows_kernel<X, Y, false, 4, 32>, 4 * 32) : rows(&norm_rows_kernel<X, Y, false, 8, 32>, 8 * 32);
                 } else if (chunks <= 2) {
                     chunks == 1 ? rows(&norm_rows_kernel<X, Y, true, 1, 32>, 1 * 32) : rows(&norm_rows_kernel<X, Y, true, 2, 32>, 2 * 32);
